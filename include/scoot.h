@@ -20,6 +20,13 @@
  *   scoot_sobol_configs  Sobol configurations (initial design, shortfall fill)
  *   scoot_rf_train       CART training of the feasibility forest (Algorithm 1)
  *
+ * and, for evaluating a configuration, the attention part of an engine's step
+ * over a paged key-value cache:
+ *
+ *   scoot_kv_tables      block tables, positions and cache slots from request lengths
+ *   scoot_kv_append      the new tokens' keys and values into their slots
+ *   scoot_paged_attention  the new tokens against their requests' keys and values
+ *
  * plus host-side preparation of per-round state (Cholesky factor of the
  * observations' covariance, box decomposition of the non-dominated region,
  * forest packing), all three in one call by scoot_round_state_build.
@@ -793,6 +800,97 @@ scoot_status scoot_select_pareto(scoot_ctx* ctx, const float* acq, int64_t lda, 
  * (there is no context, so no message). */
 scoot_status scoot_select_topq_static(const float* acq, const uint8_t* mask, int64_t n, int32_t q,
                                       int64_t* idx, float* val, int32_t* count, void* stream);
+
+/* ------------------------------------------------------------------ a serving step's attention */
+
+/* The engine parameters of the search space (Section 2, Table 1: most
+ * sequences and most batched tokens of a step, block size, chunked prefill)
+ * act on the attention part of an engine's step over a paged key-value
+ * cache.  These three calls are that part, for evaluating a configuration on
+ * the GPU (the paper's EVALUATE runs a whole engine; it states no kernels).
+ * All lengths and tables are read on the device: a step needs no host
+ * synchronisation, and can be captured in a graph and replayed. */
+
+#define SCOOT_F16  0
+#define SCOOT_BF16 1
+#define SCOOT_MAX_GROUP 128   /* query heads per key-value head */
+
+/* A paged cache: n_blocks blocks of block_size tokens; element (block, token,
+ * head, dim) of keys and of values is at block * ld_block + token * ld_token +
+ * head * ld_head + dim.  Strides count elements, are multiples of 8 and at
+ * least head_dim (either order of tokens and heads); keys and values are two
+ * arrays of this layout, 16-byte aligned.  The slot of a token is block *
+ * block_size + its place in the block. */
+typedef struct {
+    int32_t dtype;         /* SCOOT_F16 or SCOOT_BF16 */
+    int32_t head_dim;      /* 64 or 128 */
+    int32_t n_kv_heads;
+    int32_t block_size;    /* a power of two, 8 to 256 */
+    int64_t n_blocks;      /* < 2^31 */
+    int64_t ld_block, ld_token, ld_head;
+} scoot_kv_layout;
+
+/* Block tables and slot maps of one step.  Request r has cached_len[r] tokens
+ * in the cache, whose ceil(cached / block_size) blocks are the first entries
+ * of its row of block_table ([n_req][ld_table]), and brings new_len[r] tokens.
+ * In the requests' order each takes the blocks it lacks from the front of
+ * free_blocks (n_free ids) and appends them to its row.  A request whose
+ * blocks the free ones do not cover is refused: it takes none, its tokens get
+ * slot -1 and its kv_len is 0 (scoot_paged_attention then gives it zeros); a
+ * later one that needs no block is still served.
+ * Outputs: query_start[n_req + 1], the running sum of new_len; kv_len[n_req] =
+ * cached + new; for token t of the batch (requests back to back) slot[t] and
+ * position[t] (its place in its sequence, from 0); counts[2] = blocks taken,
+ * requests refused.  Tokens from query_start[n_req] up to n_tokens, the
+ * arrays' length, get slot -1 and position 0.
+ * A negative length, a sequence longer than its row (ld_table * block_size),
+ * more new tokens than n_tokens, or a block id outside 0 .. n_blocks - 1 is
+ * flagged (scoot_ctx_check: SCOOT_EDEVICE); such a request is refused, tokens
+ * past n_tokens are not written, and a token in such a block gets slot -1. */
+scoot_status scoot_kv_tables(scoot_ctx* ctx, const int32_t* cached_len, const int32_t* new_len, int32_t n_req,
+                             int32_t block_size, int64_t n_blocks, int32_t* block_table, int64_t ld_table,
+                             const int32_t* free_blocks, int64_t n_free, int32_t* query_start, int32_t* kv_len,
+                             int64_t* slot, int32_t* position, int64_t n_tokens, int32_t* counts, void* stream);
+
+/* Keys and values of n_tokens tokens into a cache: element (t, head, dim) of k
+ * is at t * k_ld_token + head * k_ld_head + dim (of v likewise; the cache's
+ * type; strides as in scoot_kv_layout) and goes to slot[t] of k_cache.  A
+ * token with a negative slot is skipped; one at or past n_blocks * block_size
+ * is skipped and flagged (scoot_ctx_check: SCOOT_EDEVICE).  Slots are
+ * distinct. */
+scoot_status scoot_kv_append(scoot_ctx* ctx, const scoot_kv_layout* layout, const void* k, int64_t k_ld_token,
+                             int64_t k_ld_head, const void* v, int64_t v_ld_token, int64_t v_ld_head,
+                             const int64_t* slot, int64_t n_tokens, void* k_cache, void* v_cache, void* stream);
+
+/* Attention of a batch of new tokens over the paged cache.  Tokens
+ * query_start[r] .. query_start[r + 1] - 1 of q are the last ones of request
+ * r's sequence of kv_len[r] tokens, all of them in the cache: token j of its n
+ * new ones has position p = kv_len[r] - n + j.  It sees the keys i < kv_len[r]
+ * with i <= p if causal, and i > p - window if window > 0.  With G = n_heads /
+ * n_kv_heads, query head h reads key-value head h / G:
+ *   out[t][h] = sum_i softmax_i(scale q[t][h] . k_i) v_i,
+ *   lse[t][h] = ln sum_i exp(scale q[t][h] . k_i).
+ * A token that sees no key (kv_len 0, or p < 0) gets zeros and -inf.  What is
+ * in the cache past kv_len, and values that a token does not see, never reach
+ * its output, be they infinite or NaN.  Rows of q past query_start[n_req] have
+ * no output.
+ * q and out: element (t, head, dim) at t * ld_token + head * ld_head + dim,
+ * the cache's type and rules of alignment and stride; lse float32
+ * [n_tokens][n_heads] or NULL; scale > 0, finite.  Scores, softmax statistics
+ * and sums are held in fp32; probabilities are rounded to the cache's type for
+ * the product with the values, as the tensor cores take them.
+ * A query_start that decreases or passes n_tokens, a kv_len outside 0 ..
+ * ld_table * block_size, or a block id outside 0 .. n_blocks - 1 is flagged
+ * (scoot_ctx_check: SCOOT_EDEVICE): a request with bad lengths has no output,
+ * a bad block counts as zeros.
+ * SCOOT_EUNSUPPORTED for other head sizes, block sizes or types, and for more
+ * than SCOOT_MAX_GROUP query heads per key-value head. */
+scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_layout* layout, const void* q, int64_t q_ld_token,
+                                   int64_t q_ld_head, int32_t n_heads, int64_t n_tokens, const int32_t* query_start,
+                                   const int32_t* kv_len, int32_t n_req, const int32_t* block_table, int64_t ld_table,
+                                   const void* k_cache, const void* v_cache, float scale, int32_t causal,
+                                   int32_t window, void* out, int64_t out_ld_token, int64_t out_ld_head, float* lse,
+                                   void* stream);
 
 /* ------------------------------------------------------------------ measurement probes */
 

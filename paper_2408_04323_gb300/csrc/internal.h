@@ -137,6 +137,10 @@ scoot_status scoot_marks_begin(scoot_ctx* ctx, void* st);
 scoot_status scoot_mark(scoot_ctx* ctx, void* st, int32_t kind);
 
 // Checks shared by the device entry points.
+scoot_status scoot_check_kv(scoot_ctx* ctx, const scoot_kv_layout* L, const void* k_cache, const void* v_cache);
+// A (token, head, dim) array of the cache's type: alignment and strides.
+scoot_status scoot_check_heads(scoot_ctx* ctx, const char* name, const void* p, int64_t ld_token, int64_t ld_head,
+                               int64_t n_tokens, int32_t n_heads, int32_t head_dim);
 scoot_status scoot_check_pool(scoot_ctx* ctx, const uint32_t* cand, int64_t n, int64_t ld, int32_t d);
 
 #ifdef __CUDACC__

@@ -78,6 +78,11 @@ class scoot_round_state(C.Structure):
                 ("cond", C.c_double * 4), ("gp", scoot_gp_layout), ("forest", scoot_forest_layout)]
 
 
+class scoot_kv_layout(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("head_dim", C.c_int32), ("n_kv_heads", C.c_int32), ("block_size", C.c_int32),
+                ("n_blocks", C.c_int64), ("ld_block", C.c_int64), ("ld_token", C.c_int64), ("ld_head", C.c_int64)]
+
+
 # scoot_node as a numpy record (host copies of trained trees)
 NODE_DTYPE = np.dtype([("val", "<f4"), ("left", "<u2"), ("feat", "u1"), ("flags", "u1")])
 
@@ -151,6 +156,10 @@ _PROTOS = {
     "scoot_fantasy_end": [_vp, _vp, _vp],
     "scoot_suggest_fantasy": [_vp, C.POINTER(scoot_gp_layout), _vp, _vp, _i32, _vp, _i64, _i64, _vp, _vp, _i32,
                               _i32, _vp, _i64, _vp, _vp, _vp, _vp, _vp],
+    "scoot_kv_tables": [_vp, _vp, _vp, _i32, _i32, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _vp],
+    "scoot_kv_append": [_vp, C.POINTER(scoot_kv_layout), _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _vp, _vp, _vp],
+    "scoot_paged_attention": [_vp, C.POINTER(scoot_kv_layout), _vp, _i64, _i64, _i32, _i64, _vp, _vp, _i32, _vp, _i64,
+                              _vp, _vp, _f32, _i32, _i32, _vp, _i64, _i64, _vp, _vp],
 }
 _STRING_FUNCS = {"scoot_last_error", "scoot_status_string"}
 EXPORTS = tuple(_PROTOS)
@@ -803,3 +812,104 @@ def scoot_fantasy_end(ctx, var_out=None, stream=None):
     import torch
     _check(lib().scoot_fantasy_end(_h(ctx), _dev(var_out, torch.float32, "var_out"), _stream(stream)),
            "scoot_fantasy_end", _h(ctx))
+
+
+# ------------------------------------------------------------------ a serving step's attention
+
+F16, BF16 = 0, 1
+MAX_GROUP = 128
+
+
+def _heads(t, dtype, name):
+    """(pointer, token stride, head stride) of a CUDA tensor [tokens][heads][dim] whose dim is contiguous.  The stride
+    of an axis of one (torch may give it any) counts as the axis's size."""
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA torch tensor (device memory)")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens][heads][dim], got {tuple(t.shape)}")
+    n, h, d = t.shape
+    st, sh, sd = t.stride()
+    if sd != 1:
+        raise ValueError(f"{name} must be contiguous along its last axis")
+    return t.data_ptr(), (st if n > 1 else h * d), (sh if h > 1 else d)
+
+
+def kv_layout(k_cache, v_cache) -> scoot_kv_layout:
+    """The layout of a cache given as CUDA tensors [blocks][tokens][heads][dim] (a transposed view of
+    [blocks][heads][tokens][dim] will do)."""
+    import torch
+    if not (k_cache.is_cuda and v_cache.is_cuda):
+        raise TypeError("k_cache and v_cache must be CUDA torch tensors (device memory)")
+    if k_cache.dtype != v_cache.dtype or k_cache.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"k_cache and v_cache must both be float16 or bfloat16, got {k_cache.dtype} and {v_cache.dtype}")
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape:
+        raise ValueError(f"k_cache and v_cache must be [blocks][tokens][heads][dim] of one shape, got "
+                         f"{tuple(k_cache.shape)} and {tuple(v_cache.shape)}")
+    nb, bs, h, d = k_cache.shape
+    sb, st, sh, sd = k_cache.stride()
+    if k_cache.stride() != v_cache.stride():
+        raise ValueError("k_cache and v_cache must have the same strides")
+    if sd != 1:
+        raise ValueError("k_cache and v_cache must be contiguous along their last axis")
+    return scoot_kv_layout(BF16 if k_cache.dtype == torch.bfloat16 else F16, d, h, bs, nb, sb if nb > 1 else bs * h * d,
+                           st, sh if h > 1 else d)
+
+
+def scoot_kv_tables(ctx, cached_len, new_len, block_table, block_size, n_blocks, free_blocks, query_start, kv_len,
+                    slot, position, counts, stream=None) -> None:
+    """Device int32: cached_len, new_len, kv_len [R]; block_table [R][width] (rows updated in place); free_blocks;
+    query_start [R + 1]; position [T]; counts [2].  slot: device int64 [T]."""
+    import torch
+    i32 = torch.int32
+    R = cached_len.numel()
+    if block_table.dim() != 2 or block_table.shape[0] != R or new_len.numel() != R or kv_len.numel() != R or \
+            query_start.numel() != R + 1 or counts.numel() != 2 or position.numel() != slot.numel():
+        raise ValueError("array lengths do not match: [R] cached_len, new_len, kv_len; [R][width] block_table; "
+                         "[R + 1] query_start; [T] slot, position; [2] counts")
+    _check(lib().scoot_kv_tables(_h(ctx), _dev(cached_len, i32, "cached_len"), _dev(new_len, i32, "new_len"), R,
+                                 int(block_size), int(n_blocks), _dev(block_table, i32, "block_table"),
+                                 block_table.shape[1], _dev(free_blocks, i32, "free_blocks"), free_blocks.numel(),
+                                 _dev(query_start, i32, "query_start"), _dev(kv_len, i32, "kv_len"),
+                                 _dev(slot, torch.int64, "slot"), _dev(position, i32, "position"), slot.numel(),
+                                 _dev(counts, i32, "counts"), _stream(stream)), "scoot_kv_tables", _h(ctx))
+
+
+def scoot_kv_append(ctx, k, v, slot, k_cache, v_cache, stream=None) -> None:
+    """k, v: device [T][heads][dim] of the cache's type (last axis contiguous); slot: device int64 [T]."""
+    import torch
+    L = kv_layout(k_cache, v_cache)
+    if k.shape != v.shape or k.shape[0] != slot.numel() or tuple(k.shape[1:]) != tuple(k_cache.shape[2:]):
+        raise ValueError(f"k and v must be [T][heads][dim] as slot and the cache have them, got {tuple(k.shape)} and "
+                         f"{tuple(v.shape)}")
+    kp, kt, kh = _heads(k, k_cache.dtype, "k")
+    vp, vt, vh = _heads(v, k_cache.dtype, "v")
+    _check(lib().scoot_kv_append(_h(ctx), C.byref(L), kp, kt, kh, vp, vt, vh, _dev(slot, torch.int64, "slot"),
+                                 slot.numel(), k_cache.data_ptr(), v_cache.data_ptr(), _stream(stream)),
+           "scoot_kv_append", _h(ctx))
+
+
+def scoot_paged_attention(ctx, q, k_cache, v_cache, block_table, query_start, kv_len, out, scale, causal=True, window=0,
+                          lse=None, stream=None) -> None:
+    """q, out: device [T][heads][dim] of the cache's type (last axis contiguous); block_table int32 [R][width],
+    query_start int32 [R + 1], kv_len int32 [R]; lse: device float32 [T][heads] or None."""
+    import torch
+    L = kv_layout(k_cache, v_cache)
+    R = kv_len.numel()
+    if q.shape != out.shape or q.dim() != 3 or q.shape[2] != L.head_dim:
+        raise ValueError(f"q and out must be [T][heads][{L.head_dim}] of one shape, got {tuple(q.shape)} and "
+                         f"{tuple(out.shape)}")
+    if block_table.dim() != 2 or block_table.shape[0] != R or query_start.numel() != R + 1 or \
+            (lse is not None and lse.shape != q.shape[:2]):
+        raise ValueError("array lengths do not match: [R] kv_len; [R][width] block_table; [R + 1] query_start; "
+                         "[T][heads] lse")
+    qp, qt, qh = _heads(q, k_cache.dtype, "q")
+    op, ot, oh = _heads(out, k_cache.dtype, "out")
+    i32 = torch.int32
+    _check(lib().scoot_paged_attention(_h(ctx), C.byref(L), qp, qt, qh, q.shape[1], q.shape[0],
+                                       _dev(query_start, i32, "query_start"), _dev(kv_len, i32, "kv_len"), R,
+                                       _dev(block_table, i32, "block_table"), block_table.shape[1],
+                                       k_cache.data_ptr(), v_cache.data_ptr(), scale, int(bool(causal)), int(window),
+                                       op, ot, oh, _dev(lse, torch.float32, "lse"), _stream(stream)),
+           "scoot_paged_attention", _h(ctx))
