@@ -123,6 +123,9 @@ scoot_status scoot_check_pool(scoot_ctx* ctx, const uint32_t* cand, int64_t n, i
     return SCOOT_OK;
 }
 
+// The error word (on a cache line pair of its own) and the counters.
+static const size_t kWordBytes = (64 + SCOOT_COUNTS) * sizeof(uint32_t);
+
 extern "C" {
 
 scoot_status scoot_ctx_create(int32_t device, scoot_ctx** out) {
@@ -136,16 +139,17 @@ scoot_status scoot_ctx_create(int32_t device, scoot_ctx** out) {
     scoot_ctx* ctx = new (std::nothrow) scoot_ctx();
     if (!ctx) return SCOOT_ENOMEM;
     ctx->device = device;
-    if (cudaSetDevice(device) != cudaSuccess || cudaMalloc(&ctx->d_err, sizeof(uint32_t)) != cudaSuccess) {
+    if (cudaSetDevice(device) != cudaSuccess || cudaMalloc(&ctx->d_err, kWordBytes) != cudaSuccess) {
         cudaGetLastError();
         delete ctx;
         return SCOOT_ECUDA;
     }
-    if (cudaMemset(ctx->d_err, 0, sizeof(uint32_t)) != cudaSuccess) {
+    if (cudaMemset(ctx->d_err, 0, kWordBytes) != cudaSuccess) {
         cudaFree(ctx->d_err);
         delete ctx;
         return SCOOT_ECUDA;
     }
+    ctx->d_count = ctx->d_err + 64;
     *out = ctx;
     return SCOOT_OK;
 }
@@ -174,6 +178,7 @@ scoot_status scoot_ctx_check(scoot_ctx* ctx, void* stream) {
     SCOOT_CUDA(ctx, cudaMemcpyAsync(&word, ctx->d_err, sizeof(word), cudaMemcpyDeviceToHost, st));
     SCOOT_CUDA(ctx, cudaStreamSynchronize(st));
     if (word) SCOOT_CUDA(ctx, cudaMemsetAsync(ctx->d_err, 0, sizeof(uint32_t), st));
+    if (word & SCOOT_DEVERR_TIMEOUT) SCOOT_CUDA(ctx, cudaMemsetAsync(ctx->d_count, 0, SCOOT_COUNTS * sizeof(uint32_t), st));
     if (word & SCOOT_DEVERR_TIMEOUT) return scoot_fail(ctx, SCOOT_ETIMEOUT, "a bounded device wait gave up");
     if (word & SCOOT_DEVERR_INDEX) return scoot_fail(ctx, SCOOT_EDEVICE, "a kernel met an index out of range");
     if (word & SCOOT_DEVERR_VALUE)

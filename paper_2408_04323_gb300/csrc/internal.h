@@ -20,6 +20,8 @@
 #define SCOOT_DEVERR_CAPACITY 4u  // a Pareto filter had more survivors than it can hold
 #define SCOOT_DEVERR_VALUE   8u   // a non-finite feature or a label other than 0/1
 
+#define SCOOT_COUNTS 1024u
+
 struct scoot_ctx {
     int32_t device = 0;
     std::string err;
@@ -28,7 +30,8 @@ struct scoot_ctx {
     bool ws_in_graph = false;    // a call being captured has used it
     std::vector<void*> ws_kept;  // earlier ones that graphs may use, freed with the context
     size_t ws_kept_bytes = 0;
-    uint32_t* d_err = nullptr;   // device error word
+    uint32_t* d_err = nullptr;   // device error word, followed by the counters
+    uint32_t* d_count = nullptr; // SCOOT_COUNTS arrival counters, zero between calls (paged_attn.cu)
     // Phase timing (scoot_ctx_set_timing): events recorded between the
     // launches of the last timed call, and the kind of each launch.
     int32_t timing = 0;

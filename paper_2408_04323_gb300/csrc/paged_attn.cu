@@ -1,110 +1,908 @@
-// Attention of a batch of new tokens over a paged key-value cache.
+// Attention of a batch of new tokens over a paged key-value cache, on the fifth-generation tensor cores.
+//
+//   out_t = sum_i softmax_i(scale q_t . k_i) v_i,   lse_t = ln sum_i exp(scale q_t . k_i)
+//
+// over the keys i that token t sees.  The keys go by in tiles of 128: S = Q K^T [128 x 128] by tcgen05.mma into tensor
+// memory, then per row the running maximum m and sum l of the softmax (in log2 units: p = 2^(c s - m), c = scale log2 e),
+// P rounded to the cache's type back into tensor memory over S, and O += P V.  O is rescaled only when a row's maximum
+// has grown by more than 2^8 since it was last: until then p stays below 2^8, which the 16-bit types and the fp32 sums
+// hold, and l and O carry the same factor, so that O / l is unchanged.
+//
+// Rows.  A query head's tokens and the G heads that share a key-value head are all rows of one product (row = token * G +
+// head), so keys and values are read once for the group.  A CTA has two slots of 128 rows, each with its own S, O and four
+// softmax warps:
+//   * more than 128 rows (a chunk of a prompt): a pair, both slots against the same tile, so that one's softmax runs
+//     under the other's products;
+//   * up to 128 rows: one slot, the slots taking successive items in turn.  With at most 64 or 32 rows (single tokens) the
+//     rows are loaded two or four times over, and the copy in lanes 32 w .. serves the w-th part of the tile's keys as
+//     rows of its own, with its own m, l and O: the exponentials, which one warp would have taken for the whole tile,
+//     are spread over the four.  The copies are joined at the end like the parts of a split item.
+//
+// Work.  An item is a (key-value head, request, up to 256 rows), its units the tiles of keys that its rows see.  All
+// units in a row, head by head and request by request, with kItemCost extra per item, are cut into equal ranges, one per
+// SM: long sequences are split, short ones follow one another, whatever the batch.  Each CTA takes the sums over
+// the requests for itself (lengths are on the device), so the call is one launch.  An item that lies in several ranges
+// leaves its parts (O, m, l) in the workspace, and the CTA that comes last (a counter per item) joins them in the
+// ranges' order, so that the result does not depend on who was last.
+//
+// Warps 0-3 and 4-7: softmax of slots 0 and 1.  Warp 8: the products (one thread).  Warp 9: the items, and the copies:
+// pages of keys and values by TMA into a ring of tiles (128-byte swizzle), a box of up to 128 tokens x 64 dimensions
+// per page and half head; queries likewise.
+//
+// Values of keys that some row may not see: a probability of 0 times an infinity or NaN is NaN, so the value tiles at
+// the ends of the sequence and along the diagonal are looked through first: rows past the ends are set to zero, and a
+// value that is not finite is replaced by zero and the item marked; rows that do see it add it at the end.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <cfloat>
+
 #include "internal.h"
+#include "mbarrier.cuh"
 
 namespace {
 
+using namespace scoot_dev;
+
+constexpr int kRows = 128;       // rows of a slot: the MMA's M and the TMEM lanes
+constexpr int kKeys = 128;       // keys of a tile
+constexpr int kThreads = 320;
+constexpr int kMmaWarp = 8, kLoadWarp = 9;
+constexpr int kRing = 4;         // items handed from the load warp to the others
+constexpr int kItemCost = 1;     // an item's start and end, in units
+constexpr int kBufs = 6;         // part buffers of a CTA (see part_buf)
+constexpr int kHalf = kKeys * 128;  // bytes of a tile's half: 128 keys x 64 dimensions
+constexpr uint32_t kS0 = 0, kO0 = 256;  // tensor memory columns: S0, S1, O0, O1
+constexpr int kMaxCtas = (int)(SCOOT_COUNTS / 2);
+constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
+
+template <int D>
+struct Shape {
+    static constexpr int kTile = kKeys * D * 2;           // bytes of a tile of keys, values or queries
+    static constexpr int kStages = (D == 128 ? 5 : 10);   // tiles of keys or values in flight
+    static constexpr int kSmem = 2 * kTile + kStages * kTile + 1024;
+};
+
 struct AttnArgs {
-    scoot_kv_layout L;
-    int32_t bs_log, n_heads, group, n_req, causal, window;
-    const void* q;
-    int64_t q_ld_token, q_ld_head, n_tokens;
+    CUtensorMap kmap, vmap, qmap[3];  // qmap[i]: tokens of 128 >> i rows
+    int32_t bs_log, n_heads, n_kv_heads, group, n_req, causal, window, bf16;
+    int32_t toks;         // tokens of a slot: 128 / group
+    int64_t n_tokens, n_blocks;
     const int32_t* query_start;
     const int32_t* kv_len;
     const int32_t* table;
     int64_t ld_table;
-    const void* k;
-    const void* v;
-    float scale;
-    void* out;
+    const uint16_t* v;    // for the marked items
+    int64_t ld_block, ld_token, ld_head;
+    float scale_log2;
+    uint16_t* out;
     int64_t out_ld_token, out_ld_head;
     float* lse;
+    float* parts;         // kBufs part buffers per CTA
+    uint32_t* count;      // arrivals per split item and slot, zero between calls
     uint32_t* err;
 };
 
-__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ void from_float(float x, __half& y) { y = __float2half_rn(x); }
-__device__ __forceinline__ void from_float(float x, __nv_bfloat16& y) { y = __float2bfloat16_rn(x); }
+// What the load warp tells the others about an item, or a part of it.
+struct Item {
+    int32_t h, r, tok, ntok;   // key-value head, request, first row of q, tokens
+    int32_t pos, kv;           // position of the first token, length of the sequence
+    int32_t begin, end;        // keys that some row of the item sees
+    int32_t u0, nu;            // this part's tiles: u0 .. u0 + nu - 1
+    int32_t slot;              // 0 or 1; 2: a pair
+    int32_t rep_log;           // copies of the rows: 1 << rep_log
+    int32_t first, n_parts;    // CTA of the first part, and how many parts
+    int32_t poison;            // a value that is not finite was replaced
+    int32_t stop;
+};
 
-// One warp per (token, query head): the keys that it sees one after another,
-// with the running maximum and sum of the softmax; a lane holds D / 32
-// consecutive dimensions.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) attn_row_kernel(const AttnArgs a) {
-    constexpr int kE = D / 32;
-    const int lane = threadIdx.x & 31;
-    const int64_t rows = a.n_tokens * a.n_heads;
-    if (blockIdx.x == 0)
-        for (int r = threadIdx.x; r < a.n_req; r += blockDim.x)
-            if (a.query_start[r] > a.query_start[r + 1]) atomicOr(a.err, SCOOT_DEVERR_INDEX);
-    for (int64_t w = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; w < rows;
-         w += ((int64_t)gridDim.x * blockDim.x) >> 5) {
-        const int64_t t = w / a.n_heads;
-        const int h = (int)(w - t * a.n_heads);
-        // the request: the last one that starts at or before t
-        int lo = 0, hi = a.n_req - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (a.query_start[mid] <= t) lo = mid;
-            else hi = mid - 1;
-        }
-        const int64_t q0 = a.query_start[lo], q1 = a.query_start[lo + 1], kv = a.kv_len[lo];
-        if (q0 < 0 || q1 > a.n_tokens || kv < 0 || kv > a.ld_table << a.bs_log) {
-            if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_INDEX);
-            continue;
-        }
-        if (t < q0 || t >= q1) continue;
-        const int64_t pos = kv - (q1 - q0) + (t - q0);
-        const int64_t end = a.causal ? min(kv, pos + 1) : kv;
-        const int64_t begin = a.window > 0 ? max((int64_t)0, pos + 1 - a.window) : 0;
-        float qf[kE], o[kE], m = -INFINITY, l = 0.0f;
-        const T* qp = static_cast<const T*>(a.q) + t * a.q_ld_token + h * a.q_ld_head + lane * kE;
-#pragma unroll
-        for (int e = 0; e < kE; ++e) {
-            qf[e] = to_float(qp[e]);
-            o[e] = 0.0f;
-        }
-        const int64_t head_at = (int64_t)(h / a.group) * a.L.ld_head + lane * kE;
-        for (int64_t i = begin; i < end; ++i) {
-            const int32_t id = a.table[lo * a.ld_table + (i >> a.bs_log)];
-            if (id < 0 || id >= a.L.n_blocks) {
-                if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_INDEX);
-                continue;
-            }
-            const int64_t at = id * a.L.ld_block + (i & ((1 << a.bs_log) - 1)) * a.L.ld_token + head_at;
-            const T* kp = static_cast<const T*>(a.k) + at;
-            const T* vp = static_cast<const T*>(a.v) + at;
-            float s = 0.0f;
-#pragma unroll
-            for (int e = 0; e < kE; ++e) s = fmaf(qf[e], to_float(kp[e]), s);
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-            s *= a.scale;
-            const float mn = fmaxf(m, s), ms = mn == -INFINITY ? 0.0f : mn;
-            const float f = expf(m - ms), p = expf(s - ms);
-            l = fmaf(l, f, p);
-#pragma unroll
-            for (int e = 0; e < kE; ++e) o[e] = fmaf(o[e], f, p * to_float(vp[e]));
-            m = mn;
-        }
-        T* op = static_cast<T*>(a.out) + t * a.out_ld_token + h * a.out_ld_head + lane * kE;
-#pragma unroll
-        for (int e = 0; e < kE; ++e) from_float(end > begin ? o[e] / l : 0.0f, op[e]);
-        if (a.lse && lane == 0) a.lse[t * a.n_heads + h] = end > begin ? m + logf(l) : -INFINITY;
-    }
+enum {
+    kSFull = 0, kPFull = 2, kPvDone = 4, kQFull = 6, kQEmpty = 8, kWg = 10, kItemFull = 12, kItemEmpty = 16, kDrain = 20,
+    kKvFull = 21, kKvEmpty = 31, kBars = 41
+};
+
+// The swizzled K-major tile of queries or keys: rows of 128 bytes, 8-row groups 1024 bytes apart.
+__device__ __forceinline__ uint64_t desc_k(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+// The value tile, whose product runs over keys (rows): 64-dimension halves kHalf bytes apart, 8-key groups 1024.
+__device__ __forceinline__ uint64_t desc_v(uint32_t addr) {
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(kHalf >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+// kind::f16, fp32 accumulator, M = 128; b_mn: B runs along its N in memory.
+__device__ __forceinline__ uint32_t idesc(bool bf16, uint32_t n, bool b_mn) {
+    return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (b_mn ? 1u << 16 : 0u) | ((n >> 3) << 17) | (8u << 24);
 }
 
-template <typename T>
-scoot_status launch_rows(scoot_ctx* ctx, const AttnArgs& a, cudaStream_t st) {
-    int sms = 0;
-    SCOOT_CUDA(ctx, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, ctx->device));
-    int64_t blocks = (a.n_tokens * a.n_heads + 7) / 8;
-    if (blocks > sms * 64) blocks = sms * 64;
-    if (a.L.head_dim == 64) attn_row_kernel<T, 64><<<(unsigned)blocks, 256, 0, st>>>(a);
-    else attn_row_kernel<T, 128><<<(unsigned)blocks, 256, 0, st>>>(a);
+// 32 consecutive columns of the calling warp's 32 lanes of tensor memory, to and from registers (lane i of the warp
+// holds its lane's row); a load is complete after tmem_wait_ld.
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* x) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]), "=r"(x[8]), "=r"(x[9]), "=r"(x[10]), "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15]), "=r"(x[16]), "=r"(x[17]), "=r"(x[18]), "=r"(x[19]), "=r"(x[20]), "=r"(x[21]), "=r"(x[22]), "=r"(x[23]), "=r"(x[24]), "=r"(x[25]), "=r"(x[26]), "=r"(x[27]), "=r"(x[28]), "=r"(x[29]), "=r"(x[30]), "=r"(x[31])
+        : "r"(addr));
+}
+
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* x) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
+        "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]), "r"(x[16]), "r"(x[17]), "r"(x[18]), "r"(x[19]), "r"(x[20]), "r"(x[21]), "r"(x[22]), "r"(x[23]), "r"(x[24]), "r"(x[25]), "r"(x[26]), "r"(x[27]), "r"(x[28]), "r"(x[29]), "r"(x[30]), "r"(x[31]));
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* x) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
+        "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]));
+}
+
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2_hw(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.0f : m; }
+
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+    if (kBf16) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+// A pair's halves that are infinite or NaN: their bits set.
+template <bool kBf16>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    const uint32_t e = kBf16 ? 0x7F80u : 0x7C00u;
+    uint32_t m = 0;
+    if ((w & e) == e) m |= 0xFFFFu;
+    if ((w & (e << 16)) == e << 16) m |= 0xFFFF0000u;
+    return m;
+}
+template <bool kBf16>
+__device__ __forceinline__ float value16(uint16_t x) {
+    return kBf16 ? __bfloat162float(__ushort_as_bfloat16(x)) : __half2float(__ushort_as_half(x));
+}
+
+// One request's lengths, empty if they are bad.
+struct Req {
+    int32_t q0, n, kv;
+};
+__device__ __forceinline__ Req load_req(const AttnArgs& a, int r, bool flag) {
+    Req q{0, 0, 0};
+    if (r >= a.n_req) return q;
+    const int q0 = a.query_start[r], q1 = a.query_start[r + 1], kv = a.kv_len[r];
+    if (q0 < 0 || q1 < q0 || q1 > a.n_tokens || kv < 0 || kv > a.ld_table << a.bs_log) {
+        if (flag) atomicOr(a.err, SCOOT_DEVERR_INDEX);
+        return q;
+    }
+    q.q0 = q0;
+    q.n = q1 - q0;
+    q.kv = kv;
+    return q;
+}
+
+// The keys [begin, end) that tokens tok0 .. tok0 + nt - 1 of n new ones see, all together.
+__device__ __forceinline__ void seen_keys(const AttnArgs& a, int kv, int n, int tok0, int nt, int& begin, int& end) {
+    const int64_t p0 = (int64_t)kv - n + tok0;
+    end = a.causal ? (int)min((int64_t)kv, p0 + nt) : kv;
+    begin = a.window > 0 ? (int)max((int64_t)0, p0 + 1 - a.window) : 0;
+    if (end <= begin) begin = end = 0;
+}
+__device__ __forceinline__ int item_units(const AttnArgs& a, int kv, int n, int j) {
+    const int per = 2 * a.toks;
+    int begin, end;
+    seen_keys(a, kv, n, j * per, min(per, n - j * per), begin, end);
+    return (end + kKeys - 1) / kKeys - begin / kKeys;
+}
+
+// Part buffers of a CTA: 0, 1 the part that ends an item begun by an earlier CTA (halves 0, 1), 2, 3 the part that begins an
+// item that goes on in the next, 4, 5 the copies of the slots' own items.  128 rows of D sums, then (m, l) of each.
+template <int D>
+__device__ __forceinline__ float* part_buf(const AttnArgs& a, int cta, int which) {
+    return a.parts + (size_t)(cta * kBufs + which) * (kRows * (D + 2));
+}
+
+// Bounded waits that pass at once after the first that gave up, so that every role runs to its end.
+struct Waiter {
+    bool ok = true;
+    __device__ __forceinline__ void thread(uint64_t* b, uint32_t use) {
+        if (ok) ok = mbar_wait(smem_u32(b), use & 1u);
+    }
+    __device__ __forceinline__ void warp(uint64_t* b, uint32_t use) {
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(b), use & 1u));
+    }
+};
+
+// Softmax of NCH chunks of 32 columns from chunk ch0 on of a row's scores, P over them and zeros in the other chunks.
+// [c0, c1): the columns that the row sees, if not all.  rescale(f) multiplies the row's O by f and returns when that
+// is done; called by whole warps.
+template <bool kBf16, int NCH, typename F>
+__device__ __forceinline__ void softmax_tile(uint32_t tS, int ch0, bool full, int c0, int c1, float c, bool first, bool live,
+                                             float& m, float& l, F&& rescale) {
+    uint32_t x[NCH * 32];
+#pragma unroll
+    for (int q = 0; q < NCH; ++q) tmem_ld32(tS + 32 * (ch0 + q), x + 32 * q);
+    tmem_wait_ld();
+    if (!full) {
+#pragma unroll
+        for (int i = 0; i < NCH * 32; ++i) {
+            const int col = 32 * ch0 + i;
+            if (col < c0 || col >= c1) x[i] = 0xFF800000u;
+        }
+    }
+    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int i = 0; i < NCH * 32; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(x[i]));
+    const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+    if (first) {
+        m = mt;
+    } else if (__any_sync(0xffffffffu, live && mt > m + 8.0f)) {
+        const float mn = fmaxf(m, mt);
+        const float f = mn == -INFINITY ? 1.0f : exp2_hw(m - mn);
+        m = mn;
+        l *= f;
+        rescale(f);
+    }
+    const float ms = finite_or_zero(m);
+    const float2 cc = make_float2(c, c), mm = make_float2(-ms, -ms);
+    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+    for (int q = 0; q < NCH; ++q) {
+        uint32_t p[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float2 s = make_float2(__uint_as_float(x[32 * q + 2 * i]), __uint_as_float(x[32 * q + 2 * i + 1]));
+            const float2 t = __ffma2_rn(s, cc, mm);
+            const float2 e = make_float2(exp2_hw(t.x), exp2_hw(t.y));
+            sum[i & 1] = __fadd2_rn(sum[i & 1], e);
+            p[i] = pack16<kBf16>(e.x, e.y);
+        }
+        tmem_st16(tS + 16 * (ch0 + q), p);
+    }
+    if (NCH < 4) {
+        uint32_t z[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[i] = 0u;
+        for (int q = 0; q < 4; ++q)
+            if (q < ch0 || q >= ch0 + NCH) tmem_st16(tS + 16 * q, z);
+    }
+    l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
+    tmem_wait_st();
+}
+
+template <bool kBf16, int D>
+__global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_constant__ AttnArgs a) {
+    using Sh = Shape<D>;
+    constexpr int kNS = Sh::kStages, kNH = D / 64;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* sQ = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* sKV = sQ + 2 * Sh::kTile;
+    __shared__ __align__(8) uint64_t bars[kBars];
+    __shared__ Item items[kRing];
+    __shared__ uint32_t tslot;
+    __shared__ int64_t warp_cost[kThreads / 32], head_cost;
+    // the threads' sums of costs, in the ring's last tile until the load warp has found its first item
+    int64_t* cost_end = reinterpret_cast<int64_t*>(sKV + (kNS - 1) * Sh::kTile);
+    __shared__ int last_flag[2];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+    if (tid == 0) {
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(&bars[kSFull + s], 1);
+            mbar_init(&bars[kPFull + s], 4);
+            mbar_init(&bars[kPvDone + s], 1);
+            mbar_init(&bars[kQFull + s], 1);
+            mbar_init(&bars[kQEmpty + s], 1);
+            mbar_init(&bars[kWg + s], 4);
+        }
+        for (int s = 0; s < kRing; ++s) {
+            mbar_init(&bars[kItemFull + s], 1);
+            mbar_init(&bars[kItemEmpty + s], 9);  // eight softmax warps and the product thread
+        }
+        mbar_init(&bars[kDrain], 1);
+        for (int s = 0; s < kNS; ++s) {
+            mbar_init(&bars[kKvFull + s], 1);
+            mbar_init(&bars[kKvEmpty + s], 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tslot)), "r"(512u));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+
+    // The cost of all items of one head: each thread k consecutive requests, then a scan.  A request of several items is
+    // summed by its warp.
+    const int k = (a.n_req + kThreads - 1) / kThreads;
+    {
+        int64_t mine = 0;
+        for (int i = 0; i < k; ++i) {
+            const int r = tid * k + i;
+            const Req q = load_req(a, r, blockIdx.x == 0);
+            const int m = (q.n + 2 * a.toks - 1) / (2 * a.toks);
+            if (m == 1) mine += kItemCost + item_units(a, q.kv, q.n, 0);
+            uint32_t big = __ballot_sync(0xffffffffu, m > 1);
+            while (big) {
+                const int src = __ffs(big) - 1;
+                big &= big - 1;
+                const int kv = __shfl_sync(0xffffffffu, q.kv, src), n = __shfl_sync(0xffffffffu, q.n, src),
+                          mm = __shfl_sync(0xffffffffu, m, src);
+                int64_t c = 0;
+                for (int j = lane; j < mm; j += 32) c += kItemCost + item_units(a, kv, n, j);
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) c += __shfl_xor_sync(0xffffffffu, c, d);
+                if (lane == src) mine += c;
+            }
+        }
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int64_t t = __shfl_up_sync(0xffffffffu, mine, d);
+            if (lane >= d) mine += t;
+        }
+        if (lane == 31) warp_cost[warp] = mine;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) mine += warp_cost[w];
+        cost_end[tid] = mine;
+        if (tid == kThreads - 1) head_cost = mine;
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = tslot;
+    const int64_t total = head_cost * a.n_kv_heads;
+    const int64_t n_cta = min((int64_t)gridDim.x, max(total, (int64_t)1));
+    const int64_t B0 = blockIdx.x < n_cta ? blockIdx.x * total / n_cta : total;
+    const int64_t B1 = blockIdx.x < n_cta ? (blockIdx.x + 1) * total / n_cta : total;
+    Waiter wait;
+
+    if (warp == kLoadWarp) {
+        // ---- items, and the copies of their tiles
+        uint32_t n_item = 0, n_load = 0, n_q[2] = {0, 0};
+        int cached = -1;  // requests 32 cached .. are in the lanes
+        Req mine{0, 0, 0};
+        auto get = [&](int r) {
+            if ((r >> 5) != cached) {
+                cached = r >> 5;
+                mine = load_req(a, cached * 32 + lane, false);
+            }
+            return Req{__shfl_sync(0xffffffffu, mine.q0, r & 31), __shfl_sync(0xffffffffu, mine.n, r & 31),
+                       __shfl_sync(0xffffffffu, mine.kv, r & 31)};
+        };
+        int h = 0, r = 0, j = 0;
+        int64_t p = B0;  // where item (h, r, j) starts
+        if (B0 < B1) {
+            h = (int)(B0 / head_cost);
+            const int64_t y = B0 - h * head_cost;
+            int lo = 0, hi = kThreads - 1;  // the first thread whose sum passes y
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (cost_end[mid] > y) hi = mid;
+                else lo = mid + 1;
+            }
+            int64_t at = lo ? cost_end[lo - 1] : 0;
+            bool found = false;
+            for (r = lo * k; !found; ) {
+                const Req q = get(r);
+                const int m = (q.n + 2 * a.toks - 1) / (2 * a.toks);
+                for (int j0 = 0; j0 < m && !found; j0 += 32) {
+                    const int64_t c = j0 + lane < m ? kItemCost + item_units(a, q.kv, q.n, j0 + lane) : 0;
+                    int64_t s = c;
+#pragma unroll
+                    for (int d = 1; d < 32; d <<= 1) {
+                        const int64_t t = __shfl_up_sync(0xffffffffu, s, d);
+                        if (lane >= d) s += t;
+                    }
+                    const uint32_t past = __ballot_sync(0xffffffffu, at + s > y);
+                    if (past) {
+                        const int src = __ffs(past) - 1;
+                        j = j0 + src;
+                        at += __shfl_sync(0xffffffffu, s - c, src);
+                        found = true;
+                    } else {
+                        at += __shfl_sync(0xffffffffu, s, 31);
+                    }
+                }
+                if (!found) ++r;
+                if (r >= a.n_req) found = true;  // not reached: y is below the sum of all
+            }
+            p = h * head_cost + at;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the tile may be copied over
+            __syncwarp();
+        }
+        const int bs = 1 << a.bs_log, box = min(bs, kKeys), n_page = kKeys / box;
+        const int page = lane / kNH, half = lane % kNH;
+        bool bad_id = false;
+        // the block of this lane's page of tile u, -1 if no row sees any of it
+        auto page_id = [&](const Item& it, int u) {
+            const int key = u * kKeys + page * box;
+            if (page >= n_page || key >= it.end || key + box <= it.begin) return -1;
+            const int id = __ldg(a.table + (int64_t)it.r * a.ld_table + (key >> a.bs_log));
+            if (id >= 0 && id < a.n_blocks) return id;
+            bad_id = true;
+            return (int)a.n_blocks;  // past the end: the copy writes zeros
+        };
+        auto load_tile = [&](const CUtensorMap* map, int u, int id, int head) {
+            const uint32_t st = n_load % kNS, use = n_load / kNS;
+            if (use > 0) wait.warp(&bars[kKvEmpty + st], use - 1);
+            if (!wait.ok) return;
+            const uint32_t n = __popc(__ballot_sync(0xffffffffu, id >= 0));
+            const uint32_t bar = smem_u32(&bars[kKvFull + st]);
+            if (lane == 0)
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n * box * 128u) : "memory");
+            __syncwarp();
+            if (id >= 0)
+                asm volatile(
+                    "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, "
+                    "%5}], [%6];" ::"r"(smem_u32(sKV) + st * Sh::kTile + half * kHalf + page * box * 128),
+                    "l"(map), "r"(half * 64), "r"(head), "r"((u * kKeys) & (bs - 1)), "r"(id), "r"(bar)
+                    : "memory");
+            ++n_load;
+        };
+        auto load_q = [&](const Item& it, int s, int tok, int head) {
+            if (n_q[s] > 0) wait.warp(&bars[kQEmpty + s], n_q[s] - 1);
+            if (!wait.ok) return;
+            const uint32_t bar = smem_u32(&bars[kQFull + s]);
+            const int rows = kRows >> it.rep_log, boxed = rows / a.group * a.group, copies = 1 << it.rep_log;
+            if (lane == 0)
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
+                             "r"((uint32_t)(copies * kNH * boxed * 128))
+                             : "memory");
+            __syncwarp();
+            if (page < copies)
+                asm volatile(
+                    "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
+                    "%4}], [%5];" ::"r"(smem_u32(sQ) + s * Sh::kTile + half * kHalf + page * rows * 128),
+                    "l"(&a.qmap[it.rep_log]), "r"(half * 64), "r"(head * a.group), "r"(tok), "r"(bar)
+                    : "memory");
+            ++n_q[s];
+        };
+        int turn = 0;
+        while (p < B1 && wait.ok) {
+            const Req q = get(r);
+            const int per = 2 * a.toks, m = (q.n + per - 1) / per;
+            if (j >= m) {  // the next request with a token, in the next head if need be
+                const uint32_t more = __ballot_sync(0xffffffffu, mine.n > 0) & ~((2u << (r & 31)) - 1u);
+                r = more ? (r & ~31) + __ffs(more) - 1 : (r & ~31) + 32;
+                j = 0;
+                if (r >= a.n_req) {
+                    r = 0;
+                    ++h;
+                    if (h >= a.n_kv_heads) break;
+                }
+                if (get(r).n == 0) j = 1;  // a fresh group of 32 starts on an empty one
+                continue;
+            }
+            Item it;
+            it.h = h;
+            it.r = r;
+            it.ntok = min(per, q.n - j * per);
+            it.tok = q.q0 + j * per;
+            it.pos = q.kv - q.n + j * per;
+            it.kv = q.kv;
+            seen_keys(a, q.kv, q.n, j * per, it.ntok, it.begin, it.end);
+            it.rep_log = it.ntok * a.group <= kRows / 4 ? 2 : it.ntok * a.group <= kRows / 2 ? 1 : 0;
+            it.poison = it.stop = 0;
+            const int t0 = it.begin / kKeys, units = (it.end + kKeys - 1) / kKeys - t0;
+            const int64_t s = p + kItemCost;  // where its units start
+            const int lo = (int)max((int64_t)0, min((int64_t)units, B0 - s)), hi = (int)max((int64_t)0, min((int64_t)units, B1 - s));
+            const bool here = units ? hi > lo : p >= B0;
+            p = s + units;
+            ++j;
+            if (!here) continue;
+            it.u0 = t0 + lo;
+            it.nu = hi - lo;
+            it.first = blockIdx.x;
+            it.n_parts = 1;
+            if (it.nu < units) {
+                it.first = (int)(((s + 1) * n_cta - 1) / total);
+                it.n_parts = (int)(((s + units) * n_cta - 1) / total) - it.first + 1;
+            }
+            it.slot = it.ntok > a.toks ? 2 : turn;
+            if (it.slot < 2) turn ^= 1;
+            const uint32_t ring = n_item % kRing;
+            if (n_item >= kRing) wait.warp(&bars[kItemEmpty + ring], n_item / kRing - 1);
+            if (!wait.ok) break;
+            if (lane == 0) {
+                items[ring] = it;
+                mbar_arrive(&bars[kItemFull + ring]);
+            }
+            __syncwarp();
+            ++n_item;
+            int id = it.nu > 0 ? page_id(it, it.u0) : -1;
+            for (int u = 0; u < it.nu && wait.ok; ++u) {
+                const int id_next = u + 1 < it.nu ? page_id(it, it.u0 + u + 1) : -1;
+                load_tile(&a.kmap, it.u0 + u, id, h);
+                if (u == 0) {
+#pragma unroll
+                    for (int sl = 0; sl < 2; ++sl)
+                        if (it.slot == 2 || it.slot == sl) load_q(it, sl, it.tok + (it.slot == 2 ? sl * a.toks : 0), h);
+                }
+                load_tile(&a.vmap, it.u0 + u, id, h);
+                id = id_next;
+            }
+        }
+        if (wait.ok && n_item >= kRing) wait.warp(&bars[kItemEmpty + n_item % kRing], n_item / kRing - 1);
+        if (wait.ok && lane == 0) {
+            items[n_item % kRing].stop = 1;
+            mbar_arrive(&bars[kItemFull + n_item % kRing]);
+        }
+        if (bad_id) atomicOr(a.err, SCOOT_DEVERR_INDEX);
+        __syncwarp();
+        if (!wait.ok) {
+            // gave up: the copies in flight land before the block ends
+            if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
+            for (uint32_t i = n_load > kNS ? n_load - kNS : 0; i < n_load; ++i)
+                mbar_wait(smem_u32(&bars[kKvFull + i % kNS]), (i / kNS) & 1u);
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                if (n_q[s] > 0) mbar_wait(smem_u32(&bars[kQFull + s]), (n_q[s] - 1) & 1u);
+        }
+    } else if (warp == kMmaWarp) {
+        // ---- the products, by one thread
+        if (lane == 0) {
+            uint32_t n_unit = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
+            struct {
+                bool on, acc, release;
+                uint32_t load;
+            } pend[2] = {{false, false, false, 0}, {false, false, false, 0}};  // products with V still to be issued
+            const uint32_t id_s = idesc(kBf16, kKeys, false), id_o = idesc(kBf16, D, true);
+            auto commit = [&](uint64_t* b) {
+                asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
+            };
+            auto values = [&](int s) {
+                const uint32_t st = pend[s].load % kNS, use = pend[s].load / kNS;
+                wait.thread(&bars[kPFull + s], n_p[s]++);
+                wait.thread(&bars[kKvFull + st], use);
+                pend[s].on = false;
+                if (!wait.ok) return;
+                fence_after();
+                const uint64_t dv = desc_v(smem_u32(sKV) + st * Sh::kTile);
+                const uint32_t o = tmem + kO0 + s * D, pp = tmem + kS0 + s * kKeys;
+#pragma unroll
+                for (int i = 0; i < kKeys / 16; ++i)
+                    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(o),
+                                 "r"(pp + 8 * i), "l"(dv + 128 * i), "r"(id_o), "r"((pend[s].acc || i > 0) ? 1u : 0u));
+                commit(&bars[kPvDone + s]);
+                if (pend[s].release) commit(&bars[kKvEmpty + st]);
+            };
+            for (uint32_t n_item = 0; wait.ok; ++n_item) {
+                wait.thread(&bars[kItemFull + n_item % kRing], n_item / kRing);
+                if (!wait.ok) break;
+                const volatile Item& it = items[n_item % kRing];
+                const bool stop = it.stop;
+                const int nu = it.nu, slot = it.slot;
+                if (stop) break;
+                mbar_arrive(&bars[kItemEmpty + n_item % kRing]);
+                for (int u = 0; u < nu && wait.ok; ++u, ++n_unit) {
+                    const uint32_t load = 2 * n_unit, st = load % kNS, use = load / kNS;
+                    // the last products of a pair go in order, whichever slot comes next
+                    if (slot == 1 && pend[0].on && pend[1].on) values(0);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        if (slot != 2 && slot != s) continue;
+                        const bool last = slot != 2 || s == 1;  // of this tile's users
+                        if (pend[s].on) values(s);
+                        if (u == 0) wait.thread(&bars[kQFull + s], n_q[s]++);
+                        wait.thread(&bars[kKvFull + st], use);
+                        if (!wait.ok) continue;
+                        fence_after();
+                        const uint64_t dq = desc_k(smem_u32(sQ) + s * Sh::kTile), dk = desc_k(smem_u32(sKV) + st * Sh::kTile);
+#pragma unroll
+                        for (int i = 0; i < D / 16; ++i) {
+                            const uint32_t off = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
+                            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                                         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem + kS0 + s * kKeys),
+                                         "l"(dq + off), "l"(dk + off), "r"(id_s), "r"(i > 0 ? 1u : 0u));
+                        }
+                        commit(&bars[kSFull + s]);
+                        if (last) commit(&bars[kKvEmpty + st]);
+                        if (u == nu - 1) commit(&bars[kQEmpty + s]);
+                        pend[s].on = true;
+                        pend[s].acc = u > 0;
+                        pend[s].release = last;
+                        pend[s].load = load + 1;
+                    }
+                    if (slot == 0 && pend[1].on) values(1);  // an earlier item's last
+                    if (slot == 1 && pend[0].on) values(0);
+                }
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                if (pend[s].on && wait.ok) values(s);
+            if (!wait.ok) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
+            commit(&bars[kDrain]);
+            mbar_wait(smem_u32(&bars[kDrain]), 0);
+        }
+    } else {
+        // ---- softmax of slot s; this thread's row of tensor memory is lane row
+        const int s = warp >> 2, row = tid & (kRows - 1);
+        const uint32_t lane_at = (uint32_t)(32 * (warp & 3)) << 16;
+        const uint32_t tS = tmem + kS0 + s * kKeys + lane_at, tO = tmem + kO0 + s * D + lane_at;
+        uint32_t n_s = 0, n_wg = 0, n_unit = 0;
+        auto wg_sync = [&]() {
+            warp_arrive(&bars[kWg + s]);
+            wait.warp(&bars[kWg + s], n_wg++);
+        };
+        for (uint32_t n_item = 0; wait.ok; ++n_item) {
+            const uint32_t ring = n_item % kRing;
+            wait.warp(&bars[kItemFull + ring], n_item / kRing);
+            if (!wait.ok) break;
+            const Item it = items[ring];
+            if (it.stop) break;
+            if (it.slot != 2 && it.slot != s) {
+                warp_arrive(&bars[kItemEmpty + ring]);
+                n_unit += it.nu;
+                continue;
+            }
+            const int half = it.slot == 2 ? s : 0;
+            const int tok0 = half * a.toks, ntok = min(a.toks, it.ntok - tok0), rows = ntok * a.group;
+            const int per_copy = kRows >> it.rep_log, rr = row & (per_copy - 1), copy = row / per_copy;
+            const int j = rr / a.group, g = rr - j * a.group;
+            const bool live = rr < rows;
+            const bool busy = __any_sync(0xffffffffu, live);
+            // keys that this row sees; that every row of the slot sees
+            const int pos = it.pos + tok0 + j;
+            int k0, k1;
+            {
+                k1 = a.causal ? min(it.kv, pos + 1) : it.kv;
+                k0 = a.window > 0 ? (int)max((int64_t)0, (int64_t)pos + 1 - a.window) : 0;
+                if (!live) k0 = k1 = 0;
+            }
+            const int all1 = a.causal ? min(it.kv, it.pos + tok0 + 1) : it.kv;
+            const int all0 = a.window > 0 ? (int)max((int64_t)0, (int64_t)it.pos + tok0 + ntok - a.window) : 0;
+            float m = -INFINITY, l = 0.0f;
+            for (int u = 0; u < it.nu; ++u, ++n_unit, ++n_s) {
+                const int t0 = (it.u0 + u) * kKeys;
+                const bool full = t0 >= all0 && t0 + kKeys <= all1;
+                wait.warp(&bars[kSFull + s], n_s);
+                fence_after();
+                if (busy) {
+                    auto rescale = [&](float f) {
+                        wait.warp(&bars[kPvDone + s], n_s - 1);
+                        fence_after();
+#pragma unroll
+                        for (int c = 0; c < D; c += 32) {
+                            uint32_t o[32];
+                            tmem_ld32(tO + c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st32(tO + c, o);
+                        }
+                    };
+                    if (it.rep_log == 0)
+                        softmax_tile<kBf16, 4>(tS, 0, full, k0 - t0, k1 - t0, a.scale_log2, u == 0, live, m, l, rescale);
+                    else if (it.rep_log == 1)
+                        softmax_tile<kBf16, 2>(tS, 2 * copy, full, k0 - t0, k1 - t0, a.scale_log2, u == 0, live, m, l, rescale);
+                    else
+                        softmax_tile<kBf16, 1>(tS, copy, full, k0 - t0, k1 - t0, a.scale_log2, u == 0, live, m, l, rescale);
+                }
+                if (!full) {
+                    // values that some row may not see: this thread looks through those of key t0 + row
+                    const uint32_t load = 2 * n_unit + 1, st = load % kNS;
+                    wait.warp(&bars[kKvFull + st], load / kNS);
+                    const int key = t0 + row;
+                    uint4* v = reinterpret_cast<uint4*>(sKV + st * Sh::kTile + row * 128);
+                    if (key < it.begin || key >= it.end) {
+#pragma unroll
+                        for (int c = 0; c < D / 8; ++c) v[(c / 8) * (kHalf / 16) + (c % 8)] = make_uint4(0, 0, 0, 0);
+                    } else if (key < all0 || key >= all1) {
+#pragma unroll
+                        for (int c = 0; c < D / 8; ++c) {
+                            uint4* at = v + (c / 8) * (kHalf / 16) + ((c ^ row) & 7);
+                            uint4 w = *at;
+                            const uint32_t bx = not_finite<kBf16>(w.x), by = not_finite<kBf16>(w.y),
+                                           bz = not_finite<kBf16>(w.z), bw = not_finite<kBf16>(w.w);
+                            if (bx | by | bz | bw) {
+                                *reinterpret_cast<volatile int32_t*>(&items[ring].poison) = 1;  // before the zero can be seen
+                                __threadfence_block();
+                                *at = make_uint4(w.x & ~bx, w.y & ~by, w.z & ~bz, w.w & ~bw);
+                            }
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                fence_before();
+                warp_arrive(&bars[kPFull + s]);
+            }
+            // ---- the end of the item: O and l of this part
+            if (it.nu > 0) {
+                wait.warp(&bars[kPvDone + s], n_s - 1);
+                fence_after();
+            }
+            const bool poison = *reinterpret_cast<volatile int32_t*>(&items[ring].poison) != 0;
+            auto load_o = [&](int c, float* o) {  // columns c .. c + 31, with the values that were replaced
+                uint32_t x[32];
+                if (it.nu > 0) {
+                    tmem_ld32(tO + c, x);
+                    tmem_wait_ld();
+                }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = it.nu > 0 ? __uint_as_float(x[i]) : 0.0f;
+                if (poison && live)
+                    for (int u = it.u0; u < it.u0 + it.nu; ++u) {
+                        const int w0 = u * kKeys + (copy << (7 - it.rep_log)), w1 = w0 + (kKeys >> it.rep_log);
+                        for (int key = max(k0, w0); key < min(k1, w1); ++key) {
+                            const int id = a.table[(int64_t)it.r * a.ld_table + (key >> a.bs_log)];
+                            if (id < 0 || id >= a.n_blocks) continue;
+                            const uint16_t* v = a.v + id * a.ld_block + (key & ((1 << a.bs_log) - 1)) * a.ld_token + it.h * a.ld_head + c;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                const uint32_t w = v[i];
+                                if (not_finite<kBf16>(w)) o[i] += value16<kBf16>((uint16_t)w);
+                            }
+                        }
+                    }
+            };
+            const int64_t head = (int64_t)it.h * a.group;
+            if (it.rep_log == 0 && it.n_parts == 1) {
+                const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+                const int64_t tok = it.tok + tok0 + j;
+                uint16_t* dst = a.out + tok * a.out_ld_token + (head + g) * a.out_ld_head;
+                if (busy) {
+#pragma unroll
+                    for (int c = 0; c < D; c += 32) {
+                        float o[32];
+                        load_o(c, o);
+                        if (live) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 8)
+                                *reinterpret_cast<uint4*>(dst + c + i) =
+                                    make_uint4(pack16<kBf16>(o[i] * inv, o[i + 1] * inv), pack16<kBf16>(o[i + 2] * inv, o[i + 3] * inv),
+                                               pack16<kBf16>(o[i + 4] * inv, o[i + 5] * inv), pack16<kBf16>(o[i + 6] * inv, o[i + 7] * inv));
+                        }
+                    }
+                    if (live && a.lse) a.lse[tok * a.n_heads + head + g] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+                }
+                warp_arrive(&bars[kItemEmpty + ring]);
+                continue;
+            }
+            const bool split = it.n_parts > 1;
+            const int part = blockIdx.x - it.first;
+            float* buf = part_buf<D>(a, blockIdx.x, split ? (part == 0 ? 2 : 0) + half : 4 + s);
+            if (busy) {
+#pragma unroll
+                for (int c = 0; c < D; c += 32) {
+                    float o[32];
+                    load_o(c, o);
+                    if (live) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            *reinterpret_cast<float4*>(buf + row * D + c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                    }
+                }
+                if (live) *reinterpret_cast<float2*>(buf + kRows * D + 2 * row) = make_float2(m, l);
+            }
+            warp_arrive(&bars[kItemEmpty + ring]);
+            bool join = true;
+            if (split) {
+                __threadfence();
+                wg_sync();
+                if (row == 0) {
+                    uint32_t* cnt = a.count + 2 * it.first + half;
+                    const bool last = atomicAdd(cnt, 1u) == (uint32_t)it.n_parts - 1;
+                    if (last) *cnt = 0;
+                    __threadfence();
+                    *reinterpret_cast<volatile int*>(&last_flag[s]) = last;
+                }
+                wg_sync();
+                join = *reinterpret_cast<volatile int*>(&last_flag[s]) != 0;
+            } else {
+                wg_sync();
+            }
+            if (join) {
+                // a warp per row: the parts' and copies' weights, then their sums
+                const int V = it.n_parts << it.rep_log, cmask = (1 << it.rep_log) - 1;
+                auto at = [&](int i) {  // of part i >> rep_log, copy i & cmask
+                    const int pt = i >> it.rep_log;
+                    return split ? part_buf<D>(a, it.first + pt, (pt == 0 ? 2 : 0) + half) : buf;
+                };
+                for (int q = warp & 3; q < rows; q += 4) {
+                    float M = -INFINITY;
+                    for (int i = lane; i < V; i += 32)
+                        M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(at(i) + kRows * D + 2 * ((i & cmask) * per_copy + q))).x);
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+                    const float Ms = finite_or_zero(M);
+                    float L = 0.0f, acc[D / 32];
+#pragma unroll
+                    for (int e = 0; e < D / 32; ++e) acc[e] = 0.0f;
+                    for (int i0 = 0; i0 < V; i0 += 32) {
+                        float w = 0.0f;
+                        if (i0 + lane < V) {
+                            const float2 ml = __ldcg(reinterpret_cast<const float2*>(
+                                at(i0 + lane) + kRows * D + 2 * (((i0 + lane) & cmask) * per_copy + q)));
+                            w = exp2_hw(ml.x - Ms);
+                            L = fmaf(w, ml.y, L);
+                        }
+                        const int n = min(32, V - i0);
+#pragma unroll 4
+                        for (int i = 0; i < n; ++i) {
+                            const float wi = __shfl_sync(0xffffffffu, w, i);
+                            const float* src = at(i0 + i) + (((i0 + i) & cmask) * per_copy + q) * D + lane * (D / 32);
+                            if (D == 128) {
+                                const float4 o = __ldcg(reinterpret_cast<const float4*>(src));
+                                acc[0] = fmaf(wi, o.x, acc[0]);
+                                acc[1] = fmaf(wi, o.y, acc[1]);
+                                acc[D / 32 - 2] = fmaf(wi, o.z, acc[D / 32 - 2]);
+                                acc[D / 32 - 1] = fmaf(wi, o.w, acc[D / 32 - 1]);
+                            } else {
+                                const float2 o = __ldcg(reinterpret_cast<const float2*>(src));
+                                acc[0] = fmaf(wi, o.x, acc[0]);
+                                acc[1] = fmaf(wi, o.y, acc[1]);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
+                    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+                    const int64_t tok = it.tok + tok0 + q / a.group, hd = head + q % a.group;
+                    uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + tok * a.out_ld_token + hd * a.out_ld_head) + lane * (D / 64);
+                    if (D == 128)
+                        *reinterpret_cast<uint2*>(dst) = make_uint2(pack16<kBf16>(acc[0] * inv, acc[1] * inv),
+                                                                    pack16<kBf16>(acc[D / 32 - 2] * inv, acc[D / 32 - 1] * inv));
+                    else
+                        *dst = pack16<kBf16>(acc[0] * inv, acc[1] * inv);
+                    if (a.lse && lane == 0) a.lse[tok * a.n_heads + hd] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+                }
+                if (!split) wg_sync();  // the buffer is free for the next item
+            }
+        }
+        if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
+    }
+    fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
+}
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// cuTensorMapEncodeTiled, from the driver (the library does not link it).
+EncodeTiled encode_tiled() {
+    static const EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            p = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+// A map of n_dim dimensions, the first of 64-element rows (128-byte swizzle); strides in elements.
+bool encode(CUtensorMap* map, bool bf16, const void* base, int n_dim, const cuuint64_t* dims, const int64_t* ld,
+            const cuuint32_t* box) {
+    cuuint64_t strides[4];
+    const cuuint32_t step[4] = {1, 1, 1, 1};
+    for (int i = 0; i + 1 < n_dim; ++i) strides[i] = (cuuint64_t)ld[i] * 2;
+    return encode_tiled()(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, n_dim,
+                          const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool kBf16, int D>
+scoot_status launch(scoot_ctx* ctx, AttnArgs& a, int sms, cudaStream_t st) {
+    scoot_status s = scoot_workspace(ctx, (size_t)sms * kBufs * kRows * (D + 2) * sizeof(float), st);
+    if (s != SCOOT_OK) return s;
+    a.parts = static_cast<float*>(ctx->ws);
+    auto kern = paged_attn_kernel<kBf16, D>;
+    SCOOT_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem));
+    kern<<<(unsigned)sms, kThreads, Shape<D>::kSmem, st>>>(a);
     SCOOT_LAUNCHED(ctx);
     return SCOOT_OK;
 }
@@ -125,7 +923,7 @@ extern "C" scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_lay
     if (n_heads / layout->n_kv_heads > SCOOT_MAX_GROUP)
         return scoot_fail(ctx, SCOOT_EUNSUPPORTED, "%d query heads per key-value head, more than %d",
                           n_heads / layout->n_kv_heads, SCOOT_MAX_GROUP);
-    if (n_tokens < 0 || n_tokens > 0x7FFFFFFFll / n_heads || n_req < 0 || ld_table < 0 || ld_table > (0x7FFFFFFFll / layout->block_size))
+    if (n_tokens < 0 || n_tokens > 0x7FFFFFFFll / n_heads || n_req < 0 || ld_table < 0 || ld_table > (0x40000000ll / layout->block_size))
         return scoot_fail(ctx, SCOOT_EINVAL, "n_tokens = %lld, n_req = %d or ld_table = %lld out of range", (long long)n_tokens,
                           n_req, (long long)ld_table);
     if (!(scale > 0.0f) || scale > 3.0e38f) return scoot_fail(ctx, SCOOT_EINVAL, "scale = %g must be positive and finite", scale);
@@ -135,31 +933,55 @@ extern "C" scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_lay
     if ((s = scoot_check_heads(ctx, "out", out, out_ld_token, out_ld_head, n_tokens, n_heads, layout->head_dim)) != SCOOT_OK)
         return s;
     if (!query_start || !kv_len || (ld_table && !block_table)) return scoot_fail(ctx, SCOOT_EINVAL, "an array is NULL");
-    AttnArgs a;
-    a.L = *layout;
-    a.bs_log = 0;
+    const int D = layout->head_dim, G = n_heads / layout->n_kv_heads;
+    if (!encode_tiled()) return scoot_fail(ctx, SCOOT_ECUDA, "the driver has no cuTensorMapEncodeTiled");
+    int sms = 0;
+    SCOOT_CUDA(ctx, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, ctx->device));
+    if (sms > kMaxCtas) sms = kMaxCtas;
+    AttnArgs a = {};
+    const bool bf16 = layout->dtype == SCOOT_BF16;
+    {
+        const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)layout->n_kv_heads, (cuuint64_t)layout->block_size,
+                                    (cuuint64_t)layout->n_blocks};
+        const int64_t ld[3] = {layout->ld_head, layout->ld_token, layout->ld_block};
+        const cuuint32_t box[4] = {64, 1, (cuuint32_t)(layout->block_size < kKeys ? layout->block_size : kKeys), 1};
+        if (!encode(&a.kmap, bf16, k_cache, 4, dims, ld, box) || !encode(&a.vmap, bf16, v_cache, 4, dims, ld, box))
+            return scoot_fail(ctx, SCOOT_EINVAL, "the cache's layout has no tensor map");
+    }
+    for (int i = 0; i < 3; ++i) {
+        const int toks = (kRows >> i) / G;
+        if (toks == 0) continue;  // a token's rows do not fit: no item uses it
+        const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)n_heads, (cuuint64_t)n_tokens};
+        const int64_t ld[2] = {q_ld_head, q_ld_token};
+        const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)toks};
+        if (!encode(&a.qmap[i], bf16, q, 3, dims, ld, box)) return scoot_fail(ctx, SCOOT_EINVAL, "q's layout has no tensor map");
+    }
     while ((1 << a.bs_log) < layout->block_size) ++a.bs_log;
     a.n_heads = n_heads;
-    a.group = n_heads / layout->n_kv_heads;
+    a.n_kv_heads = layout->n_kv_heads;
+    a.group = G;
     a.n_req = n_req;
     a.causal = causal != 0;
-    a.window = window;
-    a.q = q;
-    a.q_ld_token = q_ld_token;
-    a.q_ld_head = q_ld_head;
+    a.window = window < ld_table * layout->block_size ? window : 0;  // no sequence is longer
+    a.toks = kRows / G;
     a.n_tokens = n_tokens;
+    a.n_blocks = layout->n_blocks;
     a.query_start = query_start;
     a.kv_len = kv_len;
     a.table = block_table;
     a.ld_table = ld_table;
-    a.k = k_cache;
-    a.v = v_cache;
-    a.scale = scale;
-    a.out = out;
+    a.v = static_cast<const uint16_t*>(v_cache);
+    a.ld_block = layout->ld_block;
+    a.ld_token = layout->ld_token;
+    a.ld_head = layout->ld_head;
+    a.scale_log2 = scale * kLog2e;
+    a.out = static_cast<uint16_t*>(out);
     a.out_ld_token = out_ld_token;
     a.out_ld_head = out_ld_head;
     a.lse = lse;
+    a.count = ctx->d_count;
     a.err = ctx->d_err;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return layout->dtype == SCOOT_BF16 ? launch_rows<__nv_bfloat16>(ctx, a, st) : launch_rows<__half>(ctx, a, st);
+    if (bf16) return D == 128 ? launch<true, 128>(ctx, a, sms, st) : launch<true, 64>(ctx, a, sms, st);
+    return D == 128 ? launch<false, 128>(ctx, a, sms, st) : launch<false, 64>(ctx, a, sms, st);
 }
