@@ -47,7 +47,8 @@ using namespace scoot_dev;
 
 constexpr int kRows = 128;       // rows of a slot: the MMA's M and the TMEM lanes
 constexpr int kKeys = 128;       // keys of a tile
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;      // three warpgroups: the two softmax ones take registers from the third
+constexpr int kSoftmaxRegs = 200, kOtherRegs = 104;  // 2 * 200 + 104 = 3 * 168, what the block is launched with
 constexpr int kMmaWarp = 8, kLoadWarp = 9;
 constexpr int kRing = 4;         // items handed from the load warp to the others
 constexpr int kItemCost = 1;     // an item's start and end, in units
@@ -124,10 +125,11 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* x) {
         : "r"(addr));
 }
 
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* x) {
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t* x) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
-        "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]), "r"(x[8]), "r"(x[9]), "r"(x[10]), "r"(x[11]), "r"(x[12]), "r"(x[13]), "r"(x[14]), "r"(x[15]), "r"(x[16]), "r"(x[17]), "r"(x[18]), "r"(x[19]), "r"(x[20]), "r"(x[21]), "r"(x[22]), "r"(x[23]), "r"(x[24]), "r"(x[25]), "r"(x[26]), "r"(x[27]), "r"(x[28]), "r"(x[29]), "r"(x[30]), "r"(x[31]));
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]), "=r"(x[8]), "=r"(x[9]), "=r"(x[10]), "=r"(x[11]), "=r"(x[12]), "=r"(x[13]), "=r"(x[14]), "=r"(x[15])
+        : "r"(addr));
 }
 
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* x) {
@@ -363,6 +365,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     const int64_t B1 = blockIdx.x < n_cta ? (blockIdx.x + 1) * total / n_cta : total;
     Waiter wait;
 
+    if (warp >= kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kLoadWarp) {
         // ---- items, and the copies of their tiles
         uint32_t n_item = 0, n_load = 0, n_q[2] = {0, 0};
@@ -622,7 +626,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             commit(&bars[kDrain]);
             mbar_wait(smem_u32(&bars[kDrain]), 0);
         }
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         // ---- softmax of slot s; this thread's row of tensor memory is lane row
         const int s = warp >> 2, row = tid & (kRows - 1);
         const uint32_t lane_at = (uint32_t)(32 * (warp & 3)) << 16;
@@ -670,13 +676,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                         wait.warp(&bars[kPvDone + s], n_s - 1);
                         fence_after();
 #pragma unroll
-                        for (int c = 0; c < D; c += 32) {
-                            uint32_t o[32];
-                            tmem_ld32(tO + c, o);
+                        for (int c = 0; c < D; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(tO + c, o);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            tmem_st32(tO + c, o);
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st16(tO + c, o);
                         }
                     };
                     if (it.rep_log == 0)
