@@ -52,7 +52,8 @@ constexpr int kSoftmaxRegs = 200, kOtherRegs = 104;  // 2 * 200 + 104 = 3 * 168,
 constexpr int kMmaWarp = 8, kLoadWarp = 9;
 constexpr int kRing = 4;         // items handed from the load warp to the others
 constexpr int kItemCost = 1;     // an item's start and end, in units
-constexpr int kBufs = 6;         // part buffers of a CTA (see part_buf)
+constexpr int kBufs = 4;         // part buffers of a CTA (see part_buf)
+constexpr int kScratch = 16384;  // bytes of a slot's scratch: 32 columns of sums of its rows, or weights of parts
 constexpr int kHalf = kKeys * 128;  // bytes of a tile's half: 128 keys x 64 dimensions
 constexpr uint32_t kS0 = 0, kO0 = 256;  // tensor memory columns: S0, S1, O0, O1
 constexpr int kMaxCtas = (int)(SCOOT_COUNTS / 2);
@@ -61,8 +62,8 @@ constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
 template <int D>
 struct Shape {
     static constexpr int kTile = kKeys * D * 2;           // bytes of a tile of keys, values or queries
-    static constexpr int kStages = (D == 128 ? 5 : 10);   // tiles of keys or values in flight
-    static constexpr int kSmem = 2 * kTile + kStages * kTile + 1024;
+    static constexpr int kStages = (D == 128 ? 4 : 10);   // tiles of keys or values in flight
+    static constexpr int kSmem = 2 * kTile + kStages * kTile + 2 * kScratch;  // and the static part, up to 227 KB
 };
 
 struct AttnArgs {
@@ -150,6 +151,9 @@ __device__ __forceinline__ float exp2_hw(float x) {
 }
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.0f : m; }
 
+// 1 / l, 0 for a row that sees nothing (NaN stays).
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+
 template <bool kBf16>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
     if (kBf16) {
@@ -205,8 +209,8 @@ __device__ __forceinline__ int item_units(const AttnArgs& a, int kv, int n, int 
     return (end + kKeys - 1) / kKeys - begin / kKeys;
 }
 
-// Part buffers of a CTA: 0, 1 the part that ends an item begun by an earlier CTA (halves 0, 1), 2, 3 the part that begins an
-// item that goes on in the next, 4, 5 the copies of the slots' own items.  128 rows of D sums, then (m, l) of each.
+// Part buffers of a CTA: 0, 1 the part of an item that an earlier CTA began (halves 0, 1), 2, 3 the part that begins an item
+// that goes on in the next.  128 rows of D sums, then (m, l) of each.
 template <int D>
 __device__ __forceinline__ float* part_buf(const AttnArgs& a, int cta, int which) {
     return a.parts + (size_t)(cta * kBufs + which) * (kRows * (D + 2));
@@ -284,9 +288,10 @@ template <bool kBf16, int D>
 __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_constant__ AttnArgs a) {
     using Sh = Shape<D>;
     constexpr int kNS = Sh::kStages, kNH = D / 64;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* sQ = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    extern __shared__ __align__(1024) uint8_t smem[];
+    uint8_t* sQ = smem;
     uint8_t* sKV = sQ + 2 * Sh::kTile;
+    uint8_t* sScratch = sKV + kNS * Sh::kTile;
     __shared__ __align__(8) uint64_t bars[kBars];
     __shared__ Item items[kRing];
     __shared__ uint32_t tslot;
@@ -294,6 +299,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     // the threads' sums of costs, in the ring's last tile until the load warp has found its first item
     int64_t* cost_end = reinterpret_cast<int64_t*>(sKV + (kNS - 1) * Sh::kTile);
     __shared__ int last_flag[2];
+    __shared__ float2 ml_s[2][kRows];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
     if (tid == 0) {
@@ -652,7 +658,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             const int half = it.slot == 2 ? s : 0;
             const int tok0 = half * a.toks, ntok = min(a.toks, it.ntok - tok0), rows = ntok * a.group;
             const int per_copy = kRows >> it.rep_log, rr = row & (per_copy - 1), copy = row / per_copy;
-            const int j = rr / a.group, g = rr - j * a.group;
+            const int j = rr / a.group;
             const bool live = rr < rows;
             const bool busy = __any_sync(0xffffffffu, live);
             // keys that this row sees; that every row of the slot sees
@@ -750,11 +756,65 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                     }
             };
             const int64_t head = (int64_t)it.h * a.group;
-            if (it.rep_log == 0 && it.n_parts == 1) {
-                const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-                const int64_t tok = it.tok + tok0 + j;
-                uint16_t* dst = a.out + tok * a.out_ld_token + (head + g) * a.out_ld_head;
+            auto out_at = [&](int q) {  // of row q of the slot
+                return a.out + (int64_t)(it.tok + tok0 + q / a.group) * a.out_ld_token + (head + q % a.group) * a.out_ld_head;
+            };
+            auto lse_at = [&](int q) { return a.lse + (int64_t)(it.tok + tok0 + q / a.group) * a.n_heads + head + q % a.group; };
+            const bool whole = it.n_parts == 1;
+            const int part = blockIdx.x - it.first;
+            float* buf = part_buf<D>(a, blockIdx.x, (part == 0 ? 2 : 0) + half);
+            float* scratch = reinterpret_cast<float*>(sScratch + s * kScratch);
+            if (it.rep_log > 0) {
+                // Copies of the rows: their common maximum and sum, then the weighted sums of their O through the scratch
+                // (16-byte groups swizzled by the row), as many columns at a time as it holds of the rows in use.
+                const int copies = 1 << it.rep_log, used = rows << it.rep_log;
+                ml_s[s][row] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
+                wg_sync();
+                float M = -INFINITY, L = 0.0f;
+                for (int c = 0; c < copies; ++c) M = fmaxf(M, ml_s[s][c * per_copy + rr].x);
+                const float Ms = finite_or_zero(M);
+                for (int c = 0; c < copies; ++c) {
+                    const float2 v = ml_s[s][c * per_copy + rr];
+                    L = fmaf(exp2_hw(v.x - Ms), v.y, L);
+                }
+                const float w = exp2_hw(m - Ms), f = !whole ? w : L == 0.0f ? 0.0f : w / L;
+                if (copy == 0 && live) {
+                    if (!whole) *reinterpret_cast<float2*>(buf + kRows * D + 2 * rr) = make_float2(M, L);
+                    else if (a.lse) *lse_at(rr) = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+                }
+                const int width = used <= 32 ? min(D, 128) : used <= 64 ? 64 : 32, groups = width / 4;
+                const int g_log = 31 - __clz(groups);
+                for (int c0 = 0; c0 < D; c0 += width) {
+                    if (busy)
+                        for (int c = 0; c < width; c += 32) {
+                            float o[32];
+                            load_o(c0 + c, o);
+                            if (live) {
+                                const int at = copy * rows + rr;
+                                float4* dst = reinterpret_cast<float4*>(scratch) + at * groups;
+#pragma unroll
+                                for (int i = 0; i < 8; ++i)
+                                    dst[(c / 4 + i) ^ (at & 7)] = make_float4(o[4 * i] * f, o[4 * i + 1] * f, o[4 * i + 2] * f, o[4 * i + 3] * f);
+                            }
+                        }
+                    wg_sync();
+                    for (int e = row; e < rows << g_log; e += kRows) {
+                        const int q = e >> g_log, gq = e & (groups - 1);
+                        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (int c = 0; c < copies; ++c) {
+                            const int at = c * rows + q;
+                            const float4 v = reinterpret_cast<const float4*>(scratch)[at * groups + (gq ^ (at & 7))];
+                            t = make_float4(t.x + v.x, t.y + v.y, t.z + v.z, t.w + v.w);
+                        }
+                        if (whole) *reinterpret_cast<uint2*>(out_at(q) + c0 + 4 * gq) = make_uint2(pack16<kBf16>(t.x, t.y), pack16<kBf16>(t.z, t.w));
+                        else *reinterpret_cast<float4*>(buf + q * D + c0 + 4 * gq) = t;
+                    }
+                    if (c0 + width < D) wg_sync();
+                }
+            } else if (whole) {
+                const float inv = inverse_sum(l);
                 if (busy) {
+                    uint16_t* dst = out_at(rr);
 #pragma unroll
                     for (int c = 0; c < D; c += 32) {
                         float o[32];
@@ -767,15 +827,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                                                pack16<kBf16>(o[i + 4] * inv, o[i + 5] * inv), pack16<kBf16>(o[i + 6] * inv, o[i + 7] * inv));
                         }
                     }
-                    if (live && a.lse) a.lse[tok * a.n_heads + head + g] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+                    if (live && a.lse) *lse_at(rr) = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
                 }
-                warp_arrive(&bars[kItemEmpty + ring]);
-                continue;
-            }
-            const bool split = it.n_parts > 1;
-            const int part = blockIdx.x - it.first;
-            float* buf = part_buf<D>(a, blockIdx.x, split ? (part == 0 ? 2 : 0) + half : 4 + s);
-            if (busy) {
+            } else if (busy) {
 #pragma unroll
                 for (int c = 0; c < D; c += 32) {
                     float o[32];
@@ -789,78 +843,69 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 if (live) *reinterpret_cast<float2*>(buf + kRows * D + 2 * row) = make_float2(m, l);
             }
             warp_arrive(&bars[kItemEmpty + ring]);
-            bool join = true;
-            if (split) {
+            if (whole) continue;
+            __threadfence();
+            wg_sync();
+            if (row == 0) {
+                uint32_t* cnt = a.count + 2 * it.first + half;
+                const bool last = atomicAdd(cnt, 1u) == (uint32_t)it.n_parts - 1;
+                if (last) *cnt = 0;
                 __threadfence();
-                wg_sync();
-                if (row == 0) {
-                    uint32_t* cnt = a.count + 2 * it.first + half;
-                    const bool last = atomicAdd(cnt, 1u) == (uint32_t)it.n_parts - 1;
-                    if (last) *cnt = 0;
-                    __threadfence();
-                    *reinterpret_cast<volatile int*>(&last_flag[s]) = last;
+                *reinterpret_cast<volatile int*>(&last_flag[s]) = last;
+            }
+            wg_sync();
+            if (*reinterpret_cast<volatile int*>(&last_flag[s]) == 0) continue;
+            // The last part to come: per row the parts' common maximum and sum and each part's weight (into the scratch, a
+            // thread per row), then the weighted sums, a warp over eight rows at a time.
+            const int V = it.n_parts, batch = min(kRows, kScratch / 4 / V);
+            auto part_at = [&](int i) { return part_buf<D>(a, it.first + i, (i == 0 ? 2 : 0) + half); };
+            for (int q0 = 0; q0 < rows; q0 += batch) {
+                const int nq = min(batch, rows - q0);
+                if (q0 > 0) wg_sync();
+                if (row < nq) {
+                    float M = -INFINITY, L = 0.0f;
+#pragma unroll 8
+                    for (int i = 0; i < V; ++i) {
+                        const float2 v = __ldcg(reinterpret_cast<const float2*>(part_at(i) + kRows * D) + q0 + row);
+                        const float Mn = fmaxf(M, v.x), Ms = finite_or_zero(Mn);
+                        L = fmaf(L, exp2_hw(M - Ms), exp2_hw(v.x - Ms) * v.y);
+                        M = Mn;
+                        scratch[row * V + i] = v.x;
+                    }
+                    const float inv = inverse_sum(L), Ms = finite_or_zero(M);
+                    for (int i = 0; i < V; ++i) scratch[row * V + i] = exp2_hw(scratch[row * V + i] - Ms) * inv;
+                    if (a.lse) *lse_at(q0 + row) = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
                 }
                 wg_sync();
-                join = *reinterpret_cast<volatile int*>(&last_flag[s]) != 0;
-            } else {
-                wg_sync();
-            }
-            if (join) {
-                // a warp per row: the parts' and copies' weights, then their sums
-                const int V = it.n_parts << it.rep_log, cmask = (1 << it.rep_log) - 1;
-                auto at = [&](int i) {  // of part i >> rep_log, copy i & cmask
-                    const int pt = i >> it.rep_log;
-                    return split ? part_buf<D>(a, it.first + pt, (pt == 0 ? 2 : 0) + half) : buf;
-                };
-                for (int q = warp & 3; q < rows; q += 4) {
-                    float M = -INFINITY;
-                    for (int i = lane; i < V; i += 32)
-                        M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(at(i) + kRows * D + 2 * ((i & cmask) * per_copy + q))).x);
+                for (int q = (warp & 3) * 8; q < nq; q += 32) {
+                    constexpr int kE = D / 32;
+                    float acc[8][kE];
 #pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-                    const float Ms = finite_or_zero(M);
-                    float L = 0.0f, acc[D / 32];
+                    for (int i = 0; i < 8; ++i)
 #pragma unroll
-                    for (int e = 0; e < D / 32; ++e) acc[e] = 0.0f;
-                    for (int i0 = 0; i0 < V; i0 += 32) {
-                        float w = 0.0f;
-                        if (i0 + lane < V) {
-                            const float2 ml = __ldcg(reinterpret_cast<const float2*>(
-                                at(i0 + lane) + kRows * D + 2 * (((i0 + lane) & cmask) * per_copy + q)));
-                            w = exp2_hw(ml.x - Ms);
-                            L = fmaf(w, ml.y, L);
-                        }
-                        const int n = min(32, V - i0);
-#pragma unroll 4
-                        for (int i = 0; i < n; ++i) {
-                            const float wi = __shfl_sync(0xffffffffu, w, i);
-                            const float* src = at(i0 + i) + (((i0 + i) & cmask) * per_copy + q) * D + lane * (D / 32);
-                            if (D == 128) {
-                                const float4 o = __ldcg(reinterpret_cast<const float4*>(src));
-                                acc[0] = fmaf(wi, o.x, acc[0]);
-                                acc[1] = fmaf(wi, o.y, acc[1]);
-                                acc[D / 32 - 2] = fmaf(wi, o.z, acc[D / 32 - 2]);
-                                acc[D / 32 - 1] = fmaf(wi, o.w, acc[D / 32 - 1]);
-                            } else {
-                                const float2 o = __ldcg(reinterpret_cast<const float2*>(src));
-                                acc[0] = fmaf(wi, o.x, acc[0]);
-                                acc[1] = fmaf(wi, o.y, acc[1]);
-                            }
+                        for (int e = 0; e < kE; ++e) acc[i][e] = 0.0f;
+#pragma unroll 2
+                    for (int pt = 0; pt < V; ++pt) {
+                        const float* src = part_at(pt) + (q0 + q) * D + lane * kE;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            if (q + i >= nq) break;
+                            const float w = scratch[(q + i) * V + pt];
+                            float v[kE];
+                            if (D == 128) *reinterpret_cast<float4*>(v) = __ldcg(reinterpret_cast<const float4*>(src + i * D));
+                            else *reinterpret_cast<float2*>(v) = __ldcg(reinterpret_cast<const float2*>(src + i * D));
+#pragma unroll
+                            for (int e = 0; e < kE; ++e) acc[i][e] = fmaf(w, v[e], acc[i][e]);
                         }
                     }
 #pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
-                    const float inv = L == 0.0f ? 0.0f : 1.0f / L;
-                    const int64_t tok = it.tok + tok0 + q / a.group, hd = head + q % a.group;
-                    uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + tok * a.out_ld_token + hd * a.out_ld_head) + lane * (D / 64);
-                    if (D == 128)
-                        *reinterpret_cast<uint2*>(dst) = make_uint2(pack16<kBf16>(acc[0] * inv, acc[1] * inv),
-                                                                    pack16<kBf16>(acc[D / 32 - 2] * inv, acc[D / 32 - 1] * inv));
-                    else
-                        *dst = pack16<kBf16>(acc[0] * inv, acc[1] * inv);
-                    if (a.lse && lane == 0) a.lse[tok * a.n_heads + hd] = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+                    for (int i = 0; i < 8; ++i) {
+                        if (q + i >= nq) break;
+                        uint32_t* dst = reinterpret_cast<uint32_t*>(out_at(q0 + q + i)) + lane * (kE / 2);
+#pragma unroll
+                        for (int e = 0; e < kE / 2; ++e) dst[e] = pack16<kBf16>(acc[i][2 * e], acc[i][2 * e + 1]);
+                    }
                 }
-                if (!split) wg_sync();  // the buffer is free for the next item
             }
         }
         if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
