@@ -25,6 +25,17 @@ __device__ __forceinline__ bool mbar_try(uint32_t addr, uint32_t parity) {
     return done;
 }
 
+// Whether the phase of the given parity has completed, at once.
+__device__ __forceinline__ bool mbar_test(uint32_t addr, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(addr), "r"(parity)
+        : "memory");
+    return done;
+}
+
 // Waits (bounded) until the phase of the given parity of an mbarrier has
 // completed; false if it gave up.  The clock is read only after a try that
 // failed (which itself waits a while).

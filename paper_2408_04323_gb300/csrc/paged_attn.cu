@@ -99,9 +99,10 @@ struct Item {
     int32_t stop;
 };
 
+// The first three are [slot][parity of the slot's unit]: two units of a slot may be under way at once.
 enum {
-    kSFull = 0, kPFull = 2, kPvDone = 4, kQFull = 6, kQEmpty = 8, kWg = 10, kItemFull = 12, kItemEmpty = 16, kDrain = 20,
-    kKvFull = 21, kKvEmpty = 31, kBars = 41
+    kSFull = 0, kPFull = 4, kPvDone = 8, kQFull = 12, kQEmpty = 14, kWg = 16, kItemFull = 18, kItemEmpty = 22, kDrain = 26,
+    kKvFull = 27, kKvEmpty = 37, kBars = 47
 };
 
 // The swizzled K-major tile of queries or keys: rows of 128 bytes, 8-row groups 1024 bytes apart.
@@ -209,11 +210,23 @@ __device__ __forceinline__ int item_units(const AttnArgs& a, int kv, int n, int 
     return (end + kKeys - 1) / kKeys - begin / kKeys;
 }
 
-// Part buffers of a CTA: 0, 1 the part of an item that an earlier CTA began (halves 0, 1), 2, 3 the part that begins an item
-// that goes on in the next.  128 rows of D sums, then (m, l) of each.
+// a / b of a >= 0, b > 0, in 32 bits where they fit.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// Part buffers: 128 rows of D sums, then (m, l) of each.  A CTA has one per half (slot of a pair) for the part of an item
+// that an earlier CTA began, and one for the part that begins an item that goes on in the next; the parts of an item of
+// CTAs c, c + 1, .. are buffers 2 c + 1, 2 c + 2, 2 c + 4, ..: from 2 c + 2 on every second.
 template <int D>
-__device__ __forceinline__ float* part_buf(const AttnArgs& a, int cta, int which) {
-    return a.parts + (size_t)(cta * kBufs + which) * (kRows * (D + 2));
+constexpr int kPartFloats = kRows * (D + 2);
+template <int D>
+__device__ __forceinline__ float* part_buf(float* first, int i) {  // of part i, first that of part 0
+    return first + (size_t)(i == 0 ? 0 : 2 * i - 1) * kPartFloats<D>;
+}
+template <int D>
+__device__ __forceinline__ const float* part_buf(const float* first, int i) {
+    return first + (size_t)(i == 0 ? 0 : 2 * i - 1) * kPartFloats<D>;
 }
 
 // Bounded waits that pass at once after the first that gave up, so that every role runs to its end.
@@ -284,6 +297,108 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, int ch0, bool full, in
     tmem_wait_st();
 }
 
+// A slot's four warps meet (bounded): warps of one that gave up do not hold the others.
+struct SlotSync {
+    uint64_t* bar;
+    uint32_t n;
+    Waiter wait;
+    __device__ __forceinline__ void operator()() {
+        warp_arrive(bar);
+        wait.warp(bar, n++);
+    }
+};
+
+// Row q of a slot, tokens from tok on, the group's first head `head`: where it goes.
+__device__ __forceinline__ uint16_t* out_row(const AttnArgs& a, int tok, int head, int q) {
+    const int t = q / a.group;
+    return a.out + (int64_t)(tok + t) * a.out_ld_token + (int64_t)(head + q - t * a.group) * a.out_ld_head;
+}
+__device__ __forceinline__ float* lse_row(const AttnArgs& a, int tok, int head, int q) {
+    const int t = q / a.group;
+    return a.lse + (int64_t)(tok + t) * a.n_heads + head + q - t * a.group;
+}
+
+// Rows q .. q + R - 1 of nq: the weighted sums of their V parts, P parts at a time; a lane has D / 32 columns.
+template <bool kBf16, int D, int R, int P>
+__device__ __forceinline__ void join_rows(const AttnArgs& a, const float* part, const float* w, int V, int q0, int q, int nq,
+                                          int tok, int head) {
+    constexpr int kE = D / 32;
+    const int lane = threadIdx.x & 31;
+    float acc[R][kE];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int e = 0; e < kE; ++e) acc[i][e] = 0.0f;
+#pragma unroll 1
+    for (int p0 = 0; p0 < V; p0 += P) {
+        float v[P][R][kE], f[P][R];
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                // past the last part or row: the last one's, with no weight
+                const int pt = min(p0 + p, V - 1), row = min(q + i, nq - 1);
+                const float* src = part_buf<D>(part, pt) + (q0 + row) * D + lane * kE;
+                if (kE == 4) *reinterpret_cast<float4*>(v[p][i]) = __ldcg(reinterpret_cast<const float4*>(src));
+                else *reinterpret_cast<float2*>(v[p][i]) = __ldcg(reinterpret_cast<const float2*>(src));
+                f[p][i] = w[row * V + pt];
+            }
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (p0 + p < V)
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+#pragma unroll
+                    for (int e = 0; e < kE; ++e) acc[i][e] = fmaf(f[p][i], v[p][i][e], acc[i][e]);
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (q + i < nq) {
+            uint32_t* dst = reinterpret_cast<uint32_t*>(out_row(a, tok, head, q0 + q + i)) + lane * (kE / 2);
+#pragma unroll
+            for (int e = 0; e < kE / 2; ++e) dst[e] = pack16<kBf16>(acc[i][2 * e], acc[i][2 * e + 1]);
+        }
+}
+
+// The V parts of a split item's rows, joined by the slot whose part came last: per row the parts' common maximum and sum
+// and each part's weight (a thread per row, into the scratch), then the weighted sums, a warp over several rows.
+template <bool kBf16, int D>
+__device__ __noinline__ SlotSync join_parts(const AttnArgs& a, const float* part, int V, int rows, int tok, int head, float* w,
+                                            SlotSync sync) {
+    const int row = threadIdx.x & (kRows - 1), warp = row >> 5, batch = min(kRows, kScratch / 4 / V);
+    for (int q0 = 0; q0 < rows; q0 += batch) {
+        const int nq = min(batch, rows - q0);
+        if (q0 > 0) sync();
+        if (row < nq) {
+            float M = -INFINITY, L = 0.0f;
+#pragma unroll 1
+            for (int i0 = 0; i0 < V; i0 += 8) {
+                float2 v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    v[i] = i0 + i < V ? __ldcg(reinterpret_cast<const float2*>(part_buf<D>(part, i0 + i) + kRows * D) + q0 + row)
+                                      : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float Mn = fmaxf(M, v[i].x), Ms = finite_or_zero(Mn);
+                    L = fmaf(L, exp2_hw(M - Ms), exp2_hw(v[i].x - Ms) * v[i].y);
+                    M = Mn;
+                    if (i0 + i < V) w[row * V + i0 + i] = v[i].x;
+                }
+            }
+            const float inv = inverse_sum(L), Ms = finite_or_zero(M);
+            for (int i = 0; i < V; ++i) w[row * V + i] = exp2_hw(w[row * V + i] - Ms) * inv;
+            if (a.lse) *lse_row(a, tok, head, q0 + row) = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+        }
+        sync();
+        if (nq <= 8)
+            for (int q = 2 * warp; q < nq; q += 8) join_rows<kBf16, D, 2, 8>(a, part, w, V, q0, q, nq, tok, head);
+        else
+            for (int q = 8 * warp; q < nq; q += 32) join_rows<kBf16, D, 8, 2>(a, part, w, V, q0, q, nq, tok, head);
+    }
+    return sync;
+}
+
 template <bool kBf16, int D>
 __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_constant__ AttnArgs a) {
     using Sh = Shape<D>;
@@ -295,18 +410,20 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     __shared__ __align__(8) uint64_t bars[kBars];
     __shared__ Item items[kRing];
     __shared__ uint32_t tslot;
-    __shared__ int64_t warp_cost[kThreads / 32], head_cost;
-    // the threads' sums of costs, in the ring's last tile until the load warp has found its first item
-    int64_t* cost_end = reinterpret_cast<int64_t*>(sKV + (kNS - 1) * Sh::kTile);
+    // the threads' sums of costs and requests, in the ring's last tile until the load warp has found its first item
+    int64_t* cost_s = reinterpret_cast<int64_t*>(sKV + (kNS - 1) * Sh::kTile);
+    Req* req_s = reinterpret_cast<Req*>(cost_s + kThreads);
     __shared__ int last_flag[2];
     __shared__ float2 ml_s[2][kRows];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
     if (tid == 0) {
-        for (int s = 0; s < 2; ++s) {
+        for (int s = 0; s < 4; ++s) {
             mbar_init(&bars[kSFull + s], 1);
             mbar_init(&bars[kPFull + s], 4);
             mbar_init(&bars[kPvDone + s], 1);
+        }
+        for (int s = 0; s < 2; ++s) {
             mbar_init(&bars[kQFull + s], 1);
             mbar_init(&bars[kQEmpty + s], 1);
             mbar_init(&bars[kWg + s], 4);
@@ -322,6 +439,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == kLoadWarp && lane < 5) {
+        const CUtensorMap* map = lane == 0 ? &a.kmap : lane == 1 ? &a.vmap : &a.qmap[lane - 2];
+        asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+    }
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tslot)), "r"(512u));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -329,46 +450,35 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
 
     // The cost of all items of one head: each thread k consecutive requests, then a scan.  A request of several items is
     // summed by its warp.
-    const int k = (a.n_req + kThreads - 1) / kThreads;
-    {
-        int64_t mine = 0;
-        for (int i = 0; i < k; ++i) {
-            const int r = tid * k + i;
-            const Req q = load_req(a, r, blockIdx.x == 0);
-            const int m = (q.n + 2 * a.toks - 1) / (2 * a.toks);
-            if (m == 1) mine += kItemCost + item_units(a, q.kv, q.n, 0);
-            uint32_t big = __ballot_sync(0xffffffffu, m > 1);
-            while (big) {
-                const int src = __ffs(big) - 1;
-                big &= big - 1;
-                const int kv = __shfl_sync(0xffffffffu, q.kv, src), n = __shfl_sync(0xffffffffu, q.n, src),
-                          mm = __shfl_sync(0xffffffffu, m, src);
-                int64_t c = 0;
-                for (int j = lane; j < mm; j += 32) c += kItemCost + item_units(a, kv, n, j);
+    const int k = (a.n_req + kThreads - 1) / kThreads, per = 2 * a.toks;
+    int64_t mine = 0;
+    for (int i = 0; i < k; ++i) {
+        const int r = tid * k + i;
+        const Req q = load_req(a, r, blockIdx.x == 0);
+        if (k == 1) req_s[tid] = q;
+        if (q.n > 0 && q.n <= per) mine += kItemCost + item_units(a, q.kv, q.n, 0);
+        uint32_t big = __ballot_sync(0xffffffffu, q.n > per);
+        while (big) {
+            const int src = __ffs(big) - 1;
+            big &= big - 1;
+            const int kv = __shfl_sync(0xffffffffu, q.kv, src), n = __shfl_sync(0xffffffffu, q.n, src);
+            int64_t c = 0;
+            for (int j = lane; j < (n + per - 1) / per; j += 32) c += kItemCost + item_units(a, kv, n, j);
 #pragma unroll
-                for (int d = 16; d > 0; d >>= 1) c += __shfl_xor_sync(0xffffffffu, c, d);
-                if (lane == src) mine += c;
-            }
+            for (int d = 16; d > 0; d >>= 1) c += __shfl_xor_sync(0xffffffffu, c, d);
+            if (lane == src) mine += c;
         }
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int64_t t = __shfl_up_sync(0xffffffffu, mine, d);
-            if (lane >= d) mine += t;
-        }
-        if (lane == 31) warp_cost[warp] = mine;
-        __syncthreads();
-        for (int w = 0; w < warp; ++w) mine += warp_cost[w];
-        cost_end[tid] = mine;
-        if (tid == kThreads - 1) head_cost = mine;
     }
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t t = __shfl_up_sync(0xffffffffu, mine, d);
+        if (lane >= d) mine += t;
+    }
+    cost_s[tid] = mine;  // up to and with this thread, of its warp
     fence_before();
     __syncthreads();
     fence_after();
     const uint32_t tmem = tslot;
-    const int64_t total = head_cost * a.n_kv_heads;
-    const int64_t n_cta = min((int64_t)gridDim.x, max(total, (int64_t)1));
-    const int64_t B0 = blockIdx.x < n_cta ? blockIdx.x * total / n_cta : total;
-    const int64_t B1 = blockIdx.x < n_cta ? (blockIdx.x + 1) * total / n_cta : total;
     Waiter wait;
 
     if (warp >= kMmaWarp) {
@@ -377,38 +487,54 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         // ---- items, and the copies of their tiles
         uint32_t n_item = 0, n_load = 0, n_q[2] = {0, 0};
         int cached = -1;  // requests 32 cached .. are in the lanes
-        Req mine{0, 0, 0};
+        Req in_lane{0, 0, 0};
         auto get = [&](int r) {
             if ((r >> 5) != cached) {
                 cached = r >> 5;
-                mine = load_req(a, cached * 32 + lane, false);
+                in_lane = load_req(a, cached * 32 + lane, false);
             }
-            return Req{__shfl_sync(0xffffffffu, mine.q0, r & 31), __shfl_sync(0xffffffffu, mine.n, r & 31),
-                       __shfl_sync(0xffffffffu, mine.kv, r & 31)};
+            return Req{__shfl_sync(0xffffffffu, in_lane.q0, r & 31), __shfl_sync(0xffffffffu, in_lane.n, r & 31),
+                       __shfl_sync(0xffffffffu, in_lane.kv, r & 31)};
         };
+        // The warps' sums, one per lane, and their running sum: a head's cost at the last.  All heads' items in a row are cut
+        // into ranges of `range` units; this CTA's is [B0, B1).
+        int64_t upto = lane < kThreads / 32 ? cost_s[lane * 32 + 31] : 0;
+#pragma unroll
+        for (int d = 1; d < kThreads / 32; d <<= 1) {
+            const int64_t t = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += t;
+        }
+        const int64_t head_cost = __shfl_sync(0xffffffffu, upto, kThreads / 32 - 1), total = head_cost * a.n_kv_heads;
+        const int64_t range = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)1);
+        const int64_t B0 = min(total, blockIdx.x * range), B1 = min(total, B0 + range);
         int h = 0, r = 0, j = 0;
         int64_t p = B0;  // where item (h, r, j) starts
         if (B0 < B1) {
-            h = (int)(B0 / head_cost);
+            // the warp, then the thread, whose sum passes y, then the request, then its item
+            h = (int)quotient(B0, head_cost);
             const int64_t y = B0 - h * head_cost;
-            int lo = 0, hi = kThreads - 1;  // the first thread whose sum passes y
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (cost_end[mid] > y) hi = mid;
-                else lo = mid + 1;
+            const int w = __ffs(__ballot_sync(0xffffffffu, lane < kThreads / 32 && upto > y)) - 1;
+            int64_t at = __shfl_sync(0xffffffffu, upto, w) - cost_s[w * 32 + 31];
+            const int64_t in_warp = cost_s[w * 32 + lane];
+            const int t = __ffs(__ballot_sync(0xffffffffu, at + in_warp > y)) - 1;
+            const int64_t before = __shfl_sync(0xffffffffu, in_warp, (t + 31) & 31);
+            if (t > 0) at += before;
+            r = (w * 32 + t) * k;
+            if (k == 1) {
+                cached = w;
+                in_lane = req_s[w * 32 + lane];
             }
-            int64_t at = lo ? cost_end[lo - 1] : 0;
-            bool found = false;
-            for (r = lo * k; !found; ) {
+            for (bool found = false; !found;) {
                 const Req q = get(r);
-                const int m = (q.n + 2 * a.toks - 1) / (2 * a.toks);
-                for (int j0 = 0; j0 < m && !found; j0 += 32) {
-                    const int64_t c = j0 + lane < m ? kItemCost + item_units(a, q.kv, q.n, j0 + lane) : 0;
+                for (int j0 = 0; j0 * per < q.n && !found; j0 += 32) {
+                    const int64_t c = (j0 + lane) * per < q.n ? kItemCost + item_units(a, q.kv, q.n, j0 + lane) : 0;
                     int64_t s = c;
+                    if (q.n > per) {
 #pragma unroll
-                    for (int d = 1; d < 32; d <<= 1) {
-                        const int64_t t = __shfl_up_sync(0xffffffffu, s, d);
-                        if (lane >= d) s += t;
+                        for (int d = 1; d < 32; d <<= 1) {
+                            const int64_t up = __shfl_up_sync(0xffffffffu, s, d);
+                            if (lane >= d) s += up;
+                        }
                     }
                     const uint32_t past = __ballot_sync(0xffffffffu, at + s > y);
                     if (past) {
@@ -417,11 +543,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                         at += __shfl_sync(0xffffffffu, s - c, src);
                         found = true;
                     } else {
-                        at += __shfl_sync(0xffffffffu, s, 31);
+                        at += __shfl_sync(0xffffffffu, s, q.n > per ? 31 : 0);
                     }
                 }
-                if (!found) ++r;
-                if (r >= a.n_req) found = true;  // not reached: y is below the sum of all
+                if (!found && ++r >= a.n_req) found = true;  // not reached: y is below the sum of all
             }
             p = h * head_cost + at;
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the tile may be copied over
@@ -477,9 +602,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         int turn = 0;
         while (p < B1 && wait.ok) {
             const Req q = get(r);
-            const int per = 2 * a.toks, m = (q.n + per - 1) / per;
-            if (j >= m) {  // the next request with a token, in the next head if need be
-                const uint32_t more = __ballot_sync(0xffffffffu, mine.n > 0) & ~((2u << (r & 31)) - 1u);
+            if (j * per >= q.n) {  // the next request with a token, in the next head if need be
+                const uint32_t more = __ballot_sync(0xffffffffu, in_lane.n > 0) & ~((2u << (r & 31)) - 1u);
                 r = more ? (r & ~31) + __ffs(more) - 1 : (r & ~31) + 32;
                 j = 0;
                 if (r >= a.n_req) {
@@ -487,7 +611,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                     ++h;
                     if (h >= a.n_kv_heads) break;
                 }
-                if (get(r).n == 0) j = 1;  // a fresh group of 32 starts on an empty one
                 continue;
             }
             Item it;
@@ -512,8 +635,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             it.first = blockIdx.x;
             it.n_parts = 1;
             if (it.nu < units) {
-                it.first = (int)(((s + 1) * n_cta - 1) / total);
-                it.n_parts = (int)(((s + units) * n_cta - 1) / total) - it.first + 1;
+                it.first = (int)quotient(s, range);
+                it.n_parts = (int)quotient(s + units - 1, range) - it.first + 1;
             }
             it.slot = it.ntok > a.toks ? 2 : turn;
             if (it.slot < 2) turn ^= 1;
@@ -558,31 +681,49 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     } else if (warp == kMmaWarp) {
         // ---- the products, by one thread
         if (lane == 0) {
-            uint32_t n_unit = 0, n_q[2] = {0, 0}, n_p[2] = {0, 0};
-            struct {
-                bool on, acc, release;
-                uint32_t load;
-            } pend[2] = {{false, false, false, 0}, {false, false, false, 0}};  // products with V still to be issued
+            // Scores go to S0 and S1: a pair's slots to their own, a single slot's units to both in turn, so that the next
+            // unit's scores are computed under this one's softmax.  The product with V of the P in Sb, still to be issued:
+            // bit b of `on`, its tile's load and what it is (kSlot: slot and parity of the slot's unit, ...); older: which of
+            // the two came first.  (Two of everything, selected: an indexed array would be in local memory.)
+            enum { kSlot = 3, kPhase = 4, kAcc = 8, kRelease = 16 };
+            uint32_t n_unit = 0, n_q0 = 0, n_q1 = 0, n_s0 = 0, n_s1 = 0;
+            uint32_t on = 0, older = 0, turn = 0, load0 = 0, load1 = 0, what0 = 0, what1 = 0;
             const uint32_t id_s = idesc(kBf16, kKeys, false), id_o = idesc(kBf16, D, true);
             auto commit = [&](uint64_t* b) {
                 asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
             };
-            auto values = [&](int s) {
-                const uint32_t st = pend[s].load % kNS, use = pend[s].load / kNS;
-                wait.thread(&bars[kPFull + s], n_p[s]++);
+            auto first_pending = [&]() { return on == 3u ? older : on >> 1; };
+            auto values = [&]() {  // issues the older of the pending products
+                const uint32_t b = first_pending(), load = b ? load1 : load0, what = b ? what1 : what0;
+                const uint32_t st = load % kNS, use = load / kNS;
+                wait.thread(&bars[kPFull + (what & kSlot)], what & kPhase ? 1u : 0u);
                 wait.thread(&bars[kKvFull + st], use);
-                pend[s].on = false;
+                on &= ~(1u << b);
                 if (!wait.ok) return;
                 fence_after();
                 const uint64_t dv = desc_v(smem_u32(sKV) + st * Sh::kTile);
-                const uint32_t o = tmem + kO0 + s * D, pp = tmem + kS0 + s * kKeys;
+                const uint32_t o = tmem + kO0 + (what & kSlot) / 2 * D, pp = tmem + kS0 + b * kKeys;
 #pragma unroll
                 for (int i = 0; i < kKeys / 16; ++i)
                     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
                                  "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(o),
-                                 "r"(pp + 8 * i), "l"(dv + 128 * i), "r"(id_o), "r"((pend[s].acc || i > 0) ? 1u : 0u));
-                commit(&bars[kPvDone + s]);
-                if (pend[s].release) commit(&bars[kKvEmpty + st]);
+                                 "r"(pp + 8 * i), "l"(dv + 128 * i), "r"(id_o), "r"(i > 0 ? 1u : what & kAcc));
+                commit(&bars[kPvDone + (what & kSlot)]);
+                if (what & kRelease) commit(&bars[kKvEmpty + st]);
+            };
+            // Waits for a tile of keys; meanwhile a probability tile that gets ready is used.
+            auto wait_keys = [&](uint32_t st, uint32_t use) {
+                const uint32_t bar = smem_u32(&bars[kKvFull + st]);
+                if (!wait.ok || mbar_test(bar, use & 1u)) return;
+                const unsigned long long t0 = global_ns();
+                for (uint32_t i = 1; !mbar_test(bar, use & 1u); ++i) {
+                    if (on) {
+                        const uint32_t what = first_pending() ? what1 : what0;
+                        if (mbar_test(smem_u32(&bars[kPFull + (what & kSlot)]), what & kPhase ? 1u : 0u)) values();
+                    }
+                    if ((i & 63u) == 0 && global_ns() - t0 > kWaitNs) wait.ok = false;
+                    if (!wait.ok) return;
+                }
             };
             for (uint32_t n_item = 0; wait.ok; ++n_item) {
                 wait.thread(&bars[kItemFull + n_item % kRing], n_item / kRing);
@@ -594,40 +735,49 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 mbar_arrive(&bars[kItemEmpty + n_item % kRing]);
                 for (int u = 0; u < nu && wait.ok; ++u, ++n_unit) {
                     const uint32_t load = 2 * n_unit, st = load % kNS, use = load / kNS;
-                    // the last products of a pair go in order, whichever slot comes next
-                    if (slot == 1 && pend[0].on && pend[1].on) values(0);
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        if (slot != 2 && slot != s) continue;
-                        const bool last = slot != 2 || s == 1;  // of this tile's users
-                        if (pend[s].on) values(s);
-                        if (u == 0) wait.thread(&bars[kQFull + s], n_q[s]++);
-                        wait.thread(&bars[kKvFull + st], use);
-                        if (!wait.ok) continue;
+                    wait_keys(st, use);
+                    const uint32_t b0 = slot == 2 ? 0 : turn, b1 = slot == 2 ? 1 : turn;
+#pragma unroll 1
+                    for (uint32_t b = b0; b <= b1; ++b) {
+                        const uint32_t sl = slot == 2 ? b : slot;
+                        while ((on >> b & 1u) && wait.ok) values();
+                        if (u == 0) {
+                            wait.thread(&bars[kQFull + sl], sl ? n_q1 : n_q0);
+                            n_q0 += sl == 0;
+                            n_q1 += sl;
+                        }
+                        if (!wait.ok) break;
                         fence_after();
-                        const uint64_t dq = desc_k(smem_u32(sQ) + s * Sh::kTile), dk = desc_k(smem_u32(sKV) + st * Sh::kTile);
+                        const uint64_t dq = desc_k(smem_u32(sQ) + sl * Sh::kTile), dk = desc_k(smem_u32(sKV) + st * Sh::kTile);
+                        const uint32_t d = tmem + kS0 + b * kKeys;
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) {
                             const uint32_t off = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
                             asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                                         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem + kS0 + s * kKeys),
+                                         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
                                          "l"(dq + off), "l"(dk + off), "r"(id_s), "r"(i > 0 ? 1u : 0u));
                         }
-                        commit(&bars[kSFull + s]);
-                        if (last) commit(&bars[kKvEmpty + st]);
-                        if (u == nu - 1) commit(&bars[kQEmpty + s]);
-                        pend[s].on = true;
-                        pend[s].acc = u > 0;
-                        pend[s].release = last;
-                        pend[s].load = load + 1;
+                        const uint32_t n = sl ? n_s1 : n_s0, sn = 2 * sl + (n & 1u);
+                        n_s0 += sl == 0;
+                        n_s1 += sl;
+                        commit(&bars[kSFull + sn]);
+                        if (b == b1) commit(&bars[kKvEmpty + st]);
+                        if (u == nu - 1) commit(&bars[kQEmpty + sl]);
+                        older = on ? 1 - b : b;
+                        on |= 1u << b;
+                        const uint32_t what = sn | (n & 2u ? kPhase : 0) | (u > 0 ? kAcc : 0) | (b == b1 ? kRelease : 0);
+                        if (b) {
+                            load1 = load + 1;
+                            what1 = what;
+                        } else {
+                            load0 = load + 1;
+                            what0 = what;
+                        }
                     }
-                    if (slot == 0 && pend[1].on) values(1);  // an earlier item's last
-                    if (slot == 1 && pend[0].on) values(0);
+                    if (slot != 2) turn ^= 1u;
                 }
             }
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-                if (pend[s].on && wait.ok) values(s);
+            while (on && wait.ok) values();
             if (!wait.ok) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
             commit(&bars[kDrain]);
             mbar_wait(smem_u32(&bars[kDrain]), 0);
@@ -638,13 +788,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         // ---- softmax of slot s; this thread's row of tensor memory is lane row
         const int s = warp >> 2, row = tid & (kRows - 1);
         const uint32_t lane_at = (uint32_t)(32 * (warp & 3)) << 16;
-        const uint32_t tS = tmem + kS0 + s * kKeys + lane_at, tO = tmem + kO0 + s * D + lane_at;
-        uint32_t n_s = 0, n_wg = 0, n_unit = 0;
-        auto wg_sync = [&]() {
-            warp_arrive(&bars[kWg + s]);
-            wait.warp(&bars[kWg + s], n_wg++);
-        };
-        for (uint32_t n_item = 0; wait.ok; ++n_item) {
+        const uint32_t tO = tmem + kO0 + s * D + lane_at;
+        uint32_t n_s = 0, n_unit = 0, turn = 0;  // units of this slot, of all; the S of the next single unit
+        SlotSync wg_sync{&bars[kWg + s], 0, {}};
+        for (uint32_t n_item = 0; wait.ok && wg_sync.wait.ok; ++n_item) {
             const uint32_t ring = n_item % kRing;
             wait.warp(&bars[kItemFull + ring], n_item / kRing);
             if (!wait.ok) break;
@@ -653,6 +800,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             if (it.slot != 2 && it.slot != s) {
                 warp_arrive(&bars[kItemEmpty + ring]);
                 n_unit += it.nu;
+                turn ^= it.nu & 1;
                 continue;
             }
             const int half = it.slot == 2 ? s : 0;
@@ -675,11 +823,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             for (int u = 0; u < it.nu; ++u, ++n_unit, ++n_s) {
                 const int t0 = (it.u0 + u) * kKeys;
                 const bool full = t0 >= all0 && t0 + kKeys <= all1;
-                wait.warp(&bars[kSFull + s], n_s);
+                const uint32_t sn = 2 * s + (n_s & 1), tS = tmem + kS0 + (it.slot == 2 ? s : turn) * kKeys + lane_at;
+                turn ^= it.slot != 2;
+                wait.warp(&bars[kSFull + sn], n_s >> 1);
                 fence_after();
                 if (busy) {
                     auto rescale = [&](float f) {
-                        wait.warp(&bars[kPvDone + s], n_s - 1);
+                        wait.warp(&bars[kPvDone + (sn ^ 1)], (n_s - 1) >> 1);
                         fence_after();
 #pragma unroll
                         for (int c = 0; c < D; c += 16) {
@@ -724,15 +874,42 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 fence_before();
-                warp_arrive(&bars[kPFull + s]);
+                warp_arrive(&bars[kPFull + sn]);
             }
             // ---- the end of the item: O and l of this part
             if (it.nu > 0) {
-                wait.warp(&bars[kPvDone + s], n_s - 1);
+                wait.warp(&bars[kPvDone + 2 * s + ((n_s - 1) & 1)], (n_s - 1) >> 1);
                 fence_after();
             }
             const bool poison = *reinterpret_cast<volatile int32_t*>(&items[ring].poison) != 0;
-            auto load_o = [&](int c, float* o) {  // columns c .. c + 31, with the values that were replaced
+            if (poison && busy && it.nu > 0) {
+                // the values that were replaced, added to the rows that see them
+#pragma unroll 1
+                for (int c = 0; c < D; c += 16) {
+                    uint32_t x[16];
+                    tmem_ld16(tO + c, x);
+                    tmem_wait_ld();
+#pragma unroll 1
+                    for (int u = it.u0; u < it.u0 + it.nu; ++u) {
+                        const int w0 = u * kKeys + (copy << (7 - it.rep_log)), w1 = w0 + (kKeys >> it.rep_log);
+#pragma unroll 1
+                        for (int key = max(k0, w0); key < min(k1, w1); ++key) {
+                            const int id = a.table[(int64_t)it.r * a.ld_table + (key >> a.bs_log)];
+                            if (id < 0 || id >= a.n_blocks) continue;
+                            const uint16_t* v = a.v + id * a.ld_block + (key & ((1 << a.bs_log) - 1)) * a.ld_token + it.h * a.ld_head + c;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const uint32_t w = v[i];
+                                if (not_finite<kBf16>(w)) x[i] = __float_as_uint(__uint_as_float(x[i]) + value16<kBf16>((uint16_t)w));
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    tmem_st16(tO + c, x);
+                }
+                tmem_wait_st();
+            }
+            auto load_o = [&](int c, float* o) {  // columns c .. c + 31
                 uint32_t x[32];
                 if (it.nu > 0) {
                     tmem_ld32(tO + c, x);
@@ -740,29 +917,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 }
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = it.nu > 0 ? __uint_as_float(x[i]) : 0.0f;
-                if (poison && live)
-                    for (int u = it.u0; u < it.u0 + it.nu; ++u) {
-                        const int w0 = u * kKeys + (copy << (7 - it.rep_log)), w1 = w0 + (kKeys >> it.rep_log);
-                        for (int key = max(k0, w0); key < min(k1, w1); ++key) {
-                            const int id = a.table[(int64_t)it.r * a.ld_table + (key >> a.bs_log)];
-                            if (id < 0 || id >= a.n_blocks) continue;
-                            const uint16_t* v = a.v + id * a.ld_block + (key & ((1 << a.bs_log) - 1)) * a.ld_token + it.h * a.ld_head + c;
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                const uint32_t w = v[i];
-                                if (not_finite<kBf16>(w)) o[i] += value16<kBf16>((uint16_t)w);
-                            }
-                        }
-                    }
             };
-            const int64_t head = (int64_t)it.h * a.group;
-            auto out_at = [&](int q) {  // of row q of the slot
-                return a.out + (int64_t)(it.tok + tok0 + q / a.group) * a.out_ld_token + (head + q % a.group) * a.out_ld_head;
-            };
-            auto lse_at = [&](int q) { return a.lse + (int64_t)(it.tok + tok0 + q / a.group) * a.n_heads + head + q % a.group; };
+            const int head = it.h * a.group, tok = it.tok + tok0;
             const bool whole = it.n_parts == 1;
-            const int part = blockIdx.x - it.first;
-            float* buf = part_buf<D>(a, blockIdx.x, (part == 0 ? 2 : 0) + half);
+            // parts of half 0, then those of half 1, of all CTAs
+            float* part0 = a.parts + (size_t)(half * 2 * gridDim.x + 2 * it.first + 1) * kPartFloats<D>;
+            float* buf = part_buf<D>(part0, blockIdx.x - it.first);
             float* scratch = reinterpret_cast<float*>(sScratch + s * kScratch);
             if (it.rep_log > 0) {
                 // Copies of the rows: their common maximum and sum, then the weighted sums of their O through the scratch
@@ -780,7 +940,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 const float w = exp2_hw(m - Ms), f = !whole ? w : L == 0.0f ? 0.0f : w / L;
                 if (copy == 0 && live) {
                     if (!whole) *reinterpret_cast<float2*>(buf + kRows * D + 2 * rr) = make_float2(M, L);
-                    else if (a.lse) *lse_at(rr) = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+                    else if (a.lse) *lse_row(a, tok, head, rr) = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
                 }
                 const int width = used <= 32 ? min(D, 128) : used <= 64 ? 64 : 32, groups = width / 4;
                 const int g_log = 31 - __clz(groups);
@@ -806,7 +966,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                             const float4 v = reinterpret_cast<const float4*>(scratch)[at * groups + (gq ^ (at & 7))];
                             t = make_float4(t.x + v.x, t.y + v.y, t.z + v.z, t.w + v.w);
                         }
-                        if (whole) *reinterpret_cast<uint2*>(out_at(q) + c0 + 4 * gq) = make_uint2(pack16<kBf16>(t.x, t.y), pack16<kBf16>(t.z, t.w));
+                        if (whole) *reinterpret_cast<uint2*>(out_row(a, tok, head, q) + c0 + 4 * gq) = make_uint2(pack16<kBf16>(t.x, t.y), pack16<kBf16>(t.z, t.w));
                         else *reinterpret_cast<float4*>(buf + q * D + c0 + 4 * gq) = t;
                     }
                     if (c0 + width < D) wg_sync();
@@ -814,7 +974,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             } else if (whole) {
                 const float inv = inverse_sum(l);
                 if (busy) {
-                    uint16_t* dst = out_at(rr);
+                    uint16_t* dst = out_row(a, tok, head, rr);
 #pragma unroll
                     for (int c = 0; c < D; c += 32) {
                         float o[32];
@@ -827,7 +987,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                                                pack16<kBf16>(o[i + 4] * inv, o[i + 5] * inv), pack16<kBf16>(o[i + 6] * inv, o[i + 7] * inv));
                         }
                     }
-                    if (live && a.lse) *lse_at(rr) = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+                    if (live && a.lse) *lse_row(a, tok, head, rr) = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
                 }
             } else if (busy) {
 #pragma unroll
@@ -855,59 +1015,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             }
             wg_sync();
             if (*reinterpret_cast<volatile int*>(&last_flag[s]) == 0) continue;
-            // The last part to come: per row the parts' common maximum and sum and each part's weight (into the scratch, a
-            // thread per row), then the weighted sums, a warp over eight rows at a time.
-            const int V = it.n_parts, batch = min(kRows, kScratch / 4 / V);
-            auto part_at = [&](int i) { return part_buf<D>(a, it.first + i, (i == 0 ? 2 : 0) + half); };
-            for (int q0 = 0; q0 < rows; q0 += batch) {
-                const int nq = min(batch, rows - q0);
-                if (q0 > 0) wg_sync();
-                if (row < nq) {
-                    float M = -INFINITY, L = 0.0f;
-#pragma unroll 8
-                    for (int i = 0; i < V; ++i) {
-                        const float2 v = __ldcg(reinterpret_cast<const float2*>(part_at(i) + kRows * D) + q0 + row);
-                        const float Mn = fmaxf(M, v.x), Ms = finite_or_zero(Mn);
-                        L = fmaf(L, exp2_hw(M - Ms), exp2_hw(v.x - Ms) * v.y);
-                        M = Mn;
-                        scratch[row * V + i] = v.x;
-                    }
-                    const float inv = inverse_sum(L), Ms = finite_or_zero(M);
-                    for (int i = 0; i < V; ++i) scratch[row * V + i] = exp2_hw(scratch[row * V + i] - Ms) * inv;
-                    if (a.lse) *lse_at(q0 + row) = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
-                }
-                wg_sync();
-                for (int q = (warp & 3) * 8; q < nq; q += 32) {
-                    constexpr int kE = D / 32;
-                    float acc[8][kE];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-#pragma unroll
-                        for (int e = 0; e < kE; ++e) acc[i][e] = 0.0f;
-#pragma unroll 2
-                    for (int pt = 0; pt < V; ++pt) {
-                        const float* src = part_at(pt) + (q0 + q) * D + lane * kE;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            if (q + i >= nq) break;
-                            const float w = scratch[(q + i) * V + pt];
-                            float v[kE];
-                            if (D == 128) *reinterpret_cast<float4*>(v) = __ldcg(reinterpret_cast<const float4*>(src + i * D));
-                            else *reinterpret_cast<float2*>(v) = __ldcg(reinterpret_cast<const float2*>(src + i * D));
-#pragma unroll
-                            for (int e = 0; e < kE; ++e) acc[i][e] = fmaf(w, v[e], acc[i][e]);
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (q + i >= nq) break;
-                        uint32_t* dst = reinterpret_cast<uint32_t*>(out_at(q0 + q + i)) + lane * (kE / 2);
-#pragma unroll
-                        for (int e = 0; e < kE / 2; ++e) dst[e] = pack16<kBf16>(acc[i][2 * e], acc[i][2 * e + 1]);
-                    }
-                }
-            }
+            wg_sync = join_parts<kBf16, D>(a, part0, it.n_parts, rows, tok, head, scratch, wg_sync);
         }
+        wait.ok &= wg_sync.wait.ok;
         if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
     }
     fence_before();
