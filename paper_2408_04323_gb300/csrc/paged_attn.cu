@@ -49,7 +49,7 @@ constexpr int kRows = 128;       // rows of a slot: the MMA's M and the TMEM lan
 constexpr int kKeys = 128;       // keys of a tile
 constexpr int kThreads = 384;      // three warpgroups: the two softmax ones take registers from the third
 constexpr int kSoftmaxRegs = 200, kOtherRegs = 104;  // 2 * 200 + 104 = 3 * 168, what the block is launched with
-constexpr int kMmaWarp = 8, kLoadWarp = 9;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kValueWarp = 10;
 constexpr int kRing = 4;         // items handed from the load warp to the others
 constexpr int kItemCost = 1;     // an item's start and end, in units
 constexpr int kBufs = 4;         // part buffers of a CTA (see part_buf)
@@ -232,9 +232,6 @@ __device__ __forceinline__ const float* part_buf(const float* first, int i) {
 // Bounded waits that pass at once after the first that gave up, so that every role runs to its end.
 struct Waiter {
     bool ok = true;
-    __device__ __forceinline__ void thread(uint64_t* b, uint32_t use) {
-        if (ok) ok = mbar_wait(smem_u32(b), use & 1u);
-    }
     __device__ __forceinline__ void warp(uint64_t* b, uint32_t use) {
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(b), use & 1u));
     }
@@ -296,6 +293,99 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, int ch0, bool full, in
     l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
     tmem_wait_st();
 }
+
+// One step of a product (16 of its inner dimension), both operands in shared memory, or A in tensor memory.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t da, uint64_t db, uint32_t id, bool acc) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(da), "l"(db), "r"(id), "r"((uint32_t)acc));
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t ta, uint64_t db, uint32_t id, bool acc) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(ta), "l"(db), "r"(id), "r"((uint32_t)acc));
+}
+
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
+// A warp that copies the tiles of keys or of values, loads `at`, at + 2, .. of the ring.  One lane issues (a copy takes its
+// operands from the warp's uniform registers: 32 lanes with a copy each took 66 cycles per copy).  The lanes hold the
+// block ids of 32 pages, four tiles' at 16 tokens a block, and those of the next 32 in flight.
+template <int D>
+struct TileLoader {
+    const AttnArgs& a;
+    const CUtensorMap* map;
+    uint64_t* bars;
+    uint32_t tiles;  // shared address of the ring
+    uint32_t at;
+    int box, n_page, page_log;  // tokens of a page, pages of a tile
+    int group;                  // ids: of pages 32 group ..
+    int ids, ids_next;
+    bool bad = false;
+    static constexpr int kNone = INT32_MIN;
+    __device__ __forceinline__ TileLoader(const AttnArgs& a_, const CUtensorMap* m, uint64_t* b, uint32_t t, uint32_t first)
+        : a(a_), map(m), bars(b), tiles(t), at(first) {
+        page_log = a.bs_log < 7 ? 7 - a.bs_log : 0;
+        n_page = 1 << page_log;
+        box = kKeys >> page_log;
+    }
+    // This lane's id of the pages of group g, -1 if no row sees any of its tokens.
+    __device__ __forceinline__ int fetch(const Item& it, int g) const {
+        const int64_t key = ((int64_t)g * 32 + (threadIdx.x & 31)) * box;
+        return key < it.end && key + box > it.begin ? __ldg(a.table + (int64_t)it.r * a.ld_table + (key >> a.bs_log)) : kNone;
+    }
+    __device__ __forceinline__ void use(int raw) {
+        const bool out = raw < 0 || raw >= a.n_blocks;
+        bad |= out && raw != kNone;
+        ids = raw == kNone ? -1 : out ? (int)a.n_blocks : raw;  // past the end: the copy writes zeros
+    }
+    __device__ __forceinline__ void begin(const Item& it) {
+        group = (it.u0 << page_log) >> 5;
+        use(fetch(it, group));
+        ids_next = fetch(it, group + 1);
+    }
+    __device__ __forceinline__ void tile(const Item& it, int u, Waiter& wait) {
+        constexpr int kNS = Shape<D>::kStages;
+        const int page = u << page_log;
+        if (page >> 5 != group) {
+            group = page >> 5;
+            use(ids_next);
+            ids_next = fetch(it, group + 1);
+        }
+        const uint32_t st = at % kNS, n_use = at / kNS, bar = smem_u32(&bars[kKvFull + st]);
+        if (n_use > 0) wait.warp(&bars[kKvEmpty + st], n_use - 1);
+        if (!wait.ok) return;
+        at += 2;
+        const uint32_t here = __ballot_sync(0xffffffffu, ids >= 0) >> (page & 31), n = __popc(here & ((2u << (n_page - 1)) - 1u));
+        const bool one = elect_one();
+        if (one)
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n * box * (D * 2)) : "memory");
+        uint32_t dst = tiles + st * Shape<D>::kTile;
+        const int within = (u * kKeys) & ((1 << a.bs_log) - 1);
+#pragma unroll 4
+        for (int i = 0; i < n_page; ++i, dst += box * 128) {
+            const int id = __shfl_sync(0xffffffffu, ids, (page & 31) + i);
+            if (one && id >= 0) {
+#pragma unroll
+                for (int half = 0; half < D / 64; ++half)
+                    asm volatile(
+                        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
+                        "%4, %5}], [%6];" ::"r"(dst + half * kHalf),
+                        "l"(map), "r"(half * 64), "r"(it.h), "r"(within), "r"(id), "r"(bar)
+                        : "memory");
+            }
+        }
+        __syncwarp();
+    }
+    // After a wait that gave up: the copies in flight land before the block ends.
+    __device__ __forceinline__ void drain() const {
+        constexpr uint32_t kNS = Shape<D>::kStages;
+        for (uint32_t i = at & 1u; i < at; i += 2)
+            if (i + kNS >= at) mbar_wait(smem_u32(&bars[kKvFull + i % kNS]), (i / kNS) & 1u);
+    }
+};
 
 // A slot's four warps meet (bounded): warps of one that gave up do not hold the others.
 struct SlotSync {
@@ -415,7 +505,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     Req* req_s = reinterpret_cast<Req*>(cost_s + kThreads);
     __shared__ int last_flag[2];
     __shared__ float2 ml_s[2][kRows];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // (the same for all lanes, and by the shuffle known to be)
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
     if (tid == 0) {
         for (int s = 0; s < 4; ++s) {
@@ -430,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         }
         for (int s = 0; s < kRing; ++s) {
             mbar_init(&bars[kItemFull + s], 1);
-            mbar_init(&bars[kItemEmpty + s], 9);  // eight softmax warps and the product thread
+            mbar_init(&bars[kItemEmpty + s], 10);  // eight softmax warps, the product thread and the value warp
         }
         mbar_init(&bars[kDrain], 1);
         for (int s = 0; s < kNS; ++s) {
@@ -485,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kLoadWarp) {
         // ---- items, and the copies of their tiles
-        uint32_t n_item = 0, n_load = 0, n_q[2] = {0, 0};
+        uint32_t n_item = 0, n_q[2] = {0, 0};
         int cached = -1;  // requests 32 cached .. are in the lanes
         Req in_lane{0, 0, 0};
         auto get = [&](int r) {
@@ -552,51 +643,27 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the tile may be copied over
             __syncwarp();
         }
-        const int bs = 1 << a.bs_log, box = min(bs, kKeys), n_page = kKeys / box;
-        const int page = lane / kNH, half = lane % kNH;
-        bool bad_id = false;
-        // the block of this lane's page of tile u, -1 if no row sees any of it
-        auto page_id = [&](const Item& it, int u) {
-            const int key = u * kKeys + page * box;
-            if (page >= n_page || key >= it.end || key + box <= it.begin) return -1;
-            const int id = __ldg(a.table + (int64_t)it.r * a.ld_table + (key >> a.bs_log));
-            if (id >= 0 && id < a.n_blocks) return id;
-            bad_id = true;
-            return (int)a.n_blocks;  // past the end: the copy writes zeros
-        };
-        auto load_tile = [&](const CUtensorMap* map, int u, int id, int head) {
-            const uint32_t st = n_load % kNS, use = n_load / kNS;
-            if (use > 0) wait.warp(&bars[kKvEmpty + st], use - 1);
-            if (!wait.ok) return;
-            const uint32_t n = __popc(__ballot_sync(0xffffffffu, id >= 0));
-            const uint32_t bar = smem_u32(&bars[kKvFull + st]);
-            if (lane == 0)
-                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n * box * 128u) : "memory");
-            __syncwarp();
-            if (id >= 0)
-                asm volatile(
-                    "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, "
-                    "%5}], [%6];" ::"r"(smem_u32(sKV) + st * Sh::kTile + half * kHalf + page * box * 128),
-                    "l"(map), "r"(half * 64), "r"(head), "r"((u * kKeys) & (bs - 1)), "r"(id), "r"(bar)
-                    : "memory");
-            ++n_load;
-        };
+        TileLoader<D> keys(a, &a.kmap, bars, smem_u32(sKV), 0);
         auto load_q = [&](const Item& it, int s, int tok, int head) {
             if (n_q[s] > 0) wait.warp(&bars[kQEmpty + s], n_q[s] - 1);
             if (!wait.ok) return;
             const uint32_t bar = smem_u32(&bars[kQFull + s]);
             const int rows = kRows >> it.rep_log, boxed = rows / a.group * a.group, copies = 1 << it.rep_log;
-            if (lane == 0)
+            const CUtensorMap* map = &a.qmap[it.rep_log];
+            if (elect_one()) {
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
                              "r"((uint32_t)(copies * kNH * boxed * 128))
                              : "memory");
+                for (int c = 0; c < copies; ++c)
+#pragma unroll
+                    for (int half = 0; half < kNH; ++half)
+                        asm volatile(
+                            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, "
+                            "%3, %4}], [%5];" ::"r"(smem_u32(sQ) + s * Sh::kTile + half * kHalf + c * rows * 128),
+                            "l"(map), "r"(half * 64), "r"(head * a.group), "r"(tok), "r"(bar)
+                            : "memory");
+            }
             __syncwarp();
-            if (page < copies)
-                asm volatile(
-                    "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
-                    "%4}], [%5];" ::"r"(smem_u32(sQ) + s * Sh::kTile + half * kHalf + page * rows * 128),
-                    "l"(&a.qmap[it.rep_log]), "r"(half * 64), "r"(head * a.group), "r"(tok), "r"(bar)
-                    : "memory");
             ++n_q[s];
         };
         int turn = 0;
@@ -649,17 +716,14 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             }
             __syncwarp();
             ++n_item;
-            int id = it.nu > 0 ? page_id(it, it.u0) : -1;
+            if (it.nu > 0) keys.begin(it);
             for (int u = 0; u < it.nu && wait.ok; ++u) {
-                const int id_next = u + 1 < it.nu ? page_id(it, it.u0 + u + 1) : -1;
-                load_tile(&a.kmap, it.u0 + u, id, h);
+                keys.tile(it, it.u0 + u, wait);
                 if (u == 0) {
 #pragma unroll
                     for (int sl = 0; sl < 2; ++sl)
                         if (it.slot == 2 || it.slot == sl) load_q(it, sl, it.tok + (it.slot == 2 ? sl * a.toks : 0), h);
                 }
-                load_tile(&a.vmap, it.u0 + u, id, h);
-                id = id_next;
             }
         }
         if (wait.ok && n_item >= kRing) wait.warp(&bars[kItemEmpty + n_item % kRing], n_item / kRing - 1);
@@ -667,20 +731,35 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             items[n_item % kRing].stop = 1;
             mbar_arrive(&bars[kItemFull + n_item % kRing]);
         }
-        if (bad_id) atomicOr(a.err, SCOOT_DEVERR_INDEX);
+        if (keys.bad) atomicOr(a.err, SCOOT_DEVERR_INDEX);
         __syncwarp();
         if (!wait.ok) {
             // gave up: the copies in flight land before the block ends
             if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
-            for (uint32_t i = n_load > kNS ? n_load - kNS : 0; i < n_load; ++i)
-                mbar_wait(smem_u32(&bars[kKvFull + i % kNS]), (i / kNS) & 1u);
+            keys.drain();
 #pragma unroll
             for (int s = 0; s < 2; ++s)
                 if (n_q[s] > 0) mbar_wait(smem_u32(&bars[kQFull + s]), (n_q[s] - 1) & 1u);
         }
+    } else if (warp == kValueWarp) {
+        // ---- the copies of the values
+        TileLoader<D> vals(a, &a.vmap, bars, smem_u32(sKV), 1);
+        for (uint32_t n_item = 0; wait.ok; ++n_item) {
+            wait.warp(&bars[kItemFull + n_item % kRing], n_item / kRing);
+            if (!wait.ok) break;
+            const Item it = items[n_item % kRing];
+            if (it.stop) break;
+            warp_arrive(&bars[kItemEmpty + n_item % kRing]);
+            if (it.nu > 0) vals.begin(it);
+            for (int u = 0; u < it.nu && wait.ok; ++u) vals.tile(it, it.u0 + u, wait);
+        }
+        if (!wait.ok) {
+            if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
+            vals.drain();
+        }
     } else if (warp == kMmaWarp) {
-        // ---- the products, by one thread
-        if (lane == 0) {
+        // ---- the products.  The warp runs as one, so that the operands stay in its uniform registers, and one lane issues.
+        {
             // Scores go to S0 and S1: a pair's slots to their own, a single slot's units to both in turn, so that the next
             // unit's scores are computed under this one's softmax.  The product with V of the P in Sb, still to be issued:
             // bit b of `on`, its tile's load and what it is (kSlot: slot and parity of the slot's unit, ...); older: which of
@@ -692,47 +771,49 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             auto commit = [&](uint64_t* b) {
                 asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
             };
+            auto ready = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(bar, parity)) != 0; };
             auto first_pending = [&]() { return on == 3u ? older : on >> 1; };
             auto values = [&]() {  // issues the older of the pending products
                 const uint32_t b = first_pending(), load = b ? load1 : load0, what = b ? what1 : what0;
                 const uint32_t st = load % kNS, use = load / kNS;
-                wait.thread(&bars[kPFull + (what & kSlot)], what & kPhase ? 1u : 0u);
-                wait.thread(&bars[kKvFull + st], use);
+                wait.warp(&bars[kPFull + (what & kSlot)], what & kPhase ? 1u : 0u);
+                wait.warp(&bars[kKvFull + st], use);
                 on &= ~(1u << b);
                 if (!wait.ok) return;
                 fence_after();
+                if (elect_one()) {
                 const uint64_t dv = desc_v(smem_u32(sKV) + st * Sh::kTile);
                 const uint32_t o = tmem + kO0 + (what & kSlot) / 2 * D, pp = tmem + kS0 + b * kKeys;
 #pragma unroll
                 for (int i = 0; i < kKeys / 16; ++i)
-                    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(o),
-                                 "r"(pp + 8 * i), "l"(dv + 128 * i), "r"(id_o), "r"(i > 0 ? 1u : what & kAcc));
+                    mma_ts(o, pp + 8 * i, dv + 128 * i, id_o, i > 0 || (what & kAcc));
                 commit(&bars[kPvDone + (what & kSlot)]);
                 if (what & kRelease) commit(&bars[kKvEmpty + st]);
+                }
+                __syncwarp();
             };
             // Waits for a tile of keys; meanwhile a probability tile that gets ready is used.
             auto wait_keys = [&](uint32_t st, uint32_t use) {
                 const uint32_t bar = smem_u32(&bars[kKvFull + st]);
-                if (!wait.ok || mbar_test(bar, use & 1u)) return;
+                if (!wait.ok || ready(bar, use & 1u)) return;
                 const unsigned long long t0 = global_ns();
-                for (uint32_t i = 1; !mbar_test(bar, use & 1u); ++i) {
+                for (uint32_t i = 1; !ready(bar, use & 1u); ++i) {
                     if (on) {
                         const uint32_t what = first_pending() ? what1 : what0;
-                        if (mbar_test(smem_u32(&bars[kPFull + (what & kSlot)]), what & kPhase ? 1u : 0u)) values();
+                        if (ready(smem_u32(&bars[kPFull + (what & kSlot)]), what & kPhase ? 1u : 0u)) values();
                     }
-                    if ((i & 63u) == 0 && global_ns() - t0 > kWaitNs) wait.ok = false;
+                    if ((i & 63u) == 0 && __any_sync(0xffffffffu, global_ns() - t0 > kWaitNs)) wait.ok = false;
                     if (!wait.ok) return;
                 }
             };
             for (uint32_t n_item = 0; wait.ok; ++n_item) {
-                wait.thread(&bars[kItemFull + n_item % kRing], n_item / kRing);
+                wait.warp(&bars[kItemFull + n_item % kRing], n_item / kRing);
                 if (!wait.ok) break;
                 const volatile Item& it = items[n_item % kRing];
-                const bool stop = it.stop;
-                const int nu = it.nu, slot = it.slot;
+                const int stop = __shfl_sync(0xffffffffu, it.stop, 0), nu = __shfl_sync(0xffffffffu, it.nu, 0),
+                          slot = __shfl_sync(0xffffffffu, it.slot, 0);
                 if (stop) break;
-                mbar_arrive(&bars[kItemEmpty + n_item % kRing]);
+                warp_arrive(&bars[kItemEmpty + n_item % kRing]);
                 for (int u = 0; u < nu && wait.ok; ++u, ++n_unit) {
                     const uint32_t load = 2 * n_unit, st = load % kNS, use = load / kNS;
                     wait_keys(st, use);
@@ -742,27 +823,28 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                         const uint32_t sl = slot == 2 ? b : slot;
                         while ((on >> b & 1u) && wait.ok) values();
                         if (u == 0) {
-                            wait.thread(&bars[kQFull + sl], sl ? n_q1 : n_q0);
+                            wait.warp(&bars[kQFull + sl], sl ? n_q1 : n_q0);
                             n_q0 += sl == 0;
                             n_q1 += sl;
                         }
                         if (!wait.ok) break;
                         fence_after();
+                        const uint32_t n = sl ? n_s1 : n_s0, sn = 2 * sl + (n & 1u);
+                        if (elect_one()) {
                         const uint64_t dq = desc_k(smem_u32(sQ) + sl * Sh::kTile), dk = desc_k(smem_u32(sKV) + st * Sh::kTile);
                         const uint32_t d = tmem + kS0 + b * kKeys;
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) {
                             const uint32_t off = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
-                            asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                                         "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-                                         "l"(dq + off), "l"(dk + off), "r"(id_s), "r"(i > 0 ? 1u : 0u));
+                            mma_ss(d, dq + off, dk + off, id_s, i > 0);
                         }
-                        const uint32_t n = sl ? n_s1 : n_s0, sn = 2 * sl + (n & 1u);
-                        n_s0 += sl == 0;
-                        n_s1 += sl;
                         commit(&bars[kSFull + sn]);
                         if (b == b1) commit(&bars[kKvEmpty + st]);
                         if (u == nu - 1) commit(&bars[kQEmpty + sl]);
+                        }
+                        __syncwarp();
+                        n_s0 += sl == 0;
+                        n_s1 += sl;
                         older = on ? 1 - b : b;
                         on |= 1u << b;
                         const uint32_t what = sn | (n & 2u ? kPhase : 0) | (u > 0 ? kAcc : 0) | (b == b1 ? kRelease : 0);
@@ -778,8 +860,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 }
             }
             while (on && wait.ok) values();
-            if (!wait.ok) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
-            commit(&bars[kDrain]);
+            if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
+            if (elect_one()) commit(&bars[kDrain]);
+            __syncwarp();
             mbar_wait(smem_u32(&bars[kDrain]), 0);
         }
     }
