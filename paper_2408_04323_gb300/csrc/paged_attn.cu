@@ -319,6 +319,7 @@ struct TileLoader {
     const CUtensorMap* map;
     uint64_t* bars;
     uint32_t tiles;  // shared address of the ring
+    uint32_t st, phase;         // the next load's place in the ring, and of its barriers
     uint32_t at;
     int box, n_page, page_log;  // tokens of a page, pages of a tile
     int group;                  // ids: of pages 32 group ..
@@ -326,7 +327,7 @@ struct TileLoader {
     bool bad = false;
     static constexpr int kNone = INT32_MIN;
     __device__ __forceinline__ TileLoader(const AttnArgs& a_, const CUtensorMap* m, uint64_t* b, uint32_t t, uint32_t first)
-        : a(a_), map(m), bars(b), tiles(t), at(first) {
+        : a(a_), map(m), bars(b), tiles(t), st(first), phase(0), at(first) {
         page_log = a.bs_log < 7 ? 7 - a.bs_log : 0;
         n_page = 1 << page_log;
         box = kKeys >> page_log;
@@ -347,15 +348,15 @@ struct TileLoader {
         ids_next = fetch(it, group + 1);
     }
     __device__ __forceinline__ void tile(const Item& it, int u, Waiter& wait) {
-        constexpr int kNS = Shape<D>::kStages;
+        constexpr uint32_t kNS = Shape<D>::kStages;
         const int page = u << page_log;
         if (page >> 5 != group) {
             group = page >> 5;
             use(ids_next);
             ids_next = fetch(it, group + 1);
         }
-        const uint32_t st = at % kNS, n_use = at / kNS, bar = smem_u32(&bars[kKvFull + st]);
-        if (n_use > 0) wait.warp(&bars[kKvEmpty + st], n_use - 1);
+        const uint32_t bar = smem_u32(&bars[kKvFull + st]);
+        if (at >= kNS) wait.warp(&bars[kKvEmpty + st], phase ^ 1u);
         if (!wait.ok) return;
         at += 2;
         const uint32_t here = __ballot_sync(0xffffffffu, ids >= 0) >> (page & 31), n = __popc(here & ((2u << (n_page - 1)) - 1u));
@@ -378,6 +379,10 @@ struct TileLoader {
             }
         }
         __syncwarp();
+        if ((st += 2) >= kNS) {
+            st -= kNS;
+            phase ^= 1u;
+        }
     }
     // After a wait that gave up: the copies in flight land before the block ends.
     __device__ __forceinline__ void drain() const {
@@ -761,107 +766,138 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         // ---- the products.  The warp runs as one, so that the operands stay in its uniform registers, and one lane issues.
         {
             // Scores go to S0 and S1: a pair's slots to their own, a single slot's units to both in turn, so that the next
-            // unit's scores are computed under this one's softmax.  The product with V of the P in Sb, still to be issued:
-            // bit b of `on`, its tile's load and what it is (kSlot: slot and parity of the slot's unit, ...); older: which of
-            // the two came first.  (Two of everything, selected: an indexed array would be in local memory.)
-            enum { kSlot = 3, kPhase = 4, kAcc = 8, kRelease = 16 };
-            uint32_t n_unit = 0, n_q0 = 0, n_q1 = 0, n_s0 = 0, n_s1 = 0;
-            uint32_t on = 0, older = 0, turn = 0, load0 = 0, load1 = 0, what0 = 0, what1 = 0;
-            const uint32_t id_s = idesc(kBf16, kKeys, false), id_o = idesc(kBf16, D, true);
-            auto commit = [&](uint64_t* b) {
-                asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
+            // unit's scores are computed under this one's softmax.  pend[b] is the product with V of the P in Sb, still to
+            // be issued; older: which of two came first.  This warp's instructions are on the way of every unit: its places
+            // in the rings are counted along, a pair's two buffers are two copies of the code, and the single units' code is
+            // one copy for both (as two it did not stay in the instruction cache: decodes took 15% longer).
+            struct Pending {
+                uint32_t full, phase;   // the values' barrier and its phase
+                uint32_t p_full, p_phase, p_done;
+                uint32_t acc, empty;    // barrier to release the values to, 0: not the last to use them
+                uint32_t o;             // O's columns
+                uint64_t desc;
+            } pend[2] = {};
+            uint32_t on = 0, older = 0, turn = 0, st = 0, phase = 0, n_q0 = 0, n_q1 = 0, n_s0 = 0, n_s1 = 0;
+            const uint32_t id_s = idesc(kBf16, kKeys, false), id_o = idesc(kBf16, D, true), bar0 = smem_u32(bars);
+            const uint64_t q_desc = desc_k(smem_u32(sQ)), k_desc = desc_k(smem_u32(sKV)), v_desc = desc_v(smem_u32(sKV));
+            const bool leader = elect_one();
+            auto commit = [&](uint32_t b) {
+                asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(b) : "memory");
             };
-            auto ready = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(bar, parity)) != 0; };
-            auto first_pending = [&]() { return on == 3u ? older : on >> 1; };
-            auto values = [&]() {  // issues the older of the pending products
-                const uint32_t b = first_pending(), load = b ? load1 : load0, what = b ? what1 : what0;
-                const uint32_t st = load % kNS, use = load / kNS;
-                wait.warp(&bars[kPFull + (what & kSlot)], what & kPhase ? 1u : 0u);
-                wait.warp(&bars[kKvFull + st], use);
+            auto ready = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(b, parity)) != 0; };
+            auto await = [&](uint32_t b, uint32_t parity) {
+                if (!__all_sync(0xffffffffu, mbar_try(b, parity)) && wait.ok) wait.ok = __all_sync(0xffffffffu, mbar_wait(b, parity));
+            };
+            auto values = [&](uint32_t b) {
+                Pending p;
+                p.full = b ? pend[1].full : pend[0].full;
+                p.phase = b ? pend[1].phase : pend[0].phase;
+                p.p_full = b ? pend[1].p_full : pend[0].p_full;
+                p.p_phase = b ? pend[1].p_phase : pend[0].p_phase;
+                p.p_done = b ? pend[1].p_done : pend[0].p_done;
+                p.acc = b ? pend[1].acc : pend[0].acc;
+                p.empty = b ? pend[1].empty : pend[0].empty;
+                p.o = b ? pend[1].o : pend[0].o;
+                p.desc = b ? pend[1].desc : pend[0].desc;
+                await(p.p_full, p.p_phase);
+                await(p.full, p.phase);
                 on &= ~(1u << b);
                 if (!wait.ok) return;
                 fence_after();
-                if (elect_one()) {
-                const uint64_t dv = desc_v(smem_u32(sKV) + st * Sh::kTile);
-                const uint32_t o = tmem + kO0 + (what & kSlot) / 2 * D, pp = tmem + kS0 + b * kKeys;
+                if (leader) {
 #pragma unroll
-                for (int i = 0; i < kKeys / 16; ++i)
-                    mma_ts(o, pp + 8 * i, dv + 128 * i, id_o, i > 0 || (what & kAcc));
-                commit(&bars[kPvDone + (what & kSlot)]);
-                if (what & kRelease) commit(&bars[kKvEmpty + st]);
+                    for (int i = 0; i < kKeys / 16; ++i)
+                        mma_ts(p.o, tmem + kS0 + b * kKeys + 8 * i, p.desc + 128 * i, id_o, i > 0 || p.acc);
+                    commit(p.p_done);
+                    if (p.empty) commit(p.empty);
                 }
                 __syncwarp();
             };
-            // Waits for a tile of keys; meanwhile a probability tile that gets ready is used.
-            auto wait_keys = [&](uint32_t st, uint32_t use) {
-                const uint32_t bar = smem_u32(&bars[kKvFull + st]);
-                if (!wait.ok || ready(bar, use & 1u)) return;
-                const unsigned long long t0 = global_ns();
-                for (uint32_t i = 1; !ready(bar, use & 1u); ++i) {
-                    if (on) {
-                        const uint32_t what = first_pending() ? what1 : what0;
-                        if (ready(smem_u32(&bars[kPFull + (what & kSlot)]), what & kPhase ? 1u : 0u)) values();
-                    }
-                    if ((i & 63u) == 0 && __any_sync(0xffffffffu, global_ns() - t0 > kWaitNs)) wait.ok = false;
-                    if (!wait.ok) return;
+            auto scores = [&](uint32_t b, uint32_t sl, int u, int nu, bool last) {
+                if (u == 0) {
+                    await(bar0 + 8 * (kQFull + sl), (sl ? n_q1 : n_q0) & 1u);
+                    n_q0 += sl == 0;
+                    n_q1 += sl;
                 }
+                if (!wait.ok) return;
+                fence_after();
+                const uint32_t n = sl ? n_s1 : n_s0, sn = 8 * (2 * sl + (n & 1u));
+                n_s0 += sl == 0;
+                n_s1 += sl;
+                if (leader) {
+                    const uint64_t dq = q_desc + sl * (Sh::kTile >> 4), dk = k_desc + st * (Sh::kTile >> 4);
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint32_t off = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
+                        mma_ss(tmem + kS0 + b * kKeys, dq + off, dk + off, id_s, i > 0);
+                    }
+                    commit(bar0 + 8 * kSFull + sn);
+                    if (last) commit(bar0 + 8 * (kKvEmpty + st));
+                    if (u == nu - 1) commit(bar0 + 8 * (kQEmpty + sl));
+                }
+                __syncwarp();
+                Pending p;
+                p.full = bar0 + 8 * (kKvFull + st + 1);
+                p.phase = phase;
+                p.p_full = bar0 + 8 * kPFull + sn;
+                p.p_phase = n >> 1 & 1u;
+                p.p_done = bar0 + 8 * kPvDone + sn;
+                p.acc = u > 0;
+                p.empty = last ? bar0 + 8 * (kKvEmpty + st + 1) : 0;
+                p.o = tmem + kO0 + sl * D;
+                p.desc = v_desc + (st + 1) * (Sh::kTile >> 4);
+                if (b) pend[1] = p;
+                else pend[0] = p;
+                older = on ? 1 - b : b;
+                on |= 1u << b;
             };
             for (uint32_t n_item = 0; wait.ok; ++n_item) {
-                wait.warp(&bars[kItemFull + n_item % kRing], n_item / kRing);
+                await(bar0 + 8 * (kItemFull + n_item % kRing), n_item / kRing & 1u);
                 if (!wait.ok) break;
                 const volatile Item& it = items[n_item % kRing];
-                const int stop = __shfl_sync(0xffffffffu, it.stop, 0), nu = __shfl_sync(0xffffffffu, it.nu, 0),
+                const int stop = __shfl_sync(0xffffffffu, it.stop, 0), nu = stop ? 1 : __shfl_sync(0xffffffffu, it.nu, 0),
                           slot = __shfl_sync(0xffffffffu, it.slot, 0);
-                if (stop) break;
-                warp_arrive(&bars[kItemEmpty + n_item % kRing]);
-                for (int u = 0; u < nu && wait.ok; ++u, ++n_unit) {
-                    const uint32_t load = 2 * n_unit, st = load % kNS, use = load / kNS;
-                    wait_keys(st, use);
-                    const uint32_t b0 = slot == 2 ? 0 : turn, b1 = slot == 2 ? 1 : turn;
-#pragma unroll 1
-                    for (uint32_t b = b0; b <= b1; ++b) {
-                        const uint32_t sl = slot == 2 ? b : slot;
-                        while ((on >> b & 1u) && wait.ok) values();
-                        if (u == 0) {
-                            wait.warp(&bars[kQFull + sl], sl ? n_q1 : n_q0);
-                            n_q0 += sl == 0;
-                            n_q1 += sl;
-                        }
-                        if (!wait.ok) break;
-                        fence_after();
-                        const uint32_t n = sl ? n_s1 : n_s0, sn = 2 * sl + (n & 1u);
-                        if (elect_one()) {
-                        const uint64_t dq = desc_k(smem_u32(sQ) + sl * Sh::kTile), dk = desc_k(smem_u32(sKV) + st * Sh::kTile);
-                        const uint32_t d = tmem + kS0 + b * kKeys;
-#pragma unroll
-                        for (int i = 0; i < D / 16; ++i) {
-                            const uint32_t off = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
-                            mma_ss(d, dq + off, dk + off, id_s, i > 0);
-                        }
-                        commit(&bars[kSFull + sn]);
-                        if (b == b1) commit(&bars[kKvEmpty + st]);
-                        if (u == nu - 1) commit(&bars[kQEmpty + sl]);
-                        }
-                        __syncwarp();
-                        n_s0 += sl == 0;
-                        n_s1 += sl;
-                        older = on ? 1 - b : b;
-                        on |= 1u << b;
-                        const uint32_t what = sn | (n & 2u ? kPhase : 0) | (u > 0 ? kAcc : 0) | (b == b1 ? kRelease : 0);
-                        if (b) {
-                            load1 = load + 1;
-                            what1 = what;
-                        } else {
-                            load0 = load + 1;
-                            what0 = what;
+                if (!stop) warp_arrive(&bars[kItemEmpty + n_item % kRing]);
+                for (int u = 0; u < nu && wait.ok; ++u) {
+                    // Products that have to go first: all at the end; those of single units, if in the other order, before a
+                    // pair; the one that still needs the Sb of a single unit, and while the unit's keys are on their way
+                    // whichever gets its probabilities.
+                    const uint32_t keys = bar0 + 8 * (kKvFull + st);
+                    const bool alone = !stop && slot != 2;
+                    const uint32_t must = stop ? 3u : alone ? 1u << turn : u == 0 && on == 3u && older == 1u ? 3u : 0u;
+                    unsigned long long t0 = 0;
+                    for (uint32_t i = 0; wait.ok; ++i) {
+                        if ((on & must) == 0 && (!alone || ready(keys, phase))) break;
+                        const uint32_t f = on == 3u ? older : on >> 1;
+                        if ((on & must) || (on && ready(f ? pend[1].p_full : pend[0].p_full, f ? pend[1].p_phase : pend[0].p_phase)))
+                            values(f);
+                        else if ((i & 63u) == 63u) {
+                            const unsigned long long t = global_ns();
+                            if (t0 == 0) t0 = t;
+                            if (__any_sync(0xffffffffu, t - t0 > kWaitNs)) wait.ok = false;
                         }
                     }
-                    if (slot != 2) turn ^= 1u;
+                    if (stop || !wait.ok) break;
+                    if (alone) {
+                        scores(turn, slot, u, nu, true);
+                        turn ^= 1u;
+                    } else {
+                        if (on & 1u) values(0u);
+                        await(keys, phase);
+                        scores(0u, 0, u, nu, false);
+                        if (on & 2u) values(1u);
+                        scores(1u, 1, u, nu, true);
+                    }
+                    st += 2;
+                    if (st == kNS) {
+                        st = 0;
+                        phase ^= 1u;
+                    }
                 }
+                if (stop) break;
             }
-            while (on && wait.ok) values();
             if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
-            if (elect_one()) commit(&bars[kDrain]);
+            if (leader) commit(bar0 + 8 * kDrain);
             __syncwarp();
             mbar_wait(smem_u32(&bars[kDrain]), 0);
         }
