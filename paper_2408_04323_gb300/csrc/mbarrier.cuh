@@ -47,6 +47,20 @@ __device__ __forceinline__ bool mbar_wait(uint32_t addr, uint32_t parity) {
     return true;
 }
 
+// The same bounded by the number of tries, each of which waits a microsecond at most (a compact loop, for kernels whose
+// instructions barely fit the cache): gives up after 0.4 to 16 s.
+__device__ __forceinline__ bool mbar_wait_tries(uint32_t addr, uint32_t parity) {
+    uint32_t done = 0;
+#pragma unroll 1
+    for (uint32_t i = 0; i < (1u << 24) && !done; ++i)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(addr), "r"(parity), "r"(1000u)
+            : "memory");
+    return done;
+}
+
 __device__ __forceinline__ void mbar_init(uint64_t* b, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count));
 }

@@ -70,6 +70,7 @@ struct AttnArgs {
     CUtensorMap kmap, vmap, qmap[3];  // qmap[i]: tokens of 128 >> i rows
     int32_t bs_log, n_heads, n_kv_heads, group, n_req, causal, window, bf16;
     int32_t toks;         // tokens of a slot: 128 / group
+    int32_t inv_group;    // row / group = row * inv_group >> 16, for rows below 128
     int64_t n_tokens, n_blocks;
     const int32_t* query_start;
     const int32_t* kv_len;
@@ -164,14 +165,11 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-// A pair's halves that are infinite or NaN: their bits set.
+// A pair's halves that are infinite or NaN: their bits set.  (The exponent's complement is zero in them.)
 template <bool kBf16>
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
-    const uint32_t e = kBf16 ? 0x7F80u : 0x7C00u;
-    uint32_t m = 0;
-    if ((w & e) == e) m |= 0xFFFFu;
-    if ((w & (e << 16)) == e << 16) m |= 0xFFFF0000u;
-    return m;
+    const uint32_t e = kBf16 ? 0x7F807F80u : 0x7C007C00u;
+    return __vcmpeq2(~w & e, 0u);
 }
 template <bool kBf16>
 __device__ __forceinline__ float value16(uint16_t x) {
@@ -233,7 +231,7 @@ __device__ __forceinline__ const float* part_buf(const float* first, int i) {
 struct Waiter {
     bool ok = true;
     __device__ __forceinline__ void warp(uint64_t* b, uint32_t use) {
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(b), use & 1u));
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait_tries(smem_u32(b), use & 1u));
     }
 };
 
@@ -249,9 +247,14 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, int ch0, bool full, in
     tmem_wait_ld();
     if (!full) {
 #pragma unroll
-        for (int i = 0; i < NCH * 32; ++i) {
-            const int col = 32 * ch0 + i;
-            if (col < c0 || col >= c1) x[i] = 0xFF800000u;
+        for (int q = 0; q < NCH; ++q) {
+            // the columns of this chunk that the row sees, as bits; most chunks are seen by all the warp's rows
+            const int lo = min(max(c0 - 32 * (ch0 + q), 0), 32), hi = min(max(c1 - 32 * (ch0 + q), 0), 32);
+            const uint32_t bits = hi <= lo ? 0u : (0xFFFFFFFFu >> (32 - hi)) & (0xFFFFFFFFu << lo);
+            if (__all_sync(0xffffffffu, bits == 0xFFFFFFFFu)) continue;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (!(bits & (1u << i))) x[32 * q + i] = 0xFF800000u;
         }
     }
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -287,6 +290,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, int ch0, bool full, in
         uint32_t z[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) z[i] = 0u;
+#pragma unroll 1
         for (int q = 0; q < 4; ++q)
             if (q < ch0 || q >= ch0 + NCH) tmem_st16(tS + 16 * q, z);
     }
@@ -365,7 +369,7 @@ struct TileLoader {
             asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n * box * (D * 2)) : "memory");
         uint32_t dst = tiles + st * Shape<D>::kTile;
         const int within = (u * kKeys) & ((1 << a.bs_log) - 1);
-#pragma unroll 4
+#pragma unroll 2
         for (int i = 0; i < n_page; ++i, dst += box * 128) {
             const int id = __shfl_sync(0xffffffffu, ids, (page & 31) + i);
             if (one && id >= 0) {
@@ -387,8 +391,9 @@ struct TileLoader {
     // After a wait that gave up: the copies in flight land before the block ends.
     __device__ __forceinline__ void drain() const {
         constexpr uint32_t kNS = Shape<D>::kStages;
+#pragma unroll 1
         for (uint32_t i = at & 1u; i < at; i += 2)
-            if (i + kNS >= at) mbar_wait(smem_u32(&bars[kKvFull + i % kNS]), (i / kNS) & 1u);
+            if (i + kNS >= at) mbar_wait_tries(smem_u32(&bars[kKvFull + i % kNS]), (i / kNS) & 1u);
     }
 };
 
@@ -405,54 +410,12 @@ struct SlotSync {
 
 // Row q of a slot, tokens from tok on, the group's first head `head`: where it goes.
 __device__ __forceinline__ uint16_t* out_row(const AttnArgs& a, int tok, int head, int q) {
-    const int t = q / a.group;
+    const int t = q * a.inv_group >> 16;
     return a.out + (int64_t)(tok + t) * a.out_ld_token + (int64_t)(head + q - t * a.group) * a.out_ld_head;
 }
 __device__ __forceinline__ float* lse_row(const AttnArgs& a, int tok, int head, int q) {
-    const int t = q / a.group;
+    const int t = q * a.inv_group >> 16;
     return a.lse + (int64_t)(tok + t) * a.n_heads + head + q - t * a.group;
-}
-
-// Rows q .. q + R - 1 of nq: the weighted sums of their V parts, P parts at a time; a lane has D / 32 columns.
-template <bool kBf16, int D, int R, int P>
-__device__ __forceinline__ void join_rows(const AttnArgs& a, const float* part, const float* w, int V, int q0, int q, int nq,
-                                          int tok, int head) {
-    constexpr int kE = D / 32;
-    const int lane = threadIdx.x & 31;
-    float acc[R][kE];
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-        for (int e = 0; e < kE; ++e) acc[i][e] = 0.0f;
-#pragma unroll 1
-    for (int p0 = 0; p0 < V; p0 += P) {
-        float v[P][R][kE], f[P][R];
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                // past the last part or row: the last one's, with no weight
-                const int pt = min(p0 + p, V - 1), row = min(q + i, nq - 1);
-                const float* src = part_buf<D>(part, pt) + (q0 + row) * D + lane * kE;
-                if (kE == 4) *reinterpret_cast<float4*>(v[p][i]) = __ldcg(reinterpret_cast<const float4*>(src));
-                else *reinterpret_cast<float2*>(v[p][i]) = __ldcg(reinterpret_cast<const float2*>(src));
-                f[p][i] = w[row * V + pt];
-            }
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-            if (p0 + p < V)
-#pragma unroll
-                for (int i = 0; i < R; ++i)
-#pragma unroll
-                    for (int e = 0; e < kE; ++e) acc[i][e] = fmaf(f[p][i], v[p][i][e], acc[i][e]);
-    }
-#pragma unroll
-    for (int i = 0; i < R; ++i)
-        if (q + i < nq) {
-            uint32_t* dst = reinterpret_cast<uint32_t*>(out_row(a, tok, head, q0 + q + i)) + lane * (kE / 2);
-#pragma unroll
-            for (int e = 0; e < kE / 2; ++e) dst[e] = pack16<kBf16>(acc[i][2 * e], acc[i][2 * e + 1]);
-        }
 }
 
 // The V parts of a split item's rows, joined by the slot whose part came last: per row the parts' common maximum and sum
@@ -460,7 +423,8 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const float* part, 
 template <bool kBf16, int D>
 __device__ __noinline__ SlotSync join_parts(const AttnArgs& a, const float* part, int V, int rows, int tok, int head, float* w,
                                             SlotSync sync) {
-    const int row = threadIdx.x & (kRows - 1), warp = row >> 5, batch = min(kRows, kScratch / 4 / V);
+    const int row = threadIdx.x & (kRows - 1), batch = min(kRows, kScratch / 4 / V);
+#pragma unroll 1
     for (int q0 = 0; q0 < rows; q0 += batch) {
         const int nq = min(batch, rows - q0);
         if (q0 > 0) sync();
@@ -482,14 +446,36 @@ __device__ __noinline__ SlotSync join_parts(const AttnArgs& a, const float* part
                 }
             }
             const float inv = inverse_sum(L), Ms = finite_or_zero(M);
+#pragma unroll 1
             for (int i = 0; i < V; ++i) w[row * V + i] = exp2_hw(w[row * V + i] - Ms) * inv;
             if (a.lse) *lse_row(a, tok, head, q0 + row) = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
         }
         sync();
-        if (nq <= 8)
-            for (int q = 2 * warp; q < nq; q += 8) join_rows<kBf16, D, 2, 8>(a, part, w, V, q0, q, nq, tok, head);
-        else
-            for (int q = 8 * warp; q < nq; q += 32) join_rows<kBf16, D, 8, 2>(a, part, w, V, q0, q, nq, tok, head);
+        // a thread has four columns of a row, four rows (of this many apart) at a time with two parts each in flight
+        constexpr int kGroups = D / 4, kStep = kRows / kGroups, kR = 4;
+        const int c = row % kGroups;
+#pragma unroll 1
+        for (int q = row / kGroups; q < nq; q += kR * kStep) {
+            float4 acc[kR];
+#pragma unroll
+            for (int i = 0; i < kR; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+            for (int p = 0; p < V; ++p) {
+                const float4* src = reinterpret_cast<const float4*>(part_buf<D>(part, p) + q0 * D) + c;
+#pragma unroll
+                for (int i = 0; i < kR; ++i) {
+                    const int r = min(q + i * kStep, nq - 1);  // past the last row: the last one, not stored
+                    const float4 v = __ldcg(src + r * kGroups);
+                    const float f = w[r * V + p];
+                    acc[i] = make_float4(fmaf(f, v.x, acc[i].x), fmaf(f, v.y, acc[i].y), fmaf(f, v.z, acc[i].z), fmaf(f, v.w, acc[i].w));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kR; ++i)
+                if (q + i * kStep < nq)
+                    *reinterpret_cast<uint2*>(out_row(a, tok, head, q0 + q + i * kStep) + 4 * c) =
+                        make_uint2(pack16<kBf16>(acc[i].x, acc[i].y), pack16<kBf16>(acc[i].z, acc[i].w));
+        }
     }
     return sync;
 }
@@ -548,6 +534,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     // summed by its warp.
     const int k = (a.n_req + kThreads - 1) / kThreads, per = 2 * a.toks;
     int64_t mine = 0;
+#pragma unroll 1
     for (int i = 0; i < k; ++i) {
         const int r = tid * k + i;
         const Req q = load_req(a, r, blockIdx.x == 0);
@@ -559,7 +546,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             big &= big - 1;
             const int kv = __shfl_sync(0xffffffffu, q.kv, src), n = __shfl_sync(0xffffffffu, q.n, src);
             int64_t c = 0;
-            for (int j = lane; j < (n + per - 1) / per; j += 32) c += kItemCost + item_units(a, kv, n, j);
+            const int m = (n + per - 1) / per;
+#pragma unroll 1
+            for (int j = lane; j < m; j += 32) c += kItemCost + item_units(a, kv, n, j);
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) c += __shfl_xor_sync(0xffffffffu, c, d);
             if (lane == src) mine += c;
@@ -622,6 +611,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             }
             for (bool found = false; !found;) {
                 const Req q = get(r);
+#pragma unroll 1
                 for (int j0 = 0; j0 * per < q.n && !found; j0 += 32) {
                     const int64_t c = (j0 + lane) * per < q.n ? kItemCost + item_units(a, q.kv, q.n, j0 + lane) : 0;
                     int64_t s = c;
@@ -653,12 +643,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             if (n_q[s] > 0) wait.warp(&bars[kQEmpty + s], n_q[s] - 1);
             if (!wait.ok) return;
             const uint32_t bar = smem_u32(&bars[kQFull + s]);
-            const int rows = kRows >> it.rep_log, boxed = rows / a.group * a.group, copies = 1 << it.rep_log;
+            const int rows = kRows >> it.rep_log, boxed = (rows * a.inv_group >> 16) * a.group, copies = 1 << it.rep_log;
             const CUtensorMap* map = &a.qmap[it.rep_log];
             if (elect_one()) {
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
                              "r"((uint32_t)(copies * kNH * boxed * 128))
                              : "memory");
+#pragma unroll 1
                 for (int c = 0; c < copies; ++c)
 #pragma unroll
                     for (int half = 0; half < kNH; ++half)
@@ -722,6 +713,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             __syncwarp();
             ++n_item;
             if (it.nu > 0) keys.begin(it);
+#pragma unroll 1
             for (int u = 0; u < it.nu && wait.ok; ++u) {
                 keys.tile(it, it.u0 + u, wait);
                 if (u == 0) {
@@ -744,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             keys.drain();
 #pragma unroll
             for (int s = 0; s < 2; ++s)
-                if (n_q[s] > 0) mbar_wait(smem_u32(&bars[kQFull + s]), (n_q[s] - 1) & 1u);
+                if (n_q[s] > 0) mbar_wait_tries(smem_u32(&bars[kQFull + s]), (n_q[s] - 1) & 1u);
         }
     } else if (warp == kValueWarp) {
         // ---- the copies of the values
@@ -756,6 +748,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             if (it.stop) break;
             warp_arrive(&bars[kItemEmpty + n_item % kRing]);
             if (it.nu > 0) vals.begin(it);
+#pragma unroll 1
             for (int u = 0; u < it.nu && wait.ok; ++u) vals.tile(it, it.u0 + u, wait);
         }
         if (!wait.ok) {
@@ -786,7 +779,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             };
             auto ready = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(b, parity)) != 0; };
             auto await = [&](uint32_t b, uint32_t parity) {
-                if (!__all_sync(0xffffffffu, mbar_try(b, parity)) && wait.ok) wait.ok = __all_sync(0xffffffffu, mbar_wait(b, parity));
+                if (wait.ok) wait.ok = __all_sync(0xffffffffu, mbar_wait_tries(b, parity));
             };
             auto values = [&](uint32_t b) {
                 Pending p;
@@ -858,6 +851,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 const int stop = __shfl_sync(0xffffffffu, it.stop, 0), nu = stop ? 1 : __shfl_sync(0xffffffffu, it.nu, 0),
                           slot = __shfl_sync(0xffffffffu, it.slot, 0);
                 if (!stop) warp_arrive(&bars[kItemEmpty + n_item % kRing]);
+#pragma unroll 1
                 for (int u = 0; u < nu && wait.ok; ++u) {
                     // Products that have to go first: all at the end; those of single units, if in the other order, before a
                     // pair; the one that still needs the Sb of a single unit, and while the unit's keys are on their way
@@ -865,17 +859,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                     const uint32_t keys = bar0 + 8 * (kKvFull + st);
                     const bool alone = !stop && slot != 2;
                     const uint32_t must = stop ? 3u : alone ? 1u << turn : u == 0 && on == 3u && older == 1u ? 3u : 0u;
-                    unsigned long long t0 = 0;
+#pragma unroll 1
                     for (uint32_t i = 0; wait.ok; ++i) {
                         if ((on & must) == 0 && (!alone || ready(keys, phase))) break;
                         const uint32_t f = on == 3u ? older : on >> 1;
                         if ((on & must) || (on && ready(f ? pend[1].p_full : pend[0].p_full, f ? pend[1].p_phase : pend[0].p_phase)))
                             values(f);
-                        else if ((i & 63u) == 63u) {
-                            const unsigned long long t = global_ns();
-                            if (t0 == 0) t0 = t;
-                            if (__any_sync(0xffffffffu, t - t0 > kWaitNs)) wait.ok = false;
-                        }
+                        else wait.ok = i < (1u << 24);
                     }
                     if (stop || !wait.ok) break;
                     if (alone) {
@@ -899,7 +889,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
             if (leader) commit(bar0 + 8 * kDrain);
             __syncwarp();
-            mbar_wait(smem_u32(&bars[kDrain]), 0);
+            mbar_wait_tries(smem_u32(&bars[kDrain]), 0);
         }
     }
     } else {
@@ -925,7 +915,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             const int half = it.slot == 2 ? s : 0;
             const int tok0 = half * a.toks, ntok = min(a.toks, it.ntok - tok0), rows = ntok * a.group;
             const int per_copy = kRows >> it.rep_log, rr = row & (per_copy - 1), copy = row / per_copy;
-            const int j = rr / a.group;
+            const int j = rr * a.inv_group >> 16;
             const bool live = rr < rows;
             const bool busy = __any_sync(0xffffffffu, live);
             // keys that this row sees; that every row of the slot sees
@@ -939,6 +929,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             const int all1 = a.causal ? min(it.kv, it.pos + tok0 + 1) : it.kv;
             const int all0 = a.window > 0 ? (int)max((int64_t)0, (int64_t)it.pos + tok0 + ntok - a.window) : 0;
             float m = -INFINITY, l = 0.0f;
+#pragma unroll 1
             for (int u = 0; u < it.nu; ++u, ++n_unit, ++n_s) {
                 const int t0 = (it.u0 + u) * kKeys;
                 const bool full = t0 >= all0 && t0 + kKeys <= all1;
@@ -950,7 +941,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                     auto rescale = [&](float f) {
                         wait.warp(&bars[kPvDone + (sn ^ 1)], (n_s - 1) >> 1);
                         fence_after();
-#pragma unroll
+#pragma unroll 1
                         for (int c = 0; c < D; c += 16) {
                             uint32_t o[16];
                             tmem_ld16(tO + c, o);
@@ -974,19 +965,19 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                     const int key = t0 + row;
                     uint4* v = reinterpret_cast<uint4*>(sKV + st * Sh::kTile + row * 128);
                     if (key < it.begin || key >= it.end) {
-#pragma unroll
-                        for (int c = 0; c < D / 8; ++c) v[(c / 8) * (kHalf / 16) + (c % 8)] = make_uint4(0, 0, 0, 0);
+#pragma unroll 4
+                        for (int c = 0; c < D / 8; ++c) v[(c / 8) * (kHalf / 16) + (c ^ row) % 8] = make_uint4(0, 0, 0, 0);
                     } else if (key < all0 || key >= all1) {
-#pragma unroll
+#pragma unroll 2
                         for (int c = 0; c < D / 8; ++c) {
                             uint4* at = v + (c / 8) * (kHalf / 16) + ((c ^ row) & 7);
-                            uint4 w = *at;
-                            const uint32_t bx = not_finite<kBf16>(w.x), by = not_finite<kBf16>(w.y),
-                                           bz = not_finite<kBf16>(w.z), bw = not_finite<kBf16>(w.w);
-                            if (bx | by | bz | bw) {
+                            const uint4 w = *at;
+                            const uint4 bad = make_uint4(not_finite<kBf16>(w.x), not_finite<kBf16>(w.y), not_finite<kBf16>(w.z),
+                                                         not_finite<kBf16>(w.w));
+                            if (bad.x | bad.y | bad.z | bad.w) {
                                 *reinterpret_cast<volatile int32_t*>(&items[ring].poison) = 1;  // before the zero can be seen
                                 __threadfence_block();
-                                *at = make_uint4(w.x & ~bx, w.y & ~by, w.z & ~bz, w.w & ~bw);
+                                *at = make_uint4(w.x & ~bad.x, w.y & ~bad.y, w.z & ~bad.z, w.w & ~bad.w);
                             }
                         }
                     }
@@ -1050,8 +1041,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 ml_s[s][row] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
                 wg_sync();
                 float M = -INFINITY, L = 0.0f;
+#pragma unroll 1
                 for (int c = 0; c < copies; ++c) M = fmaxf(M, ml_s[s][c * per_copy + rr].x);
                 const float Ms = finite_or_zero(M);
+#pragma unroll 1
                 for (int c = 0; c < copies; ++c) {
                     const float2 v = ml_s[s][c * per_copy + rr];
                     L = fmaf(exp2_hw(v.x - Ms), v.y, L);
@@ -1063,8 +1056,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 }
                 const int width = used <= 32 ? min(D, 128) : used <= 64 ? 64 : 32, groups = width / 4;
                 const int g_log = 31 - __clz(groups);
+#pragma unroll 1
                 for (int c0 = 0; c0 < D; c0 += width) {
                     if (busy)
+#pragma unroll 1
                         for (int c = 0; c < width; c += 32) {
                             float o[32];
                             load_o(c0 + c, o);
@@ -1077,9 +1072,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                             }
                         }
                     wg_sync();
+#pragma unroll 1
                     for (int e = row; e < rows << g_log; e += kRows) {
                         const int q = e >> g_log, gq = e & (groups - 1);
                         float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
                         for (int c = 0; c < copies; ++c) {
                             const int at = c * rows + q;
                             const float4 v = reinterpret_cast<const float4*>(scratch)[at * groups + (gq ^ (at & 7))];
@@ -1094,7 +1091,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 const float inv = inverse_sum(l);
                 if (busy) {
                     uint16_t* dst = out_row(a, tok, head, rr);
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < D; c += 32) {
                         float o[32];
                         load_o(c, o);
@@ -1109,7 +1106,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                     if (live && a.lse) *lse_row(a, tok, head, rr) = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
                 }
             } else if (busy) {
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
                     float o[32];
                     load_o(c, o);
@@ -1244,6 +1241,7 @@ extern "C" scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_lay
     a.causal = causal != 0;
     a.window = window < ld_table * layout->block_size ? window : 0;  // no sequence is longer
     a.toks = kRows / G;
+    a.inv_group = (65536 + G - 1) / G;
     a.n_tokens = n_tokens;
     a.n_blocks = layout->n_blocks;
     a.query_start = query_start;
