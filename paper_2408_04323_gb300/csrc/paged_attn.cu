@@ -20,7 +20,8 @@
 //
 // Work.  An item is a (key-value head, request, up to 256 rows), its units the tiles of keys that its rows see.  All
 // units in a row, head by head and request by request, with kItemCost extra per item, are cut into equal ranges, one per
-// SM: long sequences are split, short ones follow one another, whatever the batch.  Each CTA takes the sums over
+// SM (a cut close to an item's start or end moves there): long sequences are split, short ones follow one another,
+// whatever the batch.  Each CTA takes the sums over
 // the requests for itself (lengths are on the device), so the call is one launch.  An item that lies in several ranges
 // leaves its parts (O, m, l) in the workspace, and the CTA that comes last (a counter per item) joins them in the
 // ranges' order, so that the result does not depend on who was last.
@@ -52,6 +53,9 @@ constexpr int kSoftmaxRegs = 200, kOtherRegs = 104;  // 2 * 200 + 104 = 3 * 168,
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kValueWarp = 10;
 constexpr int kRing = 4;         // items handed from the load warp to the others
 constexpr int kItemCost = 1;     // an item's start and end, in units
+constexpr int kMinRange = 4;     // units that a CTA takes at least
+constexpr int kSnap = 2;         // a cut this close to an item's ends moves there,
+constexpr int kPairSnap = 6;     // or to those of a pair, whose parts are 256 rows
 constexpr int kBufs = 4;         // part buffers of a CTA (see part_buf)
 constexpr int kScratch = 16384;  // bytes of a slot's scratch: 32 columns of sums of its rows, or weights of parts
 constexpr int kHalf = kKeys * 128;  // bytes of a tile's half: 128 keys x 64 dimensions
@@ -590,7 +594,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             if (lane >= d) upto += t;
         }
         const int64_t head_cost = __shfl_sync(0xffffffffu, upto, kThreads / 32 - 1), total = head_cost * a.n_kv_heads;
-        const int64_t range = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)1);
+        const int64_t range = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)kMinRange);
         const int64_t B0 = min(total, blockIdx.x * range), B1 = min(total, B0 + range);
         int h = 0, r = 0, j = 0;
         int64_t p = B0;  // where item (h, r, j) starts
@@ -688,7 +692,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             it.poison = it.stop = 0;
             const int t0 = it.begin / kKeys, units = (it.end + kKeys - 1) / kKeys - t0;
             const int64_t s = p + kItemCost;  // where its units start
-            const int lo = (int)max((int64_t)0, min((int64_t)units, B0 - s)), hi = (int)max((int64_t)0, min((int64_t)units, B1 - s));
+            const int snap = it.ntok > a.toks ? kPairSnap : kSnap;
+            auto cut = [&](int64_t b) {
+                return b >= s + units ? units : b - s < snap ? 0 : s + units - b < snap ? units : (int)(b - s);
+            };
+            const int lo = cut(B0), hi = cut(B1);
             const bool here = units ? hi > lo : p >= B0;
             p = s + units;
             ++j;
@@ -698,8 +706,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             it.first = blockIdx.x;
             it.n_parts = 1;
             if (it.nu < units) {
-                it.first = (int)quotient(s, range);
-                it.n_parts = (int)quotient(s + units - 1, range) - it.first + 1;
+                it.first = (int)quotient(s + snap - 1, range);
+                it.n_parts = (int)quotient(s + units - snap, range) - it.first + 1;
             }
             it.slot = it.ntok > a.toks ? 2 : turn;
             if (it.slot < 2) turn ^= 1;
