@@ -10,6 +10,7 @@ the functions raises ImportError: there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -815,9 +816,30 @@ def scoot_fantasy_end(ctx, var_out=None, stream=None):
 
 
 # ------------------------------------------------------------------ a serving step's attention
+#
+# These calls are a step's smallest, and made once or more per layer: their checks are inlined, and the messages left to
+# the slow path.
 
 F16, BF16 = 0, 1
 MAX_GROUP = 128
+
+
+def _ptr(t, dtype, name):
+    """_dev for a tensor that must be there, as an int."""
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    return _dev(t, dtype, name).value
+
+
+def _current_stream(device: int) -> int:
+    """Handle of the device's current stream (torch.cuda.current_stream builds an object around it, in 3 us)."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+def _on(stream, t):
+    return _current_stream(t.get_device()) if stream is None else _stream(stream)
 
 
 def _heads(t, dtype, name):
@@ -825,7 +847,7 @@ def _heads(t, dtype, name):
     of an axis of one (torch may give it any) counts as the axis's size."""
     if not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA torch tensor (device memory)")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
     if t.dim() != 3:
         raise ValueError(f"{name} must be [tokens][heads][dim], got {tuple(t.shape)}")
@@ -836,25 +858,35 @@ def _heads(t, dtype, name):
     return t.data_ptr(), (st if n > 1 else h * d), (sh if h > 1 else d)
 
 
+@functools.lru_cache(maxsize=64)
+def _layout(bf16, shape, stride):
+    nb, bs, h, d = shape
+    sb, st, sh, _ = stride
+    L = scoot_kv_layout(BF16 if bf16 else F16, d, h, bs, nb, sb if nb > 1 else bs * h * d, st, sh if h > 1 else d)
+    return L, C.byref(L)
+
+
+def _kv(k_cache, v_cache):
+    import torch
+    dt, shape, stride = k_cache.dtype, k_cache.shape, k_cache.stride()
+    if not (k_cache.is_cuda and v_cache.is_cuda):
+        raise TypeError("k_cache and v_cache must be CUDA torch tensors (device memory)")
+    if dt is not v_cache.dtype or not (dt is torch.bfloat16 or dt is torch.float16):
+        raise TypeError(f"k_cache and v_cache must both be float16 or bfloat16, got {dt} and {v_cache.dtype}")
+    if len(shape) != 4 or shape != v_cache.shape:
+        raise ValueError(f"k_cache and v_cache must be [blocks][tokens][heads][dim] of one shape, got {tuple(shape)} and "
+                         f"{tuple(v_cache.shape)}")
+    if stride != v_cache.stride():
+        raise ValueError("k_cache and v_cache must have the same strides")
+    if stride[3] != 1:
+        raise ValueError("k_cache and v_cache must be contiguous along their last axis")
+    return _layout(dt is torch.bfloat16, tuple(shape), stride)
+
+
 def kv_layout(k_cache, v_cache) -> scoot_kv_layout:
     """The layout of a cache given as CUDA tensors [blocks][tokens][heads][dim] (a transposed view of
     [blocks][heads][tokens][dim] will do)."""
-    import torch
-    if not (k_cache.is_cuda and v_cache.is_cuda):
-        raise TypeError("k_cache and v_cache must be CUDA torch tensors (device memory)")
-    if k_cache.dtype != v_cache.dtype or k_cache.dtype not in (torch.float16, torch.bfloat16):
-        raise TypeError(f"k_cache and v_cache must both be float16 or bfloat16, got {k_cache.dtype} and {v_cache.dtype}")
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape:
-        raise ValueError(f"k_cache and v_cache must be [blocks][tokens][heads][dim] of one shape, got "
-                         f"{tuple(k_cache.shape)} and {tuple(v_cache.shape)}")
-    nb, bs, h, d = k_cache.shape
-    sb, st, sh, sd = k_cache.stride()
-    if k_cache.stride() != v_cache.stride():
-        raise ValueError("k_cache and v_cache must have the same strides")
-    if sd != 1:
-        raise ValueError("k_cache and v_cache must be contiguous along their last axis")
-    return scoot_kv_layout(BF16 if k_cache.dtype == torch.bfloat16 else F16, d, h, bs, nb, sb if nb > 1 else bs * h * d,
-                           st, sh if h > 1 else d)
+    return scoot_kv_layout.from_buffer_copy(_kv(k_cache, v_cache)[0])
 
 
 def scoot_kv_tables(ctx, cached_len, new_len, block_table, block_size, n_blocks, free_blocks, query_start, kv_len,
@@ -863,31 +895,35 @@ def scoot_kv_tables(ctx, cached_len, new_len, block_table, block_size, n_blocks,
     query_start [R + 1]; position [T]; counts [2].  slot: device int64 [T]."""
     import torch
     i32 = torch.int32
-    R = cached_len.numel()
+    R, T, h = cached_len.numel(), slot.numel(), _h(ctx)
     if block_table.dim() != 2 or block_table.shape[0] != R or new_len.numel() != R or kv_len.numel() != R or \
-            query_start.numel() != R + 1 or counts.numel() != 2 or position.numel() != slot.numel():
+            query_start.numel() != R + 1 or counts.numel() != 2 or position.numel() != T:
         raise ValueError("array lengths do not match: [R] cached_len, new_len, kv_len; [R][width] block_table; "
                          "[R + 1] query_start; [T] slot, position; [2] counts")
-    _check(lib().scoot_kv_tables(_h(ctx), _dev(cached_len, i32, "cached_len"), _dev(new_len, i32, "new_len"), R,
-                                 int(block_size), int(n_blocks), _dev(block_table, i32, "block_table"),
-                                 block_table.shape[1], _dev(free_blocks, i32, "free_blocks"), free_blocks.numel(),
-                                 _dev(query_start, i32, "query_start"), _dev(kv_len, i32, "kv_len"),
-                                 _dev(slot, torch.int64, "slot"), _dev(position, i32, "position"), slot.numel(),
-                                 _dev(counts, i32, "counts"), _stream(stream)), "scoot_kv_tables", _h(ctx))
+    status = lib().scoot_kv_tables(h, _ptr(cached_len, i32, "cached_len"), _ptr(new_len, i32, "new_len"), R, block_size,
+                                   n_blocks, _ptr(block_table, i32, "block_table"), block_table.shape[1],
+                                   _ptr(free_blocks, i32, "free_blocks"), free_blocks.numel(),
+                                   _ptr(query_start, i32, "query_start"), _ptr(kv_len, i32, "kv_len"),
+                                   _ptr(slot, torch.int64, "slot"), _ptr(position, i32, "position"), T,
+                                   _ptr(counts, i32, "counts"), _on(stream, counts))
+    if status:
+        _check(status, "scoot_kv_tables", h)
 
 
 def scoot_kv_append(ctx, k, v, slot, k_cache, v_cache, stream=None) -> None:
     """k, v: device [T][heads][dim] of the cache's type (last axis contiguous); slot: device int64 [T]."""
     import torch
-    L = kv_layout(k_cache, v_cache)
-    if k.shape != v.shape or k.shape[0] != slot.numel() or tuple(k.shape[1:]) != tuple(k_cache.shape[2:]):
+    L, ref = _kv(k_cache, v_cache)
+    T, dt, h = slot.numel(), k_cache.dtype, _h(ctx)
+    if k.shape != v.shape or tuple(k.shape) != (T, L.n_kv_heads, L.head_dim):
         raise ValueError(f"k and v must be [T][heads][dim] as slot and the cache have them, got {tuple(k.shape)} and "
                          f"{tuple(v.shape)}")
-    kp, kt, kh = _heads(k, k_cache.dtype, "k")
-    vp, vt, vh = _heads(v, k_cache.dtype, "v")
-    _check(lib().scoot_kv_append(_h(ctx), C.byref(L), kp, kt, kh, vp, vt, vh, _dev(slot, torch.int64, "slot"),
-                                 slot.numel(), k_cache.data_ptr(), v_cache.data_ptr(), _stream(stream)),
-           "scoot_kv_append", _h(ctx))
+    kp, kt, kh = _heads(k, dt, "k")
+    vp, vt, vh = _heads(v, dt, "v")
+    status = lib().scoot_kv_append(h, ref, kp, kt, kh, vp, vt, vh, _ptr(slot, torch.int64, "slot"), T,
+                                   k_cache.data_ptr(), v_cache.data_ptr(), _on(stream, slot))
+    if status:
+        _check(status, "scoot_kv_append", h)
 
 
 def scoot_paged_attention(ctx, q, k_cache, v_cache, block_table, query_start, kv_len, out, scale, causal=True, window=0,
@@ -895,21 +931,22 @@ def scoot_paged_attention(ctx, q, k_cache, v_cache, block_table, query_start, kv
     """q, out: device [T][heads][dim] of the cache's type (last axis contiguous); block_table int32 [R][width],
     query_start int32 [R + 1], kv_len int32 [R]; lse: device float32 [T][heads] or None."""
     import torch
-    L = kv_layout(k_cache, v_cache)
-    R = kv_len.numel()
-    if q.shape != out.shape or q.dim() != 3 or q.shape[2] != L.head_dim:
-        raise ValueError(f"q and out must be [T][heads][{L.head_dim}] of one shape, got {tuple(q.shape)} and "
+    L, ref = _kv(k_cache, v_cache)
+    R, shape, dt, h = kv_len.numel(), q.shape, k_cache.dtype, _h(ctx)
+    if shape != out.shape or len(shape) != 3 or shape[2] != L.head_dim:
+        raise ValueError(f"q and out must be [T][heads][{L.head_dim}] of one shape, got {tuple(shape)} and "
                          f"{tuple(out.shape)}")
     if block_table.dim() != 2 or block_table.shape[0] != R or query_start.numel() != R + 1 or \
-            (lse is not None and lse.shape != q.shape[:2]):
+            (lse is not None and lse.shape != shape[:2]):
         raise ValueError("array lengths do not match: [R] kv_len; [R][width] block_table; [R + 1] query_start; "
                          "[T][heads] lse")
-    qp, qt, qh = _heads(q, k_cache.dtype, "q")
-    op, ot, oh = _heads(out, k_cache.dtype, "out")
+    qp, qt, qh = _heads(q, dt, "q")
+    op, ot, oh = _heads(out, dt, "out")
     i32 = torch.int32
-    _check(lib().scoot_paged_attention(_h(ctx), C.byref(L), qp, qt, qh, q.shape[1], q.shape[0],
-                                       _dev(query_start, i32, "query_start"), _dev(kv_len, i32, "kv_len"), R,
-                                       _dev(block_table, i32, "block_table"), block_table.shape[1],
-                                       k_cache.data_ptr(), v_cache.data_ptr(), scale, int(bool(causal)), int(window),
-                                       op, ot, oh, _dev(lse, torch.float32, "lse"), _stream(stream)),
-           "scoot_paged_attention", _h(ctx))
+    status = lib().scoot_paged_attention(h, ref, qp, qt, qh, shape[1], shape[0], _ptr(query_start, i32, "query_start"),
+                                         _ptr(kv_len, i32, "kv_len"), R, _ptr(block_table, i32, "block_table"),
+                                         block_table.shape[1], k_cache.data_ptr(), v_cache.data_ptr(), scale,
+                                         1 if causal else 0, window, op, ot, oh,
+                                         None if lse is None else _ptr(lse, torch.float32, "lse"), _on(stream, q))
+    if status:
+        _check(status, "scoot_paged_attention", h)

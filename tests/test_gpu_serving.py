@@ -61,7 +61,7 @@ def _case(rng, n, bs, c_hi, n_hi, zero=0.0):
 
 @pytest.mark.parametrize("n,bs,c_hi,n_hi,zero", [
     (1, 16, 0, 1, 0.0), (1, 8, 33, 0, 0.0), (2, 256, 300, 700, 0.0), (33, 8, 100, 1, 0.0), (57, 16, 48, 40, 0.5),
-    (300, 32, 64, 3, 0.2), (1025, 16, 40, 2, 0.1), (3001, 8, 30, 20, 0.3), (7, 64, 0, 4099, 0.0)])
+    (300, 32, 64, 3, 0.2), (1025, 16, 40, 2, 0.1), (3001, 8, 30, 20, 0.3), (7, 64, 0, 4099, 0.0), (26001, 8, 20, 3, 0.3)])
 @pytest.mark.parametrize("pad", [0, 13])
 def test_tables_match_the_plain_form(S, ctx, n, bs, c_hi, n_hi, zero, pad):
     cached, new, table, n_blocks, free = _case(np.random.default_rng(n * 100 + bs), n, bs, c_hi, n_hi, zero)
