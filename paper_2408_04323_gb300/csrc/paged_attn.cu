@@ -59,7 +59,6 @@ constexpr int kPairSnap = 6;     // or to those of a pair, whose parts are 256 r
 constexpr int kBufs = 4;         // part buffers of a CTA (see part_buf)
 constexpr int kScratch = 16384;  // bytes of a slot's scratch: 32 columns of sums of its rows, or weights of parts
 constexpr int kHalf = kKeys * 128;  // bytes of a tile's half: 128 keys x 64 dimensions
-constexpr uint32_t kS0 = 0, kO0 = 256;  // tensor memory columns: S0, S1, O0, O1
 constexpr int kMaxCtas = (int)(SCOOT_COUNTS / 2);
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
 
@@ -67,6 +66,8 @@ template <int D>
 struct Shape {
     static constexpr int kTile = kKeys * D * 2;           // bytes of a tile of keys, values or queries
     static constexpr int kStages = (D == 128 ? 4 : 10);   // tiles of keys or values in flight
+    // Tensor memory: score buffers of 128 columns from 0 on, then the slots' O.
+    static constexpr uint32_t kBuf = D == 128 ? 2 : 3, kO = 512 - 2 * D;
     static constexpr int kSmem = 2 * kTile + kStages * kTile + 2 * kScratch;  // and the static part, up to 227 KB
 };
 
@@ -104,10 +105,10 @@ struct Item {
     int32_t stop;
 };
 
-// The first three are [slot][parity of the slot's unit]: two units of a slot may be under way at once.
+// The first three are [slot][number of the slot's unit mod 3]: up to three units of a slot are under way at once.
 enum {
-    kSFull = 0, kPFull = 4, kPvDone = 8, kQFull = 12, kQEmpty = 14, kWg = 16, kItemFull = 18, kItemEmpty = 22, kDrain = 26,
-    kKvFull = 27, kKvEmpty = 37, kBars = 47
+    kSFull = 0, kPFull = 6, kPvDone = 12, kQFull = 18, kQEmpty = 20, kWg = 22, kItemFull = 24, kItemEmpty = 28, kDrain = 32,
+    kKvFull = 33, kKvEmpty = 43, kBars = 53
 };
 
 // The swizzled K-major tile of queries or keys: rows of 128 bytes, 8-row groups 1024 bytes apart.
@@ -231,12 +232,15 @@ __device__ __forceinline__ const float* part_buf(const float* first, int i) {
     return first + (size_t)(i == 0 ? 0 : 2 * i - 1) * kPartFloats<D>;
 }
 
-// Bounded waits that pass at once after the first that gave up, so that every role runs to its end.
+// Bounded waits that pass at once after the first that gave up.  A lane's `ok` is its own until all() makes it the warp's:
+// between the two the role goes on as if the wait had ended, on memory that is its own all the same.
 struct Waiter {
     bool ok = true;
-    __device__ __forceinline__ void warp(uint64_t* b, uint32_t use) {
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait_tries(smem_u32(b), use & 1u));
+    __device__ __forceinline__ void warp(uint64_t* b, uint32_t use) { at(smem_u32(b), use & 1u); }
+    __device__ __forceinline__ void at(uint32_t b, uint32_t parity) {
+        if (ok) ok = mbar_wait_tries(b, parity);
     }
+    __device__ __forceinline__ bool all() { return ok = __all_sync(0xffffffffu, ok) != 0; }
 };
 
 // Softmax of NCH chunks of 32 columns from chunk ch0 on of a row's scores, P over them and zeros in the other chunks.
@@ -365,7 +369,7 @@ struct TileLoader {
         }
         const uint32_t bar = smem_u32(&bars[kKvFull + st]);
         if (at >= kNS) wait.warp(&bars[kKvEmpty + st], phase ^ 1u);
-        if (!wait.ok) return;
+        if (!wait.all()) return;
         at += 2;
         const uint32_t here = __ballot_sync(0xffffffffu, ids >= 0) >> (page & 31), n = __popc(here & ((2u << (n_page - 1)) - 1u));
         const bool one = elect_one();
@@ -504,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
     if (tid == 0) {
-        for (int s = 0; s < 4; ++s) {
+        for (int s = 0; s < 6; ++s) {
             mbar_init(&bars[kSFull + s], 1);
             mbar_init(&bars[kPFull + s], 4);
             mbar_init(&bars[kPvDone + s], 1);
@@ -645,7 +649,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         TileLoader<D> keys(a, &a.kmap, bars, smem_u32(sKV), 0);
         auto load_q = [&](const Item& it, int s, int tok, int head) {
             if (n_q[s] > 0) wait.warp(&bars[kQEmpty + s], n_q[s] - 1);
-            if (!wait.ok) return;
+            if (!wait.all()) return;
             const uint32_t bar = smem_u32(&bars[kQFull + s]);
             const int rows = kRows >> it.rep_log, boxed = (rows * a.inv_group >> 16) * a.group, copies = 1 << it.rep_log;
             const CUtensorMap* map = &a.qmap[it.rep_log];
@@ -713,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             if (it.slot < 2) turn ^= 1;
             const uint32_t ring = n_item % kRing;
             if (n_item >= kRing) wait.warp(&bars[kItemEmpty + ring], n_item / kRing - 1);
-            if (!wait.ok) break;
+            if (!wait.all()) break;
             if (lane == 0) {
                 items[ring] = it;
                 mbar_arrive(&bars[kItemFull + ring]);
@@ -732,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             }
         }
         if (wait.ok && n_item >= kRing) wait.warp(&bars[kItemEmpty + n_item % kRing], n_item / kRing - 1);
-        if (wait.ok && lane == 0) {
+        if (wait.all() && lane == 0) {
             items[n_item % kRing].stop = 1;
             mbar_arrive(&bars[kItemFull + n_item % kRing]);
         }
@@ -751,7 +755,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         TileLoader<D> vals(a, &a.vmap, bars, smem_u32(sKV), 1);
         for (uint32_t n_item = 0; wait.ok; ++n_item) {
             wait.warp(&bars[kItemFull + n_item % kRing], n_item / kRing);
-            if (!wait.ok) break;
+            if (!wait.all()) break;
             const Item it = items[n_item % kRing];
             if (it.stop) break;
             warp_arrive(&bars[kItemEmpty + n_item % kRing]);
@@ -766,19 +770,15 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     } else if (warp == kMmaWarp) {
         // ---- the products.  The warp runs as one, so that the operands stay in its uniform registers, and one lane issues.
         {
-            // Scores go to S0 and S1: a pair's slots to their own, a single slot's units to both in turn, so that the next
-            // unit's scores are computed under this one's softmax.  pend[b] is the product with V of the P in Sb, still to
-            // be issued; older: which of two came first.  This warp's instructions are on the way of every unit: its places
-            // in the rings are counted along, a pair's two buffers are two copies of the code, and the single units' code is
-            // one copy for both (as two it did not stay in the instruction cache: decodes took 15% longer).
-            struct Pending {
-                uint32_t full, phase;   // the values' barrier and its phase
-                uint32_t p_full, p_phase, p_done;
-                uint32_t acc, empty;    // barrier to release the values to, 0: not the last to use them
-                uint32_t o;             // O's columns
-                uint64_t desc;
-            } pend[2] = {};
-            uint32_t on = 0, older = 0, turn = 0, st = 0, phase = 0, n_q0 = 0, n_q1 = 0, n_s0 = 0, n_s1 = 0;
+            // The scores of successive (unit, slot)s go to the buffers in turn, and the product with V of the P that replaces
+            // them is issued before the buffer's next scores: the scores of the next one or two run under a softmax.  todo0
+            // is the oldest such product still to be issued, of n_todo, each described by a word.  This warp's
+            // instructions are on the way of every unit: its places in the rings are counted along, and the code is short
+            // (with more copies of it, it did not stay in the instruction cache).
+            enum : uint32_t { kUnit = 7, kPhase = 8, kAcc = 16, kRelease = 32, kSlot = 64, kVPhase = 128, kVStage = 8, kBufAt = 12 };
+            uint32_t n_todo = 0, todo0 = 0, todo1 = 0, todo2 = 0;
+            uint32_t buf = 0, st = 0, phase = 0, n_q0 = 0, n_q1 = 0;
+            uint32_t unit0 = 0, unit1 = 0, uphase0 = 0, uphase1 = 0;  // the slots' next units mod 3, and their barriers' phases
             const uint32_t id_s = idesc(kBf16, kKeys, false), id_o = idesc(kBf16, D, true), bar0 = smem_u32(bars);
             const uint64_t q_desc = desc_k(smem_u32(sQ)), k_desc = desc_k(smem_u32(sKV)), v_desc = desc_v(smem_u32(sKV));
             const bool leader = elect_one();
@@ -786,114 +786,96 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(b) : "memory");
             };
             auto ready = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(b, parity)) != 0; };
-            auto await = [&](uint32_t b, uint32_t parity) {
-                if (wait.ok) wait.ok = __all_sync(0xffffffffu, mbar_wait_tries(b, parity));
-            };
-            auto values = [&](uint32_t b) {
-                Pending p;
-                p.full = b ? pend[1].full : pend[0].full;
-                p.phase = b ? pend[1].phase : pend[0].phase;
-                p.p_full = b ? pend[1].p_full : pend[0].p_full;
-                p.p_phase = b ? pend[1].p_phase : pend[0].p_phase;
-                p.p_done = b ? pend[1].p_done : pend[0].p_done;
-                p.acc = b ? pend[1].acc : pend[0].acc;
-                p.empty = b ? pend[1].empty : pend[0].empty;
-                p.o = b ? pend[1].o : pend[0].o;
-                p.desc = b ? pend[1].desc : pend[0].desc;
-                await(p.p_full, p.p_phase);
-                await(p.full, p.phase);
-                on &= ~(1u << b);
-                if (!wait.ok) return;
+            auto values = [&]() {  // the oldest product with V
+                const uint32_t w = todo0, vst = w >> kVStage & 15u;
+                wait.at(bar0 + 8 * (kPFull + (w & kUnit)), w & kPhase ? 1u : 0u);
+                wait.at(bar0 + 8 * (kKvFull + vst), w & kVPhase ? 1u : 0u);
+                todo0 = todo1;
+                todo1 = todo2;
+                --n_todo;
                 fence_after();
                 if (leader) {
+                    const uint64_t dv = v_desc + vst * (Sh::kTile >> 4);
+                    const uint32_t o = tmem + Sh::kO + (w & kSlot ? D : 0), pp = tmem + (w >> kBufAt) * kKeys;
 #pragma unroll
-                    for (int i = 0; i < kKeys / 16; ++i)
-                        mma_ts(p.o, tmem + kS0 + b * kKeys + 8 * i, p.desc + 128 * i, id_o, i > 0 || p.acc);
-                    commit(p.p_done);
-                    if (p.empty) commit(p.empty);
+                    for (int i = 0; i < kKeys / 16; ++i) mma_ts(o, pp + 8 * i, dv + 128 * i, id_o, i > 0 || (w & kAcc));
+                    commit(bar0 + 8 * (kPvDone + (w & kUnit)));
+                    if (w & kRelease) commit(bar0 + 8 * (kKvEmpty + vst));
                 }
                 __syncwarp();
             };
-            auto scores = [&](uint32_t b, uint32_t sl, int u, int nu, bool last) {
-                if (u == 0) {
-                    await(bar0 + 8 * (kQFull + sl), (sl ? n_q1 : n_q0) & 1u);
-                    n_q0 += sl == 0;
-                    n_q1 += sl;
-                }
-                if (!wait.ok) return;
-                fence_after();
-                const uint32_t n = sl ? n_s1 : n_s0, sn = 8 * (2 * sl + (n & 1u));
-                n_s0 += sl == 0;
-                n_s1 += sl;
-                if (leader) {
-                    const uint64_t dq = q_desc + sl * (Sh::kTile >> 4), dk = k_desc + st * (Sh::kTile >> 4);
-#pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        const uint32_t off = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
-                        mma_ss(tmem + kS0 + b * kKeys, dq + off, dk + off, id_s, i > 0);
-                    }
-                    commit(bar0 + 8 * kSFull + sn);
-                    if (last) commit(bar0 + 8 * (kKvEmpty + st));
-                    if (u == nu - 1) commit(bar0 + 8 * (kQEmpty + sl));
-                }
-                __syncwarp();
-                Pending p;
-                p.full = bar0 + 8 * (kKvFull + st + 1);
-                p.phase = phase;
-                p.p_full = bar0 + 8 * kPFull + sn;
-                p.p_phase = n >> 1 & 1u;
-                p.p_done = bar0 + 8 * kPvDone + sn;
-                p.acc = u > 0;
-                p.empty = last ? bar0 + 8 * (kKvEmpty + st + 1) : 0;
-                p.o = tmem + kO0 + sl * D;
-                p.desc = v_desc + (st + 1) * (Sh::kTile >> 4);
-                if (b) pend[1] = p;
-                else pend[0] = p;
-                older = on ? 1 - b : b;
-                on |= 1u << b;
+            auto scores = [&](uint32_t sl, int u, int nu, bool last) {  // last: of this tile's users
+                                        if (u == 0) {
+                                            wait.at(bar0 + 8 * (kQFull + sl), (sl ? n_q1 : n_q0) & 1u);
+                                            n_q0 += sl == 0;
+                                            n_q1 += sl;
+                                        }
+                                        fence_after();
+                                        const uint32_t n = 3 * sl + (sl ? unit1 : unit0);
+                                        if (leader) {
+                                            const uint64_t dq = q_desc + sl * (Sh::kTile >> 4), dk = k_desc + st * (Sh::kTile >> 4);
+                                            const uint32_t d = tmem + buf * kKeys;
+                #pragma unroll
+                                            for (int i = 0; i < D / 16; ++i) {
+                                                const uint32_t off = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
+                                                mma_ss(d, dq + off, dk + off, id_s, i > 0);
+                                            }
+                                            commit(bar0 + 8 * (kSFull + n));
+                                            if (last) commit(bar0 + 8 * (kKvEmpty + st));
+                                            if (u == nu - 1) commit(bar0 + 8 * (kQEmpty + sl));
+                                        }
+                                        __syncwarp();
+                                        const uint32_t w = n | ((sl ? uphase1 : uphase0) ? kPhase : 0) | (u > 0 ? kAcc : 0) | (last ? kRelease : 0) |
+                                                           (sl ? kSlot : 0) | (phase ? kVPhase : 0) | (st + 1) << kVStage | buf << kBufAt;
+                                        if (n_todo == 0) todo0 = w;
+                                        else if (n_todo == 1) todo1 = w;
+                                        else todo2 = w;
+                                        ++n_todo;
+                                        buf = buf + 1 == Sh::kBuf ? 0 : buf + 1;
+                                        if (sl) {
+                                            if (++unit1 == 3) {
+                                                unit1 = 0;
+                                                uphase1 ^= 1u;
+                                            }
+                                        } else if (++unit0 == 3) {
+                                            unit0 = 0;
+                                            uphase0 ^= 1u;
+                                        }
             };
-            for (uint32_t n_item = 0; wait.ok; ++n_item) {
-                await(bar0 + 8 * (kItemFull + n_item % kRing), n_item / kRing & 1u);
-                if (!wait.ok) break;
+            for (uint32_t n_item = 0;; ++n_item) {
+                wait.at(bar0 + 8 * (kItemFull + n_item % kRing), n_item / kRing & 1u);
+                if (!wait.all()) break;
                 const volatile Item& it = items[n_item % kRing];
-                const int stop = __shfl_sync(0xffffffffu, it.stop, 0), nu = stop ? 1 : __shfl_sync(0xffffffffu, it.nu, 0),
-                          slot = __shfl_sync(0xffffffffu, it.slot, 0);
-                if (!stop) warp_arrive(&bars[kItemEmpty + n_item % kRing]);
+                const int stop = __reduce_max_sync(0xffffffffu, it.stop), nu = __reduce_max_sync(0xffffffffu, it.nu),
+                          slot = __reduce_max_sync(0xffffffffu, it.slot);
+                if (stop) break;
+                warp_arrive(&bars[kItemEmpty + n_item % kRing]);
 #pragma unroll 1
                 for (int u = 0; u < nu && wait.ok; ++u) {
-                    // Products that have to go first: all at the end; those of single units, if in the other order, before a
-                    // pair; the one that still needs the Sb of a single unit, and while the unit's keys are on their way
-                    // whichever gets its probabilities.
                     const uint32_t keys = bar0 + 8 * (kKvFull + st);
-                    const bool alone = !stop && slot != 2;
-                    const uint32_t must = stop ? 3u : alone ? 1u << turn : u == 0 && on == 3u && older == 1u ? 3u : 0u;
-#pragma unroll 1
-                    for (uint32_t i = 0; wait.ok; ++i) {
-                        if ((on & must) == 0 && (!alone || ready(keys, phase))) break;
-                        const uint32_t f = on == 3u ? older : on >> 1;
-                        if ((on & must) || (on && ready(f ? pend[1].p_full : pend[0].p_full, f ? pend[1].p_phase : pend[0].p_phase)))
-                            values(f);
-                        else wait.ok = i < (1u << 24);
-                    }
-                    if (stop || !wait.ok) break;
-                    if (alone) {
-                        scores(turn, slot, u, nu, true);
-                        turn ^= 1u;
-                    } else {
-                        if (on & 1u) values(0u);
-                        await(keys, phase);
-                        scores(0u, 0, u, nu, false);
-                        if (on & 2u) values(1u);
-                        scores(1u, 1, u, nu, true);
+                    if (n_todo == Sh::kBuf) values();
+                    if (slot == 2) {
+                        wait.at(keys, phase);
+                        scores(0, u, nu, false);
+                        if (n_todo == Sh::kBuf) values();
+                        scores(1, u, nu, true);
+                    } else {  // a product that gets ready while the keys are on their way goes first
+                        for (uint32_t i = 0; !ready(keys, phase); ++i) {
+                            if (n_todo && ready(bar0 + 8 * (kPFull + (todo0 & kUnit)), todo0 & kPhase ? 1u : 0u)) values();
+                            else wait.ok &= i < (1u << 22);
+                            if (!wait.all()) break;
+                        }
+                        scores(slot, u, nu, true);
                     }
                     st += 2;
                     if (st == kNS) {
                         st = 0;
                         phase ^= 1u;
                     }
+                    wait.all();
                 }
-                if (stop) break;
             }
+            while (n_todo && wait.all()) values();
             if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
             if (leader) commit(bar0 + 8 * kDrain);
             __syncwarp();
@@ -905,19 +887,21 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         // ---- softmax of slot s; this thread's row of tensor memory is lane row
         const int s = warp >> 2, row = tid & (kRows - 1);
         const uint32_t lane_at = (uint32_t)(32 * (warp & 3)) << 16;
-        const uint32_t tO = tmem + kO0 + s * D + lane_at;
-        uint32_t n_s = 0, n_unit = 0, turn = 0;  // units of this slot, of all; the S of the next single unit
+        const uint32_t tO = tmem + Sh::kO + s * D + lane_at;
+        // units of all slots; the next unit's score buffer; this slot's next unit mod 3, and its barriers' phase
+        uint32_t n_unit = 0, buf = 0, unit = 0, uphase = 0;
         SlotSync wg_sync{&bars[kWg + s], 0, {}};
-        for (uint32_t n_item = 0; wait.ok && wg_sync.wait.ok; ++n_item) {
+        for (uint32_t n_item = 0;; ++n_item) {
             const uint32_t ring = n_item % kRing;
             wait.warp(&bars[kItemFull + ring], n_item / kRing);
-            if (!wait.ok) break;
+            wait.ok &= wg_sync.wait.ok;
+            if (!wait.all()) break;
             const Item it = items[ring];
             if (it.stop) break;
             if (it.slot != 2 && it.slot != s) {
                 warp_arrive(&bars[kItemEmpty + ring]);
                 n_unit += it.nu;
-                turn ^= it.nu & 1;
+                buf = (buf + it.nu) % Sh::kBuf;
                 continue;
             }
             const int half = it.slot == 2 ? s : 0;
@@ -937,17 +921,20 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             const int all1 = a.causal ? min(it.kv, it.pos + tok0 + 1) : it.kv;
             const int all0 = a.window > 0 ? (int)max((int64_t)0, (int64_t)it.pos + tok0 + ntok - a.window) : 0;
             float m = -INFINITY, l = 0.0f;
+            const uint32_t step = it.slot == 2 ? 2 : 1;
+            uint32_t b = (buf + (it.slot == 2 ? s : 0)) % Sh::kBuf;
+            buf = (buf + step * it.nu) % Sh::kBuf;
 #pragma unroll 1
-            for (int u = 0; u < it.nu; ++u, ++n_unit, ++n_s) {
+            for (int u = 0; u < it.nu; ++u, ++n_unit) {
                 const int t0 = (it.u0 + u) * kKeys;
                 const bool full = t0 >= all0 && t0 + kKeys <= all1;
-                const uint32_t sn = 2 * s + (n_s & 1), tS = tmem + kS0 + (it.slot == 2 ? s : turn) * kKeys + lane_at;
-                turn ^= it.slot != 2;
-                wait.warp(&bars[kSFull + sn], n_s >> 1);
+                const uint32_t sn = 3 * s + unit, tS = tmem + b * kKeys + lane_at;
+                b = (b + step) % Sh::kBuf;
+                wait.warp(&bars[kSFull + sn], uphase);
                 fence_after();
                 if (busy) {
                     auto rescale = [&](float f) {
-                        wait.warp(&bars[kPvDone + (sn ^ 1)], (n_s - 1) >> 1);
+                        wait.warp(&bars[kPvDone + 3 * s + (unit ? unit - 1 : 2)], unit ? uphase : uphase ^ 1u);
                         fence_after();
 #pragma unroll 1
                         for (int c = 0; c < D; c += 16) {
@@ -993,10 +980,14 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 }
                 fence_before();
                 warp_arrive(&bars[kPFull + sn]);
+                if (++unit == 3) {
+                    unit = 0;
+                    uphase ^= 1u;
+                }
             }
             // ---- the end of the item: O and l of this part
             if (it.nu > 0) {
-                wait.warp(&bars[kPvDone + 2 * s + ((n_s - 1) & 1)], (n_s - 1) >> 1);
+                wait.warp(&bars[kPvDone + 3 * s + (unit ? unit - 1 : 2)], unit ? uphase : uphase ^ 1u);
                 fence_after();
             }
             const bool poison = *reinterpret_cast<volatile int32_t*>(&items[ring].poison) != 0;
@@ -1141,7 +1132,6 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             if (*reinterpret_cast<volatile int*>(&last_flag[s]) == 0) continue;
             wg_sync = join_parts<kBf16, D>(a, part0, it.n_parts, rows, tok, head, scratch, wg_sync);
         }
-        wait.ok &= wg_sync.wait.ok;
         if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
     }
     fence_before();
