@@ -36,6 +36,19 @@ __device__ __forceinline__ bool mbar_test(uint32_t addr, uint32_t parity) {
     return done;
 }
 
+// Whether three have, their latencies overlapped.
+__device__ __forceinline__ bool mbar_test3(uint32_t a, uint32_t pa, uint32_t b, uint32_t pb, uint32_t c, uint32_t pc) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p, q, r;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 q, [%3], %4;\n\tmbarrier.test_wait.parity.shared::cta.b64 r, [%5], %6;\n\t"
+        "and.pred p, p, q;\n\tand.pred p, p, r;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(a), "r"(pa), "r"(b), "r"(pb), "r"(c), "r"(pc)
+        : "memory");
+    return done;
+}
+
 // Waits (bounded) until the phase of the given parity of an mbarrier has
 // completed; false if it gave up.  The clock is read only after a try that
 // failed (which itself waits a while).
@@ -68,9 +81,10 @@ __device__ __forceinline__ void mbar_init(uint64_t* b, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count));
 }
 
-__device__ __forceinline__ void mbar_arrive(uint64_t* b) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
+__device__ __forceinline__ void mbar_arrive_at(uint32_t addr) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(addr) : "memory");
 }
+__device__ __forceinline__ void mbar_arrive(uint64_t* b) { mbar_arrive_at(smem_u32(b)); }
 
 // Waits (bounded) for use u of a barrier that completes one phase per use.
 __device__ __forceinline__ bool mbar_wait_use(uint64_t* b, int64_t u) { return mbar_wait(smem_u32(b), (uint32_t)(u & 1)); }

@@ -105,10 +105,10 @@ struct Item {
     int32_t stop;
 };
 
-// The first three are [slot][number of the slot's unit mod 3]: up to three units of a slot are under way at once.
+// The first three are [slot][number of the slot's unit mod 3, of 4]: up to three units of a slot are under way at once.
 enum {
-    kSFull = 0, kPFull = 6, kPvDone = 12, kQFull = 18, kQEmpty = 20, kWg = 22, kItemFull = 24, kItemEmpty = 28, kDrain = 32,
-    kKvFull = 33, kKvEmpty = 43, kBars = 53
+    kSFull = 0, kPFull = 8, kPvDone = 16, kQFull = 24, kQEmpty = 26, kWg = 28, kItemFull = 30, kItemEmpty = 34, kDrain = 38,
+    kKvFull = 40, kKvEmpty = 50, kBars = 60
 };
 
 // The swizzled K-major tile of queries or keys: rows of 128 bytes, 8-row groups 1024 bytes apart.
@@ -298,7 +298,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, int ch0, bool full, in
         uint32_t z[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) z[i] = 0u;
-#pragma unroll 1
+#pragma unroll
         for (int q = 0; q < 4; ++q)
             if (q < ch0 || q >= ch0 + NCH) tmem_st16(tS + 16 * q, z);
     }
@@ -306,14 +306,17 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, int ch0, bool full, in
     tmem_wait_st();
 }
 
-// One step of a product (16 of its inner dimension), both operands in shared memory, or A in tensor memory.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t da, uint64_t db, uint32_t id, bool acc) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(da), "l"(db), "r"(id), "r"((uint32_t)acc));
+// One step of a product (16 of its inner dimension), both operands in shared memory, or A in tensor memory.  The upper
+// halves of the operands' descriptors are constants.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t da, uint32_t db, uint32_t upper, uint32_t id, bool acc) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\t"
+                 "mov.b64 db, {%2, %3};\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(d),
+                 "r"(da), "r"(db), "r"(upper), "r"(id), "r"((uint32_t)acc));
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t ta, uint64_t db, uint32_t id, bool acc) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(ta), "l"(db), "r"(id), "r"((uint32_t)acc));
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t ta, uint32_t db, uint32_t upper, uint32_t id, bool acc) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 db, {%2, %3};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}" ::"r"(d),
+                 "r"(ta), "r"(db), "r"(upper), "r"(id), "r"((uint32_t)acc));
 }
 
 __device__ __forceinline__ bool elect_one() {
@@ -337,14 +340,14 @@ struct TileLoader {
     int group;                  // ids: of pages 32 group ..
     int ids, ids_next;
     bool bad = false;
-    static constexpr int kNone = INT32_MIN;
+    static constexpr int kNone = INT32_MIN, kCopies = 4;
     __device__ __forceinline__ TileLoader(const AttnArgs& a_, const CUtensorMap* m, uint64_t* b, uint32_t t, uint32_t first)
         : a(a_), map(m), bars(b), tiles(t), st(first), phase(0), at(first) {
         page_log = a.bs_log < 7 ? 7 - a.bs_log : 0;
         n_page = 1 << page_log;
         box = kKeys >> page_log;
     }
-    // This lane's id of the pages of group g, -1 if no row sees any of its tokens.
+    // This lane's id of the pages of group g; kNone if no row sees any of its tokens.
     __device__ __forceinline__ int fetch(const Item& it, int g) const {
         const int64_t key = ((int64_t)g * 32 + (threadIdx.x & 31)) * box;
         return key < it.end && key + box > it.begin ? __ldg(a.table + (int64_t)it.r * a.ld_table + (key >> a.bs_log)) : kNone;
@@ -352,7 +355,7 @@ struct TileLoader {
     __device__ __forceinline__ void use(int raw) {
         const bool out = raw < 0 || raw >= a.n_blocks;
         bad |= out && raw != kNone;
-        ids = raw == kNone ? -1 : out ? (int)a.n_blocks : raw;  // past the end: the copy writes zeros
+        ids = out ? (int)a.n_blocks : raw;  // past the end: the copy reads nothing and writes zeros
     }
     __device__ __forceinline__ void begin(const Item& it) {
         group = (it.u0 << page_log) >> 5;
@@ -371,24 +374,36 @@ struct TileLoader {
         if (at >= kNS) wait.warp(&bars[kKvEmpty + st], phase ^ 1u);
         if (!wait.all()) return;
         at += 2;
-        const uint32_t here = __ballot_sync(0xffffffffu, ids >= 0) >> (page & 31), n = __popc(here & ((2u << (n_page - 1)) - 1u));
         const bool one = elect_one();
         if (one)
-            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n * box * (D * 2)) : "memory");
-        uint32_t dst = tiles + st * Shape<D>::kTile;
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)Shape<D>::kTile) : "memory");
+        const uint32_t dst = tiles + st * Shape<D>::kTile;
         const int within = (u * kKeys) & ((1 << a.bs_log) - 1);
-#pragma unroll 2
-        for (int i = 0; i < n_page; ++i, dst += box * 128) {
-            const int id = __shfl_sync(0xffffffffu, ids, (page & 31) + i);
-            if (one && id >= 0) {
+        auto copy = [&](int i, int id) {
 #pragma unroll
-                for (int half = 0; half < D / 64; ++half)
-                    asm volatile(
-                        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, "
-                        "%4, %5}], [%6];" ::"r"(dst + half * kHalf),
-                        "l"(map), "r"(half * 64), "r"(it.h), "r"(within), "r"(id), "r"(bar)
-                        : "memory");
+            for (int half = 0; half < D / 64; ++half)
+                asm volatile(
+                    "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, "
+                    "%5}], [%6];" ::"r"(dst + i * box * 128 + half * kHalf),
+                    "l"(map), "r"(half * 64), "r"(it.h), "r"(within), "r"(id), "r"(bar)
+                    : "memory");
+        };
+        // (straight code for kCopies pages at a time: with a branch per page a copy took 150 cycles)
+        int i = 0;
+#pragma unroll 1
+        for (; i + kCopies <= n_page; i += kCopies) {
+            int id[kCopies];
+#pragma unroll
+            for (int j = 0; j < kCopies; ++j) id[j] = __shfl_sync(0xffffffffu, ids, (page & 31) + i + j);
+            if (one) {
+#pragma unroll
+                for (int j = 0; j < kCopies; ++j) copy(i + j, id[j]);
             }
+        }
+#pragma unroll 1
+        for (; i < n_page; ++i) {
+            const int id = __shfl_sync(0xffffffffu, ids, (page & 31) + i);
+            if (one) copy(i, id);
         }
         __syncwarp();
         if ((st += 2) >= kNS) {
@@ -508,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
     if (tid == 0) {
-        for (int s = 0; s < 6; ++s) {
+        for (int s = 0; s < 8; ++s) {
             mbar_init(&bars[kSFull + s], 1);
             mbar_init(&bars[kPFull + s], 4);
             mbar_init(&bars[kPvDone + s], 1);
@@ -772,75 +787,84 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         {
             // The scores of successive (unit, slot)s go to the buffers in turn, and the product with V of the P that replaces
             // them is issued before the buffer's next scores: the scores of the next one or two run under a softmax.  todo0
-            // is the oldest such product still to be issued, of n_todo, each described by a word.  This warp's
-            // instructions are on the way of every unit: its places in the rings are counted along, and the code is short
-            // (with more copies of it, it did not stay in the instruction cache).
-            enum : uint32_t { kUnit = 7, kPhase = 8, kAcc = 16, kRelease = 32, kSlot = 64, kVPhase = 128, kVStage = 8, kBufAt = 12 };
+            // is the oldest such product still to be issued, of n_todo, each a word: its slot and the slot's unit mod 3
+            // (kSlotUnit, as the barriers are laid out), their phase, ...  This warp's instructions, six to nine cycles each, are
+            // on the way of every unit: its places in the rings are counted along, and the code is short (with more
+            // copies of it, it did not stay in the instruction cache).
+            enum : uint32_t { kSlotUnit = 7, kPhase = 8, kAcc = 16, kRelease = 32, kVPhase = 64, kVStage = 8, kBufAt = 12 };
+            constexpr uint32_t kTileDesc = Sh::kTile >> 4;
             uint32_t n_todo = 0, todo0 = 0, todo1 = 0, todo2 = 0;
-            uint32_t buf = 0, st = 0, phase = 0, n_q0 = 0, n_q1 = 0;
-            uint32_t unit0 = 0, unit1 = 0, uphase0 = 0, uphase1 = 0;  // the slots' next units mod 3, and their barriers' phases
+            uint32_t buf = 0, n_q0 = 0, n_q1 = 0;
+            uint32_t next0 = 0, next1 = 4;        // the slots' next units, as in a word
+            uint32_t v_word = 1u << kVStage;      // this unit's values: stage and phase, as in a word
             const uint32_t id_s = idesc(kBf16, kKeys, false), id_o = idesc(kBf16, D, true), bar0 = smem_u32(bars);
-            const uint64_t q_desc = desc_k(smem_u32(sQ)), k_desc = desc_k(smem_u32(sKV)), v_desc = desc_v(smem_u32(sKV));
+            const uint32_t q_desc = (uint32_t)desc_k(smem_u32(sQ)), k_desc0 = (uint32_t)desc_k(smem_u32(sKV)),
+                           v_desc = (uint32_t)desc_v(smem_u32(sKV));
+            uint32_t k_desc = k_desc0, k_bar = bar0 + 8 * kKvFull;  // this unit's keys
             const bool leader = elect_one();
             auto commit = [&](uint32_t b) {
                 asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(b) : "memory");
             };
             auto ready = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(b, parity)) != 0; };
-            auto values = [&]() {  // the oldest product with V
-                const uint32_t w = todo0, vst = w >> kVStage & 15u;
-                wait.at(bar0 + 8 * (kPFull + (w & kUnit)), w & kPhase ? 1u : 0u);
-                wait.at(bar0 + 8 * (kKvFull + vst), w & kVPhase ? 1u : 0u);
+            auto k_phase = [&]() { return v_word & kVPhase ? 1u : 0u; };
+            auto p_bar = [&]() { return bar0 + 8 * kPFull + 8 * (todo0 & kSlotUnit); };
+            auto p_phase = [&]() { return todo0 & kPhase ? 1u : 0u; };
+            auto v_bar = [&]() { return bar0 + 8 * kKvFull + 8 * (todo0 >> kVStage & 15u); };
+            auto v_phase = [&]() { return todo0 & kVPhase ? 1u : 0u; };
+            auto issue_values = [&]() {  // by the leader: the oldest product with V
+                const uint32_t dv = v_desc + (todo0 >> kVStage & 15u) * kTileDesc;
+                const uint32_t o = tmem + Sh::kO + (todo0 & 4u ? D : 0), pp = tmem + (todo0 >> kBufAt) * kKeys;
+#pragma unroll
+                for (int i = 0; i < kKeys / 16; ++i)
+                    mma_ts(o, pp + 8 * i, dv + 128 * i, (uint32_t)(desc_v(0) >> 32), id_o, i > 0 || (todo0 & kAcc));
+                commit(bar0 + 8 * kPvDone + 8 * (todo0 & kSlotUnit));
+                if (todo0 & kRelease) commit(v_bar() + 8 * (kKvEmpty - kKvFull));
+            };
+            auto issue_scores = [&](uint32_t sl, uint32_t next, bool item_end, bool last) {
+                const uint32_t dq = q_desc + sl * kTileDesc, d = tmem + buf * kKeys;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const uint32_t off = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
+                    mma_ss(d, dq + off, k_desc + off, (uint32_t)(desc_k(0) >> 32), id_s, i > 0);
+                }
+                commit(bar0 + 8 * kSFull + 8 * (next & kSlotUnit));
+                if (last) commit(k_bar + 8 * (kKvEmpty - kKvFull));
+                if (item_end) commit(bar0 + 8 * (kQEmpty + sl));
+            };
+            auto pop = [&]() {
                 todo0 = todo1;
                 todo1 = todo2;
                 --n_todo;
+            };
+            auto push = [&](uint32_t w) {
+                if (n_todo == 0) todo0 = w;
+                else if (n_todo == 1) todo1 = w;
+                else todo2 = w;
+                ++n_todo;
+                buf = buf + 1 == Sh::kBuf ? 0 : buf + 1;
+            };
+            auto advance = [&](uint32_t next) { return (next & 3u) == 2u ? (next - 2u) ^ kPhase : next + 1u; };
+            auto values = [&]() {
+                wait.at(p_bar(), p_phase());
+                wait.at(v_bar(), v_phase());
                 fence_after();
-                if (leader) {
-                    const uint64_t dv = v_desc + vst * (Sh::kTile >> 4);
-                    const uint32_t o = tmem + Sh::kO + (w & kSlot ? D : 0), pp = tmem + (w >> kBufAt) * kKeys;
-#pragma unroll
-                    for (int i = 0; i < kKeys / 16; ++i) mma_ts(o, pp + 8 * i, dv + 128 * i, id_o, i > 0 || (w & kAcc));
-                    commit(bar0 + 8 * (kPvDone + (w & kUnit)));
-                    if (w & kRelease) commit(bar0 + 8 * (kKvEmpty + vst));
-                }
+                if (leader) issue_values();
                 __syncwarp();
+                pop();
             };
             auto scores = [&](uint32_t sl, int u, int nu, bool last) {  // last: of this tile's users
-                                        if (u == 0) {
-                                            wait.at(bar0 + 8 * (kQFull + sl), (sl ? n_q1 : n_q0) & 1u);
-                                            n_q0 += sl == 0;
-                                            n_q1 += sl;
-                                        }
-                                        fence_after();
-                                        const uint32_t n = 3 * sl + (sl ? unit1 : unit0);
-                                        if (leader) {
-                                            const uint64_t dq = q_desc + sl * (Sh::kTile >> 4), dk = k_desc + st * (Sh::kTile >> 4);
-                                            const uint32_t d = tmem + buf * kKeys;
-                #pragma unroll
-                                            for (int i = 0; i < D / 16; ++i) {
-                                                const uint32_t off = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
-                                                mma_ss(d, dq + off, dk + off, id_s, i > 0);
-                                            }
-                                            commit(bar0 + 8 * (kSFull + n));
-                                            if (last) commit(bar0 + 8 * (kKvEmpty + st));
-                                            if (u == nu - 1) commit(bar0 + 8 * (kQEmpty + sl));
-                                        }
-                                        __syncwarp();
-                                        const uint32_t w = n | ((sl ? uphase1 : uphase0) ? kPhase : 0) | (u > 0 ? kAcc : 0) | (last ? kRelease : 0) |
-                                                           (sl ? kSlot : 0) | (phase ? kVPhase : 0) | (st + 1) << kVStage | buf << kBufAt;
-                                        if (n_todo == 0) todo0 = w;
-                                        else if (n_todo == 1) todo1 = w;
-                                        else todo2 = w;
-                                        ++n_todo;
-                                        buf = buf + 1 == Sh::kBuf ? 0 : buf + 1;
-                                        if (sl) {
-                                            if (++unit1 == 3) {
-                                                unit1 = 0;
-                                                uphase1 ^= 1u;
-                                            }
-                                        } else if (++unit0 == 3) {
-                                            unit0 = 0;
-                                            uphase0 ^= 1u;
-                                        }
+                if (u == 0) {
+                    wait.at(bar0 + 8 * (kQFull + sl), (sl ? n_q1 : n_q0) & 1u);
+                    n_q0 += sl == 0;
+                    n_q1 += sl;
+                }
+                const uint32_t next = sl ? next1 : next0;
+                fence_after();
+                if (leader) issue_scores(sl, next, u == nu - 1, last);
+                __syncwarp();
+                push(next | v_word | (u > 0 ? kAcc : 0) | (last ? kRelease : 0) | buf << kBufAt);
+                if (sl) next1 = advance(next);
+                else next0 = advance(next);
             };
             for (uint32_t n_item = 0;; ++n_item) {
                 wait.at(bar0 + 8 * (kItemFull + n_item % kRing), n_item / kRing & 1u);
@@ -851,29 +875,48 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 if (stop) break;
                 warp_arrive(&bars[kItemEmpty + n_item % kRing]);
 #pragma unroll 1
-                for (int u = 0; u < nu && wait.ok; ++u) {
-                    const uint32_t keys = bar0 + 8 * (kKvFull + st);
-                    if (n_todo == Sh::kBuf) values();
+                for (int u = 0; u < nu; ++u) {
                     if (slot == 2) {
-                        wait.at(keys, phase);
+                        if (n_todo == Sh::kBuf) values();
+                        wait.at(k_bar, k_phase());
                         scores(0, u, nu, false);
                         if (n_todo == Sh::kBuf) values();
                         scores(1, u, nu, true);
-                    } else {  // a product that gets ready while the keys are on their way goes first
-                        for (uint32_t i = 0; !ready(keys, phase); ++i) {
-                            if (n_todo && ready(bar0 + 8 * (kPFull + (todo0 & kUnit)), todo0 & kPhase ? 1u : 0u)) values();
+                    } else if (u > 0 && n_todo == Sh::kBuf &&
+                               __all_sync(0xffffffffu, mbar_test3(p_bar(), p_phase(), v_bar(), v_phase(), k_bar, k_phase()))) {
+                        // all that the oldest product and these scores need is there
+                        const uint32_t next = slot ? next1 : next0;
+                        fence_after();
+                        if (leader) {
+                            issue_values();
+                            issue_scores(slot, next, u == nu - 1, true);
+                        }
+                        __syncwarp();
+                        pop();
+                        push(next | v_word | kAcc | kRelease | buf << kBufAt);
+                        if (slot) next1 = advance(next);
+                        else next0 = advance(next);
+                    } else {
+                        if (n_todo == Sh::kBuf) values();
+                        // a product that gets ready while the keys are on their way goes first
+                        for (uint32_t i = 0; !ready(k_bar, k_phase()); ++i) {
+                            if (n_todo && ready(p_bar(), p_phase())) values();
                             else wait.ok &= i < (1u << 22);
                             if (!wait.all()) break;
                         }
                         scores(slot, u, nu, true);
                     }
-                    st += 2;
-                    if (st == kNS) {
-                        st = 0;
-                        phase ^= 1u;
+                    k_desc += 2 * kTileDesc;
+                    k_bar += 16;
+                    v_word += 2u << kVStage;
+                    if (k_bar == bar0 + 8 * (kKvFull + kNS)) {
+                        k_desc = k_desc0;
+                        k_bar = bar0 + 8 * kKvFull;
+                        v_word = (v_word - ((uint32_t)kNS << kVStage)) ^ kVPhase;
                     }
-                    wait.all();
+                    if (!wait.all()) break;
                 }
+                if (!wait.ok) break;
             }
             while (n_todo && wait.all()) values();
             if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
@@ -890,6 +933,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         const uint32_t tO = tmem + Sh::kO + s * D + lane_at;
         // units of all slots; the next unit's score buffer; this slot's next unit mod 3, and its barriers' phase
         uint32_t n_unit = 0, buf = 0, unit = 0, uphase = 0;
+        const uint32_t slot_bars = smem_u32(bars) + 32 * s;
         SlotSync wg_sync{&bars[kWg + s], 0, {}};
         for (uint32_t n_item = 0;; ++n_item) {
             const uint32_t ring = n_item % kRing;
@@ -924,17 +968,18 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             const uint32_t step = it.slot == 2 ? 2 : 1;
             uint32_t b = (buf + (it.slot == 2 ? s : 0)) % Sh::kBuf;
             buf = (buf + step * it.nu) % Sh::kBuf;
+            int t0 = it.u0 * kKeys;
 #pragma unroll 1
-            for (int u = 0; u < it.nu; ++u, ++n_unit) {
-                const int t0 = (it.u0 + u) * kKeys;
+            for (int u = 0; u < it.nu; ++u, ++n_unit, t0 += kKeys) {
                 const bool full = t0 >= all0 && t0 + kKeys <= all1;
-                const uint32_t sn = 3 * s + unit, tS = tmem + b * kKeys + lane_at;
-                b = (b + step) % Sh::kBuf;
-                wait.warp(&bars[kSFull + sn], uphase);
+                const uint32_t at = slot_bars + 8 * unit, tS = tmem + b * kKeys + lane_at;  // the unit's barriers
+                b += step;
+                if (b >= Sh::kBuf) b -= Sh::kBuf;
+                wait.at(at + 8 * kSFull, uphase);
                 fence_after();
                 if (busy) {
                     auto rescale = [&](float f) {
-                        wait.warp(&bars[kPvDone + 3 * s + (unit ? unit - 1 : 2)], unit ? uphase : uphase ^ 1u);
+                        wait.warp(&bars[kPvDone + 4 * s + (unit ? unit - 1 : 2)], unit ? uphase : uphase ^ 1u);
                         fence_after();
 #pragma unroll 1
                         for (int c = 0; c < D; c += 16) {
@@ -979,7 +1024,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 fence_before();
-                warp_arrive(&bars[kPFull + sn]);
+                __syncwarp();
+                if (lane == 0) mbar_arrive_at(at + 8 * kPFull);
                 if (++unit == 3) {
                     unit = 0;
                     uphase ^= 1u;
@@ -987,7 +1033,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             }
             // ---- the end of the item: O and l of this part
             if (it.nu > 0) {
-                wait.warp(&bars[kPvDone + 3 * s + (unit ? unit - 1 : 2)], unit ? uphase : uphase ^ 1u);
+                wait.warp(&bars[kPvDone + 4 * s + (unit ? unit - 1 : 2)], unit ? uphase : uphase ^ 1u);
                 fence_after();
             }
             const bool poison = *reinterpret_cast<volatile int32_t*>(&items[ring].poison) != 0;
