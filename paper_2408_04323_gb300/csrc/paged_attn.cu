@@ -176,6 +176,11 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
     const uint32_t e = kBf16 ? 0x7F807F80u : 0x7C007C00u;
     return __vcmpeq2(~w & e, 0u);
 }
+// Bits 15 and 31 set where a half's exponent is all ones (a carry out of it), other bits anything.
+template <bool kBf16>
+__device__ __forceinline__ uint32_t top_exponent(uint32_t w) {
+    return kBf16 ? (w & 0x7F807F80u) + 0x00800080u : (w & 0x7C007C00u) + 0x04000400u;
+}
 template <bool kBf16>
 __device__ __forceinline__ float value16(uint16_t x) {
     return kBf16 ? __bfloat162float(__ushort_as_bfloat16(x)) : __half2float(__ushort_as_half(x));
@@ -441,6 +446,49 @@ __device__ __forceinline__ float* lse_row(const AttnArgs& a, int tok, int head, 
     return a.lse + (int64_t)(tok + t) * a.n_heads + head + q - t * a.group;
 }
 
+// The weighted sums of V parts of rows q0 .. q0 + nq - 1 (weights w [row][V]).  A thread has four columns of R rows, 128 /
+// (D / 4) apart, with P parts of each in flight.
+template <bool kBf16, int D, int R, int P>
+__device__ __forceinline__ void join_rows(const AttnArgs& a, const float* part, const float* w, int V, int q0, int nq, int tok,
+                                          int head) {
+    constexpr int kGroups = D / 4, kStep = kRows / kGroups;
+    const int row = threadIdx.x & (kRows - 1), c = row % kGroups;
+#pragma unroll 1
+    for (int q = row / kGroups; q < nq; q += R * kStep) {
+        float4 acc[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int p0 = 0; p0 < V; p0 += P) {
+            float4 v[P][R];
+            float f[P][R];
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const int pt = min(p0 + p, V - 1);  // past the last part, or row: the last one's, not used
+                const float4* src = reinterpret_cast<const float4*>(part_buf<D>(part, pt)) + q0 * kGroups + c;
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    const int r = min(q + i * kStep, nq - 1);
+                    v[p][i] = __ldcg(src + r * kGroups);
+                    f[p][i] = w[r * V + pt];
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+                if (p0 + p < V)
+#pragma unroll
+                    for (int i = 0; i < R; ++i)
+                        acc[i] = make_float4(fmaf(f[p][i], v[p][i].x, acc[i].x), fmaf(f[p][i], v[p][i].y, acc[i].y),
+                                             fmaf(f[p][i], v[p][i].z, acc[i].z), fmaf(f[p][i], v[p][i].w, acc[i].w));
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (q + i * kStep < nq)
+                *reinterpret_cast<uint2*>(out_row(a, tok, head, q0 + q + i * kStep) + 4 * c) =
+                    make_uint2(pack16<kBf16>(acc[i].x, acc[i].y), pack16<kBf16>(acc[i].z, acc[i].w));
+    }
+}
+
 // The V parts of a split item's rows, joined by the slot whose part came last: per row the parts' common maximum and sum
 // and each part's weight (a thread per row, into the scratch), then the weighted sums, a warp over several rows.
 template <bool kBf16, int D>
@@ -451,7 +499,32 @@ __device__ __noinline__ SlotSync join_parts(const AttnArgs& a, const float* part
     for (int q0 = 0; q0 < rows; q0 += batch) {
         const int nq = min(batch, rows - q0);
         if (q0 > 0) sync();
-        if (row < nq) {
+        if (nq <= 8) {
+            // few rows: a warp per row, a lane per part
+#pragma unroll 1
+            for (int q = row >> 5; q < nq; q += kRows / 32) {
+                float M = -INFINITY, L = 0.0f;
+#pragma unroll 1
+                for (int i = row & 31; i < V; i += 32) {
+                    const float2 v = __ldcg(reinterpret_cast<const float2*>(part_buf<D>(part, i) + kRows * D) + q0 + q);
+                    const float Mn = fmaxf(M, v.x), Ms = finite_or_zero(Mn);
+                    L = fmaf(L, exp2_hw(M - Ms), exp2_hw(v.x - Ms) * v.y);
+                    M = Mn;
+                    w[q * V + i] = v.x;
+                }
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) {
+                    const float Mo = __shfl_xor_sync(0xffffffffu, M, d), Lo = __shfl_xor_sync(0xffffffffu, L, d);
+                    const float Mn = fmaxf(M, Mo), Ms = finite_or_zero(Mn);
+                    L = L * exp2_hw(M - Ms) + Lo * exp2_hw(Mo - Ms);
+                    M = Mn;
+                }
+                const float inv = inverse_sum(L), Ms = finite_or_zero(M);
+#pragma unroll 1
+                for (int i = row & 31; i < V; i += 32) w[q * V + i] = exp2_hw(w[q * V + i] - Ms) * inv;
+                if (a.lse && (row & 31) == 0) *lse_row(a, tok, head, q0 + q) = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+            }
+        } else if (row < nq) {
             float M = -INFINITY, L = 0.0f;
 #pragma unroll 1
             for (int i0 = 0; i0 < V; i0 += 8) {
@@ -474,31 +547,8 @@ __device__ __noinline__ SlotSync join_parts(const AttnArgs& a, const float* part
             if (a.lse) *lse_row(a, tok, head, q0 + row) = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
         }
         sync();
-        // a thread has four columns of a row, four rows (of this many apart) at a time with two parts each in flight
-        constexpr int kGroups = D / 4, kStep = kRows / kGroups, kR = 4;
-        const int c = row % kGroups;
-#pragma unroll 1
-        for (int q = row / kGroups; q < nq; q += kR * kStep) {
-            float4 acc[kR];
-#pragma unroll
-            for (int i = 0; i < kR; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-            for (int p = 0; p < V; ++p) {
-                const float4* src = reinterpret_cast<const float4*>(part_buf<D>(part, p) + q0 * D) + c;
-#pragma unroll
-                for (int i = 0; i < kR; ++i) {
-                    const int r = min(q + i * kStep, nq - 1);  // past the last row: the last one, not stored
-                    const float4 v = __ldcg(src + r * kGroups);
-                    const float f = w[r * V + p];
-                    acc[i] = make_float4(fmaf(f, v.x, acc[i].x), fmaf(f, v.y, acc[i].y), fmaf(f, v.z, acc[i].z), fmaf(f, v.w, acc[i].w));
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kR; ++i)
-                if (q + i * kStep < nq)
-                    *reinterpret_cast<uint2*>(out_row(a, tok, head, q0 + q + i * kStep) + 4 * c) =
-                        make_uint2(pack16<kBf16>(acc[i].x, acc[i].y), pack16<kBf16>(acc[i].z, acc[i].w));
-        }
+        if (nq <= 8) join_rows<kBf16, D, 2, 8>(a, part, w, V, q0, nq, tok, head);
+        else join_rows<kBf16, D, 4, 2>(a, part, w, V, q0, nq, tok, head);
     }
     return sync;
 }
@@ -1008,16 +1058,19 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
 #pragma unroll 4
                         for (int c = 0; c < D / 8; ++c) v[(c / 8) * (kHalf / 16) + (c ^ row) % 8] = make_uint4(0, 0, 0, 0);
                     } else if (key < all0 || key >= all1) {
-#pragma unroll 2
+                        uint32_t any = 0;
+#pragma unroll 4
                         for (int c = 0; c < D / 8; ++c) {
-                            uint4* at = v + (c / 8) * (kHalf / 16) + ((c ^ row) & 7);
-                            const uint4 w = *at;
-                            const uint4 bad = make_uint4(not_finite<kBf16>(w.x), not_finite<kBf16>(w.y), not_finite<kBf16>(w.z),
-                                                         not_finite<kBf16>(w.w));
-                            if (bad.x | bad.y | bad.z | bad.w) {
-                                *reinterpret_cast<volatile int32_t*>(&items[ring].poison) = 1;  // before the zero can be seen
-                                __threadfence_block();
-                                *at = make_uint4(w.x & ~bad.x, w.y & ~bad.y, w.z & ~bad.z, w.w & ~bad.w);
+                            const uint4 w = v[(c / 8) * (kHalf / 16) + (c ^ row) % 8];
+                            any |= top_exponent<kBf16>(w.x) | top_exponent<kBf16>(w.y) | top_exponent<kBf16>(w.z) | top_exponent<kBf16>(w.w);
+                        }
+                        if (any & 0x80008000u) {
+                            *reinterpret_cast<volatile int32_t*>(&items[ring].poison) = 1;  // before the zeros can be seen
+                            __threadfence_block();
+#pragma unroll 1
+                            for (int c = 0; c < D / 2; ++c) {
+                                uint32_t* at32 = reinterpret_cast<uint32_t*>(v + (c / 32) * (kHalf / 16)) + c % 32;
+                                *at32 &= ~not_finite<kBf16>(*at32);
                             }
                         }
                     }
