@@ -52,7 +52,8 @@ constexpr int kThreads = 384;      // three warpgroups: the two softmax ones tak
 constexpr int kSoftmaxRegs = 200, kOtherRegs = 104;  // 2 * 200 + 104 = 3 * 168, what the block is launched with
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kValueWarp = 10;
 constexpr int kRing = 4;         // items handed from the load warp to the others
-constexpr int kItemCost = 1;     // an item's start and end, in units
+constexpr int kItemCost = 1;     // an item's start and end, in units,
+constexpr int kPairCost = 5;     // and a pair's, with the tiles along its diagonal
 constexpr int kMinRange = 4;     // units that a CTA takes at least
 constexpr int kSnap = 2;         // a cut this close to an item's ends moves there,
 constexpr int kPairSnap = 6;     // or to those of a pair, whose parts are 256 rows
@@ -210,6 +211,10 @@ __device__ __forceinline__ void seen_keys(const AttnArgs& a, int kv, int n, int 
     end = a.causal ? (int)min((int64_t)kv, p0 + nt) : kv;
     begin = a.window > 0 ? (int)max((int64_t)0, p0 + 1 - a.window) : 0;
     if (end <= begin) begin = end = 0;
+}
+// The cost, in units, of item j of n tokens beside its units.
+__device__ __forceinline__ int item_cost(const AttnArgs& a, int n, int j) {
+    return n - j * 2 * a.toks > a.toks ? kPairCost : kItemCost;
 }
 __device__ __forceinline__ int item_units(const AttnArgs& a, int kv, int n, int j) {
     const int per = 2 * a.toks;
@@ -612,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         const int r = tid * k + i;
         const Req q = load_req(a, r, blockIdx.x == 0);
         if (k == 1) req_s[tid] = q;
-        if (q.n > 0 && q.n <= per) mine += kItemCost + item_units(a, q.kv, q.n, 0);
+        if (q.n > 0 && q.n <= per) mine += item_cost(a, q.n, 0) + item_units(a, q.kv, q.n, 0);
         uint32_t big = __ballot_sync(0xffffffffu, q.n > per);
         while (big) {
             const int src = __ffs(big) - 1;
@@ -621,7 +626,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             int64_t c = 0;
             const int m = (n + per - 1) / per;
 #pragma unroll 1
-            for (int j = lane; j < m; j += 32) c += kItemCost + item_units(a, kv, n, j);
+            for (int j = lane; j < m; j += 32) c += item_cost(a, n, j) + item_units(a, kv, n, j);
 #pragma unroll
             for (int d = 16; d > 0; d >>= 1) c += __shfl_xor_sync(0xffffffffu, c, d);
             if (lane == src) mine += c;
@@ -686,7 +691,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 const Req q = get(r);
 #pragma unroll 1
                 for (int j0 = 0; j0 * per < q.n && !found; j0 += 32) {
-                    const int64_t c = (j0 + lane) * per < q.n ? kItemCost + item_units(a, q.kv, q.n, j0 + lane) : 0;
+                    const int64_t c = (j0 + lane) * per < q.n ? item_cost(a, q.n, j0 + lane) + item_units(a, q.kv, q.n, j0 + lane) : 0;
                     int64_t s = c;
                     if (q.n > per) {
 #pragma unroll
@@ -760,7 +765,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             it.rep_log = it.ntok * a.group <= kRows / 4 ? 2 : it.ntok * a.group <= kRows / 2 ? 1 : 0;
             it.poison = it.stop = 0;
             const int t0 = it.begin / kKeys, units = (it.end + kKeys - 1) / kKeys - t0;
-            const int64_t s = p + kItemCost;  // where its units start
+            const int64_t s = p + item_cost(a, q.n, j);  // where its units start
             const int snap = it.ntok > a.toks ? kPairSnap : kSnap;
             auto cut = [&](int64_t b) {
                 return b >= s + units ? units : b - s < snap ? 0 : s + units - b < snap ? units : (int)(b - s);
