@@ -1,11 +1,13 @@
 // A paged key-value cache: block tables and slot maps of a serving step from
 // its requests' lengths, and the new tokens' keys and values into their slots.
+#include <algorithm>
+
 #include "internal.h"
 
 namespace {
 
 constexpr int kTabThreads = 1024;
-constexpr int kTabStaged = 24576;  // requests whose lengths fit a block's shared memory (192 KB)
+constexpr int kTabStaged = 16384;  // requests whose lengths go to shared memory (139 KB with the gaps)
 
 // What scoot_kv_tables takes, by value.
 struct TabArgs {
@@ -32,9 +34,11 @@ struct TabRequest {
     bool bad;
 };
 
-__device__ __forceinline__ TabRequest tab_request(const TabArgs& a, const int2* staged, int64_t r) {
+// (k_log: a thread's requests, for the gap after each thread's in shared memory that keeps their reads on
+// different banks.)
+__device__ __forceinline__ TabRequest tab_request(const TabArgs& a, const int2* staged, int k_log, int64_t r) {
     TabRequest q;
-    const int2 len = staged ? staged[r] : make_int2(a.cached[r], a.fresh[r]);
+    const int2 len = staged ? staged[r + (r >> k_log)] : make_int2(a.cached[r], a.fresh[r]);
     q.cached = len.x;
     q.fresh = len.y;
     const int64_t total = (int64_t)q.cached + q.fresh;
@@ -50,7 +54,7 @@ __device__ __forceinline__ TabRequest tab_request(const TabArgs& a, const int2* 
 // passes t, and its block, when the request does not hold it yet, is the free
 // one at the running sum of the blocks lacked before it: both sums run over
 // all requests.  Every block of the grid takes them for itself (thread i over
-// k consecutive requests, then a scan of the 1024 threads' sums), which costs
+// k consecutive requests, k a power of two, then a scan of the 1024 threads' sums), which costs
 // a read of 8 bytes per request from L2 where passing them on would cost a
 // second launch, and then serves its own share of the batch's tokens: a binary
 // search of the threads' sums, and a walk over the k requests of the one found.
@@ -64,17 +68,19 @@ __global__ void __launch_bounds__(kTabThreads) kv_tables_kernel(const TabArgs a)
     __shared__ int64_t warp_tok[32], warp_blk[32];
     __shared__ unsigned long long taken, refused;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int64_t k = (a.n_req + kTabThreads - 1) / kTabThreads;
+    int k_log = 0;
+    while (((int64_t)kTabThreads << k_log) < a.n_req) ++k_log;
+    const int64_t k = (int64_t)1 << k_log;
     const int64_t r0 = min((int64_t)a.n_req, tid * k), r1 = min((int64_t)a.n_req, r0 + k);
     if (tid == 0) taken = refused = 0;
     const int2* staged = a.n_req <= kTabStaged ? staged_s : nullptr;
     if (staged) {
-        for (int r = tid; r < a.n_req; r += kTabThreads) staged_s[r] = make_int2(a.cached[r], a.fresh[r]);
+        for (int r = tid; r < a.n_req; r += kTabThreads) staged_s[r + (r >> k_log)] = make_int2(a.cached[r], a.fresh[r]);
         __syncthreads();
     }
     int64_t tok = 0, blk = 0;
     for (int64_t r = r0; r < r1; ++r) {
-        const TabRequest q = tab_request(a, staged, r);
+        const TabRequest q = tab_request(a, staged, k_log, r);
         tok += q.fresh;
         blk += q.need;
     }
@@ -121,7 +127,7 @@ __global__ void __launch_bounds__(kTabThreads) kv_tables_kernel(const TabArgs a)
     if (mine || blockIdx.x == 0) {
         int64_t t = tok - my_tok, b = blk - my_blk, got = 0, lost = 0;
         for (int64_t r = r0; r < r1; ++r) {
-            const TabRequest q = tab_request(a, staged, r);
+            const TabRequest q = tab_request(a, staged, k_log, r);
             const bool fits = !q.bad && (q.need == 0 || b + q.need <= a.n_free);
             if (mine) {
                 a.query_start[r] = (int32_t)t;
@@ -169,11 +175,11 @@ __global__ void __launch_bounds__(kTabThreads) kv_tables_kernel(const TabArgs a)
             }
             int64_t start = lo ? tok_end[lo - 1] : 0, base = lo ? blk_end[lo - 1] : 0;
             int64_t r = lo * k;
-            TabRequest q = tab_request(a, staged, r);
+            TabRequest q = tab_request(a, staged, k_log, r);
             while (start + q.fresh <= t) {
                 start += q.fresh;
                 base += q.need;
-                q = tab_request(a, staged, ++r);
+                q = tab_request(a, staged, k_log, ++r);
             }
             const int64_t p = q.cached + (t - start);
             const bool fits = !q.bad && (q.need == 0 || base + q.need <= a.n_free);
@@ -297,10 +303,10 @@ scoot_status scoot_kv_tables(scoot_ctx* ctx, const int32_t* cached_len, const in
     int64_t blocks = (n_tokens + kTabThreads - 1) / kTabThreads;
     if (blocks > sms) blocks = sms;
     if (blocks < 1) blocks = 1;
-    const size_t smem = n_req <= kTabStaged ? (size_t)n_req * sizeof(int2) : 0;
+    const size_t smem = n_req <= kTabStaged ? (size_t)(n_req + std::min(n_req, kTabThreads)) * sizeof(int2) : 0;
     if (smem > 32768)  // beyond what a block has without asking, beside its static part
         SCOOT_CUDA(ctx, cudaFuncSetAttribute(kv_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)(kTabStaged * sizeof(int2))));
+                                             (int)((kTabStaged + kTabThreads) * sizeof(int2))));
     kv_tables_kernel<<<(unsigned)blocks, kTabThreads, smem, static_cast<cudaStream_t>(stream)>>>(a);
     SCOOT_LAUNCHED(ctx);
     return SCOOT_OK;
