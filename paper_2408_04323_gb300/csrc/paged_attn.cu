@@ -160,7 +160,7 @@ __device__ __forceinline__ float exp2_hw(float x) {
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.0f : m; }
 
 // 1 / l, 0 for a row that sees nothing (NaN stays).
-__device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : __fdividef(1.0f, l); }
 
 template <bool kBf16>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
@@ -527,7 +527,7 @@ __device__ __noinline__ SlotSync join_parts(const AttnArgs& a, const float* part
                 const float inv = inverse_sum(L), Ms = finite_or_zero(M);
 #pragma unroll 1
                 for (int i = row & 31; i < V; i += 32) w[q * V + i] = exp2_hw(w[q * V + i] - Ms) * inv;
-                if (a.lse && (row & 31) == 0) *lse_row(a, tok, head, q0 + q) = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+                if (a.lse && (row & 31) == 0) *lse_row(a, tok, head, q0 + q) = L == 0.0f ? -INFINITY : (M + __log2f(L)) * kLn2;
             }
         } else if (row < nq) {
             float M = -INFINITY, L = 0.0f;
@@ -549,7 +549,7 @@ __device__ __noinline__ SlotSync join_parts(const AttnArgs& a, const float* part
             const float inv = inverse_sum(L), Ms = finite_or_zero(M);
 #pragma unroll 1
             for (int i = 0; i < V; ++i) w[row * V + i] = exp2_hw(w[row * V + i] - Ms) * inv;
-            if (a.lse) *lse_row(a, tok, head, q0 + row) = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+            if (a.lse) *lse_row(a, tok, head, q0 + row) = L == 0.0f ? -INFINITY : (M + __log2f(L)) * kLn2;
         }
         sync();
         if (nq <= 8) join_rows<kBf16, D, 2, 8>(a, part, w, V, q0, nq, tok, head);
@@ -1152,10 +1152,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                     const float2 v = ml_s[s][c * per_copy + rr];
                     L = fmaf(exp2_hw(v.x - Ms), v.y, L);
                 }
-                const float w = exp2_hw(m - Ms), f = !whole ? w : L == 0.0f ? 0.0f : w / L;
+                const float w = exp2_hw(m - Ms), f = whole ? w * inverse_sum(L) : w;
                 if (copy == 0 && live) {
                     if (!whole) *reinterpret_cast<float2*>(buf + kRows * D + 2 * rr) = make_float2(M, L);
-                    else if (a.lse) *lse_row(a, tok, head, rr) = L == 0.0f ? -INFINITY : (M + log2f(L)) * kLn2;
+                    else if (a.lse) *lse_row(a, tok, head, rr) = L == 0.0f ? -INFINITY : (M + __log2f(L)) * kLn2;
                 }
                 const int width = used <= 32 ? min(D, 128) : used <= 64 ? 64 : 32, groups = width / 4;
                 const int g_log = 31 - __clz(groups);
@@ -1206,7 +1206,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                                                pack16<kBf16>(o[i + 4] * inv, o[i + 5] * inv), pack16<kBf16>(o[i + 6] * inv, o[i + 7] * inv));
                         }
                     }
-                    if (live && a.lse) *lse_row(a, tok, head, rr) = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+                    if (live && a.lse) *lse_row(a, tok, head, rr) = l == 0.0f ? -INFINITY : (m + __log2f(l)) * kLn2;
                 }
             } else if (busy) {
 #pragma unroll 1
