@@ -9,7 +9,7 @@
 // hold, and l and O carry the same factor, so that O / l is unchanged.
 //
 // Rows.  A query head's tokens and the G heads that share a key-value head are all rows of one product (row = token * G +
-// head), so keys and values are read once for the group.  A CTA has two slots of 128 rows, each with its own S, O and four
+// head), so keys and values are read once for the group.  A CTA has two slots of 128 rows, each with its own O and four
 // softmax warps:
 //   * more than 128 rows (a chunk of a prompt): a pair, both slots against the same tile, so that one's softmax runs
 //     under the other's products;
@@ -17,27 +17,35 @@
 //     rows are loaded two or four times over, and the copy in lanes 32 w .. serves the w-th part of the tile's keys as
 //     rows of its own, with its own m, l and O: the exponentials, which one warp would have taken for the whole tile,
 //     are spread over the four.  The copies are joined at the end like the parts of a split item.
+// Scores go to two buffers in tensor memory in turn, three with heads of 64, so that the next ones are computed under a
+// softmax.
 //
 // Work.  An item is a (key-value head, request, up to 256 rows), its units the tiles of keys that its rows see.  All
-// units in a row, head by head and request by request, with kItemCost extra per item, are cut into equal ranges, one per
+// units in a row, head by head and request by request, with an extra cost per item, are cut into equal ranges, one per
 // SM (a cut close to an item's start or end moves there): long sequences are split, short ones follow one another,
-// whatever the batch.  Each CTA takes the sums over
-// the requests for itself (lengths are on the device), so the call is one launch.  An item that lies in several ranges
-// leaves its parts (O, m, l) in the workspace, and the CTA that comes last (a counter per item) joins them in the
-// ranges' order, so that the result does not depend on who was last.
+// whatever the batch.  Each CTA takes the sums over the requests for itself (lengths are on the device), so the call is
+// one launch.  An item that lies in several ranges leaves its parts (O, m, l) in the workspace, and the CTA that comes last
+// (a counter per item) joins them in the ranges' order, so that the result does not depend on who was last.
 //
-// Warps 0-3 and 4-7: softmax of slots 0 and 1.  Warp 8: the products (one thread).  Warp 9: the items, and the copies:
-// pages of keys and values by TMA into a ring of tiles (128-byte swizzle), a box of up to 128 tokens x 64 dimensions
-// per page and half head; queries likewise.
+// Warps 0-3 and 4-7: softmax of slots 0 and 1.  Warp 8: the products.  Warp 9: the items, and the copies of queries and
+// keys; warp 10: those of values.  A tile comes page by page through the block table, by TMA into a ring (128-byte
+// swizzle), a box of up to 128 tokens x 64 dimensions per page and half head.
 //
 // Values of keys that some row may not see: a probability of 0 times an infinity or NaN is NaN, so the value tiles at
 // the ends of the sequence and along the diagonal are looked through first: rows past the ends are set to zero, and a
 // value that is not finite is replaced by zero and the item marked; rows that do see it add it at the end.
+//
+// What bounds it, as measured (heads of 128 in blocks of 16, four query heads per key-value head, bf16):
+//   * 256 sequences of 64 to 2560 tokens, one new token each: 220 us, 6.3 TB/s, 92% of the copy rate: HBM (a tile of
+//     64 KB per SM in 2700 cycles; scores, softmax and products of one row group take 1500).
+//   * a chunk of 8192 tokens over 8192 cached ones: 1.02 ms, 1610 TFLOP/s, 86% of the library's large product: shared
+//     memory, which feeds both operands of Q K^T (128 bytes a cycle), and the way scores - softmax - values of a slot (3000
+//     cycles for 2048 of products).
+//   * prompts in a window and small batches: starts and ends of items (about 5 us of a call: ranges, first tile, last
+//     join) and 1400 cycles of softmax per tile.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
-
-#include <cfloat>
 
 #include "internal.h"
 #include "mbarrier.cuh"
@@ -46,8 +54,8 @@ namespace {
 
 using namespace scoot_dev;
 
-constexpr int kRows = 128;       // rows of a slot: the MMA's M and the TMEM lanes
-constexpr int kKeys = 128;       // keys of a tile
+constexpr int kRows = 128;         // rows of a slot: the MMA's M and the TMEM lanes
+constexpr int kKeys = 128;         // keys of a tile
 constexpr int kThreads = 384;      // three warpgroups: the two softmax ones take registers from the third
 constexpr int kSoftmaxRegs = 200, kOtherRegs = 104;  // 2 * 200 + 104 = 3 * 168, what the block is launched with
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kValueWarp = 10;
@@ -55,9 +63,9 @@ constexpr int kRing = 4;         // items handed from the load warp to the other
 constexpr int kItemCost = 1;     // an item's start and end, in units,
 constexpr int kPairCost = 5;     // and a pair's, with the tiles along its diagonal
 constexpr int kMinRange = 4;     // units that a CTA takes at least
-constexpr int kSnap = 2;         // a cut this close to an item's ends moves there,
-constexpr int kPairSnap = 6;     // or to those of a pair, whose parts are 256 rows
-constexpr int kBufs = 4;         // part buffers of a CTA (see part_buf)
+constexpr int kSnapMin = 2;      // a cut this close to an item's ends moves there; and up to this close, if it is
+constexpr int kSnapMax = 6;      // a quarter of a range: writing, counting and joining parts costs five to nine units
+constexpr int kBufs = 4;         // part buffers of a CTA
 constexpr int kScratch = 16384;  // bytes of a slot's scratch: 32 columns of sums of its rows, or weights of parts
 constexpr int kHalf = kKeys * 128;  // bytes of a tile's half: 128 keys x 64 dimensions
 constexpr int kMaxCtas = (int)(SCOOT_COUNTS / 2);
@@ -74,7 +82,7 @@ struct Shape {
 
 struct AttnArgs {
     CUtensorMap kmap, vmap, qmap[3];  // qmap[i]: tokens of 128 >> i rows
-    int32_t bs_log, n_heads, n_kv_heads, group, n_req, causal, window, bf16;
+    int32_t bs_log, n_heads, n_kv_heads, group, n_req, causal, window;
     int32_t toks;         // tokens of a slot: 128 / group
     int32_t inv_group;    // row / group = row * inv_group >> 16, for rows below 128
     int64_t n_tokens, n_blocks;
@@ -88,7 +96,7 @@ struct AttnArgs {
     uint16_t* out;
     int64_t out_ld_token, out_ld_head;
     float* lse;
-    float* parts;         // kBufs part buffers per CTA
+    float* parts;         // kBufs part buffers per CTA (part_buf)
     uint32_t* count;      // arrivals per split item and slot, zero between calls
     uint32_t* err;
 };
@@ -599,7 +607,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kLoadWarp && lane < 5) {
+    if (warp == kLoadWarp && lane < 5 && (lane < 3 || kRows >> (lane - 2) >= a.group)) {  // (maps that are in use)
         const CUtensorMap* map = lane == 0 ? &a.kmap : lane == 1 ? &a.vmap : &a.qmap[lane - 2];
         asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
     }
@@ -645,341 +653,341 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     Waiter wait;
 
     if (warp >= kMmaWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == kLoadWarp) {
-        // ---- items, and the copies of their tiles
-        uint32_t n_item = 0, n_q[2] = {0, 0};
-        int cached = -1;  // requests 32 cached .. are in the lanes
-        Req in_lane{0, 0, 0};
-        auto get = [&](int r) {
-            if ((r >> 5) != cached) {
-                cached = r >> 5;
-                in_lane = load_req(a, cached * 32 + lane, false);
-            }
-            return Req{__shfl_sync(0xffffffffu, in_lane.q0, r & 31), __shfl_sync(0xffffffffu, in_lane.n, r & 31),
-                       __shfl_sync(0xffffffffu, in_lane.kv, r & 31)};
-        };
-        // The warps' sums, one per lane, and their running sum: a head's cost at the last.  All heads' items in a row are cut
-        // into ranges of `range` units; this CTA's is [B0, B1).
-        int64_t upto = lane < kThreads / 32 ? cost_s[lane * 32 + 31] : 0;
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (warp == kLoadWarp) {
+            // ---- items, and the copies of their tiles
+            uint32_t n_item = 0, n_q[2] = {0, 0};
+            int cached = -1;  // requests 32 cached .. are in the lanes
+            Req in_lane{0, 0, 0};
+            auto get = [&](int r) {
+                if ((r >> 5) != cached) {
+                    cached = r >> 5;
+                    in_lane = load_req(a, cached * 32 + lane, false);
+                }
+                return Req{__shfl_sync(0xffffffffu, in_lane.q0, r & 31), __shfl_sync(0xffffffffu, in_lane.n, r & 31),
+                           __shfl_sync(0xffffffffu, in_lane.kv, r & 31)};
+            };
+            // The warps' sums, one per lane, and their running sum: a head's cost at the last.  All heads' items in a row are cut
+            // into ranges of `range` units; this CTA's is [B0, B1).
+            int64_t upto = lane < kThreads / 32 ? cost_s[lane * 32 + 31] : 0;
 #pragma unroll
-        for (int d = 1; d < kThreads / 32; d <<= 1) {
-            const int64_t t = __shfl_up_sync(0xffffffffu, upto, d);
-            if (lane >= d) upto += t;
-        }
-        const int64_t head_cost = __shfl_sync(0xffffffffu, upto, kThreads / 32 - 1), total = head_cost * a.n_kv_heads;
-        const int64_t range = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)kMinRange);
-        const int64_t B0 = min(total, blockIdx.x * range), B1 = min(total, B0 + range);
-        int h = 0, r = 0, j = 0;
-        int64_t p = B0;  // where item (h, r, j) starts
-        if (B0 < B1) {
-            // the warp, then the thread, whose sum passes y, then the request, then its item
-            h = (int)quotient(B0, head_cost);
-            const int64_t y = B0 - h * head_cost;
-            const int w = __ffs(__ballot_sync(0xffffffffu, lane < kThreads / 32 && upto > y)) - 1;
-            int64_t at = __shfl_sync(0xffffffffu, upto, w) - cost_s[w * 32 + 31];
-            const int64_t in_warp = cost_s[w * 32 + lane];
-            const int t = __ffs(__ballot_sync(0xffffffffu, at + in_warp > y)) - 1;
-            const int64_t before = __shfl_sync(0xffffffffu, in_warp, (t + 31) & 31);
-            if (t > 0) at += before;
-            r = (w * 32 + t) * k;
-            if (k == 1) {
-                cached = w;
-                in_lane = req_s[w * 32 + lane];
+            for (int d = 1; d < kThreads / 32; d <<= 1) {
+                const int64_t t = __shfl_up_sync(0xffffffffu, upto, d);
+                if (lane >= d) upto += t;
             }
-            for (bool found = false; !found;) {
+            const int64_t head_cost = __shfl_sync(0xffffffffu, upto, kThreads / 32 - 1), total = head_cost * a.n_kv_heads;
+            const int64_t range = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)kMinRange);
+            const int64_t B0 = min(total, blockIdx.x * range), B1 = min(total, B0 + range);
+            const int snap = (int)max((int64_t)kSnapMin, min((int64_t)kSnapMax, range / 4));
+            int h = 0, r = 0, j = 0;
+            int64_t p = B0;  // where item (h, r, j) starts
+            if (B0 < B1) {
+                // the warp, then the thread, whose sum passes y, then the request, then its item
+                h = (int)quotient(B0, head_cost);
+                const int64_t y = B0 - h * head_cost;
+                const int w = __ffs(__ballot_sync(0xffffffffu, lane < kThreads / 32 && upto > y)) - 1;
+                int64_t at = __shfl_sync(0xffffffffu, upto, w) - cost_s[w * 32 + 31];
+                const int64_t in_warp = cost_s[w * 32 + lane];
+                const int t = __ffs(__ballot_sync(0xffffffffu, at + in_warp > y)) - 1;
+                const int64_t before = __shfl_sync(0xffffffffu, in_warp, (t + 31) & 31);
+                if (t > 0) at += before;
+                r = (w * 32 + t) * k;
+                if (k == 1) {
+                    cached = w;
+                    in_lane = req_s[w * 32 + lane];
+                }
+                for (bool found = false; !found;) {
+                    const Req q = get(r);
+#pragma unroll 1
+                    for (int j0 = 0; j0 * per < q.n && !found; j0 += 32) {
+                        const int64_t c = (j0 + lane) * per < q.n ? item_cost(a, q.n, j0 + lane) + item_units(a, q.kv, q.n, j0 + lane) : 0;
+                        int64_t s = c;
+                        if (q.n > per) {
+#pragma unroll
+                            for (int d = 1; d < 32; d <<= 1) {
+                                const int64_t up = __shfl_up_sync(0xffffffffu, s, d);
+                                if (lane >= d) s += up;
+                            }
+                        }
+                        const uint32_t past = __ballot_sync(0xffffffffu, at + s > y);
+                        if (past) {
+                            const int src = __ffs(past) - 1;
+                            j = j0 + src;
+                            at += __shfl_sync(0xffffffffu, s - c, src);
+                            found = true;
+                        } else {
+                            at += __shfl_sync(0xffffffffu, s, q.n > per ? 31 : 0);
+                        }
+                    }
+                    if (!found && ++r >= a.n_req) found = true;  // not reached: y is below the sum of all
+                }
+                p = h * head_cost + at;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the tile may be copied over
+                __syncwarp();
+            }
+            TileLoader<D> keys(a, &a.kmap, bars, smem_u32(sKV), 0);
+            auto load_q = [&](const Item& it, int s, int tok, int head) {
+                if (n_q[s] > 0) wait.warp(&bars[kQEmpty + s], n_q[s] - 1);
+                if (!wait.all()) return;
+                const uint32_t bar = smem_u32(&bars[kQFull + s]);
+                const int rows = kRows >> it.rep_log, boxed = (rows * a.inv_group >> 16) * a.group, copies = 1 << it.rep_log;
+                const CUtensorMap* map = &a.qmap[it.rep_log];
+                if (elect_one()) {
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
+                                 "r"((uint32_t)(copies * kNH * boxed * 128))
+                                 : "memory");
+#pragma unroll 1
+                    for (int c = 0; c < copies; ++c)
+#pragma unroll
+                        for (int half = 0; half < kNH; ++half)
+                            asm volatile(
+                                "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, "
+                                "%3, %4}], [%5];" ::"r"(smem_u32(sQ) + s * Sh::kTile + half * kHalf + c * rows * 128),
+                                "l"(map), "r"(half * 64), "r"(head * a.group), "r"(tok), "r"(bar)
+                                : "memory");
+                }
+                __syncwarp();
+                ++n_q[s];
+            };
+            int turn = 0;
+            while (p < B1 && wait.ok) {
                 const Req q = get(r);
-#pragma unroll 1
-                for (int j0 = 0; j0 * per < q.n && !found; j0 += 32) {
-                    const int64_t c = (j0 + lane) * per < q.n ? item_cost(a, q.n, j0 + lane) + item_units(a, q.kv, q.n, j0 + lane) : 0;
-                    int64_t s = c;
-                    if (q.n > per) {
-#pragma unroll
-                        for (int d = 1; d < 32; d <<= 1) {
-                            const int64_t up = __shfl_up_sync(0xffffffffu, s, d);
-                            if (lane >= d) s += up;
-                        }
+                if (j * per >= q.n) {  // the next request with a token, in the next head if need be
+                    const uint32_t more = __ballot_sync(0xffffffffu, in_lane.n > 0) & ~((2u << (r & 31)) - 1u);
+                    r = more ? (r & ~31) + __ffs(more) - 1 : (r & ~31) + 32;
+                    j = 0;
+                    if (r >= a.n_req) {
+                        r = 0;
+                        ++h;
+                        if (h >= a.n_kv_heads) break;
                     }
-                    const uint32_t past = __ballot_sync(0xffffffffu, at + s > y);
-                    if (past) {
-                        const int src = __ffs(past) - 1;
-                        j = j0 + src;
-                        at += __shfl_sync(0xffffffffu, s - c, src);
-                        found = true;
-                    } else {
-                        at += __shfl_sync(0xffffffffu, s, q.n > per ? 31 : 0);
-                    }
+                    continue;
                 }
-                if (!found && ++r >= a.n_req) found = true;  // not reached: y is below the sum of all
-            }
-            p = h * head_cost + at;
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the tile may be copied over
-            __syncwarp();
-        }
-        TileLoader<D> keys(a, &a.kmap, bars, smem_u32(sKV), 0);
-        auto load_q = [&](const Item& it, int s, int tok, int head) {
-            if (n_q[s] > 0) wait.warp(&bars[kQEmpty + s], n_q[s] - 1);
-            if (!wait.all()) return;
-            const uint32_t bar = smem_u32(&bars[kQFull + s]);
-            const int rows = kRows >> it.rep_log, boxed = (rows * a.inv_group >> 16) * a.group, copies = 1 << it.rep_log;
-            const CUtensorMap* map = &a.qmap[it.rep_log];
-            if (elect_one()) {
-                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar),
-                             "r"((uint32_t)(copies * kNH * boxed * 128))
-                             : "memory");
-#pragma unroll 1
-                for (int c = 0; c < copies; ++c)
-#pragma unroll
-                    for (int half = 0; half < kNH; ++half)
-                        asm volatile(
-                            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, "
-                            "%3, %4}], [%5];" ::"r"(smem_u32(sQ) + s * Sh::kTile + half * kHalf + c * rows * 128),
-                            "l"(map), "r"(half * 64), "r"(head * a.group), "r"(tok), "r"(bar)
-                            : "memory");
-            }
-            __syncwarp();
-            ++n_q[s];
-        };
-        int turn = 0;
-        while (p < B1 && wait.ok) {
-            const Req q = get(r);
-            if (j * per >= q.n) {  // the next request with a token, in the next head if need be
-                const uint32_t more = __ballot_sync(0xffffffffu, in_lane.n > 0) & ~((2u << (r & 31)) - 1u);
-                r = more ? (r & ~31) + __ffs(more) - 1 : (r & ~31) + 32;
-                j = 0;
-                if (r >= a.n_req) {
-                    r = 0;
-                    ++h;
-                    if (h >= a.n_kv_heads) break;
+                Item it;
+                it.h = h;
+                it.r = r;
+                it.ntok = min(per, q.n - j * per);
+                it.tok = q.q0 + j * per;
+                it.pos = q.kv - q.n + j * per;
+                it.kv = q.kv;
+                seen_keys(a, q.kv, q.n, j * per, it.ntok, it.begin, it.end);
+                it.rep_log = it.ntok * a.group <= kRows / 4 ? 2 : it.ntok * a.group <= kRows / 2 ? 1 : 0;
+                it.poison = it.stop = 0;
+                const int t0 = it.begin / kKeys, units = (it.end + kKeys - 1) / kKeys - t0;
+                const int64_t s = p + item_cost(a, q.n, j);  // where its units start
+                auto cut = [&](int64_t b) {
+                    return b >= s + units ? units : b - s < snap ? 0 : s + units - b < snap ? units : (int)(b - s);
+                };
+                const int lo = cut(B0), hi = cut(B1);
+                const bool here = units ? hi > lo : p >= B0;
+                p = s + units;
+                ++j;
+                if (!here) continue;
+                it.u0 = t0 + lo;
+                it.nu = hi - lo;
+                it.first = blockIdx.x;
+                it.n_parts = 1;
+                if (it.nu < units) {
+                    it.first = (int)quotient(s + snap - 1, range);
+                    it.n_parts = (int)quotient(s + units - snap, range) - it.first + 1;
                 }
-                continue;
-            }
-            Item it;
-            it.h = h;
-            it.r = r;
-            it.ntok = min(per, q.n - j * per);
-            it.tok = q.q0 + j * per;
-            it.pos = q.kv - q.n + j * per;
-            it.kv = q.kv;
-            seen_keys(a, q.kv, q.n, j * per, it.ntok, it.begin, it.end);
-            it.rep_log = it.ntok * a.group <= kRows / 4 ? 2 : it.ntok * a.group <= kRows / 2 ? 1 : 0;
-            it.poison = it.stop = 0;
-            const int t0 = it.begin / kKeys, units = (it.end + kKeys - 1) / kKeys - t0;
-            const int64_t s = p + item_cost(a, q.n, j);  // where its units start
-            const int snap = it.ntok > a.toks ? kPairSnap : kSnap;
-            auto cut = [&](int64_t b) {
-                return b >= s + units ? units : b - s < snap ? 0 : s + units - b < snap ? units : (int)(b - s);
-            };
-            const int lo = cut(B0), hi = cut(B1);
-            const bool here = units ? hi > lo : p >= B0;
-            p = s + units;
-            ++j;
-            if (!here) continue;
-            it.u0 = t0 + lo;
-            it.nu = hi - lo;
-            it.first = blockIdx.x;
-            it.n_parts = 1;
-            if (it.nu < units) {
-                it.first = (int)quotient(s + snap - 1, range);
-                it.n_parts = (int)quotient(s + units - snap, range) - it.first + 1;
-            }
-            it.slot = it.ntok > a.toks ? 2 : turn;
-            if (it.slot < 2) turn ^= 1;
-            const uint32_t ring = n_item % kRing;
-            if (n_item >= kRing) wait.warp(&bars[kItemEmpty + ring], n_item / kRing - 1);
-            if (!wait.all()) break;
-            if (lane == 0) {
-                items[ring] = it;
-                mbar_arrive(&bars[kItemFull + ring]);
-            }
-            __syncwarp();
-            ++n_item;
-            if (it.nu > 0) keys.begin(it);
-#pragma unroll 1
-            for (int u = 0; u < it.nu && wait.ok; ++u) {
-                keys.tile(it, it.u0 + u, wait);
-                if (u == 0) {
-#pragma unroll
-                    for (int sl = 0; sl < 2; ++sl)
-                        if (it.slot == 2 || it.slot == sl) load_q(it, sl, it.tok + (it.slot == 2 ? sl * a.toks : 0), h);
-                }
-            }
-        }
-        if (wait.ok && n_item >= kRing) wait.warp(&bars[kItemEmpty + n_item % kRing], n_item / kRing - 1);
-        if (wait.all() && lane == 0) {
-            items[n_item % kRing].stop = 1;
-            mbar_arrive(&bars[kItemFull + n_item % kRing]);
-        }
-        if (keys.bad) atomicOr(a.err, SCOOT_DEVERR_INDEX);
-        __syncwarp();
-        if (!wait.ok) {
-            // gave up: the copies in flight land before the block ends
-            if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
-            keys.drain();
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-                if (n_q[s] > 0) mbar_wait_tries(smem_u32(&bars[kQFull + s]), (n_q[s] - 1) & 1u);
-        }
-    } else if (warp == kValueWarp) {
-        // ---- the copies of the values
-        TileLoader<D> vals(a, &a.vmap, bars, smem_u32(sKV), 1);
-        for (uint32_t n_item = 0; wait.ok; ++n_item) {
-            wait.warp(&bars[kItemFull + n_item % kRing], n_item / kRing);
-            if (!wait.all()) break;
-            const Item it = items[n_item % kRing];
-            if (it.stop) break;
-            warp_arrive(&bars[kItemEmpty + n_item % kRing]);
-            if (it.nu > 0) vals.begin(it);
-#pragma unroll 1
-            for (int u = 0; u < it.nu && wait.ok; ++u) vals.tile(it, it.u0 + u, wait);
-        }
-        if (!wait.ok) {
-            if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
-            vals.drain();
-        }
-    } else if (warp == kMmaWarp) {
-        // ---- the products.  The warp runs as one, so that the operands stay in its uniform registers, and one lane issues.
-        {
-            // The scores of successive (unit, slot)s go to the buffers in turn, and the product with V of the P that replaces
-            // them is issued before the buffer's next scores: the scores of the next one or two run under a softmax.  todo0
-            // is the oldest such product still to be issued, of n_todo, each a word: its slot and the slot's unit mod 3
-            // (kSlotUnit, as the barriers are laid out), their phase, ...  This warp's instructions, six to nine cycles each, are
-            // on the way of every unit: its places in the rings are counted along, and the code is short (with more
-            // copies of it, it did not stay in the instruction cache).
-            enum : uint32_t { kSlotUnit = 7, kPhase = 8, kAcc = 16, kRelease = 32, kVPhase = 64, kVStage = 8, kBufAt = 12 };
-            constexpr uint32_t kTileDesc = Sh::kTile >> 4;
-            uint32_t n_todo = 0, todo0 = 0, todo1 = 0, todo2 = 0;
-            uint32_t buf = 0, n_q0 = 0, n_q1 = 0;
-            uint32_t next0 = 0, next1 = 4;        // the slots' next units, as in a word
-            uint32_t v_word = 1u << kVStage;      // this unit's values: stage and phase, as in a word
-            const uint32_t id_s = idesc(kBf16, kKeys, false), id_o = idesc(kBf16, D, true), bar0 = smem_u32(bars);
-            const uint32_t q_desc = (uint32_t)desc_k(smem_u32(sQ)), k_desc0 = (uint32_t)desc_k(smem_u32(sKV)),
-                           v_desc = (uint32_t)desc_v(smem_u32(sKV));
-            uint32_t k_desc = k_desc0, k_bar = bar0 + 8 * kKvFull;  // this unit's keys
-            const bool leader = elect_one();
-            auto commit = [&](uint32_t b) {
-                asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(b) : "memory");
-            };
-            auto ready = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(b, parity)) != 0; };
-            auto k_phase = [&]() { return v_word & kVPhase ? 1u : 0u; };
-            auto p_bar = [&]() { return bar0 + 8 * kPFull + 8 * (todo0 & kSlotUnit); };
-            auto p_phase = [&]() { return todo0 & kPhase ? 1u : 0u; };
-            auto v_bar = [&]() { return bar0 + 8 * kKvFull + 8 * (todo0 >> kVStage & 15u); };
-            auto v_phase = [&]() { return todo0 & kVPhase ? 1u : 0u; };
-            auto issue_values = [&]() {  // by the leader: the oldest product with V
-                const uint32_t dv = v_desc + (todo0 >> kVStage & 15u) * kTileDesc;
-                const uint32_t o = tmem + Sh::kO + (todo0 & 4u ? D : 0), pp = tmem + (todo0 >> kBufAt) * kKeys;
-#pragma unroll
-                for (int i = 0; i < kKeys / 16; ++i)
-                    mma_ts(o, pp + 8 * i, dv + 128 * i, (uint32_t)(desc_v(0) >> 32), id_o, i > 0 || (todo0 & kAcc));
-                commit(bar0 + 8 * kPvDone + 8 * (todo0 & kSlotUnit));
-                if (todo0 & kRelease) commit(v_bar() + 8 * (kKvEmpty - kKvFull));
-            };
-            auto issue_scores = [&](uint32_t sl, uint32_t next, bool item_end, bool last) {
-                const uint32_t dq = q_desc + sl * kTileDesc, d = tmem + buf * kKeys;
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const uint32_t off = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
-                    mma_ss(d, dq + off, k_desc + off, (uint32_t)(desc_k(0) >> 32), id_s, i > 0);
-                }
-                commit(bar0 + 8 * kSFull + 8 * (next & kSlotUnit));
-                if (last) commit(k_bar + 8 * (kKvEmpty - kKvFull));
-                if (item_end) commit(bar0 + 8 * (kQEmpty + sl));
-            };
-            auto pop = [&]() {
-                todo0 = todo1;
-                todo1 = todo2;
-                --n_todo;
-            };
-            auto push = [&](uint32_t w) {
-                if (n_todo == 0) todo0 = w;
-                else if (n_todo == 1) todo1 = w;
-                else todo2 = w;
-                ++n_todo;
-                buf = buf + 1 == Sh::kBuf ? 0 : buf + 1;
-            };
-            auto advance = [&](uint32_t next) { return (next & 3u) == 2u ? (next - 2u) ^ kPhase : next + 1u; };
-            auto values = [&]() {
-                wait.at(p_bar(), p_phase());
-                wait.at(v_bar(), v_phase());
-                fence_after();
-                if (leader) issue_values();
-                __syncwarp();
-                pop();
-            };
-            auto scores = [&](uint32_t sl, int u, int nu, bool last) {  // last: of this tile's users
-                if (u == 0) {
-                    wait.at(bar0 + 8 * (kQFull + sl), (sl ? n_q1 : n_q0) & 1u);
-                    n_q0 += sl == 0;
-                    n_q1 += sl;
-                }
-                const uint32_t next = sl ? next1 : next0;
-                fence_after();
-                if (leader) issue_scores(sl, next, u == nu - 1, last);
-                __syncwarp();
-                push(next | v_word | (u > 0 ? kAcc : 0) | (last ? kRelease : 0) | buf << kBufAt);
-                if (sl) next1 = advance(next);
-                else next0 = advance(next);
-            };
-            for (uint32_t n_item = 0;; ++n_item) {
-                wait.at(bar0 + 8 * (kItemFull + n_item % kRing), n_item / kRing & 1u);
+                it.slot = it.ntok > a.toks ? 2 : turn;
+                if (it.slot < 2) turn ^= 1;
+                const uint32_t ring = n_item % kRing;
+                if (n_item >= kRing) wait.warp(&bars[kItemEmpty + ring], n_item / kRing - 1);
                 if (!wait.all()) break;
-                const volatile Item& it = items[n_item % kRing];
-                const int stop = __reduce_max_sync(0xffffffffu, it.stop), nu = __reduce_max_sync(0xffffffffu, it.nu),
-                          slot = __reduce_max_sync(0xffffffffu, it.slot);
-                if (stop) break;
-                warp_arrive(&bars[kItemEmpty + n_item % kRing]);
-#pragma unroll 1
-                for (int u = 0; u < nu; ++u) {
-                    if (slot == 2) {
-                        if (n_todo == Sh::kBuf) values();
-                        wait.at(k_bar, k_phase());
-                        scores(0, u, nu, false);
-                        if (n_todo == Sh::kBuf) values();
-                        scores(1, u, nu, true);
-                    } else if (u > 0 && n_todo == Sh::kBuf &&
-                               __all_sync(0xffffffffu, mbar_test3(p_bar(), p_phase(), v_bar(), v_phase(), k_bar, k_phase()))) {
-                        // all that the oldest product and these scores need is there
-                        const uint32_t next = slot ? next1 : next0;
-                        fence_after();
-                        if (leader) {
-                            issue_values();
-                            issue_scores(slot, next, u == nu - 1, true);
-                        }
-                        __syncwarp();
-                        pop();
-                        push(next | v_word | kAcc | kRelease | buf << kBufAt);
-                        if (slot) next1 = advance(next);
-                        else next0 = advance(next);
-                    } else {
-                        if (n_todo == Sh::kBuf) values();
-                        // a product that gets ready while the keys are on their way goes first
-                        for (uint32_t i = 0; !ready(k_bar, k_phase()); ++i) {
-                            if (n_todo && ready(p_bar(), p_phase())) values();
-                            else wait.ok &= i < (1u << 22);
-                            if (!wait.all()) break;
-                        }
-                        scores(slot, u, nu, true);
-                    }
-                    k_desc += 2 * kTileDesc;
-                    k_bar += 16;
-                    v_word += 2u << kVStage;
-                    if (k_bar == bar0 + 8 * (kKvFull + kNS)) {
-                        k_desc = k_desc0;
-                        k_bar = bar0 + 8 * kKvFull;
-                        v_word = (v_word - ((uint32_t)kNS << kVStage)) ^ kVPhase;
-                    }
-                    if (!wait.all()) break;
+                if (lane == 0) {
+                    items[ring] = it;
+                    mbar_arrive(&bars[kItemFull + ring]);
                 }
-                if (!wait.ok) break;
+                __syncwarp();
+                ++n_item;
+                if (it.nu > 0) keys.begin(it);
+#pragma unroll 1
+                for (int u = 0; u < it.nu && wait.ok; ++u) {
+                    keys.tile(it, it.u0 + u, wait);
+                    if (u == 0) {
+#pragma unroll
+                        for (int sl = 0; sl < 2; ++sl)
+                            if (it.slot == 2 || it.slot == sl) load_q(it, sl, it.tok + (it.slot == 2 ? sl * a.toks : 0), h);
+                    }
+                }
             }
-            while (n_todo && wait.all()) values();
-            if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
-            if (leader) commit(bar0 + 8 * kDrain);
+            if (wait.ok && n_item >= kRing) wait.warp(&bars[kItemEmpty + n_item % kRing], n_item / kRing - 1);
+            if (wait.all() && lane == 0) {
+                items[n_item % kRing].stop = 1;
+                mbar_arrive(&bars[kItemFull + n_item % kRing]);
+            }
+            if (keys.bad) atomicOr(a.err, SCOOT_DEVERR_INDEX);
             __syncwarp();
-            mbar_wait_tries(smem_u32(&bars[kDrain]), 0);
+            if (!wait.ok) {
+                // gave up: the copies in flight land before the block ends
+                if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
+                keys.drain();
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+                    if (n_q[s] > 0) mbar_wait_tries(smem_u32(&bars[kQFull + s]), (n_q[s] - 1) & 1u);
+            }
+        } else if (warp == kValueWarp) {
+            // ---- the copies of the values
+            TileLoader<D> vals(a, &a.vmap, bars, smem_u32(sKV), 1);
+            for (uint32_t n_item = 0; wait.ok; ++n_item) {
+                wait.warp(&bars[kItemFull + n_item % kRing], n_item / kRing);
+                if (!wait.all()) break;
+                const Item it = items[n_item % kRing];
+                if (it.stop) break;
+                warp_arrive(&bars[kItemEmpty + n_item % kRing]);
+                if (it.nu > 0) vals.begin(it);
+#pragma unroll 1
+                for (int u = 0; u < it.nu && wait.ok; ++u) vals.tile(it, it.u0 + u, wait);
+            }
+            if (!wait.ok) {
+                if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
+                vals.drain();
+            }
+        } else if (warp == kMmaWarp) {
+            // ---- the products.  The warp runs as one, so that the operands stay in its uniform registers, and one lane issues.
+            {
+                // The scores of successive (unit, slot)s go to the buffers in turn, and the product with V of the P that replaces
+                // them is issued before the buffer's next scores: the scores of the next one or two run under a softmax.  todo0
+                // is the oldest such product still to be issued, of n_todo, each a word: its slot and the slot's unit mod 3
+                // (kSlotUnit, as the barriers are laid out), their phase, ...  This warp's instructions, six to nine cycles each, are
+                // on the way of every unit: its places in the rings are counted along, and the code is short (with more
+                // copies of it, it did not stay in the instruction cache).
+                enum : uint32_t { kSlotUnit = 7, kPhase = 8, kAcc = 16, kRelease = 32, kVPhase = 64, kVStage = 8, kBufAt = 12 };
+                constexpr uint32_t kTileDesc = Sh::kTile >> 4;
+                uint32_t n_todo = 0, todo0 = 0, todo1 = 0, todo2 = 0;
+                uint32_t buf = 0, n_q0 = 0, n_q1 = 0;
+                uint32_t next0 = 0, next1 = 4;        // the slots' next units, as in a word
+                uint32_t v_word = 1u << kVStage;      // this unit's values: stage and phase, as in a word
+                const uint32_t id_s = idesc(kBf16, kKeys, false), id_o = idesc(kBf16, D, true), bar0 = smem_u32(bars);
+                const uint32_t q_desc = (uint32_t)desc_k(smem_u32(sQ)), k_desc0 = (uint32_t)desc_k(smem_u32(sKV)),
+                               v_desc = (uint32_t)desc_v(smem_u32(sKV));
+                uint32_t k_desc = k_desc0, k_bar = bar0 + 8 * kKvFull;  // this unit's keys
+                const bool leader = elect_one();
+                auto commit = [&](uint32_t b) {
+                    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(b) : "memory");
+                };
+                auto ready = [&](uint32_t b, uint32_t parity) { return __all_sync(0xffffffffu, mbar_test(b, parity)) != 0; };
+                auto k_phase = [&]() { return v_word & kVPhase ? 1u : 0u; };
+                auto p_bar = [&]() { return bar0 + 8 * kPFull + 8 * (todo0 & kSlotUnit); };
+                auto p_phase = [&]() { return todo0 & kPhase ? 1u : 0u; };
+                auto v_bar = [&]() { return bar0 + 8 * kKvFull + 8 * (todo0 >> kVStage & 15u); };
+                auto v_phase = [&]() { return todo0 & kVPhase ? 1u : 0u; };
+                auto issue_values = [&]() {  // by the leader: the oldest product with V
+                    const uint32_t dv = v_desc + (todo0 >> kVStage & 15u) * kTileDesc;
+                    const uint32_t o = tmem + Sh::kO + (todo0 & 4u ? D : 0), pp = tmem + (todo0 >> kBufAt) * kKeys;
+#pragma unroll
+                    for (int i = 0; i < kKeys / 16; ++i)
+                        mma_ts(o, pp + 8 * i, dv + 128 * i, (uint32_t)(desc_v(0) >> 32), id_o, i > 0 || (todo0 & kAcc));
+                    commit(bar0 + 8 * kPvDone + 8 * (todo0 & kSlotUnit));
+                    if (todo0 & kRelease) commit(v_bar() + 8 * (kKvEmpty - kKvFull));
+                };
+                auto issue_scores = [&](uint32_t sl, uint32_t next, bool item_end, bool last) {
+                    const uint32_t dq = q_desc + sl * kTileDesc, d = tmem + buf * kKeys;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint32_t off = (i / 4) * (kHalf >> 4) + (i % 4) * 2;
+                        mma_ss(d, dq + off, k_desc + off, (uint32_t)(desc_k(0) >> 32), id_s, i > 0);
+                    }
+                    commit(bar0 + 8 * kSFull + 8 * (next & kSlotUnit));
+                    if (last) commit(k_bar + 8 * (kKvEmpty - kKvFull));
+                    if (item_end) commit(bar0 + 8 * (kQEmpty + sl));
+                };
+                auto pop = [&]() {
+                    todo0 = todo1;
+                    todo1 = todo2;
+                    --n_todo;
+                };
+                auto push = [&](uint32_t w) {
+                    if (n_todo == 0) todo0 = w;
+                    else if (n_todo == 1) todo1 = w;
+                    else todo2 = w;
+                    ++n_todo;
+                    buf = buf + 1 == Sh::kBuf ? 0 : buf + 1;
+                };
+                auto advance = [&](uint32_t next) { return (next & 3u) == 2u ? (next - 2u) ^ kPhase : next + 1u; };
+                auto values = [&]() {
+                    wait.at(p_bar(), p_phase());
+                    wait.at(v_bar(), v_phase());
+                    fence_after();
+                    if (leader) issue_values();
+                    __syncwarp();
+                    pop();
+                };
+                auto scores = [&](uint32_t sl, int u, int nu, bool last) {  // last: of this tile's users
+                    if (u == 0) {
+                        wait.at(bar0 + 8 * (kQFull + sl), (sl ? n_q1 : n_q0) & 1u);
+                        n_q0 += sl == 0;
+                        n_q1 += sl;
+                    }
+                    const uint32_t next = sl ? next1 : next0;
+                    fence_after();
+                    if (leader) issue_scores(sl, next, u == nu - 1, last);
+                    __syncwarp();
+                    push(next | v_word | (u > 0 ? kAcc : 0) | (last ? kRelease : 0) | buf << kBufAt);
+                    if (sl) next1 = advance(next);
+                    else next0 = advance(next);
+                };
+                for (uint32_t n_item = 0;; ++n_item) {
+                    wait.at(bar0 + 8 * (kItemFull + n_item % kRing), n_item / kRing & 1u);
+                    if (!wait.all()) break;
+                    const volatile Item& it = items[n_item % kRing];
+                    const int stop = __reduce_max_sync(0xffffffffu, it.stop), nu = __reduce_max_sync(0xffffffffu, it.nu),
+                              slot = __reduce_max_sync(0xffffffffu, it.slot);
+                    if (stop) break;
+                    warp_arrive(&bars[kItemEmpty + n_item % kRing]);
+#pragma unroll 1
+                    for (int u = 0; u < nu; ++u) {
+                        if (slot == 2) {
+                            if (n_todo == Sh::kBuf) values();
+                            wait.at(k_bar, k_phase());
+                            scores(0, u, nu, false);
+                            if (n_todo == Sh::kBuf) values();
+                            scores(1, u, nu, true);
+                        } else if (u > 0 && n_todo == Sh::kBuf &&
+                                   __all_sync(0xffffffffu, mbar_test3(p_bar(), p_phase(), v_bar(), v_phase(), k_bar, k_phase()))) {
+                            // all that the oldest product and these scores need is there
+                            const uint32_t next = slot ? next1 : next0;
+                            fence_after();
+                            if (leader) {
+                                issue_values();
+                                issue_scores(slot, next, u == nu - 1, true);
+                            }
+                            __syncwarp();
+                            pop();
+                            push(next | v_word | kAcc | kRelease | buf << kBufAt);
+                            if (slot) next1 = advance(next);
+                            else next0 = advance(next);
+                        } else {
+                            if (n_todo == Sh::kBuf) values();
+                            // a product that gets ready while the keys are on their way goes first
+                            for (uint32_t i = 0; !ready(k_bar, k_phase()); ++i) {
+                                if (n_todo && ready(p_bar(), p_phase())) values();
+                                else wait.ok &= i < (1u << 22);
+                                if (!wait.all()) break;
+                            }
+                            scores(slot, u, nu, true);
+                        }
+                        k_desc += 2 * kTileDesc;
+                        k_bar += 16;
+                        v_word += 2u << kVStage;
+                        if (k_bar == bar0 + 8 * (kKvFull + kNS)) {
+                            k_desc = k_desc0;
+                            k_bar = bar0 + 8 * kKvFull;
+                            v_word = (v_word - ((uint32_t)kNS << kVStage)) ^ kVPhase;
+                        }
+                        if (!wait.all()) break;
+                    }
+                    if (!wait.ok) break;
+                }
+                while (n_todo && wait.all()) values();
+                if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
+                if (leader) commit(bar0 + 8 * kDrain);
+                __syncwarp();
+                mbar_wait_tries(smem_u32(&bars[kDrain]), 0);
+            }
         }
-    }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         // ---- softmax of slot s; this thread's row of tensor memory is lane row
@@ -1223,9 +1231,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             }
             warp_arrive(&bars[kItemEmpty + ring]);
             if (whole) continue;
-            __threadfence();
             wg_sync();
             if (row == 0) {
+                __threadfence();  // (the slot's other threads' stores are before it by the barrier)
                 uint32_t* cnt = a.count + 2 * it.first + half;
                 const bool last = atomicAdd(cnt, 1u) == (uint32_t)it.n_parts - 1;
                 if (last) *cnt = 0;
@@ -1302,7 +1310,7 @@ extern "C" scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_lay
     if (n_heads / layout->n_kv_heads > SCOOT_MAX_GROUP)
         return scoot_fail(ctx, SCOOT_EUNSUPPORTED, "%d query heads per key-value head, more than %d",
                           n_heads / layout->n_kv_heads, SCOOT_MAX_GROUP);
-    if (n_tokens < 0 || n_tokens > 0x7FFFFFFFll / n_heads || n_req < 0 || ld_table < 0 || ld_table > (0x40000000ll / layout->block_size))
+    if (n_tokens < 0 || n_tokens > 0x40000000ll || n_tokens > 0x7FFFFFFFll / n_heads || n_req < 0 || ld_table < 0 || ld_table > (0x40000000ll / layout->block_size))
         return scoot_fail(ctx, SCOOT_EINVAL, "n_tokens = %lld, n_req = %d or ld_table = %lld out of range", (long long)n_tokens,
                           n_req, (long long)ld_table);
     if (!(scale > 0.0f) || scale > 3.0e38f) return scoot_fail(ctx, SCOOT_EINVAL, "scale = %g must be positive and finite", scale);
