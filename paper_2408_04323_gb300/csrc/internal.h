@@ -31,6 +31,8 @@ struct scoot_ctx {
     std::vector<void*> ws_kept;  // earlier ones that graphs may use, freed with the context
     size_t ws_kept_bytes = 0;
     uint32_t* d_err = nullptr;   // device error word, followed by the counters
+    int32_t sms = 0;             // multiprocessors of the device
+    uint32_t attn_set = 0;       // paged_attn.cu's kernels whose shared memory has been asked for
     uint32_t* d_count = nullptr; // SCOOT_COUNTS arrival counters, zero between calls (paged_attn.cu)
     // Phase timing (scoot_ctx_set_timing): events recorded between the
     // launches of the last timed call, and the kind of each launch.

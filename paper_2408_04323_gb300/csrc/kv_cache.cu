@@ -314,10 +314,8 @@ scoot_status scoot_kv_tables(scoot_ctx* ctx, const int32_t* cached_len, const in
     a.n_tokens = n_tokens;
     a.counts = counts;
     a.err = ctx->d_err;
-    int sms = 0;
-    SCOOT_CUDA(ctx, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, ctx->device));
     int64_t blocks = (n_tokens + kTabThreads - 1) / kTabThreads;
-    if (blocks > sms) blocks = sms;
+    if (blocks > ctx->sms) blocks = ctx->sms;
     if (blocks < 1) blocks = 1;
     const size_t smem = n_req <= kTabStaged ? (size_t)(n_req + std::min(n_req, kTabThreads)) * sizeof(int2) : 0;
     if (smem > 32768)  // beyond what a block has without asking, beside its static part

@@ -1288,7 +1288,11 @@ scoot_status launch(scoot_ctx* ctx, AttnArgs& a, int sms, cudaStream_t st) {
     if (s != SCOOT_OK) return s;
     a.parts = static_cast<float*>(ctx->ws);
     auto kern = paged_attn_kernel<kBf16, D>;
-    SCOOT_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem));
+    const uint32_t bit = 1u << (2 * kBf16 + (D == 128));
+    if (!(ctx->attn_set & bit)) {  // once per context: the call is short
+        SCOOT_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem));
+        ctx->attn_set |= bit;
+    }
     kern<<<(unsigned)sms, kThreads, Shape<D>::kSmem, st>>>(a);
     SCOOT_LAUNCHED(ctx);
     return SCOOT_OK;
@@ -1322,9 +1326,7 @@ extern "C" scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_lay
     if (!query_start || !kv_len || (ld_table && !block_table)) return scoot_fail(ctx, SCOOT_EINVAL, "an array is NULL");
     const int D = layout->head_dim, G = n_heads / layout->n_kv_heads;
     if (!encode_tiled()) return scoot_fail(ctx, SCOOT_ECUDA, "the driver has no cuTensorMapEncodeTiled");
-    int sms = 0;
-    SCOOT_CUDA(ctx, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, ctx->device));
-    if (sms > kMaxCtas) sms = kMaxCtas;
+    const int sms = ctx->sms < kMaxCtas ? ctx->sms : kMaxCtas;
     AttnArgs a = {};
     const bool bf16 = layout->dtype == SCOOT_BF16;
     {

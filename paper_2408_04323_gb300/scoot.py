@@ -845,17 +845,15 @@ def _on(stream, t):
 def _heads(t, dtype, name):
     """(pointer, token stride, head stride) of a CUDA tensor [tokens][heads][dim] whose dim is contiguous.  The stride
     of an axis of one (torch may give it any) counts as the axis's size."""
-    if not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA torch tensor (device memory)")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be [tokens][heads][dim], got {tuple(t.shape)}")
+    stride = t.stride()
+    if not (t.dtype is dtype and t.is_cuda and len(stride) == 3 and stride[2] == 1):
+        if not t.is_cuda:
+            raise TypeError(f"{name} must be a CUDA torch tensor (device memory)")
+        if t.dtype is not dtype:
+            raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+        raise ValueError(f"{name} must be [tokens][heads][dim] and contiguous along its last axis, got {tuple(t.shape)}")
     n, h, d = t.shape
-    st, sh, sd = t.stride()
-    if sd != 1:
-        raise ValueError(f"{name} must be contiguous along its last axis")
-    return t.data_ptr(), (st if n > 1 else h * d), (sh if h > 1 else d)
+    return t.data_ptr(), (stride[0] if n > 1 else h * d), (stride[1] if h > 1 else d)
 
 
 @functools.lru_cache(maxsize=64)
@@ -863,24 +861,22 @@ def _layout(bf16, shape, stride):
     nb, bs, h, d = shape
     sb, st, sh, _ = stride
     L = scoot_kv_layout(BF16 if bf16 else F16, d, h, bs, nb, sb if nb > 1 else bs * h * d, st, sh if h > 1 else d)
-    return L, C.byref(L)
+    return L, C.byref(L), d, h
 
 
 def _kv(k_cache, v_cache):
+    """(layout, reference to it, head size, key-value heads) of a cache."""
     import torch
     dt, shape, stride = k_cache.dtype, k_cache.shape, k_cache.stride()
-    if not (k_cache.is_cuda and v_cache.is_cuda):
-        raise TypeError("k_cache and v_cache must be CUDA torch tensors (device memory)")
-    if dt is not v_cache.dtype or not (dt is torch.bfloat16 or dt is torch.float16):
-        raise TypeError(f"k_cache and v_cache must both be float16 or bfloat16, got {dt} and {v_cache.dtype}")
-    if len(shape) != 4 or shape != v_cache.shape:
-        raise ValueError(f"k_cache and v_cache must be [blocks][tokens][heads][dim] of one shape, got {tuple(shape)} and "
-                         f"{tuple(v_cache.shape)}")
-    if stride != v_cache.stride():
-        raise ValueError("k_cache and v_cache must have the same strides")
-    if stride[3] != 1:
-        raise ValueError("k_cache and v_cache must be contiguous along their last axis")
-    return _layout(dt is torch.bfloat16, tuple(shape), stride)
+    if not (dt is v_cache.dtype and (dt is torch.bfloat16 or dt is torch.float16) and len(shape) == 4 and shape == v_cache.shape
+            and stride == v_cache.stride() and stride[3] == 1 and k_cache.is_cuda and v_cache.is_cuda):
+        if not (k_cache.is_cuda and v_cache.is_cuda):
+            raise TypeError("k_cache and v_cache must be CUDA torch tensors (device memory)")
+        if dt is not v_cache.dtype or not (dt is torch.bfloat16 or dt is torch.float16):
+            raise TypeError(f"k_cache and v_cache must both be float16 or bfloat16, got {dt} and {v_cache.dtype}")
+        raise ValueError("k_cache and v_cache must be [blocks][tokens][heads][dim] of one shape and the same strides, contiguous "
+                         f"along their last axis, got {tuple(shape)} and {tuple(v_cache.shape)}")
+    return _layout(dt is torch.bfloat16, shape, stride)
 
 
 def kv_layout(k_cache, v_cache) -> scoot_kv_layout:
@@ -913,9 +909,9 @@ def scoot_kv_tables(ctx, cached_len, new_len, block_table, block_size, n_blocks,
 def scoot_kv_append(ctx, k, v, slot, k_cache, v_cache, stream=None) -> None:
     """k, v: device [T][heads][dim] of the cache's type (last axis contiguous); slot: device int64 [T]."""
     import torch
-    L, ref = _kv(k_cache, v_cache)
+    _, ref, D, Hkv = _kv(k_cache, v_cache)
     T, dt, h = slot.numel(), k_cache.dtype, _h(ctx)
-    if k.shape != v.shape or tuple(k.shape) != (T, L.n_kv_heads, L.head_dim):
+    if k.shape != v.shape or k.shape != (T, Hkv, D):
         raise ValueError(f"k and v must be [T][heads][dim] as slot and the cache have them, got {tuple(k.shape)} and "
                          f"{tuple(v.shape)}")
     kp, kt, kh = _heads(k, dt, "k")
@@ -931,10 +927,10 @@ def scoot_paged_attention(ctx, q, k_cache, v_cache, block_table, query_start, kv
     """q, out: device [T][heads][dim] of the cache's type (last axis contiguous); block_table int32 [R][width],
     query_start int32 [R + 1], kv_len int32 [R]; lse: device float32 [T][heads] or None."""
     import torch
-    L, ref = _kv(k_cache, v_cache)
+    _, ref, D, _ = _kv(k_cache, v_cache)
     R, shape, dt, h = kv_len.numel(), q.shape, k_cache.dtype, _h(ctx)
-    if shape != out.shape or len(shape) != 3 or shape[2] != L.head_dim:
-        raise ValueError(f"q and out must be [T][heads][{L.head_dim}] of one shape, got {tuple(shape)} and "
+    if shape != out.shape or len(shape) != 3 or shape[2] != D:
+        raise ValueError(f"q and out must be [T][heads][{D}] of one shape, got {tuple(shape)} and "
                          f"{tuple(out.shape)}")
     if block_table.dim() != 2 or block_table.shape[0] != R or query_start.numel() != R + 1 or \
             (lse is not None and lse.shape != shape[:2]):
