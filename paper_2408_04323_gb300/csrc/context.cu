@@ -150,10 +150,6 @@ scoot_status scoot_ctx_create(int32_t device, scoot_ctx** out) {
         return SCOOT_ECUDA;
     }
     ctx->d_count = ctx->d_err + 64;
-    if (cudaDeviceGetAttribute(&ctx->sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || ctx->sms < 1) {
-        cudaGetLastError();
-        ctx->sms = 1;
-    }
     *out = ctx;
     return SCOOT_OK;
 }

@@ -31,7 +31,7 @@ struct scoot_ctx {
     std::vector<void*> ws_kept;  // earlier ones that graphs may use, freed with the context
     size_t ws_kept_bytes = 0;
     uint32_t* d_err = nullptr;   // device error word, followed by the counters
-    int32_t sms = 0;             // multiprocessors of the device
+    int32_t sms = 0;             // multiprocessors of the device, once scoot_sms has asked
     uint32_t attn_set = 0;       // paged_attn.cu's kernels whose shared memory has been asked for
     uint32_t* d_count = nullptr; // SCOOT_COUNTS arrival counters, zero between calls (paged_attn.cu)
     // Phase timing (scoot_ctx_set_timing): events recorded between the
@@ -142,10 +142,11 @@ scoot_status scoot_marks_begin(scoot_ctx* ctx, void* st);
 scoot_status scoot_mark(scoot_ctx* ctx, void* st, int32_t kind);
 
 // Checks shared by the device entry points.
+int32_t scoot_sms(scoot_ctx* ctx);  // multiprocessors of the device
 scoot_status scoot_check_kv(scoot_ctx* ctx, const scoot_kv_layout* L, const void* k_cache, const void* v_cache);
 // A (token, head, dim) array of the cache's type: alignment and strides.
 scoot_status scoot_check_heads(scoot_ctx* ctx, const char* name, const void* p, int64_t ld_token, int64_t ld_head,
-                               int64_t n_tokens, int32_t n_heads, int32_t head_dim);
+                               int32_t head_dim);
 scoot_status scoot_check_pool(scoot_ctx* ctx, const uint32_t* cand, int64_t n, int64_t ld, int32_t d);
 
 #ifdef __CUDACC__

@@ -47,6 +47,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "internal.h"
 #include "mbarrier.cuh"
 
@@ -1320,13 +1322,13 @@ extern "C" scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_lay
     if (!(scale > 0.0f) || scale > 3.0e38f) return scoot_fail(ctx, SCOOT_EINVAL, "scale = %g must be positive and finite", scale);
     if (window < 0) return scoot_fail(ctx, SCOOT_EINVAL, "window = %d < 0", window);
     if (n_tokens == 0 || n_req == 0) return SCOOT_OK;
-    if ((s = scoot_check_heads(ctx, "q", q, q_ld_token, q_ld_head, n_tokens, n_heads, layout->head_dim)) != SCOOT_OK) return s;
-    if ((s = scoot_check_heads(ctx, "out", out, out_ld_token, out_ld_head, n_tokens, n_heads, layout->head_dim)) != SCOOT_OK)
+    if ((s = scoot_check_heads(ctx, "q", q, q_ld_token, q_ld_head, layout->head_dim)) != SCOOT_OK) return s;
+    if ((s = scoot_check_heads(ctx, "out", out, out_ld_token, out_ld_head, layout->head_dim)) != SCOOT_OK)
         return s;
     if (!query_start || !kv_len || (ld_table && !block_table)) return scoot_fail(ctx, SCOOT_EINVAL, "an array is NULL");
     const int D = layout->head_dim, G = n_heads / layout->n_kv_heads;
     if (!encode_tiled()) return scoot_fail(ctx, SCOOT_ECUDA, "the driver has no cuTensorMapEncodeTiled");
-    const int sms = ctx->sms < kMaxCtas ? ctx->sms : kMaxCtas;
+    const int sms = std::min(scoot_sms(ctx), kMaxCtas);
     AttnArgs a = {};
     const bool bf16 = layout->dtype == SCOOT_BF16;
     {
