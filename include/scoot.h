@@ -870,7 +870,7 @@ scoot_status scoot_kv_append(scoot_ctx* ctx, const scoot_kv_layout* layout, cons
  * n_kv_heads, query head h reads key-value head h / G:
  *   out[t][h] = sum_i softmax_i(scale q[t][h] . k_i) v_i,
  *   lse[t][h] = ln sum_i exp(scale q[t][h] . k_i).
- * A token that sees no key (kv_len 0, or p < 0) gets zeros and -inf.  What is
+ * A token that sees no key (kv_len 0, or if causal p < 0) gets zeros and -inf.  What is
  * in the cache past kv_len, and values that a token does not see, never reach
  * its output, be they infinite or NaN.  Rows of q past query_start[n_req] have
  * no output.
@@ -883,7 +883,7 @@ scoot_status scoot_kv_append(scoot_ctx* ctx, const scoot_kv_layout* layout, cons
  * ld_table * block_size, or a block id outside 0 .. n_blocks - 1 is flagged
  * (scoot_ctx_check: SCOOT_EDEVICE): a request with bad lengths has no output,
  * a bad block counts as zeros.
- * ld_table * block_size and n_tokens are at most 2^30, n_tokens * n_heads less than 2^31.
+ * ld_table * block_size, n_tokens and n_req are at most 2^30, n_tokens * n_heads less than 2^31.
  * SCOOT_EUNSUPPORTED for other head sizes, block sizes or types, and for more
  * than SCOOT_MAX_GROUP query heads per key-value head. */
 scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_layout* layout, const void* q, int64_t q_ld_token,

@@ -1316,7 +1316,8 @@ extern "C" scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_lay
     if (n_heads / layout->n_kv_heads > SCOOT_MAX_GROUP)
         return scoot_fail(ctx, SCOOT_EUNSUPPORTED, "%d query heads per key-value head, more than %d",
                           n_heads / layout->n_kv_heads, SCOOT_MAX_GROUP);
-    if (n_tokens < 0 || n_tokens > 0x40000000ll || n_tokens > 0x7FFFFFFFll / n_heads || n_req < 0 || ld_table < 0 || ld_table > (0x40000000ll / layout->block_size))
+    if (n_tokens < 0 || n_tokens > 0x40000000ll || n_tokens > 0x7FFFFFFFll / n_heads || n_req < 0 || n_req > 0x40000000 ||
+        ld_table < 0 || ld_table > 0x40000000ll / layout->block_size)
         return scoot_fail(ctx, SCOOT_EINVAL, "n_tokens = %lld, n_req = %d or ld_table = %lld out of range", (long long)n_tokens,
                           n_req, (long long)ld_table);
     if (!(scale > 0.0f) || scale > 3.0e38f) return scoot_fail(ctx, SCOOT_EINVAL, "scale = %g must be positive and finite", scale);

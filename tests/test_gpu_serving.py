@@ -545,6 +545,24 @@ def test_attention_refuses_bad_arguments(S, ctx):
     ctx.check()
 
 
+def test_attention_refuses_more_requests_than_its_sums_hold(S, ctx):
+    """By the C entry point, whose check of the sizes comes before that of the (missing) arrays."""
+    b = Batch([(100, 4)], seed=1)
+    ref = S._kv(b.k, b.v)[1]
+
+    def message(n_req):
+        status = S.lib().scoot_paged_attention(S._h(ctx), ref, None, 512, 128, 4, 4, None, None, n_req, None, 8, b.k.data_ptr(),
+                                               b.v.data_ptr(), 1.0, 1, 0, None, 512, 128, None, None)
+        with pytest.raises(S.ScootError) as e:
+            S._check(status, "scoot_paged_attention", S._h(ctx))
+        assert e.value.status == -1
+        return str(e.value)
+
+    assert "n_req" in message(2 ** 30 + 1) and "n_req" in message(-1)
+    assert "q is NULL" in message(2 ** 30)
+    ctx.check()
+
+
 def test_nothing_to_do_is_no_error(S, ctx):
     b = Batch([(100, 4)], seed=1)
     none = torch.empty((0, 4, 64), dtype=b.q.dtype, device="cuda")
