@@ -843,7 +843,7 @@ typedef struct {
  * position[t] (its place in its sequence, from 0); counts[2] = blocks taken,
  * requests refused.  Tokens from query_start[n_req] up to n_tokens, the
  * arrays' length, get slot -1 and position 0.
- * A negative length, a sequence longer than its row (ld_table * block_size),
+ * A negative length, a sequence longer than its row (ld_table * block_size) or 2^31 - 1,
  * more new tokens than n_tokens, or a block id outside 0 .. n_blocks - 1 is
  * flagged (scoot_ctx_check: SCOOT_EDEVICE); such a request is refused, tokens
  * past n_tokens are not written, and a token in such a block gets slot -1. */

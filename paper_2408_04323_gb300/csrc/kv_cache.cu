@@ -14,6 +14,7 @@ struct TabArgs {
     const int32_t* cached;
     const int32_t* fresh;
     int32_t n_req, bs_log;
+    int64_t longest;  // tokens that a row of the table and a 32-bit length hold
     int64_t n_blocks;
     int32_t* table;
     int64_t ld_table;
@@ -42,7 +43,7 @@ __device__ __forceinline__ TabRequest tab_request(const TabArgs& a, const int2* 
     q.cached = len.x;
     q.fresh = len.y;
     const int64_t total = (int64_t)q.cached + q.fresh;
-    q.bad = q.cached < 0 || q.fresh < 0 || total > (a.ld_table << a.bs_log);
+    q.bad = q.cached < 0 || q.fresh < 0 || total > a.longest;
     q.fresh = max(q.fresh, 0);  // a bad request's tokens still have their places in the batch
     const int64_t mask = (1 << a.bs_log) - 1;
     q.held = q.bad ? 0 : (int32_t)((q.cached + mask) >> a.bs_log);
@@ -310,6 +311,7 @@ scoot_status scoot_kv_tables(scoot_ctx* ctx, const int32_t* cached_len, const in
     a.fresh = new_len;
     a.n_req = n_req;
     a.bs_log = log2_block(block_size);
+    a.longest = std::min<int64_t>(ld_table << a.bs_log, 0x7FFFFFFFll);
     a.n_blocks = n_blocks;
     a.table = block_table;
     a.ld_table = ld_table;

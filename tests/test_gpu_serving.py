@@ -122,6 +122,24 @@ def test_tables_flag_bad_values(S, ctx, what):
     ctx.check()
 
 
+def test_tables_flag_a_length_beyond_32_bits(S, ctx):
+    """Rows wide enough for 2^31 tokens: the longest length is served, and one more token refused."""
+    bs, width = 256, (1 << 23) + 1
+    table = torch.zeros((2, width), dtype=torch.int32, device="cuda")
+    longest = 2 ** 31 - 1
+    out = {k: torch.full((n,), -7, dtype=t, device="cuda") for k, n, t in
+           (("query_start", 3, torch.int32), ("kv_len", 2, torch.int32), ("slot", 2, torch.int64), ("position", 2, torch.int32),
+            ("counts", 2, torch.int32))}
+    S.scoot_kv_tables(ctx, _i32([longest - 1, longest]), _i32([1, 1]), table, bs, 4, _i32([]), out["query_start"], out["kv_len"],
+                      out["slot"], out["position"], out["counts"])
+    assert out["query_start"].tolist() == [0, 1, 2] and out["counts"].tolist() == [0, 1]
+    assert out["kv_len"].tolist() == [longest, 0]
+    assert out["position"].tolist() == [longest - 1, longest] and out["slot"].tolist() == [(longest - 1) % bs, -1]
+    with pytest.raises(S.ScootError) as e:
+        ctx.check()
+    assert e.value.status == -4
+
+
 # ---------------------------------------------------------------------------------------------- append
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
