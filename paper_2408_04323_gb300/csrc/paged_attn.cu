@@ -24,7 +24,9 @@
 // units in a row, head by head and request by request, with an extra cost per item, are cut into equal ranges, one per
 // SM (a cut close to an item's start or end moves there): long sequences are split, short ones follow one another,
 // whatever the batch.  Each CTA takes the sums over the requests for itself (lengths are on the device), so the call is
-// one launch.  An item that lies in several ranges leaves its parts (O, m, l) in the workspace, and the CTA that comes last
+// one launch.  Items without keys (a sequence of no token, tokens before their sequence) are written by the warp that finds
+// them and go no further: the product warp holds back up to kBuf products until the next units' scores are issued, and
+// relies on every item that it is handed having a unit.  An item that lies in several ranges leaves its parts (O, m, l) in the workspace, and the CTA that comes last
 // (a counter per item) joins them in the ranges' order, so that the result does not depend on who was last.
 //
 // Warps 0-3 and 4-7: softmax of slots 0 and 1.  Warp 8: the products.  Warp 9: the items, and the copies of queries and
@@ -568,6 +570,24 @@ __device__ __noinline__ SlotSync join_parts(const AttnArgs& a, const float* part
     return sync;
 }
 
+// Zeros and -inf for the rows of an item without keys, by one warp.
+template <int D>
+__device__ __forceinline__ void no_keys(const AttnArgs& a, const Item& it) {
+    const int lane = threadIdx.x & 31, rows = it.ntok * a.group;
+#pragma unroll 1
+    for (int e = lane; e < rows * (D / 8); e += 32) {
+        const int q = e / (D / 8), t = q / a.group;
+        *reinterpret_cast<uint4*>(a.out + (int64_t)(it.tok + t) * a.out_ld_token + (int64_t)(it.h * a.group + q - t * a.group) * a.out_ld_head +
+                                  8 * (e % (D / 8))) = make_uint4(0, 0, 0, 0);
+    }
+    if (a.lse)
+#pragma unroll 1
+        for (int q = lane; q < rows; q += 32) {
+            const int t = q / a.group;
+            a.lse[(int64_t)(it.tok + t) * a.n_heads + it.h * a.group + q - t * a.group] = -INFINITY;
+        }
+}
+
 template <bool kBf16, int D>
 __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_constant__ AttnArgs a) {
     using Sh = Shape<D>;
@@ -785,6 +805,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 p = s + units;
                 ++j;
                 if (!here) continue;
+                if (units == 0) {  // not into the ring: no unit of such an item would make the product warp issue what it holds back
+                    no_keys<D>(a, it);
+                    continue;
+                }
                 it.u0 = t0 + lo;
                 it.nu = hi - lo;
                 it.first = blockIdx.x;
@@ -804,7 +828,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 }
                 __syncwarp();
                 ++n_item;
-                if (it.nu > 0) keys.begin(it);
+                keys.begin(it);
 #pragma unroll 1
                 for (int u = 0; u < it.nu && wait.ok; ++u) {
                     keys.tile(it, it.u0 + u, wait);
@@ -839,7 +863,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 const Item it = items[n_item % kRing];
                 if (it.stop) break;
                 warp_arrive(&bars[kItemEmpty + n_item % kRing]);
-                if (it.nu > 0) vals.begin(it);
+                vals.begin(it);
 #pragma unroll 1
                 for (int u = 0; u < it.nu && wait.ok; ++u) vals.tile(it, it.u0 + u, wait);
             }
@@ -1100,12 +1124,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 }
             }
             // ---- the end of the item: O and l of this part
-            if (it.nu > 0) {
-                wait.warp(&bars[kPvDone + 4 * s + (unit ? unit - 1 : 2)], unit ? uphase : uphase ^ 1u);
-                fence_after();
-            }
+            wait.warp(&bars[kPvDone + 4 * s + (unit ? unit - 1 : 2)], unit ? uphase : uphase ^ 1u);
+            fence_after();
             const bool poison = *reinterpret_cast<volatile int32_t*>(&items[ring].poison) != 0;
-            if (poison && busy && it.nu > 0) {
+            if (poison && busy) {
                 // the values that were replaced, added to the rows that see them
 #pragma unroll 1
                 for (int c = 0; c < D; c += 16) {
@@ -1134,12 +1156,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             }
             auto load_o = [&](int c, float* o) {  // columns c .. c + 31
                 uint32_t x[32];
-                if (it.nu > 0) {
-                    tmem_ld32(tO + c, x);
-                    tmem_wait_ld();
-                }
+                tmem_ld32(tO + c, x);
+                tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = it.nu > 0 ? __uint_as_float(x[i]) : 0.0f;
+                for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]);
             };
             const int head = it.h * a.group, tok = it.tok + tok0;
             const bool whole = it.n_parts == 1;
