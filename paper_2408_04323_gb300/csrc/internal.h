@@ -32,7 +32,7 @@ struct scoot_ctx {
     size_t ws_kept_bytes = 0;
     uint32_t* d_err = nullptr;   // device error word, followed by the counters
     int32_t sms = 0;             // multiprocessors of the device, once scoot_sms has asked
-    uint32_t attn_set = 0;       // paged_attn.cu's kernels whose shared memory has been asked for
+    uint32_t smem_set = 0;       // kernels whose shared memory has been asked for: bits 0-3 paged_attn.cu's, 4 kv_cache.cu's tables
     uint32_t* d_count = nullptr; // SCOOT_COUNTS arrival counters, zero between calls (paged_attn.cu)
     // Phase timing (scoot_ctx_set_timing): events recorded between the
     // launches of the last timed call, and the kind of each launch.

@@ -7,6 +7,7 @@
 namespace {
 
 constexpr int kTabThreads = 1024;
+constexpr uint32_t kTabSmemBit = 1u << 4;  // of scoot_ctx::smem_set
 constexpr int kTabStaged = 16384;  // requests whose lengths go to shared memory (139 KB with the gaps)
 
 // What scoot_kv_tables takes, by value.
@@ -328,9 +329,11 @@ scoot_status scoot_kv_tables(scoot_ctx* ctx, const int32_t* cached_len, const in
     if (blocks > scoot_sms(ctx)) blocks = scoot_sms(ctx);
     if (blocks < 1) blocks = 1;
     const size_t smem = n_req <= kTabStaged ? (size_t)(n_req + std::min(n_req, kTabThreads)) * sizeof(int2) : 0;
-    if (smem > 32768)  // beyond what a block has without asking, beside its static part
+    if (!(ctx->smem_set & kTabSmemBit)) {  // once per context, whatever this call's size: the static part counts as well
         SCOOT_CUDA(ctx, cudaFuncSetAttribute(kv_tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              (int)((kTabStaged + kTabThreads) * sizeof(int2))));
+        ctx->smem_set |= kTabSmemBit;
+    }
     kv_tables_kernel<<<(unsigned)blocks, kTabThreads, smem, static_cast<cudaStream_t>(stream)>>>(a);
     SCOOT_LAUNCHED(ctx);
     return SCOOT_OK;

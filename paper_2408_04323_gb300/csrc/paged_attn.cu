@@ -1311,9 +1311,9 @@ scoot_status launch(scoot_ctx* ctx, AttnArgs& a, int sms, cudaStream_t st) {
     a.parts = static_cast<float*>(ctx->ws);
     auto kern = paged_attn_kernel<kBf16, D>;
     const uint32_t bit = 1u << (2 * kBf16 + (D == 128));
-    if (!(ctx->attn_set & bit)) {  // once per context: the call is short
+    if (!(ctx->smem_set & bit)) {  // once per context: the call is short
         SCOOT_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem));
-        ctx->attn_set |= bit;
+        ctx->smem_set |= bit;
     }
     kern<<<(unsigned)sms, kThreads, Shape<D>::kSmem, st>>>(a);
     SCOOT_LAUNCHED(ctx);
