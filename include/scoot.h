@@ -872,8 +872,8 @@ scoot_status scoot_kv_append(scoot_ctx* ctx, const scoot_kv_layout* layout, cons
  *   lse[t][h] = ln sum_i exp(scale q[t][h] . k_i).
  * A token that sees no key (kv_len 0, or if causal p < 0) gets zeros and -inf.  What is
  * in the cache past kv_len, and values that a token does not see, never reach
- * its output, be they infinite or NaN.  Rows of q past query_start[n_req] have
- * no output.
+ * its output, be they infinite or NaN; those that it sees do, whatever their
+ * weight (each is positive).  Rows of q past query_start[n_req] have no output.
  * q and out: element (t, head, dim) at t * ld_token + head * ld_head + dim,
  * the cache's type and rules of alignment and stride; lse float32
  * [n_tokens][n_heads] or NULL; scale > 0, finite.  Scores, softmax statistics

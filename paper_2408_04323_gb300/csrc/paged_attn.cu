@@ -33,9 +33,14 @@
 // keys; warp 10: those of values.  A tile comes page by page through the block table, by TMA into a ring (128-byte
 // swizzle), a box of up to 128 tokens x 64 dimensions per page and half head.
 //
-// Values of keys that some row may not see: a probability of 0 times an infinity or NaN is NaN, so the value tiles at
-// the ends of the sequence and along the diagonal are looked through first: rows past the ends are set to zero, and a
-// value that is not finite is replaced by zero and the item marked; rows that do see it add it at the end.
+// Values that are not finite: a probability of 0 times an infinity or NaN is NaN, and so
+//   * the value tiles at the ends of the sequence and along the diagonal, whose keys some row may not see, are looked through
+//     first: rows past the ends are set to zero, and a value that is not finite is replaced by zero and the item marked;
+//   * where a row's probability of a key that it sees has rounded to zero, and where a copy of a row has zeros at the keys of
+//     the other copies, the product leaves a NaN.
+// By the definition each probability is positive, and an infinity or NaN that a row sees is its sum's, whatever its weight.
+// So an item that is marked, or whose sums are not all finite, has the values of its keys looked through at its end, and
+// each row's sums set by those that it sees (odd_values); the joins give a weight of zero no say over such sums.
 //
 // What bounds it, as measured (heads of 128 in blocks of 16, four query heads per key-value head, bf16):
 //   * 256 sequences of 64 to 2560 tokens, one new token each: 220 us, 6.3 TB/s, 92% of the copy rate: HBM (a tile of
@@ -194,10 +199,8 @@ template <bool kBf16>
 __device__ __forceinline__ uint32_t top_exponent(uint32_t w) {
     return kBf16 ? (w & 0x7F807F80u) + 0x00800080u : (w & 0x7C007C00u) + 0x04000400u;
 }
-template <bool kBf16>
-__device__ __forceinline__ float value16(uint16_t x) {
-    return kBf16 ? __bfloat162float(__ushort_as_bfloat16(x)) : __half2float(__ushort_as_half(x));
-}
+// x of a sum whose weight is zero: what is finite has none, the rest all of it.
+__device__ __forceinline__ float weightless(float x) { return fabsf(x) < INFINITY ? 0.0f : x; }
 
 // One request's lengths, empty if they are bad.
 struct Req {
@@ -453,6 +456,73 @@ struct SlotSync {
     }
 };
 
+// O of a warp's rows, each of which sees the keys [k0, k1), after a part of nu tiles with values that are not finite: an
+// infinity or NaN among those that the row sees (a copy: of its own keys in a tile) decides its sum, and a copy's NaN that
+// only the others' keys account for was a zero times theirs.  The keys are [begin, end), 32 at a time, a lane each.
+template <bool kBf16, int D>
+__device__ __noinline__ void odd_values(const AttnArgs& a, uint32_t tO, int h, int r, int u0, int nu, int begin, int end, int k0, int k1,
+                                        int rep_log, int copy) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int c = 0; c < D; c += 32) {
+        uint32_t pos = 0, neg = 0, others = 0;  // columns with +inf, -inf, both (a NaN counts as both); with any of other copies
+#pragma unroll 1
+        for (int key0 = max(u0 * kKeys, begin & ~31); key0 < min((u0 + nu) * kKeys, end); key0 += 32) {
+            const int key = key0 + lane;
+            uint4 w[4] = {};
+            if (key >= begin && key < end) {
+                const int id = a.table[(int64_t)r * a.ld_table + (key >> a.bs_log)];
+                if (id >= 0 && id < a.n_blocks) {
+                    const uint4* v = reinterpret_cast<const uint4*>(a.v + id * a.ld_block + (key & ((1 << a.bs_log) - 1)) * a.ld_token +
+                                                                    h * a.ld_head + c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = v[i];
+                }
+            }
+            const uint32_t* x = reinterpret_cast<const uint32_t*>(w);
+            uint32_t p = 0, n = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t odd = not_finite<kBf16>(x[i]);
+                const uint32_t nan = odd & ~__vcmpeq2(x[i] & (kBf16 ? 0x007F007Fu : 0x03FF03FFu), 0u);
+                const uint32_t sign = __vcmpgeu2(x[i], 0x80008000u);
+                const uint32_t up = nan | (odd & ~sign), down = nan | (odd & sign);
+                p |= ((up & 1u) | (up >> 30 & 2u)) << (2 * i);
+                n |= ((down & 1u) | (down >> 30 & 2u)) << (2 * i);
+            }
+            uint32_t some = __ballot_sync(0xffffffffu, (p | n) != 0);
+            const bool own = rep_log == 0 || (key0 % kKeys) >> (7 - rep_log) == copy;
+            while (some) {
+                const int src = __ffs(some) - 1;
+                some &= some - 1;
+                const uint32_t ps = __shfl_sync(0xffffffffu, p, src), ns = __shfl_sync(0xffffffffu, n, src);
+                const bool sees = key0 + src >= k0 && key0 + src < k1;
+                if (sees && own) {
+                    pos |= ps;
+                    neg |= ns;
+                } else if (sees) {
+                    others |= ps | ns;
+                }
+            }
+        }
+        if (!__any_sync(0xffffffffu, (pos | neg | others) != 0)) continue;
+#pragma unroll 1
+        for (int half = 0; half < 32; half += 16) {
+            uint32_t o[16];
+            tmem_ld16(tO + c + half, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t bit = 1u << (half + i), up = pos & bit, down = neg & bit;
+                if (up | down) o[i] = up && down ? 0x7FFFFFFFu : up ? 0x7F800000u : 0xFF800000u;
+                else if ((others & bit) && __uint_as_float(o[i]) != __uint_as_float(o[i])) o[i] = 0u;
+            }
+            tmem_st16(tO + c + half, o);
+        }
+        tmem_wait_st();
+    }
+}
+
 // Row q of a slot, tokens from tok on, the group's first head `head`: where it goes.
 __device__ __forceinline__ uint16_t* out_row(const AttnArgs& a, int tok, int head, int q) {
     const int t = q * a.inv_group >> 16;
@@ -461,6 +531,23 @@ __device__ __forceinline__ uint16_t* out_row(const AttnArgs& a, int tok, int hea
 __device__ __forceinline__ float* lse_row(const AttnArgs& a, int tok, int head, int q) {
     const int t = q * a.inv_group >> 16;
     return a.lse + (int64_t)(tok + t) * a.n_heads + head + q - t * a.group;
+}
+
+// Four columns (at: in groups of four) of a row's V parts by their weights, where some of the sums are not finite.
+template <int D>
+__device__ __noinline__ float4 join_odd(const float* part, const float* w, int V, int at) {
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int p = 0; p < V; ++p) {
+        float4 v = __ldcg(reinterpret_cast<const float4*>(part_buf<D>(part, p)) + at);
+        float f = w[p];
+        if (f == 0.0f) {
+            v = make_float4(weightless(v.x), weightless(v.y), weightless(v.z), weightless(v.w));
+            f = 1.0f;
+        }
+        acc = make_float4(fmaf(f, v.x, acc.x), fmaf(f, v.y, acc.y), fmaf(f, v.z, acc.z), fmaf(f, v.w, acc.w));
+    }
+    return acc;
 }
 
 // The weighted sums of V parts of rows q0 .. q0 + nq - 1 (weights w [row][V]).  A thread has four columns of R rows, 128 /
@@ -500,9 +587,12 @@ __device__ __forceinline__ void join_rows(const AttnArgs& a, const float* part, 
         }
 #pragma unroll
         for (int i = 0; i < R; ++i)
-            if (q + i * kStep < nq)
+            if (q + i * kStep < nq) {
+                if (const float sum = (acc[i].x + acc[i].y) + (acc[i].z + acc[i].w); sum != sum)
+                    acc[i] = join_odd<D>(part, w + (q + i * kStep) * V, V, (q0 + q + i * kStep) * kGroups + c);
                 *reinterpret_cast<uint2*>(out_row(a, tok, head, q0 + q + i * kStep) + 4 * c) =
                     make_uint2(pack16<kBf16>(acc[i].x, acc[i].y), pack16<kBf16>(acc[i].z, acc[i].w));
+            }
     }
 }
 
@@ -1127,32 +1217,19 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             wait.warp(&bars[kPvDone + 4 * s + (unit ? unit - 1 : 2)], unit ? uphase : uphase ^ 1u);
             fence_after();
             const bool poison = *reinterpret_cast<volatile int32_t*>(&items[ring].poison) != 0;
-            if (poison && busy) {
-                // the values that were replaced, added to the rows that see them
+            if (busy) {
+                // 0 times the sums: NaN if one of them is not finite (those of a row whose scores are NaN stay as they are)
+                float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-                for (int c = 0; c < D; c += 16) {
-                    uint32_t x[16];
-                    tmem_ld16(tO + c, x);
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t x[32];
+                    tmem_ld32(tO + c, x);
                     tmem_wait_ld();
-#pragma unroll 1
-                    for (int u = it.u0; u < it.u0 + it.nu; ++u) {
-                        const int w0 = u * kKeys + (copy << (7 - it.rep_log)), w1 = w0 + (kKeys >> it.rep_log);
-#pragma unroll 1
-                        for (int key = max(k0, w0); key < min(k1, w1); ++key) {
-                            const int id = a.table[(int64_t)it.r * a.ld_table + (key >> a.bs_log)];
-                            if (id < 0 || id >= a.n_blocks) continue;
-                            const uint16_t* v = a.v + id * a.ld_block + (key & ((1 << a.bs_log) - 1)) * a.ld_token + it.h * a.ld_head + c;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const uint32_t w = v[i];
-                                if (not_finite<kBf16>(w)) x[i] = __float_as_uint(__uint_as_float(x[i]) + value16<kBf16>((uint16_t)w));
-                            }
-                        }
-                    }
-                    __syncwarp();
-                    tmem_st16(tO + c, x);
+                    for (int i = 0; i < 32; ++i) y[i & 3] = fmaf(__uint_as_float(x[i]), 0.0f, y[i & 3]);
                 }
-                tmem_wait_st();
+                if (__any_sync(0xffffffffu, poison || (live && l == l && (y[0] + y[1]) + (y[2] + y[3]) != 0.0f)))
+                    odd_values<kBf16, D>(a, tO, it.h, it.r, it.u0, it.nu, it.begin, it.end, k0, k1, it.rep_log, copy);
             }
             auto load_o = [&](int c, float* o) {  // columns c .. c + 31
                 uint32_t x[32];
@@ -1182,7 +1259,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                     const float2 v = ml_s[s][c * per_copy + rr];
                     L = fmaf(exp2_hw(v.x - Ms), v.y, L);
                 }
-                const float w = exp2_hw(m - Ms), f = whole ? w * inverse_sum(L) : w;
+                const float w = exp2_hw(m - Ms), f = whole ? w * inverse_sum(L) : w, g = f == 0.0f ? 1.0f : f;
                 if (copy == 0 && live) {
                     if (!whole) *reinterpret_cast<float2*>(buf + kRows * D + 2 * rr) = make_float2(M, L);
                     else if (a.lse) *lse_row(a, tok, head, rr) = L == 0.0f ? -INFINITY : (M + __log2f(L)) * kLn2;
@@ -1197,11 +1274,14 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                             float o[32];
                             load_o(c0 + c, o);
                             if (live) {
+                                if (f == 0.0f)
+#pragma unroll
+                                    for (int i = 0; i < 32; ++i) o[i] = weightless(o[i]);
                                 const int at = copy * rows + rr;
                                 float4* dst = reinterpret_cast<float4*>(scratch) + at * groups;
 #pragma unroll
                                 for (int i = 0; i < 8; ++i)
-                                    dst[(c / 4 + i) ^ (at & 7)] = make_float4(o[4 * i] * f, o[4 * i + 1] * f, o[4 * i + 2] * f, o[4 * i + 3] * f);
+                                    dst[(c / 4 + i) ^ (at & 7)] = make_float4(o[4 * i] * g, o[4 * i + 1] * g, o[4 * i + 2] * g, o[4 * i + 3] * g);
                             }
                         }
                     wg_sync();
