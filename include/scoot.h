@@ -876,7 +876,7 @@ scoot_status scoot_kv_append(scoot_ctx* ctx, const scoot_kv_layout* layout, cons
  * weight (each is positive).  Rows of q past query_start[n_req] have no output.
  * q and out: element (t, head, dim) at t * ld_token + head * ld_head + dim,
  * the cache's type and rules of alignment and stride; lse float32
- * [n_tokens][n_heads] or NULL; scale > 0, finite.  Scores, softmax statistics
+ * [n_tokens][n_heads] or NULL; 0 < scale <= 2.3e38.  Scores, softmax statistics
  * and sums are held in fp32; probabilities are rounded to the cache's type for
  * the product with the values, as the tensor cores take them.
  * A query_start that decreases or passes n_tokens, a kv_len outside 0 ..

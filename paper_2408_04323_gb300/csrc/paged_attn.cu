@@ -78,6 +78,7 @@ constexpr int kBufs = 4;         // part buffers of a CTA
 constexpr int kScratch = 16384;  // bytes of a slot's scratch: 32 columns of sums of its rows, or weights of parts
 constexpr int kHalf = kKeys * 128;  // bytes of a tile's half: 128 keys x 64 dimensions
 constexpr int kMaxCtas = (int)(SCOOT_COUNTS / 2);
+constexpr float kMaxScale = 2.3e38f;  // times log2 e it is still finite
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
 
 template <int D>
@@ -1420,7 +1421,8 @@ extern "C" scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_lay
         ld_table < 0 || ld_table > 0x40000000ll / layout->block_size)
         return scoot_fail(ctx, SCOOT_EINVAL, "n_tokens = %lld, n_req = %d or ld_table = %lld out of range", (long long)n_tokens,
                           n_req, (long long)ld_table);
-    if (!(scale > 0.0f) || scale > 3.0e38f) return scoot_fail(ctx, SCOOT_EINVAL, "scale = %g must be positive and finite", scale);
+    if (!(scale > 0.0f) || scale > kMaxScale)
+        return scoot_fail(ctx, SCOOT_EINVAL, "scale = %g must be positive and at most %g", scale, kMaxScale);
     if (window < 0) return scoot_fail(ctx, SCOOT_EINVAL, "window = %d < 0", window);
     if (n_tokens == 0 || n_req == 0) return SCOOT_OK;
     if ((s = scoot_check_heads(ctx, "q", q, q_ld_token, q_ld_head, layout->head_dim)) != SCOOT_OK) return s;
