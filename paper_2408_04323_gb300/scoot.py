@@ -838,6 +838,14 @@ def _current_stream(device: int) -> int:
     return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
 
 
+_I32_MAX = 0x7FFFFFFF
+
+
+def _i32_arg(x):
+    """An int as the nearest of the library's (ctypes drops the upper bits of one that does not fit)."""
+    return min(max(int(x), -1), _I32_MAX)
+
+
 def _on(stream, t):
     return _current_stream(t.get_device()) if stream is None else _stream(stream)
 
@@ -896,7 +904,9 @@ def scoot_kv_tables(ctx, cached_len, new_len, block_table, block_size, n_blocks,
             query_start.numel() != R + 1 or counts.numel() != 2 or position.numel() != T:
         raise ValueError("array lengths do not match: [R] cached_len, new_len, kv_len; [R][width] block_table; "
                          "[R + 1] query_start; [T] slot, position; [2] counts")
-    status = lib().scoot_kv_tables(h, _ptr(cached_len, i32, "cached_len"), _ptr(new_len, i32, "new_len"), R, int(block_size),
+    if R > _I32_MAX:
+        raise ValueError(f"{R} requests are more than {_I32_MAX}")
+    status = lib().scoot_kv_tables(h, _ptr(cached_len, i32, "cached_len"), _ptr(new_len, i32, "new_len"), R, _i32_arg(block_size),
                                    int(n_blocks), _ptr(block_table, i32, "block_table"), block_table.shape[1],
                                    _ptr(free_blocks, i32, "free_blocks"), free_blocks.numel(),
                                    _ptr(query_start, i32, "query_start"), _ptr(kv_len, i32, "kv_len"),
@@ -940,9 +950,9 @@ def scoot_paged_attention(ctx, q, k_cache, v_cache, block_table, query_start, kv
     op, ot, oh = _heads(out, dt, "out")
     i32 = torch.int32
     status = lib().scoot_paged_attention(h, ref, qp, qt, qh, shape[1], shape[0], _ptr(query_start, i32, "query_start"),
-                                         _ptr(kv_len, i32, "kv_len"), R, _ptr(block_table, i32, "block_table"),
+                                         _ptr(kv_len, i32, "kv_len"), _i32_arg(R), _ptr(block_table, i32, "block_table"),
                                          block_table.shape[1], k_cache.data_ptr(), v_cache.data_ptr(), float(scale),
-                                         1 if causal else 0, int(window), op, ot, oh,
+                                         1 if causal else 0, _i32_arg(window), op, ot, oh,
                                          None if lse is None else _ptr(lse, torch.float32, "lse"), _on(stream, q))
     if status:
         _check(status, "scoot_paged_attention", h)
