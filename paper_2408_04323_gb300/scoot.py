@@ -824,18 +824,38 @@ F16, BF16 = 0, 1
 MAX_GROUP = 128
 
 
-def _ptr(t, dtype, name):
-    """_dev for a tensor that must be there, as an int."""
-    if t.dtype is dtype and t.is_cuda and t.is_contiguous():
+def _handle(ctx, t, name):
+    """The context's handle, and the index of the device that a call's tensors must be on: the context's, or t's where ctx
+    is a bare handle."""
+    if isinstance(ctx, Context):
+        return ctx.handle, ctx.device
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA torch tensor (device memory)")
+    return ctx, t.get_device()
+
+
+def _elsewhere(t, name, device):
+    return ValueError(f"{name} is on device {t.get_device()}, and the call's device is {device}")
+
+
+def _ptr(t, dtype, name, device):
+    """_dev for a tensor that must be there, on the device of that index, as an int."""
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous():
         return t.data_ptr()
+    if t.is_cuda and t.get_device() != device:
+        raise _elsewhere(t, name, device)
     return _dev(t, dtype, name).value
+
+
+@functools.lru_cache(maxsize=1)
+def _raw_stream():
+    import torch
+    return getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 def _current_stream(device: int) -> int:
     """Handle of the device's current stream (torch.cuda.current_stream builds an object around it, in 3 us)."""
-    import torch
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+    return _raw_stream()(device)
 
 
 _I32_MAX = 0x7FFFFFFF
@@ -843,22 +863,24 @@ _I32_MAX = 0x7FFFFFFF
 
 def _i32_arg(x):
     """An int as the nearest of the library's (ctypes drops the upper bits of one that does not fit)."""
-    return min(max(int(x), -1), _I32_MAX)
+    return int(x) if -1 <= x <= _I32_MAX else -1 if x < 0 else _I32_MAX
 
 
-def _on(stream, t):
-    return _current_stream(t.get_device()) if stream is None else _stream(stream)
+def _on(stream, device):
+    return _current_stream(device) if stream is None else _stream(stream)
 
 
-def _heads(t, dtype, name):
+def _heads(t, dtype, name, device):
     """(pointer, token stride, head stride) of a CUDA tensor [tokens][heads][dim] whose dim is contiguous.  The stride
     of an axis of one (torch may give it any) counts as the axis's size."""
     stride = t.stride()
-    if not (t.dtype is dtype and t.is_cuda and len(stride) == 3 and stride[2] == 1):
+    if not (t.dtype is dtype and t.get_device() == device and len(stride) == 3 and stride[2] == 1):
         if not t.is_cuda:
             raise TypeError(f"{name} must be a CUDA torch tensor (device memory)")
         if t.dtype is not dtype:
             raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+        if t.get_device() != device:
+            raise _elsewhere(t, name, device)
         raise ValueError(f"{name} must be [tokens][heads][dim] and contiguous along its last axis, got {tuple(t.shape)}")
     n, h, d = t.shape
     return t.data_ptr(), (stride[0] if n > 1 else h * d), (stride[1] if h > 1 else d)
@@ -872,14 +894,19 @@ def _layout(bf16, shape, stride):
     return L, C.byref(L), d, h
 
 
-def _kv(k_cache, v_cache):
-    """(layout, reference to it, head size, key-value heads) of a cache."""
+def _kv(k_cache, v_cache, device=None):
+    """(layout, reference to it, head size, key-value heads) of a cache on the device of that index, or on k_cache's."""
     import torch
+    if device is None:
+        device = _handle(None, k_cache, "k_cache")[1]
     dt, shape, stride = k_cache.dtype, k_cache.shape, k_cache.stride()
     if not (dt is v_cache.dtype and (dt is torch.bfloat16 or dt is torch.float16) and len(shape) == 4 and shape == v_cache.shape
-            and stride == v_cache.stride() and stride[3] == 1 and k_cache.is_cuda and v_cache.is_cuda):
+            and stride == v_cache.stride() and stride[3] == 1 and k_cache.get_device() == device and v_cache.get_device() == device):
         if not (k_cache.is_cuda and v_cache.is_cuda):
             raise TypeError("k_cache and v_cache must be CUDA torch tensors (device memory)")
+        for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+            if t.get_device() != device:
+                raise _elsewhere(t, name, device)
         if dt is not v_cache.dtype or not (dt is torch.bfloat16 or dt is torch.float16):
             raise TypeError(f"k_cache and v_cache must both be float16 or bfloat16, got {dt} and {v_cache.dtype}")
         raise ValueError("k_cache and v_cache must be [blocks][tokens][heads][dim] of one shape and the same strides, contiguous "
@@ -899,19 +926,20 @@ def scoot_kv_tables(ctx, cached_len, new_len, block_table, block_size, n_blocks,
     query_start [R + 1]; position [T]; counts [2].  slot: device int64 [T]."""
     import torch
     i32 = torch.int32
-    R, T, h = cached_len.numel(), slot.numel(), _h(ctx)
+    h, device = _handle(ctx, cached_len, "cached_len")
+    R, T = cached_len.numel(), slot.numel()
     if block_table.dim() != 2 or block_table.shape[0] != R or new_len.numel() != R or kv_len.numel() != R or \
             query_start.numel() != R + 1 or counts.numel() != 2 or position.numel() != T:
         raise ValueError("array lengths do not match: [R] cached_len, new_len, kv_len; [R][width] block_table; "
                          "[R + 1] query_start; [T] slot, position; [2] counts")
     if R > _I32_MAX:
         raise ValueError(f"{R} requests are more than {_I32_MAX}")
-    status = lib().scoot_kv_tables(h, _ptr(cached_len, i32, "cached_len"), _ptr(new_len, i32, "new_len"), R, _i32_arg(block_size),
-                                   int(n_blocks), _ptr(block_table, i32, "block_table"), block_table.shape[1],
-                                   _ptr(free_blocks, i32, "free_blocks"), free_blocks.numel(),
-                                   _ptr(query_start, i32, "query_start"), _ptr(kv_len, i32, "kv_len"),
-                                   _ptr(slot, torch.int64, "slot"), _ptr(position, i32, "position"), T,
-                                   _ptr(counts, i32, "counts"), _on(stream, counts))
+    status = lib().scoot_kv_tables(h, _ptr(cached_len, i32, "cached_len", device), _ptr(new_len, i32, "new_len", device), R,
+                                   _i32_arg(block_size), int(n_blocks), _ptr(block_table, i32, "block_table", device), block_table.shape[1],
+                                   _ptr(free_blocks, i32, "free_blocks", device), free_blocks.numel(),
+                                   _ptr(query_start, i32, "query_start", device), _ptr(kv_len, i32, "kv_len", device),
+                                   _ptr(slot, torch.int64, "slot", device), _ptr(position, i32, "position", device), T,
+                                   _ptr(counts, i32, "counts", device), _on(stream, device))
     if status:
         _check(status, "scoot_kv_tables", h)
 
@@ -919,15 +947,16 @@ def scoot_kv_tables(ctx, cached_len, new_len, block_table, block_size, n_blocks,
 def scoot_kv_append(ctx, k, v, slot, k_cache, v_cache, stream=None) -> None:
     """k, v: device [T][heads][dim] of the cache's type (last axis contiguous); slot: device int64 [T]."""
     import torch
-    _, ref, D, Hkv = _kv(k_cache, v_cache)
-    T, dt, h = slot.numel(), k_cache.dtype, _h(ctx)
+    h, device = _handle(ctx, k_cache, "k_cache")
+    _, ref, D, Hkv = _kv(k_cache, v_cache, device)
+    T, dt = slot.numel(), k_cache.dtype
     if k.shape != v.shape or k.shape != (T, Hkv, D):
         raise ValueError(f"k and v must be [T][heads][dim] as slot and the cache have them, got {tuple(k.shape)} and "
                          f"{tuple(v.shape)}")
-    kp, kt, kh = _heads(k, dt, "k")
-    vp, vt, vh = _heads(v, dt, "v")
-    status = lib().scoot_kv_append(h, ref, kp, kt, kh, vp, vt, vh, _ptr(slot, torch.int64, "slot"), T,
-                                   k_cache.data_ptr(), v_cache.data_ptr(), _on(stream, slot))
+    kp, kt, kh = _heads(k, dt, "k", device)
+    vp, vt, vh = _heads(v, dt, "v", device)
+    status = lib().scoot_kv_append(h, ref, kp, kt, kh, vp, vt, vh, _ptr(slot, torch.int64, "slot", device), T,
+                                   k_cache.data_ptr(), v_cache.data_ptr(), _on(stream, device))
     if status:
         _check(status, "scoot_kv_append", h)
 
@@ -937,8 +966,9 @@ def scoot_paged_attention(ctx, q, k_cache, v_cache, block_table, query_start, kv
     """q, out: device [T][heads][dim] of the cache's type (last axis contiguous); block_table int32 [R][width],
     query_start int32 [R + 1], kv_len int32 [R]; lse: device float32 [T][heads] or None."""
     import torch
-    _, ref, D, _ = _kv(k_cache, v_cache)
-    R, shape, dt, h = kv_len.numel(), q.shape, k_cache.dtype, _h(ctx)
+    h, device = _handle(ctx, k_cache, "k_cache")
+    _, ref, D, _ = _kv(k_cache, v_cache, device)
+    R, shape, dt = kv_len.numel(), q.shape, k_cache.dtype
     if shape != out.shape or len(shape) != 3 or shape[2] != D:
         raise ValueError(f"q and out must be [T][heads][{D}] of one shape, got {tuple(shape)} and "
                          f"{tuple(out.shape)}")
@@ -946,13 +976,13 @@ def scoot_paged_attention(ctx, q, k_cache, v_cache, block_table, query_start, kv
             (lse is not None and lse.shape != shape[:2]):
         raise ValueError("array lengths do not match: [R] kv_len; [R][width] block_table; [R + 1] query_start; "
                          "[T][heads] lse")
-    qp, qt, qh = _heads(q, dt, "q")
-    op, ot, oh = _heads(out, dt, "out")
+    qp, qt, qh = _heads(q, dt, "q", device)
+    op, ot, oh = _heads(out, dt, "out", device)
     i32 = torch.int32
-    status = lib().scoot_paged_attention(h, ref, qp, qt, qh, shape[1], shape[0], _ptr(query_start, i32, "query_start"),
-                                         _ptr(kv_len, i32, "kv_len"), _i32_arg(R), _ptr(block_table, i32, "block_table"),
+    status = lib().scoot_paged_attention(h, ref, qp, qt, qh, shape[1], shape[0], _ptr(query_start, i32, "query_start", device),
+                                         _ptr(kv_len, i32, "kv_len", device), _i32_arg(R), _ptr(block_table, i32, "block_table", device),
                                          block_table.shape[1], k_cache.data_ptr(), v_cache.data_ptr(), float(scale),
                                          1 if causal else 0, _i32_arg(window), op, ot, oh,
-                                         None if lse is None else _ptr(lse, torch.float32, "lse"), _on(stream, q))
+                                         None if lse is None else _ptr(lse, torch.float32, "lse", device), _on(stream, device))
     if status:
         _check(status, "scoot_paged_attention", h)

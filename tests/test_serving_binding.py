@@ -103,3 +103,68 @@ def test_requests_beyond_32_bits_are_not_a_few(S, lib):
         _tables(S, R=2 ** 32 + 2)
     _attention(S, R=2 ** 32 + 2)
     assert lib.calls[0][9] == 2 ** 31 - 1   # which the library refuses
+
+
+def _append(S, ctx=None, change={}, **kw):
+    a = {"k": Tensor((4, 2, 64), BF16), "v": Tensor((4, 2, 64), BF16), "slot": Tensor((4,), torch.int64),
+         "k_cache": Tensor((8, 16, 2, 64), BF16), "v_cache": Tensor((8, 16, 2, 64), BF16), **change}
+    S.scoot_kv_append(ctx, *a.values(), **kw)
+
+
+def _context(S, device):
+    ctx = object.__new__(S.Context)   # without a GPU there is none to be had
+    ctx.device, ctx.handle = device, None
+    return ctx
+
+
+CALLS = {"tables": (_tables, {n: ((2,), I32) for n in ("cached_len", "new_len", "kv_len", "counts")} |
+                    {"block_table": ((2, 5), I32), "free_blocks": ((3,), I32), "query_start": ((3,), I32),
+                     "slot": ((4,), torch.int64), "position": ((4,), I32)}),
+         "append": (_append, {n: ((4, 2, 64), BF16) for n in "kv"} | {n: ((8, 16, 2, 64), BF16) for n in ("k_cache", "v_cache")} |
+                    {"slot": ((4,), torch.int64)}),
+         "attention": (_attention, {n: ((4, 4, 64), BF16) for n in ("q", "out")} |
+                       {n: ((8, 16, 2, 64), BF16) for n in ("k_cache", "v_cache")} |
+                       {"block_table": ((2, 5), I32), "query_start": ((3,), I32), "kv_len": ((2,), I32)})}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_a_tensor_on_another_device_than_the_contexts_is_refused(S, lib, name):
+    call, tensors = CALLS[name]
+    for ctx in (_context(S, 0), None):   # a bare handle's device is that of the call's first array
+        call(S, ctx)
+        for which, (shape, dtype) in tensors.items():
+            with pytest.raises(ValueError, match="device"):
+                call(S, ctx, change={which: Tensor(shape, dtype, device=1)})
+    with pytest.raises(ValueError, match="device"):
+        call(S, _context(S, 1))
+    assert len(lib.calls) == 2
+
+
+def test_a_lse_on_another_device_is_refused(S, lib):
+    _attention(S, lse=Tensor((4, 4), torch.float32))
+    with pytest.raises(ValueError, match="lse"):
+        _attention(S, lse=Tensor((4, 4), torch.float32, device=1))
+    assert len(lib.calls) == 1
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_host_memory_is_refused(S, lib, name):
+    call, tensors = CALLS[name]
+    host = {which: torch.zeros(shape, dtype=dtype) for which, (shape, dtype) in tensors.items()}
+    for ctx in (_context(S, 0), None):
+        for which, t in host.items():
+            with pytest.raises(TypeError, match="CUDA"):
+                call(S, ctx, change={which: t})
+        with pytest.raises(TypeError, match="CUDA"):
+            call(S, ctx, change=host)
+    if name != "tables":
+        with pytest.raises(TypeError, match="CUDA"):
+            S.kv_layout(host["k_cache"], host["v_cache"])
+    assert not lib.calls
+
+
+def test_the_default_stream_is_the_devices_current_one(S, lib):
+    for device, ctx in ((0, _context(S, 0)), (0, None)):
+        for call, at in ((_tables, 16), (_append, 12), (_attention, 21)):
+            call(S, ctx)
+            assert lib.calls[-1][at] == 1000 + device
