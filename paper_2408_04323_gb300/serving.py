@@ -54,12 +54,20 @@ class AttentionEngine:
 
     def step(self, new, q, k, v, out):
         """new [max_seqs]: new tokens per row; q, out [layers][tokens][heads][dim] and k, v [layers][tokens][kv heads][dim]
-        with the rows' tokens back to back.  Fills out; returns the number of tokens."""
-        new = np.asarray(new, np.int32)
+        with the rows' tokens back to back.  Fills out; returns the number of tokens.  A step that cannot be (counts,
+        lengths, blocks or shapes) is refused before anything is changed."""
+        new = np.asarray(new, np.int64)
+        if new.shape != self.cached.shape or new.min(initial=0) < 0:
+            raise ValueError(f"new must be {len(self.cached)} counts, none of them negative, got {new.tolist()}")
         n = int(new.sum())
         if n > self.max_tokens or (self.cached + new).max(initial=0) > self.max_len:
             raise ValueError(f"{n} tokens, or a sequence of {(self.cached + new).max(initial=0)}, beyond {self.max_tokens} "
                              f"and {self.max_len}")
+        layers, (kv_heads, dim) = len(self.k_cache), self.k_cache.shape[-2:]
+        for name, x, heads in (("q", q, q.shape[-2]), ("k", k, kv_heads), ("v", v, kv_heads), ("out", out, q.shape[-2])):
+            if x.dim() != 4 or len(x) < layers or x.shape[1] < n or x.shape[2:] != (heads, dim) or heads % kv_heads:
+                raise ValueError(f"{name} must be [{layers}][at least {n}][{heads}][{dim}], the query heads a multiple of {kv_heads}, "
+                                 f"got {tuple(x.shape)}")
         need = [self.blocks_for(r, int(c)) for r, c in enumerate(new)]
         if sum(need) > len(self.free):
             raise RuntimeError(f"{sum(need)} blocks wanted, {len(self.free)} free")
@@ -83,7 +91,7 @@ class AttentionEngine:
         for r, m in enumerate(need):
             self.blocks[r] += self.free[:m]
             del self.free[:m]
-        self.cached += new
+        self.cached += new.astype(np.int32)
         return n
 
     def finish(self, row: int) -> None:
