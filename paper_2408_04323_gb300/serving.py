@@ -109,18 +109,22 @@ class AttentionProbe:
     def __init__(self, ctx: S.Context, prompts, outputs, n_layers: int = 2, n_heads: int = 32, n_kv_heads: int = 8,
                  head_dim: int = 128, cache_bytes: int = 1 << 30, dtype=torch.bfloat16, seed: int = 0):
         self.ctx, self.prompts, self.outputs = ctx, [int(p) for p in prompts], [int(o) for o in outputs]
+        if len(self.prompts) != len(self.outputs) or not self.prompts or min(self.prompts + self.outputs) < 1:
+            raise ValueError("prompts and outputs must be one length each per request, all of them at least 1")
         self.shape = (n_layers, n_heads, n_kv_heads, head_dim)
         self.cache_bytes, self.dtype, self.seed = int(cache_bytes), dtype, seed
 
     def evaluate(self, max_num_seqs: int, max_num_batched_tokens: int, block_size: int, chunked_prefill: bool,
                  memory_utilization: float = 0.9):
         """{"ttft", "tpot": mean seconds, "throughput": output tokens per second, "steps"}, or None if the configuration
-        cannot serve the requests (a prompt that fits neither the step nor the cache: the engine would crash)."""
+        cannot serve the requests (a prompt that fits neither the step nor the cache: the engine would crash; or steps of no
+        sequence or token)."""
         L, H, Hkv, D = self.shape
         longest = max(p + o for p, o in zip(self.prompts, self.outputs))
         per_block = 2 * 2 * L * block_size * Hkv * D
         n_blocks = int(self.cache_bytes * memory_utilization) // per_block
-        if n_blocks < -(-longest // block_size) or (not chunked_prefill and max(self.prompts) > max_num_batched_tokens):
+        if n_blocks < -(-longest // block_size) or (not chunked_prefill and max(self.prompts) > max_num_batched_tokens) or \
+                min(max_num_seqs, max_num_batched_tokens) < 1:
             return None
         seqs, budget = min(max_num_seqs, len(self.prompts)), max_num_batched_tokens
         eng = AttentionEngine(self.ctx, L, H, Hkv, D, block_size, n_blocks, seqs, budget, longest, self.dtype)

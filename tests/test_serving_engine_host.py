@@ -81,3 +81,15 @@ def test_arrays_that_do_not_fit_are_refused(serving, which, change):
     with pytest.raises(ValueError):
         eng.step([3, 3, 0, 0], *x)
     assert _state(eng) == before and not serving.calls
+
+
+@pytest.mark.parametrize("prompts,outputs", [([5, 7], [1, 0]), ([0, 7], [1, 1]), ([5, -7], [1, 1]), ([5, 7], [1]), ([5], [1, 1]), ([], [])])
+def test_requests_that_cannot_be_served_are_refused(serving, prompts, outputs):
+    """An output of no token has no step at which it ends."""
+    with pytest.raises(ValueError):
+        serving.AttentionProbe(Ctx(), prompts, outputs)
+
+
+@pytest.mark.parametrize("seqs,tokens", [(0, 64), (8, 0), (-1, 64)])
+def test_a_configuration_without_sequences_or_tokens_serves_nothing(serving, seqs, tokens):
+    assert serving.AttentionProbe(Ctx(), [5, 7], [2, 1]).evaluate(seqs, tokens, 16, True) is None
