@@ -52,10 +52,11 @@ class AttentionEngine:
         """Blocks that n_new more tokens of the row would take."""
         return -(-(int(self.cached[row]) + n_new) // self.block_size) - len(self.blocks[row])
 
-    def step(self, new, q, k, v, out):
+    def step(self, new, q, k, v, out, run=None):
         """new [max_seqs]: new tokens per row; q, out [layers][tokens][heads][dim] and k, v [layers][tokens][kv heads][dim]
         with the rows' tokens back to back.  Fills out; returns the number of tokens.  A step that cannot be (counts,
-        lengths, blocks or shapes) is refused before anything is changed."""
+        lengths, blocks or shapes) is refused before anything is changed.  run: called in place of the function that it is
+        given, which queues the step's work on the current stream; it may do so more than once, with the same result."""
         new = np.asarray(new, np.int64)
         if new.shape != self.cached.shape or new.min(initial=0) < 0:
             raise ValueError(f"new must be {len(self.cached)} counts, none of them negative, got {new.tolist()}")
@@ -78,16 +79,20 @@ class AttentionEngine:
         copied.synchronize()  # of the step before last
         host = stage.numpy()
         host[:rows], host[rows:2 * rows], host[2 * rows:size] = self.cached, new, self.free[:taken]
-        self.inputs[:size].copy_(stage[:size], non_blocking=True)
-        copied.record()
         slot, position = self.slot[:n], self.position[:n]
-        S.scoot_kv_tables(self.ctx, self.inputs[:rows], self.inputs[rows:2 * rows], self.table, self.block_size,
-                          self.n_blocks, self.inputs[2 * rows:size], self.query_start, self.kv_len, slot, position, self.counts)
-        for layer in range(len(self.k_cache)):
-            kc, vc = self.k_cache[layer], self.v_cache[layer]
-            S.scoot_kv_append(self.ctx, k[layer, :n], v[layer, :n], slot, kc, vc)
-            S.scoot_paged_attention(self.ctx, q[layer, :n], kc, vc, self.table, self.query_start, self.kv_len,
-                                    out[layer, :n], self.scale, window=self.window)
+
+        def launch():
+            self.inputs[:size].copy_(stage[:size], non_blocking=True)
+            copied.record()
+            S.scoot_kv_tables(self.ctx, self.inputs[:rows], self.inputs[rows:2 * rows], self.table, self.block_size,
+                              self.n_blocks, self.inputs[2 * rows:size], self.query_start, self.kv_len, slot, position, self.counts)
+            for layer in range(len(self.k_cache)):
+                kc, vc = self.k_cache[layer], self.v_cache[layer]
+                S.scoot_kv_append(self.ctx, k[layer, :n], v[layer, :n], slot, kc, vc)
+                S.scoot_paged_attention(self.ctx, q[layer, :n], kc, vc, self.table, self.query_start, self.kv_len,
+                                        out[layer, :n], self.scale, window=self.window)
+
+        launch() if run is None else run(launch)
         for r, m in enumerate(need):
             self.blocks[r] += self.free[:m]
             del self.free[:m]
@@ -103,8 +108,11 @@ class AttentionEngine:
 
 class AttentionProbe:
     """Serves requests (prompt and output lengths, all there at the start) with an AttentionEngine under a configuration
-    and measures the steps on the GPU.  Stands in for the engine in Algorithm 1's evaluation where only the
+    and measures the steps on the GPU: the time of its work alone, not that of the host, which plans and queues each step
+    while a delay holds the GPU back.  Stands in for the engine in Algorithm 1's evaluation where only the
     attention's share of a step is wanted, or to try the loop without an engine: queries, keys and values are random."""
+
+    SHORTEST_DELAY, LONGEST_DELAY = 1 << 12, 1 << 22  # iterations of the delay's kernel: some 70 us and 70 ms
 
     def __init__(self, ctx: S.Context, prompts, outputs, n_layers: int = 2, n_heads: int = 32, n_kv_heads: int = 8,
                  head_dim: int = 128, cache_bytes: int = 1 << 30, dtype=torch.bfloat16, seed: int = 0):
@@ -113,6 +121,24 @@ class AttentionProbe:
             raise ValueError("prompts and outputs must be one length each per request, all of them at least 1")
         self.shape = (n_layers, n_heads, n_kv_heads, head_dim)
         self.cache_bytes, self.dtype, self.seed = int(cache_bytes), dtype, seed
+        self.delay = self.SHORTEST_DELAY  # about as long as queueing a step takes
+
+    def _timed(self, marks, sink):
+        """A step's run: queues it behind a delay, and again behind a longer one if the GPU came to the step before all
+        of it was queued, so that its marks hold no time in which the GPU waits for the host."""
+        def run(launch):
+            while True:
+                start, stop = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+                S.scoot_probe_fma(self.ctx, False, 1, self.delay, sink)
+                start.record()
+                launch()
+                stop.record()
+                if not start.query() or self.delay >= self.LONGEST_DELAY:
+                    marks.append((start, stop))
+                    self.delay = max(self.SHORTEST_DELAY, self.delay - self.delay // 64)  # (a pause of the host passes)
+                    return
+                self.delay *= 2
+        return run
 
     def evaluate(self, max_num_seqs: int, max_num_batched_tokens: int, block_size: int, chunked_prefill: bool,
                  memory_utilization: float = 0.9):
@@ -139,6 +165,7 @@ class AttentionProbe:
         left = np.zeros(seqs, int)                 # prompt tokens still to take
         promised = 0                               # blocks that running requests may still take
         marks, first, last = [], {}, {}
+        timed = self._timed(marks, torch.zeros(1, device="cuda"))
         while waiting or any(r is not None for r in row_of):
             for row in range(seqs):                # admit while the cache has room for the whole request
                 if row_of[row] is not None or not waiting:
@@ -164,10 +191,7 @@ class AttentionProbe:
                 new[r] = n
                 room -= n
             before = len(eng.free)
-            marks.append((torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)))
-            marks[-1][0].record()
-            eng.step(new, q, k, v, out)
-            marks[-1][1].record()
+            eng.step(new, q, k, v, out, timed)
             promised -= before - len(eng.free)
             for r in np.flatnonzero(new):
                 i = row_of[r]
