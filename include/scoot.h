@@ -834,10 +834,12 @@ typedef struct {
  * in the cache, whose ceil(cached / block_size) blocks are the first entries
  * of its row of block_table ([n_req][ld_table]), and brings new_len[r] tokens.
  * In the requests' order each takes the blocks it lacks from the front of
- * free_blocks (n_free ids) and appends them to its row.  A request whose
- * blocks the free ones do not cover is refused: it takes none, its tokens get
- * slot -1 and its kv_len is 0 (scoot_paged_attention then gives it zeros); a
- * later one that needs no block is still served.
+ * free_blocks (n_free ids) and appends them to its row.  A request is refused
+ * if all that the requests up to and with it lack, refused ones included, is
+ * more than n_free: it takes none, its tokens get slot -1 and its kv_len is 0
+ * (scoot_paged_attention then gives it zeros).  So after the first refusal every
+ * later request that lacks a block is refused, few as its blocks may be, and
+ * one that lacks none is still served.
  * Outputs: query_start[n_req + 1], the running sum of new_len; kv_len[n_req] =
  * cached + new; for token t of the batch (requests back to back) slot[t] and
  * position[t] (its place in its sequence, from 0); counts[2] = blocks taken,

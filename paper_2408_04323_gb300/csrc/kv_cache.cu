@@ -64,8 +64,9 @@ __device__ __forceinline__ TabRequest tab_request(const TabArgs& a, const int2* 
 // each thread's (14.4 us without the gaps, 12.4 with them, for 8192 requests and
 // 65,413 tokens).  The first token of a block that the request lacks writes its
 // table entry.  Bound by latency: a launch, the lengths, the scan, an entry, a
-// slot; 6.3 us for 48 requests of one token each.  Sums of 32 bits in the walk
-// and twice the blocks measured the same (12.4 us).
+// slot; 4.1 us for 48 requests of one token each among ten calls of a captured
+// graph, 10.8 for the 8192 (a call through the binding 7.7 and 12.3).  Sums of 32
+// bits in the walk and twice the blocks measured the same (12.4 us).
 __global__ void __launch_bounds__(kTabThreads) kv_tables_kernel(const TabArgs a) {
     extern __shared__ int2 staged_s[];
     __shared__ int64_t tok_end[kTabThreads], blk_end[kTabThreads];  // sums up to and with each thread
@@ -203,8 +204,8 @@ __global__ void __launch_bounds__(kTabThreads) kv_tables_kernel(const TabArgs a)
 }
 
 // A block takes kAppend consecutive 16-byte pieces of the tokens' keys, and the same of their values; a thread two of
-// them, 256 apart, with all its loads under way before the first store.  Bound by HBM: 67 MB of keys and as much of values
-// in and out in 83 us.  (A piece per thread with its token by a 64-bit division: 88 us.)
+// them, 256 apart, with all its loads under way before the first store.  Bound by HBM: 134 MB of keys and as much of values,
+// read and written (537 MB), in 82 us.  (A piece per thread with its token by a 64-bit division: 88 us.)
 constexpr int kAppendThreads = 256, kAppendPer = 2, kAppend = kAppendThreads * kAppendPer;
 
 __global__ void __launch_bounds__(kAppendThreads)

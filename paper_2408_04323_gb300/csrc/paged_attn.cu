@@ -42,14 +42,16 @@
 // So an item that is marked, or whose sums are not all finite, has the values of its keys looked through at its end, and
 // each row's sums set by those that it sees (odd_values); the joins give a weight of zero no say over such sums.
 //
-// What bounds it, as measured (heads of 128 in blocks of 16, four query heads per key-value head, bf16):
+// What bounds it, as measured in calls one after the other (heads of 128 in blocks of 16, four query heads per key-value
+// head, bf16):
 //   * 256 sequences of 64 to 2560 tokens, one new token each: 220 us, 6.3 TB/s, 92% of the copy rate: HBM (a tile of
 //     64 KB per SM in 2700 cycles; scores, softmax and products of one row group take 1500).
-//   * a chunk of 8192 tokens over 8192 cached ones: 1.02 ms, 1610 TFLOP/s, 86% of the library's large product: shared
-//     memory, which feeds both operands of Q K^T (128 bytes a cycle), and the way scores - softmax - values of a slot (3000
-//     cycles for 2048 of products).
-//   * prompts in a window and small batches: starts and ends of items (about 5 us of a call: ranges, first tile, last
-//     join) and 1400 cycles of softmax per tile.
+//   * a chunk of 8192 tokens over 8192 cached ones: 1.10 to 1.17 ms as the card's power allows, 1410 to 1500 TFLOP/s, 76 to
+//     80% of the library's large product; the tensor pipe is busy in 68% of the cycles.  The rest is, as reckoned, the way
+//     scores - softmax - values of a slot (3000 cycles for 2048 of products) and the shared memory that feeds both operands
+//     of Q K^T.
+//   * prompts in a window (heads of 64): 54 us, the tensor pipe busy in 27% and the schedulers in 40% of the active cycles:
+//     1400 cycles of softmax per tile, and starts and ends of items (about 5 us of a call: ranges, first tile, last join).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
