@@ -116,3 +116,26 @@ def test_many_tokens_before_their_sequence(S, D, requests):
         S.scoot_paged_attention(ctx, q, kc, vc, _i32(table), _i32(start), _i32(kv), out, D ** -0.5, lse=lse)
         ctx.check()
     _compare(q, kc, vc, table, start, kv, D, "bf16", out, lse)
+
+
+def test_zeros_go_where_the_strides_say_and_nowhere_else(S):
+    """Refused prompts' rows in a slice of a wider output, without and with lse."""
+    H, Hkv, D, bs = 12, 2, 64, 16
+    kv = np.array([0, 90] * 20)
+    new = np.array([70, 1] * 20)
+    start = np.concatenate([[0], np.cumsum(new)])
+    table = np.full((len(kv), 6), -1)
+    table[1::2] = np.random.default_rng(1).permutation(20 * 6).reshape(20, 6)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    kc, vc = (torch.randn((120, bs, Hkv, D), generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn((int(start[-1]), H, D), generator=g, device="cuda").bfloat16()
+    wide = torch.full((q.shape[0], H + 2, 2 * D), 5.0, device="cuda", dtype=q.dtype)
+    out, again, lse = wide[:, 1:-1, D:], torch.full_like(q, 3.0), torch.full(q.shape[:2], 3.0, device="cuda")
+    args = (q, kc, vc, _i32(table), _i32(start), _i32(kv))
+    with S.Context(torch.cuda.current_device()) as ctx:
+        S.scoot_paged_attention(ctx, *args, out, D ** -0.5)
+        S.scoot_paged_attention(ctx, *args, again, D ** -0.5, lse=lse)
+        ctx.check()
+    assert torch.equal(out, again)
+    assert (wide[:, 0] == 5).all() and (wide[:, -1] == 5).all() and (wide[:, :, :D] == 5).all()
+    _compare(q, kc, vc, table, start, kv, D, "bf16", again, lse)
