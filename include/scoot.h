@@ -26,6 +26,10 @@
  *   scoot_kv_tables      block tables, positions and cache slots from request lengths
  *   scoot_kv_append      the new tokens' keys and values into their slots
  *   scoot_paged_attention  the new tokens against their requests' keys and values
+ *   scoot_rotary         heads turned by their tokens' positions, and back
+ *   scoot_kv_append_rotary  scoot_kv_append with keys and queries turned on the way
+ *   scoot_kv_append8     the same into a cache of 8-bit floats
+ *   scoot_paged_attention8  attention over that cache
  *
  * plus host-side preparation of per-round state (Cholesky factor of the
  * observations' covariance, box decomposition of the non-dominated region,
@@ -813,6 +817,7 @@ scoot_status scoot_select_topq_static(const float* acq, const uint8_t* mask, int
 
 #define SCOOT_F16  0
 #define SCOOT_BF16 1
+#define SCOOT_E4M3 2          /* 8-bit floats: the caches of scoot_kv_append8 and scoot_paged_attention8 */
 #define SCOOT_MAX_GROUP 128   /* query heads per key-value head */
 
 /* A paged cache: n_blocks blocks of block_size tokens; element (block, token,
@@ -822,7 +827,7 @@ scoot_status scoot_select_topq_static(const float* acq, const uint8_t* mask, int
  * arrays of this layout, 16-byte aligned.  The slot of a token is block *
  * block_size + its place in the block. */
 typedef struct {
-    int32_t dtype;         /* SCOOT_F16 or SCOOT_BF16 */
+    int32_t dtype;         /* SCOOT_F16 or SCOOT_BF16; SCOOT_E4M3 where a call says so */
     int32_t head_dim;      /* 64 or 128 */
     int32_t n_kv_heads;
     int32_t block_size;    /* a power of two, 8 to 256 */
@@ -894,6 +899,89 @@ scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_layout* layout
                                    const void* k_cache, const void* v_cache, float scale, int32_t causal,
                                    int32_t window, void* out, int64_t out_ld_token, int64_t out_ld_head, float* lse,
                                    void* stream);
+
+/* Rotary positions.  The first rot_dim dimensions of a head are turned in pairs,
+ *   (a, b) -> magnitude (a cos t - b sin t, b cos t + a sin t),  t = position * frequency of the pair,
+ * pair i being dimensions i and i + rot_dim / 2, or 2 i and 2 i + 1 if interleaved; the others pass unchanged. */
+typedef struct {
+    const uint64_t* turns;   /* device, [rot_dim / 2]: the pairs' frequencies by scoot_rotary_turns */
+    int32_t rot_dim;         /* a multiple of 16, at most head_dim */
+    int32_t interleaved;
+    float magnitude;         /* 1, or what a stretched context's scores are to grow by (its square) */
+    int32_t reserved;
+} scoot_rotation;
+
+/* Frequencies of rot_dim / 2 pairs in radians per position: base^(-2 i / rot_dim), stretched for contexts `factor` times as
+ * long as the model was made for:
+ *   LINEAR  every frequency by 1 / factor (positions are squeezed);
+ *   BASE    base * factor^(rot_dim / (rot_dim - 2)) in place of base, which leaves the fastest pair and slows the slowest by
+ *           factor;
+ *   PARTS   f g + f / factor (1 - g), g = (original_len f / 2 pi - low) / (high - low) within 0 .. 1: pairs that turn more than
+ *           `high` times in the original context stay, those that turn less than `low` times are slowed by factor.
+ * A caller with frequencies of its own needs only scoot_rotary_turns.  Host only, in fp64. */
+#define SCOOT_STRETCH_NONE   0
+#define SCOOT_STRETCH_LINEAR 1
+#define SCOOT_STRETCH_BASE   2
+#define SCOOT_STRETCH_PARTS  3
+scoot_status scoot_rotary_frequencies(int32_t rot_dim, double base, int32_t stretch, double factor, double low, double high,
+                                      double original_len, double* h_frequency);
+/* Frequencies as fractions of a turn in units of 2^-64 (whole turns per position are dropped: positions are integers), for
+ * scoot_rotation.turns.  With them an angle is exact modulo a turn at any position, to 2^-33 of a turn. */
+scoot_status scoot_rotary_turns(const double* h_frequency, int32_t n, uint64_t* h_turns);
+
+/* y = x turned by its tokens' positions (any int32), or turned back if inverse: a rotation's transpose, which takes
+ * gradients of y to gradients of x (and undoes it where magnitude is 1).  x and y: element (t, head, dim) at t * ld_token +
+ * head * ld_head + dim, dtype SCOOT_F16 or SCOOT_BF16, alignment and strides as in scoot_kv_layout; y may be x (with its
+ * strides) but not overlap it otherwise.  head_dim: a multiple of 16 from 16 to 256.  Computed in fp32 and rounded once. */
+scoot_status scoot_rotary(scoot_ctx* ctx, const scoot_rotation* rotation, int32_t dtype, const void* x, int64_t x_ld_token,
+                          int64_t x_ld_head, int32_t n_heads, int32_t head_dim, const int32_t* position, int64_t n_tokens,
+                          int32_t inverse, void* y, int64_t y_ld_token, int64_t y_ld_head, void* stream);
+
+/* scoot_kv_append of keys turned by position[t], and of values as they are; the queries q (n_heads heads, NULL and 0 for none)
+ * are turned into q_out, which may be q.  A token whose slot is negative (or past the cache, which is flagged) is skipped
+ * altogether: its row of q_out stays as it was. */
+scoot_status scoot_kv_append_rotary(scoot_ctx* ctx, const scoot_kv_layout* layout, const scoot_rotation* rotation, const void* q,
+                                    int64_t q_ld_token, int64_t q_ld_head, int32_t n_heads, void* q_out, int64_t q_out_ld_token,
+                                    int64_t q_out_ld_head, const void* k, int64_t k_ld_token, int64_t k_ld_head, const void* v,
+                                    int64_t v_ld_token, int64_t v_ld_head, const int64_t* slot, const int32_t* position,
+                                    int64_t n_tokens, void* k_cache, void* v_cache, void* stream);
+
+/* Keys and values into a cache of 8-bit floats: layout->dtype SCOOT_E4M3 (4 exponent bits of bias 7, 3 fraction bits), strides
+ * multiples of 16, and a scale for each block and head, k_scale and v_scale float32 [n_blocks][n_kv_heads].  The number that a
+ * code stands for is its own value times its block's scale.  A new token's numbers, keys turned as in scoot_kv_append_rotary if
+ * rotation is not NULL, are divided by the scale and rounded once, to the nearest, ties to even.
+ * The scale of a block is the least power of two s >= 2^-100 with |x| <= 448 s for the new tokens' x, or the one that it
+ * has if the block holds earlier tokens (its first new token is not its first) and that is at least s.  If theirs is
+ * smaller, their codes are divided by the growth and rounded again, which changes only those that get smaller than
+ * 2^-6 of the new scale, by at most 2^-10 of it.
+ * The tokens of a block follow one another in the batch, in the order of their slots, as scoot_kv_tables leaves them;
+ * negative slots and those past the cache as in scoot_kv_append_rotary.  A number that is not finite is stored as zero and
+ * flagged (scoot_ctx_check: SCOOT_EINVAL), so that no code is a NaN; so is a held scale that is negative or not finite, the
+ * block's earlier tokens then counting as zeros.
+ * k, v, q, q_out: of dtype SCOOT_F16 or SCOOT_BF16.  rotation NULL: position may be NULL, and q is NULL. */
+scoot_status scoot_kv_append8(scoot_ctx* ctx, const scoot_kv_layout* layout, int32_t dtype, const scoot_rotation* rotation,
+                              const void* q, int64_t q_ld_token, int64_t q_ld_head, int32_t n_heads, void* q_out,
+                              int64_t q_out_ld_token, int64_t q_out_ld_head, const void* k, int64_t k_ld_token,
+                              int64_t k_ld_head, const void* v, int64_t v_ld_token, int64_t v_ld_head, const int64_t* slot,
+                              const int32_t* position, int64_t n_tokens, void* k_cache, void* v_cache, float* k_scale,
+                              float* v_scale, void* stream);
+
+/* scoot_paged_attention over an 8-bit cache: key i of head h is its code times k_scale[block of i][h], value i likewise with
+ * v_scale (any finite scales, not negative; scoot_kv_append8 makes powers of two).  q and out are of `dtype`, SCOOT_F16 or
+ * SCOOT_BF16.  max_new: no request brings more than so many tokens (0: any number); it says which kernels have work,
+ * and a request that brings more is flagged like one with bad lengths.  All else as there, but that
+ *  - probabilities, times their values' scales, are rounded to fp16 for the product with the values' codes (those so small
+ *    that they pass fp16's range to 2^-32 of the largest scale among the values gone by);
+ *  - a scale that is negative or not finite is flagged (scoot_ctx_check: SCOOT_EINVAL) and counts as zero;
+ *  - of the two codes that the format reserves for NaN, which scoot_kv_append8 never writes, a token that sees one among its
+ *    keys or values gets NaN or some number there; a token that does not is not touched by it. */
+scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_layout* layout, int32_t dtype, const void* q,
+                                    int64_t q_ld_token, int64_t q_ld_head, int32_t n_heads, int64_t n_tokens,
+                                    const int32_t* query_start, const int32_t* kv_len, int32_t n_req,
+                                    const int32_t* block_table, int64_t ld_table, const void* k_cache, const void* v_cache,
+                                    const float* k_scale, const float* v_scale, float scale, int32_t causal, int32_t window,
+                                    int32_t max_new, void* out, int64_t out_ld_token, int64_t out_ld_head, float* lse,
+                                    void* stream);
 
 /* ------------------------------------------------------------------ measurement probes */
 

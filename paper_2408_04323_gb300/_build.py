@@ -18,7 +18,7 @@ LIB = os.path.join(PKG, "libscoot.so")
 SOURCES = ["context.cu", "host_prep.cpp", "compact.cu", "prune_rf.cu", "score.cu", "ehvi.cu", "topq.cu", "fantasy.cu", "pareto.cu",
            "sobol.cu", "rf_train.cu",
            "gp_device.cu", "round_state.cpp", "probes.cu", "posterior_tc.cu",
-           "kv_cache.cu", "paged_attn.cu"]
+           "kv_cache.cu", "paged_attn.cu", "rotary.cu", "kv_append8.cu", "paged_attn8.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall"]
 

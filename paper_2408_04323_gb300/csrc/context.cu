@@ -183,8 +183,8 @@ scoot_status scoot_ctx_check(scoot_ctx* ctx, void* stream) {
     if (word & SCOOT_DEVERR_INDEX) return scoot_fail(ctx, SCOOT_EDEVICE, "a kernel met an index out of range");
     if (word & SCOOT_DEVERR_VALUE)
         return scoot_fail(ctx, SCOOT_EINVAL,
-                          "a kernel met a non-finite feature, a label other than 0/1, or a fantasy state that does "
-                          "not match its call");
+                          "a kernel met a non-finite feature, key, value or scale, a label other than 0/1, or a fantasy state "
+                          "that does not match its call");
     if (word & SCOOT_DEVERR_CAPACITY)
         return scoot_fail(ctx, SCOOT_EUNSUPPORTED,
                           "a kernel ran out of capacity (more than %d candidates survived the pivots of a Pareto "

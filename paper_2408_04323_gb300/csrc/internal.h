@@ -32,7 +32,7 @@ struct scoot_ctx {
     size_t ws_kept_bytes = 0;
     uint32_t* d_err = nullptr;   // device error word, followed by the counters
     int32_t sms = 0;             // multiprocessors of the device, once scoot_sms has asked
-    uint32_t smem_set = 0;       // kernels whose shared memory has been asked for: bits 0-3 paged_attn.cu's, 4 kv_cache.cu's tables
+    uint32_t smem_set = 0;       // kernels whose shared memory has been asked for: bits 0-3 paged_attn.cu's, 4 kv_cache.cu's tables, 5-8 kv_append8.cu's, 9-12 paged_attn8.cu's
     uint32_t* d_count = nullptr; // SCOOT_COUNTS arrival counters, zero between calls (paged_attn.cu)
     // Phase timing (scoot_ctx_set_timing): events recorded between the
     // launches of the last timed call, and the kind of each launch.
@@ -147,6 +147,10 @@ scoot_status scoot_check_kv(scoot_ctx* ctx, const scoot_kv_layout* L, const void
 // A (token, head, dim) array of the cache's type: alignment and strides.
 scoot_status scoot_check_heads(scoot_ctx* ctx, const char* name, const void* p, int64_t ld_token, int64_t ld_head,
                                int32_t head_dim);
+// The same for an 8-bit cache and its scales; and a call's counts of tokens and heads.
+scoot_status scoot_check_kv8(scoot_ctx* ctx, const scoot_kv_layout* L, const void* k_cache, const void* v_cache, const float* k_scale,
+                             const float* v_scale);
+scoot_status scoot_check_tokens(scoot_ctx* ctx, int64_t n_tokens, int64_t heads);
 scoot_status scoot_check_pool(scoot_ctx* ctx, const uint32_t* cand, int64_t n, int64_t ld, int32_t d);
 
 #ifdef __CUDACC__

@@ -1,0 +1,342 @@
+// Keys and values into a paged cache of 8-bit floats (four exponent and three fraction bits) with a scale per block of tokens
+// and head.
+//
+//   s = least power of two with amax <= 448 s,   code = rn(x / s)
+//
+// over all that the block holds of the head.  A power of two, so that a scale that grows (new tokens with larger numbers in a
+// block that held some) changes only the exponents of the older codes: they are exact still, but for those that get so
+// small that they lose fraction bits, whose error stays below half of the least step.  With any other scale every growth would
+// round all of them again.  The format's steps are relative, so that nothing is lost by not using the scale's fraction.
+#include <cuda_fp8.h>
+
+#include <algorithm>
+
+#include "rotary.cuh"
+
+namespace {
+
+using namespace scoot_dev;
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxWindow = 32;   // tokens among which a block of threads looks for the first ones of its runs
+constexpr int kMaxBlock = 256;   // the largest block_size
+constexpr int kSteps = 4;        // steps of a run whose numbers stay in registers between the two looks at them
+constexpr int kWords = (kMaxWindow + kMaxBlock) / 32 + 1;
+
+struct Append8Args {
+    Rotation rot;               // turned = 0: none
+    int32_t n_heads, n_kv_heads;
+    int32_t bs_log, window;
+    int64_t n_tokens, n_slots;
+    const int32_t* position;
+    const uint16_t* q;
+    int64_t q_ld_token, q_ld_head;
+    uint16_t* y;
+    int64_t y_ld_token, y_ld_head;
+    const uint16_t* kv[2];
+    int64_t kv_ld_token[2], kv_ld_head[2];
+    const int64_t* slot;
+    int64_t ld_block, ld_token, ld_head;
+    uint8_t* cache[2];
+    float* scale[2];
+    uint32_t* err;
+};
+
+// Two numbers as codes (of magnitude 448 at most), and back.
+__device__ __forceinline__ uint32_t encode2(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float2 decode2(uint32_t w) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)w));
+    return __half22float2(*reinterpret_cast<const __half2*>(&r));
+}
+
+// The least power of two s >= 2^-100 with amax <= 448 s = 1.75 * 2^8 s; amax finite.
+__device__ __forceinline__ float least_scale(float amax) {
+    const uint32_t b = __float_as_uint(amax);
+    const int e = (int)(b >> 23) - 8 + ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return __uint_as_float((uint32_t)max(e, 27) << 23);
+}
+
+// Tokens of a batch in one block follow one another, a run: slots s, s + 1, ..  A block of threads takes the runs that begin
+// among its `window` tokens: the cosines and sines of their tokens, their queries, and then, a warp per (run, head), keys
+// and values: D / 16 lanes per token, each with a task's 16 dimensions, and so 32 / (D / 16) tokens a step.  A warp has the
+// scale to itself: no atomics, and no order to depend on.
+template <bool kBf16, int D>
+__global__ void __launch_bounds__(kThreads) kv_append8_kernel(const Append8Args a) {
+    constexpr int kTasks = D / 16, kTokens = 32 / kTasks;
+    extern __shared__ float4 cs[];
+    __shared__ uint32_t goes_on[kWords], begins[kWords];  // bit i: token t0 + i continues a run; begins one
+    __shared__ int run_at[kMaxWindow], run_n[kMaxWindow];
+    __shared__ int n_runs, last;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int64_t t0 = (int64_t)blockIdx.x * a.window;
+    const int bs = 1 << a.bs_log;
+    if (tid == 0) n_runs = last = 0;
+    for (int i = tid; i < kWords * 32; i += kThreads) {  // (whole warps)
+        bool on = false, first = false;
+        if (i < a.window + bs && t0 + i < a.n_tokens) {
+            const int64_t s = a.slot[t0 + i];
+            const bool there = s >= 0 && s < a.n_slots;
+            if (s >= a.n_slots && i < a.window) atomicOr(a.err, SCOOT_DEVERR_INDEX);
+            on = there && (s & (bs - 1)) && t0 + i > 0 && a.slot[t0 + i - 1] == s - 1;
+            first = there && !on;
+        }
+        const uint32_t w_on = __ballot_sync(0xffffffffu, on), w_first = __ballot_sync(0xffffffffu, first);
+        if (lane == 0) {
+            goes_on[i >> 5] = w_on;
+            begins[i >> 5] = w_first;
+        }
+    }
+    __syncthreads();
+    if (tid < a.window && begins[tid >> 5] >> (tid & 31) & 1u) {
+        int n = 1;
+        while (tid + n < kWords * 32) {  // up to the next token that does not go on: at most bs - 1 further
+            const int i = tid + n;
+            const uint32_t stops = ~goes_on[i >> 5] >> (i & 31);
+            if (stops) {
+                n += __ffs(stops) - 1;
+                break;
+            }
+            n += 32 - (i & 31);
+        }
+        const int at = atomicAdd(&n_runs, 1);
+        run_at[at] = tid;
+        run_n[at] = n;
+        atomicMax(&last, tid + n);
+    }
+    __syncthreads();
+    const int end = last, pairs = 8 * a.rot.turned;
+    auto mine = [&](int i) {  // whether token t0 + i is of a run that begins here
+        if (begins[i >> 5] >> (i & 31) & 1u) return i < a.window;
+        if (!(goes_on[i >> 5] >> (i & 31) & 1u)) return false;
+        for (int w = i >> 5;; --w) {  // its run's first token
+            uint32_t b = begins[w];
+            if (w == i >> 5) b &= (2u << (i & 31)) - 1u;
+            if (b) return w * 32 + 31 - __clz(b) < a.window;
+            if (w == 0) return false;
+        }
+    };
+    if (a.rot.turned) {
+        for (int e = tid; e < end * pairs; e += kThreads) {
+            const int t = e / pairs, pair = e - t * pairs;
+            reinterpret_cast<float2*>(cs)[t * pairs + rotation_place(a.rot, pair)] = rotation_at(a.rot, pair, a.position[t0 + t]);
+        }
+        __syncthreads();
+        const uint32_t per_token = (uint32_t)a.n_heads * kTasks, all = end * per_token;
+        for (uint32_t e = tid; e < all; e += kThreads) {
+            const uint32_t t = e / per_token, c = e - t * per_token;
+            if (!mine((int)t)) continue;
+            const int head = (int)(c / kTasks), j = (int)(c % kTasks);
+            const uint16_t* p = a.q + (t0 + t) * a.q_ld_token + head * a.q_ld_head;
+            uint16_t* y = a.y + (t0 + t) * a.y_ld_token + head * a.y_ld_head;
+            const int ca = 8 * a.rot.chunk_a(j), cb = 8 * a.rot.chunk_b(j);
+            uint4 ra = *reinterpret_cast<const uint4*>(p + ca), rb = *reinterpret_cast<const uint4*>(p + cb);
+            if (j < a.rot.turned) {
+                float x[8], z[8];
+                turn_task<kBf16>(a.rot, cs + t * (pairs / 2), j, ra, rb, x, z);
+                ra = make_uint4(pack16_rn<kBf16>(x[0], x[1]), pack16_rn<kBf16>(x[2], x[3]), pack16_rn<kBf16>(x[4], x[5]), pack16_rn<kBf16>(x[6], x[7]));
+                rb = make_uint4(pack16_rn<kBf16>(z[0], z[1]), pack16_rn<kBf16>(z[2], z[3]), pack16_rn<kBf16>(z[4], z[5]), pack16_rn<kBf16>(z[6], z[7]));
+            }
+            *reinterpret_cast<uint4*>(y + ca) = ra;
+            *reinterpret_cast<uint4*>(y + cb) = rb;
+        }
+    }
+
+    const int sub = lane / kTasks, j = lane % kTasks;
+    const int units = n_runs * a.n_kv_heads;
+    Rotation none = a.rot;
+    none.turned = 0;
+    bool odd = false;
+#pragma unroll 1
+    for (int u = warp; u < units; u += kWarps) {
+        const int r = u / a.n_kv_heads, head = u - r * a.n_kv_heads;
+        const int at = run_at[r], n = run_n[r];
+        const int64_t t1 = t0 + at, s1 = a.slot[t1], block = s1 >> a.bs_log;
+        const int in_block = (int)(s1 & (bs - 1));
+#pragma unroll 1
+        for (int kv = 0; kv < 2; ++kv) {
+            const Rotation rot = kv == 0 ? a.rot : none;
+            const int ca = 8 * rot.chunk_a(j), cb = 8 * rot.chunk_b(j);
+            float* scale_at = a.scale[kv] + block * a.n_kv_heads + head;
+            const float held = in_block ? __shfl_sync(0xffffffffu, lane == 0 ? *scale_at : 0.0f, 0) : 0.0f;
+            const uint16_t* src = a.kv[kv] + t1 * a.kv_ld_token[kv] + head * a.kv_ld_head[kv];
+            uint8_t* cache = a.cache[kv] + block * a.ld_block + head * a.ld_head;
+            uint4 ra[kSteps], rb[kSteps];
+            auto load = [&](int i0) {
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    const int t = i0 + i * kTokens + sub;
+                    ra[i] = rb[i] = make_uint4(0, 0, 0, 0);
+                    if (t < n) {
+                        const uint16_t* p = src + t * a.kv_ld_token[kv];
+                        ra[i] = *reinterpret_cast<const uint4*>(p + ca);
+                        rb[i] = *reinterpret_cast<const uint4*>(p + cb);
+                    }
+                }
+            };
+            // step i's numbers, those that are not finite as zeros
+            auto numbers = [&](int i, int t, float* x) {
+                turn_task<kBf16>(rot, cs + (at + min(t, n - 1)) * (pairs / 2), j, ra[i], rb[i], x, x + 8);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (!(fabsf(x[e]) < INFINITY)) {
+                        x[e] = 0.0f;
+                        odd = true;
+                    }
+            };
+            float top = 0.0f;
+#pragma unroll 1
+            for (int i0 = 0; i0 < n; i0 += kSteps * kTokens) {
+                load(i0);
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    float x[16];
+                    numbers(i, i0 + i * kTokens + sub, x);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[e]));
+                }
+            }
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            float s = least_scale(top);
+            if (in_block) {
+                const bool bad = !(held >= 0.0f && held < INFINITY);
+                odd |= bad;
+                if (held >= s && !bad) {
+                    s = held;
+                } else {
+                    // the scale has grown: the older tokens' codes by the growth
+                    const float f = bad ? 0.0f : held / s;
+                    for (int i = sub; i < in_block; i += kTokens) {
+                        uint4* p = reinterpret_cast<uint4*>(cache + i * a.ld_token + 16 * j);
+                        const uint4 w = *p;
+                        auto again = [&](uint32_t v) {
+                            const float2 lo = decode2(v & 0xFFFFu), hi = decode2(v >> 16);
+                            return encode2(lo.x * f, lo.y * f) | encode2(hi.x * f, hi.y * f) << 16;
+                        };
+                        *p = make_uint4(again(w.x), again(w.y), again(w.z), again(w.w));
+                    }
+                }
+            }
+            if (lane == 0) *scale_at = s;
+            const float inv = 1.0f / s;  // (a scale that was held may be any number)
+#pragma unroll 1
+            for (int i0 = 0; i0 < n; i0 += kSteps * kTokens) {
+                if (n > kSteps * kTokens) load(i0);
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    const int t = i0 + i * kTokens + sub;
+                    float x[16];
+                    numbers(i, t, x);
+                    if (t >= n) continue;
+                    uint8_t* p = cache + (in_block + t) * a.ld_token;
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        w[e] = encode2(x[4 * e] * inv, x[4 * e + 1] * inv) | encode2(x[4 * e + 2] * inv, x[4 * e + 3] * inv) << 16;
+                    *reinterpret_cast<uint2*>(p + ca) = make_uint2(w[0], w[1]);
+                    *reinterpret_cast<uint2*>(p + cb) = make_uint2(w[2], w[3]);
+                }
+            }
+        }
+    }
+    if (odd) atomicOr(a.err, SCOOT_DEVERR_VALUE);
+}
+
+template <bool kBf16, int D>
+scoot_status launch(scoot_ctx* ctx, Append8Args& a, cudaStream_t st) {
+    // few tokens: one each, so that there are blocks for all multiprocessors
+    const int64_t most = 8ll * scoot_sms(ctx);
+    a.window = 1;
+    while (a.window < kMaxWindow && (a.n_tokens + a.window - 1) / a.window > most) a.window *= 2;
+    const int64_t blocks = (a.n_tokens + a.window - 1) / a.window;
+    const size_t smem = (size_t)(a.window + (1 << a.bs_log)) * a.rot.turned * 8 * sizeof(float2);
+    auto kern = kv_append8_kernel<kBf16, D>;
+    const uint32_t bit = 1u << (5 + 2 * kBf16 + (D == 128));
+    if (!(ctx->smem_set & bit)) {  // once per context, for the largest window and block
+        SCOOT_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (kMaxWindow + kMaxBlock) * D / 2 * (int)sizeof(float2)));
+        ctx->smem_set |= bit;
+    }
+    kern<<<(unsigned)blocks, kThreads, smem, st>>>(a);
+    SCOOT_LAUNCHED(ctx);
+    return SCOOT_OK;
+}
+
+}  // namespace
+
+scoot_status scoot_check_kv8(scoot_ctx* ctx, const scoot_kv_layout* L, const void* k_cache, const void* v_cache, const float* k_scale,
+                             const float* v_scale) {
+    if (!L) return scoot_fail(ctx, SCOOT_EINVAL, "layout is NULL");
+    if (L->dtype != SCOOT_E4M3) return scoot_fail(ctx, SCOOT_EUNSUPPORTED, "the cache's dtype = %d is not SCOOT_E4M3", L->dtype);
+    scoot_kv_layout as16 = *L;
+    as16.dtype = SCOOT_BF16;
+    scoot_status s = scoot_check_kv(ctx, &as16, k_cache, v_cache);
+    if (s != SCOOT_OK) return s;
+    if ((L->ld_block | L->ld_token | L->ld_head) & 15)
+        return scoot_fail(ctx, SCOOT_EINVAL, "the cache's strides %lld, %lld and %lld must be multiples of 16", (long long)L->ld_block,
+                          (long long)L->ld_token, (long long)L->ld_head);
+    if (!k_scale || !v_scale) return scoot_fail(ctx, SCOOT_EINVAL, "k_scale or v_scale is NULL");
+    if ((reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale)) & 3u)
+        return scoot_fail(ctx, SCOOT_EINVAL, "k_scale or v_scale is not 4-byte aligned");
+    return SCOOT_OK;
+}
+
+extern "C" scoot_status scoot_kv_append8(scoot_ctx* ctx, const scoot_kv_layout* layout, int32_t dtype, const scoot_rotation* rotation,
+                                         const void* q, int64_t q_ld_token, int64_t q_ld_head, int32_t n_heads, void* q_out,
+                                         int64_t q_out_ld_token, int64_t q_out_ld_head, const void* k, int64_t k_ld_token,
+                                         int64_t k_ld_head, const void* v, int64_t v_ld_token, int64_t v_ld_head,
+                                         const int64_t* slot, const int32_t* position, int64_t n_tokens, void* k_cache,
+                                         void* v_cache, float* k_scale, float* v_scale, void* stream) {
+    scoot_status s = scoot_enter(ctx);
+    if (s != SCOOT_OK) return s;
+    if ((s = scoot_check_kv8(ctx, layout, k_cache, v_cache, k_scale, v_scale)) != SCOOT_OK) return s;
+    if (dtype != SCOOT_F16 && dtype != SCOOT_BF16)
+        return scoot_fail(ctx, SCOOT_EUNSUPPORTED, "dtype = %d is neither SCOOT_F16 nor SCOOT_BF16", dtype);
+    const int D = layout->head_dim;
+    Append8Args a = {};
+    if (n_heads < 0 || (n_heads && !rotation)) return scoot_fail(ctx, SCOOT_EINVAL, "n_heads = %d: queries come with a rotation", n_heads);
+    if (rotation && (s = scoot_check_rotation(ctx, rotation, D, false, &a.rot)) != SCOOT_OK) return s;
+    if ((s = scoot_check_tokens(ctx, n_tokens, (int64_t)n_heads + 2ll * layout->n_kv_heads)) != SCOOT_OK) return s;
+    if (n_tokens == 0) return SCOOT_OK;
+    if (n_heads) {
+        if ((s = scoot_check_heads(ctx, "q", q, q_ld_token, q_ld_head, D)) != SCOOT_OK) return s;
+        if ((s = scoot_check_heads(ctx, "q_out", q_out, q_out_ld_token, q_out_ld_head, D)) != SCOOT_OK) return s;
+    }
+    if ((s = scoot_check_heads(ctx, "k", k, k_ld_token, k_ld_head, D)) != SCOOT_OK) return s;
+    if ((s = scoot_check_heads(ctx, "v", v, v_ld_token, v_ld_head, D)) != SCOOT_OK) return s;
+    if (!slot || (rotation && !position)) return scoot_fail(ctx, SCOOT_EINVAL, "slot or position is NULL");
+    a.n_heads = n_heads;
+    a.n_kv_heads = layout->n_kv_heads;
+    while ((1 << a.bs_log) < layout->block_size) ++a.bs_log;
+    a.n_tokens = n_tokens;
+    a.n_slots = layout->n_blocks << a.bs_log;
+    a.position = position;
+    a.q = static_cast<const uint16_t*>(q);
+    a.q_ld_token = q_ld_token;
+    a.q_ld_head = q_ld_head;
+    a.y = static_cast<uint16_t*>(q_out);
+    a.y_ld_token = q_out_ld_token;
+    a.y_ld_head = q_out_ld_head;
+    a.kv[0] = static_cast<const uint16_t*>(k);
+    a.kv[1] = static_cast<const uint16_t*>(v);
+    a.kv_ld_token[0] = k_ld_token;
+    a.kv_ld_token[1] = v_ld_token;
+    a.kv_ld_head[0] = k_ld_head;
+    a.kv_ld_head[1] = v_ld_head;
+    a.slot = slot;
+    a.ld_block = layout->ld_block;
+    a.ld_token = layout->ld_token;
+    a.ld_head = layout->ld_head;
+    a.cache[0] = static_cast<uint8_t*>(k_cache);
+    a.cache[1] = static_cast<uint8_t*>(v_cache);
+    a.scale[0] = k_scale;
+    a.scale[1] = v_scale;
+    a.err = ctx->d_err;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dtype == SCOOT_BF16) return D == 128 ? launch<true, 128>(ctx, a, st) : launch<true, 64>(ctx, a, st);
+    return D == 128 ? launch<false, 128>(ctx, a, st) : launch<false, 64>(ctx, a, st);
+}

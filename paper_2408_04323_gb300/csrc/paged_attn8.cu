@@ -1,0 +1,799 @@
+// Attention of a batch of new tokens over a paged key-value cache of 8-bit floats, a scale per block of tokens and head.
+//
+//   out_t = sum_i softmax_i(scale s_b(i) q_t . k_i) s'_b(i) v_i,   lse_t = ln sum_i exp(scale s_b(i) q_t . k_i)
+//
+// over the keys i that token t sees; k_i, v_i are codes, s_b and s'_b their blocks' scales.
+//
+// This kernel serves requests of few rows (a row is a token's query head; single tokens above all), which bytes bound: a
+// warp is a worker of its own, with up to 16 rows against keys in tiles of 32.  Codes become fp16, which holds all of them, on
+// their way from shared memory into the operands of the tensor cores (mma.m16n8k16: the tcgen05 forms take 64 or 128 rows,
+// and their operands would have to be written back to shared memory).  Queries become fp16 as well, bf16 ones divided by a
+// power of two of their row so that the largest is below 2^15: what that rounds is below 2^-39 of the row's largest.
+//
+// Dimensions and keys are dealt to the operands' places as the loads want them.  Q K^T: lane (g, c) = (lane / 4, lane % 4) has
+// key g and of it the 16-byte pieces c and c + 4, four dimensions per step, and the same ones of its query rows.  P V: column g
+// of product t is dimension g D / 8 + t, so that a lane reads whole pieces of four keys' values, and has 32 (16) consecutive
+// dimensions of the result.
+//
+// Running maximum m and sum l as elsewhere: p = 2^(c s - m), and O is rescaled only where a maximum has grown by more than 2^8.
+// The values' scales go into the probabilities: fp16 of p s'_b / r * 2^7, r the largest scale of values met so far, which
+// stays below 2^15 and rounds what is below 2^-21 of r with an error of 2^-32 r at most; O is in units of r 2^-7.
+//
+// Work: items (request, key-value head, 16 rows) in a row, each costing its tiles and a constant, are cut into equal ranges, a
+// warp each (a cut close to an item's start or end moves there).  Warps of a block take neighbouring ranges.  An item that
+// lies in several leaves its parts (O, m, l) in the workspace; at the end of a block its warps join the block's parts of
+// each item, and of an item that lies in several blocks the last block joins those, in the ranges' order.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <cfloat>
+
+#include "internal.h"
+#include "mbarrier.cuh"
+
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kRows = 16, kKeys = 32;
+constexpr int kItemCost = 2;    // an item's start and end, in tiles
+constexpr int kMinRange = 4;    // cost that a warp takes at least
+constexpr int kSnap = 2;        // a cut this close to the start or end of an item's tiles moves there
+constexpr int kMaxBlocks = (int)(SCOOT_COUNTS / 2);
+constexpr float kMaxScale = 2.3e38f;  // times log2 e it is still finite
+constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
+
+template <int D>
+struct Shape {
+    static constexpr int kTile = kKeys * D;              // bytes of a tile's keys, or values
+    static constexpr int kStage = 2 * kTile + 64;        // and the scales of its four groups of eight
+    static constexpr int kStages = D == 128 ? 3 : 6;
+    static constexpr int kSmem = kWarps * kStages * kStage;
+    static constexpr int kPart = kRows * (D + 2);        // floats of a part: O, then (m, l) of each row
+};
+
+struct Attn8Args {
+    int32_t bs_log, n_heads, n_kv_heads, group, n_req, causal, window, max_new;
+    int32_t toks, per_token;   // tokens of an item, and items of a token (more than one: groups of more than 16 heads)
+    int64_t n_tokens, n_blocks;
+    const int32_t* query_start;
+    const int32_t* kv_len;
+    const int32_t* table;
+    int64_t ld_table;
+    const uint16_t* q;
+    int64_t q_ld_token, q_ld_head;
+    const uint8_t* k;
+    const uint8_t* v;
+    int64_t ld_block, ld_token, ld_head;
+    const float* k_scale;
+    const float* v_scale;
+    float scale_log2;
+    uint16_t* out;
+    int64_t out_ld_token, out_ld_head;
+    float* lse;
+    float* parts;          // two per warp, then two per block
+    uint32_t* count;       // arrivals of blocks per split item, zero between calls
+    uint32_t* err;
+};
+
+struct Item {
+    int32_t r, h;          // request, key-value head
+    int32_t tok, head;     // first token (of the batch), first query head
+    int32_t rows, heads;   // rows, and heads among them: row = token * heads + head
+    int32_t pos, kv;       // position of the first token, length of the sequence
+    int32_t begin, end;    // keys that some row sees
+    int32_t first, n_parts;  // worker of the first part, and how many parts
+};
+
+__device__ __forceinline__ float exp2_hw(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.0f : m; }
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : __fdividef(1.0f, l); }
+
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <bool kBf16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+    if (!kBf16) return half2_bits(lo, hi);
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+// Two codes as fp16 (exact).
+__device__ __forceinline__ uint32_t decode_lo(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ uint32_t decode_hi(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
+    return r;
+}
+// The codes that the format reserves for NaN as 448.
+__device__ __forceinline__ uint32_t without_nan(uint32_t w) {
+    const uint32_t nan = ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+    return w & ~(nan >> 7);
+}
+__device__ __forceinline__ void mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void lds(uint32_t addr, uint32_t* w) {
+    if (N == 4) asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr));
+    else asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr));
+}
+
+// Where piece j (16 bytes) of a tile's row lies: the lanes of a load's phase find theirs on different banks.
+template <int D>
+__device__ __forceinline__ uint32_t key_at(int row, int j) {
+    return D == 128 ? row * 128 + ((j ^ ((row & 1) << 2)) << 4) : row * 64 + (j << 4);
+}
+template <int D>
+__device__ __forceinline__ uint32_t value_at(int row, int j) {
+    return D == 128 ? row * 128 + ((j ^ (row & 6)) << 4) : (row >> 1) * 128 + (((((row & 1) << 2) + j) ^ (row & 6)) << 4);
+}
+
+struct Req {
+    int32_t q0, n, kv;
+};
+// One request's lengths, empty if they are bad.
+__device__ __forceinline__ Req load_req(const Attn8Args& a, int r, bool flag) {
+    Req q{0, 0, 0};
+    if (r >= a.n_req) return q;
+    const int q0 = a.query_start[r], q1 = a.query_start[r + 1], kv = a.kv_len[r];
+    if (q0 < 0 || q1 < q0 || q1 > a.n_tokens || kv < 0 || kv > a.ld_table << a.bs_log || (a.max_new > 0 && q1 - q0 > a.max_new)) {
+        if (flag) atomicOr(a.err, SCOOT_DEVERR_INDEX);
+        return q;
+    }
+    q.q0 = q0;
+    q.n = q1 - q0;
+    q.kv = kv;
+    return q;
+}
+
+__device__ __forceinline__ int item_count(const Attn8Args& a, int n) { return (n + a.toks - 1) / a.toks * a.per_token; }
+// The keys [begin, end) that some row of item j sees.
+__device__ __forceinline__ void seen_keys(const Attn8Args& a, int kv, int n, int j, int& begin, int& end) {
+    const int tok = a.per_token > 1 ? j / a.per_token : j * a.toks, nt = min(a.toks, n - tok);
+    const int64_t p0 = (int64_t)kv - n + tok;
+    end = a.causal ? (int)min((int64_t)kv, p0 + nt) : kv;
+    begin = a.window > 0 ? (int)max((int64_t)0, p0 + 1 - a.window) : 0;
+    if (end <= begin) begin = end = 0;
+}
+__device__ __forceinline__ int item_cost(const Attn8Args& a, int kv, int n, int j) {
+    int begin, end;
+    seen_keys(a, kv, n, j, begin, end);
+    return kItemCost + (end + kKeys - 1) / kKeys - begin / kKeys;
+}
+// The cost of a head's items of a request, by the whole warp.
+__device__ __forceinline__ int64_t head_cost(const Attn8Args& a, int kv, int n) {
+    const int m = item_count(a, n);
+    int64_t c = 0;
+    for (int j = threadIdx.x & 31; j < m; j += 32) c += item_cost(a, kv, n, j);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) c += __shfl_xor_sync(0xffffffffu, c, d);
+    return c;
+}
+
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+__device__ __forceinline__ uint16_t* out_row(const Attn8Args& a, const Item& it, int q) {
+    const int t = q / it.heads;
+    return a.out + (int64_t)(it.tok + t) * a.out_ld_token + (int64_t)(it.head + q - t * it.heads) * a.out_ld_head;
+}
+__device__ __forceinline__ float* lse_row(const Attn8Args& a, const Item& it, int q) {
+    const int t = q / it.heads;
+    return a.lse + (int64_t)(it.tok + t) * a.n_heads + it.head + q - t * it.heads;
+}
+
+// n parts joined by the whole block: part i is at part(i).  out: the item's rows (final), or a part again (to != NULL).
+template <bool kBf16, int D, typename F>
+__device__ __forceinline__ void join(const Attn8Args& a, const Item& it, int n, float* to, F&& part) {
+    constexpr int kQuads = D / 4;
+    for (int e = threadIdx.x; e < it.rows * kQuads; e += kThreads) {
+        const int q = e / kQuads, c = e % kQuads;
+        float M = -INFINITY, L = 0.0f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i0 = 0; i0 < n; i0 += 4) {
+            float2 ml[4];
+            float4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float* p = part(min(i0 + i, n - 1));
+                ml[i] = __ldcg(reinterpret_cast<const float2*>(p + kRows * D) + q);
+                v[i] = __ldcg(reinterpret_cast<const float4*>(p + q * D) + c);
+                if (i0 + i >= n) {
+                    ml[i] = make_float2(-INFINITY, 0.0f);
+                    v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+            }
+            const float Mn = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), M), Ms = finite_or_zero(Mn);
+            const float f = exp2_hw(M - Ms);
+            L *= f;
+            o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+            M = Mn;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float w = exp2_hw(ml[i].x - Ms);
+                L = fmaf(w, ml[i].y, L);
+                o = make_float4(fmaf(w, v[i].x, o.x), fmaf(w, v[i].y, o.y), fmaf(w, v[i].z, o.z), fmaf(w, v[i].w, o.w));
+            }
+        }
+        if (to) {
+            reinterpret_cast<float4*>(to + q * D)[c] = o;
+            if (c == 0) reinterpret_cast<float2*>(to + kRows * D)[q] = make_float2(M, L);
+        } else {
+            const float inv = inverse_sum(L);
+            *reinterpret_cast<uint2*>(out_row(a, it, q) + 4 * c) = make_uint2(pack16<kBf16>(o.x * inv, o.y * inv), pack16<kBf16>(o.z * inv, o.w * inv));
+            if (c == 0 && a.lse) *lse_row(a, it, q) = L == 0.0f ? -INFINITY : (M + __log2f(L)) * kLn2;
+        }
+    }
+}
+
+template <bool kBf16, int D>
+__global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args a) {
+    using Sh = Shape<D>;
+    constexpr int kSteps = D / 16, kPieces = D / 16, kCols = D / 8;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ int64_t cost_s[kThreads];
+    __shared__ Item items[kWarps + 1];  // of the block's split items: one that came in, and one that begins with each warp's last
+    __shared__ int last_s[2];
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    const int g = lane >> 2, c = lane & 3;
+
+    // The cost of all items: each thread k consecutive requests, then a scan.
+    const int k = (a.n_req + kThreads - 1) / kThreads;
+    if (tid <= kWarps) items[tid].n_parts = 0;
+    int64_t mine = 0;
+#pragma unroll 1
+    for (int i = 0; i < k; ++i) {
+        const Req q = load_req(a, tid * k + i, blockIdx.x == 0);
+        const bool one = item_count(a, q.n) == 1;
+        if (one) mine += item_cost(a, q.kv, q.n, 0);
+        uint32_t big = __ballot_sync(0xffffffffu, q.n > 0 && !one);
+        while (big) {
+            const int src = __ffs(big) - 1;
+            big &= big - 1;
+            const int64_t cost = head_cost(a, __shfl_sync(0xffffffffu, q.kv, src), __shfl_sync(0xffffffffu, q.n, src));
+            if (lane == src) mine += cost;
+        }
+    }
+    mine *= a.n_kv_heads;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int64_t t = __shfl_up_sync(0xffffffffu, mine, d);
+        if (lane >= d) mine += t;
+    }
+    cost_s[tid] = mine;  // up to and with this thread, of its warp
+    __syncthreads();
+    int64_t upto = lane < kWarps ? cost_s[lane * 32 + 31] : 0;
+#pragma unroll
+    for (int d = 1; d < kWarps; d <<= 1) {
+        const int64_t t = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += t;
+    }
+    const int64_t total = __shfl_sync(0xffffffffu, upto, kWarps - 1);
+    const int worker = blockIdx.x * kWarps + warp, n_workers = gridDim.x * kWarps;
+    const int64_t range = max(quotient(total + n_workers - 1, n_workers), (int64_t)kMinRange);
+    const int64_t B0 = min(total, worker * range), B1 = min(total, B0 + range);
+
+    int cached = -1;  // requests 32 cached .. are in the lanes
+    Req in_lane{0, 0, 0};
+    auto get = [&](int r) {
+        if ((r >> 5) != cached) {
+            cached = r >> 5;
+            in_lane = load_req(a, cached * 32 + lane, false);
+        }
+        return Req{__shfl_sync(0xffffffffu, in_lane.q0, r & 31), __shfl_sync(0xffffffffu, in_lane.n, r & 31),
+                   __shfl_sync(0xffffffffu, in_lane.kv, r & 31)};
+    };
+    int r = 0, h = 0, j = 0;
+    int64_t p = B0;  // where item (r, h, j) starts
+    if (B0 < B1) {
+        // the warp's sum that passes B0, then the thread's, then the request, its head and its item
+        const int w = __ffs(__ballot_sync(0xffffffffu, lane < kWarps && upto > B0)) - 1;
+        int64_t at = __shfl_sync(0xffffffffu, upto, w) - cost_s[w * 32 + 31];
+        const int64_t in_warp = cost_s[w * 32 + lane];
+        const int t = __ffs(__ballot_sync(0xffffffffu, at + in_warp > B0)) - 1;
+        const int64_t before = __shfl_sync(0xffffffffu, in_warp, (t + 31) & 31);
+        if (t > 0) at += before;
+        r = (w * 32 + t) * k;
+        while (r < a.n_req) {
+            const Req q = get(r);
+            const int64_t one = q.n > 0 ? head_cost(a, q.kv, q.n) : 0;
+            if (at + one * a.n_kv_heads > B0) {
+                h = (int)quotient(B0 - at, one);
+                at += h * one;
+                break;
+            }
+            at += one * a.n_kv_heads;
+            ++r;
+        }
+        const Req q = get(min(r, a.n_req - 1));
+        const int m = item_count(a, q.n);
+        for (int j0 = 0; j0 < m; j0 += 32) {
+            const int64_t cost = j0 + lane < m ? item_cost(a, q.kv, q.n, j0 + lane) : 0;
+            int64_t s = cost;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int64_t up = __shfl_up_sync(0xffffffffu, s, d);
+                if (lane >= d) s += up;
+            }
+            const uint32_t past = __ballot_sync(0xffffffffu, at + s > B0);
+            if (past) {
+                const int src = __ffs(past) - 1;
+                j = j0 + src;
+                at += __shfl_sync(0xffffffffu, s - cost, src);
+                break;
+            }
+            at += __shfl_sync(0xffffffffu, s, 31);
+        }
+        p = at;
+    }
+
+    const uint32_t ring = scoot_dev::smem_u32(smem) + warp * Sh::kStages * Sh::kStage;
+    bool bad_id = false, bad_scale = false;
+    while (p < B1) {
+        const Req rq = get(r);
+        if (j >= item_count(a, rq.n)) {  // the next head, or the next request with a token
+            j = 0;
+            if (rq.n > 0 && ++h < a.n_kv_heads) continue;
+            h = 0;
+            const uint32_t more = __ballot_sync(0xffffffffu, in_lane.n > 0) & ~((2u << (r & 31)) - 1u);
+            r = more ? (r & ~31) + __ffs(more) - 1 : (r & ~31) + 32;
+            if (r >= a.n_req) break;
+            continue;
+        }
+        Item it;
+        it.r = r;
+        it.h = h;
+        {
+            const int tok = a.per_token > 1 ? j / a.per_token : j * a.toks, sub = a.per_token > 1 ? j % a.per_token : 0;
+            it.heads = a.per_token > 1 ? min(kRows, a.group - sub * kRows) : a.group;
+            it.rows = min(a.toks, rq.n - tok) * it.heads;
+            it.tok = rq.q0 + tok;
+            it.head = h * a.group + sub * kRows;
+            it.pos = rq.kv - rq.n + tok;
+            it.kv = rq.kv;
+        }
+        seen_keys(a, rq.kv, rq.n, j, it.begin, it.end);
+        const int tile0 = it.begin / kKeys, units = (it.end + kKeys - 1) / kKeys - tile0;
+        const int64_t s0 = p + kItemCost;  // where its tiles start
+        auto cut = [&](int64_t b) { return b >= s0 + units ? units : b - s0 < kSnap ? 0 : s0 + units - b < kSnap ? units : (int)(b - s0); };
+        const int lo = cut(B0), hi = cut(B1);
+        const bool here = units ? hi > lo : p >= B0;
+        p = s0 + units;
+        ++j;
+        if (!here) continue;
+        it.first = worker;
+        it.n_parts = 1;
+        if (hi - lo < units) {
+            it.first = (int)quotient(s0 + kSnap - 1, range);
+            it.n_parts = (int)quotient(s0 + units - kSnap, range) - it.first + 1;
+        }
+
+        // ---- copies: the ids of 32 blocks are in the lanes, those of the next 32 on their way
+        const int32_t* row_ids = a.table + (int64_t)it.r * a.ld_table;
+        const int bs = 1 << a.bs_log;
+        auto fetch = [&](int group) {
+            const int64_t key = ((int64_t)group * 32 + lane) << a.bs_log;
+            return key < it.end && key + bs > it.begin ? __ldg(row_ids + group * 32 + lane) : INT32_MIN;
+        };
+        int group = -1, ids = 0, ids_next = 0;
+        auto use = [&](int raw) {
+            const bool out = raw < 0 || raw >= a.n_blocks;
+            bad_id |= out && raw != INT32_MIN;
+            ids = out ? -1 : raw;
+        };
+        auto load = [&](int u, int stage) {  // tile u of the sequence
+            const int key0 = u * kKeys, b0 = key0 >> a.bs_log;
+            if (b0 >> 5 != group) {
+                use(group >= 0 ? ids_next : fetch(b0 >> 5));
+                group = b0 >> 5;
+                ids_next = fetch(group + 1);
+            }
+            const uint32_t dst = ring + stage * Sh::kStage;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int e = i * 32 + lane, row = e / kPieces, piece = e % kPieces, key = key0 + row;
+                const int id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
+                const bool there = id >= 0 && key >= it.begin && key < it.end;
+                const int64_t at = there ? id * a.ld_block + (key & (bs - 1)) * a.ld_token + it.h * a.ld_head + piece * 16 : 0;
+                copy16(dst + key_at<D>(row, piece), a.k + at, there);
+                copy16(dst + Sh::kTile + value_at<D>(row, piece), a.v + at, there);
+            }
+            const int key = key0 + 8 * (lane & 3);
+            const int id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
+            if (lane < 8) {
+                const bool there = id >= 0 && key + 8 > it.begin && key < it.end;
+                copy4(dst + 2 * Sh::kTile + 4 * lane, (lane < 4 ? a.k_scale : a.v_scale) + (there ? (int64_t)id * a.n_kv_heads + it.h : 0), there);
+            }
+        };
+        const int u0 = tile0 + lo, u1 = tile0 + hi;
+#pragma unroll
+        for (int i = 0; i < Sh::kStages - 1; ++i) {
+            if (u0 + i < u1) load(u0 + i, i);
+            copies_end();
+        }
+
+        // ---- queries: rows g and g + 8
+        uint32_t qa[kSteps][4];
+        float c_row[2];       // scale of the row's scores, to log2
+        int k0[2], k1[2];     // keys that the row sees
+        bool same = true;     // all rows see the same keys
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = g + 8 * i, t = row / it.heads;
+            const bool live = row < it.rows;
+            const int pos = it.pos + t;
+            k1[i] = live ? (a.causal ? min(it.kv, pos + 1) : it.kv) : 0;
+            k0[i] = live && a.window > 0 ? (int)max((int64_t)0, (int64_t)pos + 1 - a.window) : 0;
+            same &= !live || (k1[i] >= it.end && k0[i] <= it.begin);
+            const uint16_t* src = a.q + (int64_t)(it.tok + t) * a.q_ld_token + (int64_t)(it.head + row - t * it.heads) * a.q_ld_head;
+            uint32_t w[kSteps][2];
+#pragma unroll
+            for (int s = 0; s < kSteps; s += 2) {
+                const uint4 x = live ? *reinterpret_cast<const uint4*>(src + (s / 4) * 64 + 16 * c + (s % 4) * 4) : make_uint4(0, 0, 0, 0);
+                w[s][0] = x.x;
+                w[s][1] = x.y;
+                w[s + 1][0] = x.z;
+                w[s + 1][1] = x.w;
+            }
+            c_row[i] = a.scale_log2;
+            if (kBf16) {
+                uint32_t top = 0;  // the largest magnitude, as bits
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) top = __vmaxu2(top, w[s][e] & 0x7FFF7FFFu);
+                top = max(top & 0xFFFFu, top >> 16);
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                // 2^(14 - its exponent), and its inverse; a row of zeros, or with what is not finite, as it is
+                const int e = (int)(top >> 7), up = top == 0 || e == 255 ? 0 : min(14 + 127 - e, 126);
+                const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+                c_row[i] = fminf(c_row[i] * __uint_as_float((uint32_t)(127 - up) << 23), FLT_MAX);
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                    for (int e2 = 0; e2 < 2; ++e2)
+                        w[s][e2] = half2_bits(__uint_as_float(w[s][e2] << 16) * f, __uint_as_float(w[s][e2] & 0xFFFF0000u) * f);
+            }
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s) {
+                qa[s][i] = w[s][0];
+                qa[s][i + 2] = w[s][1];
+            }
+        }
+        same = __all_sync(0xffffffffu, same);
+
+        float o[kCols][4];
+#pragma unroll
+        for (int t = 0; t < kCols; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[t][e] = 0.0f;
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+        float vref = 0x1p-100f;
+        auto scale_o = [&](float f0, float f1) {
+#pragma unroll
+            for (int t = 0; t < kCols; ++t) {
+                o[t][0] *= f0;
+                o[t][1] *= f0;
+                o[t][2] *= f1;
+                o[t][3] *= f1;
+            }
+        };
+        int stage = 0;
+#pragma unroll 1
+        for (int u = u0; u < u1; ++u) {
+            copies_wait<Sh::kStages - 2>();
+            __syncwarp();
+            if (u + Sh::kStages - 1 < u1) load(u + Sh::kStages - 1, stage == 0 ? Sh::kStages - 1 : stage - 1);
+            copies_end();
+            const uint32_t st = ring + stage * Sh::kStage;
+            if (++stage == Sh::kStages) stage = 0;
+            float ks[4], vs[4];
+            lds<4>(st + 2 * Sh::kTile, reinterpret_cast<uint32_t*>(ks));
+            lds<4>(st + 2 * Sh::kTile + 16, reinterpret_cast<uint32_t*>(vs));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool kb = !(ks[i] >= 0.0f && ks[i] < INFINITY), vb = !(vs[i] >= 0.0f && vs[i] < INFINITY);
+                bad_scale |= kb || vb;
+                if (kb) ks[i] = 0.0f;
+                if (vb) vs[i] = 0.0f;
+            }
+            // scores
+            float x[4][4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                x[t][0] = x[t][1] = x[t][2] = x[t][3] = 0.0f;
+#pragma unroll
+                for (int half = 0; half < D / 64; ++half) {
+                    uint32_t w[4];
+                    lds<4>(st + key_at<D>(8 * t + g, c + 4 * half), w);
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) mma(x[t], qa[4 * half + s], decode_lo(w[s]), decode_hi(w[s]));
+                }
+            }
+            const int key0 = u * kKeys + 2 * c;
+            const bool full = same && u * kKeys >= it.begin && (u + 1) * kKeys <= it.end;
+            float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                // (finite: a score of zero stays zero)
+                const float ck[2] = {fminf(c_row[0] * ks[t], FLT_MAX), fminf(c_row[1] * ks[t], FLT_MAX)};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = e >> 1, key = key0 + 8 * t + (e & 1);
+                    float s = x[t][e] * ck[i];
+                    if (!full && (key < k0[i] || key >= k1[i])) s = -INFINITY;
+                    x[t][e] = s;
+                    mx[i] = fmaxf(mx[i], s);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
+                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
+            }
+            if (u == u0) {
+                m[0] = mx[0];
+                m[1] = mx[1];
+            } else if (__any_sync(0xffffffffu, mx[0] > m[0] + 8.0f || mx[1] > m[1] + 8.0f)) {
+                float f[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float mn = fmaxf(m[i], mx[i]);
+                    f[i] = mn == -INFINITY ? 1.0f : exp2_hw(m[i] - mn);
+                    m[i] = mn;
+                    l[i] *= f[i];
+                }
+                scale_o(f[0], f[1]);
+            }
+            const float vmax = fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3]));
+            if (vmax > vref) {  // (the same for all lanes)
+                const float f = vref / vmax;
+                scale_o(f, f);
+                vref = vmax;
+            }
+            const float inv_ref = 128.0f / vref, ms[2] = {finite_or_zero(m[0]), finite_or_zero(m[1])};
+            uint32_t pa[2][4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const float f = vs[t] * inv_ref;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float e0 = exp2_hw(x[t][2 * i] - ms[i]), e1 = exp2_hw(x[t][2 * i + 1] - ms[i]);
+                    l[i] += e0 + e1;
+                    pa[t >> 1][2 * (t & 1) + i] = half2_bits(e0 * f, e1 * f);
+                }
+            }
+            // values
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                constexpr int kW = D / 32;  // words of a key's piece
+                uint32_t w[4][kW];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = 16 * kk + 2 * c + (i & 1) + 8 * (i >> 1);
+                    if (D == 128) lds<kW>(st + Sh::kTile + value_at<D>(row, g), w[i]);
+                    else lds<kW>(st + Sh::kTile + value_at<D>(row, g >> 1) + 8 * (g & 1), w[i]);
+                    if (!same) {  // (a value that some row does not see, times its zero)
+#pragma unroll
+                        for (int e = 0; e < kW; ++e) w[i][e] = without_nan(w[i][e]);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < kW; ++e) {
+                    const uint32_t a01 = __byte_perm(w[0][e], w[1][e], 0x5140), a23 = __byte_perm(w[0][e], w[1][e], 0x7362);
+                    const uint32_t b01 = __byte_perm(w[2][e], w[3][e], 0x5140), b23 = __byte_perm(w[2][e], w[3][e], 0x7362);
+                    mma(o[4 * e], pa[kk], decode_lo(a01), decode_lo(b01));
+                    mma(o[4 * e + 1], pa[kk], decode_hi(a01), decode_hi(b01));
+                    mma(o[4 * e + 2], pa[kk], decode_lo(a23), decode_lo(b23));
+                    mma(o[4 * e + 3], pa[kk], decode_hi(a23), decode_hi(b23));
+                }
+            }
+        }
+        __syncwarp();  // before the ring is filled for the next item
+
+        // ---- the end of the item
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+        }
+        const bool whole = it.n_parts == 1;
+        const bool begins = it.first == worker;
+        float* part = a.parts + (size_t)(2 * worker + begins) * Sh::kPart;
+        if (!whole && lane == 0 && (begins || warp == 0)) items[begins ? 1 + warp : 0] = it;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = g + 8 * i;
+            if (row >= it.rows) continue;
+            // columns t of the lane's two: kCols consecutive dimensions each
+            if (whole) {
+                const float f = inverse_sum(l[i]) * 0x1p-7f;
+                uint16_t* dst = out_row(a, it, row) + c * (D / 4);
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int t = 0; t < kCols; t += 8) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            w[e] = pack16<kBf16>(o[t + 2 * e][2 * i + n] * f * vref, o[t + 2 * e + 1][2 * i + n] * f * vref);
+                        *reinterpret_cast<uint4*>(dst + n * kCols + t) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                if (c == 0 && a.lse) *lse_row(a, it, row) = l[i] == 0.0f ? -INFINITY : (m[i] + __log2f(l[i])) * kLn2;
+            } else {
+                const float f = vref * 0x1p-7f;
+                float* dst = part + row * D + c * (D / 4);
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int t = 0; t < kCols; t += 4)
+                        *reinterpret_cast<float4*>(dst + n * kCols + t) = make_float4(o[t][2 * i + n] * f, o[t + 1][2 * i + n] * f,
+                                                                                     o[t + 2][2 * i + n] * f, o[t + 3][2 * i + n] * f);
+                if (c == 0) reinterpret_cast<float2*>(part + kRows * D)[row] = make_float2(m[i], l[i]);
+            }
+        }
+    }
+    if (bad_id) atomicOr(a.err, SCOOT_DEVERR_INDEX);
+    if (bad_scale) atomicOr(a.err, SCOOT_DEVERR_VALUE);
+
+    // ---- split items: the block's parts of each, then the blocks'
+    __syncthreads();
+    const int w0 = blockIdx.x * kWarps, w1 = w0 + kWarps - 1;
+    float* mine_out = a.parts + (size_t)(2 * n_workers + 2 * blockIdx.x) * Sh::kPart;
+#pragma unroll 1
+    for (int i = 0; i <= kWarps; ++i) {
+        const Item it = items[i];
+        if (it.n_parts == 0) continue;
+        const int first = max(it.first, w0), n = min(it.first + it.n_parts - 1, w1) - first + 1;
+        const bool all = n == it.n_parts;
+        join<kBf16, D>(a, it, n, all ? nullptr : mine_out + (it.first >= w0 ? Sh::kPart : 0), [&](int q) {
+            return a.parts + (size_t)(2 * (first + q) + (first + q == it.first ? 1 : 0)) * Sh::kPart;
+        });
+    }
+    __syncthreads();
+    if (tid == 0) {
+        last_s[0] = last_s[1] = 0;
+        __threadfence();  // (the block's other threads' stores are before it by the barrier)
+        for (int side = 0; side < 2; ++side) {
+            // the item that came in, or the one that goes on in the next block
+            Item it;
+            it.n_parts = 0;
+            if (side == 0) it = items[0];
+            else
+                for (int i = 1; i <= kWarps; ++i)
+                    if (items[i].n_parts && items[i].first + items[i].n_parts - 1 > w1) it = items[i];
+            if (it.n_parts == 0) continue;
+            const int b0 = it.first / kWarps, b1 = (it.first + it.n_parts - 1) / kWarps;
+            const bool last = atomicAdd(a.count + b0, 1u) == (uint32_t)(b1 - b0);
+            if (last) a.count[b0] = 0;
+            last_s[side] = last;
+        }
+        __threadfence();
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int side = 0; side < 2; ++side) {
+        if (!last_s[side]) continue;
+        int i = 0;
+        if (side == 1)
+            for (i = kWarps; !(items[i].n_parts && items[i].first + items[i].n_parts - 1 > w1);) --i;
+        const Item it = items[i];
+        const int b0 = it.first / kWarps, b1 = (it.first + it.n_parts - 1) / kWarps;
+        join<kBf16, D>(a, it, b1 - b0 + 1, nullptr, [&](int q) {
+            return a.parts + (size_t)(2 * n_workers + 2 * (b0 + q) + (q == 0 ? 1 : 0)) * Sh::kPart;
+        });
+    }
+}
+
+template <bool kBf16, int D>
+scoot_status launch(scoot_ctx* ctx, Attn8Args& a, int sms, cudaStream_t st) {
+    using Sh = Shape<D>;
+    scoot_status s = scoot_workspace(ctx, (size_t)sms * 2 * (kWarps + 1) * Sh::kPart * sizeof(float), st);
+    if (s != SCOOT_OK) return s;
+    a.parts = static_cast<float*>(ctx->ws);
+    auto kern = attn8_rows_kernel<kBf16, D>;
+    const uint32_t bit = 1u << (9 + 2 * kBf16 + (D == 128));
+    if (!(ctx->smem_set & bit)) {  // once per context: the call is short
+        SCOOT_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem));
+        ctx->smem_set |= bit;
+    }
+    kern<<<(unsigned)sms, kThreads, Sh::kSmem, st>>>(a);
+    SCOOT_LAUNCHED(ctx);
+    return SCOOT_OK;
+}
+
+}  // namespace
+
+extern "C" scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_layout* layout, int32_t dtype, const void* q,
+                                               int64_t q_ld_token, int64_t q_ld_head, int32_t n_heads, int64_t n_tokens,
+                                               const int32_t* query_start, const int32_t* kv_len, int32_t n_req,
+                                               const int32_t* block_table, int64_t ld_table, const void* k_cache,
+                                               const void* v_cache, const float* k_scale, const float* v_scale, float scale,
+                                               int32_t causal, int32_t window, int32_t max_new, void* out, int64_t out_ld_token,
+                                               int64_t out_ld_head, float* lse, void* stream) {
+    scoot_status s = scoot_enter(ctx);
+    if (s != SCOOT_OK) return s;
+    if ((s = scoot_check_kv8(ctx, layout, k_cache, v_cache, k_scale, v_scale)) != SCOOT_OK) return s;
+    if (dtype != SCOOT_F16 && dtype != SCOOT_BF16)
+        return scoot_fail(ctx, SCOOT_EUNSUPPORTED, "dtype = %d is neither SCOOT_F16 nor SCOOT_BF16", dtype);
+    if (n_heads < 1 || n_heads % layout->n_kv_heads)
+        return scoot_fail(ctx, SCOOT_EINVAL, "n_heads = %d is not a multiple of n_kv_heads = %d", n_heads, layout->n_kv_heads);
+    if (n_heads / layout->n_kv_heads > SCOOT_MAX_GROUP)
+        return scoot_fail(ctx, SCOOT_EUNSUPPORTED, "%d query heads per key-value head, more than %d",
+                          n_heads / layout->n_kv_heads, SCOOT_MAX_GROUP);
+    if (n_tokens < 0 || n_tokens > 0x40000000ll || n_tokens > 0x7FFFFFFFll / n_heads || n_req < 0 || n_req > 0x40000000 ||
+        ld_table < 0 || ld_table > 0x40000000ll / layout->block_size)
+        return scoot_fail(ctx, SCOOT_EINVAL, "n_tokens = %lld, n_req = %d or ld_table = %lld out of range", (long long)n_tokens,
+                          n_req, (long long)ld_table);
+    if (!(scale > 0.0f) || scale > kMaxScale)
+        return scoot_fail(ctx, SCOOT_EINVAL, "scale = %g must be positive and at most %g", scale, kMaxScale);
+    if (window < 0 || max_new < 0) return scoot_fail(ctx, SCOOT_EINVAL, "window = %d or max_new = %d < 0", window, max_new);
+    if (n_tokens == 0 || n_req == 0) return SCOOT_OK;
+    const int D = layout->head_dim, G = n_heads / layout->n_kv_heads;
+    if ((s = scoot_check_heads(ctx, "q", q, q_ld_token, q_ld_head, D)) != SCOOT_OK) return s;
+    if ((s = scoot_check_heads(ctx, "out", out, out_ld_token, out_ld_head, D)) != SCOOT_OK) return s;
+    if (!query_start || !kv_len || (ld_table && !block_table)) return scoot_fail(ctx, SCOOT_EINVAL, "an array is NULL");
+    const int sms = std::min(scoot_sms(ctx), kMaxBlocks);
+    Attn8Args a = {};
+    while ((1 << a.bs_log) < layout->block_size) ++a.bs_log;
+    a.n_heads = n_heads;
+    a.n_kv_heads = layout->n_kv_heads;
+    a.group = G;
+    a.n_req = n_req;
+    a.causal = causal != 0;
+    a.window = window < ld_table * layout->block_size ? window : 0;  // no sequence is longer
+    a.max_new = max_new;
+    a.toks = G <= kRows ? kRows / G : 1;
+    a.per_token = (G + kRows - 1) / kRows;
+    a.n_tokens = n_tokens;
+    a.n_blocks = layout->n_blocks;
+    a.query_start = query_start;
+    a.kv_len = kv_len;
+    a.table = block_table;
+    a.ld_table = ld_table;
+    a.q = static_cast<const uint16_t*>(q);
+    a.q_ld_token = q_ld_token;
+    a.q_ld_head = q_ld_head;
+    a.k = static_cast<const uint8_t*>(k_cache);
+    a.v = static_cast<const uint8_t*>(v_cache);
+    a.ld_block = layout->ld_block;
+    a.ld_token = layout->ld_token;
+    a.ld_head = layout->ld_head;
+    a.k_scale = k_scale;
+    a.v_scale = v_scale;
+    a.scale_log2 = scale * kLog2e;
+    a.out = static_cast<uint16_t*>(out);
+    a.out_ld_token = out_ld_token;
+    a.out_ld_head = out_ld_head;
+    a.lse = lse;
+    a.count = ctx->d_count;
+    a.err = ctx->d_err;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dtype == SCOOT_BF16) return D == 128 ? launch<true, 128>(ctx, a, sms, st) : launch<true, 64>(ctx, a, sms, st);
+    return D == 128 ? launch<false, 128>(ctx, a, sms, st) : launch<false, 64>(ctx, a, sms, st);
+}

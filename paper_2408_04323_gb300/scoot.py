@@ -84,6 +84,11 @@ class scoot_kv_layout(C.Structure):
                 ("n_blocks", C.c_int64), ("ld_block", C.c_int64), ("ld_token", C.c_int64), ("ld_head", C.c_int64)]
 
 
+class scoot_rotation(C.Structure):
+    _fields_ = [("turns", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float),
+                ("reserved", C.c_int32)]
+
+
 # scoot_node as a numpy record (host copies of trained trees)
 NODE_DTYPE = np.dtype([("val", "<f4"), ("left", "<u2"), ("feat", "u1"), ("flags", "u1")])
 
@@ -161,6 +166,15 @@ _PROTOS = {
     "scoot_kv_append": [_vp, C.POINTER(scoot_kv_layout), _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _vp, _vp, _vp],
     "scoot_paged_attention": [_vp, C.POINTER(scoot_kv_layout), _vp, _i64, _i64, _i32, _i64, _vp, _vp, _i32, _vp, _i64,
                               _vp, _vp, _f32, _i32, _i32, _vp, _i64, _i64, _vp, _vp],
+    "scoot_rotary_frequencies": [_i32, C.c_double, _i32, C.c_double, C.c_double, C.c_double, C.c_double, _vp],
+    "scoot_rotary_turns": [_vp, _i32, _vp],
+    "scoot_rotary": [_vp, C.POINTER(scoot_rotation), _i32, _vp, _i64, _i64, _i32, _i32, _vp, _i64, _i32, _vp, _i64, _i64, _vp],
+    "scoot_kv_append_rotary": [_vp, C.POINTER(scoot_kv_layout), C.POINTER(scoot_rotation), _vp, _i64, _i64, _i32, _vp, _i64, _i64,
+                               _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _vp],
+    "scoot_kv_append8": [_vp, C.POINTER(scoot_kv_layout), _i32, C.POINTER(scoot_rotation), _vp, _i64, _i64, _i32, _vp, _i64, _i64,
+                         _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp],
+    "scoot_paged_attention8": [_vp, C.POINTER(scoot_kv_layout), _i32, _vp, _i64, _i64, _i32, _i64, _vp, _vp, _i32, _vp, _i64,
+                               _vp, _vp, _vp, _vp, _f32, _i32, _i32, _i32, _vp, _i64, _i64, _vp, _vp],
 }
 _STRING_FUNCS = {"scoot_last_error", "scoot_status_string"}
 EXPORTS = tuple(_PROTOS)
@@ -820,7 +834,7 @@ def scoot_fantasy_end(ctx, var_out=None, stream=None):
 # These calls are a step's smallest, and made once or more per layer: their checks are inlined, and the messages left to
 # the slow path.
 
-F16, BF16 = 0, 1
+F16, BF16, E4M3 = 0, 1, 2
 MAX_GROUP = 128
 
 
@@ -887,10 +901,10 @@ def _heads(t, dtype, name, device):
 
 
 @functools.lru_cache(maxsize=64)
-def _layout(bf16, shape, stride):
+def _layout(dtype, shape, stride):
     nb, bs, h, d = shape
     sb, st, sh, _ = stride
-    L = scoot_kv_layout(BF16 if bf16 else F16, d, h, bs, nb, sb if nb > 1 else bs * h * d, st, sh if h > 1 else d)
+    L = scoot_kv_layout(dtype, d, h, bs, nb, sb if nb > 1 else bs * h * d, st, sh if h > 1 else d)
     return L, C.byref(L), d, h
 
 
@@ -911,7 +925,7 @@ def _kv(k_cache, v_cache, device=None):
             raise TypeError(f"k_cache and v_cache must both be float16 or bfloat16, got {dt} and {v_cache.dtype}")
         raise ValueError("k_cache and v_cache must be [blocks][tokens][heads][dim] of one shape and the same strides, contiguous "
                          f"along their last axis, got {tuple(shape)} and {tuple(v_cache.shape)}")
-    return _layout(dt is torch.bfloat16, shape, stride)
+    return _layout(BF16 if dt is torch.bfloat16 else F16, shape, stride)
 
 
 def kv_layout(k_cache, v_cache) -> scoot_kv_layout:
@@ -986,3 +1000,180 @@ def scoot_paged_attention(ctx, q, k_cache, v_cache, block_table, query_start, kv
                                          None if lse is None else _ptr(lse, torch.float32, "lse", device), _on(stream, device))
     if status:
         _check(status, "scoot_paged_attention", h)
+
+
+# ------------------------------------------------------------------ rotary positions and an 8-bit cache
+
+STRETCH = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def scoot_rotary_frequencies(rot_dim: int, base: float = 10000.0, stretch: str = "none", factor: float = 1.0, low: float = 1.0,
+                             high: float = 32.0, original_len: float = 0.0) -> np.ndarray:
+    """float64 [rot_dim / 2]: radians per position of each pair.  stretch: "none", "linear", "base" or "parts"."""
+    if stretch not in STRETCH:
+        raise ValueError(f"stretch must be one of {', '.join(STRETCH)}, got {stretch!r}")
+    out = np.empty(max(1, int(rot_dim) // 2))
+    _check(lib().scoot_rotary_frequencies(_i32_arg(rot_dim), float(base), STRETCH[stretch], float(factor), float(low), float(high),
+                                          float(original_len), _host(out)), "scoot_rotary_frequencies")
+    return out
+
+
+def scoot_rotary_turns(h_frequency) -> np.ndarray:
+    """uint64 [n] of float64 [n]: the frequencies in 2^-64 of a turn."""
+    out = np.empty(len(h_frequency), np.uint64)
+    _check(lib().scoot_rotary_turns(_host(h_frequency, dtype=np.float64, name="h_frequency"), len(out), _host(out)), "scoot_rotary_turns")
+    return out
+
+
+class Rotation:
+    """A rotation's frequencies on a device, made once per model.  frequencies: float64 [rot_dim / 2] radians per position,
+    in place of those of scoot_rotary_frequencies.  device: an index (default: the current one)."""
+
+    def __init__(self, rot_dim: int, base: float = 10000.0, interleaved: bool = False, stretch: str = "none", factor: float = 1.0,
+                 low: float = 1.0, high: float = 32.0, original_len: float = 0.0, magnitude: float = 1.0, frequencies=None, device=None):
+        import torch
+        if frequencies is None:
+            frequencies = scoot_rotary_frequencies(rot_dim, base, stretch, factor, low, high, original_len)
+        if len(frequencies) * 2 != rot_dim:
+            raise ValueError(f"{len(frequencies)} frequencies for {rot_dim} dimensions")
+        self.device = torch.cuda.current_device() if device is None else int(device)
+        self.turns = torch.from_numpy(scoot_rotary_turns(np.ascontiguousarray(frequencies, np.float64)).view(np.int64)).to(f"cuda:{self.device}")
+        self.rot_dim, self.interleaved, self.magnitude = int(rot_dim), bool(interleaved), float(magnitude)
+        self.struct = scoot_rotation(self.turns.data_ptr(), self.rot_dim, self.interleaved, self.magnitude, 0)
+        self.ref = C.byref(self.struct)
+
+
+def _rotation(rotation, device):
+    if not isinstance(rotation, Rotation):
+        raise TypeError(f"rotation must be a Rotation, got {type(rotation).__name__}")
+    if rotation.device != device:
+        raise ValueError(f"rotation is on device {rotation.device}, and the call's device is {device}")
+    return rotation.ref
+
+
+def _code(t, name):
+    """The library's number of a 16-bit type."""
+    import torch
+    if t.dtype is torch.bfloat16:
+        return BF16
+    if t.dtype is torch.float16:
+        return F16
+    raise TypeError(f"{name} must have dtype float16 or bfloat16, got {t.dtype}")
+
+
+def _kv8(k_cache, v_cache, k_scale, v_scale, device):
+    """_kv for an 8-bit cache, and the pointers of its scales."""
+    import torch
+    dt, shape, stride = k_cache.dtype, k_cache.shape, k_cache.stride()
+    f8 = torch.float8_e4m3fn
+    if not (dt is f8 and v_cache.dtype is f8 and len(shape) == 4 and shape == v_cache.shape and stride == v_cache.stride()
+            and stride[3] == 1 and k_cache.get_device() == device and v_cache.get_device() == device):
+        if not (k_cache.is_cuda and v_cache.is_cuda):
+            raise TypeError("k_cache and v_cache must be CUDA torch tensors (device memory)")
+        for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+            if t.get_device() != device:
+                raise _elsewhere(t, name, device)
+        if dt is not f8 or v_cache.dtype is not f8:
+            raise TypeError(f"k_cache and v_cache must both be float8_e4m3fn, got {dt} and {v_cache.dtype}")
+        raise ValueError("k_cache and v_cache must be [blocks][tokens][heads][dim] of one shape and the same strides, contiguous "
+                         f"along their last axis, got {tuple(shape)} and {tuple(v_cache.shape)}")
+    if k_scale.shape != (shape[0], shape[2]) or v_scale.shape != k_scale.shape:
+        raise ValueError(f"k_scale and v_scale must be [blocks][heads], {shape[0]} by {shape[2]}, got {tuple(k_scale.shape)} and "
+                         f"{tuple(v_scale.shape)}")
+    f32 = torch.float32
+    return (*_layout(E4M3, shape, stride), _ptr(k_scale, f32, "k_scale", device), _ptr(v_scale, f32, "v_scale", device))
+
+
+def scoot_rotary(ctx, rotation, x, position, out, inverse=False, stream=None) -> None:
+    """x, out: device [T][heads][dim] of one 16-bit type (last axis contiguous; out may be x); position: device int32 [T]."""
+    import torch
+    h, device = _handle(ctx, x, "x")
+    if x.dim() != 3 or x.shape != out.shape or position.numel() != x.shape[0]:
+        raise ValueError(f"x and out must be [T][heads][dim] of one shape, and position [T], got {tuple(x.shape)}, {tuple(out.shape)} "
+                         f"and {tuple(position.shape)}")
+    T, H, D = x.shape
+    xp, xt, xh = _heads(x, x.dtype, "x", device)
+    op, ot, oh = _heads(out, x.dtype, "out", device)
+    status = lib().scoot_rotary(h, _rotation(rotation, device), _code(x, "x"), xp, xt, xh, H, D,
+                                _ptr(position, torch.int32, "position", device), T, 1 if inverse else 0, op, ot, oh, _on(stream, device))
+    if status:
+        _check(status, "scoot_rotary", h)
+
+
+def _append_args(k, v, slot, position, q, q_out, Hkv, D, dt, device):
+    """(queries' pointers and strides, heads, keys', values', slot, position, tokens) of an append with a rotation."""
+    import torch
+    T = slot.numel()
+    if k.shape != v.shape or k.shape != (T, Hkv, D) or (position is not None and position.numel() != T):
+        raise ValueError(f"k and v must be [T][heads][dim] as slot and the cache have them, and position [T], got {tuple(k.shape)}, "
+                         f"{tuple(v.shape)} and {None if position is None else tuple(position.shape)}")
+    qs = (None, 0, 0, 0, None, 0, 0)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out come together")
+    if q is not None:
+        if q.shape != q_out.shape or q.dim() != 3 or q.shape[0] != T or q.shape[2] != D:
+            raise ValueError(f"q and q_out must be [{T}][heads][{D}] of one shape, got {tuple(q.shape)} and {tuple(q_out.shape)}")
+        qs = (*_heads(q, dt, "q", device), q.shape[1], *_heads(q_out, dt, "q_out", device))
+    return (*qs, *_heads(k, dt, "k", device), *_heads(v, dt, "v", device), _ptr(slot, torch.int64, "slot", device),
+            None if position is None else _ptr(position, torch.int32, "position", device), T)
+
+
+def scoot_kv_append_rotary(ctx, rotation, k, v, slot, position, k_cache, v_cache, q=None, q_out=None, stream=None) -> None:
+    """k, v: device [T][heads][dim] of the cache's type (last axis contiguous); slot: device int64 [T]; position: device int32
+    [T]; q, q_out: device [T][query heads][dim] of that type or None (q_out may be q)."""
+    h, device = _handle(ctx, k_cache, "k_cache")
+    _, ref, D, Hkv = _kv(k_cache, v_cache, device)
+    if position is None:
+        raise ValueError("position must be given")
+    status = lib().scoot_kv_append_rotary(h, ref, _rotation(rotation, device),
+                                          *_append_args(k, v, slot, position, q, q_out, Hkv, D, k_cache.dtype, device),
+                                          k_cache.data_ptr(), v_cache.data_ptr(), _on(stream, device))
+    if status:
+        _check(status, "scoot_kv_append_rotary", h)
+
+
+def scoot_kv_append8(ctx, k, v, slot, k_cache, v_cache, k_scale, v_scale, rotation=None, position=None, q=None, q_out=None,
+                     stream=None) -> None:
+    """k, v: device [T][heads][dim] of one 16-bit type (last axis contiguous); slot: device int64 [T]; k_cache, v_cache: device
+    float8_e4m3fn [blocks][tokens][heads][dim]; k_scale, v_scale: device float32 [blocks][heads], updated.  rotation with
+    position (device int32 [T]) turns the keys, and q [T][query heads][dim] into q_out if they are given."""
+    h, device = _handle(ctx, k_cache, "k_cache")
+    _, ref, D, Hkv, ks, vs = _kv8(k_cache, v_cache, k_scale, v_scale, device)
+    if rotation is None and (q is not None or position is not None):
+        raise ValueError("position and q come with a rotation")
+    if rotation is not None and position is None:
+        raise ValueError("a rotation comes with position")
+    status = lib().scoot_kv_append8(h, ref, _code(k, "k"), None if rotation is None else _rotation(rotation, device),
+                                    *_append_args(k, v, slot, position, q, q_out, Hkv, D, k.dtype, device),
+                                    k_cache.data_ptr(), v_cache.data_ptr(), ks, vs, _on(stream, device))
+    if status:
+        _check(status, "scoot_kv_append8", h)
+
+
+def scoot_paged_attention8(ctx, q, k_cache, v_cache, k_scale, v_scale, block_table, query_start, kv_len, out, scale, causal=True,
+                           window=0, lse=None, max_new=0, stream=None) -> None:
+    """q, out: device [T][heads][dim] of one 16-bit type (last axis contiguous); k_cache, v_cache: device float8_e4m3fn
+    [blocks][tokens][heads][dim]; k_scale, v_scale: device float32 [blocks][heads]; block_table int32 [R][width], query_start
+    int32 [R + 1], kv_len int32 [R]; lse: device float32 [T][heads] or None; max_new: most new tokens of a request, 0 if
+    that is not known."""
+    import torch
+    h, device = _handle(ctx, k_cache, "k_cache")
+    _, ref, D, _, ks, vs = _kv8(k_cache, v_cache, k_scale, v_scale, device)
+    R, shape = kv_len.numel(), q.shape
+    if shape != out.shape or len(shape) != 3 or shape[2] != D:
+        raise ValueError(f"q and out must be [T][heads][{D}] of one shape, got {tuple(shape)} and "
+                         f"{tuple(out.shape)}")
+    if block_table.dim() != 2 or block_table.shape[0] != R or query_start.numel() != R + 1 or \
+            (lse is not None and lse.shape != shape[:2]):
+        raise ValueError("array lengths do not match: [R] kv_len; [R][width] block_table; [R + 1] query_start; "
+                         "[T][heads] lse")
+    qp, qt, qh = _heads(q, q.dtype, "q", device)
+    op, ot, oh = _heads(out, q.dtype, "out", device)
+    i32 = torch.int32
+    status = lib().scoot_paged_attention8(h, ref, _code(q, "q"), qp, qt, qh, shape[1], shape[0],
+                                          _ptr(query_start, i32, "query_start", device), _ptr(kv_len, i32, "kv_len", device), _i32_arg(R),
+                                          _ptr(block_table, i32, "block_table", device), block_table.shape[1], k_cache.data_ptr(),
+                                          v_cache.data_ptr(), ks, vs, float(scale), 1 if causal else 0, _i32_arg(window), _i32_arg(max_new),
+                                          op, ot, oh, None if lse is None else _ptr(lse, torch.float32, "lse", device), _on(stream, device))
+    if status:
+        _check(status, "scoot_paged_attention8", h)
