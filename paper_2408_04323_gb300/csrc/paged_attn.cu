@@ -58,8 +58,8 @@
 
 #include <algorithm>
 
-#include "internal.h"
 #include "mbarrier.cuh"
+#include "paged_attn8.cuh"
 
 namespace {
 
@@ -67,9 +67,15 @@ using namespace scoot_dev;
 
 constexpr int kRows = 128;         // rows of a slot: the MMA's M and the TMEM lanes
 constexpr int kKeys = 128;         // keys of a tile
-constexpr int kThreads = 384;      // three warpgroups: the two softmax ones take registers from the third
-constexpr int kSoftmaxRegs = 200, kOtherRegs = 104;  // 2 * 200 + 104 = 3 * 168, what the block is launched with
-constexpr int kMmaWarp = 8, kLoadWarp = 9, kValueWarp = 10;
+// Warpgroups: two of softmax, which take registers from the third; with codes a fourth, which turns them into tiles.
+template <bool k8>
+constexpr int kThreads = k8 ? 512 : 384;
+template <bool k8>
+constexpr int kSoftmaxRegs = k8 ? 168 : 200;  // 2 * 200 + 104 = 3 * 168, 2 * 168 + 96 + 80 = 4 * 128: what the block is launched with
+template <bool k8>
+constexpr int kOtherRegs = k8 ? 96 : 104;
+constexpr int kCodeRegs = 80;
+constexpr int kMmaWarp = 8, kLoadWarp = 9, kValueWarp = 10, kTurnWarp = 10, kCodeWarp = 12;
 constexpr int kRing = 4;         // items handed from the load warp to the others
 constexpr int kItemCost = 1;     // an item's start and end, in units,
 constexpr int kPairCost = 5;     // and a pair's, with the tiles along its diagonal
@@ -83,10 +89,10 @@ constexpr int kMaxCtas = (int)(SCOOT_COUNTS / 2);
 constexpr float kMaxScale = 2.3e38f;  // times log2 e it is still finite
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
 
-template <int D>
+template <int D, bool k8 = false>
 struct Shape {
     static constexpr int kTile = kKeys * D * 2;           // bytes of a tile of keys, values or queries
-    static constexpr int kStages = (D == 128 ? 4 : 10);   // tiles of keys or values in flight
+    static constexpr int kStages = (D == 128 ? 4 : 10) - (k8 && D == 64 ? 2 : 0);  // tiles of keys or values in flight
     // Tensor memory: score buffers of 128 columns from 0 on, then the slots' O.
     static constexpr uint32_t kBuf = D == 128 ? 2 : 3, kO = 512 - 2 * D;
     static constexpr int kSmem = 2 * kTile + kStages * kTile + 2 * kScratch;  // and the static part, up to 227 KB
@@ -111,6 +117,13 @@ struct AttnArgs {
     float* parts;         // kBufs part buffers per CTA (part_buf)
     uint32_t* count;      // arrivals per split item and slot, zero between calls
     uint32_t* err;
+    // with codes: bytes in place of elements in the strides, scales [block][head], and the requests that are another kernel's
+    const uint8_t* k8;
+    const uint8_t* v8;
+    const float* k_scale;
+    const float* v_scale;
+    int32_t max_new;      // a request with more tokens is bad (0: none is)
+    int32_t few;          // requests of up to so many tokens are left out
 };
 
 // What the load warp tells the others about an item, or a part of it.
@@ -129,7 +142,7 @@ struct Item {
 // The first three are [slot][number of the slot's unit mod 3, of 4]: up to three units of a slot are under way at once.
 enum {
     kSFull = 0, kPFull = 8, kPvDone = 16, kQFull = 24, kQEmpty = 26, kWg = 28, kItemFull = 30, kItemEmpty = 34, kDrain = 38,
-    kKvFull = 40, kKvEmpty = 50, kBars = 60
+    kKvFull = 40, kKvEmpty = 50, kQReady = 60, kBars = 62
 };
 
 // The swizzled K-major tile of queries or keys: rows of 128 bytes, 8-row groups 1024 bytes apart.
@@ -209,14 +222,16 @@ __device__ __forceinline__ float weightless(float x) { return fabsf(x) < INFINIT
 struct Req {
     int32_t q0, n, kv;
 };
+template <bool k8>
 __device__ __forceinline__ Req load_req(const AttnArgs& a, int r, bool flag) {
     Req q{0, 0, 0};
     if (r >= a.n_req) return q;
     const int q0 = a.query_start[r], q1 = a.query_start[r + 1], kv = a.kv_len[r];
-    if (q0 < 0 || q1 < q0 || q1 > a.n_tokens || kv < 0 || kv > a.ld_table << a.bs_log) {
+    if (q0 < 0 || q1 < q0 || q1 > a.n_tokens || kv < 0 || kv > a.ld_table << a.bs_log || (k8 && a.max_new > 0 && q1 - q0 > a.max_new)) {
         if (flag) atomicOr(a.err, SCOOT_DEVERR_INDEX);
         return q;
     }
+    if (k8 && q1 - q0 <= a.few) return q;
     q.q0 = q0;
     q.n = q1 - q0;
     q.kv = kv;
@@ -681,10 +696,255 @@ __device__ __forceinline__ void no_keys(const AttnArgs& a, const Item& it) {
         }
 }
 
-template <bool kBf16, int D>
-__global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_constant__ AttnArgs a) {
-    using Sh = Shape<D>;
-    constexpr int kNS = Sh::kStages, kNH = D / 64;
+// ---------------------------------------------------------------------------------------------- codes
+
+constexpr int kUpRing = 4;     // items of a slot whose rows' exponents are at hand, likewise
+constexpr int kScaleRing = 8;  // tiles whose scales are at hand: a tile's place is taken again when its softmax is long done
+
+// Two codes as fp16 (exact); the format's NaN as 448.
+__device__ __forceinline__ uint32_t decode_lo(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ uint32_t decode_hi(uint32_t w) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ uint32_t without_nan(uint32_t w) {
+    const uint32_t nan = ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+    return w & ~(nan >> 7);
+}
+__device__ __forceinline__ void st_shared16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// The four warps that make the tiles of keys and values: codes from global memory, through registers, into fp16 tiles of the
+// layout that the products read.  Warp w has keys 32 w .. of a tile: D / 16 lanes a key, 16 codes each.  While a tile is
+// written the next one's codes are on their way into the same registers.  With the keys go the scales of the tile's
+// sixteen groups of eight keys, those of the values as well.
+template <int D>
+__device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, const Item* items, uint32_t tiles, float* scale_s, Waiter& wait) {
+    using Sh = Shape<D, true>;
+    constexpr uint32_t kNS = Sh::kStages;
+    constexpr int kPieces = D / 16, kLoads = kPieces, kPer = 32 / kPieces;  // pieces of a key; loads of a lane; keys of a load
+    const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) - kCodeWarp;
+    const int sub = lane / kPieces, piece = lane % kPieces;
+    const int bs = 1 << a.bs_log;
+    uint32_t at = 0, n_unit = 0;  // tiles made; units
+    bool bad = false, bad_scale = false;
+#pragma unroll 1
+    for (uint32_t n_item = 0;; ++n_item) {
+        const uint32_t slot = n_item % kRing;
+        wait.warp(&bars[kItemFull + slot], n_item / kRing);
+        if (!wait.all()) break;
+        const Item it = items[slot];
+        if (it.stop) break;
+        warp_arrive(&bars[kItemEmpty + slot]);
+        const int32_t* row = a.table + (int64_t)it.r * a.ld_table;
+        // ids of 32 blocks in the lanes, and those of the next 32
+        int group = -1, ids = 0, ids_next = 0;
+        auto fetch = [&](int g) {
+            const int64_t key = ((int64_t)g * 32 + lane) << a.bs_log;
+            return key < it.end && key + bs > it.begin ? __ldg(row + g * 32 + lane) : INT32_MIN;
+        };
+        auto turn_to = [&](int key0) {
+            const int g = (key0 >> a.bs_log) >> 5;
+            if (g == group) return;
+            const int raw = group >= 0 ? ids_next : fetch(g);
+            const bool out = raw < 0 || raw >= a.n_blocks;
+            bad |= out && raw != INT32_MIN;
+            ids = out ? -1 : raw;
+            group = g;
+            ids_next = fetch(g + 1);
+        };
+        uint4 code[kLoads];
+        auto load = [&](int i, int u, const uint8_t* from) {  // codes of this lane's key i of tile u
+            const int key = u * kKeys + 32 * w + i * kPer + sub;
+            const int id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
+            code[i] = make_uint4(0, 0, 0, 0);
+            if (id >= 0 && key >= it.begin && key < it.end)
+                code[i] = __ldg(reinterpret_cast<const uint4*>(from + id * a.ld_block + (key & (bs - 1)) * a.ld_token + it.h * a.ld_head) + piece);
+        };
+        float scale = 0.0f;
+        auto load_scale = [&](int u) {  // warp w: of the keys' groups 4 w .. 4 w + 3 (lanes 0 - 3), and of the values'
+            const int key = u * kKeys + 32 * w + 8 * (lane & 3);
+            const int id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
+            scale = 0.0f;
+            if (lane < 8 && id >= 0 && key + 8 > it.begin && key < it.end)
+                scale = __ldg((lane < 4 ? a.k_scale : a.v_scale) + (int64_t)id * a.n_kv_heads + it.h);
+        };
+        // a tile that some row does not see all of
+        const int64_t all1 = a.causal ? min((int64_t)it.kv, (int64_t)it.pos + 1) : it.kv;
+        const int64_t all0 = a.window > 0 ? max((int64_t)0, (int64_t)it.pos + it.ntok - a.window) : 0;
+        turn_to(it.u0 * kKeys + 32 * w);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) load(i, it.u0, a.k8);
+        load_scale(it.u0);
+#pragma unroll 1
+        for (int n = 0; n < 2 * it.nu && wait.ok; ++n) {
+            const bool values = n & 1;
+            const int u = it.u0 + (n >> 1), next = it.u0 + ((n + 1) >> 1);
+            const uint32_t st = at % kNS;
+            if (at >= kNS) wait.warp(&bars[kKvEmpty + st], at / kNS - 1);
+            if (!wait.all()) break;
+            if (!values && lane < 8) {
+                if (!(scale >= 0.0f && scale < INFINITY)) {
+                    bad_scale = true;
+                    scale = 0.0f;
+                }
+                scale_s[(n_unit % kScaleRing) * 32 + (lane < 4 ? 0 : 16) + 4 * w + (lane & 3)] = scale;
+            }
+            const bool odd = values && ((int64_t)u * kKeys < all0 || (int64_t)u * kKeys + kKeys > all1);
+            if (odd) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i)
+                    code[i] = make_uint4(without_nan(code[i].x), without_nan(code[i].y), without_nan(code[i].z), without_nan(code[i].w));
+            }
+            const bool more = n + 1 < 2 * it.nu;
+            if (more && values) turn_to(next * kKeys + 32 * w);
+            const uint8_t* from = values ? a.k8 : a.v8;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int key = 32 * w + i * kPer + sub;
+                const uint4 c = code[i];
+                // 16 dimensions: two 16-byte chunks of a half's row; the halves' lanes write them in different orders (banks)
+                const uint32_t at_row = tiles + st * Sh::kTile + (piece >> 2) * kHalf + key * 128, ch = 2 * (piece & 3);
+                const uint32_t lo[4] = {decode_lo(c.x), decode_hi(c.x), decode_lo(c.y), decode_hi(c.y)};
+                const uint32_t hi[4] = {decode_lo(c.z), decode_hi(c.z), decode_lo(c.w), decode_hi(c.w)};
+                const bool swap = piece & 4;
+                const uint32_t at_lo = at_row + ((ch ^ (key & 7)) << 4), at_hi = at_row + (((ch + 1) ^ (key & 7)) << 4);
+                st_shared16(swap ? at_hi : at_lo, swap ? hi[0] : lo[0], swap ? hi[1] : lo[1], swap ? hi[2] : lo[2], swap ? hi[3] : lo[3]);
+                st_shared16(swap ? at_lo : at_hi, swap ? lo[0] : hi[0], swap ? lo[1] : hi[1], swap ? lo[2] : hi[2], swap ? lo[3] : hi[3]);
+                if (more) load(i, next, from);
+            }
+            if (more && values) load_scale(next);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            warp_arrive(&bars[kKvFull + st]);
+            ++at;
+            n_unit += values;
+        }
+        if (!wait.ok) break;
+    }
+    if (bad) atomicOr(a.err, SCOOT_DEVERR_INDEX);
+    if (bad_scale) atomicOr(a.err, SCOOT_DEVERR_VALUE);
+    if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
+}
+
+// bf16 queries as fp16, in place: each row divided by a power of two that brings its largest below 2^15 (what that rounds is
+// below 2^-39 of the largest), whose exponent goes to up.  A row of zeros, or with what is not finite, stays as it is.  By a
+// warp of its own: with the softmax warps, the products would wait for them at each item, and they for the products.
+template <int D>
+__device__ __forceinline__ void turn_queries(uint8_t* tile, int8_t* up) {
+#pragma unroll 1
+    for (int row = threadIdx.x & 31; row < kRows; row += 32) {
+        uint4* p = reinterpret_cast<uint4*>(tile + row * 128);
+        auto chunk = [&](int i) -> uint4& { return p[(i / 8) * (kHalf / 16) + ((i ^ row) & 7)]; };
+        uint4 x[D / 8];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+            x[i] = chunk(i);
+            top = __vmaxu2(__vmaxu2(__vmaxu2(top, x[i].x & 0x7FFF7FFFu), x[i].y & 0x7FFF7FFFu), __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu));
+        }
+        top = max(top & 0xFFFFu, top >> 16);
+        const int e = (int)(top >> 7), n = top == 0 || e == 255 ? 0 : min(14 + 127 - e, 126);
+        const float f = __uint_as_float((uint32_t)(127 + n) << 23);
+        auto turn = [&](uint32_t w) { return pack16<false>(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xFFFF0000u) * f); };
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) chunk(i) = make_uint4(turn(x[i].x), turn(x[i].y), turn(x[i].z), turn(x[i].w));
+        up[row] = (int8_t)n;
+    }
+}
+
+// softmax_tile over scores of codes: group g of eight keys has the scales sc[g] (keys) and sc[16 + g] (values).  P is fp16 of
+// p sc[16 + g] / vref * 2^7, vref the largest of the values' scales so far: O is in units of vref 2^-7, and grows with it.
+template <int NCH, typename F>
+__device__ __forceinline__ void softmax_codes(uint32_t tS, int ch0, bool full, int c0, int c1, float c, bool first, bool live, float& m,
+                                              float& l, float& vref, const float* sc, F&& rescale) {
+    uint32_t x[NCH * 32];
+#pragma unroll
+    for (int q = 0; q < NCH; ++q) tmem_ld32(tS + 32 * (ch0 + q), x + 32 * q);
+    tmem_wait_ld();
+    if (!full) {
+#pragma unroll
+        for (int q = 0; q < NCH; ++q) {
+            const int lo = min(max(c0 - 32 * (ch0 + q), 0), 32), hi = min(max(c1 - 32 * (ch0 + q), 0), 32);
+            const uint32_t bits = hi <= lo ? 0u : (0xFFFFFFFFu >> (32 - hi)) & (0xFFFFFFFFu << lo);
+            if (__all_sync(0xffffffffu, bits == 0xFFFFFFFFu)) continue;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (!(bits & (1u << i))) x[32 * q + i] = 0xFF800000u;
+        }
+    }
+    const float4* ks = reinterpret_cast<const float4*>(sc) + ch0;
+    const float4* vs = ks + 4;
+    // (not zero, so that what is masked stays -inf; finite, so that a score of zero stays zero)
+    auto times = [&](float s) { return fminf(fmaxf(c * s, 1e-37f), 3.4e38f); };
+    float mt = -INFINITY, vmax = 0.0f;
+#pragma unroll
+    for (int q = 0; q < NCH; ++q) {
+        const float4 k4 = ks[q], v4 = vs[q];
+        const float kk[4] = {k4.x, k4.y, k4.z, k4.w};
+        vmax = fmaxf(vmax, fmaxf(fmaxf(v4.x, v4.y), fmaxf(v4.z, v4.w)));
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const uint32_t* y = x + 32 * q + 8 * g;
+            float mx[2] = {__uint_as_float(y[0]), __uint_as_float(y[1])};
+#pragma unroll
+            for (int i = 2; i < 8; ++i) mx[i & 1] = fmaxf(mx[i & 1], __uint_as_float(y[i]));
+            mt = fmaxf(mt, fmaxf(mx[0], mx[1]) * times(kk[g]));
+        }
+    }
+    if (first) {
+        m = mt;
+        vref = fmaxf(vmax, 0x1p-100f);
+    } else if (__any_sync(0xffffffffu, live && mt > m + 8.0f) || vmax > vref) {
+        const float mn = fmaxf(m, mt);
+        const float f = mn == -INFINITY ? 1.0f : exp2_hw(m - mn), vn = fmaxf(vref, vmax);
+        m = mn;
+        l *= f;
+        rescale(f * (vref / vn));
+        vref = vn;
+    }
+    const float ms = finite_or_zero(m), inv = __fdividef(128.0f, vref);
+    const float2 mm = make_float2(-ms, -ms);
+    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+    for (int q = 0; q < NCH; ++q) {
+        const float4 k4 = ks[q], v4 = vs[q];
+        const float kk[4] = {k4.x, k4.y, k4.z, k4.w}, vv[4] = {v4.x, v4.y, v4.z, v4.w};
+        uint32_t p[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float ck = times(kk[i / 4]), vk = vv[i / 4] * inv;
+            const float2 s = make_float2(__uint_as_float(x[32 * q + 2 * i]), __uint_as_float(x[32 * q + 2 * i + 1]));
+            const float2 t = __ffma2_rn(s, make_float2(ck, ck), mm);
+            const float2 e = make_float2(exp2_hw(t.x), exp2_hw(t.y));
+            sum[i & 1] = __fadd2_rn(sum[i & 1], e);
+            const float2 pv = __fmul2_rn(e, make_float2(vk, vk));
+            p[i] = pack16<false>(pv.x, pv.y);
+        }
+        tmem_st16(tS + 16 * (ch0 + q), p);
+    }
+    if (NCH < 4) {
+        uint32_t z[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[i] = 0u;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (q < ch0 || q >= ch0 + NCH) tmem_st16(tS + 16 * q, z);
+    }
+    l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
+    tmem_wait_st();
+}
+
+template <bool kBf16, int D, bool k8>
+__global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __grid_constant__ AttnArgs a) {
+    using Sh = Shape<D, k8>;
+    constexpr int kNS = Sh::kStages, kNH = D / 64, kNT = kThreads<k8>;
+    constexpr bool kTurn = k8 && kBf16;  // queries are turned into fp16 before they are used
     extern __shared__ __align__(1024) uint8_t smem[];
     uint8_t* sQ = smem;
     uint8_t* sKV = sQ + 2 * Sh::kTile;
@@ -694,9 +954,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     __shared__ uint32_t tslot;
     // the threads' sums of costs and requests, in the ring's last tile until the load warp has found its first item
     int64_t* cost_s = reinterpret_cast<int64_t*>(sKV + (kNS - 1) * Sh::kTile);
-    Req* req_s = reinterpret_cast<Req*>(cost_s + kThreads);
+    Req* req_s = reinterpret_cast<Req*>(cost_s + kNT);
     __shared__ int last_flag[2];
-    __shared__ float2 ml_s[2][kRows];
+    // m and l of copies; with codes in the scratch (there is no more shared memory to be had), and a ring of tiles' scales
+    __shared__ float2 ml_own[k8 ? 1 : 2][k8 ? 1 : kRows];
+    __shared__ __align__(16) float scale_s[k8 ? kScaleRing : 1][k8 ? 32 : 1];
+    __shared__ int8_t up_s[kTurn ? 2 * kUpRing : 1][kTurn ? kRows : 1];
     // (the same for all lanes, and by the shuffle known to be)
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
@@ -710,19 +973,20 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             mbar_init(&bars[kQFull + s], 1);
             mbar_init(&bars[kQEmpty + s], 1);
             mbar_init(&bars[kWg + s], 4);
+            if (kTurn) mbar_init(&bars[kQReady + s], 1);
         }
         for (int s = 0; s < kRing; ++s) {
             mbar_init(&bars[kItemFull + s], 1);
-            mbar_init(&bars[kItemEmpty + s], 10);  // eight softmax warps, the product thread and the value warp
+            mbar_init(&bars[kItemEmpty + s], kTurn ? 15 : k8 ? 13 : 10);  // eight softmax warps, the product thread, and the value warp or those of codes and of queries
         }
         mbar_init(&bars[kDrain], 1);
         for (int s = 0; s < kNS; ++s) {
-            mbar_init(&bars[kKvFull + s], 1);
+            mbar_init(&bars[kKvFull + s], k8 ? 4 : 1);
             mbar_init(&bars[kKvEmpty + s], 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == kLoadWarp && lane < 5 && (lane < 3 || kRows >> (lane - 2) >= a.group)) {  // (maps that are in use)
+    if (warp == kLoadWarp && lane >= (k8 ? 2 : 0) && lane < 5 && (lane < 3 || kRows >> (lane - 2) >= a.group)) {  // (maps that are in use)
         const CUtensorMap* map = lane == 0 ? &a.kmap : lane == 1 ? &a.vmap : &a.qmap[lane - 2];
         asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
     }
@@ -733,12 +997,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
 
     // The cost of all items of one head: each thread k consecutive requests, then a scan.  A request of several items is
     // summed by its warp.
-    const int k = (a.n_req + kThreads - 1) / kThreads, per = 2 * a.toks;
+    const int k = (a.n_req + kNT - 1) / kNT, per = 2 * a.toks;
     int64_t mine = 0;
 #pragma unroll 1
     for (int i = 0; i < k; ++i) {
         const int r = tid * k + i;
-        const Req q = load_req(a, r, blockIdx.x == 0);
+        const Req q = load_req<k8>(a, r, blockIdx.x == 0);
         if (k == 1) req_s[tid] = q;
         if (q.n > 0 && q.n <= per) mine += item_cost(a, q.n, 0) + item_units(a, q.kv, q.n, 0);
         uint32_t big = __ballot_sync(0xffffffffu, q.n > per);
@@ -767,8 +1031,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
     const uint32_t tmem = tslot;
     Waiter wait;
 
-    if (warp >= kMmaWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (k8 && warp >= kCodeWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCodeRegs));
+        if constexpr (k8) code_tiles<D>(a, bars, items, smem_u32(sKV), &scale_s[0][0], wait);
+    } else if (warp >= kMmaWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs<k8>));
         if (warp == kLoadWarp) {
             // ---- items, and the copies of their tiles
             uint32_t n_item = 0, n_q[2] = {0, 0};
@@ -777,20 +1044,20 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             auto get = [&](int r) {
                 if ((r >> 5) != cached) {
                     cached = r >> 5;
-                    in_lane = load_req(a, cached * 32 + lane, false);
+                    in_lane = load_req<k8>(a, cached * 32 + lane, false);
                 }
                 return Req{__shfl_sync(0xffffffffu, in_lane.q0, r & 31), __shfl_sync(0xffffffffu, in_lane.n, r & 31),
                            __shfl_sync(0xffffffffu, in_lane.kv, r & 31)};
             };
             // The warps' sums, one per lane, and their running sum: a head's cost at the last.  All heads' items in a row are cut
             // into ranges of `range` units; this CTA's is [B0, B1).
-            int64_t upto = lane < kThreads / 32 ? cost_s[lane * 32 + 31] : 0;
+            int64_t upto = lane < kNT / 32 ? cost_s[lane * 32 + 31] : 0;
 #pragma unroll
-            for (int d = 1; d < kThreads / 32; d <<= 1) {
+            for (int d = 1; d < kNT / 32; d <<= 1) {
                 const int64_t t = __shfl_up_sync(0xffffffffu, upto, d);
                 if (lane >= d) upto += t;
             }
-            const int64_t head_cost = __shfl_sync(0xffffffffu, upto, kThreads / 32 - 1), total = head_cost * a.n_kv_heads;
+            const int64_t head_cost = __shfl_sync(0xffffffffu, upto, kNT / 32 - 1), total = head_cost * a.n_kv_heads;
             const int64_t range = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)kMinRange);
             const int64_t B0 = min(total, blockIdx.x * range), B1 = min(total, B0 + range);
             const int snap = (int)max((int64_t)kSnapMin, min((int64_t)kSnapMax, range / 4));
@@ -800,7 +1067,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 // the warp, then the thread, whose sum passes y, then the request, then its item
                 h = (int)quotient(B0, head_cost);
                 const int64_t y = B0 - h * head_cost;
-                const int w = __ffs(__ballot_sync(0xffffffffu, lane < kThreads / 32 && upto > y)) - 1;
+                const int w = __ffs(__ballot_sync(0xffffffffu, lane < kNT / 32 && upto > y)) - 1;
                 int64_t at = __shfl_sync(0xffffffffu, upto, w) - cost_s[w * 32 + 31];
                 const int64_t in_warp = cost_s[w * 32 + lane];
                 const int t = __ffs(__ballot_sync(0xffffffffu, at + in_warp > y)) - 1;
@@ -840,7 +1107,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the tile may be copied over
                 __syncwarp();
             }
-            TileLoader<D> keys(a, &a.kmap, bars, smem_u32(sKV), 0);
+            TileLoader<D> keys(a, &a.kmap, bars, smem_u32(sKV), 0);  // (with codes not used)
             auto load_q = [&](const Item& it, int s, int tok, int head) {
                 if (n_q[s] > 0) wait.warp(&bars[kQEmpty + s], n_q[s] - 1);
                 if (!wait.all()) return;
@@ -921,10 +1188,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 }
                 __syncwarp();
                 ++n_item;
-                keys.begin(it);
+                if (!k8) keys.begin(it);
 #pragma unroll 1
-                for (int u = 0; u < it.nu && wait.ok; ++u) {
-                    keys.tile(it, it.u0 + u, wait);
+                for (int u = 0; u < (k8 ? 1 : it.nu) && wait.ok; ++u) {
+                    if (!k8) keys.tile(it, it.u0 + u, wait);
                     if (u == 0) {
 #pragma unroll
                         for (int sl = 0; sl < 2; ++sl)
@@ -947,7 +1214,26 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 for (int s = 0; s < 2; ++s)
                     if (n_q[s] > 0) mbar_wait_tries(smem_u32(&bars[kQFull + s]), (n_q[s] - 1) & 1u);
             }
-        } else if (warp == kValueWarp) {
+        } else if (kTurn && warp >= kTurnWarp) {
+            // ---- the queries of a slot
+            const int s = warp - kTurnWarp;
+            uint32_t n_q = 0;
+            for (uint32_t n_item = 0;; ++n_item) {
+                wait.warp(&bars[kItemFull + n_item % kRing], n_item / kRing);
+                if (!wait.all()) break;
+                const int slot = items[n_item % kRing].slot, stop = items[n_item % kRing].stop;
+                if (stop) break;
+                warp_arrive(&bars[kItemEmpty + n_item % kRing]);
+                if (slot != 2 && slot != s) continue;
+                wait.warp(&bars[kQFull + s], n_q);
+                if (!wait.all()) break;
+                if constexpr (kTurn) turn_queries<D>(sQ + s * Sh::kTile, up_s[s * kUpRing + n_q % kUpRing]);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                warp_arrive(&bars[kQReady + s]);
+                ++n_q;
+            }
+            if (!wait.ok && lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
+        } else if (!k8 && warp == kValueWarp) {
             // ---- the copies of the values
             TileLoader<D> vals(a, &a.vmap, bars, smem_u32(sKV), 1);
             for (uint32_t n_item = 0; wait.ok; ++n_item) {
@@ -979,7 +1265,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 uint32_t buf = 0, n_q0 = 0, n_q1 = 0;
                 uint32_t next0 = 0, next1 = 4;        // the slots' next units, as in a word
                 uint32_t v_word = 1u << kVStage;      // this unit's values: stage and phase, as in a word
-                const uint32_t id_s = idesc(kBf16, kKeys, false), id_o = idesc(kBf16, D, true), bar0 = smem_u32(bars);
+                const uint32_t id_s = idesc(kBf16 && !k8, kKeys, false), id_o = idesc(kBf16 && !k8, D, true), bar0 = smem_u32(bars);
                 const uint32_t q_desc = (uint32_t)desc_k(smem_u32(sQ)), k_desc0 = (uint32_t)desc_k(smem_u32(sKV)),
                                v_desc = (uint32_t)desc_v(smem_u32(sKV));
                 uint32_t k_desc = k_desc0, k_bar = bar0 + 8 * kKvFull;  // this unit's keys
@@ -1036,7 +1322,14 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 };
                 auto scores = [&](uint32_t sl, int u, int nu, bool last) {  // last: of this tile's users
                     if (u == 0) {
-                        wait.at(bar0 + 8 * (kQFull + sl), (sl ? n_q1 : n_q0) & 1u);
+                        const uint32_t q_bar = bar0 + 8 * ((kTurn ? kQReady : kQFull) + sl), q_phase = (sl ? n_q1 : n_q0) & 1u;
+                        if (k8)  // (as for keys below)
+                            for (uint32_t i = 0; !ready(q_bar, q_phase); ++i) {
+                                if (n_todo && ready(p_bar(), p_phase())) values();
+                                else wait.ok &= i < (1u << 22);
+                                if (!wait.all()) break;
+                            }
+                        wait.at(q_bar, q_phase);
                         n_q0 += sl == 0;
                         n_q1 += sl;
                     }
@@ -1108,7 +1401,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs<k8>));
         // ---- softmax of slot s; this thread's row of tensor memory is lane row
         const int s = warp >> 2, row = tid & (kRows - 1);
         const uint32_t lane_at = (uint32_t)(32 * (warp & 3)) << 16;
@@ -1117,6 +1410,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
         uint32_t n_unit = 0, buf = 0, unit = 0, uphase = 0;
         const uint32_t slot_bars = smem_u32(bars) + 32 * s;
         SlotSync wg_sync{&bars[kWg + s], 0, {}};
+        float2* ml = k8 ? reinterpret_cast<float2*>(sScratch + s * kScratch) : ml_own[k8 ? 0 : s];
+        uint32_t n_turned = 0;  // items of this slot
         for (uint32_t n_item = 0;; ++n_item) {
             const uint32_t ring = n_item % kRing;
             wait.warp(&bars[kItemFull + ring], n_item / kRing);
@@ -1147,6 +1442,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             const int all1 = a.causal ? min(it.kv, it.pos + tok0 + 1) : it.kv;
             const int all0 = a.window > 0 ? (int)max((int64_t)0, (int64_t)it.pos + tok0 + ntok - a.window) : 0;
             float m = -INFINITY, l = 0.0f;
+            float c_row = a.scale_log2, vref = 0x1p-100f;  // with codes: scale of the row's scores; O is in units of vref 2^-7
             const uint32_t step = it.slot == 2 ? 2 : 1;
             uint32_t b = (buf + (it.slot == 2 ? s : 0)) % Sh::kBuf;
             buf = (buf + step * it.nu) % Sh::kBuf;
@@ -1159,6 +1455,10 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 if (b >= Sh::kBuf) b -= Sh::kBuf;
                 wait.at(at + 8 * kSFull, uphase);
                 fence_after();
+                if (kTurn && u == 0) {  // (there before the queries were used)
+                    const int n = up_s[s * kUpRing + n_turned++ % kUpRing][row];
+                    c_row = fminf(c_row * __uint_as_float((uint32_t)(127 - n) << 23), 3.4e38f);
+                }
                 if (busy) {
                     auto rescale = [&](float f) {
                         wait.warp(&bars[kPvDone + 4 * s + (unit ? unit - 1 : 2)], unit ? uphase : uphase ^ 1u);
@@ -1173,14 +1473,22 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                             tmem_st16(tO + c, o);
                         }
                     };
-                    if (it.rep_log == 0)
+                    if constexpr (k8) {
+                        const float* sc = scale_s[n_unit % kScaleRing];
+                        if (it.rep_log == 0)
+                            softmax_codes<4>(tS, 0, full, k0 - t0, k1 - t0, c_row, u == 0, live, m, l, vref, sc, rescale);
+                        else if (it.rep_log == 1)
+                            softmax_codes<2>(tS, 2 * copy, full, k0 - t0, k1 - t0, c_row, u == 0, live, m, l, vref, sc, rescale);
+                        else
+                            softmax_codes<1>(tS, copy, full, k0 - t0, k1 - t0, c_row, u == 0, live, m, l, vref, sc, rescale);
+                    } else if (it.rep_log == 0)
                         softmax_tile<kBf16, 4>(tS, 0, full, k0 - t0, k1 - t0, a.scale_log2, u == 0, live, m, l, rescale);
                     else if (it.rep_log == 1)
                         softmax_tile<kBf16, 2>(tS, 2 * copy, full, k0 - t0, k1 - t0, a.scale_log2, u == 0, live, m, l, rescale);
                     else
                         softmax_tile<kBf16, 1>(tS, copy, full, k0 - t0, k1 - t0, a.scale_log2, u == 0, live, m, l, rescale);
                 }
-                if (!full) {
+                if (!k8 && !full) {
                     // values that some row may not see: this thread looks through those of key t0 + row
                     const uint32_t load = 2 * n_unit + 1, st = load % kNS;
                     wait.warp(&bars[kKvFull + st], load / kNS);
@@ -1220,7 +1528,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
             wait.warp(&bars[kPvDone + 4 * s + (unit ? unit - 1 : 2)], unit ? uphase : uphase ^ 1u);
             fence_after();
             const bool poison = *reinterpret_cast<volatile int32_t*>(&items[ring].poison) != 0;
-            if (busy) {
+            if (!k8 && busy) {
                 // 0 times the sums: NaN if one of them is not finite (those of a row whose scores are NaN stay as they are)
                 float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
@@ -1241,6 +1549,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]);
             };
+            const float unit_o = k8 ? vref * 0x1p-7f : 1.0f;
             const int head = it.h * a.group, tok = it.tok + tok0;
             const bool whole = it.n_parts == 1;
             // parts of half 0, then those of half 1, of all CTAs
@@ -1251,18 +1560,19 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                 // Copies of the rows: their common maximum and sum, then the weighted sums of their O through the scratch
                 // (16-byte groups swizzled by the row), as many columns at a time as it holds of the rows in use.
                 const int copies = 1 << it.rep_log, used = rows << it.rep_log;
-                ml_s[s][row] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
+                ml[row] = live ? make_float2(m, l) : make_float2(-INFINITY, 0.0f);
                 wg_sync();
                 float M = -INFINITY, L = 0.0f;
 #pragma unroll 1
-                for (int c = 0; c < copies; ++c) M = fmaxf(M, ml_s[s][c * per_copy + rr].x);
+                for (int c = 0; c < copies; ++c) M = fmaxf(M, ml[c * per_copy + rr].x);
                 const float Ms = finite_or_zero(M);
 #pragma unroll 1
                 for (int c = 0; c < copies; ++c) {
-                    const float2 v = ml_s[s][c * per_copy + rr];
+                    const float2 v = ml[c * per_copy + rr];
                     L = fmaf(exp2_hw(v.x - Ms), v.y, L);
                 }
-                const float w = exp2_hw(m - Ms), f = whole ? w * inverse_sum(L) : w, g = f == 0.0f ? 1.0f : f;
+                const float w = exp2_hw(m - Ms), f = whole ? w * inverse_sum(L) : w, g = k8 ? f * unit_o : f == 0.0f ? 1.0f : f;
+                if (k8) wg_sync();  // (m and l were in the scratch)
                 if (copy == 0 && live) {
                     if (!whole) *reinterpret_cast<float2*>(buf + kRows * D + 2 * rr) = make_float2(M, L);
                     else if (a.lse) *lse_row(a, tok, head, rr) = L == 0.0f ? -INFINITY : (M + __log2f(L)) * kLn2;
@@ -1277,7 +1587,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                             float o[32];
                             load_o(c0 + c, o);
                             if (live) {
-                                if (f == 0.0f)
+                                if (!k8 && f == 0.0f)
 #pragma unroll
                                     for (int i = 0; i < 32; ++i) o[i] = weightless(o[i]);
                                 const int at = copy * rows + rr;
@@ -1304,7 +1614,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                     if (c0 + width < D) wg_sync();
                 }
             } else if (whole) {
-                const float inv = inverse_sum(l);
+                const float inv = inverse_sum(l) * unit_o;
                 if (busy) {
                     uint16_t* dst = out_row(a, tok, head, rr);
 #pragma unroll 1
@@ -1329,7 +1639,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_attn_kernel(const __grid_co
                     if (live) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)
-                            *reinterpret_cast<float4*>(buf + row * D + c + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                            *reinterpret_cast<float4*>(buf + row * D + c + i) = make_float4(o[i] * unit_o, o[i + 1] * unit_o, o[i + 2] * unit_o, o[i + 3] * unit_o);
                     }
                 }
                 if (live) *reinterpret_cast<float2*>(buf + kRows * D + 2 * row) = make_float2(m, l);
@@ -1387,23 +1697,81 @@ bool encode(CUtensorMap* map, bool bf16, const void* base, int n_dim, const cuui
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool kBf16, int D>
-scoot_status launch(scoot_ctx* ctx, AttnArgs& a, int sms, cudaStream_t st) {
-    scoot_status s = scoot_workspace(ctx, (size_t)sms * kBufs * kRows * (D + 2) * sizeof(float), st);
-    if (s != SCOOT_OK) return s;
-    a.parts = static_cast<float*>(ctx->ws);
-    auto kern = paged_attn_kernel<kBf16, D>;
-    const uint32_t bit = 1u << (2 * kBf16 + (D == 128));
+template <bool kBf16, int D, bool k8>
+scoot_status launch(scoot_ctx* ctx, const AttnArgs& a, int sms, cudaStream_t st) {
+    auto kern = paged_attn_kernel<kBf16, D, k8>;
+    const uint32_t bit = 1u << ((k8 ? 13 : 0) + 2 * kBf16 + (D == 128));
     if (!(ctx->smem_set & bit)) {  // once per context: the call is short
-        SCOOT_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem));
+        SCOOT_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D, k8>::kSmem));
         ctx->smem_set |= bit;
     }
-    kern<<<(unsigned)sms, kThreads, Shape<D>::kSmem, st>>>(a);
+    kern<<<(unsigned)sms, kThreads<k8>, Shape<D, k8>::kSmem, st>>>(a);
     SCOOT_LAUNCHED(ctx);
     return SCOOT_OK;
 }
+template <bool k8>
+scoot_status launch(scoot_ctx* ctx, const AttnArgs& a, bool bf16, int D, int sms, cudaStream_t st) {
+    if (bf16) return D == 128 ? launch<true, 128, k8>(ctx, a, sms, st) : launch<true, 64, k8>(ctx, a, sms, st);
+    return D == 128 ? launch<false, 128, k8>(ctx, a, sms, st) : launch<false, 64, k8>(ctx, a, sms, st);
+}
+
+// The maps of the queries' boxes.
+bool encode_queries(AttnArgs& a, bool bf16, int D, int G, int n_heads, int64_t n_tokens, const void* q, int64_t ld_token, int64_t ld_head) {
+    for (int i = 0; i < 3; ++i) {
+        const int toks = (kRows >> i) / G;
+        if (toks == 0) continue;  // a token's rows do not fit: no item uses it
+        const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)n_heads, (cuuint64_t)n_tokens};
+        const int64_t ld[2] = {ld_head, ld_token};
+        const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)toks};
+        if (!encode(&a.qmap[i], bf16, q, 3, dims, ld, box)) return false;
+    }
+    return true;
+}
 
 }  // namespace
+
+size_t scoot_attn8_tile_bytes(int head_dim) { return (size_t)kBufs * kRows * (head_dim + 2) * sizeof(float); }
+
+scoot_status scoot_attn8_tiles(scoot_ctx* ctx, const scoot_kv_layout* layout, const Attn8Args& args, bool bf16, int sms, cudaStream_t st) {
+    const int D = layout->head_dim, G = args.group;
+    if (!encode_tiled()) return scoot_fail(ctx, SCOOT_ECUDA, "the driver has no cuTensorMapEncodeTiled");
+    AttnArgs a = {};
+    if (!encode_queries(a, bf16, D, G, args.n_heads, args.n_tokens, args.q, args.q_ld_token, args.q_ld_head))
+        return scoot_fail(ctx, SCOOT_EINVAL, "q's layout has no tensor map");
+    a.bs_log = args.bs_log;
+    a.n_heads = args.n_heads;
+    a.n_kv_heads = args.n_kv_heads;
+    a.group = G;
+    a.n_req = args.n_req;
+    a.causal = args.causal;
+    a.window = args.window;
+    a.toks = kRows / G;
+    a.inv_group = (65536 + G - 1) / G;
+    a.n_tokens = args.n_tokens;
+    a.n_blocks = args.n_blocks;
+    a.query_start = args.query_start;
+    a.kv_len = args.kv_len;
+    a.table = args.table;
+    a.ld_table = args.ld_table;
+    a.ld_block = args.ld_block;
+    a.ld_token = args.ld_token;
+    a.ld_head = args.ld_head;
+    a.scale_log2 = args.scale_log2;
+    a.out = args.out;
+    a.out_ld_token = args.out_ld_token;
+    a.out_ld_head = args.out_ld_head;
+    a.lse = args.lse;
+    a.parts = args.tile_parts;
+    a.count = args.tile_count;
+    a.err = args.err;
+    a.k8 = args.k;
+    a.v8 = args.v;
+    a.k_scale = args.k_scale;
+    a.v_scale = args.v_scale;
+    a.max_new = args.max_new;
+    a.few = args.few;
+    return launch<true>(ctx, a, bf16, D, sms, st);
+}
 
 extern "C" scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_layout* layout, const void* q,
                                               int64_t q_ld_token, int64_t q_ld_head, int32_t n_heads, int64_t n_tokens,
@@ -1444,14 +1812,8 @@ extern "C" scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_lay
         if (!encode(&a.kmap, bf16, k_cache, 4, dims, ld, box) || !encode(&a.vmap, bf16, v_cache, 4, dims, ld, box))
             return scoot_fail(ctx, SCOOT_EINVAL, "the cache's layout has no tensor map");
     }
-    for (int i = 0; i < 3; ++i) {
-        const int toks = (kRows >> i) / G;
-        if (toks == 0) continue;  // a token's rows do not fit: no item uses it
-        const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)n_heads, (cuuint64_t)n_tokens};
-        const int64_t ld[2] = {q_ld_head, q_ld_token};
-        const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)toks};
-        if (!encode(&a.qmap[i], bf16, q, 3, dims, ld, box)) return scoot_fail(ctx, SCOOT_EINVAL, "q's layout has no tensor map");
-    }
+    if (!encode_queries(a, bf16, D, G, n_heads, n_tokens, q, q_ld_token, q_ld_head))
+        return scoot_fail(ctx, SCOOT_EINVAL, "q's layout has no tensor map");
     while ((1 << a.bs_log) < layout->block_size) ++a.bs_log;
     a.n_heads = n_heads;
     a.n_kv_heads = layout->n_kv_heads;
@@ -1479,6 +1841,8 @@ extern "C" scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_lay
     a.count = ctx->d_count;
     a.err = ctx->d_err;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (bf16) return D == 128 ? launch<true, 128>(ctx, a, sms, st) : launch<true, 64>(ctx, a, sms, st);
-    return D == 128 ? launch<false, 128>(ctx, a, sms, st) : launch<false, 64>(ctx, a, sms, st);
+    s = scoot_workspace(ctx, (size_t)sms * kBufs * kRows * (D + 2) * sizeof(float), st);
+    if (s != SCOOT_OK) return s;
+    a.parts = static_cast<float*>(ctx->ws);
+    return launch<false>(ctx, a, bf16, D, sms, st);
 }

@@ -29,8 +29,8 @@
 #include <algorithm>
 #include <cfloat>
 
-#include "internal.h"
 #include "mbarrier.cuh"
+#include "paged_attn8.cuh"
 
 namespace {
 
@@ -39,7 +39,8 @@ constexpr int kRows = 16, kKeys = 32;
 constexpr int kItemCost = 2;    // an item's start and end, in tiles
 constexpr int kMinRange = 4;    // cost that a warp takes at least
 constexpr int kSnap = 2;        // a cut this close to the start or end of an item's tiles moves there
-constexpr int kMaxBlocks = (int)(SCOOT_COUNTS / 2);
+constexpr int kMaxBlocks = (int)(SCOOT_COUNTS / 4);  // a counter each, and two for the tiles kernel, apart
+constexpr int kFewRows = 32;    // requests of up to so many rows
 constexpr float kMaxScale = 2.3e38f;  // times log2 e it is still finite
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
 
@@ -50,30 +51,6 @@ struct Shape {
     static constexpr int kStages = D == 128 ? 3 : 6;
     static constexpr int kSmem = kWarps * kStages * kStage;
     static constexpr int kPart = kRows * (D + 2);        // floats of a part: O, then (m, l) of each row
-};
-
-struct Attn8Args {
-    int32_t bs_log, n_heads, n_kv_heads, group, n_req, causal, window, max_new;
-    int32_t toks, per_token;   // tokens of an item, and items of a token (more than one: groups of more than 16 heads)
-    int64_t n_tokens, n_blocks;
-    const int32_t* query_start;
-    const int32_t* kv_len;
-    const int32_t* table;
-    int64_t ld_table;
-    const uint16_t* q;
-    int64_t q_ld_token, q_ld_head;
-    const uint8_t* k;
-    const uint8_t* v;
-    int64_t ld_block, ld_token, ld_head;
-    const float* k_scale;
-    const float* v_scale;
-    float scale_log2;
-    uint16_t* out;
-    int64_t out_ld_token, out_ld_head;
-    float* lse;
-    float* parts;          // two per warp, then two per block
-    uint32_t* count;       // arrivals of blocks per split item, zero between calls
-    uint32_t* err;
 };
 
 struct Item {
@@ -163,6 +140,7 @@ __device__ __forceinline__ Req load_req(const Attn8Args& a, int r, bool flag) {
         if (flag) atomicOr(a.err, SCOOT_DEVERR_INDEX);
         return q;
     }
+    if (q1 - q0 > a.few) return q;
     q.q0 = q0;
     q.n = q1 - q0;
     q.kv = kv;
@@ -711,11 +689,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
 }
 
 template <bool kBf16, int D>
-scoot_status launch(scoot_ctx* ctx, Attn8Args& a, int sms, cudaStream_t st) {
+scoot_status launch(scoot_ctx* ctx, const Attn8Args& a, int sms, cudaStream_t st) {
     using Sh = Shape<D>;
-    scoot_status s = scoot_workspace(ctx, (size_t)sms * 2 * (kWarps + 1) * Sh::kPart * sizeof(float), st);
-    if (s != SCOOT_OK) return s;
-    a.parts = static_cast<float*>(ctx->ws);
     auto kern = attn8_rows_kernel<kBf16, D>;
     const uint32_t bit = 1u << (9 + 2 * kBf16 + (D == 128));
     if (!(ctx->smem_set & bit)) {  // once per context: the call is short
@@ -791,9 +766,24 @@ extern "C" scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_la
     a.out_ld_token = out_ld_token;
     a.out_ld_head = out_ld_head;
     a.lse = lse;
-    a.count = ctx->d_count;
+    a.count = ctx->d_count + 2 * kMaxBlocks;
+    a.tile_count = ctx->d_count;
     a.err = ctx->d_err;
+    a.few = kFewRows / G;
+    // The host does not know the lengths: without max_new both kernels are launched, and one may find nothing to do.
+    const bool rows = a.few > 0, tiles = max_new == 0 || max_new > a.few;
+    const size_t part = (D == 128 ? Shape<128>::kPart : Shape<64>::kPart) * sizeof(float);
+    const size_t row_bytes = rows ? (size_t)sms * 2 * (kWarps + 1) * part : 0;
+    s = scoot_workspace(ctx, row_bytes + (tiles ? sms * scoot_attn8_tile_bytes(D) : 0), stream);
+    if (s != SCOOT_OK) return s;
+    a.parts = static_cast<float*>(ctx->ws);
+    a.tile_parts = a.parts + row_bytes / sizeof(float);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == SCOOT_BF16) return D == 128 ? launch<true, 128>(ctx, a, sms, st) : launch<true, 64>(ctx, a, sms, st);
-    return D == 128 ? launch<false, 128>(ctx, a, sms, st) : launch<false, 64>(ctx, a, sms, st);
+    const bool bf16 = dtype == SCOOT_BF16;
+    if (rows) {
+        if (bf16) s = D == 128 ? launch<true, 128>(ctx, a, sms, st) : launch<true, 64>(ctx, a, sms, st);
+        else s = D == 128 ? launch<false, 128>(ctx, a, sms, st) : launch<false, 64>(ctx, a, sms, st);
+        if (s != SCOOT_OK) return s;
+    }
+    return tiles ? scoot_attn8_tiles(ctx, layout, a, bf16, sms, st) : SCOOT_OK;
 }
