@@ -71,10 +71,10 @@ constexpr int kKeys = 128;         // keys of a tile
 template <bool k8>
 constexpr int kThreads = k8 ? 512 : 384;
 template <bool k8>
-constexpr int kSoftmaxRegs = k8 ? 168 : 200;  // 2 * 200 + 104 = 3 * 168, 2 * 168 + 96 + 80 = 4 * 128: what the block is launched with
+constexpr int kSoftmaxRegs = k8 ? 184 : 200;  // 2 * 200 + 104 = 3 * 168, 2 * 184 + 72 + 72 = 4 * 128: what the block is launched with
 template <bool k8>
-constexpr int kOtherRegs = k8 ? 96 : 104;
-constexpr int kCodeRegs = 80;
+constexpr int kOtherRegs = k8 ? 72 : 104;
+constexpr int kCodeRegs = 72;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kValueWarp = 10, kTurnWarp = 10, kCodeWarp = 12;
 constexpr int kRing = 4;         // items handed from the load warp to the others
 constexpr int kItemCost = 1;     // an item's start and end, in units,
@@ -699,7 +699,21 @@ __device__ __forceinline__ void no_keys(const AttnArgs& a, const Item& it) {
 // ---------------------------------------------------------------------------------------------- codes
 
 constexpr int kUpRing = 4;     // items of a slot whose rows' exponents are at hand, likewise
-constexpr int kScaleRing = 8;  // tiles whose scales are at hand: a tile's place is taken again when its softmax is long done
+// Tiles whose scales are at hand, a place being taken again when its softmax is done: the keys of unit n are written when the
+// scores of the unit before in their place of the ring (n - 2; n - 4) are there, and those wait for the softmax of the
+// unit that had their score buffer (two; three units before).
+template <int D>
+constexpr int kScaleRing = D == 128 ? 6 : 8;
+
+// A tile's scales: sixteen groups of eight keys, of keys and then of values.  Where all of either kind are the same number
+// times powers of two (zeros aside), as scoot_kv_append8 makes them, `even` is set and the codes in the tiles are in units
+// of the largest, so that softmax has one scale per tile.  Else they are in units of their groups' own.  They are multiplied by
+// 2^7 (448 is below 65504 2^-7), so that what fp16 cannot hold of them is below 2^-32 of the largest scale.
+struct TileScales {
+    float k[16], v[16];
+    float k_top, v_top;
+    int32_t even, unused;
+};
 
 // Two codes as fp16 (exact); the format's NaN as 448.
 __device__ __forceinline__ uint32_t decode_lo(uint32_t w) {
@@ -720,19 +734,28 @@ __device__ __forceinline__ void st_shared16(uint32_t addr, uint32_t a, uint32_t 
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
+__device__ __forceinline__ uint32_t times_half2(uint32_t a, uint32_t b) {
+    const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
 // The four warps that make the tiles of keys and values: codes from global memory, through registers, into fp16 tiles of the
-// layout that the products read.  Warp w has keys 32 w .. of a tile: D / 16 lanes a key, 16 codes each.  While a tile is
-// written the next one's codes are on their way into the same registers.  With the keys go the scales of the tile's
-// sixteen groups of eight keys, those of the values as well.
+// layout that the products read.  Warp w has keys 32 w .. of a tile, a lane sixteen dimensions of eight (four) keys in a
+// row, so that it has one block and one scale per tile.  While a tile is written the next one's codes are on their way
+// into the same registers.  With the keys go the tile's scales.
 template <int D>
-__device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, const Item* items, uint32_t tiles, float* scale_s, Waiter& wait) {
+__device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, const Item* items, uint32_t tiles, TileScales* scales, Waiter& wait) {
     using Sh = Shape<D, true>;
     constexpr uint32_t kNS = Sh::kStages;
-    constexpr int kPieces = D / 16, kLoads = kPieces, kPer = 32 / kPieces;  // pieces of a key; loads of a lane; keys of a load
+    constexpr int kPieces = D / 16, kLoads = kPieces;  // pieces of a key; keys of a lane
     const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) - kCodeWarp;
-    const int sub = lane / kPieces, piece = lane % kPieces;
+    const int sub = lane / kPieces, piece = lane % kPieces, first = 32 * w + kLoads * sub;
     const int bs = 1 << a.bs_log;
-    uint32_t at = 0, n_unit = 0;  // tiles made; units
+    // Where the lane's first chunk of its first key goes in a tile: 16 dimensions are two chunks of a row, and the lanes that
+    // meet in a phase of the store write them in different orders (banks).
+    const bool swap = D == 128 ? piece & 4 : sub & 1;
+    const uint32_t place = (piece >> 2) * kHalf + first * 128 + (((2 * (piece & 3) + swap) ^ (first & 7)) << 4);
+    uint32_t st = 0, at = 0, n_unit = 0;  // the next tile's place; tiles made; units
     bool bad = false, bad_scale = false;
 #pragma unroll 1
     for (uint32_t n_item = 0;; ++n_item) {
@@ -743,58 +766,76 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
         if (it.stop) break;
         warp_arrive(&bars[kItemEmpty + slot]);
         const int32_t* row = a.table + (int64_t)it.r * a.ld_table;
+        const int64_t head_at = it.h * a.ld_head + 16 * piece;
         // ids of 32 blocks in the lanes, and those of the next 32
         int group = -1, ids = 0, ids_next = 0;
         auto fetch = [&](int g) {
             const int64_t key = ((int64_t)g * 32 + lane) << a.bs_log;
             return key < it.end && key + bs > it.begin ? __ldg(row + g * 32 + lane) : INT32_MIN;
         };
-        auto turn_to = [&](int key0) {
-            const int g = (key0 >> a.bs_log) >> 5;
-            if (g == group) return;
-            const int raw = group >= 0 ? ids_next : fetch(g);
-            const bool out = raw < 0 || raw >= a.n_blocks;
-            bad |= out && raw != INT32_MIN;
-            ids = out ? -1 : raw;
-            group = g;
-            ids_next = fetch(g + 1);
+        int64_t from = 0;    // of the lane's first key
+        int lo = 0, hi = 0;  // of its keys, those that are there
+        float scale = 0.0f;  // group lane & 15 of the keys' scales, or of the values'
+        auto turn_to = [&](int u) {
+            const int key0 = u * kKeys, g = (key0 >> a.bs_log) >> 5;
+            if (g != group) {
+                const int raw = group >= 0 ? ids_next : fetch(g);
+                const bool out = raw < 0 || raw >= a.n_blocks;
+                bad |= out && raw != INT32_MIN;
+                ids = out ? -1 : raw;
+                group = g;
+                ids_next = fetch(g + 1);
+            }
+            const int key = key0 + first;
+            const int id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
+            from = id * a.ld_block + (key & (bs - 1)) * a.ld_token + head_at;
+            lo = id < 0 ? kLoads : it.begin - key;
+            hi = it.end - key;
+            const int key8 = key0 + 8 * (lane & 15);
+            const int id8 = __shfl_sync(0xffffffffu, ids, (key8 >> a.bs_log) & 31);
+            scale = 0.0f;
+            if (id8 >= 0 && key8 + 8 > it.begin && key8 < it.end)
+                scale = __ldg((lane < 16 ? a.k_scale : a.v_scale) + (int64_t)id8 * a.n_kv_heads + it.h);
         };
         uint4 code[kLoads];
-        auto load = [&](int i, int u, const uint8_t* from) {  // codes of this lane's key i of tile u
-            const int key = u * kKeys + 32 * w + i * kPer + sub;
-            const int id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
+        auto load = [&](int i, const uint8_t* p) {  // codes of this lane's key i
             code[i] = make_uint4(0, 0, 0, 0);
-            if (id >= 0 && key >= it.begin && key < it.end)
-                code[i] = __ldg(reinterpret_cast<const uint4*>(from + id * a.ld_block + (key & (bs - 1)) * a.ld_token + it.h * a.ld_head) + piece);
-        };
-        float scale = 0.0f;
-        auto load_scale = [&](int u) {  // warp w: of the keys' groups 4 w .. 4 w + 3 (lanes 0 - 3), and of the values'
-            const int key = u * kKeys + 32 * w + 8 * (lane & 3);
-            const int id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
-            scale = 0.0f;
-            if (lane < 8 && id >= 0 && key + 8 > it.begin && key < it.end)
-                scale = __ldg((lane < 4 ? a.k_scale : a.v_scale) + (int64_t)id * a.n_kv_heads + it.h);
+            if (i >= lo && i < hi) code[i] = __ldg(reinterpret_cast<const uint4*>(p + from + i * a.ld_token));
         };
         // a tile that some row does not see all of
         const int64_t all1 = a.causal ? min((int64_t)it.kv, (int64_t)it.pos + 1) : it.kv;
         const int64_t all0 = a.window > 0 ? max((int64_t)0, (int64_t)it.pos + it.ntok - a.window) : 0;
-        turn_to(it.u0 * kKeys + 32 * w);
+        turn_to(it.u0);
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) load(i, it.u0, a.k8);
-        load_scale(it.u0);
+        for (int i = 0; i < kLoads; ++i) load(i, a.k8);
+        uint32_t k_times = 0, v_times = 0;  // what the lane's codes are multiplied by, twice
 #pragma unroll 1
-        for (int n = 0; n < 2 * it.nu && wait.ok; ++n) {
+        for (int n = 0; n < 2 * it.nu; ++n) {
             const bool values = n & 1;
-            const int u = it.u0 + (n >> 1), next = it.u0 + ((n + 1) >> 1);
-            const uint32_t st = at % kNS;
+            const int u = it.u0 + (n >> 1);
             if (at >= kNS) wait.warp(&bars[kKvEmpty + st], at / kNS - 1);
             if (!wait.all()) break;
-            if (!values && lane < 8) {
+            if (!values) {
                 if (!(scale >= 0.0f && scale < INFINITY)) {
                     bad_scale = true;
                     scale = 0.0f;
                 }
-                scale_s[(n_unit % kScaleRing) * 32 + (lane < 4 ? 0 : 16) + 4 * w + (lane & 3)] = scale;
+                uint32_t top = __float_as_uint(scale);
+#pragma unroll
+                for (int d = 8; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+                const uint32_t bits = __float_as_uint(scale), diff = top - bits;  // of the exponents, if the fractions are the same
+                const bool even = __all_sync(0xffffffffu, bits == 0 || ((diff & 0x7FFFFFu) == 0 && bits >= 0x800000u));
+                const int d = (int)(diff >> 23);
+                const uint32_t ratio = !even ? 22u << 10 : bits == 0 || d > 31 ? 0u : d < 22 ? (uint32_t)(22 - d) << 10 : 1u << (31 - d);  // 2^(7 - d)
+                const uint32_t rk = __shfl_sync(0xffffffffu, ratio, first >> 3), rv = __shfl_sync(0xffffffffu, ratio, 16 + (first >> 3));
+                k_times = rk | rk << 16;
+                v_times = rv | rv << 16;
+                if (w == 0) {
+                    TileScales& t = scales[n_unit % kScaleRing<D>];
+                    (lane < 16 ? t.k : t.v)[lane & 15] = scale;
+                    if (lane == 0) t.even = even;
+                    if ((lane & 15) == 0) (lane == 0 ? t.k_top : t.v_top) = __uint_as_float(top);
+                }
             }
             const bool odd = values && ((int64_t)u * kKeys < all0 || (int64_t)u * kKeys + kKeys > all1);
             if (odd) {
@@ -803,26 +844,25 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
                     code[i] = make_uint4(without_nan(code[i].x), without_nan(code[i].y), without_nan(code[i].z), without_nan(code[i].w));
             }
             const bool more = n + 1 < 2 * it.nu;
-            if (more && values) turn_to(next * kKeys + 32 * w);
-            const uint8_t* from = values ? a.k8 : a.v8;
+            if (more && values) turn_to(u + 1);
+            if (!more) lo = kLoads;
+            const uint8_t* p = values ? a.k8 : a.v8;
+            const uint32_t times = values ? v_times : k_times, to = tiles + st * Sh::kTile + place;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int key = 32 * w + i * kPer + sub;
                 const uint4 c = code[i];
-                // 16 dimensions: two 16-byte chunks of a half's row; the halves' lanes write them in different orders (banks)
-                const uint32_t at_row = tiles + st * Sh::kTile + (piece >> 2) * kHalf + key * 128, ch = 2 * (piece & 3);
-                const uint32_t lo[4] = {decode_lo(c.x), decode_hi(c.x), decode_lo(c.y), decode_hi(c.y)};
-                const uint32_t hi[4] = {decode_lo(c.z), decode_hi(c.z), decode_lo(c.w), decode_hi(c.w)};
-                const bool swap = piece & 4;
-                const uint32_t at_lo = at_row + ((ch ^ (key & 7)) << 4), at_hi = at_row + (((ch + 1) ^ (key & 7)) << 4);
-                st_shared16(swap ? at_hi : at_lo, swap ? hi[0] : lo[0], swap ? hi[1] : lo[1], swap ? hi[2] : lo[2], swap ? hi[3] : lo[3]);
-                st_shared16(swap ? at_lo : at_hi, swap ? lo[0] : hi[0], swap ? lo[1] : hi[1], swap ? lo[2] : hi[2], swap ? lo[3] : hi[3]);
-                if (more) load(i, next, from);
+                load(i, p);
+                const uint32_t x0 = swap ? c.z : c.x, x1 = swap ? c.w : c.y, y0 = swap ? c.x : c.z, y1 = swap ? c.y : c.w;
+                const uint32_t dst = (to ^ (i << 4)) + i * 128;
+                st_shared16(dst, times_half2(decode_lo(x0), times), times_half2(decode_hi(x0), times), times_half2(decode_lo(x1), times),
+                            times_half2(decode_hi(x1), times));
+                st_shared16(dst ^ 16, times_half2(decode_lo(y0), times), times_half2(decode_hi(y0), times), times_half2(decode_lo(y1), times),
+                            times_half2(decode_hi(y1), times));
             }
-            if (more && values) load_scale(next);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             warp_arrive(&bars[kKvFull + st]);
             ++at;
+            if (++st == kNS) st = 0;
             n_unit += values;
         }
         if (!wait.ok) break;
@@ -858,77 +898,26 @@ __device__ __forceinline__ void turn_queries(uint8_t* tile, int8_t* up) {
     }
 }
 
-// softmax_tile over scores of codes: group g of eight keys has the scales sc[g] (keys) and sc[16 + g] (values).  P is fp16 of
-// p sc[16 + g] / vref * 2^7, vref the largest of the values' scales so far: O is in units of vref 2^-7, and grows with it.
-template <int NCH, typename F>
-__device__ __forceinline__ void softmax_codes(uint32_t tS, int ch0, bool full, int c0, int c1, float c, bool first, bool live, float& m,
-                                              float& l, float& vref, const float* sc, F&& rescale) {
-    uint32_t x[NCH * 32];
+// What softmax_codes and its uneven form begin with: scores, -inf for the keys that the row does not see.
+template <int NCH>
+__device__ __forceinline__ void load_scores(uint32_t tS, int ch0, bool full, int c0, int c1, uint32_t* x) {
 #pragma unroll
     for (int q = 0; q < NCH; ++q) tmem_ld32(tS + 32 * (ch0 + q), x + 32 * q);
     tmem_wait_ld();
-    if (!full) {
-#pragma unroll
-        for (int q = 0; q < NCH; ++q) {
-            const int lo = min(max(c0 - 32 * (ch0 + q), 0), 32), hi = min(max(c1 - 32 * (ch0 + q), 0), 32);
-            const uint32_t bits = hi <= lo ? 0u : (0xFFFFFFFFu >> (32 - hi)) & (0xFFFFFFFFu << lo);
-            if (__all_sync(0xffffffffu, bits == 0xFFFFFFFFu)) continue;
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (!(bits & (1u << i))) x[32 * q + i] = 0xFF800000u;
-        }
-    }
-    const float4* ks = reinterpret_cast<const float4*>(sc) + ch0;
-    const float4* vs = ks + 4;
-    // (not zero, so that what is masked stays -inf; finite, so that a score of zero stays zero)
-    auto times = [&](float s) { return fminf(fmaxf(c * s, 1e-37f), 3.4e38f); };
-    float mt = -INFINITY, vmax = 0.0f;
+    if (full) return;
 #pragma unroll
     for (int q = 0; q < NCH; ++q) {
-        const float4 k4 = ks[q], v4 = vs[q];
-        const float kk[4] = {k4.x, k4.y, k4.z, k4.w};
-        vmax = fmaxf(vmax, fmaxf(fmaxf(v4.x, v4.y), fmaxf(v4.z, v4.w)));
+        const int lo = min(max(c0 - 32 * (ch0 + q), 0), 32), hi = min(max(c1 - 32 * (ch0 + q), 0), 32);
+        const uint32_t bits = hi <= lo ? 0u : (0xFFFFFFFFu >> (32 - hi)) & (0xFFFFFFFFu << lo);
+        if (__all_sync(0xffffffffu, bits == 0xFFFFFFFFu)) continue;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const uint32_t* y = x + 32 * q + 8 * g;
-            float mx[2] = {__uint_as_float(y[0]), __uint_as_float(y[1])};
-#pragma unroll
-            for (int i = 2; i < 8; ++i) mx[i & 1] = fmaxf(mx[i & 1], __uint_as_float(y[i]));
-            mt = fmaxf(mt, fmaxf(mx[0], mx[1]) * times(kk[g]));
-        }
+        for (int i = 0; i < 32; ++i)
+            if (!(bits & (1u << i))) x[32 * q + i] = 0xFF800000u;
     }
-    if (first) {
-        m = mt;
-        vref = fmaxf(vmax, 0x1p-100f);
-    } else if (__any_sync(0xffffffffu, live && mt > m + 8.0f) || vmax > vref) {
-        const float mn = fmaxf(m, mt);
-        const float f = mn == -INFINITY ? 1.0f : exp2_hw(m - mn), vn = fmaxf(vref, vmax);
-        m = mn;
-        l *= f;
-        rescale(f * (vref / vn));
-        vref = vn;
-    }
-    const float ms = finite_or_zero(m), inv = __fdividef(128.0f, vref);
-    const float2 mm = make_float2(-ms, -ms);
-    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-    for (int q = 0; q < NCH; ++q) {
-        const float4 k4 = ks[q], v4 = vs[q];
-        const float kk[4] = {k4.x, k4.y, k4.z, k4.w}, vv[4] = {v4.x, v4.y, v4.z, v4.w};
-        uint32_t p[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float ck = times(kk[i / 4]), vk = vv[i / 4] * inv;
-            const float2 s = make_float2(__uint_as_float(x[32 * q + 2 * i]), __uint_as_float(x[32 * q + 2 * i + 1]));
-            const float2 t = __ffma2_rn(s, make_float2(ck, ck), mm);
-            const float2 e = make_float2(exp2_hw(t.x), exp2_hw(t.y));
-            sum[i & 1] = __fadd2_rn(sum[i & 1], e);
-            const float2 pv = __fmul2_rn(e, make_float2(vk, vk));
-            p[i] = pack16<false>(pv.x, pv.y);
-        }
-        tmem_st16(tS + 16 * (ch0 + q), p);
-    }
-    if (NCH < 4) {
+}
+template <int NCH>
+__device__ __forceinline__ void store_zeros(uint32_t tS, int ch0) {
+    if constexpr (NCH < 4) {
         uint32_t z[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) z[i] = 0u;
@@ -936,8 +925,111 @@ __device__ __forceinline__ void softmax_codes(uint32_t tS, int ch0, bool full, i
         for (int q = 0; q < 4; ++q)
             if (q < ch0 || q >= ch0 + NCH) tmem_st16(tS + 16 * q, z);
     }
-    l += (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
+}
+// A row's scale times one of keys: not zero, so that what is masked stays -inf; finite, so that a score of zero stays zero.
+__device__ __forceinline__ float score_scale(float c, float s) { return fminf(fmaxf(c * s, 1e-37f), 3.4e38f); }
+
+// A row's state between tiles: O is in units of vref 2^-14, vref the largest of the values' scales so far.
+struct RowState {
+    float m, l, vref;
+    // The factor of O for a tile whose largest score is mt, and whose values' largest scale vt; 1 if it stays as it is.
+    // (vt is the same for a warp, and what is returned other than 1 for one lane is a rescaling for all.)
+    __device__ __forceinline__ bool grow(float mt, float vt, bool first, bool live, float& f) {
+        if (first) {
+            m = mt;
+            vref = fmaxf(vt, 0x1p-100f);
+            return false;
+        }
+        if (!__any_sync(0xffffffffu, live && mt > m + 8.0f) && !(vt > vref)) return false;
+        const float mn = fmaxf(m, mt), vn = fmaxf(vref, vt);
+        f = mn == -INFINITY ? 1.0f : exp2_hw(m - mn);
+        m = mn;
+        l *= f;
+        f *= vref / vn;
+        vref = vn;
+        return true;
+    }
+};
+
+// softmax_tile over scores of codes: keys' codes in units of t.k_top, values' in units of t.v_top.  P is fp16 of
+// p v_top / vref * 2^7 (below 2^15), the factor, 2^-17 at least, going into the exponent.
+template <int NCH, typename F>
+__device__ __forceinline__ void softmax_codes(uint32_t tS, int ch0, bool full, int c0, int c1, float c, bool first, bool live, RowState& s,
+                                              const TileScales& t, F&& rescale) {
+    uint32_t x[NCH * 32];
+    load_scores<NCH>(tS, ch0, full, c0, c1, x);
+    const float ck = score_scale(c, t.k_top), vt = t.v_top;
+    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, f;
+#pragma unroll
+    for (int i = 0; i < NCH * 32; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(x[i]));
+    if (s.grow(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * ck, vt, first, live, f)) rescale(f);
+    const float factor = __fdividef(vt, s.vref) * 128.0f;
+    const float ms = __log2f(factor) - finite_or_zero(s.m);
+    const float2 cc = make_float2(ck, ck), mm = make_float2(ms, ms);
+    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+    for (int q = 0; q < NCH; ++q) {
+        uint32_t p[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float2 y = make_float2(__uint_as_float(x[32 * q + 2 * i]), __uint_as_float(x[32 * q + 2 * i + 1]));
+            const float2 z = __ffma2_rn(y, cc, mm);
+            const float2 e = make_float2(exp2_hw(z.x), exp2_hw(z.y));
+            sum[i & 1] = __fadd2_rn(sum[i & 1], e);
+            p[i] = pack16<false>(e.x, e.y);
+        }
+        tmem_st16(tS + 16 * (ch0 + q), p);
+    }
+    store_zeros<NCH>(tS, ch0);
+    s.l += __fdividef((sum[0].x + sum[1].x) + (sum[0].y + sum[1].y), factor);
     tmem_wait_st();
+}
+
+// The same where the groups' scales differ by more than powers of two, or where the values' are nothing beside those gone by
+// (as an exponent's part, so small a factor would cost the scores' last places), n chunks of 32 columns from ch0 on, one at a
+// time: the row's largest score and the largest scale of values, then P and its sum.
+__device__ __noinline__ float2 uneven_max(uint32_t tS, int ch0, int n, bool full, int c0, int c1, float c, const TileScales& t) {
+    float mt = -INFINITY, vt = 0.0f;
+    uint32_t x[32];
+#pragma unroll 1
+    for (int q = ch0; q < ch0 + n; ++q) {
+        load_scores<1>(tS, q, full, c0, c1, x);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            float mx = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mx = fmaxf(mx, __uint_as_float(x[8 * g + i]));
+            mt = fmaxf(mt, mx * score_scale(c, t.even ? t.k_top : t.k[4 * q + g]));
+            vt = fmaxf(vt, t.even ? t.v_top : t.v[4 * q + g]);
+        }
+    }
+    return make_float2(mt, vt);
+}
+__device__ __noinline__ float uneven_p(uint32_t tS, int ch0, int n, bool full, int c0, int c1, float c, float m, float vref, const TileScales& t) {
+    const float ms = finite_or_zero(m), inv = __fdividef(128.0f, vref);
+    float sum = 0.0f;
+    uint32_t x[32];
+#pragma unroll 1
+    for (int q = 0; q < 4; ++q) {  // (P is half as wide as the scores: what it is written over has been read)
+        uint32_t p[16];
+        if (q < ch0 || q >= ch0 + n) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[i] = 0u;
+        } else {
+            load_scores<1>(tS, q, full, c0, c1, x);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int g = 4 * q + i / 4;
+                const float ck = score_scale(c, t.even ? t.k_top : t.k[g]), vk = (t.even ? t.v_top : t.v[g]) * inv;
+                const float e0 = exp2_hw(fmaf(__uint_as_float(x[2 * i]), ck, -ms)), e1 = exp2_hw(fmaf(__uint_as_float(x[2 * i + 1]), ck, -ms));
+                sum += e0 + e1;
+                p[i] = pack16<false>(e0 * vk, e1 * vk);
+            }
+        }
+        tmem_st16(tS + 16 * q, p);
+        tmem_wait_st();
+    }
+    return sum;
 }
 
 template <bool kBf16, int D, bool k8>
@@ -958,7 +1050,7 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
     __shared__ int last_flag[2];
     // m and l of copies; with codes in the scratch (there is no more shared memory to be had), and a ring of tiles' scales
     __shared__ float2 ml_own[k8 ? 1 : 2][k8 ? 1 : kRows];
-    __shared__ __align__(16) float scale_s[k8 ? kScaleRing : 1][k8 ? 32 : 1];
+    __shared__ TileScales scale_s[k8 ? kScaleRing<D> : 1];
     __shared__ int8_t up_s[kTurn ? 2 * kUpRing : 1][kTurn ? kRows : 1];
     // (the same for all lanes, and by the shuffle known to be)
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -1033,7 +1125,7 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
 
     if (k8 && warp >= kCodeWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCodeRegs));
-        if constexpr (k8) code_tiles<D>(a, bars, items, smem_u32(sKV), &scale_s[0][0], wait);
+        if constexpr (k8) code_tiles<D>(a, bars, items, smem_u32(sKV), scale_s, wait);
     } else if (warp >= kMmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs<k8>));
         if (warp == kLoadWarp) {
@@ -1441,8 +1533,9 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
             }
             const int all1 = a.causal ? min(it.kv, it.pos + tok0 + 1) : it.kv;
             const int all0 = a.window > 0 ? (int)max((int64_t)0, (int64_t)it.pos + tok0 + ntok - a.window) : 0;
-            float m = -INFINITY, l = 0.0f;
-            float c_row = a.scale_log2, vref = 0x1p-100f;  // with codes: scale of the row's scores; O is in units of vref 2^-7
+            RowState state{-INFINITY, 0.0f, 0x1p-100f};
+            float &m = state.m, &l = state.l;
+            float c_row = a.scale_log2 * 0x1p-7f;  // with codes: scale of the row's scores, whose keys are up by 2^7
             const uint32_t step = it.slot == 2 ? 2 : 1;
             uint32_t b = (buf + (it.slot == 2 ? s : 0)) % Sh::kBuf;
             buf = (buf + step * it.nu) % Sh::kBuf;
@@ -1474,13 +1567,19 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
                         }
                     };
                     if constexpr (k8) {
-                        const float* sc = scale_s[n_unit % kScaleRing];
-                        if (it.rep_log == 0)
-                            softmax_codes<4>(tS, 0, full, k0 - t0, k1 - t0, c_row, u == 0, live, m, l, vref, sc, rescale);
+                        const TileScales& t = scale_s[n_unit % kScaleRing<D>];
+                        if (!t.even || t.v_top < state.vref * 0x1p-24f) {
+                            const int nch = 4 >> it.rep_log, ch0 = copy * nch;
+                            const float2 most = uneven_max(tS, ch0, nch, full, k0 - t0, k1 - t0, c_row, t);
+                            float f;
+                            if (state.grow(most.x, most.y, u == 0, live, f)) rescale(f);
+                            state.l += uneven_p(tS, ch0, nch, full, k0 - t0, k1 - t0, c_row, state.m, state.vref, t);
+                        } else if (it.rep_log == 0)
+                            softmax_codes<4>(tS, 0, full, k0 - t0, k1 - t0, c_row, u == 0, live, state, t, rescale);
                         else if (it.rep_log == 1)
-                            softmax_codes<2>(tS, 2 * copy, full, k0 - t0, k1 - t0, c_row, u == 0, live, m, l, vref, sc, rescale);
+                            softmax_codes<2>(tS, 2 * copy, full, k0 - t0, k1 - t0, c_row, u == 0, live, state, t, rescale);
                         else
-                            softmax_codes<1>(tS, copy, full, k0 - t0, k1 - t0, c_row, u == 0, live, m, l, vref, sc, rescale);
+                            softmax_codes<1>(tS, copy, full, k0 - t0, k1 - t0, c_row, u == 0, live, state, t, rescale);
                     } else if (it.rep_log == 0)
                         softmax_tile<kBf16, 4>(tS, 0, full, k0 - t0, k1 - t0, a.scale_log2, u == 0, live, m, l, rescale);
                     else if (it.rep_log == 1)
@@ -1549,7 +1648,7 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]);
             };
-            const float unit_o = k8 ? vref * 0x1p-7f : 1.0f;
+            const float unit_o = k8 ? state.vref * 0x1p-14f : 1.0f;  // (P and the values are up by 2^7 each)
             const int head = it.h * a.group, tok = it.tok + tok0;
             const bool whole = it.n_parts == 1;
             // parts of half 0, then those of half 1, of all CTAs
