@@ -80,16 +80,17 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
-// Two codes as fp16 (exact).
+// Two codes of a word as fp16 (exact).
 __device__ __forceinline__ uint32_t decode_lo(uint32_t w) {
     uint32_t r;
     asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(w));
     return r;
 }
-__device__ __forceinline__ uint32_t decode_hi(uint32_t w) {
-    uint32_t r;
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
-    return r;
+__device__ __forceinline__ uint32_t decode_hi(uint32_t w) { return decode_lo(w >> 16); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 // The codes that the format reserves for NaN as 448.
 __device__ __forceinline__ uint32_t without_nan(uint32_t w) {
@@ -101,7 +102,10 @@ __device__ __forceinline__ void mma(float* d, const uint32_t* a, uint32_t b0, ui
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {  // or zeros
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
@@ -118,14 +122,16 @@ __device__ __forceinline__ void lds(uint32_t addr, uint32_t* w) {
     else asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr));
 }
 
-// Where piece j (16 bytes) of a tile's row lies: the lanes of a load's phase find theirs on different banks.
+// Where piece j (16 bytes) of key row + i of a tile lies, i below the number of keys that a lane copies: the lanes of a load's
+// phase find theirs on different banks.
 template <int D>
-__device__ __forceinline__ uint32_t key_at(int row, int j) {
-    return D == 128 ? row * 128 + ((j ^ ((row & 1) << 2)) << 4) : row * 64 + (j << 4);
+__device__ __forceinline__ uint32_t key_at(int row, int j, int i = 0) {
+    return D == 128 ? row * 128 + i * 128 + ((j ^ ((row & 1) << 2) ^ ((i & 1) << 2)) << 4) : row * 64 + i * 64 + (j << 4);
 }
 template <int D>
-__device__ __forceinline__ uint32_t value_at(int row, int j) {
-    return D == 128 ? row * 128 + ((j ^ (row & 6)) << 4) : (row >> 1) * 128 + (((((row & 1) << 2) + j) ^ (row & 6)) << 4);
+__device__ __forceinline__ uint32_t value_at(int row, int j, int i = 0) {
+    return D == 128 ? row * 128 + i * 128 + ((j ^ (row & 6) ^ (i & 6)) << 4)
+                    : (row >> 1) * 128 + (i >> 1) * 128 + ((j ^ ((row & 1) << 2) ^ (row & 6) ^ ((i & 1) << 2) ^ (i & 6)) << 4);
 }
 
 struct Req {
@@ -329,6 +335,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
         p = at;
     }
 
+    constexpr int kCopies = D / 16;
+    const int piece = lane % kPieces, first = lane / kPieces * kCopies;
     const uint32_t ring = scoot_dev::smem_u32(smem) + warp * Sh::kStages * Sh::kStage;
     bool bad_id = false, bad_scale = false;
     while (p < B1) {
@@ -373,44 +381,67 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
         // ---- copies: the ids of 32 blocks are in the lanes, those of the next 32 on their way
         const int32_t* row_ids = a.table + (int64_t)it.r * a.ld_table;
         const int bs = 1 << a.bs_log;
+        const int64_t head_at = it.h * a.ld_head + 16 * piece;
         auto fetch = [&](int group) {
             const int64_t key = ((int64_t)group * 32 + lane) << a.bs_log;
             return key < it.end && key + bs > it.begin ? __ldg(row_ids + group * 32 + lane) : INT32_MIN;
         };
         int group = -1, ids = 0, ids_next = 0;
+        bool lacks = false;  // some id of the group is bad, or its block not wanted
         auto use = [&](int raw) {
             const bool out = raw < 0 || raw >= a.n_blocks;
             bad_id |= out && raw != INT32_MIN;
             ids = out ? -1 : raw;
+            lacks = __any_sync(0xffffffffu, bad_id);
         };
-        auto load = [&](int u, int stage) {  // tile u of the sequence
-            const int key0 = u * kKeys, b0 = key0 >> a.bs_log;
+        // A lane copies piece `piece` of kCopies keys in a row, which lie in one block.  Where they are is found a tile ahead.
+        int id = 0;
+        int64_t at = 0;
+        auto find = [&](int u) {
+            const int b0 = u * kKeys >> a.bs_log;
             if (b0 >> 5 != group) {
                 use(group >= 0 ? ids_next : fetch(b0 >> 5));
                 group = b0 >> 5;
                 ids_next = fetch(group + 1);
             }
+            const int key = u * kKeys + first;
+            id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
+            at = id * a.ld_block + (key & (bs - 1)) * a.ld_token + head_at;
+        };
+        auto load = [&](int u, int stage, bool more) {  // tile u of the sequence
+            const int key0 = u * kKeys, key = key0 + first;
             const uint32_t dst = ring + stage * Sh::kStage;
+            const uint8_t *pk = a.k + at, *pv = a.v + at;
+            const bool in = piece < 2 && (first & 7) == 0, there8 = id >= 0 && key + 8 > it.begin && key < it.end;
+            const float* scale_at = (piece == 0 ? a.k_scale : a.v_scale) + (there8 ? (int64_t)id * a.n_kv_heads + it.h : 0);
+            if (!lacks && key0 >= it.begin && key0 + kKeys <= it.end) {
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const int e = i * 32 + lane, row = e / kPieces, piece = e % kPieces, key = key0 + row;
-                const int id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
-                const bool there = id >= 0 && key >= it.begin && key < it.end;
-                const int64_t at = there ? id * a.ld_block + (key & (bs - 1)) * a.ld_token + it.h * a.ld_head + piece * 16 : 0;
-                copy16(dst + key_at<D>(row, piece), a.k + at, there);
-                copy16(dst + Sh::kTile + value_at<D>(row, piece), a.v + at, there);
+                for (int i = 0; i < kCopies; ++i) {
+                    copy16(dst + key_at<D>(first, piece, i), pk);
+                    copy16(dst + Sh::kTile + value_at<D>(first, piece, i), pv);
+                    pk += a.ld_token;
+                    pv += a.ld_token;
+                }
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < kCopies; ++i) {
+                    const bool there = id >= 0 && key + i >= it.begin && key + i < it.end;
+                    copy16(dst + key_at<D>(first, piece, i), there ? pk : a.k, there);
+                    copy16(dst + Sh::kTile + value_at<D>(first, piece, i), there ? pv : a.v, there);
+                    pk += a.ld_token;
+                    pv += a.ld_token;
+                }
             }
-            const int key = key0 + 8 * (lane & 3);
-            const int id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
-            if (lane < 8) {
-                const bool there = id >= 0 && key + 8 > it.begin && key < it.end;
-                copy4(dst + 2 * Sh::kTile + 4 * lane, (lane < 4 ? a.k_scale : a.v_scale) + (there ? (int64_t)id * a.n_kv_heads + it.h : 0), there);
-            }
+            if (in) copy4(dst + 2 * Sh::kTile + 16 * piece + first / 2, scale_at, there8);  // of a group of eight keys
+            if (more) find(u + 1);
         };
         const int u0 = tile0 + lo, u1 = tile0 + hi;
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < Sh::kStages - 1; ++i) {
-            if (u0 + i < u1) load(u0 + i, i);
+            if (u0 + i < u1) {
+                if (i == 0) find(u0);
+                load(u0 + i, i, u0 + i + 1 < u1);
+            }
             copies_end();
         }
 
@@ -418,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
         uint32_t qa[kSteps][4];
         float c_row[2];       // scale of the row's scores, to log2
         int k0[2], k1[2];     // keys that the row sees
-        bool same = true;     // all rows see the same keys
+        int all0 = it.begin, all1 = it.end;  // keys that all rows see
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int row = g + 8 * i, t = row / it.heads;
@@ -426,7 +457,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
             const int pos = it.pos + t;
             k1[i] = live ? (a.causal ? min(it.kv, pos + 1) : it.kv) : 0;
             k0[i] = live && a.window > 0 ? (int)max((int64_t)0, (int64_t)pos + 1 - a.window) : 0;
-            same &= !live || (k1[i] >= it.end && k0[i] <= it.begin);
+            if (live) {
+                all0 = max(all0, k0[i]);
+                all1 = min(all1, k1[i]);
+            }
             const uint16_t* src = a.q + (int64_t)(it.tok + t) * a.q_ld_token + (int64_t)(it.head + row - t * it.heads) * a.q_ld_head;
             uint32_t w[kSteps][2];
 #pragma unroll
@@ -463,7 +497,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
                 qa[s][i + 2] = w[s][1];
             }
         }
-        same = __all_sync(0xffffffffu, same);
+        all0 = __reduce_max_sync(0xffffffffu, all0);
+        all1 = __reduce_min_sync(0xffffffffu, all1);
+        const bool large = __any_sync(0xffffffffu, c_row[0] > 1.0f || c_row[1] > 1.0f);  // a product with a scale may pass fp32
 
         float o[kCols][4];
 #pragma unroll
@@ -471,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[t][e] = 0.0f;
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-        float vref = 0x1p-100f;
+        float vref = 0x1p-100f, inv_ref = 0.0f;
         auto scale_o = [&](float f0, float f1) {
 #pragma unroll
             for (int t = 0; t < kCols; ++t) {
@@ -486,58 +522,73 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
         for (int u = u0; u < u1; ++u) {
             copies_wait<Sh::kStages - 2>();
             __syncwarp();
-            if (u + Sh::kStages - 1 < u1) load(u + Sh::kStages - 1, stage == 0 ? Sh::kStages - 1 : stage - 1);
+            if (u + Sh::kStages - 1 < u1) load(u + Sh::kStages - 1, stage == 0 ? Sh::kStages - 1 : stage - 1, u + Sh::kStages < u1);
             copies_end();
             const uint32_t st = ring + stage * Sh::kStage;
             if (++stage == Sh::kStages) stage = 0;
-            float ks[4], vs[4];
-            lds<4>(st + 2 * Sh::kTile, reinterpret_cast<uint32_t*>(ks));
-            lds<4>(st + 2 * Sh::kTile + 16, reinterpret_cast<uint32_t*>(vs));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const bool kb = !(ks[i] >= 0.0f && ks[i] < INFINITY), vb = !(vs[i] >= 0.0f && vs[i] < INFINITY);
-                bad_scale |= kb || vb;
-                if (kb) ks[i] = 0.0f;
-                if (vb) vs[i] = 0.0f;
+            uint32_t ks[4], vs[4];
+            lds<4>(st + 2 * Sh::kTile, ks);
+            lds<4>(st + 2 * Sh::kTile + 16, vs);
+            if (lane < 8) {
+                float own;
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(own) : "r"(st + 2 * Sh::kTile + 4 * lane));
+                bad_scale |= !(own >= 0.0f && own < INFINITY);
             }
             // scores
             float x[4][4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 x[t][0] = x[t][1] = x[t][2] = x[t][3] = 0.0f;
-#pragma unroll
-                for (int half = 0; half < D / 64; ++half) {
-                    uint32_t w[4];
-                    lds<4>(st + key_at<D>(8 * t + g, c + 4 * half), w);
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) mma(x[t], qa[4 * half + s], decode_lo(w[s]), decode_hi(w[s]));
-                }
+                // (as bits: what is not finite, or negative, is above the others)
+                if (ks[t] >= 0x7F800000u) ks[t] = 0u;
+                if (vs[t] >= 0x7F800000u) vs[t] = 0u;
             }
-            const int key0 = u * kKeys + 2 * c;
-            const bool full = same && u * kKeys >= it.begin && (u + 1) * kKeys <= it.end;
-            float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                // (finite: a score of zero stays zero)
-                const float ck[2] = {fminf(c_row[0] * ks[t], FLT_MAX), fminf(c_row[1] * ks[t], FLT_MAX)};
+            for (int half = 0; half < D / 64; ++half) {
+                uint32_t w[4][4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = e >> 1, key = key0 + 8 * t + (e & 1);
-                    float s = x[t][e] * ck[i];
-                    if (!full && (key < k0[i] || key >= k1[i])) s = -INFINITY;
-                    x[t][e] = s;
-                    mx[i] = fmaxf(mx[i], s);
-                }
+                for (int t = 0; t < 4; ++t) lds<4>(st + key_at<D>(8 * t + g, c + 4 * half), w[t]);
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) mma(x[t], qa[4 * half + s], decode_lo(w[t][s]), decode_hi(w[t][s]));
             }
+            float ck[4][2];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) ck[t][i] = c_row[i] * __uint_as_float(ks[t]);
+            const bool partial = u * kKeys < all0 || (u + 1) * kKeys > all1;
+            if (partial || large) {
+                const int key0 = u * kKeys + 2 * c;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = e >> 1, key = key0 + 8 * t + (e & 1);
+                        if (key < k0[i] || key >= k1[i]) x[t][e] = -INFINITY;
+                        // (not zero, so that what is masked stays -inf; finite, so that a score of zero stays zero)
+                        ck[t][i] = fminf(fmaxf(ck[t][i], 1e-37f), FLT_MAX);
+                    }
+            }
+            float mx[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
+                float y[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) y[t] = fmaxf(x[t][2 * i], x[t][2 * i + 1]) * ck[t][i];
+                mx[i] = fmaxf(max3(y[0], y[1], y[2]), y[3]);
                 mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
                 mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
             }
+            const float vmax = fmaxf(max3(__uint_as_float(vs[0]), __uint_as_float(vs[1]), __uint_as_float(vs[2])), __uint_as_float(vs[3]));
             if (u == u0) {
                 m[0] = mx[0];
                 m[1] = mx[1];
-            } else if (__any_sync(0xffffffffu, mx[0] > m[0] + 8.0f || mx[1] > m[1] + 8.0f)) {
+                vref = fmaxf(vmax, 0x1p-100f);
+                inv_ref = 128.0f / vref;
+            } else if (__any_sync(0xffffffffu, mx[0] > m[0] + 8.0f || mx[1] > m[1] + 8.0f) || vmax > vref) {
+                const float vn = fmaxf(vref, vmax);
                 float f[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -546,26 +597,27 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
                     m[i] = mn;
                     l[i] *= f[i];
                 }
-                scale_o(f[0], f[1]);
+                scale_o(f[0] * (vref / vn), f[1] * (vref / vn));
+                vref = vn;
+                inv_ref = 128.0f / vref;
             }
-            const float vmax = fmaxf(fmaxf(vs[0], vs[1]), fmaxf(vs[2], vs[3]));
-            if (vmax > vref) {  // (the same for all lanes)
-                const float f = vref / vmax;
-                scale_o(f, f);
-                vref = vmax;
-            }
-            const float inv_ref = 128.0f / vref, ms[2] = {finite_or_zero(m[0]), finite_or_zero(m[1])};
+            const float ms[2] = {-finite_or_zero(m[0]), -finite_or_zero(m[1])};
             uint32_t pa[2][4];
+            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const float f = vs[t] * inv_ref;
+                const float f = __uint_as_float(vs[t]) * inv_ref;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const float e0 = exp2_hw(x[t][2 * i] - ms[i]), e1 = exp2_hw(x[t][2 * i + 1] - ms[i]);
-                    l[i] += e0 + e1;
-                    pa[t >> 1][2 * (t & 1) + i] = half2_bits(e0 * f, e1 * f);
+                    const float2 z = __ffma2_rn(make_float2(x[t][2 * i], x[t][2 * i + 1]), make_float2(ck[t][i], ck[t][i]), make_float2(ms[i], ms[i]));
+                    const float2 e = make_float2(exp2_hw(z.x), exp2_hw(z.y));
+                    sum[i] = __fadd2_rn(sum[i], e);
+                    const float2 pf = __fmul2_rn(e, make_float2(f, f));
+                    pa[t >> 1][2 * (t & 1) + i] = half2_bits(pf.x, pf.y);
                 }
             }
+            l[0] += sum[0].x + sum[0].y;
+            l[1] += sum[1].x + sum[1].y;
             // values
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
@@ -576,7 +628,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
                     const int row = 16 * kk + 2 * c + (i & 1) + 8 * (i >> 1);
                     if (D == 128) lds<kW>(st + Sh::kTile + value_at<D>(row, g), w[i]);
                     else lds<kW>(st + Sh::kTile + value_at<D>(row, g >> 1) + 8 * (g & 1), w[i]);
-                    if (!same) {  // (a value that some row does not see, times its zero)
+                    if (partial) {  // (a value that some row does not see, times its zero)
 #pragma unroll
                         for (int e = 0; e < kW; ++e) w[i][e] = without_nan(w[i][e]);
                     }
