@@ -1829,6 +1829,17 @@ bool encode_queries(AttnArgs& a, bool bf16, int D, int G, int n_heads, int64_t n
 
 }  // namespace
 
+bool scoot_encode_codes(CUtensorMap* map, const scoot_kv_layout* L, const void* cache, int tokens) {
+    if (!encode_tiled()) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)L->head_dim, (cuuint64_t)L->n_kv_heads, (cuuint64_t)L->block_size, (cuuint64_t)L->n_blocks};
+    const cuuint64_t strides[3] = {(cuuint64_t)L->ld_head, (cuuint64_t)L->ld_token, (cuuint64_t)L->ld_block};
+    const cuuint32_t box[4] = {(cuuint32_t)L->head_dim, 1, (cuuint32_t)std::min(L->block_size, tokens), 1}, step[4] = {1, 1, 1, 1};
+    // (no wider reads than asked for: rows of other heads lie between)
+    return encode_tiled()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(cache), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          L->head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 size_t scoot_attn8_tile_bytes(int head_dim) { return (size_t)kBufs * kRows * (head_dim + 2) * sizeof(float); }
 
 scoot_status scoot_attn8_tiles(scoot_ctx* ctx, const scoot_kv_layout* layout, const Attn8Args& args, bool bf16, int sms, cudaStream_t st) {

@@ -11,7 +11,7 @@
 // power of two of their row so that the largest is below 2^15: what that rounds is below 2^-39 of the row's largest.
 //
 // Dimensions and keys are dealt to the operands' places as the loads want them.  Q K^T: lane (g, c) = (lane / 4, lane % 4) has
-// key g and of it the 16-byte pieces c and c + 4, four dimensions per step, and the same ones of its query rows.  P V: column g
+// key g and of it 32 (16) dimensions in a row, four per step, and the same ones of its query rows.  P V: column g
 // of product t is dimension g D / 8 + t, so that a lane reads whole pieces of four keys' values, and has 32 (16) consecutive
 // dimensions of the result.
 //
@@ -23,11 +23,13 @@
 // warp each (a cut close to an item's start or end moves there).  Warps of a block take neighbouring ranges.  An item that
 // lies in several leaves its parts (O, m, l) in the workspace; at the end of a block its warps join the block's parts of
 // each item, and of an item that lies in several blocks the last block joins those, in the ranges' order.
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 #include "mbarrier.cuh"
 #include "paged_attn8.cuh"
@@ -47,10 +49,16 @@ constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
 template <int D>
 struct Shape {
     static constexpr int kTile = kKeys * D;              // bytes of a tile's keys, or values
-    static constexpr int kStage = 2 * kTile + 64;        // and the scales of its four groups of eight
+    static constexpr int kStage = 2 * kTile;
     static constexpr int kStages = D == 128 ? 3 : 6;
-    static constexpr int kSmem = kWarps * kStages * kStage;
+    static constexpr int kScales = kWarps * kStages * kStage;     // after the warps' rings those of their tiles' scales: 64 bytes each
+    static constexpr int kSmem = kScales + kWarps * kStages * 64;
     static constexpr int kPart = kRows * (D + 2);        // floats of a part: O, then (m, l) of each row
+};
+
+// Boxes of up to 32 tokens of a block and head.
+struct KvMaps {
+    CUtensorMap k, v;
 };
 
 struct Item {
@@ -102,12 +110,6 @@ __device__ __forceinline__ void mma(float* d, const uint32_t* a, uint32_t b0, ui
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {  // or zeros
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, bool there) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
@@ -122,16 +124,10 @@ __device__ __forceinline__ void lds(uint32_t addr, uint32_t* w) {
     else asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr));
 }
 
-// Where piece j (16 bytes) of key row + i of a tile lies, i below the number of keys that a lane copies: the lanes of a load's
-// phase find theirs on different banks.
+// Where piece j (16 bytes) of key `row` of a tile lies (the copies' swizzle of 128 or 64 bytes).
 template <int D>
-__device__ __forceinline__ uint32_t key_at(int row, int j, int i = 0) {
-    return D == 128 ? row * 128 + i * 128 + ((j ^ ((row & 1) << 2) ^ ((i & 1) << 2)) << 4) : row * 64 + i * 64 + (j << 4);
-}
-template <int D>
-__device__ __forceinline__ uint32_t value_at(int row, int j, int i = 0) {
-    return D == 128 ? row * 128 + i * 128 + ((j ^ (row & 6) ^ (i & 6)) << 4)
-                    : (row >> 1) * 128 + (i >> 1) * 128 + ((j ^ ((row & 1) << 2) ^ (row & 6) ^ ((i & 1) << 2) ^ (i & 6)) << 4);
+__device__ __forceinline__ uint32_t piece_at(int row, int j) {
+    return D == 128 ? row * 128 + ((j ^ (row & 7)) << 4) : row * 64 + ((j ^ ((row >> 1) & 3)) << 4);
 }
 
 struct Req {
@@ -190,64 +186,75 @@ __device__ __forceinline__ float* lse_row(const Attn8Args& a, const Item& it, in
     return a.lse + (int64_t)(it.tok + t) * a.n_heads + it.head + q - t * it.heads;
 }
 
-// n parts joined by the whole block: part i is at part(i).  out: the item's rows (final), or a part again (to != NULL).
+// Four columns (at: in groups of four) of row q of n parts, joined: part i is at part(i).  The item's row (final), or that of a
+// part again (to != NULL).
 template <bool kBf16, int D, typename F>
-__device__ __forceinline__ void join(const Attn8Args& a, const Item& it, int n, float* to, F&& part) {
-    constexpr int kQuads = D / 4;
-    for (int e = threadIdx.x; e < it.rows * kQuads; e += kThreads) {
-        const int q = e / kQuads, c = e % kQuads;
-        float M = -INFINITY, L = 0.0f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int i0 = 0; i0 < n; i0 += 4) {
-            float2 ml[4];
-            float4 v[4];
+__device__ __forceinline__ void join(const Attn8Args& a, const Item& it, int q, int c, int n, float* to, F&& part) {
+    constexpr int kAtOnce = 8;
+    float M = -INFINITY, L = 0.0f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += kAtOnce) {
+        float2 ml[kAtOnce];
+        float4 v[kAtOnce];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float* p = part(min(i0 + i, n - 1));
+        for (int i = 0; i < kAtOnce; ++i) {
+            ml[i] = make_float2(-INFINITY, 0.0f);
+            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i0 + i < n) {
+                const float* p = part(i0 + i);
                 ml[i] = __ldcg(reinterpret_cast<const float2*>(p + kRows * D) + q);
                 v[i] = __ldcg(reinterpret_cast<const float4*>(p + q * D) + c);
-                if (i0 + i >= n) {
-                    ml[i] = make_float2(-INFINITY, 0.0f);
-                    v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                }
             }
-            const float Mn = fmaxf(fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), M), Ms = finite_or_zero(Mn);
-            const float f = exp2_hw(M - Ms);
-            L *= f;
-            o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
-            M = Mn;
+        }
+        float Mn = M;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float w = exp2_hw(ml[i].x - Ms);
-                L = fmaf(w, ml[i].y, L);
-                o = make_float4(fmaf(w, v[i].x, o.x), fmaf(w, v[i].y, o.y), fmaf(w, v[i].z, o.z), fmaf(w, v[i].w, o.w));
-            }
+        for (int i = 0; i < kAtOnce; ++i) Mn = fmaxf(Mn, ml[i].x);
+        const float Ms = finite_or_zero(Mn), f = exp2_hw(M - Ms);
+        L *= f;
+        o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
+        M = Mn;
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const float w = exp2_hw(ml[i].x - Ms);
+            L = fmaf(w, ml[i].y, L);
+            o = make_float4(fmaf(w, v[i].x, o.x), fmaf(w, v[i].y, o.y), fmaf(w, v[i].z, o.z), fmaf(w, v[i].w, o.w));
         }
-        if (to) {
-            reinterpret_cast<float4*>(to + q * D)[c] = o;
-            if (c == 0) reinterpret_cast<float2*>(to + kRows * D)[q] = make_float2(M, L);
-        } else {
-            const float inv = inverse_sum(L);
-            *reinterpret_cast<uint2*>(out_row(a, it, q) + 4 * c) = make_uint2(pack16<kBf16>(o.x * inv, o.y * inv), pack16<kBf16>(o.z * inv, o.w * inv));
-            if (c == 0 && a.lse) *lse_row(a, it, q) = L == 0.0f ? -INFINITY : (M + __log2f(L)) * kLn2;
-        }
+    }
+    if (to) {
+        reinterpret_cast<float4*>(to + q * D)[c] = o;
+        if (c == 0) reinterpret_cast<float2*>(to + kRows * D)[q] = make_float2(M, L);
+    } else {
+        const float inv = inverse_sum(L);
+        *reinterpret_cast<uint2*>(out_row(a, it, q) + 4 * c) = make_uint2(pack16<kBf16>(o.x * inv, o.y * inv), pack16<kBf16>(o.z * inv, o.w * inv));
+        if (c == 0 && a.lse) *lse_row(a, it, q) = L == 0.0f ? -INFINITY : (M + __log2f(L)) * kLn2;
     }
 }
 
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 template <bool kBf16, int D>
-__global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args a) {
+__global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ KvMaps maps) {
     using Sh = Shape<D>;
-    constexpr int kSteps = D / 16, kPieces = D / 16, kCols = D / 8;
-    extern __shared__ __align__(128) uint8_t smem[];
+    constexpr int kSteps = D / 16, kCols = D / 8;
+    extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int64_t cost_s[kThreads];
     __shared__ Item items[kWarps + 1];  // of the block's split items: one that came in, and one that begins with each warp's last
-    __shared__ int last_s[2];
+    __shared__ int last_s[2], failed;
+    __shared__ __align__(8) uint64_t bars[kWarps * Sh::kStages];
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int g = lane >> 2, c = lane & 3;
 
     // The cost of all items: each thread k consecutive requests, then a scan.
     const int k = (a.n_req + kThreads - 1) / kThreads;
     if (tid <= kWarps) items[tid].n_parts = 0;
+    if (tid == 0) failed = 0;
+    if (tid < kWarps * Sh::kStages) scoot_dev::mbar_init(&bars[tid], 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     int64_t mine = 0;
 #pragma unroll 1
     for (int i = 0; i < k; ++i) {
@@ -304,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
         r = (w * 32 + t) * k;
         while (r < a.n_req) {
             const Req q = get(r);
-            const int64_t one = q.n > 0 ? head_cost(a, q.kv, q.n) : 0;
+            const int64_t one = q.n == 0 ? 0 : item_count(a, q.n) == 1 ? item_cost(a, q.kv, q.n, 0) : head_cost(a, q.kv, q.n);
             if (at + one * a.n_kv_heads > B0) {
                 h = (int)quotient(B0 - at, one);
                 at += h * one;
@@ -315,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
         }
         const Req q = get(min(r, a.n_req - 1));
         const int m = item_count(a, q.n);
-        for (int j0 = 0; j0 < m; j0 += 32) {
+        for (int j0 = 0; m > 1 && j0 < m; j0 += 32) {
             const int64_t cost = j0 + lane < m ? item_cost(a, q.kv, q.n, j0 + lane) : 0;
             int64_t s = cost;
 #pragma unroll
@@ -335,11 +342,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
         p = at;
     }
 
-    constexpr int kCopies = D / 16;
-    const int piece = lane % kPieces, first = lane / kPieces * kCopies;
     const uint32_t ring = scoot_dev::smem_u32(smem) + warp * Sh::kStages * Sh::kStage;
+    const uint32_t ring_scales = scoot_dev::smem_u32(smem) + Sh::kScales + warp * Sh::kStages * 64;
+    const uint32_t bar0 = scoot_dev::smem_u32(&bars[warp * Sh::kStages]);
+    const bool one_lane = elect_one();
+    uint32_t to_load = 0, stage = 0, phase = 0;  // places in the ring: of the next load, and of the next tile with its barrier's phase
+    bool ok = true;
     bool bad_id = false, bad_scale = false;
-    while (p < B1) {
+    while (p < B1 && ok) {
         const Req rq = get(r);
         if (j >= item_count(a, rq.n)) {  // the next head, or the next request with a token
             j = 0;
@@ -381,67 +391,60 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
         // ---- copies: the ids of 32 blocks are in the lanes, those of the next 32 on their way
         const int32_t* row_ids = a.table + (int64_t)it.r * a.ld_table;
         const int bs = 1 << a.bs_log;
-        const int64_t head_at = it.h * a.ld_head + 16 * piece;
         auto fetch = [&](int group) {
             const int64_t key = ((int64_t)group * 32 + lane) << a.bs_log;
             return key < it.end && key + bs > it.begin ? __ldg(row_ids + group * 32 + lane) : INT32_MIN;
         };
         int group = -1, ids = 0, ids_next = 0;
-        bool lacks = false;  // some id of the group is bad, or its block not wanted
         auto use = [&](int raw) {
             const bool out = raw < 0 || raw >= a.n_blocks;
             bad_id |= out && raw != INT32_MIN;
-            ids = out ? -1 : raw;
-            lacks = __any_sync(0xffffffffu, bad_id);
+            ids = out ? (int)a.n_blocks : raw;  // past the end: the copy reads nothing and writes zeros
         };
-        // A lane copies piece `piece` of kCopies keys in a row, which lie in one block.  Where they are is found a tile ahead.
-        int id = 0;
-        int64_t at = 0;
-        auto find = [&](int u) {
-            const int b0 = u * kKeys >> a.bs_log;
+        auto load = [&](int u) {  // tile u of the sequence: a copy of keys and one of values per page
+            const int key0 = u * kKeys, b0 = key0 >> a.bs_log;
             if (b0 >> 5 != group) {
                 use(group >= 0 ? ids_next : fetch(b0 >> 5));
                 group = b0 >> 5;
                 ids_next = fetch(group + 1);
             }
-            const int key = u * kKeys + first;
-            id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
-            at = id * a.ld_block + (key & (bs - 1)) * a.ld_token + head_at;
-        };
-        auto load = [&](int u, int stage, bool more) {  // tile u of the sequence
-            const int key0 = u * kKeys, key = key0 + first;
-            const uint32_t dst = ring + stage * Sh::kStage;
-            const uint8_t *pk = a.k + at, *pv = a.v + at;
-            const bool in = piece < 2 && (first & 7) == 0, there8 = id >= 0 && key + 8 > it.begin && key < it.end;
-            const float* scale_at = (piece == 0 ? a.k_scale : a.v_scale) + (there8 ? (int64_t)id * a.n_kv_heads + it.h : 0);
-            if (!lacks && key0 >= it.begin && key0 + kKeys <= it.end) {
+            const uint32_t bar = bar0 + 8 * to_load, dst = ring + to_load * Sh::kStage;
+            if (one_lane)
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)Sh::kStage) : "memory");
+            auto copy = [&](int id, int within, uint32_t at) {
+                if (!one_lane) return;
+                asm volatile(
+                    "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(at),
+                    "l"(&maps.k), "r"(0), "r"(it.h), "r"(within), "r"(id), "r"(bar)
+                    : "memory");
+                asm volatile(
+                    "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(at + Sh::kTile),
+                    "l"(&maps.v), "r"(0), "r"(it.h), "r"(within), "r"(id), "r"(bar)
+                    : "memory");
+            };
+            auto pages = [&](auto n) {
+                constexpr int N = decltype(n)::value;
+                int id[N];
 #pragma unroll
-                for (int i = 0; i < kCopies; ++i) {
-                    copy16(dst + key_at<D>(first, piece, i), pk);
-                    copy16(dst + Sh::kTile + value_at<D>(first, piece, i), pv);
-                    pk += a.ld_token;
-                    pv += a.ld_token;
-                }
-            } else {
-#pragma unroll 1
-                for (int i = 0; i < kCopies; ++i) {
-                    const bool there = id >= 0 && key + i >= it.begin && key + i < it.end;
-                    copy16(dst + key_at<D>(first, piece, i), there ? pk : a.k, there);
-                    copy16(dst + Sh::kTile + value_at<D>(first, piece, i), there ? pv : a.v, there);
-                    pk += a.ld_token;
-                    pv += a.ld_token;
-                }
+                for (int i = 0; i < N; ++i) id[i] = __shfl_sync(0xffffffffu, ids, (b0 + i) & 31);
+#pragma unroll
+                for (int i = 0; i < N; ++i) copy(id[i], N == 1 ? key0 & (bs - 1) : 0, dst + i * (Sh::kTile / N));
+            };
+            if (bs == 16) pages(std::integral_constant<int, 2>());
+            else if (bs == 8) pages(std::integral_constant<int, 4>());
+            else pages(std::integral_constant<int, 1>());
+            // the scales of four groups of eight keys, and of their values
+            const int key = key0 + 8 * (lane & 3), id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
+            if (lane < 8) {
+                const bool there = id < a.n_blocks && key + 8 > it.begin && key < it.end;
+                copy4(ring_scales + to_load * 64 + 4 * lane, (lane < 4 ? a.k_scale : a.v_scale) + (there ? (int64_t)id * a.n_kv_heads + it.h : 0), there);
             }
-            if (in) copy4(dst + 2 * Sh::kTile + 16 * piece + first / 2, scale_at, there8);  // of a group of eight keys
-            if (more) find(u + 1);
+            if (++to_load == Sh::kStages) to_load = 0;
         };
         const int u0 = tile0 + lo, u1 = tile0 + hi;
 #pragma unroll 1
         for (int i = 0; i < Sh::kStages - 1; ++i) {
-            if (u0 + i < u1) {
-                if (i == 0) find(u0);
-                load(u0 + i, i, u0 + i + 1 < u1);
-            }
+            if (u0 + i < u1) load(u0 + i);
             copies_end();
         }
 
@@ -465,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
             uint32_t w[kSteps][2];
 #pragma unroll
             for (int s = 0; s < kSteps; s += 2) {
-                const uint4 x = live ? *reinterpret_cast<const uint4*>(src + (s / 4) * 64 + 16 * c + (s % 4) * 4) : make_uint4(0, 0, 0, 0);
+                const uint4 x = live ? *reinterpret_cast<const uint4*>(src + (D / 4) * c + 4 * s) : make_uint4(0, 0, 0, 0);
                 w[s][0] = x.x;
                 w[s][1] = x.y;
                 w[s + 1][0] = x.z;
@@ -517,21 +520,25 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
                 o[t][3] *= f1;
             }
         };
-        int stage = 0;
 #pragma unroll 1
         for (int u = u0; u < u1; ++u) {
             copies_wait<Sh::kStages - 2>();
+            ok = __all_sync(0xffffffffu, scoot_dev::mbar_wait_tries(bar0 + 8 * stage, phase));
             __syncwarp();
-            if (u + Sh::kStages - 1 < u1) load(u + Sh::kStages - 1, stage == 0 ? Sh::kStages - 1 : stage - 1, u + Sh::kStages < u1);
+            if (!ok) break;
+            if (u + Sh::kStages - 1 < u1) load(u + Sh::kStages - 1);
             copies_end();
-            const uint32_t st = ring + stage * Sh::kStage;
-            if (++stage == Sh::kStages) stage = 0;
+            const uint32_t st = ring + stage * Sh::kStage, sc = ring_scales + stage * 64;
+            if (++stage == Sh::kStages) {
+                stage = 0;
+                phase ^= 1u;
+            }
             uint32_t ks[4], vs[4];
-            lds<4>(st + 2 * Sh::kTile, ks);
-            lds<4>(st + 2 * Sh::kTile + 16, vs);
+            lds<4>(sc, ks);
+            lds<4>(sc + 16, vs);
             if (lane < 8) {
                 float own;
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(own) : "r"(st + 2 * Sh::kTile + 4 * lane));
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(own) : "r"(sc + 4 * lane));
                 bad_scale |= !(own >= 0.0f && own < INFINITY);
             }
             // scores
@@ -547,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
             for (int half = 0; half < D / 64; ++half) {
                 uint32_t w[4][4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) lds<4>(st + key_at<D>(8 * t + g, c + 4 * half), w[t]);
+                for (int t = 0; t < 4; ++t) lds<4>(st + piece_at<D>(8 * t + g, D / 64 * c + half), w[t]);
 #pragma unroll
                 for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -626,8 +633,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int row = 16 * kk + 2 * c + (i & 1) + 8 * (i >> 1);
-                    if (D == 128) lds<kW>(st + Sh::kTile + value_at<D>(row, g), w[i]);
-                    else lds<kW>(st + Sh::kTile + value_at<D>(row, g >> 1) + 8 * (g & 1), w[i]);
+                    if (D == 128) lds<kW>(st + Sh::kTile + piece_at<D>(row, g), w[i]);
+                    else lds<kW>(st + Sh::kTile + piece_at<D>(row, g >> 1) + 8 * (g & 1), w[i]);
                     if (partial) {  // (a value that some row does not see, times its zero)
 #pragma unroll
                         for (int e = 0; e < kW; ++e) w[i][e] = without_nan(w[i][e]);
@@ -645,6 +652,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
             }
         }
         __syncwarp();  // before the ring is filled for the next item
+        if (!ok) {     // a copy did not come: what is under way lands before the block ends
+            if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
+            failed = 1;
+#pragma unroll 1
+            for (int i = 0; i < Sh::kStages; ++i)
+                if (i != (int)stage) scoot_dev::mbar_wait_tries(bar0 + 8 * i, i < (int)stage ? phase ^ 1u : phase);
+            break;
+        }
 
         // ---- the end of the item
 #pragma unroll
@@ -693,17 +708,25 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
 
     // ---- split items: the block's parts of each, then the blocks'
     __syncthreads();
+    if (failed) return;
     const int w0 = blockIdx.x * kWarps, w1 = w0 + kWarps - 1;
     float* mine_out = a.parts + (size_t)(2 * n_workers + 2 * blockIdx.x) * Sh::kPart;
+    constexpr int kQuads = D / 4;
+    int before = 0;  // rows of the items before
 #pragma unroll 1
-    for (int i = 0; i <= kWarps; ++i) {
-        const Item it = items[i];
-        if (it.n_parts == 0) continue;
+    for (int e = tid, i = 0; i <= kWarps;) {
+        const int rows = items[i].n_parts ? items[i].rows : 0, q = e / kQuads - before;
+        if (q >= rows) {
+            before += rows;
+            ++i;
+            continue;
+        }
+        const Item& it = items[i];
         const int first = max(it.first, w0), n = min(it.first + it.n_parts - 1, w1) - first + 1;
-        const bool all = n == it.n_parts;
-        join<kBf16, D>(a, it, n, all ? nullptr : mine_out + (it.first >= w0 ? Sh::kPart : 0), [&](int q) {
-            return a.parts + (size_t)(2 * (first + q) + (first + q == it.first ? 1 : 0)) * Sh::kPart;
+        join<kBf16, D>(a, it, q, e % kQuads, n, n == it.n_parts ? nullptr : mine_out + (it.first >= w0 ? Sh::kPart : 0), [&](int k) {
+            return a.parts + (size_t)(2 * (first + k) + (first + k == it.first ? 1 : 0)) * Sh::kPart;
         });
+        e += kThreads;
     }
     __syncthreads();
     if (tid == 0) {
@@ -732,16 +755,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const Attn8Args
         int i = 0;
         if (side == 1)
             for (i = kWarps; !(items[i].n_parts && items[i].first + items[i].n_parts - 1 > w1);) --i;
-        const Item it = items[i];
+        const Item& it = items[i];
         const int b0 = it.first / kWarps, b1 = (it.first + it.n_parts - 1) / kWarps;
-        join<kBf16, D>(a, it, b1 - b0 + 1, nullptr, [&](int q) {
-            return a.parts + (size_t)(2 * n_workers + 2 * (b0 + q) + (q == 0 ? 1 : 0)) * Sh::kPart;
-        });
+        for (int e = tid; e < it.rows * kQuads; e += kThreads)
+            join<kBf16, D>(a, it, e / kQuads, e % kQuads, b1 - b0 + 1, nullptr, [&](int k) {
+                return a.parts + (size_t)(2 * n_workers + 2 * (b0 + k) + (k == 0 ? 1 : 0)) * Sh::kPart;
+            });
     }
 }
 
 template <bool kBf16, int D>
-scoot_status launch(scoot_ctx* ctx, const Attn8Args& a, int sms, cudaStream_t st) {
+scoot_status launch(scoot_ctx* ctx, const Attn8Args& a, const KvMaps& maps, int sms, cudaStream_t st) {
     using Sh = Shape<D>;
     auto kern = attn8_rows_kernel<kBf16, D>;
     const uint32_t bit = 1u << (9 + 2 * kBf16 + (D == 128));
@@ -749,7 +773,7 @@ scoot_status launch(scoot_ctx* ctx, const Attn8Args& a, int sms, cudaStream_t st
         SCOOT_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem));
         ctx->smem_set |= bit;
     }
-    kern<<<(unsigned)sms, kThreads, Sh::kSmem, st>>>(a);
+    kern<<<(unsigned)sms, kThreads, Sh::kSmem, st>>>(a, maps);
     SCOOT_LAUNCHED(ctx);
     return SCOOT_OK;
 }
@@ -833,8 +857,11 @@ extern "C" scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_la
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool bf16 = dtype == SCOOT_BF16;
     if (rows) {
-        if (bf16) s = D == 128 ? launch<true, 128>(ctx, a, sms, st) : launch<true, 64>(ctx, a, sms, st);
-        else s = D == 128 ? launch<false, 128>(ctx, a, sms, st) : launch<false, 64>(ctx, a, sms, st);
+        KvMaps maps;
+        if (!scoot_encode_codes(&maps.k, layout, k_cache, kKeys) || !scoot_encode_codes(&maps.v, layout, v_cache, kKeys))
+            return scoot_fail(ctx, SCOOT_EINVAL, "the cache's layout has no tensor map");
+        if (bf16) s = D == 128 ? launch<true, 128>(ctx, a, maps, sms, st) : launch<true, 64>(ctx, a, maps, sms, st);
+        else s = D == 128 ? launch<false, 128>(ctx, a, maps, sms, st) : launch<false, 64>(ctx, a, maps, sms, st);
         if (s != SCOOT_OK) return s;
     }
     return tiles ? scoot_attn8_tiles(ctx, layout, a, bf16, sms, st) : SCOOT_OK;

@@ -1,6 +1,8 @@
 // What the two kernels of attention over an 8-bit cache share.
 #pragma once
 
+#include <cuda.h>
+
 #include "internal.h"
 
 struct Attn8Args {
@@ -33,3 +35,5 @@ struct Attn8Args {
 // The tiles kernel (paged_attn.cu): requests of more than args.few tokens.  Its workspace, per multiprocessor.
 scoot_status scoot_attn8_tiles(scoot_ctx* ctx, const scoot_kv_layout* layout, const Attn8Args& args, bool bf16, int sms, cudaStream_t st);
 size_t scoot_attn8_tile_bytes(int head_dim);
+// The map of an 8-bit cache: boxes of up to `tokens` tokens of a block and head, rows of head_dim bytes swizzled by their size.
+bool scoot_encode_codes(CUtensorMap* map, const scoot_kv_layout* layout, const void* cache, int tokens);
