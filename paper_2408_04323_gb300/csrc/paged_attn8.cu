@@ -36,8 +36,7 @@
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kRows = 16, kKeys = 32;
+constexpr int kKeys = 32;
 constexpr int kItemCost = 2;    // an item's start and end, in tiles
 constexpr int kMinRange = 4;    // cost that a warp takes at least
 constexpr int kSnap = 2;        // a cut this close to the start or end of an item's tiles moves there
@@ -46,11 +45,13 @@ constexpr int kFewRows = 32;    // requests of up to so many rows
 constexpr float kMaxScale = 2.3e38f;  // times log2 e it is still finite
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
 
-template <int D>
+template <int D, int NT>
 struct Shape {
+    static constexpr int kRows = 8 * NT;                 // of an item: the products' N
+    static constexpr int kWarps = NT == 1 ? 12 : 8, kThreads = 32 * kWarps;  // as many as have the registers
     static constexpr int kTile = kKeys * D;              // bytes of a tile's keys, or values
     static constexpr int kStage = 2 * kTile;
-    static constexpr int kStages = D == 128 ? 3 : 6;
+    static constexpr int kStages = (NT == 1 ? 2 : 3) * (D == 128 ? 1 : 2);
     static constexpr int kScales = kWarps * kStages * kStage;     // after the warps' rings those of their tiles' scales: 64 bytes each
     static constexpr int kSmem = kScales + kWarps * kStages * 64;
     static constexpr int kPart = kRows * (D + 2);        // floats of a part: O, then (m, l) of each row
@@ -186,48 +187,92 @@ __device__ __forceinline__ float* lse_row(const Attn8Args& a, const Item& it, in
     return a.lse + (int64_t)(it.tok + t) * a.n_heads + it.head + q - t * it.heads;
 }
 
-// Four columns (at: in groups of four) of row q of n parts, joined: part i is at part(i).  The item's row (final), or that of a
-// part again (to != NULL).
-template <bool kBf16, int D, typename F>
-__device__ __forceinline__ void join(const Attn8Args& a, const Item& it, int q, int c, int n, float* to, F&& part) {
-    constexpr int kAtOnce = 8;
-    float M = -INFINITY, L = 0.0f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+// n parts of an item, of which `first` is the first: the others lie `step` floats apart from `second` on.
+struct Parts {
+    const float *first, *second;
+    int64_t step;
+    int32_t n;
+    __device__ __forceinline__ const float* at(int i) const { return i == 0 ? first : second + (i - 1) * step; }
+};
+
+// Parts joined, T tasks of a thread at once with P parts of each in flight.  Task e < total is four columns of a row of one of
+// `count` items; source(i, to) gives item i's parts, and where its rows go if they are parts again (else to the outputs).
+template <bool kBf16, int D, int kRows, int kThreads, int T, int P, typename F>
+__device__ __forceinline__ void join(const Attn8Args& a, const Item* items, int count, int total, F&& source) {
+    constexpr int kQuads = D / 4;
 #pragma unroll 1
-    for (int i0 = 0; i0 < n; i0 += kAtOnce) {
-        float2 ml[kAtOnce];
-        float4 v[kAtOnce];
+    for (int e0 = threadIdx.x; e0 < total; e0 += T * kThreads) {
+        Parts parts[T];
+        float* to[T];
+        int at[T], row[T], most = 0;
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            ml[i] = make_float2(-INFINITY, 0.0f);
-            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (i0 + i < n) {
-                const float* p = part(i0 + i);
-                ml[i] = __ldcg(reinterpret_cast<const float2*>(p + kRows * D) + q);
-                v[i] = __ldcg(reinterpret_cast<const float4*>(p + q * D) + c);
+        for (int t = 0; t < T; ++t) {
+            const int e = e0 + t * kThreads;
+            int q = e / kQuads, i = 0;
+            while (i < count && q >= (items[i].n_parts ? items[i].rows : 0)) q -= items[i].n_parts ? items[i].rows : 0, ++i;
+            at[t] = i;
+            row[t] = q;
+            to[t] = nullptr;
+            parts[t].n = 0;
+            if (i < count) parts[t] = source(i, to[t]);
+            most = max(most, parts[t].n);
+        }
+        const int c = threadIdx.x % kQuads;  // (of all tasks: kThreads is a multiple)
+        float M[T], L[T];
+        float4 o[T];
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            M[t] = -INFINITY;
+            L[t] = 0.0f;
+            o[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll 1
+        for (int i0 = 0; i0 < most; i0 += P) {
+            float2 ml[T][P];
+            float4 v[T][P];
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    ml[t][i] = make_float2(-INFINITY, 0.0f);
+                    v[t][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (i0 + i < parts[t].n) {
+                        const float* p = parts[t].at(i0 + i);
+                        ml[t][i] = __ldcg(reinterpret_cast<const float2*>(p + kRows * D) + row[t]);
+                        v[t][i] = __ldcg(reinterpret_cast<const float4*>(p + row[t] * D) + c);
+                    }
+                }
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+                float Mn = M[t];
+#pragma unroll
+                for (int i = 0; i < P; ++i) Mn = fmaxf(Mn, ml[t][i].x);
+                const float Ms = finite_or_zero(Mn), f = exp2_hw(M[t] - Ms);
+                L[t] *= f;
+                o[t] = make_float4(o[t].x * f, o[t].y * f, o[t].z * f, o[t].w * f);
+                M[t] = Mn;
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    const float w = exp2_hw(ml[t][i].x - Ms);
+                    L[t] = fmaf(w, ml[t][i].y, L[t]);
+                    o[t] = make_float4(fmaf(w, v[t][i].x, o[t].x), fmaf(w, v[t][i].y, o[t].y), fmaf(w, v[t][i].z, o[t].z), fmaf(w, v[t][i].w, o[t].w));
+                }
             }
         }
-        float Mn = M;
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) Mn = fmaxf(Mn, ml[i].x);
-        const float Ms = finite_or_zero(Mn), f = exp2_hw(M - Ms);
-        L *= f;
-        o = make_float4(o.x * f, o.y * f, o.z * f, o.w * f);
-        M = Mn;
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const float w = exp2_hw(ml[i].x - Ms);
-            L = fmaf(w, ml[i].y, L);
-            o = make_float4(fmaf(w, v[i].x, o.x), fmaf(w, v[i].y, o.y), fmaf(w, v[i].z, o.z), fmaf(w, v[i].w, o.w));
+        for (int t = 0; t < T; ++t) {
+            if (parts[t].n == 0) continue;
+            if (to[t]) {
+                reinterpret_cast<float4*>(to[t] + row[t] * D)[c] = o[t];
+                if (c == 0) reinterpret_cast<float2*>(to[t] + kRows * D)[row[t]] = make_float2(M[t], L[t]);
+            } else {
+                const Item& it = items[at[t]];
+                const float inv = inverse_sum(L[t]);
+                *reinterpret_cast<uint2*>(out_row(a, it, row[t]) + 4 * c) =
+                    make_uint2(pack16<kBf16>(o[t].x * inv, o[t].y * inv), pack16<kBf16>(o[t].z * inv, o[t].w * inv));
+                if (c == 0 && a.lse) *lse_row(a, it, row[t]) = L[t] == 0.0f ? -INFINITY : (M[t] + __log2f(L[t])) * kLn2;
+            }
         }
-    }
-    if (to) {
-        reinterpret_cast<float4*>(to + q * D)[c] = o;
-        if (c == 0) reinterpret_cast<float2*>(to + kRows * D)[q] = make_float2(M, L);
-    } else {
-        const float inv = inverse_sum(L);
-        *reinterpret_cast<uint2*>(out_row(a, it, q) + 4 * c) = make_uint2(pack16<kBf16>(o.x * inv, o.y * inv), pack16<kBf16>(o.z * inv, o.w * inv));
-        if (c == 0 && a.lse) *lse_row(a, it, q) = L == 0.0f ? -INFINITY : (M + __log2f(L)) * kLn2;
     }
 }
 
@@ -237,10 +282,10 @@ __device__ __forceinline__ bool elect_one() {
     return p != 0;
 }
 
-template <bool kBf16, int D>
-__global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ KvMaps maps) {
-    using Sh = Shape<D>;
-    constexpr int kSteps = D / 16, kCols = D / 8;
+template <bool kBf16, int D, int NT>
+__global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ KvMaps maps) {
+    using Sh = Shape<D, NT>;
+    constexpr int kRows = Sh::kRows, kWarps = Sh::kWarps, kThreads = Sh::kThreads, kSteps = D / 16, kDims = D / 16;  // steps of Q K^T; sixteens of dimensions of O
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int64_t cost_s[kThreads];
     __shared__ Item items[kWarps + 1];  // of the block's split items: one that came in, and one that begins with each warp's last
@@ -443,96 +488,86 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const __grid_co
         };
         const int u0 = tile0 + lo, u1 = tile0 + hi;
 #pragma unroll 1
-        for (int i = 0; i < Sh::kStages - 1; ++i) {
+        for (int i = 0; i < Sh::kStages; ++i) {
             if (u0 + i < u1) load(u0 + i);
             copies_end();
         }
 
-        // ---- queries: rows g and g + 8
-        uint32_t qa[kSteps][4];
-        float c_row[2];       // scale of the row's scores, to log2
-        int k0[2], k1[2];     // keys that the row sees
+        // ---- queries: row 8 nt + g as an operand, rows 8 nt + 2 c and the next as columns of the results
+        uint32_t qb[NT][kSteps][2];
+        float c_row[NT][2];              // scale of a row's scores, to log2
+        int k0[NT][2], k1[NT][2];        // keys that a row sees
         int all0 = it.begin, all1 = it.end;  // keys that all rows see
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = g + 8 * i, t = row / it.heads;
-            const bool live = row < it.rows;
-            const int pos = it.pos + t;
-            k1[i] = live ? (a.causal ? min(it.kv, pos + 1) : it.kv) : 0;
-            k0[i] = live && a.window > 0 ? (int)max((int64_t)0, (int64_t)pos + 1 - a.window) : 0;
-            if (live) {
-                all0 = max(all0, k0[i]);
-                all1 = min(all1, k1[i]);
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = 8 * nt + 2 * c + i, pos = it.pos + row / it.heads;
+                const bool live = row < it.rows;
+                k1[nt][i] = live ? (a.causal ? min(it.kv, pos + 1) : it.kv) : 0;
+                k0[nt][i] = live && a.window > 0 ? (int)max((int64_t)0, (int64_t)pos + 1 - a.window) : 0;
+                if (live) {
+                    all0 = max(all0, k0[nt][i]);
+                    all1 = min(all1, k1[nt][i]);
+                }
             }
+            const int row = 8 * nt + g, t = row / it.heads;
             const uint16_t* src = a.q + (int64_t)(it.tok + t) * a.q_ld_token + (int64_t)(it.head + row - t * it.heads) * a.q_ld_head;
-            uint32_t w[kSteps][2];
 #pragma unroll
             for (int s = 0; s < kSteps; s += 2) {
-                const uint4 x = live ? *reinterpret_cast<const uint4*>(src + (D / 4) * c + 4 * s) : make_uint4(0, 0, 0, 0);
-                w[s][0] = x.x;
-                w[s][1] = x.y;
-                w[s + 1][0] = x.z;
-                w[s + 1][1] = x.w;
+                const uint4 x = row < it.rows ? *reinterpret_cast<const uint4*>(src + (D / 4) * c + 4 * s) : make_uint4(0, 0, 0, 0);
+                qb[nt][s][0] = x.x;
+                qb[nt][s][1] = x.y;
+                qb[nt][s + 1][0] = x.z;
+                qb[nt][s + 1][1] = x.w;
             }
-            c_row[i] = a.scale_log2;
+            float cr = a.scale_log2;
             if (kBf16) {
                 uint32_t top = 0;  // the largest magnitude, as bits
 #pragma unroll
                 for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) top = __vmaxu2(top, w[s][e] & 0x7FFF7FFFu);
+                    for (int e = 0; e < 2; ++e) top = __vmaxu2(top, qb[nt][s][e] & 0x7FFF7FFFu);
                 top = max(top & 0xFFFFu, top >> 16);
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 // 2^(14 - its exponent), and its inverse; a row of zeros, or with what is not finite, as it is
                 const int e = (int)(top >> 7), up = top == 0 || e == 255 ? 0 : min(14 + 127 - e, 126);
                 const float f = __uint_as_float((uint32_t)(127 + up) << 23);
-                c_row[i] = fminf(c_row[i] * __uint_as_float((uint32_t)(127 - up) << 23), FLT_MAX);
+                cr = fminf(cr * __uint_as_float((uint32_t)(127 - up) << 23), FLT_MAX);
 #pragma unroll
                 for (int s = 0; s < kSteps; ++s)
 #pragma unroll
                     for (int e2 = 0; e2 < 2; ++e2)
-                        w[s][e2] = half2_bits(__uint_as_float(w[s][e2] << 16) * f, __uint_as_float(w[s][e2] & 0xFFFF0000u) * f);
+                        qb[nt][s][e2] = half2_bits(__uint_as_float(qb[nt][s][e2] << 16) * f, __uint_as_float(qb[nt][s][e2] & 0xFFFF0000u) * f);
             }
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                qa[s][i] = w[s][0];
-                qa[s][i + 2] = w[s][1];
-            }
+            c_row[nt][0] = __shfl_sync(0xffffffffu, cr, 8 * c);      // (lane 4 g' has row g')
+            c_row[nt][1] = __shfl_sync(0xffffffffu, cr, 8 * c + 4);
         }
         all0 = __reduce_max_sync(0xffffffffu, all0);
         all1 = __reduce_min_sync(0xffffffffu, all1);
-        const bool large = __any_sync(0xffffffffu, c_row[0] > 1.0f || c_row[1] > 1.0f);  // a product with a scale may pass fp32
+        bool large = false;  // a product with a scale may pass fp32
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) large |= c_row[nt][0] > 1.0f || c_row[nt][1] > 1.0f;
+        large = __any_sync(0xffffffffu, large);
 
-        float o[kCols][4];
+        float o[NT][kDims][4], m[NT][2], l[NT][2], vref = 0x1p-100f, inv_ref = 0.0f;
 #pragma unroll
-        for (int t = 0; t < kCols; ++t)
+        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[t][e] = 0.0f;
-        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-        float vref = 0x1p-100f, inv_ref = 0.0f;
-        auto scale_o = [&](float f0, float f1) {
+            for (int t = 0; t < kDims; ++t)
 #pragma unroll
-            for (int t = 0; t < kCols; ++t) {
-                o[t][0] *= f0;
-                o[t][1] *= f0;
-                o[t][2] *= f1;
-                o[t][3] *= f1;
-            }
-        };
+                for (int e = 0; e < 4; ++e) o[nt][t][e] = 0.0f;
+            m[nt][0] = m[nt][1] = -INFINITY;
+            l[nt][0] = l[nt][1] = 0.0f;
+        }
 #pragma unroll 1
         for (int u = u0; u < u1; ++u) {
-            copies_wait<Sh::kStages - 2>();
+            const uint32_t st = ring + stage * Sh::kStage, sc = ring_scales + stage * 64;
+            copies_wait<Sh::kStages - 1>();
             ok = __all_sync(0xffffffffu, scoot_dev::mbar_wait_tries(bar0 + 8 * stage, phase));
             __syncwarp();
             if (!ok) break;
-            if (u + Sh::kStages - 1 < u1) load(u + Sh::kStages - 1);
-            copies_end();
-            const uint32_t st = ring + stage * Sh::kStage, sc = ring_scales + stage * 64;
-            if (++stage == Sh::kStages) {
-                stage = 0;
-                phase ^= 1u;
-            }
             uint32_t ks[4], vs[4];
             lds<4>(sc, ks);
             lds<4>(sc + 16, vs);
@@ -541,98 +576,135 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const __grid_co
                 asm volatile("ld.shared.f32 %0, [%1];" : "=f"(own) : "r"(sc + 4 * lane));
                 bad_scale |= !(own >= 0.0f && own < INFINITY);
             }
-            // scores
-            float x[4][4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                x[t][0] = x[t][1] = x[t][2] = x[t][3] = 0.0f;
                 // (as bits: what is not finite, or negative, is above the others)
                 if (ks[t] >= 0x7F800000u) ks[t] = 0u;
                 if (vs[t] >= 0x7F800000u) vs[t] = 0u;
             }
+            // scores: sixteen keys by eight rows a product
+            float x[2][NT][4];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) x[mt][nt][0] = x[mt][nt][1] = x[mt][nt][2] = x[mt][nt][3] = 0.0f;
 #pragma unroll
             for (int half = 0; half < D / 64; ++half) {
-                uint32_t w[4][4];
+                uint32_t w[2][2][4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) lds<4>(st + piece_at<D>(8 * t + g, D / 64 * c + half), w[t]);
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) lds<4>(st + piece_at<D>(16 * mt + 8 * i + g, D / 64 * c + half), w[mt][i]);
 #pragma unroll
                 for (int s = 0; s < 4; ++s)
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) mma(x[t], qa[4 * half + s], decode_lo(w[t][s]), decode_hi(w[t][s]));
-            }
-            float ck[4][2];
+                    for (int mt = 0; mt < 2; ++mt) {
+                        const uint32_t ka[4] = {decode_lo(w[mt][0][s]), decode_lo(w[mt][1][s]), decode_hi(w[mt][0][s]), decode_hi(w[mt][1][s])};
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) ck[t][i] = c_row[i] * __uint_as_float(ks[t]);
-            const bool partial = u * kKeys < all0 || (u + 1) * kKeys > all1;
-            if (partial || large) {
-                const int key0 = u * kKeys + 2 * c;
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = e >> 1, key = key0 + 8 * t + (e & 1);
-                        if (key < k0[i] || key >= k1[i]) x[t][e] = -INFINITY;
-                        // (not zero, so that what is masked stays -inf; finite, so that a score of zero stays zero)
-                        ck[t][i] = fminf(fmaxf(ck[t][i], 1e-37f), FLT_MAX);
+                        for (int nt = 0; nt < NT; ++nt) mma(x[mt][nt], ka, qb[nt][4 * half + s][0], qb[nt][4 * half + s][1]);
                     }
             }
-            float mx[2];
+            // softmax: x[mt][nt][2 i + e] is of key 16 mt + 8 i + g and row 8 nt + 2 c + e
+            const bool partial = u * kKeys < all0 || (u + 1) * kKeys > all1;
+            float ck[2][2][NT][2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float y[4];
+            for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                for (int t = 0; t < 4; ++t) y[t] = fmaxf(x[t][2 * i], x[t][2 * i + 1]) * ck[t][i];
-                mx[i] = fmaxf(max3(y[0], y[1], y[2]), y[3]);
-                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
-                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) ck[mt][i][nt][e] = c_row[nt][e] * __uint_as_float(ks[2 * mt + i]);
+            if (partial || large) {
+                const int key0 = u * kKeys + g;
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int key = key0 + 16 * mt + 8 * i;
+                                if (key < k0[nt][e] || key >= k1[nt][e]) x[mt][nt][2 * i + e] = -INFINITY;
+                                // (not zero, so that what is masked stays -inf; finite, so that a score of zero stays zero)
+                                ck[mt][i][nt][e] = fminf(fmaxf(ck[mt][i][nt][e], 1e-37f), FLT_MAX);
+                            }
             }
+            float mx[NT][2];
+            bool grown = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float y = fmaxf(max3(x[0][nt][e] * ck[0][0][nt][e], x[0][nt][2 + e] * ck[0][1][nt][e], x[1][nt][e] * ck[1][0][nt][e]),
+                                    x[1][nt][2 + e] * ck[1][1][nt][e]);
+                    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 4));
+                    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 8));
+                    y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 16));
+                    mx[nt][e] = y;
+                    grown |= y > m[nt][e] + 8.0f;
+                }
             const float vmax = fmaxf(max3(__uint_as_float(vs[0]), __uint_as_float(vs[1]), __uint_as_float(vs[2])), __uint_as_float(vs[3]));
             if (u == u0) {
-                m[0] = mx[0];
-                m[1] = mx[1];
                 vref = fmaxf(vmax, 0x1p-100f);
                 inv_ref = 128.0f / vref;
-            } else if (__any_sync(0xffffffffu, mx[0] > m[0] + 8.0f || mx[1] > m[1] + 8.0f) || vmax > vref) {
-                const float vn = fmaxf(vref, vmax);
-                float f[2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float mn = fmaxf(m[i], mx[i]);
-                    f[i] = mn == -INFINITY ? 1.0f : exp2_hw(m[i] - mn);
-                    m[i] = mn;
-                    l[i] *= f[i];
+                for (int nt = 0; nt < NT; ++nt) {
+                    m[nt][0] = mx[nt][0];
+                    m[nt][1] = mx[nt][1];
                 }
-                scale_o(f[0] * (vref / vn), f[1] * (vref / vn));
+            } else if (__any_sync(0xffffffffu, grown) || vmax > vref) {
+                const float vn = fmaxf(vref, vmax), fv = vref / vn;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float f[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float mn = fmaxf(m[nt][e], mx[nt][e]);
+                        f[e] = mn == -INFINITY ? 1.0f : exp2_hw(m[nt][e] - mn);
+                        m[nt][e] = mn;
+                        l[nt][e] *= f[e];
+                        f[e] *= fv;
+                    }
+#pragma unroll
+                    for (int t = 0; t < kDims; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[nt][t][e] *= f[e & 1];
+                }
                 vref = vn;
                 inv_ref = 128.0f / vref;
             }
-            const float ms[2] = {-finite_or_zero(m[0]), -finite_or_zero(m[1])};
-            uint32_t pa[2][4];
-            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            // P of sixteen keys by eight rows, turned round to be the other operand: lane (g, c) gets keys 2 c and the next of row g
+            uint32_t pb[2][NT][2];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const float f = __uint_as_float(vs[t]) * inv_ref;
+            for (int nt = 0; nt < NT; ++nt) {
+                const float2 ms = make_float2(-finite_or_zero(m[nt][0]), -finite_or_zero(m[nt][1]));
+                float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float2 z = __ffma2_rn(make_float2(x[t][2 * i], x[t][2 * i + 1]), make_float2(ck[t][i], ck[t][i]), make_float2(ms[i], ms[i]));
-                    const float2 e = make_float2(exp2_hw(z.x), exp2_hw(z.y));
-                    sum[i] = __fadd2_rn(sum[i], e);
-                    const float2 pf = __fmul2_rn(e, make_float2(f, f));
-                    pa[t >> 1][2 * (t & 1) + i] = half2_bits(pf.x, pf.y);
-                }
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float f = __uint_as_float(vs[2 * mt + i]) * inv_ref;
+                        const float2 z = __ffma2_rn(make_float2(x[mt][nt][2 * i], x[mt][nt][2 * i + 1]),
+                                                    make_float2(ck[mt][i][nt][0], ck[mt][i][nt][1]), ms);
+                        const float2 e = make_float2(exp2_hw(z.x), exp2_hw(z.y));
+                        sum = __fadd2_rn(sum, e);
+                        const float2 pf = __fmul2_rn(e, make_float2(f, f));
+                        const uint32_t w = half2_bits(pf.x, pf.y);
+                        asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(pb[mt][nt][i]) : "r"(w));
+                    }
+                l[nt][0] += sum.x;
+                l[nt][1] += sum.y;
             }
-            l[0] += sum[0].x + sum[0].y;
-            l[1] += sum[1].x + sum[1].y;
-            // values
+            // values: sixteen dimensions by eight rows a product
 #pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
+            for (int mt = 0; mt < 2; ++mt) {
                 constexpr int kW = D / 32;  // words of a key's piece
                 uint32_t w[4][kW];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int row = 16 * kk + 2 * c + (i & 1) + 8 * (i >> 1);
+                    const int row = 16 * mt + 2 * c + (i & 1) + 8 * (i >> 1);
                     if (D == 128) lds<kW>(st + Sh::kTile + piece_at<D>(row, g), w[i]);
                     else lds<kW>(st + Sh::kTile + piece_at<D>(row, g >> 1) + 8 * (g & 1), w[i]);
                     if (partial) {  // (a value that some row does not see, times its zero)
@@ -642,17 +714,24 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const __grid_co
                 }
 #pragma unroll
                 for (int e = 0; e < kW; ++e) {
-                    const uint32_t a01 = __byte_perm(w[0][e], w[1][e], 0x5140), a23 = __byte_perm(w[0][e], w[1][e], 0x7362);
-                    const uint32_t b01 = __byte_perm(w[2][e], w[3][e], 0x5140), b23 = __byte_perm(w[2][e], w[3][e], 0x7362);
-                    mma(o[4 * e], pa[kk], decode_lo(a01), decode_lo(b01));
-                    mma(o[4 * e + 1], pa[kk], decode_hi(a01), decode_hi(b01));
-                    mma(o[4 * e + 2], pa[kk], decode_lo(a23), decode_lo(b23));
-                    mma(o[4 * e + 3], pa[kk], decode_hi(a23), decode_hi(b23));
+#pragma unroll
+                    for (int h2 = 0; h2 < 2; ++h2) {
+                        const uint32_t lo2 = __byte_perm(w[0][e], w[1][e], h2 ? 0x7362 : 0x5140), hi2 = __byte_perm(w[2][e], w[3][e], h2 ? 0x7362 : 0x5140);
+                        const uint32_t va[4] = {decode_lo(lo2), decode_hi(lo2), decode_lo(hi2), decode_hi(hi2)};
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) mma(o[nt][2 * e + h2], va, pb[mt][nt][0], pb[mt][nt][1]);
+                    }
                 }
             }
+            __syncwarp();  // the tile has been read
+            if (u + Sh::kStages < u1) load(u + Sh::kStages);
+            copies_end();
+            if (++stage == Sh::kStages) {
+                stage = 0;
+                phase ^= 1u;
+            }
         }
-        __syncwarp();  // before the ring is filled for the next item
-        if (!ok) {     // a copy did not come: what is under way lands before the block ends
+        if (!ok) {  // a copy did not come: what is under way lands before the block ends
             if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
             failed = 1;
 #pragma unroll 1
@@ -661,47 +740,41 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const __grid_co
             break;
         }
 
-        // ---- the end of the item
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-        }
+        // ---- the end of the item: the lane has 16 (8) dimensions in a row of rows 8 nt + 2 c and the next
         const bool whole = it.n_parts == 1;
         const bool begins = it.first == worker;
         float* part = a.parts + (size_t)(2 * worker + begins) * Sh::kPart;
         if (!whole && lane == 0 && (begins || warp == 0)) items[begins ? 1 + warp : 0] = it;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = g + 8 * i;
-            if (row >= it.rows) continue;
-            // columns t of the lane's two: kCols consecutive dimensions each
-            if (whole) {
-                const float f = inverse_sum(l[i]) * 0x1p-7f;
-                uint16_t* dst = out_row(a, it, row) + c * (D / 4);
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+            for (int e = 0; e < 2; ++e) {
+                l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 4);
+                l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 8);
+                l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 16);
+                const int row = 8 * nt + 2 * c + e;
+                if (row >= it.rows) continue;
+                if (whole) {
+                    const float f = inverse_sum(l[nt][e]) * 0x1p-7f;
+                    uint16_t* dst = out_row(a, it, row) + g * (D / 8);
 #pragma unroll
-                    for (int t = 0; t < kCols; t += 8) {
+                    for (int t = 0; t < kDims; t += 4) {
                         uint32_t w[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            w[e] = pack16<kBf16>(o[t + 2 * e][2 * i + n] * f * vref, o[t + 2 * e + 1][2 * i + n] * f * vref);
-                        *reinterpret_cast<uint4*>(dst + n * kCols + t) = make_uint4(w[0], w[1], w[2], w[3]);
+                        for (int i = 0; i < 4; ++i) w[i] = pack16<kBf16>(o[nt][t + i][e] * f * vref, o[nt][t + i][2 + e] * f * vref);
+                        *reinterpret_cast<uint4*>(dst + 2 * t) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
-                if (c == 0 && a.lse) *lse_row(a, it, row) = l[i] == 0.0f ? -INFINITY : (m[i] + __log2f(l[i])) * kLn2;
-            } else {
-                const float f = vref * 0x1p-7f;
-                float* dst = part + row * D + c * (D / 4);
+                    if (g == 0 && a.lse) *lse_row(a, it, row) = l[nt][e] == 0.0f ? -INFINITY : (m[nt][e] + __log2f(l[nt][e])) * kLn2;
+                } else {
+                    const float f = vref * 0x1p-7f;
+                    float* dst = part + row * D + g * (D / 8);
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int t = 0; t < kCols; t += 4)
-                        *reinterpret_cast<float4*>(dst + n * kCols + t) = make_float4(o[t][2 * i + n] * f, o[t + 1][2 * i + n] * f,
-                                                                                     o[t + 2][2 * i + n] * f, o[t + 3][2 * i + n] * f);
-                if (c == 0) reinterpret_cast<float2*>(part + kRows * D)[row] = make_float2(m[i], l[i]);
+                    for (int t = 0; t < kDims; t += 2)
+                        *reinterpret_cast<float4*>(dst + 2 * t) =
+                            make_float4(o[nt][t][e] * f, o[nt][t][2 + e] * f, o[nt][t + 1][e] * f, o[nt][t + 1][2 + e] * f);
+                    if (g == 0) reinterpret_cast<float2*>(part + kRows * D)[row] = make_float2(m[nt][e], l[nt][e]);
+                }
             }
-        }
     }
     if (bad_id) atomicOr(a.err, SCOOT_DEVERR_INDEX);
     if (bad_scale) atomicOr(a.err, SCOOT_DEVERR_VALUE);
@@ -710,72 +783,69 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_rows_kernel(const __grid_co
     __syncthreads();
     if (failed) return;
     const int w0 = blockIdx.x * kWarps, w1 = w0 + kWarps - 1;
-    float* mine_out = a.parts + (size_t)(2 * n_workers + 2 * blockIdx.x) * Sh::kPart;
-    constexpr int kQuads = D / 4;
-    int before = 0;  // rows of the items before
+    float* joined = a.parts + (size_t)2 * n_workers * Sh::kPart;  // two per block
+    int rows = 0;
 #pragma unroll 1
-    for (int e = tid, i = 0; i <= kWarps;) {
-        const int rows = items[i].n_parts ? items[i].rows : 0, q = e / kQuads - before;
-        if (q >= rows) {
-            before += rows;
-            ++i;
-            continue;
-        }
+    for (int i = 0; i <= kWarps; ++i) rows += items[i].n_parts ? items[i].rows : 0;
+    const auto source = [&](int i, float*& to) {
         const Item& it = items[i];
         const int first = max(it.first, w0), n = min(it.first + it.n_parts - 1, w1) - first + 1;
-        join<kBf16, D>(a, it, q, e % kQuads, n, n == it.n_parts ? nullptr : mine_out + (it.first >= w0 ? Sh::kPart : 0), [&](int k) {
-            return a.parts + (size_t)(2 * (first + k) + (first + k == it.first ? 1 : 0)) * Sh::kPart;
-        });
-        e += kThreads;
-    }
+        if (n < it.n_parts) to = joined + (size_t)(2 * blockIdx.x + (it.first >= w0 ? 1 : 0)) * Sh::kPart;
+        return Parts{a.parts + (size_t)(2 * first + (first == it.first ? 1 : 0)) * Sh::kPart, a.parts + (size_t)(2 * first + 2) * Sh::kPart,
+                     2 * Sh::kPart, n};
+    };
+    if (rows * (D / 4) <= kThreads) join<kBf16, D, kRows, kThreads, 1, 8>(a, items, kWarps + 1, rows * (D / 4), source);
+    else join<kBf16, D, kRows, kThreads, 4, 2>(a, items, kWarps + 1, rows * (D / 4), source);
     __syncthreads();
+    // The item that came in, and the one that goes on in the next block.
     if (tid == 0) {
-        last_s[0] = last_s[1] = 0;
-        __threadfence();  // (the block's other threads' stores are before it by the barrier)
-        for (int side = 0; side < 2; ++side) {
-            // the item that came in, or the one that goes on in the next block
-            Item it;
-            it.n_parts = 0;
-            if (side == 0) it = items[0];
-            else
-                for (int i = 1; i <= kWarps; ++i)
-                    if (items[i].n_parts && items[i].first + items[i].n_parts - 1 > w1) it = items[i];
-            if (it.n_parts == 0) continue;
-            const int b0 = it.first / kWarps, b1 = (it.first + it.n_parts - 1) / kWarps;
-            const bool last = atomicAdd(a.count + b0, 1u) == (uint32_t)(b1 - b0);
-            if (last) a.count[b0] = 0;
-            last_s[side] = last;
+        int out = -1;
+#pragma unroll 1
+        for (int i = 1; i <= kWarps; ++i)
+            if (items[i].n_parts && items[i].first + items[i].n_parts - 1 > w1) out = i;
+        last_s[0] = last_s[1] = -1;
+        if (items[0].n_parts || out > 0) {
+            __threadfence();  // (the block's other threads' stores are before it by the barrier)
+            for (int side = 0; side < 2; ++side) {
+                const int i = side ? out : 0;
+                if (i < 0 || items[i].n_parts == 0) continue;
+                const int b0 = items[i].first / kWarps, b1 = (items[i].first + items[i].n_parts - 1) / kWarps;
+                if (atomicAdd(a.count + b0, 1u) != (uint32_t)(b1 - b0)) continue;
+                a.count[b0] = 0;
+                last_s[side] = i;
+            }
+            __threadfence();
         }
-        __threadfence();
     }
     __syncthreads();
 #pragma unroll 1
     for (int side = 0; side < 2; ++side) {
-        if (!last_s[side]) continue;
-        int i = 0;
-        if (side == 1)
-            for (i = kWarps; !(items[i].n_parts && items[i].first + items[i].n_parts - 1 > w1);) --i;
-        const Item& it = items[i];
-        const int b0 = it.first / kWarps, b1 = (it.first + it.n_parts - 1) / kWarps;
-        for (int e = tid; e < it.rows * kQuads; e += kThreads)
-            join<kBf16, D>(a, it, e / kQuads, e % kQuads, b1 - b0 + 1, nullptr, [&](int k) {
-                return a.parts + (size_t)(2 * n_workers + 2 * (b0 + k) + (k == 0 ? 1 : 0)) * Sh::kPart;
-            });
+        const int i = last_s[side];
+        if (i < 0) continue;
+        join<kBf16, D, kRows, kThreads, 1, 8>(a, items + i, 1, items[i].rows * (D / 4), [&](int, float*&) {
+            const int b0 = items[i].first / kWarps, b1 = (items[i].first + items[i].n_parts - 1) / kWarps;
+            return Parts{joined + (size_t)(2 * b0 + 1) * Sh::kPart, joined + (size_t)(2 * b0 + 2) * Sh::kPart, 2 * Sh::kPart, b1 - b0 + 1};
+        });
     }
 }
 
-template <bool kBf16, int D>
+template <bool kBf16, int D, int NT>
 scoot_status launch(scoot_ctx* ctx, const Attn8Args& a, const KvMaps& maps, int sms, cudaStream_t st) {
-    using Sh = Shape<D>;
-    auto kern = attn8_rows_kernel<kBf16, D>;
-    const uint32_t bit = 1u << (9 + 2 * kBf16 + (D == 128));
+    using Sh = Shape<D, NT>;
+    auto kern = attn8_rows_kernel<kBf16, D, NT>;
+    const uint32_t bit = 1u << (17 + 4 * (NT - 1) + 2 * kBf16 + (D == 128));
     if (!(ctx->smem_set & bit)) {  // once per context: the call is short
         SCOOT_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kSmem));
         ctx->smem_set |= bit;
     }
-    kern<<<(unsigned)sms, kThreads, Sh::kSmem, st>>>(a, maps);
+    kern<<<(unsigned)sms, Sh::kThreads, Sh::kSmem, st>>>(a, maps);
     SCOOT_LAUNCHED(ctx);
     return SCOOT_OK;
+}
+template <int NT>
+scoot_status launch(scoot_ctx* ctx, const Attn8Args& a, const KvMaps& maps, bool bf16, int D, int sms, cudaStream_t st) {
+    if (bf16) return D == 128 ? launch<true, 128, NT>(ctx, a, maps, sms, st) : launch<true, 64, NT>(ctx, a, maps, sms, st);
+    return D == 128 ? launch<false, 128, NT>(ctx, a, maps, sms, st) : launch<false, 64, NT>(ctx, a, maps, sms, st);
 }
 
 }  // namespace
@@ -819,8 +889,9 @@ extern "C" scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_la
     a.causal = causal != 0;
     a.window = window < ld_table * layout->block_size ? window : 0;  // no sequence is longer
     a.max_new = max_new;
-    a.toks = G <= kRows ? kRows / G : 1;
-    a.per_token = (G + kRows - 1) / kRows;
+    const int row_tiles = G <= 8 ? 1 : 2, item_rows = 8 * row_tiles;
+    a.toks = G <= item_rows ? item_rows / G : 1;
+    a.per_token = (G + item_rows - 1) / item_rows;
     a.n_tokens = n_tokens;
     a.n_blocks = layout->n_blocks;
     a.query_start = query_start;
@@ -848,8 +919,8 @@ extern "C" scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_la
     a.few = kFewRows / G;
     // The host does not know the lengths: without max_new both kernels are launched, and one may find nothing to do.
     const bool rows = a.few > 0, tiles = max_new == 0 || max_new > a.few;
-    const size_t part = (D == 128 ? Shape<128>::kPart : Shape<64>::kPart) * sizeof(float);
-    const size_t row_bytes = rows ? (size_t)sms * 2 * (kWarps + 1) * part : 0;
+    const size_t part = (size_t)item_rows * (D + 2) * sizeof(float);
+    const size_t row_bytes = rows ? (size_t)sms * 2 * ((row_tiles == 1 ? Shape<64, 1>::kWarps : Shape<64, 2>::kWarps) + 1) * part : 0;
     s = scoot_workspace(ctx, row_bytes + (tiles ? sms * scoot_attn8_tile_bytes(D) : 0), stream);
     if (s != SCOOT_OK) return s;
     a.parts = static_cast<float*>(ctx->ws);
@@ -860,8 +931,7 @@ extern "C" scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_la
         KvMaps maps;
         if (!scoot_encode_codes(&maps.k, layout, k_cache, kKeys) || !scoot_encode_codes(&maps.v, layout, v_cache, kKeys))
             return scoot_fail(ctx, SCOOT_EINVAL, "the cache's layout has no tensor map");
-        if (bf16) s = D == 128 ? launch<true, 128>(ctx, a, maps, sms, st) : launch<true, 64>(ctx, a, maps, sms, st);
-        else s = D == 128 ? launch<false, 128>(ctx, a, maps, sms, st) : launch<false, 64>(ctx, a, maps, sms, st);
+        s = row_tiles == 1 ? launch<1>(ctx, a, maps, bf16, D, sms, st) : launch<2>(ctx, a, maps, bf16, D, sms, st);
         if (s != SCOOT_OK) return s;
     }
     return tiles ? scoot_attn8_tiles(ctx, layout, a, bf16, sms, st) : SCOOT_OK;
