@@ -20,7 +20,7 @@
 #define SCOOT_DEVERR_CAPACITY 4u  // a Pareto filter had more survivors than it can hold
 #define SCOOT_DEVERR_VALUE   8u   // a non-finite feature or a label other than 0/1
 
-#define SCOOT_COUNTS 1024u
+#define SCOOT_COUNTS 8192u
 
 struct scoot_ctx {
     int32_t device = 0;

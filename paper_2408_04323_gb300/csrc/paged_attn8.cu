@@ -36,11 +36,16 @@
 
 namespace {
 
-constexpr int kKeys = 32;
-constexpr int kItemCost = 2;    // an item's start and end, in tiles
+constexpr int kItemCost = 2;    // an item's start and end, in tiles,
 constexpr int kMinRange = 4;    // cost that a warp takes at least
 constexpr int kSnap = 2;        // a cut this close to the start or end of an item's tiles moves there
-constexpr int kMaxBlocks = (int)(SCOOT_COUNTS / 4);  // a counter each, and two for the tiles kernel, apart
+constexpr int kMaxBlocks = 256;
+constexpr int kShare = 4;       // warps that take as many heads' keys of the same tokens at a time, at most
+// Counters, apart: two per block of the tiles kernel, one per warp of this, kShare per block of this.
+constexpr int kWarpCounts = 2 * kMaxBlocks, kBlockCounts = kWarpCounts + 12 * kMaxBlocks;
+static_assert(kBlockCounts + kShare * kMaxBlocks <= (int)SCOOT_COUNTS, "counters");
+constexpr int kFewParts = 8;    // parts that the warp that comes last joins by itself
+constexpr int kItems = 8;       // items of a warp between its copies and their attention
 constexpr int kFewRows = 32;    // requests of up to so many rows
 constexpr float kMaxScale = 2.3e38f;  // times log2 e it is still finite
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
@@ -49,11 +54,13 @@ template <int D, int NT>
 struct Shape {
     static constexpr int kRows = 8 * NT;                 // of an item: the products' N
     static constexpr int kWarps = NT == 1 ? 12 : 8, kThreads = 32 * kWarps;  // as many as have the registers
+    static constexpr int kKeys = D == 128 ? 32 : 64;     // of a tile
     static constexpr int kTile = kKeys * D;              // bytes of a tile's keys, or values
     static constexpr int kStage = 2 * kTile;
-    static constexpr int kStages = (NT == 1 ? 2 : 3) * (D == 128 ? 1 : 2);
-    static constexpr int kScales = kWarps * kStages * kStage;     // after the warps' rings those of their tiles' scales: 64 bytes each
-    static constexpr int kSmem = kScales + kWarps * kStages * 64;
+    static constexpr int kStages = NT == 1 ? 2 : 3;
+    static constexpr int kScales = kWarps * kStages * kStage;     // after the warps' rings those of their tiles' scales
+    static constexpr int kScale = kKeys;                 // bytes of them: groups of eight keys, and of values
+    static constexpr int kSmem = kScales + kWarps * kStages * kScale;
     static constexpr int kPart = kRows * (D + 2);        // floats of a part: O, then (m, l) of each row
 };
 
@@ -68,7 +75,8 @@ struct Item {
     int32_t rows, heads;   // rows, and heads among them: row = token * heads + head
     int32_t pos, kv;       // position of the first token, length of the sequence
     int32_t begin, end;    // keys that some row sees
-    int32_t first, n_parts;  // worker of the first part, and how many parts
+    int32_t u0, u1;        // this part's tiles
+    int32_t first, n_parts;  // team of the first part, and how many parts
 };
 
 __device__ __forceinline__ float exp2_hw(float x) {
@@ -159,16 +167,18 @@ __device__ __forceinline__ void seen_keys(const Attn8Args& a, int kv, int n, int
     begin = a.window > 0 ? (int)max((int64_t)0, p0 + 1 - a.window) : 0;
     if (end <= begin) begin = end = 0;
 }
+template <int kKeys>
 __device__ __forceinline__ int item_cost(const Attn8Args& a, int kv, int n, int j) {
     int begin, end;
     seen_keys(a, kv, n, j, begin, end);
     return kItemCost + (end + kKeys - 1) / kKeys - begin / kKeys;
 }
 // The cost of a head's items of a request, by the whole warp.
+template <int kKeys>
 __device__ __forceinline__ int64_t head_cost(const Attn8Args& a, int kv, int n) {
     const int m = item_count(a, n);
     int64_t c = 0;
-    for (int j = threadIdx.x & 31; j < m; j += 32) c += item_cost(a, kv, n, j);
+    for (int j = threadIdx.x & 31; j < m; j += 32) c += item_cost<kKeys>(a, kv, n, j);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) c += __shfl_xor_sync(0xffffffffu, c, d);
     return c;
@@ -198,10 +208,10 @@ struct Parts {
 // Parts joined, T tasks of a thread at once with P parts of each in flight.  Task e < total is four columns of a row of one of
 // `count` items; source(i, to) gives item i's parts, and where its rows go if they are parts again (else to the outputs).
 template <bool kBf16, int D, int kRows, int kThreads, int T, int P, typename F>
-__device__ __forceinline__ void join(const Attn8Args& a, const Item* items, int count, int total, F&& source) {
+__device__ __forceinline__ void join(const Attn8Args& a, const Item* items, int count, int total, int me, F&& source) {
     constexpr int kQuads = D / 4;
 #pragma unroll 1
-    for (int e0 = threadIdx.x; e0 < total; e0 += T * kThreads) {
+    for (int e0 = me; e0 < total; e0 += T * kThreads) {
         Parts parts[T];
         float* to[T];
         int at[T], row[T], most = 0;
@@ -217,7 +227,7 @@ __device__ __forceinline__ void join(const Attn8Args& a, const Item* items, int 
             if (i < count) parts[t] = source(i, to[t]);
             most = max(most, parts[t].n);
         }
-        const int c = threadIdx.x % kQuads;  // (of all tasks: kThreads is a multiple)
+        const int c = me % kQuads;  // (of all tasks: kThreads is a multiple)
         float M[T], L[T];
         float4 o[T];
 #pragma unroll
@@ -282,22 +292,115 @@ __device__ __forceinline__ bool elect_one() {
     return p != 0;
 }
 
+// Where a warp is among the items of its range, in shared memory: what is done per item stays out of the registers of what is
+// done per tile.
+struct Cursor {
+    int64_t at, begin, end, range;  // start of the next item; the range; its length
+    int32_t r, h, j, team;          // the next item: request, heads, which of the heads'
+    int32_t member;                 // the head is h share + member
+    Req req;                        // r's lengths
+};
+
+// The ids of 32 blocks of an item's request in the lanes; INT32_MIN for those that no row sees any of.
+__device__ __forceinline__ int fetch_ids(const Attn8Args& a, const Item& it, int group) {
+    const int block = group * 32 + (threadIdx.x & 31);
+    const int64_t key = (int64_t)block << a.bs_log;
+    return key < it.end && key + (1 << a.bs_log) > it.begin ? __ldg(a.table + (int64_t)it.r * a.ld_table + block) : INT32_MIN;
+}
+
+// A range's next item with keys goes to *to; false if there is none.  Those without keys get their zeros here.  By a warp.
+template <int D, int kRows, int kKeys>
+__device__ __noinline__ bool next_item(const Attn8Args& a, Cursor* cur, Item* to) {
+    const int lane = threadIdx.x & 31;
+    Cursor c = *cur;
+    bool found = false;
+    while (c.at < c.end) {
+        if (c.j >= item_count(a, c.req.n)) {  // the next head, or the next request with a token
+            c.j = 0;
+            if (c.req.n > 0 && ++c.h < a.n_kv_heads / a.share) continue;
+            c.h = 0;
+            for (++c.r; c.r < a.n_req;) {
+                const Req q = load_req(a, c.r + lane, false);
+                const uint32_t some = __ballot_sync(0xffffffffu, q.n > 0);
+                if (some) {
+                    const int src = __ffs(some) - 1;
+                    c.r += src;
+                    c.req = Req{__shfl_sync(0xffffffffu, q.q0, src), __shfl_sync(0xffffffffu, q.n, src), __shfl_sync(0xffffffffu, q.kv, src)};
+                    break;
+                }
+                c.r += 32;
+            }
+            if (c.r >= a.n_req) {
+                c.at = c.end;
+                break;
+            }
+        }
+        Item it;
+        it.r = c.r;
+        it.h = c.h * a.share + c.member;
+        const int tok = a.per_token > 1 ? c.j / a.per_token : c.j * a.toks, sub = a.per_token > 1 ? c.j % a.per_token : 0;
+        it.heads = a.per_token > 1 ? min(kRows, a.group - sub * kRows) : a.group;
+        it.rows = min(a.toks, c.req.n - tok) * it.heads;
+        it.tok = c.req.q0 + tok;
+        it.head = it.h * a.group + sub * kRows;
+        it.pos = c.req.kv - c.req.n + tok;
+        it.kv = c.req.kv;
+        seen_keys(a, c.req.kv, c.req.n, c.j, it.begin, it.end);
+        const int tile0 = it.begin / kKeys, units = (it.end + kKeys - 1) / kKeys - tile0;
+        const int64_t start = c.at, s0 = start + kItemCost;  // where its tiles start
+        auto cut = [&](int64_t b) { return b >= s0 + units ? units : b - s0 < kSnap ? 0 : s0 + units - b < kSnap ? units : (int)(b - s0); };
+        const int lo = cut(c.begin), hi = cut(c.end);
+        c.at = s0 + units;
+        ++c.j;
+        if (units == 0 && start >= c.begin) {
+            for (int e = lane; e < it.rows * (D / 8); e += 32)
+                *reinterpret_cast<uint4*>(out_row(a, it, e / (D / 8)) + 8 * (e % (D / 8))) = make_uint4(0, 0, 0, 0);
+            if (a.lse)
+                for (int q = lane; q < it.rows; q += 32) *lse_row(a, it, q) = -INFINITY;
+        }
+        if (hi <= lo) continue;
+        it.first = c.team;
+        it.n_parts = 1;
+        if (hi - lo < units) {
+            it.first = (int)quotient(s0 + kSnap - 1, c.range);
+            it.n_parts = (int)quotient(s0 + units - kSnap, c.range) - it.first + 1;
+        }
+        it.u0 = tile0 + lo;
+        it.u1 = tile0 + hi;
+        if (lane == 0) *to = it;
+        // queries on their way to the L2 cache
+        for (int e = lane; e < it.rows * (D / 64); e += 32) {
+            const int q = e / (D / 64), t = q / it.heads;
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(a.q + (int64_t)(it.tok + t) * a.q_ld_token + (int64_t)(it.head + q - t * it.heads) * a.q_ld_head +
+                                                          e % (D / 64) * 64));
+        }
+        found = true;
+        break;
+    }
+    __syncwarp();
+    if (lane == 0) *cur = c;
+    __syncwarp();
+    return found;
+}
+
 template <bool kBf16, int D, int NT>
 __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(const __grid_constant__ Attn8Args a, const __grid_constant__ KvMaps maps) {
     using Sh = Shape<D, NT>;
-    constexpr int kRows = Sh::kRows, kWarps = Sh::kWarps, kThreads = Sh::kThreads, kSteps = D / 16, kDims = D / 16;  // steps of Q K^T; sixteens of dimensions of O
+    constexpr int kRows = Sh::kRows, kWarps = Sh::kWarps, kThreads = Sh::kThreads, kKeys = Sh::kKeys, kM = kKeys / 16, kG = kKeys / 8, kSteps = D / 16, kDims = D / 16;  // steps of Q K^T; sixteens of dimensions of O
     extern __shared__ __align__(1024) uint8_t smem[];
     __shared__ int64_t cost_s[kThreads];
-    __shared__ Item items[kWarps + 1];  // of the block's split items: one that came in, and one that begins with each warp's last
-    __shared__ int last_s[2], failed;
+    __shared__ Item items[kShare + kWarps];  // of the block's items of many parts: those that came in, and one that begins with each warp's last
+    __shared__ Item queue_s[kWarps][kItems];
+    __shared__ Cursor cursor_s[kWarps];
+    __shared__ int last_s[kShare + kWarps], failed, many;
     __shared__ __align__(8) uint64_t bars[kWarps * Sh::kStages];
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int g = lane >> 2, c = lane & 3;
 
     // The cost of all items: each thread k consecutive requests, then a scan.
     const int k = (a.n_req + kThreads - 1) / kThreads;
-    if (tid <= kWarps) items[tid].n_parts = 0;
-    if (tid == 0) failed = 0;
+    if (tid < kShare + kWarps) items[tid].n_parts = 0;
+    if (tid == 0) failed = many = 0;
     if (tid < kWarps * Sh::kStages) scoot_dev::mbar_init(&bars[tid], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     int64_t mine = 0;
@@ -305,16 +408,17 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
     for (int i = 0; i < k; ++i) {
         const Req q = load_req(a, tid * k + i, blockIdx.x == 0);
         const bool one = item_count(a, q.n) == 1;
-        if (one) mine += item_cost(a, q.kv, q.n, 0);
+        if (one) mine += item_cost<kKeys>(a, q.kv, q.n, 0);
         uint32_t big = __ballot_sync(0xffffffffu, q.n > 0 && !one);
         while (big) {
             const int src = __ffs(big) - 1;
             big &= big - 1;
-            const int64_t cost = head_cost(a, __shfl_sync(0xffffffffu, q.kv, src), __shfl_sync(0xffffffffu, q.n, src));
+            const int64_t cost = head_cost<kKeys>(a, __shfl_sync(0xffffffffu, q.kv, src), __shfl_sync(0xffffffffu, q.n, src));
             if (lane == src) mine += cost;
         }
     }
-    mine *= a.n_kv_heads;
+    const int heads = a.n_kv_heads / a.share;
+    mine *= heads;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
         const int64_t t = __shfl_up_sync(0xffffffffu, mine, d);
@@ -330,8 +434,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
     }
     const int64_t total = __shfl_sync(0xffffffffu, upto, kWarps - 1);
     const int worker = blockIdx.x * kWarps + warp, n_workers = gridDim.x * kWarps;
-    const int64_t range = max(quotient(total + n_workers - 1, n_workers), (int64_t)kMinRange);
-    const int64_t B0 = min(total, worker * range), B1 = min(total, B0 + range);
+    const int team = worker / a.share, member = worker % a.share, n_teams = n_workers / a.share;
+    const int64_t range = max(quotient(total + n_teams - 1, n_teams), (int64_t)kMinRange);
+    const int64_t B0 = min(total, team * range), B1 = min(total, B0 + range);
 
     int cached = -1;  // requests 32 cached .. are in the lanes
     Req in_lane{0, 0, 0};
@@ -356,19 +461,19 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
         r = (w * 32 + t) * k;
         while (r < a.n_req) {
             const Req q = get(r);
-            const int64_t one = q.n == 0 ? 0 : item_count(a, q.n) == 1 ? item_cost(a, q.kv, q.n, 0) : head_cost(a, q.kv, q.n);
-            if (at + one * a.n_kv_heads > B0) {
+            const int64_t one = q.n == 0 ? 0 : item_count(a, q.n) == 1 ? item_cost<kKeys>(a, q.kv, q.n, 0) : head_cost<kKeys>(a, q.kv, q.n);
+            if (at + one * heads > B0) {
                 h = (int)quotient(B0 - at, one);
                 at += h * one;
                 break;
             }
-            at += one * a.n_kv_heads;
+            at += one * heads;
             ++r;
         }
         const Req q = get(min(r, a.n_req - 1));
         const int m = item_count(a, q.n);
         for (int j0 = 0; m > 1 && j0 < m; j0 += 32) {
-            const int64_t cost = j0 + lane < m ? item_cost(a, q.kv, q.n, j0 + lane) : 0;
+            const int64_t cost = j0 + lane < m ? item_cost<kKeys>(a, q.kv, q.n, j0 + lane) : 0;
             int64_t s = cost;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -385,119 +490,114 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
             at += __shfl_sync(0xffffffffu, s, 31);
         }
         p = at;
+        if (lane == 0) cursor_s[warp] = Cursor{p, B0, B1, range, r, h, j, team, member, q};
+    } else if (lane == 0) {
+        cursor_s[warp] = Cursor{0, 0, 0, range, 0, 0, 0, team, member, Req{0, 0, 0}};
     }
+    __syncwarp();
 
     const uint32_t ring = scoot_dev::smem_u32(smem) + warp * Sh::kStages * Sh::kStage;
-    const uint32_t ring_scales = scoot_dev::smem_u32(smem) + Sh::kScales + warp * Sh::kStages * 64;
+    const uint32_t ring_scales = scoot_dev::smem_u32(smem) + Sh::kScales + warp * Sh::kStages * Sh::kScale;
     const uint32_t bar0 = scoot_dev::smem_u32(&bars[warp * Sh::kStages]);
     const bool one_lane = elect_one();
     uint32_t to_load = 0, stage = 0, phase = 0;  // places in the ring: of the next load, and of the next tile with its barrier's phase
     bool ok = true;
     bool bad_id = false, bad_scale = false;
-    while (p < B1 && ok) {
-        const Req rq = get(r);
-        if (j >= item_count(a, rq.n)) {  // the next head, or the next request with a token
-            j = 0;
-            if (rq.n > 0 && ++h < a.n_kv_heads) continue;
-            h = 0;
-            const uint32_t more = __ballot_sync(0xffffffffu, in_lane.n > 0) & ~((2u << (r & 31)) - 1u);
-            r = more ? (r & ~31) + __ffs(more) - 1 : (r & ~31) + 32;
-            if (r >= a.n_req) break;
-            continue;
-        }
-        Item it;
-        it.r = r;
-        it.h = h;
-        {
-            const int tok = a.per_token > 1 ? j / a.per_token : j * a.toks, sub = a.per_token > 1 ? j % a.per_token : 0;
-            it.heads = a.per_token > 1 ? min(kRows, a.group - sub * kRows) : a.group;
-            it.rows = min(a.toks, rq.n - tok) * it.heads;
-            it.tok = rq.q0 + tok;
-            it.head = h * a.group + sub * kRows;
-            it.pos = rq.kv - rq.n + tok;
-            it.kv = rq.kv;
-        }
-        seen_keys(a, rq.kv, rq.n, j, it.begin, it.end);
-        const int tile0 = it.begin / kKeys, units = (it.end + kKeys - 1) / kKeys - tile0;
-        const int64_t s0 = p + kItemCost;  // where its tiles start
-        auto cut = [&](int64_t b) { return b >= s0 + units ? units : b - s0 < kSnap ? 0 : s0 + units - b < kSnap ? units : (int)(b - s0); };
-        const int lo = cut(B0), hi = cut(B1);
-        const bool here = units ? hi > lo : p >= B0;
-        p = s0 + units;
-        ++j;
-        if (!here) continue;
-        it.first = worker;
-        it.n_parts = 1;
-        if (hi - lo < units) {
-            it.first = (int)quotient(s0 + kSnap - 1, range);
-            it.n_parts = (int)quotient(s0 + units - kSnap, range) - it.first + 1;
-        }
+    const int bs = 1 << a.bs_log;
+    // An item's n parts from that of team t on: a warp's first buffer has the part of an item that began before it, the second that
+    // of one that begins with it and goes on.
+    auto parts_at = [&](int t, int begun, int who, int n) {
+        return Parts{a.parts + (size_t)(2 * (t * a.share + who) + (t == begun)) * Sh::kPart, a.parts + (size_t)2 * ((t + 1) * a.share + who) * Sh::kPart,
+                     (int64_t)2 * a.share * Sh::kPart, n};
+    };
 
-        // ---- copies: the ids of 32 blocks are in the lanes, those of the next 32 on their way
-        const int32_t* row_ids = a.table + (int64_t)it.r * a.ld_table;
-        const int bs = 1 << a.bs_log;
-        auto fetch = [&](int group) {
-            const int64_t key = ((int64_t)group * 32 + lane) << a.bs_log;
-            return key < it.end && key + bs > it.begin ? __ldg(row_ids + group * 32 + lane) : INT32_MIN;
+    uint32_t n_made = 0, n_taken = 0;  // items found, and those whose copies have begun
+    int first_ids = 0;                 // ids of the first 32 blocks of the last one found, in the lanes
+    auto find = [&]() {
+        Item* to = &queue_s[warp][n_made % kItems];
+        if (!next_item<D, kRows, kKeys>(a, &cursor_s[warp], to)) return;
+        ++n_made;
+        first_ids = fetch_ids(a, *to, (to->u0 * kKeys >> a.bs_log) >> 5);
+    };
+
+    // The next tile's copies: of keys and of values per page, and the scales of its groups of eight keys.
+    int group = 0, ids = 0, ids_next = 0, load_u = 0, load_u1 = 0;
+    auto use = [&](int raw) {
+        const bool out = raw < 0 || raw >= a.n_blocks;
+        bad_id |= out && raw != INT32_MIN;
+        ids = out ? (int)a.n_blocks : raw;  // past the end: the copy reads nothing and writes zeros
+    };
+    auto load = [&]() {
+        if (load_u == load_u1) {
+            if (n_taken == n_made) return;
+            const Item& it = queue_s[warp][n_taken % kItems];
+            load_u = it.u0;
+            load_u1 = it.u1;
+            group = (load_u * kKeys >> a.bs_log) >> 5;
+            use(first_ids);
+            ids_next = fetch_ids(a, it, group + 1);
+            ++n_taken;
+            find();
+        }
+        const Item& it = queue_s[warp][(n_taken - 1) % kItems];
+        const int key0 = load_u++ * kKeys, b0 = key0 >> a.bs_log, head = it.h;
+        if (b0 >> 5 != group) {
+            use(ids_next);
+            group = b0 >> 5;
+            ids_next = fetch_ids(a, it, group + 1);
+        }
+        const uint32_t bar = bar0 + 8 * to_load, dst = ring + to_load * Sh::kStage;
+        if (one_lane)
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)Sh::kStage) : "memory");
+        auto copy = [&](int id, int within, uint32_t at) {
+            if (!one_lane) return;
+            asm volatile(
+                "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(at),
+                "l"(&maps.k), "r"(0), "r"(head), "r"(within), "r"(id), "r"(bar)
+                : "memory");
+            asm volatile(
+                "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(at + Sh::kTile),
+                "l"(&maps.v), "r"(0), "r"(head), "r"(within), "r"(id), "r"(bar)
+                : "memory");
         };
-        int group = -1, ids = 0, ids_next = 0;
-        auto use = [&](int raw) {
-            const bool out = raw < 0 || raw >= a.n_blocks;
-            bad_id |= out && raw != INT32_MIN;
-            ids = out ? (int)a.n_blocks : raw;  // past the end: the copy reads nothing and writes zeros
-        };
-        auto load = [&](int u) {  // tile u of the sequence: a copy of keys and one of values per page
-            const int key0 = u * kKeys, b0 = key0 >> a.bs_log;
-            if (b0 >> 5 != group) {
-                use(group >= 0 ? ids_next : fetch(b0 >> 5));
-                group = b0 >> 5;
-                ids_next = fetch(group + 1);
-            }
-            const uint32_t bar = bar0 + 8 * to_load, dst = ring + to_load * Sh::kStage;
-            if (one_lane)
-                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((uint32_t)Sh::kStage) : "memory");
-            auto copy = [&](int id, int within, uint32_t at) {
-                if (!one_lane) return;
-                asm volatile(
-                    "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(at),
-                    "l"(&maps.k), "r"(0), "r"(it.h), "r"(within), "r"(id), "r"(bar)
-                    : "memory");
-                asm volatile(
-                    "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(at + Sh::kTile),
-                    "l"(&maps.v), "r"(0), "r"(it.h), "r"(within), "r"(id), "r"(bar)
-                    : "memory");
-            };
-            auto pages = [&](auto n) {
-                constexpr int N = decltype(n)::value;
-                int id[N];
+        auto pages = [&](auto n) {
+            constexpr int N = decltype(n)::value;
+            int id[N];
 #pragma unroll
-                for (int i = 0; i < N; ++i) id[i] = __shfl_sync(0xffffffffu, ids, (b0 + i) & 31);
+            for (int i = 0; i < N; ++i) id[i] = __shfl_sync(0xffffffffu, ids, (b0 + i) & 31);
 #pragma unroll
-                for (int i = 0; i < N; ++i) copy(id[i], N == 1 ? key0 & (bs - 1) : 0, dst + i * (Sh::kTile / N));
-            };
-            if (bs == 16) pages(std::integral_constant<int, 2>());
-            else if (bs == 8) pages(std::integral_constant<int, 4>());
-            else pages(std::integral_constant<int, 1>());
-            // the scales of four groups of eight keys, and of their values
-            const int key = key0 + 8 * (lane & 3), id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
-            if (lane < 8) {
-                const bool there = id < a.n_blocks && key + 8 > it.begin && key < it.end;
-                copy4(ring_scales + to_load * 64 + 4 * lane, (lane < 4 ? a.k_scale : a.v_scale) + (there ? (int64_t)id * a.n_kv_heads + it.h : 0), there);
-            }
-            if (++to_load == Sh::kStages) to_load = 0;
+            for (int i = 0; i < N; ++i) copy(id[i], N == 1 ? key0 & (bs - 1) : 0, dst + i * (Sh::kTile / N));
         };
-        const int u0 = tile0 + lo, u1 = tile0 + hi;
+        if (bs >= kKeys) pages(std::integral_constant<int, 1>());
+        else if (bs == 16) pages(std::integral_constant<int, kKeys / 16>());
+        else if (bs == 8) pages(std::integral_constant<int, kKeys / 8>());
+        else pages(std::integral_constant<int, kKeys / 32>());
+        const int key = key0 + 8 * (lane & (kG - 1)), id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
+        if (lane < 2 * kG) {
+            const bool there = id < a.n_blocks && key + 8 > it.begin && key < it.end;
+            copy4(ring_scales + to_load * Sh::kScale + 4 * lane, (lane < kG ? a.k_scale : a.v_scale) + (there ? (int64_t)id * a.n_kv_heads + head : 0), there);
+        }
+        if (++to_load == Sh::kStages) to_load = 0;
+    };
+
+    find();
 #pragma unroll 1
-        for (int i = 0; i < Sh::kStages; ++i) {
-            if (u0 + i < u1) load(u0 + i);
-            copies_end();
-        }
-
-        // ---- queries: row 8 nt + g as an operand, rows 8 nt + 2 c and the next as columns of the results
+    for (int i = 0; i < Sh::kStages; ++i) {
+        load();
+        copies_end();
+    }
+    // The copies run ahead of the products by the ring's places, across items.
+#pragma unroll 1
+    for (uint32_t n_done = 0; n_done < n_made && ok; ++n_done) {
+        const Item& it = queue_s[warp][n_done % kItems];
         uint32_t qb[NT][kSteps][2];
         float c_row[NT][2];              // scale of a row's scores, to log2
         int k0[NT][2], k1[NT][2];        // keys that a row sees
-        int all0 = it.begin, all1 = it.end;  // keys that all rows see
+        int all0, all1;                  // keys that all rows see
+        bool large;                      // a product with a scale may pass fp32
+        float o[NT][kDims][4], m[NT][2], l[NT][2], vref = 0x1p-100f, inv_ref = 0.0f;
+        all0 = it.begin;
+        all1 = it.end;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -546,12 +646,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
         }
         all0 = __reduce_max_sync(0xffffffffu, all0);
         all1 = __reduce_min_sync(0xffffffffu, all1);
-        bool large = false;  // a product with a scale may pass fp32
+        large = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) large |= c_row[nt][0] > 1.0f || c_row[nt][1] > 1.0f;
         large = __any_sync(0xffffffffu, large);
 
-        float o[NT][kDims][4], m[NT][2], l[NT][2], vref = 0x1p-100f, inv_ref = 0.0f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -562,43 +661,46 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
             l[nt][0] = l[nt][1] = 0.0f;
         }
 #pragma unroll 1
-        for (int u = u0; u < u1; ++u) {
-            const uint32_t st = ring + stage * Sh::kStage, sc = ring_scales + stage * 64;
+        for (int u = it.u0, u1 = it.u1, u_first = it.u0; u < u1; ++u) {
+            const uint32_t st = ring + stage * Sh::kStage, sc = ring_scales + stage * Sh::kScale;
             copies_wait<Sh::kStages - 1>();
             ok = __all_sync(0xffffffffu, scoot_dev::mbar_wait_tries(bar0 + 8 * stage, phase));
             __syncwarp();
             if (!ok) break;
-            uint32_t ks[4], vs[4];
-            lds<4>(sc, ks);
-            lds<4>(sc + 16, vs);
-            if (lane < 8) {
+            uint32_t ks[kG], vs[kG];
+#pragma unroll
+            for (int t = 0; t < kG; t += 4) {
+                lds<4>(sc + 4 * t, ks + t);
+                lds<4>(sc + 4 * kG + 4 * t, vs + t);
+            }
+            if (lane < 2 * kG) {
                 float own;
                 asm volatile("ld.shared.f32 %0, [%1];" : "=f"(own) : "r"(sc + 4 * lane));
                 bad_scale |= !(own >= 0.0f && own < INFINITY);
             }
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
+            for (int t = 0; t < kG; ++t) {
                 // (as bits: what is not finite, or negative, is above the others)
                 if (ks[t] >= 0x7F800000u) ks[t] = 0u;
                 if (vs[t] >= 0x7F800000u) vs[t] = 0u;
             }
             // scores: sixteen keys by eight rows a product
-            float x[2][NT][4];
+            float x[kM][NT][4];
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
+            for (int mt = 0; mt < kM; ++mt)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) x[mt][nt][0] = x[mt][nt][1] = x[mt][nt][2] = x[mt][nt][3] = 0.0f;
 #pragma unroll
             for (int half = 0; half < D / 64; ++half) {
-                uint32_t w[2][2][4];
+                uint32_t w[kM][2][4];
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt)
+                for (int mt = 0; mt < kM; ++mt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) lds<4>(st + piece_at<D>(16 * mt + 8 * i + g, D / 64 * c + half), w[mt][i]);
 #pragma unroll
                 for (int s = 0; s < 4; ++s)
 #pragma unroll
-                    for (int mt = 0; mt < 2; ++mt) {
+                    for (int mt = 0; mt < kM; ++mt) {
                         const uint32_t ka[4] = {decode_lo(w[mt][0][s]), decode_lo(w[mt][1][s]), decode_hi(w[mt][0][s]), decode_hi(w[mt][1][s])};
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) mma(x[mt][nt], ka, qb[nt][4 * half + s][0], qb[nt][4 * half + s][1]);
@@ -606,9 +708,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
             }
             // softmax: x[mt][nt][2 i + e] is of key 16 mt + 8 i + g and row 8 nt + 2 c + e
             const bool partial = u * kKeys < all0 || (u + 1) * kKeys > all1;
-            float ck[2][2][NT][2];
+            float ck[kM][2][NT][2];
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
+            for (int mt = 0; mt < kM; ++mt)
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -618,7 +720,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
             if (partial || large) {
                 const int key0 = u * kKeys + g;
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt)
+                for (int mt = 0; mt < kM; ++mt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -637,16 +739,19 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float y = fmaxf(max3(x[0][nt][e] * ck[0][0][nt][e], x[0][nt][2 + e] * ck[0][1][nt][e], x[1][nt][e] * ck[1][0][nt][e]),
-                                    x[1][nt][2 + e] * ck[1][1][nt][e]);
+                    float y = fmaxf(x[0][nt][e] * ck[0][0][nt][e], x[0][nt][2 + e] * ck[0][1][nt][e]);
+#pragma unroll
+                    for (int mt = 1; mt < kM; ++mt) y = max3(y, x[mt][nt][e] * ck[mt][0][nt][e], x[mt][nt][2 + e] * ck[mt][1][nt][e]);
                     y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 4));
                     y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 8));
                     y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 16));
                     mx[nt][e] = y;
                     grown |= y > m[nt][e] + 8.0f;
                 }
-            const float vmax = fmaxf(max3(__uint_as_float(vs[0]), __uint_as_float(vs[1]), __uint_as_float(vs[2])), __uint_as_float(vs[3]));
-            if (u == u0) {
+            float vmax = fmaxf(__uint_as_float(vs[0]), __uint_as_float(vs[1]));
+#pragma unroll
+            for (int t = 2; t < kG; t += 2) vmax = max3(vmax, __uint_as_float(vs[t]), __uint_as_float(vs[t + 1]));
+            if (u == u_first) {
                 vref = fmaxf(vmax, 0x1p-100f);
                 inv_ref = 128.0f / vref;
 #pragma unroll
@@ -676,13 +781,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                 inv_ref = 128.0f / vref;
             }
             // P of sixteen keys by eight rows, turned round to be the other operand: lane (g, c) gets keys 2 c and the next of row g
-            uint32_t pb[2][NT][2];
+            uint32_t pb[kM][NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const float2 ms = make_float2(-finite_or_zero(m[nt][0]), -finite_or_zero(m[nt][1]));
                 float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int mt = 0; mt < 2; ++mt)
+                for (int mt = 0; mt < kM; ++mt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const float f = __uint_as_float(vs[2 * mt + i]) * inv_ref;
@@ -699,7 +804,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
             }
             // values: sixteen dimensions by eight rows a product
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt) {
+            for (int mt = 0; mt < kM; ++mt) {
                 constexpr int kW = D / 32;  // words of a key's piece
                 uint32_t w[4][kW];
 #pragma unroll
@@ -724,27 +829,22 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                 }
             }
             __syncwarp();  // the tile has been read
-            if (u + Sh::kStages < u1) load(u + Sh::kStages);
-            copies_end();
             if (++stage == Sh::kStages) {
                 stage = 0;
                 phase ^= 1u;
             }
+            load();
+            copies_end();
         }
-        if (!ok) {  // a copy did not come: what is under way lands before the block ends
-            if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
-            failed = 1;
-#pragma unroll 1
-            for (int i = 0; i < Sh::kStages; ++i)
-                if (i != (int)stage) scoot_dev::mbar_wait_tries(bar0 + 8 * i, i < (int)stage ? phase ^ 1u : phase);
-            break;
-        }
-
+        if (!ok) break;
         // ---- the end of the item: the lane has 16 (8) dimensions in a row of rows 8 nt + 2 c and the next
         const bool whole = it.n_parts == 1;
-        const bool begins = it.first == worker;
+        const bool begins = it.first == team;
         float* part = a.parts + (size_t)(2 * worker + begins) * Sh::kPart;
-        if (!whole && lane == 0 && (begins || warp == 0)) items[begins ? 1 + warp : 0] = it;
+        if (it.n_parts > kFewParts && lane == 0) {
+            many = 1;
+            if (begins || warp < a.share) items[begins ? kShare + warp : member] = it;
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -775,56 +875,73 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                     if (g == 0) reinterpret_cast<float2*>(part + kRows * D)[row] = make_float2(m[nt][e], l[nt][e]);
                 }
             }
+        if (!whole && it.n_parts <= kFewParts) {
+            __syncwarp();
+            bool last = false;
+            if (lane == 0) {
+                __threadfence();  // (the warp's other lanes' stores are before it)
+                uint32_t* count = a.warp_count + it.first * a.share + member;
+                last = atomicAdd(count, 1u) == (uint32_t)it.n_parts - 1;
+                if (last) *count = 0;
+                __threadfence();
+            }
+            if (__any_sync(0xffffffffu, last)) {
+                __syncwarp();
+                join<kBf16, D, kRows, 32, 4, 2>(a, &it, 1, it.rows * (D / 4), lane, [&](int, float*&) {
+                    return parts_at(it.first, it.first, member, it.n_parts);
+                });
+            }
+        }
+    }
+    if (!ok) {  // a copy did not come: what is under way lands before the block ends
+        if (lane == 0) atomicOr(a.err, SCOOT_DEVERR_TIMEOUT);
+        failed = 1;
+#pragma unroll 1
+        for (int i = 0; i < Sh::kStages; ++i)
+            if (i != (int)stage) scoot_dev::mbar_wait_tries(bar0 + 8 * i, i < (int)stage ? phase ^ 1u : phase);
     }
     if (bad_id) atomicOr(a.err, SCOOT_DEVERR_INDEX);
     if (bad_scale) atomicOr(a.err, SCOOT_DEVERR_VALUE);
 
     // ---- split items: the block's parts of each, then the blocks'
     __syncthreads();
-    if (failed) return;
-    const int w0 = blockIdx.x * kWarps, w1 = w0 + kWarps - 1;
-    float* joined = a.parts + (size_t)2 * n_workers * Sh::kPart;  // two per block
+    if (failed || !many) return;
+    const int teams = kWarps / a.share, t0 = blockIdx.x * teams, t1 = t0 + teams - 1;
+    float* joined = a.parts + (size_t)2 * n_workers * Sh::kPart;  // 2 kShare per block
     int rows = 0;
 #pragma unroll 1
-    for (int i = 0; i <= kWarps; ++i) rows += items[i].n_parts ? items[i].rows : 0;
+    for (int i = 0; i < kShare + kWarps; ++i) rows += items[i].n_parts ? items[i].rows : 0;
     const auto source = [&](int i, float*& to) {
         const Item& it = items[i];
-        const int first = max(it.first, w0), n = min(it.first + it.n_parts - 1, w1) - first + 1;
-        if (n < it.n_parts) to = joined + (size_t)(2 * blockIdx.x + (it.first >= w0 ? 1 : 0)) * Sh::kPart;
-        return Parts{a.parts + (size_t)(2 * first + (first == it.first ? 1 : 0)) * Sh::kPart, a.parts + (size_t)(2 * first + 2) * Sh::kPart,
-                     2 * Sh::kPart, n};
+        const int first = max(it.first, t0), n = min(it.first + it.n_parts - 1, t1) - first + 1, who = it.h % a.share;
+        if (n < it.n_parts) to = joined + (size_t)((2 * blockIdx.x + (it.first >= t0 ? 1 : 0)) * kShare + who) * Sh::kPart;
+        return parts_at(first, it.first, who, n);
     };
-    if (rows * (D / 4) <= kThreads) join<kBf16, D, kRows, kThreads, 1, 8>(a, items, kWarps + 1, rows * (D / 4), source);
-    else join<kBf16, D, kRows, kThreads, 4, 2>(a, items, kWarps + 1, rows * (D / 4), source);
+    if (rows * (D / 4) <= kThreads) join<kBf16, D, kRows, kThreads, 1, 8>(a, items, kShare + kWarps, rows * (D / 4), tid, source);
+    else join<kBf16, D, kRows, kThreads, 4, 2>(a, items, kShare + kWarps, rows * (D / 4), tid, source);
     __syncthreads();
-    // The item that came in, and the one that goes on in the next block.
-    if (tid == 0) {
-        int out = -1;
-#pragma unroll 1
-        for (int i = 1; i <= kWarps; ++i)
-            if (items[i].n_parts && items[i].first + items[i].n_parts - 1 > w1) out = i;
-        last_s[0] = last_s[1] = -1;
-        if (items[0].n_parts || out > 0) {
+    // Of the items that lie in other blocks as well: whether this was the last.
+    if (tid < kShare + kWarps) {
+        const Item& it = items[tid];
+        bool last = false;
+        if (it.n_parts && (it.first < t0 || it.first + it.n_parts - 1 > t1)) {
             __threadfence();  // (the block's other threads' stores are before it by the barrier)
-            for (int side = 0; side < 2; ++side) {
-                const int i = side ? out : 0;
-                if (i < 0 || items[i].n_parts == 0) continue;
-                const int b0 = items[i].first / kWarps, b1 = (items[i].first + items[i].n_parts - 1) / kWarps;
-                if (atomicAdd(a.count + b0, 1u) != (uint32_t)(b1 - b0)) continue;
-                a.count[b0] = 0;
-                last_s[side] = i;
-            }
+            const int b0 = it.first / teams, b1 = (it.first + it.n_parts - 1) / teams;
+            uint32_t* count = a.block_count + b0 * kShare + it.h % a.share;
+            last = atomicAdd(count, 1u) == (uint32_t)(b1 - b0);
+            if (last) *count = 0;
             __threadfence();
         }
+        last_s[tid] = last;
     }
     __syncthreads();
 #pragma unroll 1
-    for (int side = 0; side < 2; ++side) {
-        const int i = last_s[side];
-        if (i < 0) continue;
-        join<kBf16, D, kRows, kThreads, 1, 8>(a, items + i, 1, items[i].rows * (D / 4), [&](int, float*&) {
-            const int b0 = items[i].first / kWarps, b1 = (items[i].first + items[i].n_parts - 1) / kWarps;
-            return Parts{joined + (size_t)(2 * b0 + 1) * Sh::kPart, joined + (size_t)(2 * b0 + 2) * Sh::kPart, 2 * Sh::kPart, b1 - b0 + 1};
+    for (int i = 0; i < kShare + kWarps; ++i) {
+        if (!last_s[i]) continue;
+        join<kBf16, D, kRows, kThreads, 1, 8>(a, items + i, 1, items[i].rows * (D / 4), tid, [&](int, float*&) {
+            const int b0 = items[i].first / teams, b1 = (items[i].first + items[i].n_parts - 1) / teams, who = items[i].h % a.share;
+            return Parts{joined + (size_t)((2 * b0 + 1) * kShare + who) * Sh::kPart, joined + (size_t)((2 * b0 + 2) * kShare + who) * Sh::kPart,
+                         2 * kShare * Sh::kPart, b1 - b0 + 1};
         });
     }
 }
@@ -892,6 +1009,12 @@ extern "C" scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_la
     const int row_tiles = G <= 8 ? 1 : 2, item_rows = 8 * row_tiles;
     a.toks = G <= item_rows ? item_rows / G : 1;
     a.per_token = (G + item_rows - 1) / item_rows;
+    // Heads of the same tokens lie side by side in most caches: together they are read at 5.7 TB/s, one after the other at 4.7
+    // (256 sequences, 8 heads of 128).  With fewer items than warps each is split into many parts instead, whose joins would fall
+    // to the same blocks: three long sequences of 4 heads take 45 us alone, 76 together.
+    const int warps = row_tiles == 1 ? Shape<64, 1>::kWarps : Shape<64, 2>::kWarps;
+    a.share = (int64_t)n_req * layout->n_kv_heads < (int64_t)sms * warps ? 1 : kShare;
+    while (layout->n_kv_heads % a.share) a.share /= 2;
     a.n_tokens = n_tokens;
     a.n_blocks = layout->n_blocks;
     a.query_start = query_start;
@@ -913,14 +1036,15 @@ extern "C" scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_la
     a.out_ld_token = out_ld_token;
     a.out_ld_head = out_ld_head;
     a.lse = lse;
-    a.count = ctx->d_count + 2 * kMaxBlocks;
+    a.warp_count = ctx->d_count + kWarpCounts;
+    a.block_count = ctx->d_count + kBlockCounts;
     a.tile_count = ctx->d_count;
     a.err = ctx->d_err;
     a.few = kFewRows / G;
     // The host does not know the lengths: without max_new both kernels are launched, and one may find nothing to do.
     const bool rows = a.few > 0, tiles = max_new == 0 || max_new > a.few;
     const size_t part = (size_t)item_rows * (D + 2) * sizeof(float);
-    const size_t row_bytes = rows ? (size_t)sms * 2 * ((row_tiles == 1 ? Shape<64, 1>::kWarps : Shape<64, 2>::kWarps) + 1) * part : 0;
+    const size_t row_bytes = rows ? (size_t)sms * 2 * (warps + kShare) * part : 0;
     s = scoot_workspace(ctx, row_bytes + (tiles ? sms * scoot_attn8_tile_bytes(D) : 0), stream);
     if (s != SCOOT_OK) return s;
     a.parts = static_cast<float*>(ctx->ws);
@@ -929,7 +1053,8 @@ extern "C" scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_la
     const bool bf16 = dtype == SCOOT_BF16;
     if (rows) {
         KvMaps maps;
-        if (!scoot_encode_codes(&maps.k, layout, k_cache, kKeys) || !scoot_encode_codes(&maps.v, layout, v_cache, kKeys))
+        const int keys = D == 128 ? Shape<128, 1>::kKeys : Shape<64, 1>::kKeys;
+        if (!scoot_encode_codes(&maps.k, layout, k_cache, keys) || !scoot_encode_codes(&maps.v, layout, v_cache, keys))
             return scoot_fail(ctx, SCOOT_EINVAL, "the cache's layout has no tensor map");
         s = row_tiles == 1 ? launch<1>(ctx, a, maps, bf16, D, sms, st) : launch<2>(ctx, a, maps, bf16, D, sms, st);
         if (s != SCOOT_OK) return s;

@@ -9,6 +9,7 @@ struct Attn8Args {
     int32_t bs_log, n_heads, n_kv_heads, group, n_req, causal, window, max_new;
     int32_t few;               // requests of up to so many tokens are the rows kernel's, the others the tiles kernel's
     int32_t toks, per_token;   // rows kernel: tokens of an item, and items of a token (more than one: groups of more than 16 heads)
+    int32_t share;             // rows kernel: heads that as many warps take together
     int64_t n_tokens, n_blocks;
     const int32_t* query_start;
     const int32_t* kv_len;
@@ -26,7 +27,8 @@ struct Attn8Args {
     int64_t out_ld_token, out_ld_head;
     float* lse;
     float* parts;              // two per warp, then two per block
-    uint32_t* count;           // arrivals of blocks per split item, zero between calls
+    uint32_t* warp_count;      // arrivals per split item, by its first warp, zero between calls
+    uint32_t* block_count;     // likewise of blocks
     float* tile_parts;         // the tiles kernel's
     uint32_t* tile_count;
     uint32_t* err;
