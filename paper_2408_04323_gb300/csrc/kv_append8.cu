@@ -20,7 +20,7 @@ using namespace scoot_dev;
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxWindow = 32;   // tokens among which a block of threads looks for the first ones of its runs
 constexpr int kMaxBlock = 256;   // the largest block_size
-constexpr int kSteps = 4;        // steps of a run whose numbers stay in registers between the two looks at them
+constexpr int kPer = 2;          // queries' tasks of a thread under way at once
 constexpr int kWords = (kMaxWindow + kMaxBlock) / 32 + 1;
 
 struct Append8Args {
@@ -61,21 +61,43 @@ __device__ __forceinline__ float least_scale(float amax) {
     return __uint_as_float((uint32_t)max(e, 27) << 23);
 }
 
+// A lane's sixteen numbers of a token: the chunks at ca and cb of a head's row at p, turned if they are keys.
+template <bool kBf16>
+__device__ __forceinline__ void load(const Append8Args& a, const uint16_t* p, int ca, int cb, const float4* cs, int j, bool turn, float* x) {
+    Rotation rot = a.rot;
+    if (!turn) rot.turned = 0;
+    turn_task<kBf16>(rot, cs, j, *reinterpret_cast<const uint4*>(p + ca), *reinterpret_cast<const uint4*>(p + cb), x, x + 8);
+}
+__device__ __forceinline__ void largest(const float* x, float& top, float& nan) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        top = fmaxf(top, fabsf(x[e]));
+        nan = fmaf(x[e], 0.0f, nan);
+    }
+}
+__device__ __forceinline__ void finite(float* x) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        if (!(fabsf(x[e]) < INFINITY)) x[e] = 0.0f;
+}
+
 // Tokens of a batch in one block follow one another, a run: slots s, s + 1, ..  A block of threads takes the runs that begin
 // among its `window` tokens: the cosines and sines of their tokens, their queries, and then, a warp per (run, head), keys
 // and values: D / 16 lanes per token, each with a task's 16 dimensions, and so 32 / (D / 16) tokens a step.  A warp has the
 // scale to itself: no atomics, and no order to depend on.
 template <bool kBf16, int D>
-__global__ void __launch_bounds__(kThreads) kv_append8_kernel(const Append8Args a) {
+__global__ void __launch_bounds__(kThreads, 4) kv_append8_kernel(const Append8Args a) {
     constexpr int kTasks = D / 16, kTokens = 32 / kTasks;
     extern __shared__ float4 cs[];
     __shared__ uint32_t goes_on[kWords], begins[kWords];  // bit i: token t0 + i continues a run; begins one
     __shared__ int run_at[kMaxWindow], run_n[kMaxWindow];
     __shared__ int n_runs, last;
+    __shared__ bool mine[kMaxWindow + kMaxBlock];         // token t0 + i is of a run that begins here
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t t0 = (int64_t)blockIdx.x * a.window;
     const int bs = 1 << a.bs_log;
     if (tid == 0) n_runs = last = 0;
+    for (int i = tid; i < a.window + bs; i += kThreads) mine[i] = false;
     for (int i = tid; i < kWords * 32; i += kThreads) {  // (whole warps)
         bool on = false, first = false;
         if (i < a.window + bs && t0 + i < a.n_tokens) {
@@ -107,19 +129,10 @@ __global__ void __launch_bounds__(kThreads) kv_append8_kernel(const Append8Args 
         run_at[at] = tid;
         run_n[at] = n;
         atomicMax(&last, tid + n);
+        for (int i = 0; i < n; ++i) mine[tid + i] = true;
     }
     __syncthreads();
     const int end = last, pairs = 8 * a.rot.turned;
-    auto mine = [&](int i) {  // whether token t0 + i is of a run that begins here
-        if (begins[i >> 5] >> (i & 31) & 1u) return i < a.window;
-        if (!(goes_on[i >> 5] >> (i & 31) & 1u)) return false;
-        for (int w = i >> 5;; --w) {  // its run's first token
-            uint32_t b = begins[w];
-            if (w == i >> 5) b &= (2u << (i & 31)) - 1u;
-            if (b) return w * 32 + 31 - __clz(b) < a.window;
-            if (w == 0) return false;
-        }
-    };
     if (a.rot.turned) {
         for (int e = tid; e < end * pairs; e += kThreads) {
             const int t = e / pairs, pair = e - t * pairs;
@@ -127,29 +140,42 @@ __global__ void __launch_bounds__(kThreads) kv_append8_kernel(const Append8Args 
         }
         __syncthreads();
         const uint32_t per_token = (uint32_t)a.n_heads * kTasks, all = end * per_token;
-        for (uint32_t e = tid; e < all; e += kThreads) {
-            const uint32_t t = e / per_token, c = e - t * per_token;
-            if (!mine((int)t)) continue;
-            const int head = (int)(c / kTasks), j = (int)(c % kTasks);
-            const uint16_t* p = a.q + (t0 + t) * a.q_ld_token + head * a.q_ld_head;
-            uint16_t* y = a.y + (t0 + t) * a.y_ld_token + head * a.y_ld_head;
+#pragma unroll 1
+        for (uint32_t e0 = tid; e0 < all; e0 += kPer * kThreads) {
+            uint4 ra[kPer], rb[kPer];
+            uint16_t* y[kPer];
+            int tok[kPer];
+            const int j = (int)(e0 % kTasks);  // (of all of the thread's tasks: kThreads is a multiple)
             const int ca = 8 * a.rot.chunk_a(j), cb = 8 * a.rot.chunk_b(j);
-            uint4 ra = *reinterpret_cast<const uint4*>(p + ca), rb = *reinterpret_cast<const uint4*>(p + cb);
-            if (j < a.rot.turned) {
-                float x[8], z[8];
-                turn_task<kBf16>(a.rot, cs + t * (pairs / 2), j, ra, rb, x, z);
-                ra = make_uint4(pack16_rn<kBf16>(x[0], x[1]), pack16_rn<kBf16>(x[2], x[3]), pack16_rn<kBf16>(x[4], x[5]), pack16_rn<kBf16>(x[6], x[7]));
-                rb = make_uint4(pack16_rn<kBf16>(z[0], z[1]), pack16_rn<kBf16>(z[2], z[3]), pack16_rn<kBf16>(z[4], z[5]), pack16_rn<kBf16>(z[6], z[7]));
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const uint32_t e = e0 + i * kThreads, t = e / per_token;
+                y[i] = nullptr;
+                if (e >= all || !mine[t]) continue;
+                const int head = (int)((e - t * per_token) / kTasks);
+                const uint16_t* p = a.q + (t0 + t) * a.q_ld_token + head * a.q_ld_head;
+                y[i] = a.y + (t0 + t) * a.y_ld_token + head * a.y_ld_head;
+                tok[i] = (int)t;
+                ra[i] = *reinterpret_cast<const uint4*>(p + ca);
+                rb[i] = *reinterpret_cast<const uint4*>(p + cb);
             }
-            *reinterpret_cast<uint4*>(y + ca) = ra;
-            *reinterpret_cast<uint4*>(y + cb) = rb;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                if (!y[i]) continue;
+                if (j < a.rot.turned) {
+                    float x[8], z[8];
+                    turn_task<kBf16>(a.rot, cs + tok[i] * (pairs / 2), j, ra[i], rb[i], x, z);
+                    ra[i] = make_uint4(pack16_rn<kBf16>(x[0], x[1]), pack16_rn<kBf16>(x[2], x[3]), pack16_rn<kBf16>(x[4], x[5]), pack16_rn<kBf16>(x[6], x[7]));
+                    rb[i] = make_uint4(pack16_rn<kBf16>(z[0], z[1]), pack16_rn<kBf16>(z[2], z[3]), pack16_rn<kBf16>(z[4], z[5]), pack16_rn<kBf16>(z[6], z[7]));
+                }
+                *reinterpret_cast<uint4*>(y[i] + ca) = ra[i];
+                *reinterpret_cast<uint4*>(y[i] + cb) = rb[i];
+            }
         }
     }
 
     const int sub = lane / kTasks, j = lane % kTasks;
-    const int units = n_runs * a.n_kv_heads;
-    Rotation none = a.rot;
-    none.turned = 0;
+    const int units = n_runs * a.n_kv_heads, ka = 8 * a.rot.chunk_a(j), kb = 8 * a.rot.chunk_b(j);
     bool odd = false;
 #pragma unroll 1
     for (int u = warp; u < units; u += kWarps) {
@@ -157,62 +183,58 @@ __global__ void __launch_bounds__(kThreads) kv_append8_kernel(const Append8Args 
         const int at = run_at[r], n = run_n[r];
         const int64_t t1 = t0 + at, s1 = a.slot[t1], block = s1 >> a.bs_log;
         const int in_block = (int)(s1 & (bs - 1));
+        const int64_t scale_at = block * a.n_kv_heads + head;
+        const uint16_t* src[2] = {a.kv[0] + t1 * a.kv_ld_token[0] + head * a.kv_ld_head[0], a.kv[1] + t1 * a.kv_ld_token[1] + head * a.kv_ld_head[1]};
+        const int64_t to = block * a.ld_block + in_block * a.ld_token + head * a.ld_head;
+        // (a power of two may be any number where the caller made the scale)
+        float held = 0.0f;  // lanes 0 and 1: of keys and of values
+        if (in_block && lane < 2) held = a.scale[lane][scale_at];
+        // Twice over the run's numbers, the second time from L1: once for the largest, once for the codes.
+        float top[2] = {0.0f, 0.0f}, nan[2] = {0.0f, 0.0f};
 #pragma unroll 1
+        for (int t = sub; t < n; t += kTokens) {
+            float x[16];
+            load<kBf16>(a, src[0] + t * a.kv_ld_token[0], ka, kb, cs + (at + t) * (pairs / 2), j, true, x);
+            largest(x, top[0], nan[0]);
+            load<kBf16>(a, src[1] + t * a.kv_ld_token[1], 16 * j, 16 * j + 8, nullptr, j, false, x);
+            largest(x, top[1], nan[1]);
+        }
+        float inv[2];
+        bool bad[2];
+#pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
-            const Rotation rot = kv == 0 ? a.rot : none;
-            const int ca = 8 * rot.chunk_a(j), cb = 8 * rot.chunk_b(j);
-            float* scale_at = a.scale[kv] + block * a.n_kv_heads + head;
-            const float held = in_block ? __shfl_sync(0xffffffffu, lane == 0 ? *scale_at : 0.0f, 0) : 0.0f;
-            const uint16_t* src = a.kv[kv] + t1 * a.kv_ld_token[kv] + head * a.kv_ld_head[kv];
-            uint8_t* cache = a.cache[kv] + block * a.ld_block + head * a.ld_head;
-            uint4 ra[kSteps], rb[kSteps];
-            auto load = [&](int i0) {
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i) {
-                    const int t = i0 + i * kTokens + sub;
-                    ra[i] = rb[i] = make_uint4(0, 0, 0, 0);
-                    if (t < n) {
-                        const uint16_t* p = src + t * a.kv_ld_token[kv];
-                        ra[i] = *reinterpret_cast<const uint4*>(p + ca);
-                        rb[i] = *reinterpret_cast<const uint4*>(p + cb);
-                    }
-                }
-            };
-            // step i's numbers, those that are not finite as zeros
-            auto numbers = [&](int i, int t, float* x) {
-                turn_task<kBf16>(rot, cs + (at + min(t, n - 1)) * (pairs / 2), j, ra[i], rb[i], x, x + 8);
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (!(fabsf(x[e]) < INFINITY)) {
-                        x[e] = 0.0f;
-                        odd = true;
-                    }
-            };
-            float top = 0.0f;
-#pragma unroll 1
-            for (int i0 = 0; i0 < n; i0 += kSteps * kTokens) {
-                load(i0);
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i) {
+            bad[kv] = __any_sync(0xffffffffu, nan[kv] != 0.0f);  // (0 times what is not finite is NaN)
+            if (bad[kv]) {                                       // once more, without it
+                odd = true;
+                top[kv] = 0.0f;
+                for (int t = sub; t < n; t += kTokens) {
                     float x[16];
-                    numbers(i, i0 + i * kTokens + sub, x);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(x[e]));
+                    if (kv == 0) load<kBf16>(a, src[0] + t * a.kv_ld_token[0], ka, kb, cs + (at + t) * (pairs / 2), j, true, x);
+                    else load<kBf16>(a, src[1] + t * a.kv_ld_token[1], 16 * j, 16 * j + 8, nullptr, j, false, x);
+                    finite(x);
+                    largest(x, top[kv], nan[kv]);
                 }
             }
+        }
 #pragma unroll
-            for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            float s = least_scale(top);
+        for (int d = 16; d > 0; d >>= 1) {
+            top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], d));
+            top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], d));
+        }
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            float s = least_scale(top[kv]);
             if (in_block) {
-                const bool bad = !(held >= 0.0f && held < INFINITY);
-                odd |= bad;
-                if (held >= s && !bad) {
-                    s = held;
+                const float h = __shfl_sync(0xffffffffu, held, kv);
+                const bool wrong = !(h >= 0.0f && h < INFINITY);
+                odd |= wrong;
+                if (h >= s && !wrong) {
+                    s = h;
                 } else {
                     // the scale has grown: the older tokens' codes by the growth
-                    const float f = bad ? 0.0f : held / s;
+                    const float f = wrong ? 0.0f : h / s;
                     for (int i = sub; i < in_block; i += kTokens) {
-                        uint4* p = reinterpret_cast<uint4*>(cache + i * a.ld_token + 16 * j);
+                        uint4* p = reinterpret_cast<uint4*>(a.cache[kv] + to + (int64_t)(i - in_block) * a.ld_token + 16 * j);
                         const uint4 w = *p;
                         auto again = [&](uint32_t v) {
                             const float2 lo = decode2(v & 0xFFFFu), hi = decode2(v >> 16);
@@ -222,26 +244,26 @@ __global__ void __launch_bounds__(kThreads) kv_append8_kernel(const Append8Args 
                     }
                 }
             }
-            if (lane == 0) *scale_at = s;
-            const float inv = 1.0f / s;  // (a scale that was held may be any number)
+            if (lane == 0) a.scale[kv][scale_at] = s;
+            inv[kv] = 1.0f / s;
+        }
+        auto store = [&](int kv, int t, int ca, int cb, float* x) {
+            if (bad[kv]) finite(x);
+            uint8_t* p = a.cache[kv] + to + t * a.ld_token;
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[e] = encode2(x[4 * e] * inv[kv], x[4 * e + 1] * inv[kv]) | encode2(x[4 * e + 2] * inv[kv], x[4 * e + 3] * inv[kv]) << 16;
+            *reinterpret_cast<uint2*>(p + ca) = make_uint2(w[0], w[1]);
+            *reinterpret_cast<uint2*>(p + cb) = make_uint2(w[2], w[3]);
+        };
 #pragma unroll 1
-            for (int i0 = 0; i0 < n; i0 += kSteps * kTokens) {
-                if (n > kSteps * kTokens) load(i0);
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i) {
-                    const int t = i0 + i * kTokens + sub;
-                    float x[16];
-                    numbers(i, t, x);
-                    if (t >= n) continue;
-                    uint8_t* p = cache + (in_block + t) * a.ld_token;
-                    uint32_t w[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        w[e] = encode2(x[4 * e] * inv, x[4 * e + 1] * inv) | encode2(x[4 * e + 2] * inv, x[4 * e + 3] * inv) << 16;
-                    *reinterpret_cast<uint2*>(p + ca) = make_uint2(w[0], w[1]);
-                    *reinterpret_cast<uint2*>(p + cb) = make_uint2(w[2], w[3]);
-                }
-            }
+        for (int t = sub; t < n; t += kTokens) {
+            float x[16];
+            load<kBf16>(a, src[0] + t * a.kv_ld_token[0], ka, kb, cs + (at + t) * (pairs / 2), j, true, x);
+            store(0, t, ka, kb, x);
+            load<kBf16>(a, src[1] + t * a.kv_ld_token[1], 16 * j, 16 * j + 8, nullptr, j, false, x);
+            store(1, t, 16 * j, 16 * j + 8, x);
         }
     }
     if (odd) atomicOr(a.err, SCOOT_DEVERR_VALUE);
