@@ -17,22 +17,17 @@ namespace {
 
 using namespace scoot_dev;
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = kRotaryThreads, kWarps = kThreads / 32;
 constexpr int kMaxWindow = 32;   // tokens among which a block of threads looks for the first ones of its runs
 constexpr int kMaxBlock = 256;   // the largest block_size
-constexpr int kPer = 2;          // queries' tasks of a thread under way at once
 constexpr int kWords = (kMaxWindow + kMaxBlock) / 32 + 1;
 
 struct Append8Args {
     Rotation rot;               // turned = 0: none
-    int32_t n_heads, n_kv_heads;
-    int32_t bs_log, window;
+    int32_t n_kv_heads, bs_log, window;
+    int64_t kv_blocks;          // blocks of threads that take keys and values; the others queries
     int64_t n_tokens, n_slots;
     const int32_t* position;
-    const uint16_t* q;
-    int64_t q_ld_token, q_ld_head;
-    uint16_t* y;
-    int64_t y_ld_token, y_ld_head;
     const uint16_t* kv[2];
     int64_t kv_ld_token[2], kv_ld_head[2];
     const int64_t* slot;
@@ -40,6 +35,7 @@ struct Append8Args {
     uint8_t* cache[2];
     float* scale[2];
     uint32_t* err;
+    RotaryArgs queries;
 };
 
 // Two numbers as codes (of magnitude 448 at most), and back.
@@ -61,19 +57,11 @@ __device__ __forceinline__ float least_scale(float amax) {
     return __uint_as_float((uint32_t)max(e, 27) << 23);
 }
 
-// A lane's sixteen numbers of a token: the chunks at ca and cb of a head's row at p, turned if they are keys.
-template <bool kBf16>
-__device__ __forceinline__ void load(const Append8Args& a, const uint16_t* p, int ca, int cb, const float4* cs, int j, bool turn, float* x) {
-    Rotation rot = a.rot;
-    if (!turn) rot.turned = 0;
-    turn_task<kBf16>(rot, cs, j, *reinterpret_cast<const uint4*>(p + ca), *reinterpret_cast<const uint4*>(p + cb), x, x + 8);
-}
-__device__ __forceinline__ void largest(const float* x, float& top, float& nan) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        top = fmaxf(top, fabsf(x[e]));
-        nan = fmaf(x[e], 0.0f, nan);
-    }
+// The largest magnitude; NaN if there is one.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
 }
 __device__ __forceinline__ void finite(float* x) {
 #pragma unroll
@@ -81,23 +69,21 @@ __device__ __forceinline__ void finite(float* x) {
         if (!(fabsf(x[e]) < INFINITY)) x[e] = 0.0f;
 }
 
-// Tokens of a batch in one block follow one another, a run: slots s, s + 1, ..  A block of threads takes the runs that begin
-// among its `window` tokens: the cosines and sines of their tokens, their queries, and then, a warp per (run, head), keys
-// and values: D / 16 lanes per token, each with a task's 16 dimensions, and so 32 / (D / 16) tokens a step.  A warp has the
-// scale to itself: no atomics, and no order to depend on.
 template <bool kBf16, int D>
 __global__ void __launch_bounds__(kThreads, 4) kv_append8_kernel(const Append8Args a) {
     constexpr int kTasks = D / 16, kTokens = 32 / kTasks;
     extern __shared__ float4 cs[];
+    if (blockIdx.x >= a.kv_blocks) {
+        rotary_block<kBf16>(a.queries, blockIdx.x - a.kv_blocks, cs);
+        return;
+    }
     __shared__ uint32_t goes_on[kWords], begins[kWords];  // bit i: token t0 + i continues a run; begins one
     __shared__ int run_at[kMaxWindow], run_n[kMaxWindow];
     __shared__ int n_runs, last;
-    __shared__ bool mine[kMaxWindow + kMaxBlock];         // token t0 + i is of a run that begins here
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t t0 = (int64_t)blockIdx.x * a.window;
     const int bs = 1 << a.bs_log;
     if (tid == 0) n_runs = last = 0;
-    for (int i = tid; i < a.window + bs; i += kThreads) mine[i] = false;
     for (int i = tid; i < kWords * 32; i += kThreads) {  // (whole warps)
         bool on = false, first = false;
         if (i < a.window + bs && t0 + i < a.n_tokens) {
@@ -129,7 +115,6 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append8_kernel(const Append8Ar
         run_at[at] = tid;
         run_n[at] = n;
         atomicMax(&last, tid + n);
-        for (int i = 0; i < n; ++i) mine[tid + i] = true;
     }
     __syncthreads();
     const int end = last, pairs = 8 * a.rot.turned;
@@ -139,43 +124,12 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append8_kernel(const Append8Ar
             reinterpret_cast<float2*>(cs)[t * pairs + rotation_place(a.rot, pair)] = rotation_at(a.rot, pair, a.position[t0 + t]);
         }
         __syncthreads();
-        const uint32_t per_token = (uint32_t)a.n_heads * kTasks, all = end * per_token;
-#pragma unroll 1
-        for (uint32_t e0 = tid; e0 < all; e0 += kPer * kThreads) {
-            uint4 ra[kPer], rb[kPer];
-            uint16_t* y[kPer];
-            int tok[kPer];
-            const int j = (int)(e0 % kTasks);  // (of all of the thread's tasks: kThreads is a multiple)
-            const int ca = 8 * a.rot.chunk_a(j), cb = 8 * a.rot.chunk_b(j);
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const uint32_t e = e0 + i * kThreads, t = e / per_token;
-                y[i] = nullptr;
-                if (e >= all || !mine[t]) continue;
-                const int head = (int)((e - t * per_token) / kTasks);
-                const uint16_t* p = a.q + (t0 + t) * a.q_ld_token + head * a.q_ld_head;
-                y[i] = a.y + (t0 + t) * a.y_ld_token + head * a.y_ld_head;
-                tok[i] = (int)t;
-                ra[i] = *reinterpret_cast<const uint4*>(p + ca);
-                rb[i] = *reinterpret_cast<const uint4*>(p + cb);
-            }
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                if (!y[i]) continue;
-                if (j < a.rot.turned) {
-                    float x[8], z[8];
-                    turn_task<kBf16>(a.rot, cs + tok[i] * (pairs / 2), j, ra[i], rb[i], x, z);
-                    ra[i] = make_uint4(pack16_rn<kBf16>(x[0], x[1]), pack16_rn<kBf16>(x[2], x[3]), pack16_rn<kBf16>(x[4], x[5]), pack16_rn<kBf16>(x[6], x[7]));
-                    rb[i] = make_uint4(pack16_rn<kBf16>(z[0], z[1]), pack16_rn<kBf16>(z[2], z[3]), pack16_rn<kBf16>(z[4], z[5]), pack16_rn<kBf16>(z[6], z[7]));
-                }
-                *reinterpret_cast<uint4*>(y[i] + ca) = ra[i];
-                *reinterpret_cast<uint4*>(y[i] + cb) = rb[i];
-            }
-        }
     }
 
     const int sub = lane / kTasks, j = lane % kTasks;
     const int units = n_runs * a.n_kv_heads, ka = 8 * a.rot.chunk_a(j), kb = 8 * a.rot.chunk_b(j);
+    Rotation none = a.rot;
+    none.turned = 0;
     bool odd = false;
 #pragma unroll 1
     for (int u = warp; u < units; u += kWarps) {
@@ -189,33 +143,44 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append8_kernel(const Append8Ar
         // (a power of two may be any number where the caller made the scale)
         float held = 0.0f;  // lanes 0 and 1: of keys and of values
         if (in_block && lane < 2) held = a.scale[lane][scale_at];
-        // Twice over the run's numbers, the second time from L1: once for the largest, once for the codes.
-        float top[2] = {0.0f, 0.0f}, nan[2] = {0.0f, 0.0f};
+        // The lane's sixteen numbers of token t, of keys (turned) or of values.
+        auto numbers = [&](int kv, int t, float* x) {
+            const uint16_t* p = src[kv] + t * a.kv_ld_token[kv];
+            if (kv == 0) turn_task<kBf16>(a.rot, cs + (at + t) * (pairs / 2), j, *reinterpret_cast<const uint4*>(p + ka), *reinterpret_cast<const uint4*>(p + kb), x, x + 8);
+            else turn_task<kBf16>(none, nullptr, j, *reinterpret_cast<const uint4*>(p + 16 * j), *reinterpret_cast<const uint4*>(p + 16 * j + 8), x, x + 8);
+        };
+        // Twice over the run's numbers, the second time from L1: for the largest, and for the codes.
+        float top[2] = {0.0f, 0.0f};
+        uint32_t top16 = 0;  // of values, which nothing turns: as bits of 16, two at a time
 #pragma unroll 1
         for (int t = sub; t < n; t += kTokens) {
+            const uint4* pv = reinterpret_cast<const uint4*>(src[1] + t * a.kv_ld_token[1] + 16 * j);
+            const uint4 v0 = pv[0], v1 = pv[1];
             float x[16];
-            load<kBf16>(a, src[0] + t * a.kv_ld_token[0], ka, kb, cs + (at + t) * (pairs / 2), j, true, x);
-            largest(x, top[0], nan[0]);
-            load<kBf16>(a, src[1] + t * a.kv_ld_token[1], 16 * j, 16 * j + 8, nullptr, j, false, x);
-            largest(x, top[1], nan[1]);
+            numbers(0, t, x);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top[0] = max_nan(top[0], fabsf(x[e]));
+            const uint32_t w[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top16 = __vmaxu2(top16, w[e] & 0x7FFF7FFFu);
+        }
+        top[1] = unpack16<kBf16>(max(top16 & 0xFFFFu, top16 >> 16)).x;  // (what is not finite is above the others)
+        const bool bad = __any_sync(0xffffffffu, !(top[0] < INFINITY) || !(top[1] < INFINITY));
+        if (bad) {  // once more, without it
+            odd = true;
+            top[0] = top[1] = 0.0f;
+#pragma unroll 1
+            for (int t = sub; t < n; t += kTokens)
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    float x[16];
+                    numbers(kv, t, x);
+                    finite(x);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) top[kv] = fmaxf(top[kv], fabsf(x[e]));
+                }
         }
         float inv[2];
-        bool bad[2];
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-            bad[kv] = __any_sync(0xffffffffu, nan[kv] != 0.0f);  // (0 times what is not finite is NaN)
-            if (bad[kv]) {                                       // once more, without it
-                odd = true;
-                top[kv] = 0.0f;
-                for (int t = sub; t < n; t += kTokens) {
-                    float x[16];
-                    if (kv == 0) load<kBf16>(a, src[0] + t * a.kv_ld_token[0], ka, kb, cs + (at + t) * (pairs / 2), j, true, x);
-                    else load<kBf16>(a, src[1] + t * a.kv_ld_token[1], 16 * j, 16 * j + 8, nullptr, j, false, x);
-                    finite(x);
-                    largest(x, top[kv], nan[kv]);
-                }
-            }
-        }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) {
             top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], d));
@@ -247,43 +212,43 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append8_kernel(const Append8Ar
             if (lane == 0) a.scale[kv][scale_at] = s;
             inv[kv] = 1.0f / s;
         }
-        auto store = [&](int kv, int t, int ca, int cb, float* x) {
-            if (bad[kv]) finite(x);
-            uint8_t* p = a.cache[kv] + to + t * a.ld_token;
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                w[e] = encode2(x[4 * e] * inv[kv], x[4 * e + 1] * inv[kv]) | encode2(x[4 * e + 2] * inv[kv], x[4 * e + 3] * inv[kv]) << 16;
-            *reinterpret_cast<uint2*>(p + ca) = make_uint2(w[0], w[1]);
-            *reinterpret_cast<uint2*>(p + cb) = make_uint2(w[2], w[3]);
-        };
 #pragma unroll 1
-        for (int t = sub; t < n; t += kTokens) {
-            float x[16];
-            load<kBf16>(a, src[0] + t * a.kv_ld_token[0], ka, kb, cs + (at + t) * (pairs / 2), j, true, x);
-            store(0, t, ka, kb, x);
-            load<kBf16>(a, src[1] + t * a.kv_ld_token[1], 16 * j, 16 * j + 8, nullptr, j, false, x);
-            store(1, t, 16 * j, 16 * j + 8, x);
-        }
+        for (int t = sub; t < n; t += kTokens)
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                float x[16];
+                numbers(kv, t, x);
+                if (bad) finite(x);
+                uint8_t* p = a.cache[kv] + to + t * a.ld_token;
+                uint32_t w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    w[e] = encode2(x[4 * e] * inv[kv], x[4 * e + 1] * inv[kv]) | encode2(x[4 * e + 2] * inv[kv], x[4 * e + 3] * inv[kv]) << 16;
+                *reinterpret_cast<uint2*>(p + (kv ? 16 * j : ka)) = make_uint2(w[0], w[1]);
+                *reinterpret_cast<uint2*>(p + (kv ? 16 * j + 8 : kb)) = make_uint2(w[2], w[3]);
+            }
     }
     if (odd) atomicOr(a.err, SCOOT_DEVERR_VALUE);
 }
 
 template <bool kBf16, int D>
 scoot_status launch(scoot_ctx* ctx, Append8Args& a, cudaStream_t st) {
-    // few tokens: one each, so that there are blocks for all multiprocessors
-    const int64_t most = 8ll * scoot_sms(ctx);
-    a.window = 1;
-    while (a.window < kMaxWindow && (a.n_tokens + a.window - 1) / a.window > most) a.window *= 2;
-    const int64_t blocks = (a.n_tokens + a.window - 1) / a.window;
-    const size_t smem = (size_t)(a.window + (1 << a.bs_log)) * a.rot.turned * 8 * sizeof(float2);
+    a.window = rotary_window(ctx, a.n_tokens, kMaxWindow, true);
+    a.kv_blocks = (a.n_tokens + a.window - 1) / a.window;
+    int64_t q_blocks = 0;
+    size_t smem = (size_t)(a.window + (1 << a.bs_log)) * a.rot.turned * 8 * sizeof(float2);
+    if (a.queries.n_q) {
+        a.queries.window = rotary_window(ctx, a.n_tokens, kRotaryWindow, true);
+        q_blocks = (a.n_tokens + a.queries.window - 1) / a.queries.window;
+        smem = std::max(smem, (size_t)a.queries.window * a.rot.turned * 8 * sizeof(float2));
+    }
     auto kern = kv_append8_kernel<kBf16, D>;
     const uint32_t bit = 1u << (5 + 2 * kBf16 + (D == 128));
     if (!(ctx->smem_set & bit)) {  // once per context, for the largest window and block
         SCOOT_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (kMaxWindow + kMaxBlock) * D / 2 * (int)sizeof(float2)));
         ctx->smem_set |= bit;
     }
-    kern<<<(unsigned)blocks, kThreads, smem, st>>>(a);
+    kern<<<(unsigned)(a.kv_blocks + q_blocks), kThreads, smem, st>>>(a);
     SCOOT_LAUNCHED(ctx);
     return SCOOT_OK;
 }
@@ -331,18 +296,23 @@ extern "C" scoot_status scoot_kv_append8(scoot_ctx* ctx, const scoot_kv_layout* 
     if ((s = scoot_check_heads(ctx, "k", k, k_ld_token, k_ld_head, D)) != SCOOT_OK) return s;
     if ((s = scoot_check_heads(ctx, "v", v, v_ld_token, v_ld_head, D)) != SCOOT_OK) return s;
     if (!slot || (rotation && !position)) return scoot_fail(ctx, SCOOT_EINVAL, "slot or position is NULL");
-    a.n_heads = n_heads;
     a.n_kv_heads = layout->n_kv_heads;
     while ((1 << a.bs_log) < layout->block_size) ++a.bs_log;
     a.n_tokens = n_tokens;
     a.n_slots = layout->n_blocks << a.bs_log;
     a.position = position;
-    a.q = static_cast<const uint16_t*>(q);
-    a.q_ld_token = q_ld_token;
-    a.q_ld_head = q_ld_head;
-    a.y = static_cast<uint16_t*>(q_out);
-    a.y_ld_token = q_out_ld_token;
-    a.y_ld_head = q_out_ld_head;
+    a.queries.rot = a.rot;
+    a.queries.n_q = n_heads;
+    a.queries.tasks = D / 16;
+    a.queries.n_tokens = n_tokens;
+    a.queries.position = position;
+    a.queries.q = {static_cast<const uint16_t*>(q), q_ld_token, q_ld_head};
+    a.queries.y = static_cast<uint16_t*>(q_out);
+    a.queries.y_ld_token = q_out_ld_token;
+    a.queries.y_ld_head = q_out_ld_head;
+    a.queries.slot = slot;
+    a.queries.n_slots = a.n_slots;
+    a.queries.err = ctx->d_err;
     a.kv[0] = static_cast<const uint16_t*>(k);
     a.kv[1] = static_cast<const uint16_t*>(v);
     a.kv_ld_token[0] = k_ld_token;

@@ -8,110 +8,18 @@ namespace {
 
 using namespace scoot_dev;
 
-constexpr int kThreads = 256;
-constexpr int kMaxWindow = 16;  // tokens of a block of threads
-constexpr int kPer = 2;         // tasks of a thread under way at once
-
-struct Heads {
-    const uint16_t* p;
-    int64_t ld_token, ld_head;
-};
-
-struct RotaryArgs {
-    Rotation rot;
-    int32_t n_q, n_k, n_v;      // heads turned in place of y's, turned into the cache, copied into it
-    int32_t tasks;              // of a head: head_dim / 16
-    int32_t window;
-    int64_t n_tokens;
-    const int32_t* position;
-    Heads q, k, v;
-    uint16_t* y;
-    int64_t y_ld_token, y_ld_head;
-    const int64_t* slot;        // NULL: no cache
-    int32_t bs_log;
-    int64_t n_slots, ld_block, ld_token, ld_head;
-    uint16_t* k_cache;
-    uint16_t* v_cache;
-    uint32_t* err;
-};
-
-// A block takes `window` tokens: their cosines and sines once for all heads, into shared memory, then a task (16 dimensions of
-// a head: two chunks of eight that hold whole pairs) per thread, kPer of them in flight.
 template <bool kBf16>
-__global__ void __launch_bounds__(kThreads) rotary_kernel(const RotaryArgs a) {
+__global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const RotaryArgs a) {
     extern __shared__ float4 cs[];
-    const int64_t t0 = (int64_t)blockIdx.x * a.window;
-    const int n = (int)min((int64_t)a.window, a.n_tokens - t0), pairs = 8 * a.rot.turned;
-    for (int e = threadIdx.x; e < n * pairs; e += kThreads) {
-        const int t = e / pairs, pair = e - t * pairs;
-        reinterpret_cast<float2*>(cs)[t * pairs + rotation_place(a.rot, pair)] = rotation_at(a.rot, pair, a.position[t0 + t]);
-    }
-    __syncthreads();
-    const uint32_t per_token = (uint32_t)(a.n_q + a.n_k + a.n_v) * a.tasks, all = n * per_token;
-    for (uint32_t e0 = threadIdx.x; e0 < all; e0 += kThreads * kPer) {
-        uint4 ra[kPer], rb[kPer];
-        uint16_t* to[kPer];
-        int task[kPer], tok[kPer];
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            const uint32_t e = e0 + i * kThreads;
-            to[i] = nullptr;
-            if (e >= all) continue;
-            const uint32_t t = e / per_token, c = e - t * per_token;
-            int head = (int)(c / a.tasks);
-            const int j = (int)(c - head * a.tasks);
-            const int64_t token = t0 + t;
-            int64_t s = 0;
-            if (a.slot) {
-                s = a.slot[token];
-                if (s >= a.n_slots && c == 0) atomicOr(a.err, SCOOT_DEVERR_INDEX);
-                if (s < 0 || s >= a.n_slots) continue;
-            }
-            const bool isq = head < a.n_q, isv = head >= a.n_q + a.n_k;
-            Heads src = a.q;
-            if (!isq) {
-                head -= a.n_q;
-                src = a.k;
-                if (isv) {
-                    head -= a.n_k;
-                    src = a.v;
-                }
-                to[i] = (isv ? a.v_cache : a.k_cache) + (s >> a.bs_log) * a.ld_block + (s & ((1 << a.bs_log) - 1)) * a.ld_token + head * a.ld_head;
-            } else {
-                to[i] = a.y + token * a.y_ld_token + head * a.y_ld_head;
-            }
-            task[i] = isv ? j | 0x40000000 : j;
-            tok[i] = (int)t;
-            const uint16_t* p = src.p + token * src.ld_token + head * src.ld_head;
-            ra[i] = *reinterpret_cast<const uint4*>(p + 8 * (isv ? 2 * j : a.rot.chunk_a(j)));
-            rb[i] = *reinterpret_cast<const uint4*>(p + 8 * (isv ? 2 * j + 1 : a.rot.chunk_b(j)));
-        }
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            if (!to[i]) continue;
-            const bool isv = task[i] & 0x40000000;
-            const int j = task[i] & 0x3FFFFFFF;
-            if (!isv && j < a.rot.turned) {
-                float x[8], y[8];
-                turn_task<kBf16>(a.rot, cs + tok[i] * (pairs / 2), j, ra[i], rb[i], x, y);
-                ra[i] = make_uint4(pack16_rn<kBf16>(x[0], x[1]), pack16_rn<kBf16>(x[2], x[3]), pack16_rn<kBf16>(x[4], x[5]), pack16_rn<kBf16>(x[6], x[7]));
-                rb[i] = make_uint4(pack16_rn<kBf16>(y[0], y[1]), pack16_rn<kBf16>(y[2], y[3]), pack16_rn<kBf16>(y[4], y[5]), pack16_rn<kBf16>(y[6], y[7]));
-            }
-            *reinterpret_cast<uint4*>(to[i] + 8 * (isv ? 2 * j : a.rot.chunk_a(j))) = ra[i];
-            *reinterpret_cast<uint4*>(to[i] + 8 * (isv ? 2 * j + 1 : a.rot.chunk_b(j))) = rb[i];
-        }
-    }
+    rotary_block<kBf16>(a, blockIdx.x, cs);
 }
 
 scoot_status launch(scoot_ctx* ctx, RotaryArgs& a, bool bf16, cudaStream_t st) {
-    // few tokens: one each, so that there are blocks for all multiprocessors
-    const int64_t most = 8ll * scoot_sms(ctx);
-    a.window = 1;
-    while (a.window < kMaxWindow && (a.n_tokens + a.window - 1) / a.window > most) a.window *= 2;
+    a.window = rotary_window(ctx, a.n_tokens, kRotaryWindow, a.slot != nullptr);
     a.err = ctx->d_err;
     const int64_t blocks = (a.n_tokens + a.window - 1) / a.window;
     const size_t smem = (size_t)a.window * a.rot.turned * 8 * sizeof(float2);
-    (bf16 ? rotary_kernel<true> : rotary_kernel<false>)<<<(unsigned)blocks, kThreads, smem, st>>>(a);
+    (bf16 ? rotary_kernel<true> : rotary_kernel<false>)<<<(unsigned)blocks, kRotaryThreads, smem, st>>>(a);
     SCOOT_LAUNCHED(ctx);
     return SCOOT_OK;
 }

@@ -1064,22 +1064,21 @@ def _code(t, name):
 def _kv8(k_cache, v_cache, k_scale, v_scale, device):
     """_kv for an 8-bit cache, and the pointers of its scales."""
     import torch
-    dt, shape, stride = k_cache.dtype, k_cache.shape, k_cache.stride()
-    f8 = torch.float8_e4m3fn
-    if not (dt is f8 and v_cache.dtype is f8 and len(shape) == 4 and shape == v_cache.shape and stride == v_cache.stride()
-            and stride[3] == 1 and k_cache.get_device() == device and v_cache.get_device() == device):
+    f8, shape, stride = torch.float8_e4m3fn, k_cache.shape, k_cache.stride()
+    if not (k_cache.dtype is f8 and v_cache.dtype is f8 and len(stride) == 4 and stride[3] == 1 and stride == v_cache.stride()
+            and shape == v_cache.shape and k_cache.get_device() == device and v_cache.get_device() == device):
         if not (k_cache.is_cuda and v_cache.is_cuda):
             raise TypeError("k_cache and v_cache must be CUDA torch tensors (device memory)")
         for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
             if t.get_device() != device:
                 raise _elsewhere(t, name, device)
-        if dt is not f8 or v_cache.dtype is not f8:
-            raise TypeError(f"k_cache and v_cache must both be float8_e4m3fn, got {dt} and {v_cache.dtype}")
+        if k_cache.dtype is not f8 or v_cache.dtype is not f8:
+            raise TypeError(f"k_cache and v_cache must both be float8_e4m3fn, got {k_cache.dtype} and {v_cache.dtype}")
         raise ValueError("k_cache and v_cache must be [blocks][tokens][heads][dim] of one shape and the same strides, contiguous "
                          f"along their last axis, got {tuple(shape)} and {tuple(v_cache.shape)}")
-    if k_scale.shape != (shape[0], shape[2]) or v_scale.shape != k_scale.shape:
-        raise ValueError(f"k_scale and v_scale must be [blocks][heads], {shape[0]} by {shape[2]}, got {tuple(k_scale.shape)} and "
-                         f"{tuple(v_scale.shape)}")
+    n, _, H, _ = shape
+    if k_scale.shape != (n, H) or v_scale.shape != (n, H):
+        raise ValueError(f"k_scale and v_scale must be [blocks][heads], {n} by {H}, got {tuple(k_scale.shape)} and {tuple(v_scale.shape)}")
     f32 = torch.float32
     return (*_layout(E4M3, shape, stride), _ptr(k_scale, f32, "k_scale", device), _ptr(v_scale, f32, "v_scale", device))
 
@@ -1100,21 +1099,32 @@ def scoot_rotary(ctx, rotation, x, position, out, inverse=False, stream=None) ->
         _check(status, "scoot_rotary", h)
 
 
-def _append_args(k, v, slot, position, q, q_out, Hkv, D, dt, device):
+def _heads_of(t, dtype, T, H, D, name, device):
+    """_heads of a tensor [T][H][D]."""
+    stride = t.stride()
+    if t.dtype is dtype and t.get_device() == device and len(stride) == 3 and stride[2] == 1:
+        n, h, d = t.shape
+        if n == T and h == H and d == D:
+            return t.data_ptr(), (stride[0] if n > 1 else h * d), (stride[1] if h > 1 else d)
+    elif len(stride) == 3:
+        return _heads(t, dtype, name, device)
+    raise ValueError(f"{name} must be [{T}][{H}][{D}], as slot and the cache have tokens, heads and dimensions, got {tuple(t.shape)}")
+
+
+def _append_args(k, v, slot, position, q, q_out, H, D, dt, device):
     """(queries' pointers and strides, heads, keys', values', slot, position, tokens) of an append with a rotation."""
     import torch
     T = slot.numel()
-    if k.shape != v.shape or k.shape != (T, Hkv, D) or (position is not None and position.numel() != T):
-        raise ValueError(f"k and v must be [T][heads][dim] as slot and the cache have them, and position [T], got {tuple(k.shape)}, "
-                         f"{tuple(v.shape)} and {None if position is None else tuple(position.shape)}")
-    qs = (None, 0, 0, 0, None, 0, 0)
-    if (q is None) != (q_out is None):
-        raise ValueError("q and q_out come together")
-    if q is not None:
-        if q.shape != q_out.shape or q.dim() != 3 or q.shape[0] != T or q.shape[2] != D:
-            raise ValueError(f"q and q_out must be [{T}][heads][{D}] of one shape, got {tuple(q.shape)} and {tuple(q_out.shape)}")
-        qs = (*_heads(q, dt, "q", device), q.shape[1], *_heads(q_out, dt, "q_out", device))
-    return (*qs, *_heads(k, dt, "k", device), *_heads(v, dt, "v", device), _ptr(slot, torch.int64, "slot", device),
+    if q is None or q_out is None:
+        if q is not q_out:
+            raise ValueError("q and q_out come together")
+        qs = (None, 0, 0, 0, None, 0, 0)
+    else:
+        Hq = q.shape[1] if len(q.shape) == 3 else 0
+        qs = (*_heads_of(q, dt, T, Hq, D, "q", device), Hq, *_heads_of(q_out, dt, T, Hq, D, "q_out", device))
+    if position is not None and position.numel() != T:
+        raise ValueError(f"position must be [{T}] as slot is, got {tuple(position.shape)}")
+    return (*qs, *_heads_of(k, dt, T, H, D, "k", device), *_heads_of(v, dt, T, H, D, "v", device), _ptr(slot, torch.int64, "slot", device),
             None if position is None else _ptr(position, torch.int32, "position", device), T)
 
 
