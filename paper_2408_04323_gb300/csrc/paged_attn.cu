@@ -71,9 +71,9 @@ constexpr int kKeys = 128;         // keys of a tile
 template <bool k8>
 constexpr int kThreads = k8 ? 512 : 384;
 template <bool k8>
-constexpr int kSoftmaxRegs = k8 ? 184 : 200;  // 2 * 200 + 104 = 3 * 168, 2 * 184 + 72 + 72 = 4 * 128: what the block is launched with
+constexpr int kSoftmaxRegs = k8 ? 192 : 200;  // 2 * 200 + 104 = 3 * 168, 2 * 192 + 56 + 72 = 4 * 128: what the block is launched with
 template <bool k8>
-constexpr int kOtherRegs = k8 ? 72 : 104;
+constexpr int kOtherRegs = k8 ? 56 : 104;
 constexpr int kCodeRegs = 72;
 constexpr int kMmaWarp = 8, kLoadWarp = 9, kValueWarp = 10, kTurnWarp = 10, kCodeWarp = 12;
 constexpr int kRing = 4;         // items handed from the load warp to the others
@@ -751,10 +751,10 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
     const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) - kCodeWarp;
     const int sub = lane / kPieces, piece = lane % kPieces, first = 32 * w + kLoads * sub;
     const int bs = 1 << a.bs_log;
-    // Where the lane's first chunk of its first key goes in a tile: 16 dimensions are two chunks of a row, and the lanes that
-    // meet in a phase of the store write them in different orders (banks).
-    const bool swap = D == 128 ? piece & 4 : sub & 1;
-    const uint32_t place = (piece >> 2) * kHalf + first * 128 + (((2 * (piece & 3) + swap) ^ (first & 7)) << 4);
+    // Sixteen dimensions are two chunks of a row.  Of the lanes that meet in a phase of a store, half take their keys two by two
+    // the other way round: their rows' swizzles differ in the last bit, and so do their banks.
+    const int turn = D == 128 ? piece >> 2 : sub & 1;
+    const uint32_t place = (piece >> 2) * kHalf + (first + turn) * 128 + (((2 * (piece & 3)) ^ ((first + turn) & 7)) << 4);
     uint32_t st = 0, at = 0, n_unit = 0;  // the next tile's place; tiles made; units
     bool bad = false, bad_scale = false;
 #pragma unroll 1
@@ -773,8 +773,8 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
             const int64_t key = ((int64_t)g * 32 + lane) << a.bs_log;
             return key < it.end && key + bs > it.begin ? __ldg(row + g * 32 + lane) : INT32_MIN;
         };
-        int64_t from = 0;    // of the lane's first key
-        int lo = 0, hi = 0;  // of its keys, those that are there
+        int64_t from0 = 0, from1 = 0;  // of the lane's first two keys
+        uint32_t there = 0;            // those of its keys that are to be had, as bits
         float scale = 0.0f;  // group lane & 15 of the keys' scales, or of the values'
         auto turn_to = [&](int u) {
             const int key0 = u * kKeys, g = (key0 >> a.bs_log) >> 5;
@@ -788,9 +788,11 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
             }
             const int key = key0 + first;
             const int id = __shfl_sync(0xffffffffu, ids, (key >> a.bs_log) & 31);
-            from = id * a.ld_block + (key & (bs - 1)) * a.ld_token + head_at;
-            lo = id < 0 ? kLoads : it.begin - key;
-            hi = it.end - key;
+            from0 = id * a.ld_block + ((key + turn) & (bs - 1)) * a.ld_token + head_at;
+            from1 = from0 + (turn ? -a.ld_token : a.ld_token);
+            const int lo = min(max(it.begin - key, 0), kLoads), hi = min(max(it.end - key, 0), kLoads);
+            there = id < 0 || hi <= lo ? 0u : (1u << hi) - (1u << lo);
+            if (turn) there = (there & 0x55u) << 1 | (there & 0xAAu) >> 1;
             const int key8 = key0 + 8 * (lane & 15);
             const int id8 = __shfl_sync(0xffffffffu, ids, (key8 >> a.bs_log) & 31);
             scale = 0.0f;
@@ -798,9 +800,9 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
                 scale = __ldg((lane < 16 ? a.k_scale : a.v_scale) + (int64_t)id8 * a.n_kv_heads + it.h);
         };
         uint4 code[kLoads];
-        auto load = [&](int i, const uint8_t* p) {  // codes of this lane's key i
+        auto load = [&](int i, const uint8_t* p) {  // codes of this lane's key i ^ turn
             code[i] = make_uint4(0, 0, 0, 0);
-            if (i >= lo && i < hi) code[i] = __ldg(reinterpret_cast<const uint4*>(p + from + i * a.ld_token));
+            if (there >> i & 1u) code[i] = __ldg(reinterpret_cast<const uint4*>(p + (i & 1 ? from1 : from0) + (i & ~1) * a.ld_token));
         };
         // a tile that some row does not see all of
         const int64_t all1 = a.causal ? min((int64_t)it.kv, (int64_t)it.pos + 1) : it.kv;
@@ -845,19 +847,18 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
             }
             const bool more = n + 1 < 2 * it.nu;
             if (more && values) turn_to(u + 1);
-            if (!more) lo = kLoads;
+            if (!more) there = 0;
             const uint8_t* p = values ? a.k8 : a.v8;
             const uint32_t times = values ? v_times : k_times, to = tiles + st * Sh::kTile + place;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const uint4 c = code[i];
                 load(i, p);
-                const uint32_t x0 = swap ? c.z : c.x, x1 = swap ? c.w : c.y, y0 = swap ? c.x : c.z, y1 = swap ? c.y : c.w;
-                const uint32_t dst = (to ^ (i << 4)) + i * 128;
-                st_shared16(dst, times_half2(decode_lo(x0), times), times_half2(decode_hi(x0), times), times_half2(decode_lo(x1), times),
-                            times_half2(decode_hi(x1), times));
-                st_shared16(dst ^ 16, times_half2(decode_lo(y0), times), times_half2(decode_hi(y0), times), times_half2(decode_lo(y1), times),
-                            times_half2(decode_hi(y1), times));
+                const uint32_t dst = to ^ (i * 144);  // row i ^ turn, whose swizzle has it as well
+                st_shared16(dst, times_half2(decode_lo(c.x), times), times_half2(decode_hi(c.x), times), times_half2(decode_lo(c.y), times),
+                            times_half2(decode_hi(c.y), times));
+                st_shared16(dst ^ 16, times_half2(decode_lo(c.z), times), times_half2(decode_hi(c.z), times), times_half2(decode_lo(c.w), times),
+                            times_half2(decode_hi(c.w), times));
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             warp_arrive(&bars[kKvFull + st]);
@@ -881,21 +882,29 @@ __device__ __forceinline__ void turn_queries(uint8_t* tile, int8_t* up) {
     for (int row = threadIdx.x & 31; row < kRows; row += 32) {
         uint4* p = reinterpret_cast<uint4*>(tile + row * 128);
         auto chunk = [&](int i) -> uint4& { return p[(i / 8) * (kHalf / 16) + ((i ^ row) & 7)]; };
-        uint4 x[D / 8];
         uint32_t top = 0;
-#pragma unroll
+#pragma unroll 4
         for (int i = 0; i < D / 8; ++i) {
-            x[i] = chunk(i);
-            top = __vmaxu2(__vmaxu2(__vmaxu2(top, x[i].x & 0x7FFF7FFFu), x[i].y & 0x7FFF7FFFu), __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu));
+            const uint4 x = chunk(i);
+            top = __vmaxu2(__vmaxu2(__vmaxu2(top, x.x & 0x7FFF7FFFu), x.y & 0x7FFF7FFFu), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
         }
         top = max(top & 0xFFFFu, top >> 16);
         const int e = (int)(top >> 7), n = top == 0 || e == 255 ? 0 : min(14 + 127 - e, 126);
         const float f = __uint_as_float((uint32_t)(127 + n) << 23);
         auto turn = [&](uint32_t w) { return pack16<false>(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xFFFF0000u) * f); };
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) chunk(i) = make_uint4(turn(x[i].x), turn(x[i].y), turn(x[i].z), turn(x[i].w));
+#pragma unroll 4
+        for (int i = 0; i < D / 8; ++i) {
+            const uint4 x = chunk(i);
+            chunk(i) = make_uint4(turn(x.x), turn(x.y), turn(x.z), turn(x.w));
+        }
         up[row] = (int8_t)n;
     }
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 // What softmax_codes and its uneven form begin with: scores, -inf for the keys that the row does not see.
@@ -961,7 +970,7 @@ __device__ __forceinline__ void softmax_codes(uint32_t tS, int ch0, bool full, i
     const float ck = score_scale(c, t.k_top), vt = t.v_top;
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, f;
 #pragma unroll
-    for (int i = 0; i < NCH * 32; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(x[i]));
+    for (int i = 0; i < NCH * 16; ++i) mx[i & 3] = max3(mx[i & 3], __uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
     if (s.grow(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * ck, vt, first, live, f)) rescale(f);
     const float factor = __fdividef(vt, s.vref) * 128.0f;
     const float ms = __log2f(factor) - finite_or_zero(s.m);
@@ -1509,7 +1518,7 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
             wait.warp(&bars[kItemFull + ring], n_item / kRing);
             wait.ok &= wg_sync.wait.ok;
             if (!wait.all()) break;
-            const Item it = items[ring];
+            Item it = items[ring];
             if (it.stop) break;
             if (it.slot != 2 && it.slot != s) {
                 warp_arrive(&bars[kItemEmpty + ring]);
@@ -1517,11 +1526,20 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
                 buf = (buf + it.nu) % Sh::kBuf;
                 continue;
             }
-            const int half = it.slot == 2 ? s : 0;
-            const int tok0 = half * a.toks, ntok = min(a.toks, it.ntok - tok0), rows = ntok * a.group;
-            const int per_copy = kRows >> it.rep_log, rr = row & (per_copy - 1), copy = row / per_copy;
-            const int j = rr * a.inv_group >> 16;
-            const bool live = rr < rows;
+            int half, tok0, ntok, rows, per_copy, rr, copy, j;
+            bool live;
+            auto place = [&]() {  // this thread's row of the item
+                half = it.slot == 2 ? s : 0;
+                tok0 = half * a.toks;
+                ntok = min(a.toks, it.ntok - tok0);
+                rows = ntok * a.group;
+                per_copy = kRows >> it.rep_log;
+                rr = row & (per_copy - 1);
+                copy = row / per_copy;
+                j = rr * a.inv_group >> 16;
+                live = rr < rows;
+            };
+            place();
             const bool busy = __any_sync(0xffffffffu, live);
             // keys that this row sees; that every row of the slot sees
             const int pos = it.pos + tok0 + j;
@@ -1624,6 +1642,11 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
                 }
             }
             // ---- the end of the item: O and l of this part
+            if constexpr (k8) {  // (read again: what only the end needs would take registers from the tiles)
+                asm volatile("" ::: "memory");
+                it = items[ring];
+                place();
+            }
             wait.warp(&bars[kPvDone + 4 * s + (unit ? unit - 1 : 2)], unit ? uphase : uphase ^ 1u);
             fence_after();
             const bool poison = *reinterpret_cast<volatile int32_t*>(&items[ring].poison) != 0;
