@@ -37,14 +37,14 @@
 namespace {
 
 constexpr int kItemCost = 2;    // an item's start and end, in tiles,
-constexpr int kMinRange = 4;    // cost that a warp takes at least
+constexpr int kMinRange = 3;    // cost that a warp takes at least
 constexpr int kSnap = 2;        // a cut this close to the start or end of an item's tiles moves there
 constexpr int kMaxBlocks = 256;
 constexpr int kShare = 4;       // warps that take as many heads' keys of the same tokens at a time, at most
 // Counters, apart: two per block of the tiles kernel, one per warp of this, kShare per block of this.
 constexpr int kWarpCounts = 2 * kMaxBlocks, kBlockCounts = kWarpCounts + 12 * kMaxBlocks;
 static_assert(kBlockCounts + kShare * kMaxBlocks <= (int)SCOOT_COUNTS, "counters");
-constexpr int kFewParts = 8;    // parts that the warp that comes last joins by itself
+constexpr int kFewParts = 16;   // parts that the warp that comes last joins by itself
 constexpr int kItems = 8;       // items of a warp between its copies and their attention
 constexpr int kFewRows = 32;    // requests of up to so many rows
 constexpr float kMaxScale = 2.3e38f;  // times log2 e it is still finite
@@ -308,9 +308,9 @@ __device__ __forceinline__ int fetch_ids(const Attn8Args& a, const Item& it, int
     return key < it.end && key + (1 << a.bs_log) > it.begin ? __ldg(a.table + (int64_t)it.r * a.ld_table + block) : INT32_MIN;
 }
 
-// A range's next item with keys goes to *to; false if there is none.  Those without keys get their zeros here.  By a warp.
+// A range's next item with keys goes to *to; false if there is none.  reqs: the requests' lengths, or NULL where they are many.  Those without keys get their zeros here.  By a warp.
 template <int D, int kRows, int kKeys>
-__device__ __noinline__ bool next_item(const Attn8Args& a, Cursor* cur, Item* to) {
+__device__ __noinline__ bool next_item(const Attn8Args& a, Cursor* cur, Item* to, const Req* reqs) {
     const int lane = threadIdx.x & 31;
     Cursor c = *cur;
     bool found = false;
@@ -320,7 +320,7 @@ __device__ __noinline__ bool next_item(const Attn8Args& a, Cursor* cur, Item* to
             if (c.req.n > 0 && ++c.h < a.n_kv_heads / a.share) continue;
             c.h = 0;
             for (++c.r; c.r < a.n_req;) {
-                const Req q = load_req(a, c.r + lane, false);
+                const Req q = !reqs ? load_req(a, c.r + lane, false) : c.r + lane < a.n_req ? reqs[c.r + lane] : Req{0, 0, 0};
                 const uint32_t some = __ballot_sync(0xffffffffu, q.n > 0);
                 if (some) {
                     const int src = __ffs(some) - 1;
@@ -391,7 +391,10 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
     __shared__ int64_t cost_s[kThreads];
     __shared__ Item items[kShare + kWarps];  // of the block's items of many parts: those that came in, and one that begins with each warp's last
     __shared__ Item queue_s[kWarps][kItems];
+    __shared__ Item ends_s[kWarps][2];  // of a range's two split items, those of few parts
     __shared__ Cursor cursor_s[kWarps];
+    __shared__ Attn8Args args_s;       // for next_item: a call reads the parameters' own memory slowly
+    __shared__ Req req_s[kThreads];    // with at most kThreads requests: theirs
     __shared__ int last_s[kShare + kWarps], failed, many;
     __shared__ __align__(8) uint64_t bars[kWarps * Sh::kStages];
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -400,13 +403,17 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
     // The cost of all items: each thread k consecutive requests, then a scan.
     const int k = (a.n_req + kThreads - 1) / kThreads;
     if (tid < kShare + kWarps) items[tid].n_parts = 0;
+    if (tid < 2 * kWarps) ends_s[tid / 2][tid % 2].n_parts = 0;
     if (tid == 0) failed = many = 0;
+    if (tid < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(tid ? &maps.v : &maps.k) : "memory");
+    for (int i = tid; i < (int)(sizeof(Attn8Args) / 4); i += kThreads) reinterpret_cast<uint32_t*>(&args_s)[i] = reinterpret_cast<const uint32_t*>(&a)[i];
     if (tid < kWarps * Sh::kStages) scoot_dev::mbar_init(&bars[tid], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     int64_t mine = 0;
 #pragma unroll 1
     for (int i = 0; i < k; ++i) {
         const Req q = load_req(a, tid * k + i, blockIdx.x == 0);
+        if (k == 1) req_s[tid] = q;
         const bool one = item_count(a, q.n) == 1;
         if (one) mine += item_cost<kKeys>(a, q.kv, q.n, 0);
         uint32_t big = __ballot_sync(0xffffffffu, q.n > 0 && !one);
@@ -441,6 +448,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
     int cached = -1;  // requests 32 cached .. are in the lanes
     Req in_lane{0, 0, 0};
     auto get = [&](int r) {
+        if (k == 1) return req_s[r];
         if ((r >> 5) != cached) {
             cached = r >> 5;
             in_lane = load_req(a, cached * 32 + lane, false);
@@ -511,11 +519,17 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                      (int64_t)2 * a.share * Sh::kPart, n};
     };
 
+    // Of a split item's few parts, how many were there before the warp's.  By a lane; the warp's other lanes' stores are before it.
+    auto add_one = [&](const Item& it) {
+        __threadfence();
+        return atomicAdd(a.warp_count + it.first * a.share + member, 1u);
+    };
+    uint32_t came = 0;
     uint32_t n_made = 0, n_taken = 0;  // items found, and those whose copies have begun
     int first_ids = 0;                 // ids of the first 32 blocks of the last one found, in the lanes
     auto find = [&]() {
         Item* to = &queue_s[warp][n_made % kItems];
-        if (!next_item<D, kRows, kKeys>(a, &cursor_s[warp], to)) return;
+        if (!next_item<D, kRows, kKeys>(args_s, &cursor_s[warp], to, k == 1 ? req_s : nullptr)) return;
         ++n_made;
         first_ids = fetch_ids(a, *to, (to->u0 * kKeys >> a.bs_log) >> 5);
     };
@@ -528,6 +542,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
         ids = out ? (int)a.n_blocks : raw;  // past the end: the copy reads nothing and writes zeros
     };
     auto load = [&]() {
+        bool taken = false;
         if (load_u == load_u1) {
             if (n_taken == n_made) return;
             const Item& it = queue_s[warp][n_taken % kItems];
@@ -537,7 +552,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
             use(first_ids);
             ids_next = fetch_ids(a, it, group + 1);
             ++n_taken;
-            find();
+            taken = true;
         }
         const Item& it = queue_s[warp][(n_taken - 1) % kItems];
         const int key0 = load_u++ * kKeys, b0 = key0 >> a.bs_log, head = it.h;
@@ -578,6 +593,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
             copy4(ring_scales + to_load * Sh::kScale + 4 * lane, (lane < kG ? a.k_scale : a.v_scale) + (there ? (int64_t)id * a.n_kv_heads + head : 0), there);
         }
         if (++to_load == Sh::kStages) to_load = 0;
+        if (taken) find();  // (after the copies, which wait for nothing of it)
     };
 
     find();
@@ -588,7 +604,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
     }
     // The copies run ahead of the products by the ring's places, across items.
 #pragma unroll 1
-    for (uint32_t n_done = 0; n_done < n_made && ok; ++n_done) {
+    for (uint32_t n_done = 0; n_done < n_taken && ok; ++n_done) {
         const Item& it = queue_s[warp][n_done % kItems];
         uint32_t qb[NT][kSteps][2];
         float c_row[NT][2];              // scale of a row's scores, to log2
@@ -841,9 +857,10 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
         const bool whole = it.n_parts == 1;
         const bool begins = it.first == team;
         float* part = a.parts + (size_t)(2 * worker + begins) * Sh::kPart;
-        if (it.n_parts > kFewParts && lane == 0) {
-            many = 1;
-            if (begins || warp < a.share) items[begins ? kShare + warp : member] = it;
+        if (!whole && lane == 0) {
+            if (it.n_parts <= kFewParts) ends_s[warp][begins] = it;
+            else many = 1;
+            if (it.n_parts > kFewParts && (begins || warp < a.share)) items[begins ? kShare + warp : member] = it;
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -875,22 +892,29 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                     if (g == 0) reinterpret_cast<float2*>(part + kRows * D)[row] = make_float2(m[nt][e], l[nt][e]);
                 }
             }
-        if (!whole && it.n_parts <= kFewParts) {
+        if (!whole && !begins && it.n_parts <= kFewParts) {
             __syncwarp();
-            bool last = false;
-            if (lane == 0) {
-                __threadfence();  // (the warp's other lanes' stores are before it)
-                uint32_t* count = a.warp_count + it.first * a.share + member;
-                last = atomicAdd(count, 1u) == (uint32_t)it.n_parts - 1;
-                if (last) *count = 0;
-                __threadfence();
-            }
-            if (__any_sync(0xffffffffu, last)) {
-                __syncwarp();
-                join<kBf16, D, kRows, 32, 4, 2>(a, &it, 1, it.rows * (D / 4), lane, [&](int, float*&) {
-                    return parts_at(it.first, it.first, member, it.n_parts);
-                });
-            }
+            if (lane == 0) came = add_one(it);  // (its result is not waited for here)
+        }
+    }
+    // Of the range's split items, the one that began before it and the one that goes on after it: whether the other parts are there.
+    __syncwarp();
+    if (ok) {
+        bool last = false;
+        if (lane < 2 && ends_s[warp][lane].n_parts) {
+            const Item& it = ends_s[warp][lane];
+            if (lane == 1) came = add_one(it);
+            last = came == (uint32_t)it.n_parts - 1;
+            if (last) a.warp_count[it.first * a.share + member] = 0;
+            __threadfence();
+        }
+        uint32_t done = __ballot_sync(0xffffffffu, last);
+#pragma unroll 1
+        for (; done; done &= done - 1) {
+            const Item* it = &ends_s[warp][__ffs(done) - 1];
+            join<kBf16, D, kRows, 32, 4, 4>(a, it, 1, it->rows * (D / 4), lane, [&](int, float*&) {
+                return parts_at(it->first, it->first, member, it->n_parts);
+            });
         }
     }
     if (!ok) {  // a copy did not come: what is under way lands before the block ends
