@@ -1785,6 +1785,7 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
     }
     fence_before();
     __syncthreads();
+    if (k8) asm volatile("griddepcontrol.wait;" ::: "memory");  // (this kernel's end is then the end of that of few rows, too)
     if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u));
 }
 
@@ -1820,21 +1821,32 @@ bool encode(CUtensorMap* map, bool bf16, const void* base, int n_dim, const cuui
 }
 
 template <bool kBf16, int D, bool k8>
-scoot_status launch(scoot_ctx* ctx, const AttnArgs& a, int sms, cudaStream_t st) {
+scoot_status launch(scoot_ctx* ctx, const AttnArgs& a, int sms, cudaStream_t st, bool beside) {
     auto kern = paged_attn_kernel<kBf16, D, k8>;
     const uint32_t bit = 1u << ((k8 ? 13 : 0) + 2 * kBf16 + (D == 128));
     if (!(ctx->smem_set & bit)) {  // once per context: the call is short
         SCOOT_CUDA(ctx, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D, k8>::kSmem));
         ctx->smem_set |= bit;
     }
-    kern<<<(unsigned)sms, kThreads<k8>, Shape<D, k8>::kSmem, st>>>(a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)sms);
+    cfg.blockDim = dim3(kThreads<k8>);
+    cfg.dynamicSmemBytes = Shape<D, k8>::kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = beside ? 1 : 0;
+    SCOOT_CUDA(ctx, cudaLaunchKernelEx(&cfg, kern, a));
     SCOOT_LAUNCHED(ctx);
     return SCOOT_OK;
 }
+// beside: the kernel before it in the stream is the same call's, reads and writes nothing of this one's, and lets it begin.
 template <bool k8>
-scoot_status launch(scoot_ctx* ctx, const AttnArgs& a, bool bf16, int D, int sms, cudaStream_t st) {
-    if (bf16) return D == 128 ? launch<true, 128, k8>(ctx, a, sms, st) : launch<true, 64, k8>(ctx, a, sms, st);
-    return D == 128 ? launch<false, 128, k8>(ctx, a, sms, st) : launch<false, 64, k8>(ctx, a, sms, st);
+scoot_status launch(scoot_ctx* ctx, const AttnArgs& a, bool bf16, int D, int sms, cudaStream_t st, bool beside = false) {
+    if (bf16) return D == 128 ? launch<true, 128, k8>(ctx, a, sms, st, beside) : launch<true, 64, k8>(ctx, a, sms, st, beside);
+    return D == 128 ? launch<false, 128, k8>(ctx, a, sms, st, beside) : launch<false, 64, k8>(ctx, a, sms, st, beside);
 }
 
 // The maps of the queries' boxes.
@@ -1865,7 +1877,7 @@ bool scoot_encode_codes(CUtensorMap* map, const scoot_kv_layout* L, const void* 
 
 size_t scoot_attn8_tile_bytes(int head_dim) { return (size_t)kBufs * kRows * (head_dim + 2) * sizeof(float); }
 
-scoot_status scoot_attn8_tiles(scoot_ctx* ctx, const scoot_kv_layout* layout, const Attn8Args& args, bool bf16, int sms, cudaStream_t st) {
+scoot_status scoot_attn8_tiles(scoot_ctx* ctx, const scoot_kv_layout* layout, const Attn8Args& args, bool bf16, int sms, cudaStream_t st, bool beside) {
     const int D = layout->head_dim, G = args.group;
     if (!encode_tiled()) return scoot_fail(ctx, SCOOT_ECUDA, "the driver has no cuTensorMapEncodeTiled");
     AttnArgs a = {};
@@ -1903,7 +1915,7 @@ scoot_status scoot_attn8_tiles(scoot_ctx* ctx, const scoot_kv_layout* layout, co
     a.v_scale = args.v_scale;
     a.max_new = args.max_new;
     a.few = args.few;
-    return launch<true>(ctx, a, bf16, D, sms, st);
+    return launch<true>(ctx, a, bf16, D, sms, st, beside);
 }
 
 extern "C" scoot_status scoot_paged_attention(scoot_ctx* ctx, const scoot_kv_layout* layout, const void* q,

@@ -35,7 +35,7 @@ struct Attn8Args {
 };
 
 // The tiles kernel (paged_attn.cu): requests of more than args.few tokens.  Its workspace, per multiprocessor.
-scoot_status scoot_attn8_tiles(scoot_ctx* ctx, const scoot_kv_layout* layout, const Attn8Args& args, bool bf16, int sms, cudaStream_t st);
+scoot_status scoot_attn8_tiles(scoot_ctx* ctx, const scoot_kv_layout* layout, const Attn8Args& args, bool bf16, int sms, cudaStream_t st, bool beside);
 size_t scoot_attn8_tile_bytes(int head_dim);
 // The map of an 8-bit cache: boxes of up to `tokens` tokens of a block and head, rows of head_dim bytes swizzled by their size.
 bool scoot_encode_codes(CUtensorMap* map, const scoot_kv_layout* layout, const void* cache, int tokens);
