@@ -8,7 +8,9 @@ configuration and reports the latencies and the throughput, which `loop.TuningLo
 
     python -m paper_2408_04323_gb300.serving
 
-The step's work is the library's: scoot_kv_tables once, then scoot_kv_append and scoot_paged_attention per layer.
+The step's work is the library's: scoot_kv_tables once, then scoot_kv_append and scoot_paged_attention per layer, or
+with rotary positions scoot_kv_append_rotary, or over a cache of 8-bit floats scoot_kv_append8 and
+scoot_paged_attention8.
 """
 from __future__ import annotations
 
@@ -24,16 +26,30 @@ class AttentionEngine:
     A sequence has a row (0 .. max_seqs - 1) for as long as it runs; a step gives every row a number of new tokens (0 for
     rows that sit out).  Lengths and tables live on the device; the host keeps the lengths and each row's blocks as
     well, by the rule that the device follows (blocks from the front of the free list, in the rows' order), and so knows
-    what is free without asking.  Everything is asynchronous on the current stream."""
+    what is free without asking.  Everything is asynchronous on the current stream.
+
+    rotation (a scoot.Rotation): keys are turned by their tokens' positions as they go into the cache, and queries, in a copy
+    of the engine's, before they meet them.  cache8: the caches hold e4m3 codes with a scale per block and head, half the
+    bytes; dtype is that of queries, keys, values and outputs either way."""
 
     def __init__(self, ctx: S.Context, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, block_size: int,
-                 n_blocks: int, max_seqs: int, max_tokens: int, max_len: int, dtype=torch.bfloat16, window: int = 0):
+                 n_blocks: int, max_seqs: int, max_tokens: int, max_len: int, dtype=torch.bfloat16, window: int = 0,
+                 rotation: S.Rotation | None = None, cache8: bool = False):
+        if rotation is not None:
+            S._rotation(rotation, ctx.device)
+            if rotation.rot_dim > head_dim:
+                raise ValueError(f"a rotation of {rotation.rot_dim} dimensions for heads of {head_dim}")
         self.ctx, self.block_size, self.n_blocks = ctx, int(block_size), int(n_blocks)
         self.max_tokens, self.max_len, self.window = int(max_tokens), int(max_len), int(window)
         self.scale = head_dim ** -0.5
         dev = torch.device("cuda", ctx.device)
         shape = (n_layers, n_blocks, block_size, n_kv_heads, head_dim)
-        self.k_cache, self.v_cache = (torch.empty(shape, dtype=dtype, device=dev) for _ in range(2))
+        self.rotation, self.cache8 = rotation, bool(cache8)
+        self.k_cache, self.v_cache = (torch.empty(shape, dtype=torch.float8_e4m3fn if cache8 else dtype, device=dev) for _ in range(2))
+        if cache8:
+            self.k_scale, self.v_scale = (torch.zeros((n_layers, n_blocks, n_kv_heads), dtype=torch.float32, device=dev) for _ in range(2))
+        if rotation is not None:  # a layer's turned queries (not in place: a step's work may be queued more than once)
+            self.turned = torch.empty((max_tokens, n_heads, head_dim), dtype=dtype, device=dev)
         width = -(-max_len // block_size)
         self.table = torch.full((max_seqs, width), -1, dtype=torch.int32, device=dev)
         # cached and new lengths, and the free blocks that the step takes: one copy from two pinned buffers in turn
@@ -69,6 +85,8 @@ class AttentionEngine:
             if x.dim() != 4 or len(x) < layers or x.shape[1] < n or x.shape[2:] != (heads, dim) or heads % kv_heads:
                 raise ValueError(f"{name} must be [{layers}][at least {n}][{heads}][{dim}], the query heads a multiple of {kv_heads}, "
                                  f"got {tuple(x.shape)}")
+        if self.rotation is not None and q.shape[-2] != self.turned.shape[1]:
+            raise ValueError(f"q has {q.shape[-2]} heads, and the engine was made for {self.turned.shape[1]}")
         need = [self.blocks_for(r, int(c)) for r, c in enumerate(new)]
         if sum(need) > len(self.free):
             raise RuntimeError(f"{sum(need)} blocks wanted, {len(self.free)} free")
@@ -87,10 +105,7 @@ class AttentionEngine:
             S.scoot_kv_tables(self.ctx, self.inputs[:rows], self.inputs[rows:2 * rows], self.table, self.block_size,
                               self.n_blocks, self.inputs[2 * rows:size], self.query_start, self.kv_len, slot, position, self.counts)
             for layer in range(len(self.k_cache)):
-                kc, vc = self.k_cache[layer], self.v_cache[layer]
-                S.scoot_kv_append(self.ctx, k[layer, :n], v[layer, :n], slot, kc, vc)
-                S.scoot_paged_attention(self.ctx, q[layer, :n], kc, vc, self.table, self.query_start, self.kv_len,
-                                        out[layer, :n], self.scale, window=self.window)
+                self._layer(layer, q[layer, :n], k[layer, :n], v[layer, :n], slot, position, out[layer, :n], int(new.max(initial=0)))
 
         launch() if run is None else run(launch)
         for r, m in enumerate(need):
@@ -98,6 +113,24 @@ class AttentionEngine:
             del self.free[:m]
         self.cached += new.astype(np.int32)
         return n
+
+    def _layer(self, layer, q, k, v, slot, position, out, max_new):
+        ctx, kc, vc = self.ctx, self.k_cache[layer], self.v_cache[layer]
+        turned = q if self.rotation is None else self.turned[:len(q)]
+        if self.cache8:
+            scales = self.k_scale[layer], self.v_scale[layer]
+            if self.rotation is None:
+                S.scoot_kv_append8(ctx, k, v, slot, kc, vc, *scales)
+            else:
+                S.scoot_kv_append8(ctx, k, v, slot, kc, vc, *scales, self.rotation, position, q, turned)
+            S.scoot_paged_attention8(ctx, turned, kc, vc, *scales, self.table, self.query_start, self.kv_len, out, self.scale,
+                                     window=self.window, max_new=max_new)
+            return
+        if self.rotation is None:
+            S.scoot_kv_append(ctx, k, v, slot, kc, vc)
+        else:
+            S.scoot_kv_append_rotary(ctx, self.rotation, k, v, slot, position, kc, vc, q, turned)
+        S.scoot_paged_attention(ctx, turned, kc, vc, self.table, self.query_start, self.kv_len, out, self.scale, window=self.window)
 
     def finish(self, row: int) -> None:
         """Gives the row's blocks back."""
@@ -110,17 +143,20 @@ class AttentionProbe:
     """Serves requests (prompt and output lengths, all there at the start) with an AttentionEngine under a configuration
     and measures the steps on the GPU: the time of its work alone, not that of the host, which plans and queues each step
     while a delay holds the GPU back.  Stands in for the engine in Algorithm 1's evaluation where only the
-    attention's share of a step is wanted, or to try the loop without an engine: queries, keys and values are random."""
+    attention's share of a step is wanted, or to try the loop without an engine: queries, keys and values are random.
+    rotation and cache8 as in AttentionEngine: cache_bytes then hold about twice the blocks."""
 
     SHORTEST_DELAY, LONGEST_DELAY = 1 << 12, 1 << 22  # iterations of the delay's kernel: some 70 us and 70 ms
 
     def __init__(self, ctx: S.Context, prompts, outputs, n_layers: int = 2, n_heads: int = 32, n_kv_heads: int = 8,
-                 head_dim: int = 128, cache_bytes: int = 1 << 30, dtype=torch.bfloat16, seed: int = 0):
+                 head_dim: int = 128, cache_bytes: int = 1 << 30, dtype=torch.bfloat16, seed: int = 0,
+                 rotation: S.Rotation | None = None, cache8: bool = False):
         self.ctx, self.prompts, self.outputs = ctx, [int(p) for p in prompts], [int(o) for o in outputs]
         if len(self.prompts) != len(self.outputs) or not self.prompts or min(self.prompts + self.outputs) < 1:
             raise ValueError("prompts and outputs must be one length each per request, all of them at least 1")
         self.shape = (n_layers, n_heads, n_kv_heads, head_dim)
         self.cache_bytes, self.dtype, self.seed = int(cache_bytes), dtype, seed
+        self.rotation, self.cache8 = rotation, bool(cache8)
         self.delay = self.SHORTEST_DELAY  # about as long as queueing a step takes
 
     def _timed(self, marks, sink):
@@ -147,18 +183,20 @@ class AttentionProbe:
         sequence or token)."""
         L, H, Hkv, D = self.shape
         longest = max(p + o for p, o in zip(self.prompts, self.outputs))
-        per_block = 2 * 2 * L * block_size * Hkv * D
+        per_block = 2 * L * Hkv * (block_size * D + 4 if self.cache8 else 2 * block_size * D)  # (4: a scale)
         n_blocks = int(self.cache_bytes * memory_utilization) // per_block
         if n_blocks < -(-longest // block_size) or (not chunked_prefill and max(self.prompts) > max_num_batched_tokens) or \
                 min(max_num_seqs, max_num_batched_tokens) < 1:
             return None
         seqs, budget = min(max_num_seqs, len(self.prompts)), max_num_batched_tokens
-        eng = AttentionEngine(self.ctx, L, H, Hkv, D, block_size, n_blocks, seqs, budget, longest, self.dtype)
+        eng = AttentionEngine(self.ctx, L, H, Hkv, D, block_size, n_blocks, seqs, budget, longest, self.dtype, rotation=self.rotation,
+                              cache8=self.cache8)
         gen = torch.Generator(device="cuda").manual_seed(self.seed)
         q = torch.randn((L, budget, H, D), generator=gen, device="cuda", dtype=torch.float32).to(self.dtype)
         k, v = (torch.randn((L, budget, Hkv, D), generator=gen, device="cuda", dtype=torch.float32).to(self.dtype) for _ in range(2))
         out = torch.empty_like(q)
-        warm = AttentionEngine(self.ctx, 1, H, Hkv, D, block_size, 1, 1, 1, 1, self.dtype)  # code and workspace are there
+        warm = AttentionEngine(self.ctx, 1, H, Hkv, D, block_size, 1, 1, 1, 1, self.dtype, rotation=self.rotation,
+                               cache8=self.cache8)  # code and workspace are there
         warm.step([1], q[:1], k[:1], v[:1], out[:1])
         waiting = list(range(len(self.prompts)))[::-1]
         row_of: list[int | None] = [None] * seqs   # the request of each row
