@@ -954,7 +954,8 @@ scoot_status scoot_kv_append_rotary(scoot_ctx* ctx, const scoot_kv_layout* layou
  * has if the block holds earlier tokens (its first new token is not its first) and that is at least s.  If theirs is
  * smaller, their codes are divided by the growth and rounded again, which changes only those that get smaller than
  * 2^-6 of the new scale, by at most 2^-10 of it.
- * The tokens of a block follow one another in the batch, in the order of their slots, as scoot_kv_tables leaves them;
+ * The tokens of a block follow one another in the batch, in the order of their slots, as scoot_kv_tables leaves them (of
+ * a block that comes up twice the scale and the codes may be of either run);
  * negative slots and those past the cache as in scoot_kv_append_rotary.  A number that is not finite is stored as zero and
  * flagged (scoot_ctx_check: SCOOT_EINVAL), so that no code is a NaN; so is a held scale that is negative or not finite, the
  * block's earlier tokens then counting as zeros.

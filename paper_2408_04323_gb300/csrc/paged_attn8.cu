@@ -5,24 +5,38 @@
 // over the keys i that token t sees; k_i, v_i are codes, s_b and s'_b their blocks' scales.
 //
 // This kernel serves requests of few rows (a row is a token's query head; single tokens above all), which bytes bound: a
-// warp is a worker of its own, with up to 16 rows against keys in tiles of 32.  Codes become fp16, which holds all of them, on
-// their way from shared memory into the operands of the tensor cores (mma.m16n8k16: the tcgen05 forms take 64 or 128 rows,
-// and their operands would have to be written back to shared memory).  Queries become fp16 as well, bf16 ones divided by a
-// power of two of their row so that the largest is below 2^15: what that rounds is below 2^-39 of the row's largest.
+// warp is a worker of its own, with 8 or 16 rows against tiles of 32 keys (64 with heads of 64).  Codes become fp16, which
+// holds all of them, on their way from shared memory into the operands of the tensor cores (mma.m16n8k16: the tcgen05 forms
+// take 64 or 128 rows, and their operands would have to be written back to shared memory).  Keys, and values by dimensions, are
+// the products' first operand, sixteen at a time, and the rows the second, eight at a time: with rows as the first a group
+// of four heads left twelve of sixteen empty.  Queries become fp16 as well, bf16 ones divided by a power of two of their row
+// so that the largest is below 2^15: what that rounds is below 2^-39 of the row's largest.
 //
 // Dimensions and keys are dealt to the operands' places as the loads want them.  Q K^T: lane (g, c) = (lane / 4, lane % 4) has
-// key g and of it 32 (16) dimensions in a row, four per step, and the same ones of its query rows.  P V: column g
-// of product t is dimension g D / 8 + t, so that a lane reads whole pieces of four keys' values, and has 32 (16) consecutive
-// dimensions of the result.
+// of sixteen keys g and g + 8, and of each D / 4 dimensions in a row, four per step, and the same ones of row g.  The result's
+// transpose (movmatrix) is P as the second operand.  P V: rows g and g + 8 of product t are dimensions g D / 8 + 2 t and
+// the next, so that a lane reads whole pieces of four keys' values, and has D / 8 consecutive dimensions of two rows' results.
 //
 // Running maximum m and sum l as elsewhere: p = 2^(c s - m), and O is rescaled only where a maximum has grown by more than 2^8.
 // The values' scales go into the probabilities: fp16 of p s'_b / r * 2^7, r the largest scale of values met so far, which
 // stays below 2^15 and rounds what is below 2^-21 of r with an error of 2^-32 r at most; O is in units of r 2^-7.
 //
-// Work: items (request, key-value head, 16 rows) in a row, each costing its tiles and a constant, are cut into equal ranges, a
-// warp each (a cut close to an item's start or end moves there).  Warps of a block take neighbouring ranges.  An item that
-// lies in several leaves its parts (O, m, l) in the workspace; at the end of a block its warps join the block's parts of
-// each item, and of an item that lies in several blocks the last block joins those, in the ranges' order.
+// Work: items (request, key-value head, rows) in a row, each costing its tiles and a constant, are cut into equal ranges for as
+// many teams as the work is worth, the same number on each multiprocessor (a cut close to an item's start or end moves
+// there).  A team is a warp, or `share` warps for the same tokens of as many heads.  A warp copies its tiles, page by page
+// by TMA and their scales beside them, into a ring of its own, ahead across items; where its next item lies is kept in
+// shared memory, out of the registers of the loop over tiles.  An item that lies in several ranges leaves its parts (O, m, l)
+// in the workspace.  Of few parts the warp that comes last joins them.  Of many, the block joins its own at its end, and the
+// last of an item's blocks joins the blocks', in the ranges' order: results do not depend on who was last.
+//
+// What bounds it, as measured per call in a captured graph, on tensors in use one after the other:
+//   * 256 sequences of 64 to 2560 tokens, 32 heads over 8 of 128, one new token each, bf16: 121 to 127 us, 5.5 to 5.8 TB/s, 81 to
+//     85% of the copy rate.  A warp takes 3000 cycles for a tile of 8 KB with eleven others beside it, which is DRAM's rate; costs
+//     and ranges (2.5 us), the first tiles, and the ends of items (queries, parts, counters) are the rest.
+//   * three sequences of 20,000 to 65,535, 28 heads over 4, fp16: 44 us, 3.3 TB/s: as much again for the first tile and the joins
+//     of parts within and across blocks (7 us) as for the keys and values.
+//   * one token over 777: 15.8 us: a chain of latencies, two thirds of it before the first product.
+//   * 128 sequences of 1500 with 4 new tokens each: 95 to 98 us, products of sixteen rows.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -37,7 +51,7 @@
 namespace {
 
 constexpr int kItemCost = 2;    // an item's start and end, in tiles,
-constexpr int kMinRange = 3;    // cost that a warp takes at least
+constexpr int kMinRange = 2;    // cost that a warp takes at least (a token over 1000 keys, 8 heads: 15.6 us, with 3 16.1)
 constexpr int kSnap = 2;        // a cut this close to the start or end of an item's tiles moves there
 constexpr int kMaxBlocks = 256;
 constexpr int kShare = 4;       // warps that take as many heads' keys of the same tokens at a time, at most
@@ -46,7 +60,11 @@ constexpr int kWarpCounts = 2 * kMaxBlocks, kBlockCounts = kWarpCounts + 12 * kM
 static_assert(kBlockCounts + kShare * kMaxBlocks <= (int)SCOOT_COUNTS, "counters");
 constexpr int kFewParts = 16;   // parts that the warp that comes last joins by itself
 constexpr int kItems = 8;       // items of a warp between its copies and their attention
-constexpr int kFewRows = 32;    // requests of up to so many rows
+// Requests of up to so many items per head are this kernel's.  Each item reads the keys again, mostly from DRAM; the tiles kernel
+// reads them once, but makes tiles for 128 rows.  128 sequences of 1500 keys, 32 heads of 128: over 8 heads of keys, items of eight
+// rows, 81 us with one, 128 with two, 222 with three and 308 with four, of sixteen rows 95 and 175, the tiles kernel 231 to 236
+// whatever the rows; over 2 heads, two items of sixteen, 63 against 67, and over one 49 against 34.
+constexpr int kFewItems = 2;
 constexpr float kMaxScale = 2.3e38f;  // times log2 e it is still finite
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
 
@@ -72,7 +90,7 @@ struct KvMaps {
 struct Item {
     int32_t r, h;          // request, key-value head
     int32_t tok, head;     // first token (of the batch), first query head
-    int32_t rows, heads;   // rows, and heads among them: row = token * heads + head
+    int32_t rows;          // row = token * group + head
     int32_t pos, kv;       // position of the first token, length of the sequence
     int32_t begin, end;    // keys that some row sees
     int32_t u0, u1;        // this part's tiles
@@ -158,10 +176,10 @@ __device__ __forceinline__ Req load_req(const Attn8Args& a, int r, bool flag) {
     return q;
 }
 
-__device__ __forceinline__ int item_count(const Attn8Args& a, int n) { return (n + a.toks - 1) / a.toks * a.per_token; }
+__device__ __forceinline__ int item_count(const Attn8Args& a, int n) { return (n + a.toks - 1) / a.toks; }
 // The keys [begin, end) that some row of item j sees.
 __device__ __forceinline__ void seen_keys(const Attn8Args& a, int kv, int n, int j, int& begin, int& end) {
-    const int tok = a.per_token > 1 ? j / a.per_token : j * a.toks, nt = min(a.toks, n - tok);
+    const int tok = j * a.toks, nt = min(a.toks, n - tok);
     const int64_t p0 = (int64_t)kv - n + tok;
     end = a.causal ? (int)min((int64_t)kv, p0 + nt) : kv;
     begin = a.window > 0 ? (int)max((int64_t)0, p0 + 1 - a.window) : 0;
@@ -189,12 +207,12 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
 }
 
 __device__ __forceinline__ uint16_t* out_row(const Attn8Args& a, const Item& it, int q) {
-    const int t = q / it.heads;
-    return a.out + (int64_t)(it.tok + t) * a.out_ld_token + (int64_t)(it.head + q - t * it.heads) * a.out_ld_head;
+    const int t = q / a.group;
+    return a.out + (int64_t)(it.tok + t) * a.out_ld_token + (int64_t)(it.head + q - t * a.group) * a.out_ld_head;
 }
 __device__ __forceinline__ float* lse_row(const Attn8Args& a, const Item& it, int q) {
-    const int t = q / it.heads;
-    return a.lse + (int64_t)(it.tok + t) * a.n_heads + it.head + q - t * it.heads;
+    const int t = q / a.group;
+    return a.lse + (int64_t)(it.tok + t) * a.n_heads + it.head + q - t * a.group;
 }
 
 // n parts of an item, of which `first` is the first: the others lie `step` floats apart from `second` on.
@@ -309,7 +327,7 @@ __device__ __forceinline__ int fetch_ids(const Attn8Args& a, const Item& it, int
 }
 
 // A range's next item with keys goes to *to; false if there is none.  reqs: the requests' lengths, or NULL where they are many.  Those without keys get their zeros here.  By a warp.
-template <int D, int kRows, int kKeys>
+template <int D, int kKeys>
 __device__ __noinline__ bool next_item(const Attn8Args& a, Cursor* cur, Item* to, const Req* reqs) {
     const int lane = threadIdx.x & 31;
     Cursor c = *cur;
@@ -338,11 +356,10 @@ __device__ __noinline__ bool next_item(const Attn8Args& a, Cursor* cur, Item* to
         Item it;
         it.r = c.r;
         it.h = c.h * a.share + c.member;
-        const int tok = a.per_token > 1 ? c.j / a.per_token : c.j * a.toks, sub = a.per_token > 1 ? c.j % a.per_token : 0;
-        it.heads = a.per_token > 1 ? min(kRows, a.group - sub * kRows) : a.group;
-        it.rows = min(a.toks, c.req.n - tok) * it.heads;
+        const int tok = c.j * a.toks;
+        it.rows = min(a.toks, c.req.n - tok) * a.group;
         it.tok = c.req.q0 + tok;
-        it.head = it.h * a.group + sub * kRows;
+        it.head = it.h * a.group;
         it.pos = c.req.kv - c.req.n + tok;
         it.kv = c.req.kv;
         seen_keys(a, c.req.kv, c.req.n, c.j, it.begin, it.end);
@@ -370,8 +387,8 @@ __device__ __noinline__ bool next_item(const Attn8Args& a, Cursor* cur, Item* to
         if (lane == 0) *to = it;
         // queries on their way to the L2 cache
         for (int e = lane; e < it.rows * (D / 64); e += 32) {
-            const int q = e / (D / 64), t = q / it.heads;
-            asm volatile("prefetch.global.L2 [%0];" ::"l"(a.q + (int64_t)(it.tok + t) * a.q_ld_token + (int64_t)(it.head + q - t * it.heads) * a.q_ld_head +
+            const int q = e / (D / 64), t = q / a.group;
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(a.q + (int64_t)(it.tok + t) * a.q_ld_token + (int64_t)(it.head + q - t * a.group) * a.q_ld_head +
                                                           e % (D / 64) * 64));
         }
         found = true;
@@ -440,13 +457,15 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
         if (lane >= d) upto += t;
     }
     const int64_t total = __shfl_sync(0xffffffffu, upto, kWarps - 1);
+    const int n_workers = gridDim.x * kWarps, n_teams = n_workers / a.share;
     // The kernel of the requests of more rows may begin on each multiprocessor that is done here (without items it begins after
     // this one, on all of them at once: taking them up one by one cost 1 % of a prefill of 619 us).
     if (total > 0) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int worker = blockIdx.x * kWarps + warp, n_workers = gridDim.x * kWarps;
-    const int team = worker / a.share, member = worker % a.share, n_teams = n_workers / a.share;
+    // As many teams as the work is worth, the same number on each multiprocessor.
     const int64_t range = max(quotient(total + n_teams - 1, n_teams), (int64_t)kMinRange);
-    const int64_t B0 = min(total, team * range), B1 = min(total, B0 + range);
+    const int teams = (int)quotient(quotient(total + range - 1, range) + gridDim.x - 1, gridDim.x);
+    const int mine_of = warp / a.share, member = warp % a.share, team = blockIdx.x * teams + mine_of;
+    const int64_t B0 = mine_of < teams ? min(total, team * range) : total, B1 = min(total, B0 + range);
 
     int cached = -1;  // requests 32 cached .. are in the lanes
     Req in_lane{0, 0, 0};
@@ -532,7 +551,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
     int first_ids = 0;                 // ids of the first 32 blocks of the last one found, in the lanes
     auto find = [&]() {
         Item* to = &queue_s[warp][n_made % kItems];
-        if (!next_item<D, kRows, kKeys>(args_s, &cursor_s[warp], to, k == 1 ? req_s : nullptr)) return;
+        if (!next_item<D, kKeys>(args_s, &cursor_s[warp], to, k == 1 ? req_s : nullptr)) return;
         ++n_made;
         first_ids = fetch_ids(a, *to, (to->u0 * kKeys >> a.bs_log) >> 5);
     };
@@ -621,7 +640,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int row = 8 * nt + 2 * c + i, pos = it.pos + row / it.heads;
+                const int row = 8 * nt + 2 * c + i, pos = it.pos + row / a.group;
                 const bool live = row < it.rows;
                 k1[nt][i] = live ? (a.causal ? min(it.kv, pos + 1) : it.kv) : 0;
                 k0[nt][i] = live && a.window > 0 ? (int)max((int64_t)0, (int64_t)pos + 1 - a.window) : 0;
@@ -630,8 +649,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                     all1 = min(all1, k1[nt][i]);
                 }
             }
-            const int row = 8 * nt + g, t = row / it.heads;
-            const uint16_t* src = a.q + (int64_t)(it.tok + t) * a.q_ld_token + (int64_t)(it.head + row - t * it.heads) * a.q_ld_head;
+            const int row = 8 * nt + g, t = row / a.group;
+            const uint16_t* src = a.q + (int64_t)(it.tok + t) * a.q_ld_token + (int64_t)(it.head + row - t * a.group) * a.q_ld_head;
 #pragma unroll
             for (int s = 0; s < kSteps; s += 2) {
                 const uint4 x = row < it.rows ? *reinterpret_cast<const uint4*>(src + (D / 4) * c + 4 * s) : make_uint4(0, 0, 0, 0);
@@ -859,7 +878,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
         // ---- the end of the item: the lane has 16 (8) dimensions in a row of rows 8 nt + 2 c and the next
         const bool whole = it.n_parts == 1;
         const bool begins = it.first == team;
-        float* part = a.parts + (size_t)(2 * worker + begins) * Sh::kPart;
+        float* part = a.parts + (size_t)(2 * (team * a.share + member) + begins) * Sh::kPart;
         if (!whole && lane == 0) {
             if (it.n_parts <= kFewParts) ends_s[warp][begins] = it;
             else many = 1;
@@ -912,6 +931,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
             __threadfence();
         }
         uint32_t done = __ballot_sync(0xffffffffu, last);
+        __syncwarp();
 #pragma unroll 1
         for (; done; done &= done - 1) {
             const Item* it = &ends_s[warp][__ffs(done) - 1];
@@ -933,7 +953,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
     // ---- split items: the block's parts of each, then the blocks'
     __syncthreads();
     if (failed || !many) return;
-    const int teams = kWarps / a.share, t0 = blockIdx.x * teams, t1 = t0 + teams - 1;
+    const int t0 = blockIdx.x * teams, t1 = t0 + teams - 1;
     float* joined = a.parts + (size_t)2 * n_workers * Sh::kPart;  // 2 kShare per block
     int rows = 0;
 #pragma unroll 1
@@ -965,7 +985,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
 #pragma unroll 1
     for (int i = 0; i < kShare + kWarps; ++i) {
         if (!last_s[i]) continue;
-        join<kBf16, D, kRows, kThreads, 1, 8>(a, items + i, 1, items[i].rows * (D / 4), tid, [&](int, float*&) {
+        join<kBf16, D, kRows, kThreads, 1, 16>(a, items + i, 1, items[i].rows * (D / 4), tid, [&](int, float*&) {
             const int b0 = items[i].first / teams, b1 = (items[i].first + items[i].n_parts - 1) / teams, who = items[i].h % a.share;
             return Parts{joined + (size_t)((2 * b0 + 1) * kShare + who) * Sh::kPart, joined + (size_t)((2 * b0 + 2) * kShare + who) * Sh::kPart,
                          2 * kShare * Sh::kPart, b1 - b0 + 1};
@@ -1033,9 +1053,10 @@ extern "C" scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_la
     a.causal = causal != 0;
     a.window = window < ld_table * layout->block_size ? window : 0;  // no sequence is longer
     a.max_new = max_new;
-    const int row_tiles = G <= 8 ? 1 : 2, item_rows = 8 * row_tiles;
-    a.toks = G <= item_rows ? item_rows / G : 1;
-    a.per_token = (G + item_rows - 1) / item_rows;
+    // Items of sixteen rows where the group needs them, or all requests may have more than eight and are this kernel's (above);
+    // else of eight, for which twelve warps have the registers and not eight: single tokens of the first of those in 77 us, not 86.
+    const int row_tiles = G > 8 || (max_new * (int64_t)G > 8 && max_new <= kFewItems * (16 / G)) ? 2 : 1, item_rows = 8 * row_tiles;
+    a.toks = std::max(1, item_rows / G);
     // Heads of the same tokens lie side by side in most caches: together they are read at 5.7 TB/s, one after the other at 4.7
     // (256 sequences, 8 heads of 128).  With fewer items than warps each is split into many parts instead, whose joins would fall
     // to the same blocks: three long sequences of 4 heads take 45 us alone, 76 together.
@@ -1067,7 +1088,7 @@ extern "C" scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_la
     a.block_count = ctx->d_count + kBlockCounts;
     a.tile_count = ctx->d_count;
     a.err = ctx->d_err;
-    a.few = kFewRows / G;
+    a.few = G <= item_rows ? kFewItems * a.toks : 0;
     // The host does not know the lengths: without max_new both kernels are launched, and one may find nothing to do.
     const bool rows = a.few > 0, tiles = max_new == 0 || max_new > a.few;
     const size_t part = (size_t)item_rows * (D + 2) * sizeof(float);

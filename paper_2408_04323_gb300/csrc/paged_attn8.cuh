@@ -8,7 +8,7 @@
 struct Attn8Args {
     int32_t bs_log, n_heads, n_kv_heads, group, n_req, causal, window, max_new;
     int32_t few;               // requests of up to so many tokens are the rows kernel's, the others the tiles kernel's
-    int32_t toks, per_token;   // rows kernel: tokens of an item, and items of a token (more than one: groups of more than 16 heads)
+    int32_t toks;              // rows kernel: tokens of an item
     int32_t share;             // rows kernel: heads that as many warps take together
     int64_t n_tokens, n_blocks;
     const int32_t* query_start;

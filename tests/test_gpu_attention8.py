@@ -127,6 +127,15 @@ def test_head_groups(S, ctx, H, Hkv, requests):
     Batch(requests, H=H, Hkv=Hkv, D=64 if H % 3 else 128, seed=H).check(S, ctx)
 
 
+@pytest.mark.parametrize("H,Hkv,most", [(2, 2, 8), (2, 2, 16), (2, 2, 17), (2, 2, 32), (2, 2, 33), (12, 4, 5), (8, 2, 4), (8, 2, 8), (8, 2, 9), (5, 1, 3),
+                                        (5, 1, 6), (7, 1, 2), (7, 1, 5), (8, 1, 2), (8, 1, 4), (9, 1, 2), (16, 1, 2), (16, 1, 3)])
+@pytest.mark.parametrize("D,dtype,window", [(128, "bf16", 0), (64, "fp16", 0), (64, "bf16", 37)])
+def test_a_few_tokens_each(S, ctx, H, Hkv, most, D, dtype, window):
+    """With the most that a request brings known: around the numbers of rows at which another kernel or form takes over."""
+    requests = [(400, most), (33, 1), (90, max(1, most - 1)), (1500, most), (most, most), (most // 2, most), (0, 0), (257, 2)]
+    Batch(requests, dtype=dtype, H=H, Hkv=Hkv, D=D, seed=most + H, extra_rows=2).check(S, ctx, window=window)
+
+
 @pytest.mark.parametrize("bs", [8, 16, 32, 64, 128, 256])
 @pytest.mark.parametrize("layout", ["nhd", "hnd"])
 @pytest.mark.parametrize("D", [64, 128])
