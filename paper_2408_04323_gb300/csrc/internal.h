@@ -33,7 +33,7 @@ struct scoot_ctx {
     uint32_t* d_err = nullptr;   // device error word, followed by the counters
     int32_t sms = 0;             // multiprocessors of the device, once scoot_sms has asked
     uint32_t smem_set = 0;       // kernels whose shared memory has been asked for: bits 0-3 and 13-16 paged_attn.cu's, 4 kv_cache.cu's tables, 5-8 kv_append8.cu's, 17-24 paged_attn8.cu's
-    uint32_t* d_count = nullptr; // SCOOT_COUNTS arrival counters, zero between calls (paged_attn.cu)
+    uint32_t* d_count = nullptr; // SCOOT_COUNTS arrival counters, zero between calls (paged_attn.cu, paged_attn8.cu)
     // Phase timing (scoot_ctx_set_timing): events recorded between the
     // launches of the last timed call, and the kind of each launch.
     int32_t timing = 0;

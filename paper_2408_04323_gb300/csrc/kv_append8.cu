@@ -7,6 +7,14 @@
 // block that held some) changes only the exponents of the older codes: they are exact still, but for those that get so
 // small that they lose fraction bits, whose error stays below half of the least step.  With any other scale every growth would
 // round all of them again.  The format's steps are relative, so that nothing is lost by not using the scale's fraction.
+//
+// A run, the batch's tokens of one block, and a head are a warp's, so that scale and codes need no atomics: a block of threads
+// takes the runs that begin among its window of tokens.  Queries are turned by blocks of their own.
+//
+// What bounds it: 32 k tokens of prompts, 32 heads of queries over 8 of 128, bf16: 140 us in a graph, 4.9 TB/s, 77% of the copy rate
+// (queries alone 88 us, keys and values alone 60): issue slots and DRAM both two thirds busy.  With numbers and codes in one
+// look through shared memory it took longer; with keys after values, and two blocks per multiprocessor, 331 us.  A token each for
+// 256 requests: 5.3 us, of decodes and chunks with heads of 64 13.3 us: the chain slot - numbers - scale - older codes - codes.
 #include <cuda_fp8.h>
 
 #include <algorithm>
