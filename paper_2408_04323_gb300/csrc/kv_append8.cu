@@ -11,10 +11,11 @@
 // A run, the batch's tokens of one block, and a head are a warp's, so that scale and codes need no atomics: a block of threads
 // takes the runs that begin among its window of tokens.  Queries are turned by blocks of their own.
 //
-// What bounds it: 32 k tokens of prompts, 32 heads of queries over 8 of 128, bf16: 140 us in a graph, 4.9 TB/s, 77% of the copy rate
-// (queries alone 88 us, keys and values alone 60): issue slots and DRAM both two thirds busy.  With numbers and codes in one
-// look through shared memory it took longer; with keys after values, and two blocks per multiprocessor, 331 us.  A token each for
-// 256 requests: 5.3 us, of decodes and chunks with heads of 64 13.3 us: the chain slot - numbers - scale - older codes - codes.
+// What bounds it: 32 k tokens of prompts, 32 heads of queries over 8 of 128, bf16: 136 us in a graph, 5.4 TB/s, 79% of the copy rate
+// (queries alone 88 us, keys and values alone 60): issue slots and DRAM both two thirds busy.  Runs staged in shared memory took
+// longer; held in registers between the two looks, with half as many blocks per multiprocessor, 189 us; values after keys 141.
+// A token each for 256 requests: 5.2 us, of decodes and chunks with heads of 64 13.2 us: the chain slot - numbers - scale - older
+// codes - codes.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -157,6 +158,12 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append8_kernel(const Append8Ar
             if (kv == 0) turn_task<kBf16>(a.rot, cs + (at + t) * (pairs / 2), j, *reinterpret_cast<const uint4*>(p + ka), *reinterpret_cast<const uint4*>(p + kb), x, x + 8);
             else turn_task<kBf16>(none, nullptr, j, *reinterpret_cast<const uint4*>(p + 16 * j), *reinterpret_cast<const uint4*>(p + 16 * j + 8), x, x + 8);
         };
+        // All of the run's lines on their way at once, without registers (prompts of 32 k tokens: 139 us without, 136 with).
+        constexpr int kLines = D * 2 / 128;
+        for (int e = lane; e < 2 * kLines * n; e += 32) {
+            const int kv = e & 1, t = (e >> 1) / kLines, i = (e >> 1) % kLines;
+            asm volatile("prefetch.global.L1 [%0];" ::"l"(src[kv] + t * a.kv_ld_token[kv] + 64 * i));
+        }
         // Twice over the run's numbers, the second time from L1: for the largest, and for the codes.
         float top[2] = {0.0f, 0.0f};
         uint32_t top16 = 0;  // of values, which nothing turns: as bits of 16, two at a time
