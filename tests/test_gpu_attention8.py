@@ -343,6 +343,46 @@ def test_another_stream_and_another_context(S, ctx):
     assert torch.equal(first[0], out) and torch.equal(first[1], lse)
 
 
+def test_calls_in_a_row_and_two_graphs_of_one_context(S, ctx):
+    """Requests of both kernels and of many parts, each call's outputs taken and overwritten right behind it, and two captured
+    graphs over the same workspace and counters replayed in turn."""
+    batches = [Batch([(900, 1)] * 40 + [(700, 300), (1500, 700)], H=8, Hkv=2, D=128, seed=31), Batch([(30000, 1), (77, 2), (9000, 40)], H=6, Hkv=2, D=64, seed=32)]
+    outs = [(torch.full_like(b.q, 3.0), torch.full(b.q.shape[:2], 3.0, device="cuda")) for b in batches]
+    index = [[_i32(b.table), _i32(b.query_start), _i32(b.kv_len)] for b in batches]
+    k16 = [torch.randn((4, 16, 2, 128), device="cuda").bfloat16() for _ in range(2)]
+    q16, o16, i16 = torch.randn((1, 8, 128), device="cuda").bfloat16(), torch.empty((1, 8, 128), device="cuda").bfloat16(), \
+        [_i32([[0, 1, 2, 3]]), _i32([0, 1]), _i32([60])]
+
+    def call(i):
+        b, (out, lse) = batches[i], outs[i]
+        S.scoot_paged_attention8(ctx, b.q, *b.cache, *b.scale, *index[i], out, b.factor, lse=lse)
+
+    for i in (0, 1, 0):   # (the workspace is there)
+        call(i)
+    want = [[t.clone() for t in o] for o in outs]
+    for o, b in zip(want, batches):
+        b.compare(*o)
+    taken = []
+    for n in range(20):
+        call(n % 2)
+        taken.append([t.clone() for t in outs[n % 2]])
+        for t in outs[n % 2]:
+            t.fill_(float("nan"))
+        S.scoot_paged_attention(ctx, q16, *k16, *i16, o16, 1.0)
+    graphs = [torch.cuda.CUDAGraph() for _ in batches]
+    for i, g in enumerate(graphs):
+        with torch.cuda.graph(g):
+            call(i)
+    for n in range(20):
+        graphs[n % 2].replay()
+        taken.append([t.clone() for t in outs[n % 2]])
+        for t in outs[n % 2]:
+            t.fill_(float("nan"))
+    ctx.check()
+    for n, got in enumerate(taken):
+        assert all(torch.equal(a, b) for a, b in zip(got, want[n % 2])), n
+
+
 def _step(S, ctx, cached, new, D, H, Hkv, bs, dtype, graphed=False, window=0):
     """Tables, append and attention of a step of an 8-bit cache with rotary positions, and what they should give."""
     rng = np.random.default_rng(len(cached))
