@@ -464,8 +464,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
     // As many teams as the work is worth, the same number on each multiprocessor.
     const int64_t range = max(quotient(total + n_teams - 1, n_teams), (int64_t)kMinRange);
     const int teams = (int)quotient(quotient(total + range - 1, range) + gridDim.x - 1, gridDim.x);
-    const int mine_of = warp / a.share, member = warp % a.share, team = blockIdx.x * teams + mine_of;
-    const int64_t B0 = mine_of < teams ? min(total, team * range) : total, B1 = min(total, B0 + range);
+    const int nth = warp / a.share, member = warp % a.share, team = blockIdx.x * teams + nth;
+    const int64_t B0 = nth < teams ? min(total, team * range) : total, B1 = min(total, B0 + range);
 
     int cached = -1;  // requests 32 cached .. are in the lanes
     Req in_lane{0, 0, 0};
