@@ -30,12 +30,12 @@
 // last of an item's blocks joins the blocks', in the ranges' order: results do not depend on who was last.
 //
 // What bounds it, as measured per call in a captured graph, on tensors in use one after the other:
-//   * 256 sequences of 64 to 2560 tokens, 32 heads over 8 of 128, one new token each, bf16: 121 to 127 us, 5.5 to 5.8 TB/s, 81 to
-//     85% of the copy rate.  A warp takes 3000 cycles for a tile of 8 KB with eleven others beside it, which is DRAM's rate; costs
+//   * 256 sequences of 64 to 2560 tokens, 32 heads over 8 of 128, one new token each, bf16: 118 to 123 us, 5.6 to 5.9 TB/s, 83
+//     to 87% of the copy rate.  A warp takes 3000 cycles for a tile of 8 KB with eleven others beside it, which is DRAM's rate; costs
 //     and ranges (2.5 us), the first tiles, and the ends of items (queries, parts, counters) are the rest.
 //   * three sequences of 20,000 to 65,535, 28 heads over 4, fp16: 44 us, 3.3 TB/s: as much again for the first tile and the joins
 //     of parts within and across blocks (7 us) as for the keys and values.
-//   * one token over 777: 15.8 us: a chain of latencies, two thirds of it before the first product.
+//   * one token over 777: 15.6 us: a chain of latencies, two thirds of it before the first product.
 //   * 128 sequences of 1500 with 4 new tokens each: 95 to 98 us, products of sixteen rows.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -50,8 +50,10 @@
 
 namespace {
 
-constexpr int kItemCost = 2;    // an item's start and end, in tiles,
-constexpr int kMinRange = 2;    // cost that a warp takes at least (a token over 1000 keys, 8 heads: 15.6 us, with 3 16.1)
+// An item's start and end, in tiles: 256 sequences to 2560 tokens take 123 to 127 us with 2, 122 to 123 with 4 to 6; one of 4000 18
+// and 15.6, 128 of 500 40 and 37, of 1500 81 and 84.
+constexpr int kItemCost = 4;
+constexpr int kMinRange = 2;    // cost that a warp takes at least (a token over 777 keys, 8 heads: 15.6 us, with 3 16.1)
 constexpr int kSnap = 2;        // a cut this close to the start or end of an item's tiles moves there
 constexpr int kMaxBlocks = 256;
 constexpr int kShare = 4;       // warps that take as many heads' keys of the same tokens at a time, at most
