@@ -702,6 +702,7 @@ __device__ __forceinline__ void no_keys(const AttnArgs& a, const Item& it) {
 
 // ---------------------------------------------------------------------------------------------- codes
 
+constexpr int kKeyFall = 22;   // powers of two by which keys' scales differ at most where they are in units of the largest
 constexpr int kUpRing = 4;     // items of a slot whose rows' exponents are at hand, likewise
 // Tiles whose scales are at hand, a place being taken again when its softmax is done: the keys of unit n are written when the
 // scores of the unit before in their place of the ring (n - 2; n - 4) are there, and those wait for the softmax of the
@@ -712,7 +713,8 @@ constexpr int kScaleRing = D == 128 ? 6 : 8;
 // A tile's scales: sixteen groups of eight keys, of keys and then of values.  Where all of either kind are the same number
 // times powers of two (zeros aside), as scoot_kv_append8 makes them, `even` is set and the codes in the tiles are in units
 // of the largest, so that softmax has one scale per tile.  Else they are in units of their groups' own.  They are multiplied by
-// 2^7 (448 is below 65504 2^-7), so that what fp16 cannot hold of them is below 2^-32 of the largest scale.
+// 2^7 (448 is below 65504 2^-7), so that what fp16 cannot hold of values is below 2^-32 of the largest scale.  Keys stay exact
+// (a score is no better than its worst key's last bit): a code's is 2^-9, times 2^7 2^-kKeyFall the least that fp16 has.
 struct TileScales {
     float k[16], v[16];
     float k_top, v_top;
@@ -830,8 +832,8 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
 #pragma unroll
                 for (int d = 8; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
                 const uint32_t bits = __float_as_uint(scale), diff = top - bits;  // of the exponents, if the fractions are the same
-                const bool even = __all_sync(0xffffffffu, bits == 0 || ((diff & 0x7FFFFFu) == 0 && bits >= 0x800000u));
                 const int d = (int)(diff >> 23);
+                const bool even = __all_sync(0xffffffffu, bits == 0 || ((diff & 0x7FFFFFu) == 0 && bits >= 0x800000u && (lane >= 16 || d <= kKeyFall)));
                 const uint32_t ratio = !even ? 22u << 10 : bits == 0 || d > 31 ? 0u : d < 22 ? (uint32_t)(22 - d) << 10 : 1u << (31 - d);  // 2^(7 - d)
                 const uint32_t rk = __shfl_sync(0xffffffffu, ratio, first >> 3), rv = __shfl_sync(0xffffffffu, ratio, 16 + (first >> 3));
                 k_times = rk | rk << 16;

@@ -1,0 +1,85 @@
+"""Attention over an 8-bit paged cache (scoot_paged_attention8) where scales lie far apart: blocks that a token does not see never
+change its result, and keys keep their codes beside others of any size."""
+import numpy as np
+import pytest
+
+import serving8_ref as R8
+from test_gpu_attention8 import F8, Batch, S, ctx  # noqa: F401
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+# (requests, heads, heads of keys, window, (request, key) in the block that some rows see and others do not): those of many rows
+# for one kernel, of few for the other
+UNSEEN = [([(440, 300), (90, 1)], 4, 2, 0, (0, 439)),        # a chunk's last block
+          ([(500, 300)], 4, 1, 100, (0, 270)),               # in a window: a block that leaves and one that enters it
+          ([(700, 600)], 2, 2, 40, (0, 115)),
+          ([(98, 4), (33, 1)], 4, 2, 0, (0, 97)),            # few rows
+          ([(996, 8)], 1, 1, 0, (0, 995)),
+          ([(300, 8), (200, 3)], 4, 4, 10, (0, 279))]
+
+
+def _seen(b, r, block, window):
+    """Which tokens of request r see a key of its block's: bool [tokens]."""
+    q0, q1, kv = int(b.query_start[r]), int(b.query_start[r + 1]), int(b.kv_len[r])
+    p = kv - (q1 - q0) + np.arange(q1 - q0)
+    first, last = block * b.bs, min(kv, (block + 1) * b.bs) - 1
+    return (p >= first) & ((p - window < last) if window else True)
+
+
+def _compare(b, out, lse, want, rows):
+    o, z, eo, ez = want
+    got, gl = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    assert np.isfinite(got[rows]).all() and np.isfinite(gl[rows]).all()
+    assert (np.abs(got - o)[rows] <= eo[rows]).all(), np.max((np.abs(got - o) / np.maximum(eo, 1e-30))[rows])
+    assert (np.abs(gl - z)[rows] <= ez[rows]).all()
+
+
+def _calls(b, S, ctx, **kw):
+    """The call without and with the most that a request brings."""
+    for most in (0, int(np.diff(b.query_start).max())):
+        out, lse = b.run(S, ctx, max_new=most, **kw)
+        ctx.check()
+        yield out, lse
+
+
+def _unseen(S, ctx, case, dtype, D, which, far):
+    requests, H, Hkv, window, (r, key) = case
+    b = Batch(requests, dtype=dtype, H=H, Hkv=Hkv, D=D, seed=D + len(requests), spread=1)
+    want = b.want(window=window)   # as the tokens that do not see the block have it, whatever its scale
+    block = key // b.bs
+    for j in which:
+        b.scale[j][int(b.table[r, block])] *= far
+    rows = np.ones(len(b.q), bool)
+    rows[int(b.query_start[r]):int(b.query_start[r + 1])] = ~_seen(b, r, block, window)
+    assert rows.any() and not rows.all()
+    for out, lse in _calls(b, S, ctx, window=window):
+        _compare(b, out, lse, want, rows)
+
+
+@pytest.mark.parametrize("case", UNSEEN)
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("fp16", 64)])
+@pytest.mark.parametrize("far", [2.0 ** 26, 2.0 ** 40, 1.3 * 2.0 ** 60])
+def test_keys_that_a_token_does_not_see_leave_no_trace(S, ctx, case, dtype, D, far):
+    _unseen(S, ctx, case, dtype, D, (0,), far)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("far", [2.0 ** 24, 2.0 ** 34, 2.0 ** 60])
+@pytest.mark.parametrize("requests,H,Hkv", [([(400, 200)], 4, 2), ([(300, 2), (90, 1)], 4, 2)])
+def test_keys_beside_much_larger_ones_keep_their_codes(S, ctx, D, far, requests, H, Hkv):
+    """A block whose keys every token sees and gives no weight: its scores are far below the others', and further with a scale `far`
+    times as large, which changes nothing but their distance."""
+    b = Batch(requests, H=H, Hkv=Hkv, D=D, seed=5, spread=1)
+    b.q = b.q.abs() + 0.5
+    for r in range(len(requests)):
+        c = b.cache[0].view(torch.uint8)[int(b.table[r, 3])]
+        c[:] = torch.full_like(c, -64.0, dtype=torch.float32).to(F8).view(torch.uint8)
+    at = [int(b.table[r, 3]) for r in range(len(requests))]
+    # scores of -64 scale sum(q) / sqrt(D): 100 or more in size, that is a weight below e^-60 beside scores within some tens
+    b.scale[0][at] = 0.25
+    want = b.want()
+    assert (want[1] > -25).all()
+    b.scale[0][at] = 0.25 * far
+    for out, lse in _calls(b, S, ctx):
+        _compare(b, out, lse, want, slice(None))
