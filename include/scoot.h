@@ -972,7 +972,7 @@ scoot_status scoot_kv_append8(scoot_ctx* ctx, const scoot_kv_layout* layout, int
  * SCOOT_BF16.  max_new: no request brings more than so many tokens (0: any number); it says which kernels have work,
  * and a request that brings more is flagged like one with bad lengths.  All else as there, but that
  *  - probabilities, times their values' scales, are rounded to fp16 for the product with the values' codes (those so small
- *    that they pass fp16's range to 2^-32 of the largest scale among the values gone by);
+ *    that they pass fp16's range to 2^-28 of the largest scale among the values that the token sees);
  *  - a scale that is negative or not finite is flagged (scoot_ctx_check: SCOOT_EINVAL) and counts as zero;
  *  - of the two codes that the format reserves for NaN, which scoot_kv_append8 never writes, a token that sees one among its
  *    keys or values gets NaN or some number there; a token that does not is not touched by it. */

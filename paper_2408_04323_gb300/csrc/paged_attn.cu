@@ -703,6 +703,7 @@ __device__ __forceinline__ void no_keys(const AttnArgs& a, const Item& it) {
 // ---------------------------------------------------------------------------------------------- codes
 
 constexpr int kKeyFall = 22;   // powers of two by which keys' scales differ at most where they are in units of the largest
+constexpr int kHiddenFall = 4; // and values' in a tile that some row does not see all of
 constexpr int kUpRing = 4;     // items of a slot whose rows' exponents are at hand, likewise
 // Tiles whose scales are at hand, a place being taken again when its softmax is done: the keys of unit n are written when the
 // scores of the unit before in their place of the ring (n - 2; n - 4) are there, and those wait for the softmax of the
@@ -713,7 +714,9 @@ constexpr int kScaleRing = D == 128 ? 6 : 8;
 // A tile's scales: sixteen groups of eight keys, of keys and then of values.  Where all of either kind are the same number
 // times powers of two (zeros aside), as scoot_kv_append8 makes them, `even` is set and the codes in the tiles are in units
 // of the largest, so that softmax has one scale per tile.  Else they are in units of their groups' own.  They are multiplied by
-// 2^7 (448 is below 65504 2^-7), so that what fp16 cannot hold of values is below 2^-32 of the largest scale.  Keys stay exact
+// 2^7 (448 is below 65504 2^-7), so that what fp16 cannot hold of values is below 2^-32 of the largest scale.  A tile that some
+// row does not see all of is even only where no value's scale is below 2^-kHiddenFall of the largest: a row of it may see the
+// smaller ones alone, whose results are then rounded by 2^-28 of their own, and not by what is hidden.  Keys stay exact
 // (a score is no better than its worst key's last bit): a code's is 2^-9, times 2^7 2^-kKeyFall the least that fp16 has.
 struct TileScales {
     float k[16], v[16];
@@ -810,9 +813,10 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
             code[i] = make_uint4(0, 0, 0, 0);
             if (there >> i & 1u) code[i] = __ldg(reinterpret_cast<const uint4*>(p + (i & 1 ? from1 : from0) + (i & ~1) * a.ld_token));
         };
-        // a tile that some row does not see all of
-        const int64_t all1 = a.causal ? min((int64_t)it.kv, (int64_t)it.pos + 1) : it.kv;
-        const int64_t all0 = a.window > 0 ? max((int64_t)0, (int64_t)it.pos + it.ntok - a.window) : 0;
+        // the tiles that every row sees all of
+        const int all1 = (a.causal ? min(it.kv, it.pos + 1) : it.kv) >> 7;
+        const int all0 = a.window > 0 ? (int)((max((int64_t)0, (int64_t)it.pos + it.ntok - a.window) + kKeys - 1) >> 7) : 0;
+        static_assert(kKeys == 1 << 7, "tiles");
         turn_to(it.u0);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) load(i, a.k8);
@@ -823,6 +827,7 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
             const int u = it.u0 + (n >> 1);
             if (at >= kNS) wait.warp(&bars[kKvEmpty + st], at / kNS - 1);
             if (!wait.all()) break;
+            const bool odd = u < all0 || u >= all1;
             if (!values) {
                 if (!(scale >= 0.0f && scale < INFINITY)) {
                     bad_scale = true;
@@ -833,7 +838,12 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
                 for (int d = 8; d > 0; d >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
                 const uint32_t bits = __float_as_uint(scale), diff = top - bits;  // of the exponents, if the fractions are the same
                 const int d = (int)(diff >> 23);
-                const bool even = __all_sync(0xffffffffu, bits == 0 || ((diff & 0x7FFFFFu) == 0 && bits >= 0x800000u && (lane >= 16 || d <= kKeyFall)));
+                bool fits = bits == 0 || ((diff & 0x7FFFFFu) == 0 && bits >= 0x800000u && (lane >= 16 || d <= kKeyFall));
+                if (odd && lane >= 16) {
+                    const int key8 = u * kKeys + 8 * (lane & 15);
+                    fits &= bits == 0 ? key8 + 8 <= it.begin || key8 >= it.end : d <= kHiddenFall;
+                }
+                const bool even = __all_sync(0xffffffffu, fits);
                 const uint32_t ratio = !even ? 22u << 10 : bits == 0 || d > 31 ? 0u : d < 22 ? (uint32_t)(22 - d) << 10 : 1u << (31 - d);  // 2^(7 - d)
                 const uint32_t rk = __shfl_sync(0xffffffffu, ratio, first >> 3), rv = __shfl_sync(0xffffffffu, ratio, 16 + (first >> 3));
                 k_times = rk | rk << 16;
@@ -845,8 +855,7 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
                     if ((lane & 15) == 0) (lane == 0 ? t.k_top : t.v_top) = __uint_as_float(top);
                 }
             }
-            const bool odd = values && ((int64_t)u * kKeys < all0 || (int64_t)u * kKeys + kKeys > all1);
-            if (odd) {
+            if (values && odd) {
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i)
                     code[i] = make_uint4(without_nan(code[i].x), without_nan(code[i].y), without_nan(code[i].z), without_nan(code[i].w));
@@ -944,18 +953,21 @@ __device__ __forceinline__ void store_zeros(uint32_t tS, int ch0) {
 // A row's scale times one of keys: not zero, so that what is masked stays -inf; finite, so that a score of zero stays zero.
 __device__ __forceinline__ float score_scale(float c, float s) { return fminf(fmaxf(c * s, 1e-37f), 3.4e38f); }
 
-// A row's state between tiles: O is in units of vref 2^-14, vref the largest of the values' scales so far.
+// Whether a row that sees columns [c0, c1) of a tile sees any of [from, to).
+__device__ __forceinline__ bool sees(int c0, int c1, int from, int to) { return max(c0, from) < min(c1, to); }
+
+// A row's state between tiles: O is in units of vref 2^-14, vref the largest of the values' scales that the row has seen so far.
 struct RowState {
     float m, l, vref;
-    // The factor of O for a tile whose largest score is mt, and whose values' largest scale vt; 1 if it stays as it is.
-    // (vt is the same for a warp, and what is returned other than 1 for one lane is a rescaling for all.)
+    // The factor of O for a tile whose largest score is mt, and whose values' largest scale, of those that the row sees, vt; 1 if it
+    // stays as it is.  (A rescaling for one lane is one for its warp.)
     __device__ __forceinline__ bool grow(float mt, float vt, bool first, bool live, float& f) {
         if (first) {
             m = mt;
             vref = fmaxf(vt, 0x1p-100f);
             return false;
         }
-        if (!__any_sync(0xffffffffu, live && mt > m + 8.0f) && !(vt > vref)) return false;
+        if (!__any_sync(0xffffffffu, (live && mt > m + 8.0f) || vt > vref)) return false;
         const float mn = fmaxf(m, mt), vn = fmaxf(vref, vt);
         f = mn == -INFINITY ? 1.0f : exp2_hw(m - mn);
         m = mn;
@@ -967,18 +979,19 @@ struct RowState {
 };
 
 // softmax_tile over scores of codes: keys' codes in units of t.k_top, values' in units of t.v_top.  P is fp16 of
-// p v_top / vref * 2^7 (below 2^15), the factor, 2^-17 at least, going into the exponent.
+// p v_top / vref * 2^7 (below 2^15), the factor, 2^-17 at least, going into the exponent.  (It is bounded for rows that see
+// nothing of the tile, whose vref may be far below, and whose p are zeros.)
 template <int NCH, typename F>
 __device__ __forceinline__ void softmax_codes(uint32_t tS, int ch0, bool full, int c0, int c1, float c, bool first, bool live, RowState& s,
                                               const TileScales& t, F&& rescale) {
     uint32_t x[NCH * 32];
     load_scores<NCH>(tS, ch0, full, c0, c1, x);
-    const float ck = score_scale(c, t.k_top), vt = t.v_top;
+    const float ck = score_scale(c, t.k_top), vt = sees(c0, c1, 32 * ch0, 32 * (ch0 + NCH)) ? t.v_top : 0.0f;
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, f;
 #pragma unroll
     for (int i = 0; i < NCH * 16; ++i) mx[i & 3] = max3(mx[i & 3], __uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
     if (s.grow(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * ck, vt, first, live, f)) rescale(f);
-    const float factor = __fdividef(vt, s.vref) * 128.0f;
+    const float factor = fminf(__fdividef(t.v_top, s.vref) * 128.0f, 128.0f);
     const float ms = __log2f(factor) - finite_or_zero(s.m);
     const float2 cc = make_float2(ck, ck), mm = make_float2(ms, ms);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -1002,7 +1015,7 @@ __device__ __forceinline__ void softmax_codes(uint32_t tS, int ch0, bool full, i
 
 // The same where the groups' scales differ by more than powers of two, or where the values' are nothing beside those gone by
 // (as an exponent's part, so small a factor would cost the scores' last places), n chunks of 32 columns from ch0 on, one at a
-// time: the row's largest score and the largest scale of values, then P and its sum.
+// time: the row's largest score and the largest scale of values that it sees, then P and its sum.
 __device__ __noinline__ float2 uneven_max(uint32_t tS, int ch0, int n, bool full, int c0, int c1, float c, const TileScales& t) {
     float mt = -INFINITY, vt = 0.0f;
     uint32_t x[32];
@@ -1015,7 +1028,7 @@ __device__ __noinline__ float2 uneven_max(uint32_t tS, int ch0, int n, bool full
 #pragma unroll
             for (int i = 0; i < 8; ++i) mx = fmaxf(mx, __uint_as_float(x[8 * g + i]));
             mt = fmaxf(mt, mx * score_scale(c, t.even ? t.k_top : t.k[4 * q + g]));
-            vt = fmaxf(vt, t.even ? t.v_top : t.v[4 * q + g]);
+            if (sees(c0, c1, 32 * q + 8 * g, 32 * q + 8 * g + 8)) vt = fmaxf(vt, t.even ? t.v_top : t.v[4 * q + g]);
         }
     }
     return make_float2(mt, vt);
@@ -1035,7 +1048,7 @@ __device__ __noinline__ float uneven_p(uint32_t tS, int ch0, int n, bool full, i
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int g = 4 * q + i / 4;
-                const float ck = score_scale(c, t.even ? t.k_top : t.k[g]), vk = (t.even ? t.v_top : t.v[g]) * inv;
+                const float ck = score_scale(c, t.even ? t.k_top : t.k[g]), vk = fminf((t.even ? t.v_top : t.v[g]) * inv, 128.0f);  // (of what is hidden)
                 const float e0 = exp2_hw(fmaf(__uint_as_float(x[2 * i]), ck, -ms)), e1 = exp2_hw(fmaf(__uint_as_float(x[2 * i + 1]), ck, -ms));
                 sum += e0 + e1;
                 p[i] = pack16<false>(e0 * vk, e1 * vk);
@@ -1592,7 +1605,7 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
                     };
                     if constexpr (k8) {
                         const TileScales& t = scale_s[n_unit % kScaleRing<D>];
-                        if (!t.even || t.v_top < state.vref * 0x1p-24f) {
+                        if (__any_sync(0xffffffffu, !t.even || t.v_top < state.vref * 0x1p-24f)) {
                             const int nch = 4 >> it.rep_log, ch0 = copy * nch;
                             const float2 most = uneven_max(tS, ch0, nch, full, k0 - t0, k1 - t0, c_row, t);
                             float f;

@@ -18,8 +18,9 @@
 // the next, so that a lane reads whole pieces of four keys' values, and has D / 8 consecutive dimensions of two rows' results.
 //
 // Running maximum m and sum l as elsewhere: p = 2^(c s - m), and O is rescaled only where a maximum has grown by more than 2^8.
-// The values' scales go into the probabilities: fp16 of p s'_b / r * 2^7, r the largest scale of values met so far, which
-// stays below 2^15 and rounds what is below 2^-21 of r with an error of 2^-32 r at most; O is in units of r 2^-7.
+// The values' scales go into the probabilities: fp16 of p s'_b / r * 2^7, r the largest scale of values that the row has seen so
+// far, which stays below 2^15 (2^15 129 / 128 where r is let be) and rounds what is below 2^-21 of r with an error of 2^-32 r at
+// most; O is in units of r 2^-7.  r is each row's own: a tile's values may be hidden from some.
 //
 // Work: items (request, key-value head, rows) in a row, each costing its tiles and a constant, are cut into equal ranges for as
 // many teams as the work is worth, the same number on each multiprocessor (a cut close to an item's start or end moves
@@ -106,6 +107,9 @@ __device__ __forceinline__ float exp2_hw(float x) {
 }
 __device__ __forceinline__ float finite_or_zero(float m) { return m == -INFINITY ? 0.0f : m; }
 __device__ __forceinline__ float inverse_sum(float l) { return l == 0.0f ? 0.0f : __fdividef(1.0f, l); }
+
+// 128 / x of a scale, infinite for zero.  (In quarters: __fdividef takes divisors up to 2^126.)
+__device__ __forceinline__ float unit_of(float x) { return __fdividef(32.0f, 0.25f * x); }
 
 __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
@@ -634,8 +638,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
         float c_row[NT][2];              // scale of a row's scores, to log2
         int k0[NT][2], k1[NT][2];        // keys that a row sees
         int all0, all1;                  // keys that all rows see
+        const bool several = it.rows > a.group;  // tokens, so that some rows see keys that others do not
         bool large;                      // a product with a scale may pass fp32
-        float o[NT][kDims][4], m[NT][2], l[NT][2], vref = 0x1p-100f, inv_ref = 0.0f;
+        float o[NT][kDims][4], m[NT][2], l[NT][2], inv_ref[NT][2];  // O in units of 1 / inv_ref
         all0 = it.begin;
         all1 = it.end;
 #pragma unroll
@@ -698,7 +703,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[nt][t][e] = 0.0f;
             m[nt][0] = m[nt][1] = -INFINITY;
-            l[nt][0] = l[nt][1] = 0.0f;
+            l[nt][0] = l[nt][1] = inv_ref[nt][0] = inv_ref[nt][1] = 0.0f;
         }
 #pragma unroll 1
         for (int u = it.u0, u1 = it.u1, u_first = it.u0; u < u1; ++u) {
@@ -773,6 +778,26 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                                 ck[mt][i][nt][e] = fminf(fmaxf(ck[mt][i][nt][e], 1e-37f), FLT_MAX);
                             }
             }
+            // the largest scale of the values that a row sees
+            float vmax = fmaxf(__uint_as_float(vs[0]), __uint_as_float(vs[1])), vt[NT][2];
+#pragma unroll
+            for (int t = 2; t < kG; t += 2) vmax = max3(vmax, __uint_as_float(vs[t]), __uint_as_float(vs[t + 1]));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) vt[nt][0] = vt[nt][1] = vmax;
+            const bool hides = partial && several;
+            if (hides) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        vt[nt][e] = 0.0f;
+#pragma unroll
+                        for (int t = 0; t < kG; ++t) {
+                            const int key = u * kKeys + 8 * t;
+                            if (max(k0[nt][e], key) < min(k1[nt][e], key + 8)) vt[nt][e] = fmaxf(vt[nt][e], __uint_as_float(vs[t]));
+                        }
+                    }
+            }
             float mx[NT][2];
             bool grown = false;
 #pragma unroll
@@ -786,39 +811,34 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                     y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 8));
                     y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, 16));
                     mx[nt][e] = y;
-                    grown |= y > m[nt][e] + 8.0f;
+                    grown |= y > m[nt][e] + 8.0f || vt[nt][e] * inv_ref[nt][e] > 129.0f;  // (128 and a rounding: nothing new)
                 }
-            float vmax = fmaxf(__uint_as_float(vs[0]), __uint_as_float(vs[1]));
-#pragma unroll
-            for (int t = 2; t < kG; t += 2) vmax = max3(vmax, __uint_as_float(vs[t]), __uint_as_float(vs[t + 1]));
             if (u == u_first) {
-                vref = fmaxf(vmax, 0x1p-100f);
-                inv_ref = 128.0f / vref;
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    m[nt][0] = mx[nt][0];
-                    m[nt][1] = mx[nt][1];
-                }
-            } else if (__any_sync(0xffffffffu, grown) || vmax > vref) {
-                const float vn = fmaxf(vref, vmax), fv = vref / vn;
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        m[nt][e] = mx[nt][e];
+                        inv_ref[nt][e] = unit_of(fmaxf(vt[nt][e], 0x1p-100f));
+                    }
+            } else if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     float f[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const float mn = fmaxf(m[nt][e], mx[nt][e]);
+                        const float mn = fmaxf(m[nt][e], mx[nt][e]), inv = fminf(inv_ref[nt][e], unit_of(vt[nt][e]));
                         f[e] = mn == -INFINITY ? 1.0f : exp2_hw(m[nt][e] - mn);
                         m[nt][e] = mn;
                         l[nt][e] *= f[e];
-                        f[e] *= fv;
+                        f[e] *= __fdividef(inv, inv_ref[nt][e]);
+                        inv_ref[nt][e] = inv;
                     }
 #pragma unroll
                     for (int t = 0; t < kDims; ++t)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[nt][t][e] *= f[e & 1];
                 }
-                vref = vn;
-                inv_ref = 128.0f / vref;
             }
             // P of sixteen keys by eight rows, turned round to be the other operand: lane (g, c) gets keys 2 c and the next of row g
             uint32_t pb[kM][NT][2];
@@ -830,12 +850,14 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                 for (int mt = 0; mt < kM; ++mt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const float f = __uint_as_float(vs[2 * mt + i]) * inv_ref;
+                        float2 f = __fmul2_rn(make_float2(__uint_as_float(vs[2 * mt + i]), __uint_as_float(vs[2 * mt + i])),
+                                              make_float2(inv_ref[nt][0], inv_ref[nt][1]));
+                        if (hides) f = make_float2(fminf(f.x, 256.0f), fminf(f.y, 256.0f));  // (hidden values: 0 times what may be infinite)
                         const float2 z = __ffma2_rn(make_float2(x[mt][nt][2 * i], x[mt][nt][2 * i + 1]),
                                                     make_float2(ck[mt][i][nt][0], ck[mt][i][nt][1]), ms);
                         const float2 e = make_float2(exp2_hw(z.x), exp2_hw(z.y));
                         sum = __fadd2_rn(sum, e);
-                        const float2 pf = __fmul2_rn(e, make_float2(f, f));
+                        const float2 pf = __fmul2_rn(e, f);
                         const uint32_t w = half2_bits(pf.x, pf.y);
                         asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(pb[mt][nt][i]) : "r"(w));
                     }
@@ -895,24 +917,24 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                 l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 16);
                 const int row = 8 * nt + 2 * c + e;
                 if (row >= it.rows) continue;
+                const float unit = __fdividef(1.0f, inv_ref[nt][e]);
                 if (whole) {
-                    const float f = inverse_sum(l[nt][e]) * 0x1p-7f;
+                    const float f = inverse_sum(l[nt][e]);
                     uint16_t* dst = out_row(a, it, row) + g * (D / 8);
 #pragma unroll
                     for (int t = 0; t < kDims; t += 4) {
                         uint32_t w[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) w[i] = pack16<kBf16>(o[nt][t + i][e] * f * vref, o[nt][t + i][2 + e] * f * vref);
+                        for (int i = 0; i < 4; ++i) w[i] = pack16<kBf16>(o[nt][t + i][e] * f * unit, o[nt][t + i][2 + e] * f * unit);
                         *reinterpret_cast<uint4*>(dst + 2 * t) = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                     if (g == 0 && a.lse) *lse_row(a, it, row) = l[nt][e] == 0.0f ? -INFINITY : (m[nt][e] + __log2f(l[nt][e])) * kLn2;
                 } else {
-                    const float f = vref * 0x1p-7f;
                     float* dst = part + row * D + g * (D / 8);
 #pragma unroll
                     for (int t = 0; t < kDims; t += 2)
                         *reinterpret_cast<float4*>(dst + 2 * t) =
-                            make_float4(o[nt][t][e] * f, o[nt][t][2 + e] * f, o[nt][t + 1][e] * f, o[nt][t + 1][2 + e] * f);
+                            make_float4(o[nt][t][e] * unit, o[nt][t][2 + e] * unit, o[nt][t + 1][e] * unit, o[nt][t + 1][2 + e] * unit);
                     if (g == 0) reinterpret_cast<float2*>(part + kRows * D)[row] = make_float2(m[nt][e], l[nt][e]);
                 }
             }

@@ -43,9 +43,10 @@ def _calls(b, S, ctx, **kw):
         yield out, lse
 
 
-def _unseen(S, ctx, case, dtype, D, which, far):
+def _unseen(S, ctx, case, dtype, D, which, far, zeros=0):
     requests, H, Hkv, window, (r, key) = case
     b = Batch(requests, dtype=dtype, H=H, Hkv=Hkv, D=D, seed=D + len(requests), spread=1)
+    b.scale[1][b.table[r, :zeros]] = 0.0
     want = b.want(window=window)   # as the tokens that do not see the block have it, whatever its scale
     block = key // b.bs
     for j in which:
@@ -62,6 +63,20 @@ def _unseen(S, ctx, case, dtype, D, which, far):
 @pytest.mark.parametrize("far", [2.0 ** 26, 2.0 ** 40, 1.3 * 2.0 ** 60])
 def test_keys_that_a_token_does_not_see_leave_no_trace(S, ctx, case, dtype, D, far):
     _unseen(S, ctx, case, dtype, D, (0,), far)
+
+
+@pytest.mark.parametrize("case", UNSEEN)
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("fp16", 64)])
+@pytest.mark.parametrize("far", [2.0 ** 3, 2.0 ** 5, 2.0 ** 12, 2.0 ** 23, 2.0 ** 40, 1.3 * 2.0 ** 60, 2.0 ** 110])
+def test_values_that_a_token_does_not_see_leave_no_trace(S, ctx, case, dtype, D, far):
+    _unseen(S, ctx, case, dtype, D, (1,), far)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("fp16", 64)])
+@pytest.mark.parametrize("case,zeros", [(UNSEEN[2], 7), (UNSEEN[4], 60), (([(300, 8)], 4, 4, 10, (0, 279)), 17)])
+def test_values_of_zero_beside_hidden_ones(S, ctx, case, dtype, D, zeros):
+    """Tokens that see zeros alone, or these before others, where a block that they do not see is large."""
+    _unseen(S, ctx, case, dtype, D, (1,), 2.0 ** 40, zeros)
 
 
 @pytest.mark.parametrize("D", [64, 128])
