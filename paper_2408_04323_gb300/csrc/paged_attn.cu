@@ -953,6 +953,9 @@ __device__ __forceinline__ void store_zeros(uint32_t tS, int ch0) {
 // A row's scale times one of keys: not zero, so that what is masked stays -inf; finite, so that a score of zero stays zero.
 __device__ __forceinline__ float score_scale(float c, float s) { return fminf(fmaxf(c * s, 1e-37f), 3.4e38f); }
 
+// a / b of scales, b at least 2^-100.  (In quarters: __fdividef takes divisors up to 2^126.)
+__device__ __forceinline__ float scale_quotient(float a, float b) { return __fdividef(0.25f * a, 0.25f * b); }
+
 // Whether a row that sees columns [c0, c1) of a tile sees any of [from, to).
 __device__ __forceinline__ bool sees(int c0, int c1, int from, int to) { return max(c0, from) < min(c1, to); }
 
@@ -991,7 +994,7 @@ __device__ __forceinline__ void softmax_codes(uint32_t tS, int ch0, bool full, i
 #pragma unroll
     for (int i = 0; i < NCH * 16; ++i) mx[i & 3] = max3(mx[i & 3], __uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
     if (s.grow(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * ck, vt, first, live, f)) rescale(f);
-    const float factor = fminf(__fdividef(t.v_top, s.vref) * 128.0f, 128.0f);
+    const float factor = fminf(scale_quotient(t.v_top, s.vref) * 128.0f, 128.0f);
     const float ms = __log2f(factor) - finite_or_zero(s.m);
     const float2 cc = make_float2(ck, ck), mm = make_float2(ms, ms);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -1034,7 +1037,7 @@ __device__ __noinline__ float2 uneven_max(uint32_t tS, int ch0, int n, bool full
     return make_float2(mt, vt);
 }
 __device__ __noinline__ float uneven_p(uint32_t tS, int ch0, int n, bool full, int c0, int c1, float c, float m, float vref, const TileScales& t) {
-    const float ms = finite_or_zero(m), inv = __fdividef(128.0f, vref);
+    const float ms = finite_or_zero(m), inv = scale_quotient(128.0f, vref);
     float sum = 0.0f;
     uint32_t x[32];
 #pragma unroll 1

@@ -1,5 +1,5 @@
 """Attention over an 8-bit paged cache (scoot_paged_attention8) where scales lie far apart: blocks that a token does not see never
-change its result, and keys keep their codes beside others of any size."""
+change its result, keys keep their codes beside others of any size, and scales reach the end of fp32."""
 import numpy as np
 import pytest
 
@@ -98,3 +98,19 @@ def test_keys_beside_much_larger_ones_keep_their_codes(S, ctx, D, far, requests,
     b.scale[0][at] = 0.25 * far
     for out, lse in _calls(b, S, ctx):
         _compare(b, out, lse, want, slice(None))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("scale", [1.5 * 2.0 ** 126, 2.0 ** 127, 2.0 ** 126])
+@pytest.mark.parametrize("requests", [[(200, 130)], [(300, 2), (90, 1)], [(150, 100), (33, 1)]])
+@pytest.mark.parametrize("even", [True, False])
+def test_values_scales_near_the_end_of_fp32(S, ctx, D, scale, requests, even):
+    """With codes of 2^-9 to 2^-7, so that sums of values stay within fp32."""
+    b = Batch(requests, dtype="bf16", H=4, Hkv=2, D=D, seed=9)
+    c = b.cache[1].view(torch.uint8)
+    c[:] = torch.where(c & 0x7F == 0x7F, c, c & 0x83)   # (the least codes, and the reserved ones where no request is)
+    s = torch.isnan(b.scale[1])
+    b.scale[1] = torch.where(s, b.scale[1], scale)
+    if not even:
+        b.scale[1][::2] *= 0.7
+    b.check(S, ctx)
