@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append8_kernel(const Append8Ar
                     s = h;
                 } else {
                     // the scale has grown: the older tokens' codes by the growth
-                    const float f = wrong ? 0.0f : h / s;
+                    const float f = h / s;
                     for (int i = sub; i < in_block; i += kTokens) {
                         uint4* p = reinterpret_cast<uint4*>(a.cache[kv] + to + (int64_t)(i - in_block) * a.ld_token + 16 * j);
                         const uint4 w = *p;
@@ -220,7 +220,8 @@ __global__ void __launch_bounds__(kThreads, 4) kv_append8_kernel(const Append8Ar
                             const float2 lo = decode2(v & 0xFFFFu), hi = decode2(v >> 16);
                             return encode2(lo.x * f, lo.y * f) | encode2(hi.x * f, hi.y * f) << 16;
                         };
-                        *p = make_uint4(again(w.x), again(w.y), again(w.z), again(w.w));
+                        // (under a scale that cannot be, zeros: what is a NaN stays one when multiplied)
+                        *p = wrong ? make_uint4(0, 0, 0, 0) : make_uint4(again(w.x), again(w.y), again(w.z), again(w.w));
                     }
                 }
             }
