@@ -394,10 +394,10 @@ struct TileLoader {
         n_page = 1 << page_log;
         box = kKeys >> page_log;
     }
-    // This lane's id of the pages of group g; kNone if no row sees any of its tokens.
+    // This lane's id of the pages of group g; kNone if no row sees any of its tokens (and for no other: negative ids are -1).
     __device__ __forceinline__ int fetch(const Item& it, int g) const {
         const int64_t key = ((int64_t)g * 32 + (threadIdx.x & 31)) * box;
-        return key < it.end && key + box > it.begin ? __ldg(a.table + (int64_t)it.r * a.ld_table + (key >> a.bs_log)) : kNone;
+        return key < it.end && key + box > it.begin ? max(__ldg(a.table + (int64_t)it.r * a.ld_table + (key >> a.bs_log)), -1) : kNone;
     }
     __device__ __forceinline__ void use(int raw) {
         const bool out = raw < 0 || raw >= a.n_blocks;
@@ -780,7 +780,7 @@ __device__ __forceinline__ void code_tiles(const AttnArgs& a, uint64_t* bars, co
         int group = -1, ids = 0, ids_next = 0;
         auto fetch = [&](int g) {
             const int64_t key = ((int64_t)g * 32 + lane) << a.bs_log;
-            return key < it.end && key + bs > it.begin ? __ldg(row + g * 32 + lane) : INT32_MIN;
+            return key < it.end && key + bs > it.begin ? max(__ldg(row + g * 32 + lane), -1) : INT32_MIN;
         };
         int64_t from0 = 0, from1 = 0;  // of the lane's first two keys
         uint32_t there = 0;            // those of its keys that are to be had, as bits

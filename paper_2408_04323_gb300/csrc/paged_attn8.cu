@@ -325,11 +325,12 @@ struct Cursor {
     Req req;                        // r's lengths
 };
 
-// The ids of 32 blocks of an item's request in the lanes; INT32_MIN for those that no row sees any of.
+// The ids of 32 blocks of an item's request in the lanes; INT32_MIN for those that no row sees any of, and for no other: negative
+// ids are -1.
 __device__ __forceinline__ int fetch_ids(const Attn8Args& a, const Item& it, int group) {
     const int block = group * 32 + (threadIdx.x & 31);
     const int64_t key = (int64_t)block << a.bs_log;
-    return key < it.end && key + (1 << a.bs_log) > it.begin ? __ldg(a.table + (int64_t)it.r * a.ld_table + block) : INT32_MIN;
+    return key < it.end && key + (1 << a.bs_log) > it.begin ? max(__ldg(a.table + (int64_t)it.r * a.ld_table + block), -1) : INT32_MIN;
 }
 
 // A range's next item with keys goes to *to; false if there is none.  reqs: the requests' lengths, or NULL where they are many.  Those without keys get their zeros here.  By a warp.
