@@ -926,7 +926,8 @@ typedef struct {
 scoot_status scoot_rotary_frequencies(int32_t rot_dim, double base, int32_t stretch, double factor, double low, double high,
                                       double original_len, double* h_frequency);
 /* Frequencies as fractions of a turn in units of 2^-64 (whole turns per position are dropped: positions are integers), for
- * scoot_rotation.turns.  With them an angle is exact modulo a turn at any position, to 2^-33 of a turn. */
+ * scoot_rotation.turns, off by less than a unit for frequencies up to 2^40.  With them an angle is exact modulo a turn at any
+ * position, to 2^-33 of a turn; the kernels use 32 bits of it, and so have sines and cosines of an angle off by at most 2^-28. */
 scoot_status scoot_rotary_turns(const double* h_frequency, int32_t n, uint64_t* h_turns);
 
 /* y = x turned by its tokens' positions (any int32), or turned back if inverse: a rotation's transpose, which takes

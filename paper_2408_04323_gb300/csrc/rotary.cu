@@ -78,9 +78,17 @@ scoot_status scoot_rotary_turns(const double* h_frequency, int32_t n, uint64_t* 
     if (n < 1 || !h_frequency || !h_turns) return SCOOT_EINVAL;
     for (int i = 0; i < n; ++i)
         if (!std::isfinite(h_frequency[i])) return SCOOT_EINVAL;
+    // 1 / 2 pi in two words (off by 2^-110): the product in two words as well, whose whole turns are dropped one by one.
+    const double inverse = 0x1.45f306dc9c883p-3, inverse_low = -0x1.6b01ec5417056p-57;
     for (int i = 0; i < n; ++i) {
-        const double turns = std::fabs(h_frequency[i]) / (2.0 * M_PI), part = turns - std::floor(turns);
-        const uint64_t t = (uint64_t)std::ldexp(part, 64);  // part < 1, so below 2^64; its last places, below 2^-64, are dropped
+        const double f = std::fabs(h_frequency[i]);
+        const double turns = std::fma(f, inverse, 0.0);  // (rounded here on every machine, and not fused into what follows)
+        double low = std::fma(f, inverse_low, std::fma(f, inverse, -turns));
+        low -= std::floor(low + 0.5);
+        const double units = std::ldexp(turns - std::floor(turns), 64), whole = std::floor(units);  // below 2^64
+        const double rest = units - whole + std::ldexp(low, 64);                                    // of either sign
+        uint64_t t = (uint64_t)whole;
+        t = rest < 0.0 ? t - (uint64_t)(0.5 - rest) : t + (uint64_t)(0.5 + rest);
         h_turns[i] = h_frequency[i] < 0.0 ? 0 - t : t;
     }
     return SCOOT_OK;

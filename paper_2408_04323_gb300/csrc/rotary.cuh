@@ -4,7 +4,8 @@
 //
 // Frequencies are kept as fractions of a turn, in units of 2^-64.  Their product with a position, modulo 2^64, is the angle
 // modulo a turn without any rounding but the frequency's own (below 2^-64 of a turn per position: 2^-33 at the farthest), in two
-// integer multiplications; only what is left of the angle within an eighth of a turn goes to a float.
+// integer multiplications; only what is left of the angle within an eighth of a turn goes to a float, in units of 2^-32 (up
+// to 2^-29 of a sine).
 //
 // What bounds it, in a graph: 2 bytes in and 2 out of an element.  32 k tokens with their keys and values into the cache (28 and 4
 // heads of 128, fp16): 96 us, 6.2 TB/s, 92% of the copy rate; gradients of as many tokens turned back: 39 us, 88%.  256 tokens: 2.8
