@@ -954,7 +954,9 @@ scoot_status scoot_kv_append_rotary(scoot_ctx* ctx, const scoot_kv_layout* layou
  * The scale of a block is the least power of two s >= 2^-100 with |x| <= 448 s for the new tokens' x, or the one that it
  * has if the block holds earlier tokens (its first new token is not its first) and that is at least s.  If theirs is
  * smaller, their codes are divided by the growth and rounded again, which changes only those that get smaller than
- * 2^-6 of the new scale, by at most 2^-10 of it.
+ * 2^-6 of the new scale, by at most 2^-10 of it.  (A held scale may be any number that the caller has put there.  By one that is
+ * no power of two the new numbers are divided in fp32, by its inverse, before they are rounded, and a growth from it rounds
+ * all older codes again.)
  * The tokens of a block follow one another in the batch, in the order of their slots, as scoot_kv_tables leaves them (of
  * a block that comes up twice the scale and the codes may be of either run);
  * negative slots and those past the cache as in scoot_kv_append_rotary.  A number that is not finite is stored as zero and

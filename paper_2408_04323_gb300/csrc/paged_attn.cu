@@ -52,8 +52,8 @@
 //     80% of the library's large product; the tensor pipe is busy in 68% of the cycles.  The rest is, as reckoned, the way
 //     scores - softmax - values of a slot (3000 cycles for 2048 of products) and the shared memory that feeds both operands
 //     of Q K^T.
-//   * a chunk of 4096 tokens over 8192 cached ones, in codes: 620 us, 1110 TFLOP/s, 59%: the tensor pipe is busy in 48% of the active
-//     cycles; the converting warps take 1700 cycles a tile and a slot's way scores - softmax - values 3450 (2048 of products).
+//   * a chunk of 4096 tokens over 8192 cached ones, in codes: 625 to 632 us, 1090 TFLOP/s, 59% (in 16 bits 452 to 460): the tensor pipe
+//     is busy in 47% of the active cycles; the converting warps take 1700 cycles a tile and a slot's way scores - softmax - values 3450 (2048 of products).
 //   * prompts in a window (heads of 64): 54 us, the tensor pipe busy in 27% and the schedulers in 40% of the active cycles:
 //     1400 cycles of softmax per tile, and starts and ends of items (about 5 us of a call: ranges, first tile, last join).
 #include <cuda.h>

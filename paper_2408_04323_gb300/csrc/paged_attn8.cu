@@ -34,9 +34,10 @@
 //   * 256 sequences of 64 to 2560 tokens, 32 heads over 8 of 128, one new token each, bf16: 118 to 123 us, 5.6 to 5.9 TB/s, 83
 //     to 87% of the copy rate.  A warp takes 3000 cycles for a tile of 8 KB with eleven others beside it, which is DRAM's rate; costs
 //     and ranges (2.5 us), the first tiles, and the ends of items (queries, parts, counters) are the rest.
-//   * three sequences of 20,000 to 65,535, 28 heads over 4, fp16: 44 us, 3.3 TB/s: as much again for the first tile and the joins
+//   * three sequences of 20,000 to 65,535, 28 heads over 4, fp16: 44 to 47 us, 3.2 TB/s: as much again for the first tile and the joins
 //     of parts within and across blocks (7 us) as for the keys and values.
-//   * one token over 777: 15.6 us: a chain of latencies, two thirds of it before the first product.
+//   * one token over 777: 15.4 to 16.1 us (over a 16-bit cache 14.0 to 14.5): a chain of latencies, two thirds of it before the first
+//     product.
 //   * 128 sequences of 1500 with 4 new tokens each: 95 to 98 us, products of sixteen rows.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -51,8 +52,8 @@
 
 namespace {
 
-// An item's start and end, in tiles: 256 sequences to 2560 tokens take 123 to 127 us with 2, 122 to 123 with 4 to 6; one of 4000 18
-// and 15.6, 128 of 500 40 and 37, of 1500 81 and 84.
+// An item's start and end, in tiles.  With 2 and with 4, in turn on one device: 256 sequences to 2560 tokens 122 us both, one of 4000
+// 18.2 and 16.4, 128 of 500 39.8 and 37.1, of 1500 79.6 and 82.6, three of 40,000 41.7 and 40.3.
 constexpr int kItemCost = 4;
 constexpr int kMinRange = 2;    // cost that a warp takes at least (a token over 777 keys, 8 heads: 15.6 us, with 3 16.1)
 constexpr int kSnap = 2;        // a cut this close to the start or end of an item's tiles moves there
@@ -64,9 +65,10 @@ static_assert(kBlockCounts + kShare * kMaxBlocks <= (int)SCOOT_COUNTS, "counters
 constexpr int kFewParts = 16;   // parts that the warp that comes last joins by itself
 constexpr int kItems = 8;       // items of a warp between its copies and their attention
 // Requests of up to so many items per head are this kernel's.  Each item reads the keys again, mostly from DRAM; the tiles kernel
-// reads them once, but makes tiles for 128 rows.  128 sequences of 1500 keys, 32 heads of 128: over 8 heads of keys, items of eight
-// rows, 81 us with one, 128 with two, 222 with three and 308 with four, of sixteen rows 95 and 175, the tiles kernel 231 to 236
-// whatever the rows; over 2 heads, two items of sixteen, 63 against 67, and over one 49 against 34.
+// reads them once, but makes tiles for 128 rows.  128 sequences of 1500 keys, 32 heads of 128, each kernel made to take them: over 8
+// heads of keys, items of eight rows, 79 us with one (a token), 140 with two, 234 with three and 293 with four, of sixteen rows
+// 95 and 180, the tiles kernel 232 to 242 whatever the rows; over 2 heads, items of sixteen, 42 and 66 against 67 and 69; 16 heads
+// over one 35 and 49 against 32 and 34.
 constexpr int kFewItems = 2;
 constexpr float kMaxScale = 2.3e38f;  // times log2 e it is still finite
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
@@ -1079,7 +1081,7 @@ extern "C" scoot_status scoot_paged_attention8(scoot_ctx* ctx, const scoot_kv_la
     a.window = window < ld_table * layout->block_size ? window : 0;  // no sequence is longer
     a.max_new = max_new;
     // Items of sixteen rows where the group needs them, or all requests may have more than eight and are this kernel's (above);
-    // else of eight, for which twelve warps have the registers and not eight: single tokens of the first of those in 77 us, not 86.
+    // else of eight, for which twelve warps have the registers and not eight: single tokens of the first of those in 82 us, not 88.
     const int row_tiles = G > 8 || (max_new * (int64_t)G > 8 && max_new <= kFewItems * (16 / G)) ? 2 : 1, item_rows = 8 * row_tiles;
     a.toks = std::max(1, item_rows / G);
     // Heads of the same tokens lie side by side in most caches: together they are read at 5.7 TB/s, one after the other at 4.7
