@@ -953,37 +953,38 @@ __device__ __forceinline__ void store_zeros(uint32_t tS, int ch0) {
 // A row's scale times one of keys: not zero, so that what is masked stays -inf; finite, so that a score of zero stays zero.
 __device__ __forceinline__ float score_scale(float c, float s) { return fminf(fmaxf(c * s, 1e-37f), 3.4e38f); }
 
-// a / b of scales, b at least 2^-100.  (In quarters: __fdividef takes divisors up to 2^126.)
-__device__ __forceinline__ float scale_quotient(float a, float b) { return __fdividef(0.25f * a, 0.25f * b); }
+// 128 / x of a scale, infinite for zero.  (In quarters: __fdividef takes divisors up to 2^126.)
+__device__ __forceinline__ float unit_of(float x) { return __fdividef(32.0f, 0.25f * x); }
 
 // Whether a row that sees columns [c0, c1) of a tile sees any of [from, to).
 __device__ __forceinline__ bool sees(int c0, int c1, int from, int to) { return max(c0, from) < min(c1, to); }
 
-// A row's state between tiles: O is in units of vref 2^-14, vref the largest of the values' scales that the row has seen so far.
+// A row's state between tiles: O is in units of 2^-7 / inv, inv 128 over the largest of the values' scales that the row has seen so
+// far.
 struct RowState {
-    float m, l, vref;
+    float m, l, inv;
     // The factor of O for a tile whose largest score is mt, and whose values' largest scale, of those that the row sees, vt; 1 if it
     // stays as it is.  (A rescaling for one lane is one for its warp.)
     __device__ __forceinline__ bool grow(float mt, float vt, bool first, bool live, float& f) {
         if (first) {
             m = mt;
-            vref = fmaxf(vt, 0x1p-100f);
+            inv = unit_of(fmaxf(vt, 0x1p-100f));
             return false;
         }
-        if (!__any_sync(0xffffffffu, (live && mt > m + 8.0f) || vt > vref)) return false;
-        const float mn = fmaxf(m, mt), vn = fmaxf(vref, vt);
+        if (!__any_sync(0xffffffffu, (live && mt > m + 8.0f) || vt * inv > 129.0f)) return false;  // (128 and a rounding: nothing new)
+        const float mn = fmaxf(m, mt), next = fminf(inv, unit_of(vt));
         f = mn == -INFINITY ? 1.0f : exp2_hw(m - mn);
         m = mn;
         l *= f;
-        f *= vref / vn;
-        vref = vn;
+        f *= __fdividef(next, inv);
+        inv = next;
         return true;
     }
 };
 
 // softmax_tile over scores of codes: keys' codes in units of t.k_top, values' in units of t.v_top.  P is fp16 of
-// p v_top / vref * 2^7 (below 2^15), the factor, 2^-17 at least, going into the exponent.  (It is bounded for rows that see
-// nothing of the tile, whose vref may be far below, and whose p are zeros.)
+// p v_top inv (up to 2^8 129), the factor, 2^-17 at least, going into the exponent.  (It is bounded for rows that see nothing of
+// the tile, whose inv may be far above, and whose p are zeros.)
 template <int NCH, typename F>
 __device__ __forceinline__ void softmax_codes(uint32_t tS, int ch0, bool full, int c0, int c1, float c, bool first, bool live, RowState& s,
                                               const TileScales& t, F&& rescale) {
@@ -994,7 +995,7 @@ __device__ __forceinline__ void softmax_codes(uint32_t tS, int ch0, bool full, i
 #pragma unroll
     for (int i = 0; i < NCH * 16; ++i) mx[i & 3] = max3(mx[i & 3], __uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
     if (s.grow(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * ck, vt, first, live, f)) rescale(f);
-    const float factor = fminf(scale_quotient(t.v_top, s.vref) * 128.0f, 128.0f);
+    const float factor = fminf(t.v_top * s.inv, 256.0f);
     const float ms = __log2f(factor) - finite_or_zero(s.m);
     const float2 cc = make_float2(ck, ck), mm = make_float2(ms, ms);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -1036,8 +1037,8 @@ __device__ __noinline__ float2 uneven_max(uint32_t tS, int ch0, int n, bool full
     }
     return make_float2(mt, vt);
 }
-__device__ __noinline__ float uneven_p(uint32_t tS, int ch0, int n, bool full, int c0, int c1, float c, float m, float vref, const TileScales& t) {
-    const float ms = finite_or_zero(m), inv = scale_quotient(128.0f, vref);
+__device__ __noinline__ float uneven_p(uint32_t tS, int ch0, int n, bool full, int c0, int c1, float c, float m, float inv, const TileScales& t) {
+    const float ms = finite_or_zero(m);
     float sum = 0.0f;
     uint32_t x[32];
 #pragma unroll 1
@@ -1051,7 +1052,7 @@ __device__ __noinline__ float uneven_p(uint32_t tS, int ch0, int n, bool full, i
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int g = 4 * q + i / 4;
-                const float ck = score_scale(c, t.even ? t.k_top : t.k[g]), vk = fminf((t.even ? t.v_top : t.v[g]) * inv, 128.0f);  // (of what is hidden)
+                const float ck = score_scale(c, t.even ? t.k_top : t.k[g]), vk = fminf((t.even ? t.v_top : t.v[g]) * inv, 256.0f);  // (of what is hidden)
                 const float e0 = exp2_hw(fmaf(__uint_as_float(x[2 * i]), ck, -ms)), e1 = exp2_hw(fmaf(__uint_as_float(x[2 * i + 1]), ck, -ms));
                 sum += e0 + e1;
                 p[i] = pack16<false>(e0 * vk, e1 * vk);
@@ -1573,7 +1574,7 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
             }
             const int all1 = a.causal ? min(it.kv, it.pos + tok0 + 1) : it.kv;
             const int all0 = a.window > 0 ? (int)max((int64_t)0, (int64_t)it.pos + tok0 + ntok - a.window) : 0;
-            RowState state{-INFINITY, 0.0f, 0x1p-100f};
+            RowState state{-INFINITY, 0.0f, 0x1p107f};
             float &m = state.m, &l = state.l;
             float c_row = a.scale_log2 * 0x1p-7f;  // with codes: scale of the row's scores, whose keys are up by 2^7
             const uint32_t step = it.slot == 2 ? 2 : 1;
@@ -1608,12 +1609,12 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
                     };
                     if constexpr (k8) {
                         const TileScales& t = scale_s[n_unit % kScaleRing<D>];
-                        if (__any_sync(0xffffffffu, !t.even || t.v_top < state.vref * 0x1p-24f)) {
+                        if (__any_sync(0xffffffffu, !t.even || t.v_top * state.inv < 0x1p-17f)) {
                             const int nch = 4 >> it.rep_log, ch0 = copy * nch;
                             const float2 most = uneven_max(tS, ch0, nch, full, k0 - t0, k1 - t0, c_row, t);
                             float f;
                             if (state.grow(most.x, most.y, u == 0, live, f)) rescale(f);
-                            state.l += uneven_p(tS, ch0, nch, full, k0 - t0, k1 - t0, c_row, state.m, state.vref, t);
+                            state.l += uneven_p(tS, ch0, nch, full, k0 - t0, k1 - t0, c_row, state.m, state.inv, t);
                         } else if (it.rep_log == 0)
                             softmax_codes<4>(tS, 0, full, k0 - t0, k1 - t0, c_row, u == 0, live, state, t, rescale);
                         else if (it.rep_log == 1)
@@ -1693,7 +1694,7 @@ __global__ void __launch_bounds__(kThreads<k8>, 1) paged_attn_kernel(const __gri
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]);
             };
-            const float unit_o = k8 ? state.vref * 0x1p-14f : 1.0f;  // (P and the values are up by 2^7 each)
+            const float unit_o = k8 ? __fdividef(0x1p-7f, state.inv) : 1.0f;  // (P and the values are up by 2^7 each)
             const int head = it.h * a.group, tok = it.tok + tok0;
             const bool whole = it.n_parts == 1;
             // parts of half 0, then those of half 1, of all CTAs

@@ -765,7 +765,26 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) ck[mt][i][nt][e] = c_row[nt][e] * __uint_as_float(ks[2 * mt + i]);
+            // the largest scale of the values that a row sees
+            float vmax = fmaxf(__uint_as_float(vs[0]), __uint_as_float(vs[1])), vt[NT][2];
+#pragma unroll
+            for (int t = 2; t < kG; t += 2) vmax = max3(vmax, __uint_as_float(vs[t]), __uint_as_float(vs[t + 1]));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) vt[nt][0] = vt[nt][1] = vmax;
             if (partial || large) {
+                if (partial && several) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            vt[nt][e] = 0.0f;
+#pragma unroll
+                            for (int t = 0; t < kG; ++t) {
+                                const int key = u * kKeys + 8 * t;
+                                if (max(k0[nt][e], key) < min(k1[nt][e], key + 8)) vt[nt][e] = fmaxf(vt[nt][e], __uint_as_float(vs[t]));
+                            }
+                        }
+                }
                 const int key0 = u * kKeys + g;
 #pragma unroll
                 for (int mt = 0; mt < kM; ++mt)
@@ -780,26 +799,6 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                                 // (not zero, so that what is masked stays -inf; finite, so that a score of zero stays zero)
                                 ck[mt][i][nt][e] = fminf(fmaxf(ck[mt][i][nt][e], 1e-37f), FLT_MAX);
                             }
-            }
-            // the largest scale of the values that a row sees
-            float vmax = fmaxf(__uint_as_float(vs[0]), __uint_as_float(vs[1])), vt[NT][2];
-#pragma unroll
-            for (int t = 2; t < kG; t += 2) vmax = max3(vmax, __uint_as_float(vs[t]), __uint_as_float(vs[t + 1]));
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) vt[nt][0] = vt[nt][1] = vmax;
-            const bool hides = partial && several;
-            if (hides) {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        vt[nt][e] = 0.0f;
-#pragma unroll
-                        for (int t = 0; t < kG; ++t) {
-                            const int key = u * kKeys + 8 * t;
-                            if (max(k0[nt][e], key) < min(k1[nt][e], key + 8)) vt[nt][e] = fmaxf(vt[nt][e], __uint_as_float(vs[t]));
-                        }
-                    }
             }
             float mx[NT][2];
             bool grown = false;
@@ -853,14 +852,13 @@ __global__ void __launch_bounds__(Shape<D, NT>::kThreads, 1) attn8_rows_kernel(c
                 for (int mt = 0; mt < kM; ++mt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        float2 f = __fmul2_rn(make_float2(__uint_as_float(vs[2 * mt + i]), __uint_as_float(vs[2 * mt + i])),
-                                              make_float2(inv_ref[nt][0], inv_ref[nt][1]));
-                        if (hides) f = make_float2(fminf(f.x, 256.0f), fminf(f.y, 256.0f));  // (hidden values: 0 times what may be infinite)
+                        const float v = __uint_as_float(vs[2 * mt + i]);
                         const float2 z = __ffma2_rn(make_float2(x[mt][nt][2 * i], x[mt][nt][2 * i + 1]),
                                                     make_float2(ck[mt][i][nt][0], ck[mt][i][nt][1]), ms);
                         const float2 e = make_float2(exp2_hw(z.x), exp2_hw(z.y));
                         sum = __fadd2_rn(sum, e);
-                        const float2 pf = __fmul2_rn(e, f);
+                        // (in this order what is hidden is zero, however large its scale over the row's)
+                        const float2 pf = __fmul2_rn(__fmul2_rn(e, make_float2(inv_ref[nt][0], inv_ref[nt][1])), make_float2(v, v));
                         const uint32_t w = half2_bits(pf.x, pf.y);
                         asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(pb[mt][nt][i]) : "r"(w));
                     }
